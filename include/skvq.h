@@ -14,7 +14,7 @@
  *   - Return value: SKVQ_OK or a negative SKVQ_ERR_* code.  On an error nothing
  *     is launched.  Conditions only the device can see (a sequence that would
  *     exceed its capacity) leave that sequence untouched and OR a bit into
- *     skvq_cache::status.
+ *     the cache's status word.
  *   - Kernels of one call, and of consecutive calls on a stream, are chained with programmatic
  *     dependent launches: a kernel may be scheduled while its predecessor on the stream drains
  *     and waits on the device before it touches that predecessor's results.  Nothing changes for
@@ -52,6 +52,10 @@ extern "C" {
                                      wait ran out); the affected tokens contribute nothing to the result */
 #define SKVQ_STATUS_BOUNDS 4       /* only from a library built with -DSKVQ_CHECKED (a debugging build): a kernel was about to
                                      use a row, slot or partial index outside its buffer; the access was skipped */
+
+#define SKVQ_STATUS_BAD_BATCH 8    /* paged calls: a sequence's lens/starts/slots entry is out of range; that sequence was skipped */
+#define SKVQ_STATUS_BAD_PAGE 16    /* paged calls: a page-table entry is not a page of the pool; its tokens were skipped */
+#define SKVQ_STATUS_BAD_POSITION 32 /* skvq_rope_apply: a position lies outside the table; that token's rows were not written */
 
 /* Rows of the quantized segment are allocated in multiples of this many tokens so
  * that a kernel may stage whole tiles; see skvq_quant_capacity(). */
@@ -252,6 +256,190 @@ int skvq_decode_step_host(const skvq_config *cfg, const skvq_cache *cache, const
 #define SKVQ_NOALLOC_SCRATCH_BYTES (8u << 20)
 int skvq_decode_attention_noalloc(const skvq_config *cfg, const skvq_cache *cache, const void *q, void *out,
                                   float sm_scale, int32_t max_len_hint, int32_t n_splits, void *cuda_stream);
+
+/* ------------------------------------------------------------------------------------------------------------------
+ * Rotary positions, and a paged 4-bit cache for serving engines: keys are rotated, reordered and quantized straight
+ * into pages that sequences share and give back; attention takes any number of queries per sequence.
+ *
+ * Notation: T rows of new tokens packed back to back, sequence b owns rows [starts[b], starts[b+1]), n_b of them;
+ * L_b = lens[b] counts the sequence's tokens INCLUDING those n_b, so the rows are its last n_b tokens and row i of
+ * them is token (and position) L_b - n_b + i.  P = page_tokens, R = ring_tokens, W = window, D = head_dim, G =
+ * group_size, ng = D/G.
+ * The calls keep no state: lengths, page table and starts are the caller's device arrays, read on the device.
+ * ------------------------------------------------------------------------------------------------------------------ */
+
+/* Element types of k, v, q and outputs. */
+#define SKVQ_F16 0
+#define SKVQ_BF16 1
+#define SKVQ_F32 2  /* skvq_rope_apply only */
+
+/* How the frequencies of a rotation are stretched for contexts longer than the model was trained on. */
+#define SKVQ_ROPE_PLAIN 0  /* f_j = base^(-2j/rot_dim) */
+#define SKVQ_ROPE_LINEAR 1 /* f_j / factor (position interpolation) */
+#define SKVQ_ROPE_NTK 2    /* base * factor^(rot_dim/(rot_dim-2)) in place of base; rot_dim > 2 */
+#define SKVQ_ROPE_YARN 3   /* f_j / factor where the pair turns fewer than `slow` times over original_positions, f_j where it
+                              turns more than `fast` times, a linear mix in the number of turns between; amplitude 0.1 ln(factor) + 1 */
+typedef struct skvq_rope_scaling {
+    int32_t kind;               /* SKVQ_ROPE_* */
+    int32_t original_positions; /* YARN: positions of the training context, >= 1 */
+    double base;                /* > 1, e.g. 10000 */
+    double factor;              /* >= 1; ignored by PLAIN */
+    double fast, slow;          /* YARN: turns, fast > slow >= 0 (e.g. 32 and 1) */
+} skvq_rope_scaling;
+
+/* Frequencies f_j (radians per position), j = 0..rot_dim/2-1, and the amplitude that multiplies cos and sin.  Host only:
+ * both outputs are host pointers.  rot_dim even, 2..256. */
+int skvq_rope_frequencies(int32_t rot_dim, const skvq_rope_scaling *scaling, double *frequencies_host, double *amplitude_host);
+
+/* The table a rotation reads: row p = {amplitude cos(p f_j), amplitude sin(p f_j)} for j = 0..n_freq-1, fp32, computed from
+ * angles reduced in 64 bits (the angle of position 10^6 needs them); p = first_position .. first_position + n_positions - 1
+ * land in rows 0 .. n_positions - 1 of `table`, so a table can be extended in place.
+ *   frequencies_host  host double [n_freq], 1 <= n_freq <= 128 (any scheme; skvq_rope_frequencies has four)
+ *   table             device float [n_positions][n_freq][2] */
+int skvq_rope_table(const double *frequencies_host, int32_t n_freq, double amplitude, int64_t first_position,
+                    int32_t n_positions, void *table, void *cuda_stream);
+
+/* A rotation (host struct): the first rot_dim channels of a head, position p by row p of the table. */
+typedef struct skvq_rope {
+    const void *table;   /* device float [n_positions][rot_dim/2][2] {cos, sin}, 16-byte aligned */
+    int32_t rot_dim;     /* even, 2..head_dim */
+    int32_t interleaved; /* 0: pair j = channels (j, j + rot_dim/2); 1: pair j = channels (2j, 2j+1) */
+    int32_t n_positions; /* rows of the table */
+} skvq_rope;
+
+/* One operand of skvq_rope_apply (host struct).  Strides are in elements, between tokens and between heads; the channels of
+ * a head are contiguous.  y may be x itself (same pointer and strides); other overlaps are not allowed. */
+typedef struct skvq_rope_tensor {
+    const void *x;
+    void *y;
+    int64_t x_token_stride, x_head_stride, y_token_stride, y_head_stride;
+    int32_t n_heads;
+} skvq_rope_tensor;
+
+/*
+ * Rotary positions of packed tokens, queries and keys in one launch:
+ *   y1 = x1 c - x2 s,  y2 = x2 c + x1 s   for every pair, {c, s} = table[positions[t]][j];
+ * fp32, each product rounded, then the sum, then once to the type; channels at or beyond rot_dim are copied.
+ * inverse = 1 rotates back (s -> -s): the gradient of the rotation with respect to x, for an amplitude of 1 also its inverse.
+ *   a, b        operands, e.g. queries and keys; b may be NULL
+ *   positions   device int32 [n_tokens]; a token whose position is outside the table is not written and sets
+ *               SKVQ_STATUS_BAD_POSITION
+ *   head_dim    1..512, rot_dim <= head_dim;  dtype SKVQ_F16, SKVQ_BF16 or SKVQ_F32
+ *   status      device int32 or NULL
+ * x and y need the alignment of their type only (16-byte alignment and strides that are multiples of 16 bytes are faster).
+ */
+int skvq_rope_apply(const skvq_rope *rope, int32_t dtype, int32_t head_dim, const skvq_rope_tensor *a,
+                    const skvq_rope_tensor *b, const int32_t *positions, int32_t n_tokens, int32_t inverse, int32_t *status,
+                    void *cuda_stream);
+
+/* Shape of a paged cache (host struct). */
+typedef struct skvq_paged_config {
+    int32_t n_q_heads;   /* Hq, a multiple of Hkv, Hq/Hkv <= 16 */
+    int32_t n_kv_heads;  /* Hkv */
+    int32_t head_dim;    /* D: 64 or 128 */
+    int32_t group_size;  /* G: 32, 64 or 128, <= D */
+    int32_t window;      /* W >= 0 newest tokens of a sequence are attended unquantized */
+    int32_t ring_tokens; /* R >= W rows per slot of the ring; R - W tokens can be taken back (lens lowered) without
+                            touching what the window then needs */
+    int32_t page_tokens; /* P: 16, 32, 64, 128 or 256 tokens per page */
+    int32_t n_pages;     /* pages of the pool */
+    int32_t n_slots;     /* slots of the ring (sequences that can be live at once) */
+    int32_t dtype;       /* SKVQ_F16 or SKVQ_BF16: k, v, q, out and the ring */
+} skvq_paged_config;
+
+/*
+ * The pool (host struct of device pointers), row-major:
+ *   k_codes/v_codes  uint8  [n_pages][Hkv][P][D/2]    code j of a row in bits [4j, 4j+4) of its little-endian bit stream,
+ *                                                     j counted in reordered order (the 4-bit rows of skvq_cache)
+ *   k_meta/v_meta    half2  [n_pages][Hkv][P][ng]     {scale h, zero z}; value h*code + z
+ *   k_win/v_win      dtype  [n_slots][Hkv][R][D]      ring; token t in row t % R, reordered order; may be NULL when W == 0
+ *   reorder_k/_v     int32  [Hkv][D]                  stored[j] = source[idx[j]], rows are permutations; NULL = identity
+ *   alpha_k/_v       float  [Hkv][ng]                 clip factors; NULL = 1
+ *   status           int32  [1] or NULL               SKVQ_STATUS_* bits are OR-ed in
+ * EVERY token is quantized into its page when it is appended, and the newest are kept in the ring as well: a page is
+ * complete at any time (it can be shared, moved or kept for another request with the same prefix).
+ */
+typedef struct skvq_paged_cache {
+    void *k_codes, *v_codes;
+    void *k_meta, *v_meta;
+    void *k_win, *v_win;
+    const int32_t *reorder_k, *reorder_v;
+    const float *alpha_k, *alpha_v;
+    int32_t *status;
+} skvq_paged_cache;
+
+/* The sequences of one step (host struct of device pointers and host bounds). */
+typedef struct skvq_paged_batch {
+    const int32_t *page_table; /* [n_seqs][max_pages]: token t of sequence b lives in page page_table[b][t / P] */
+    const int32_t *lens;       /* [n_seqs] */
+    const int32_t *starts;     /* [n_seqs + 1], non-decreasing; rows at or beyond starts[n_seqs] are left alone */
+    const int32_t *slots;      /* [n_seqs] ring slot of every sequence, or NULL: sequence b uses slot b */
+    int32_t n_seqs;            /* 1..2048 */
+    int32_t max_pages;         /* row length of page_table */
+    int32_t n_tokens;          /* T: rows that k, v, q and outputs have */
+    int32_t max_new;           /* host upper bound on n_b; max_new * Hq/Hkv <= 2^30 */
+    int32_t max_len;           /* host upper bound on lens[], <= max_pages * P */
+} skvq_paged_batch;
+
+/* Validate a paged configuration (host only). */
+int skvq_check_paged_config(const skvq_paged_config *cfg);
+
+/* Bytes of k_codes, v_codes, k_meta, v_meta, k_win, v_win (in that order) for cfg.  Host only. */
+int skvq_paged_cache_sizes(const skvq_paged_config *cfg, size_t bytes_out[6]);
+
+/*
+ * Append the new tokens of every sequence: rotate the keys (rope != NULL; token t by row t of the table; the rotated key is
+ * rounded to dtype), reorder, quantize each group, write the rows to their pages, and the last min(n_b, R) of them to the ring
+ * as well.  The quantizer is that of skvq_quantize_append at 4 bits with fp16 parameters, but for the step's quotient:
+ *   lo = alpha*min, hi = alpha*max, h = fp16((hi-lo) * fp32(1/15)), z = fp16(lo), code = clamp(rint((x - z)/h), 0, 15)
+ * (the product with 1/15 is within one fp32 step of the quotient by 15; h == 0 -> code 0).
+ *   k, v             dtype [T][Hkv][D]; k_stride/v_stride: elements between tokens (a multiple of 8, >= Hkv*D)
+ * A sequence is skipped and SKVQ_STATUS_BAD_BATCH set when its starts are not 0 <= starts[b] <= starts[b+1] <= T, n_b exceeds
+ * max_new or L_b, L_b exceeds max_len or the table's rows, or its slot is not in [0, n_slots); a token whose page-table entry is
+ * not in [0, n_pages) is skipped and sets SKVQ_STATUS_BAD_PAGE.  Two tokens of one call must not share a page row, two sequences
+ * with new tokens no slot.  Magnitudes beyond the fp16 range (and NaN) give unspecified rows: the parameters are fp16.
+ * Repeating a call with the same arguments gives the same cache.
+ */
+int skvq_paged_append(const skvq_paged_config *cfg, const skvq_paged_cache *cache, const skvq_paged_batch *batch,
+                      const skvq_rope *rope, const void *k, const void *v, int64_t k_stride, int64_t v_stride, void *cuda_stream);
+
+/*
+ * The last n_b tokens of every sequence as values, channels back in source order: h*code + z in fp32, rounded to dtype; with
+ * window = 1 the newest W tokens of a sequence come from the ring instead (what attention sees).  Keys come out rotated, as
+ * they are held.  Rows of skipped sequences and tokens (see skvq_paged_append) are left alone.
+ *   k, v             dtype [T][Hkv][D], token strides as for skvq_paged_append; either may be NULL
+ */
+int skvq_paged_read(const skvq_paged_config *cfg, const skvq_paged_cache *cache, const skvq_paged_batch *batch, int32_t window,
+                    void *k, void *v, int64_t k_stride, int64_t v_stride, void *cuda_stream);
+
+/* Options of one paged attention call (host struct). */
+typedef struct skvq_paged_attn_args {
+    float sm_scale;       /* softmax scale, e.g. 1/sqrt(D) */
+    int32_t causal;       /* 1: row i of a sequence sees tokens 0 .. L_b - n_b + i; 0: all L_b tokens */
+    int32_t n_splits;     /* 0: the library chooses; n > 0: about n pieces of the context per (sequence, KV head) */
+    void *workspace;      /* device scratch of at least skvq_paged_workspace_size() bytes; may be NULL when that is 0 */
+    size_t workspace_bytes;
+} skvq_paged_attn_args;
+
+/* Scratch bytes that skvq_paged_attention needs (depends on the host bounds in `batch`, not on the device arrays, and on the
+ * GPU's SM count).  0 also on bad arguments.  Host only. */
+size_t skvq_paged_workspace_size(const skvq_paged_config *cfg, const skvq_paged_batch *batch, int32_t n_splits);
+
+/*
+ * Attention of the new tokens' queries over the cache (append first: the cache then holds them):
+ *   q' = rope(q) rounded to dtype (rope != NULL),  s_t = sm_scale sum_j q'_j K~[t][j],  p = softmax over the tokens the row sees,
+ *   out_j = sum_t p_t V~[t][j]
+ * K~, V~ as skvq_paged_read(window = 1) defines them, unrounded.  Scores, softmax statistics and sums are fp32.
+ * A row that sees no token (n_b > L_b, or L_b = 0) gives zeros and a log-sum-exp of -infinity.
+ *   q, out           dtype [T][Hq][D], token strides in elements (multiples of 8, >= Hq*D)
+ *   lse              float [T][Hq], natural logarithm of the softmax denominator of every row, or NULL
+ * Skipped sequences (as for skvq_paged_append, except that n_b may exceed L_b): their rows are left alone.  Tokens behind a bad
+ * page-table entry are left out of the softmax and SKVQ_STATUS_BAD_PAGE is set.  Rows of the cache at or beyond L_b are never
+ * used, whatever they hold.  The workspace is overwritten; calls sharing one must be stream-ordered.
+ */
+int skvq_paged_attention(const skvq_paged_config *cfg, const skvq_paged_cache *cache, const skvq_paged_batch *batch,
+                         const skvq_rope *rope, const void *q, int64_t q_stride, void *out, int64_t out_stride, void *lse,
+                         const skvq_paged_attn_args *args, void *cuda_stream);
 
 #ifdef __cplusplus
 }

@@ -6,6 +6,7 @@ on first use; if it has not been built the call raises -- there is no fallback.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 
@@ -22,13 +23,20 @@ SKVQ_NOALLOC_SCRATCH_BYTES = 8 << 20
 SKVQ_STATUS_OVERFLOW = 1
 SKVQ_STATUS_COPY_TIMEOUT = 2
 SKVQ_STATUS_BOUNDS = 4
+SKVQ_STATUS_BAD_BATCH = 8
+SKVQ_STATUS_BAD_PAGE = 16
+SKVQ_STATUS_BAD_POSITION = 32
 SKVQ_TOKEN_ALIGN = 64
 SKVQ_GROUP_GRANULE = 32
 SKVQ_BITS_TERNARY = 15
+SKVQ_F16, SKVQ_BF16, SKVQ_F32 = 0, 1, 2
+SKVQ_ROPE_PLAIN, SKVQ_ROPE_LINEAR, SKVQ_ROPE_NTK, SKVQ_ROPE_YARN = 0, 1, 2, 3
 
 EXPORTS = ["skvq_version", "skvq_strerror", "skvq_launch_count", "skvq_check_config", "skvq_quant_capacity",
            "skvq_cache_sizes", "skvq_sink_bytes", "skvq_quantize_append", "skvq_workspace_size", "skvq_decode_attention",
-           "skvq_step_staging_size", "skvq_decode_step_host", "skvq_decode_attention_noalloc", "skvq_check_group_bounds"]
+           "skvq_step_staging_size", "skvq_decode_step_host", "skvq_decode_attention_noalloc", "skvq_check_group_bounds",
+           "skvq_rope_frequencies", "skvq_rope_table", "skvq_rope_apply", "skvq_check_paged_config", "skvq_paged_cache_sizes",
+           "skvq_paged_append", "skvq_paged_read", "skvq_paged_workspace_size", "skvq_paged_attention"]
 
 
 class SkvqConfig(ctypes.Structure):
@@ -46,6 +54,41 @@ class SkvqAttnArgs(ctypes.Structure):
     _fields_ = [("sm_scale", ctypes.c_float), ("max_len_hint", ctypes.c_int32), ("n_splits", ctypes.c_int32),
                 ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t),
                 ("ev_begin", ctypes.c_void_p), ("ev_end", ctypes.c_void_p)]
+
+
+class SkvqRopeScaling(ctypes.Structure):
+    _fields_ = [("kind", ctypes.c_int32), ("original_positions", ctypes.c_int32)] + \
+        [(n, ctypes.c_double) for n in ("base", "factor", "fast", "slow")]
+
+
+class SkvqRope(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p)] + [(n, ctypes.c_int32) for n in ("rot_dim", "interleaved", "n_positions")]
+
+
+class SkvqRopeTensor(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("y", ctypes.c_void_p)] + \
+        [(n, ctypes.c_int64) for n in ("x_token_stride", "x_head_stride", "y_token_stride", "y_head_stride")] + \
+        [("n_heads", ctypes.c_int32)]
+
+
+class SkvqPagedConfig(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_q_heads", "n_kv_heads", "head_dim", "group_size", "window", "ring_tokens",
+                                              "page_tokens", "n_pages", "n_slots", "dtype")]
+
+
+class SkvqPagedCacheStruct(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k_codes", "v_codes", "k_meta", "v_meta", "k_win", "v_win", "reorder_k",
+                                               "reorder_v", "alpha_k", "alpha_v", "status")]
+
+
+class SkvqPagedBatch(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("page_table", "lens", "starts", "slots")] + \
+        [(n, ctypes.c_int32) for n in ("n_seqs", "max_pages", "n_tokens", "max_new", "max_len")]
+
+
+class SkvqPagedAttnArgs(ctypes.Structure):
+    _fields_ = [("sm_scale", ctypes.c_float), ("causal", ctypes.c_int32), ("n_splits", ctypes.c_int32),
+                ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t)]
 
 
 class SkvqError(RuntimeError):
@@ -98,6 +141,26 @@ def lib() -> ctypes.CDLL:
         L.skvq_decode_attention_noalloc.restype = c_int
         L.skvq_decode_attention_noalloc.argtypes = [P(SkvqConfig), P(SkvqCacheStruct), vp, vp, ctypes.c_float,
                                                     ctypes.c_int32, ctypes.c_int32, vp]
+        i32, i64, f64 = ctypes.c_int32, ctypes.c_int64, ctypes.c_double
+        paged = [P(SkvqPagedConfig), P(SkvqPagedCacheStruct), P(SkvqPagedBatch)]
+        L.skvq_rope_frequencies.restype = c_int
+        L.skvq_rope_frequencies.argtypes = [i32, P(SkvqRopeScaling), P(f64), P(f64)]
+        L.skvq_rope_table.restype = c_int
+        L.skvq_rope_table.argtypes = [P(f64), i32, f64, i64, i32, vp, vp]
+        L.skvq_rope_apply.restype = c_int
+        L.skvq_rope_apply.argtypes = [P(SkvqRope), i32, i32, P(SkvqRopeTensor), P(SkvqRopeTensor), vp, i32, i32, vp, vp]
+        L.skvq_check_paged_config.restype = c_int
+        L.skvq_check_paged_config.argtypes = [P(SkvqPagedConfig)]
+        L.skvq_paged_cache_sizes.restype = c_int
+        L.skvq_paged_cache_sizes.argtypes = [P(SkvqPagedConfig), P(c_sz)]
+        L.skvq_paged_append.restype = c_int
+        L.skvq_paged_append.argtypes = [*paged, P(SkvqRope), vp, vp, i64, i64, vp]
+        L.skvq_paged_read.restype = c_int
+        L.skvq_paged_read.argtypes = [*paged, i32, vp, vp, i64, i64, vp]
+        L.skvq_paged_workspace_size.restype = c_sz
+        L.skvq_paged_workspace_size.argtypes = [P(SkvqPagedConfig), P(SkvqPagedBatch), i32]
+        L.skvq_paged_attention.restype = c_int
+        L.skvq_paged_attention.argtypes = [*paged, P(SkvqRope), vp, i64, vp, i64, vp, P(SkvqPagedAttnArgs), vp]
         _lib = L
     return _lib
 
@@ -182,6 +245,56 @@ def skvq_decode_attention_noalloc(cfg, cache, q, out, sm_scale, max_len_hint, n_
     _check(lib().skvq_decode_attention_noalloc(ctypes.byref(cfg), ctypes.byref(cache), _dptr(q), _dptr(out),
                                                float(sm_scale), int(max_len_hint), int(n_splits), _stream(stream)),
            "skvq_decode_attention_noalloc")
+
+
+def skvq_rope_frequencies(rot_dim: int, scaling: SkvqRopeScaling) -> tuple[list[float], float]:
+    """Frequencies (radians per position) of the rot_dim/2 pairs and the amplitude of cos and sin."""
+    f, amplitude = (ctypes.c_double * max(rot_dim // 2, 1))(), ctypes.c_double()
+    _check(lib().skvq_rope_frequencies(rot_dim, ctypes.byref(scaling), f, ctypes.byref(amplitude)), "skvq_rope_frequencies")
+    return list(f), amplitude.value
+
+
+def skvq_rope_table(frequencies, amplitude: float, first_position: int, n_positions: int, table, stream=None) -> None:
+    f = (ctypes.c_double * len(frequencies))(*frequencies)
+    _check(lib().skvq_rope_table(f, len(frequencies), amplitude, first_position, n_positions, _dptr(table), _stream(stream)),
+           "skvq_rope_table")
+
+
+def skvq_rope_apply(rope: SkvqRope, dtype: int, head_dim: int, a: SkvqRopeTensor, b, positions, n_tokens: int,
+                    inverse: int = 0, status=None, stream=None) -> None:
+    _check(lib().skvq_rope_apply(ctypes.byref(rope), dtype, head_dim, ctypes.byref(a), None if b is None else ctypes.byref(b),
+                                 _dptr(positions), n_tokens, inverse, _dptr(status), _stream(stream)), "skvq_rope_apply")
+
+
+def skvq_check_paged_config(cfg: SkvqPagedConfig) -> int:
+    return lib().skvq_check_paged_config(ctypes.byref(cfg))
+
+
+def skvq_paged_cache_sizes(cfg: SkvqPagedConfig) -> list[int]:
+    out = (ctypes.c_size_t * 6)()
+    _check(lib().skvq_paged_cache_sizes(ctypes.byref(cfg), out), "skvq_paged_cache_sizes")
+    return list(out)
+
+
+def skvq_paged_append(cfg, cache, batch, rope, k, v, k_stride: int, v_stride: int, stream=None) -> None:
+    _check(lib().skvq_paged_append(ctypes.byref(cfg), ctypes.byref(cache), ctypes.byref(batch),
+                                   None if rope is None else ctypes.byref(rope), _dptr(k), _dptr(v), k_stride, v_stride,
+                                   _stream(stream)), "skvq_paged_append")
+
+
+def skvq_paged_read(cfg, cache, batch, window: int, k, v, k_stride: int, v_stride: int, stream=None) -> None:
+    _check(lib().skvq_paged_read(ctypes.byref(cfg), ctypes.byref(cache), ctypes.byref(batch), window, _dptr(k), _dptr(v),
+                                 k_stride, v_stride, _stream(stream)), "skvq_paged_read")
+
+
+def skvq_paged_workspace_size(cfg, batch, n_splits: int = 0) -> int:
+    return int(lib().skvq_paged_workspace_size(ctypes.byref(cfg), ctypes.byref(batch), n_splits))
+
+
+def skvq_paged_attention(cfg, cache, batch, rope, q, q_stride: int, out, out_stride: int, lse, args, stream=None) -> None:
+    _check(lib().skvq_paged_attention(ctypes.byref(cfg), ctypes.byref(cache), ctypes.byref(batch),
+                                      None if rope is None else ctypes.byref(rope), _dptr(q), q_stride, _dptr(out), out_stride,
+                                      _dptr(lse), ctypes.byref(args), _stream(stream)), "skvq_paged_attention")
 
 
 # ---------------------------------------------------------------- device-memory holder
@@ -274,4 +387,144 @@ class SkvqCache:
         if out is None:
             out = torch.empty_like(q)
         skvq_decode_attention(self.cfg, self.struct, q, out, self.attn_args(sm_scale, max_len_hint, n_splits), stream)
+        return out
+
+
+# ---------------------------------------------------------------- rotary positions and the paged cache
+_DTYPES = {torch.float16: SKVQ_F16, torch.bfloat16: SKVQ_BF16, torch.float32: SKVQ_F32}
+
+
+_HERE = contextlib.nullcontext()
+
+
+def _on(device: torch.device):
+    """The calls launch on the current device: make it the tensors' own."""
+    return _HERE if torch.cuda.current_device() == device.index else torch.cuda.device(device)
+
+
+class RopeTable:
+    """A rotation: its cos/sin table (fp32 [positions, rot_dim/2, 2] on the GPU) and the pairing of channels."""
+
+    def __init__(self, table, rot_dim: int, interleaved: bool = False):
+        assert table.is_cuda and table.dtype == torch.float32 and table.is_contiguous()
+        assert table.dim() == 3 and tuple(table.shape[1:]) == (rot_dim // 2, 2), "table: [positions, rot_dim/2, 2]"
+        self.table, self.rot_dim, self.interleaved, self.device = table, rot_dim, bool(interleaved), table.device
+        self.struct = SkvqRope(table.data_ptr(), rot_dim, 1 if interleaved else 0, table.shape[0])
+
+    @classmethod
+    def build(cls, rot_dim: int, n_positions: int, interleaved: bool = False, base: float = 10000.0,
+              kind: int = SKVQ_ROPE_PLAIN, factor: float = 1.0, original_positions: int = 0, fast: float = 32.0,
+              slow: float = 1.0, device="cuda:0"):
+        """The table of positions 0..n_positions-1 for one of the SKVQ_ROPE_* scalings."""
+        f, amplitude = skvq_rope_frequencies(rot_dim, SkvqRopeScaling(kind, original_positions, base, factor, fast, slow))
+        table = torch.empty((n_positions, rot_dim // 2, 2), dtype=torch.float32, device=device)
+        with _on(table.device):
+            skvq_rope_table(f, amplitude, 0, n_positions, table)
+        return cls(table, rot_dim, interleaved)
+
+    def apply(self, positions, q, q_out=None, k=None, k_out=None, inverse: bool = False, status=None, stream=None) -> None:
+        """Rotate q [T, heads, D] and, in the same launch, k: into q_out/k_out, in place without them.  positions: int32 [T]."""
+        q_out, k_out = (q if q_out is None else q_out), (k if k_out is None else k_out)
+        T, _, D = q.shape
+        assert positions.dtype == torch.int32 and positions.is_contiguous() and positions.numel() == T
+        ops = []
+        for x, y in ((q, q_out), (k, k_out)):
+            if x is None:
+                ops.append(None)
+                continue
+            assert x.device == y.device == positions.device == self.device and x.dtype == y.dtype == q.dtype
+            assert x.shape == y.shape and x.shape[0] == T and x.shape[2] == D and (D == 1 or (x.stride(2) == 1 and y.stride(2) == 1))
+            ops.append(SkvqRopeTensor(x.data_ptr(), y.data_ptr(), x.stride(0), x.stride(1), y.stride(0), y.stride(1), x.shape[1]))
+        with _on(self.device):
+            skvq_rope_apply(self.struct, _DTYPES[q.dtype], D, ops[0], ops[1], positions, T, 1 if inverse else 0, status, stream)
+
+
+class SkvqPagedCache:
+    """The pool of a paged 4-bit cache (torch tensors as device memory) and the C structs.
+
+    dtype: torch.float16 or torch.bfloat16; reorder_k/_v: int32 [Hkv, D] or None; alpha_k/_v: float32 [Hkv, D/G] or None;
+    ring_tokens: rows per ring slot (default: window); buffers: an engine's own tensors for any of k_codes, v_codes, k_meta,
+    v_meta, k_win, v_win instead of new ones."""
+
+    def __init__(self, n_q_heads, n_kv_heads, head_dim, group_size, window, page_tokens, n_pages, n_slots, dtype=torch.float16,
+                 reorder_k=None, reorder_v=None, alpha_k=None, alpha_v=None, ring_tokens=None, buffers=None, device="cuda:0"):
+        self.cfg = SkvqPagedConfig(n_q_heads, n_kv_heads, head_dim, group_size, window, window if ring_tokens is None else ring_tokens,
+                                   page_tokens, n_pages, n_slots, _DTYPES[dtype])
+        _check(skvq_check_paged_config(self.cfg), "skvq_check_paged_config")
+        self.dtype = dtype
+        H, D, ng, R = n_kv_heads, head_dim, head_dim // group_size, self.cfg.ring_tokens if window else 0
+        shapes = {"k_codes": (n_pages, H, page_tokens, D // 2), "k_meta": (n_pages, H, page_tokens, ng, 2), "k_win": (n_slots, H, R, D)}
+        kinds = {"codes": torch.uint8, "meta": torch.float16, "win": dtype}
+        given = dict(buffers or {})
+        self.device = next(iter(given.values())).device if given else torch.empty(0, device=device).device      # with its index
+        for name in ("k_codes", "v_codes", "k_meta", "v_meta", "k_win", "v_win"):
+            shape, kind = shapes["k" + name[1:]], kinds[name[2:]]
+            t = given.pop(name, None)
+            if t is None:
+                t = torch.zeros(shape, dtype=kind, device=self.device)
+            assert t.is_cuda and t.device == self.device and t.dtype == kind and tuple(t.shape) == shape and t.is_contiguous(), name
+            setattr(self, name, t)
+        assert not given, f"unknown buffers {sorted(given)}"
+        assert [t.numel() * t.element_size() for t in (self.k_codes, self.v_codes, self.k_meta, self.v_meta, self.k_win, self.v_win)] == \
+            skvq_paged_cache_sizes(self.cfg)
+        self.status = torch.zeros((4,), dtype=torch.int32, device=self.device)
+
+        def small(x, kind, shape):
+            return None if x is None else torch.as_tensor(x, dtype=kind).reshape(shape).contiguous().to(self.device)
+        self.reorder_k, self.reorder_v = small(reorder_k, torch.int32, (H, D)), small(reorder_v, torch.int32, (H, D))
+        self.alpha_k, self.alpha_v = small(alpha_k, torch.float32, (H, ng)), small(alpha_v, torch.float32, (H, ng))
+        self.struct = SkvqPagedCacheStruct(*[_dptr(t) if t is None or t.numel() else None for t in (
+            self.k_codes, self.v_codes, self.k_meta, self.v_meta, self.k_win, self.v_win, self.reorder_k, self.reorder_v,
+            self.alpha_k, self.alpha_v, self.status)])
+
+    def batch(self, page_table, lens, starts, n_tokens: int, max_new: int, max_len: int, slots=None) -> SkvqPagedBatch:
+        """The sequences of a step: page_table int32 [n, max_pages], lens int32 [n] (tokens including the new ones), starts
+        int32 [n + 1] (their rows among the n_tokens packed ones), slots int32 [n] or None; max_new and max_len bound them."""
+        n = page_table.shape[0]
+        for t, count in ((page_table, page_table.numel()), (lens, n), (starts, n + 1), (slots, n)):
+            assert t is None or (t.device == self.device and t.dtype == torch.int32 and t.is_contiguous() and t.numel() == count)
+        b = SkvqPagedBatch(page_table.data_ptr(), lens.data_ptr(), starts.data_ptr(), _dptr(slots), n, page_table.shape[1],
+                           n_tokens, max_new, max_len)
+        b.keep = (page_table, lens, starts, slots)
+        return b
+
+    def _rows(self, x, batch, heads):
+        assert x.device == self.device and x.dtype == self.dtype and x.dim() == 3 and x.shape[0] >= batch.n_tokens
+        D = self.cfg.head_dim
+        assert tuple(x.shape[1:]) == (heads, D) and x.stride(2) == 1 and (heads == 1 or x.stride(1) == D), "rows: heads and channels contiguous"
+        return x.stride(0) if x.shape[0] > 1 else heads * D
+
+    def append(self, batch, k, v, rope=None, stream=None) -> None:
+        """k, v: [T, Hkv, D] in the cache's type, any token stride that is a multiple of 8."""
+        ks, vs = self._rows(k, batch, self.cfg.n_kv_heads), self._rows(v, batch, self.cfg.n_kv_heads)
+        with _on(self.device):
+            skvq_paged_append(self.cfg, self.struct, batch, None if rope is None else rope.struct, k, v, ks, vs, stream)
+
+    def read(self, batch, k=None, v=None, window: bool = True, stream=None):
+        """The new tokens' rows of the cache as values [T, Hkv, D], in source order; into k and v where they are given."""
+        shape = (batch.n_tokens, self.cfg.n_kv_heads, self.cfg.head_dim)
+        with _on(self.device):
+            k = torch.empty(shape, dtype=self.dtype, device=self.device) if k is None else k
+            v = torch.empty(shape, dtype=self.dtype, device=self.device) if v is None else v
+            skvq_paged_read(self.cfg, self.struct, batch, 1 if window else 0, k, v, self._rows(k, batch, shape[1]),
+                            self._rows(v, batch, shape[1]), stream)
+        return k, v
+
+    def attention(self, batch, q, sm_scale, out=None, causal: bool = True, rope=None, lse=None, n_splits: int = 0,
+                  workspace=None, stream=None):
+        """q [T, Hq, D] -> out [T, Hq, D]; lse: optional float32 [T, Hq].  Without a workspace (a tensor of at least
+        skvq_paged_workspace_size bytes) each call takes one of its own from torch's allocator on the stream it runs on, so calls
+        on several streams and captured graphs never share it."""
+        c = self.cfg
+        with _on(self.device), (_HERE if stream is None else torch.cuda.stream(stream)):
+            out = torch.empty((batch.n_tokens, c.n_q_heads, c.head_dim), dtype=self.dtype, device=self.device) if out is None else out
+            ws = workspace
+            if ws is None:
+                need = skvq_paged_workspace_size(c, batch, n_splits)
+                ws = torch.empty((need + 15) // 16 * 4, dtype=torch.float32, device=self.device)
+            assert ws.device == self.device and (lse is None or (lse.dtype == torch.float32 and lse.is_contiguous() and lse.device == self.device and
+                                                                 lse.numel() >= batch.n_tokens * c.n_q_heads))
+            args = SkvqPagedAttnArgs(sm_scale, 1 if causal else 0, n_splits, ws.data_ptr(), ws.numel() * ws.element_size())
+            skvq_paged_attention(c, self.struct, batch, None if rope is None else rope.struct, q, self._rows(q, batch, c.n_q_heads),
+                                 out, self._rows(out, batch, c.n_q_heads), lse, args, stream)
         return out
