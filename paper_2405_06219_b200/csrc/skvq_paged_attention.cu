@@ -8,10 +8,14 @@
 //
 // With q' the rotated, reordered query, the scores of a quantized token are formed without dequantizing the key:
 //   q'.K~_t = sum_g h_{t,g} (sum_{j in g} q'_j c_{t,j}) + sum_g z_{t,g} (sum_{j in g} q'_j)
-// the inner sums on mma.m16n8k16 with fp32 accumulators, one per group: 16 tokens' codes (exact in fp16) are the A operand, 8
-// query rows the B operand, so that what costs instructions -- unpacking codes -- is shared by all rows and a single query
-// wastes no more than the 8 columns.  Values are formed as fp16(h c + z) in registers (one rounding, 2^-11 at most) as the A
-// operand of the transposed product (V~^T P^T) and multiplied by the probabilities in fp16.  A probability is held times 2^14
+// the inner sums on mma.m16n8k16 with fp32 accumulators, one per group: 16 tokens' codes are the A operand, 8 query rows the B
+// operand, so that what costs instructions -- unpacking codes -- is shared by all rows and a single query wastes no more than
+// the 8 columns.  A code goes in as 1024 + c (one instruction: its nibble under the bits of 1024) or, where the nibble lies four
+// bits higher, as 1024 + 16 c against q'/16; the accumulators start at minus 1024 times the sum of the operand's q', so they end at
+// sum q' c.  On the way they reach 1024 |q'| per term: of fp32's 24 bits that leaves 17 for the sum of codes, an error of h 2^-9
+// sum |q'| at the very most (16 truncated additions of 2^-23).  Values enter the transposed product (V~^T P^T) as fp16(h c)
+// (one rounding, 2^-11 at most: h times 1024 + c, minus 1024 h, in one multiply-add) and the zero points as one more row tile of
+// it, exact, so nothing is added per element; probabilities are rounded to fp16.  A probability is held times 2^14
 // relative to the running maximum: fp16 then resolves 2^-38 of the largest, so a million small ones still add up; their
 // sum is kept in fp32.
 // Fragments: the channels of a k-step and the tokens of a row are free to choose as long as both operands agree.  A lane's
@@ -34,7 +38,8 @@ using mmak::smem_u32;
 constexpr int kSplitWarps = 4;
 constexpr int kSplitThreads = kSplitWarps * 32;
 constexpr int kTile = 32;             // tokens per warp tile
-constexpr int kRingCost = 4;          // a window tile moves 16-bit rows: about four times the bytes
+constexpr int kRingTile = 16;         // tokens per warp tile of the unquantized window: its rows fill the warp's whole ring
+constexpr int kRingCost = 2;          // and move about twice a code tile's bytes
 constexpr int kStages = 2;
 constexpr float kPScaleLog2 = 14.0f;
 
@@ -64,8 +69,12 @@ struct Geometry {
     static constexpr int JROW = D + 4;                 // floats per row of a warp's accumulators in shared memory
     static constexpr int RINGS = kSplitWarps * kStages * STAGE;
     static constexpr int JOIN = kSplitWarps * ROWS * JROW * 4;
-    static constexpr int POOL = RINGS > JOIN ? RINGS : JOIN;      // both hold, at other times, the raw queries too
-    static constexpr int SMEM = POOL + ROWS * QROW * 2;
+    static constexpr int POOL = RINGS > JOIN ? RINGS : JOIN;
+    static constexpr int QS = ROWS * QROW * 2;         // queries, odd channels times 1/16; then the queries; then the queries in source order
+    static constexpr int SMEM = POOL + 3 * QS;
+    static constexpr int RROW = D * 2;                 // bytes of a window row
+    static constexpr int RCHUNKS = RROW / 16;
+    static_assert(2 * kRingTile * RROW <= kStages * STAGE, "a window tile fits the warp's ring");
 };
 
 // Position of 16-byte piece c of row t inside the tile: rows that one load instruction touches fall into different banks.
@@ -94,15 +103,36 @@ __device__ __forceinline__ uint32_t h2_fma(uint32_t a, uint32_t b, uint32_t c)
     asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
     return r;
 }
-// Four nibble pairs (i, i + 4) of a word as exact fp16 pairs.  1024 + c is fp16 0x6400 | c, 1024 + 16 c is 0x6400 | c << 4.
-__device__ __forceinline__ void nibble_pairs(uint32_t w, uint32_t (&r)[4])
+// Four nibble pairs (i, i + 4) of a word as fp16 pairs: 1024 + c is 0x6400 | c, 1024 + 16 c is 0x6400 | c << 4.
+__device__ __forceinline__ void raw_pairs(uint32_t w, uint32_t (&r)[4])      // 1024 + c, 1024 + 16 c, 1024 + c, 1024 + 16 c
 {
-    constexpr uint32_t M = 0x64006400u, SIXTEENTH = 0x2C002C00u, MINUS64 = 0xD400D400u;
+    constexpr uint32_t M = 0x64006400u;
     const uint32_t u = w >> 8;
-    r[0] = h2_sub(and_or(w, 0x000F000Fu, M), M);
-    r[1] = h2_fma(and_or(w, 0x00F000F0u, M), SIXTEENTH, MINUS64);
-    r[2] = h2_sub(and_or(u, 0x000F000Fu, M), M);
-    r[3] = h2_fma(and_or(u, 0x00F000F0u, M), SIXTEENTH, MINUS64);
+    r[0] = and_or(w, 0x000F000Fu, M);
+    r[1] = and_or(w, 0x00F000F0u, M);
+    r[2] = and_or(u, 0x000F000Fu, M);
+    r[3] = and_or(u, 0x00F000F0u, M);
+}
+// Is one of the four halves above `top`?
+__device__ __forceinline__ bool any_above(uint32_t a, uint32_t b, uint32_t top)
+{
+    uint32_t m;
+    asm("max.f16x2 %0, %1, %2;" : "=r"(m) : "r"(a), "r"(b));
+    return (m & 0x7FFFu) > (top & 0x7FFFu) || ((m >> 16) & 0x7FFFu) > (top >> 16);
+}
+__device__ __forceinline__ uint32_t h2_mul(uint32_t a, uint32_t b)
+{
+    uint32_t r;
+    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+// d = a b + c with an accumulator of its own
+__device__ __forceinline__ void mma16816_from(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1, float c0,
+                                              float c1, float c2, float c3)
+{
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%12,%13};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c0), "f"(c1), "f"(c2), "f"(c3));
 }
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t v)      // of 16-bit elements; lane 4r + c holds columns 2c, 2c + 1 of row r
 {
@@ -126,7 +156,7 @@ template <> __device__ __forceinline__ uint32_t as_h2<__nv_bfloat16>(uint32_t v)
 
 // What a sequence contributes to the flat partition.
 struct SeqCost {
-    int tiles_c, tiles_r;      // 32-token tiles of quantized tokens, of the window
+    int tiles_c, tiles_r;      // tiles of quantized tokens (32), of the window (16)
     int cost;                  // of one item, at least 1
     int m_tiles;               // items per KV head
 };
@@ -136,7 +166,7 @@ __device__ __forceinline__ SeqCost seq_cost(const PagedArgs &p, const PagedSeq &
     const int rep = p.cfg.n_q_heads / p.cfg.n_kv_heads;
     const int lq = max(s.len - p.cfg.window, 0);
     c.tiles_c = (lq + kTile - 1) / kTile;
-    c.tiles_r = (s.len - lq + kTile - 1) / kTile;
+    c.tiles_r = (s.len - lq + kRingTile - 1) / kRingTile;
     c.cost = max(c.tiles_c + kRingCost * c.tiles_r, 1);
     c.m_tiles = (s.n * rep + rows - 1) / rows;
     return c;
@@ -152,9 +182,10 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 4 ? 2 : (NT == 2 ? 3 : 4)
     const skvq_paged_config &cfg = p.cfg;
     extern __shared__ __align__(128) uint8_t smem[];
     long long *pre = reinterpret_cast<long long *>(smem + Geo::SMEM);      // [n_seqs + 1] cost of the sequences before b
-    __half *qs = reinterpret_cast<__half *>(smem + Geo::POOL);
+    __half *qs = reinterpret_cast<__half *>(smem + Geo::POOL), *qr = qs + ROWS * Geo::QROW;
+    T *raw = reinterpret_cast<T *>(qr + ROWS * Geo::QROW);      // [ROWS][QROW]
     __shared__ long long scan_sh[kSplitWarps];
-    __shared__ float row_scale[ROWS], q_sum[ROWS][4];
+    __shared__ float row_scale[ROWS], q_sum[ROWS][4], q_off[ROWS][4], q_max[ROWS][4];      // per 32-channel granule
     __shared__ float ml_sh[kSplitWarps][ROWS][2];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, j = lane & 3;
     const int rep = cfg.n_q_heads / cfg.n_kv_heads, B = p.batch.n_seqs;
@@ -236,80 +267,129 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 4 ? 2 : (NT == 2 ? 3 : 4)
         const int seg0 = tile_of(off), seg1 = tile_of(off + take);
         const int c0 = min(seg0, sc.tiles_c), c1 = max(min(min(seg1, sc.tiles_c), (limit_hi + kTile - 1) / kTile), c0);
         const int q0 = c0 + (int)((long long)(c1 - c0) * warp / kSplitWarps), q1 = c0 + (int)((long long)(c1 - c0) * (warp + 1) / kSplitWarps);
-        const int P = cfg.page_tokens;
+        const int P = cfg.page_tokens, page_shift = __ffs(P) - 1;
         const int32_t *table = p.batch.page_table + (int64_t)b * p.batch.max_pages;
         // Page ids of 32 consecutive 16-token blocks, one per lane; -1 past the quantized tokens, -2 for an id outside the pool.
         auto load_pages = [&](int block) {
             const int t = (block + lane) * 16;
             int id = -1;
             if (t < lq) {
-                id = table[t / P];
+                id = table[t >> page_shift];
                 if (id < 0 || id >= cfg.n_pages) { id = -2; set_status(p.c.status, SKVQ_STATUS_BAD_PAGE); }
             }
             return id;
         };
         int pages_base = q0 * 2, pages = q0 < q1 ? load_pages(pages_base) : -1, pages_next = q0 < q1 ? load_pages(pages_base + 32) : -1;
 
-        // ---- queries: rotate, round to T, reorder; fp16 rows (bf16 rows times a power of two), group sums
-        for (int r = tid >> 3; r < ROWS; r += kSplitThreads / 8) {
-            const int part = tid & 7;      // 8 threads per row, CPT channels each
-            T *raw = reinterpret_cast<T *>(smem);        // [ROWS][D], before the rings are in use
-            const int i = (row_base + r) / rep, head = hk * rep + (row_base + r) % rep;
-            const int pos = L - seq.n + i;
-            const T *src = static_cast<const T *>(a.q) + (int64_t)(seq.row0 + i) * a.q_stride + (int64_t)head * D;
-            if (r < R) {
-                const float2 *rope = static_cast<const float2 *>(p.rope.table);
-                const int half = p.rope.rot_dim / 2;
-#pragma unroll 4
-                for (int k = 0; k < Geo::CPT; ++k) {
-                    const int c = part + 8 * k;
-                    T x = src[c];
-                    if (rope && pos >= 0 && c < p.rope.rot_dim) {
-                        const bool second = p.rope.interleaved ? c & 1 : c >= half;
-                        const int pair = p.rope.interleaved ? c >> 1 : (second ? c - half : c);
-                        const int partner = p.rope.interleaved ? c ^ 1 : (second ? c - half : c + half);
-                        const float2 cs = rope[(int64_t)pos * half + pair];
-                        const float own = Elem<T>::to_float(x), other = Elem<T>::to_float(src[partner]);
-                        x = Elem<T>::from_float(second ? rotate_second(other, own, cs.x, cs.y) : rotate_first(own, other, cs.x, cs.y));
+        // ---- quantized tokens
+        const uint32_t ring = smem_u32(smem) + warp * kStages * Geo::STAGE;
+        const uint8_t *ring_ptr = smem + warp * kStages * Geo::STAGE;
+        const uint32_t codes_dst = (lane / Geo::CHUNKS) * Geo::ROW + piece_at<D>(lane / Geo::CHUNKS, lane % Geo::CHUNKS) * 16;
+        const uint8_t *km_pool = static_cast<const uint8_t *>(p.c.k_meta), *vm_pool = static_cast<const uint8_t *>(p.c.v_meta);
+        uint32_t bad = 0;      // bit 2 * stage + block: the block has no page
+        auto fetch = [&](int tile, int stage) {
+            if (tile < q1) {
+                if (tile * 2 >= pages_base + 32) {
+                    pages_base += 32;
+                    pages = pages_next;
+                    pages_next = load_pages(pages_base + 32);
+                }
+                const int ida = __shfl_sync(0xffffffffu, pages, tile * 2 - pages_base), idb = __shfl_sync(0xffffffffu, pages, tile * 2 + 1 - pages_base);
+                bad = (bad & ~(3u << (2 * stage))) | ((ida < 0 ? 1u : 0u) | (idb < 0 ? 2u : 0u)) << (2 * stage);
+                // The codes of a 16-token block are contiguous in the pool, and a lane's pieces of the tile lie 32 pieces apart:
+                // one address per block and tensor, constant offsets from there.
+                const uint32_t base = ring + stage * Geo::STAGE;
+                const int64_t ra = ((int64_t)ida * cfg.n_kv_heads + hk) * P + ((tile * kTile) & (P - 1));
+                const int64_t rb = ((int64_t)idb * cfg.n_kv_heads + hk) * P + ((tile * kTile + 16) & (P - 1));
+                constexpr int HALF = Geo::CHUNKS / 2;
+#pragma unroll
+                for (int blk = 0; blk < 2; ++blk) {
+                    if ((blk ? idb : ida) >= 0) {
+                        const int64_t at = (blk ? rb : ra) * Geo::ROW + lane * 16;
+                        const uint8_t *kc = static_cast<const uint8_t *>(p.c.k_codes) + at, *vc = static_cast<const uint8_t *>(p.c.v_codes) + at;
+#pragma unroll
+                        for (int k = 0; k < HALF; ++k) {
+                            const uint32_t dst = base + codes_dst + (blk * HALF + k) * 512;
+                            cp16(dst, kc + k * 512);
+                            cp16(dst + Geo::CODES, vc + k * 512);
+                        }
                     }
-                    raw[r * D + c] = x;
+                }
+                // parameters: PIECES 16-byte pieces per tensor, the first half of them block a's
+                constexpr int PIECES = kTile * NG / 4;
+                if constexpr (PIECES <= 16) {
+                    const int side = lane >= PIECES, piece = lane - side * PIECES;
+                    const bool second = piece >= PIECES / 2;
+                    if (lane < 2 * PIECES && (second ? idb : ida) >= 0)
+                        cp16(base + 2 * Geo::CODES + lane * 16, (side ? vm_pool : km_pool) + (second ? rb : ra) * (NG * 4) + (piece - second * (PIECES / 2)) * 16);
+                } else {
+                    const bool second = lane >= PIECES / 2;
+                    if ((second ? idb : ida) >= 0) {
+                        const int64_t at = (second ? rb : ra) * (NG * 4) + (lane - second * (PIECES / 2)) * 16;
+                        cp16(base + 2 * Geo::CODES + lane * 16, km_pool + at);
+                        cp16(base + 2 * Geo::CODES + Geo::META + lane * 16, vm_pool + at);
+                    }
                 }
             }
-            __syncwarp();
-            float x[Geo::CPT], mx = 0.f, sum = 0.f;
+            cp_commit();
+        };
 #pragma unroll
-            for (int k = 0; k < Geo::CPT; ++k) {
-                const int c = part * Geo::CPT + k;
-                const int s = p.c.reorder_k ? p.c.reorder_k[hk * D + c] & (D - 1) : c;
-                x[k] = r < R ? Elem<T>::to_float(raw[r * D + s]) : 0.f;
-                mx = fmaxf(mx, fabsf(x[k]));
-            }
-            float up = 1.f;
-            if (!__is_same(T, __half)) {
-                // bf16 has more range than fp16: bring the row's largest to [2^13, 2^14), exactly
-#pragma unroll
-                for (int m = 1; m < 8; m <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, m));
-                if (mx > 0.f && mx < CUDART_INF_F) {
-                    int e;
-                    frexpf(mx, &e);
-                    up = ldexpf(1.f, min(14 - e, 126));
+        for (int k = 0; k < kStages - 1; ++k) fetch(q0 + k, k);
+        // ---- queries: rotate, round to T, reorder; fp16 rows times a power of two, sums of every 32-channel granule.  A thread
+        // per channel (of D = 64: of two rows at a time), so that the few rows of a decode step take one trip to memory
+        {
+            constexpr int STEP = kSplitThreads / D, PARTS = D / 32;
+            const int c = tid % D, r_first = tid / D, part = c / 32;
+            const int from = p.c.reorder_k ? p.c.reorder_k[hk * D + c] & (D - 1) : c;
+            const float2 *rope = static_cast<const float2 *>(p.rope.table);
+            const int half = p.rope.rot_dim / 2;
+            const bool turn = rope && c < p.rope.rot_dim, second = p.rope.interleaved ? c & 1 : c >= half;
+            const int pair = p.rope.interleaved ? c >> 1 : (second ? c - half : c);
+            const int partner = p.rope.interleaved ? c ^ 1 : (second ? c - half : c + half);
+#pragma unroll 4
+            for (int r = r_first; r < R; r += STEP) {
+                const int i = (row_base + r) / rep, head = hk * rep + (row_base + r) % rep, pos = L - seq.n + i;
+                const T *src = static_cast<const T *>(a.q) + (int64_t)(seq.row0 + i) * a.q_stride + (int64_t)head * D;
+                T x = src[c];
+                if (turn && pos >= 0) {
+                    const float2 cs = rope[(int64_t)pos * half + pair];
+                    const float own = Elem<T>::to_float(x), other = Elem<T>::to_float(src[partner]);
+                    x = Elem<T>::from_float(second ? rotate_second(other, own, cs.x, cs.y) : rotate_first(own, other, cs.x, cs.y));
                 }
+                raw[r * Geo::QROW + c] = x;
             }
-#pragma unroll
-            for (int k = 0; k < Geo::CPT; ++k) {
-                const __half v = __float2half_rn(x[k] * up);
-                sum += __half2float(v);
-                qs[r * Geo::QROW + part * Geo::CPT + k] = v;
+            __syncthreads();
+#pragma unroll 4
+            for (int r = r_first; r < R; r += STEP) {
+                const float mx = mmak::warp_max(fabsf(Elem<T>::to_float(raw[r * Geo::QROW + from])));
+                if (lane == 0) q_max[r][part] = mx;
             }
-            const int per_group = 8 / NG;
+            __syncthreads();
+            const float sign = a.sm_scale < 0.f ? -1.f : (a.sm_scale == 0.f ? 0.f : 1.f);      // the rows' scale is positive
+#pragma unroll 2
+            for (int r = r_first; r < ROWS; r += STEP) {
+                __half v = __float2half_rn(0.f), w = v;
+                float sum = 0.f, off_sum = 0.f, up = 1.f;
+                if (r < R && sign != 0.f) {
+                    float mx = q_max[r][0];
 #pragma unroll
-            for (int m = 1; m < per_group; m <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, m);
-            if (part % per_group == 0) q_sum[r][part / per_group] = sum;
-            if (part == 0) row_scale[r] = a.sm_scale * 1.4426950408889634f / up;
+                    for (int k = 1; k < PARTS; ++k) mx = fmaxf(mx, q_max[r][k]);
+                    // bring the row's largest to [2^13, 2^14): exact, whatever the range of the type
+                    if (mx > 0.f && mx < CUDART_INF_F) up = __int_as_float((127 + min(13 - (__float_as_int(mx) >> 23) + 127, 60)) << 23);
+                    v = __float2half_rn(Elem<T>::to_float(raw[r * Geo::QROW + from]) * (up * sign));
+                    w = c & 1 ? __hmul(v, __float2half_rn(0.0625f)) : v;
+                    sum = mmak::warp_sum(__half2float(v));
+                    off_sum = mmak::warp_sum(__half2float(w));
+                }
+                qr[r * Geo::QROW + c] = v;
+                qs[r * Geo::QROW + c] = w;
+                if (lane == 0) { q_sum[r][part] = sum; q_off[r][part] = -1024.f * off_sum; }
+                if (c == 0) row_scale[r] = (sign == 0.f ? 1.f : fabsf(a.sm_scale)) * 1.4426950408889634f / up;
+            }
         }
         __syncthreads();
         uint32_t bq[NT][Geo::SETS * 2][2];
-        float rs[NT][2], qsum[NT][2][NG];
+        float rs[NT][2], qsum[NT][2][NG], qoff[NT][2][NG];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
 #pragma unroll
@@ -324,11 +404,19 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 4 ? 2 : (NT == 2 ? 3 : 4)
             for (int e = 0; e < 2; ++e) {
                 rs[n][e] = row_scale[8 * n + 2 * j + e];
 #pragma unroll
-                for (int k = 0; k < NG; ++k) qsum[n][e][k] = q_sum[8 * n + 2 * j + e][k];
+                for (int k = 0; k < NG; ++k) {
+                    constexpr int PER = Geo::SETS / NG;      // granules per group
+                    float u = 0.f, v = 0.f;
+#pragma unroll
+                    for (int m = 0; m < PER; ++m) { u += q_sum[8 * n + 2 * j + e][k * PER + m]; v += q_off[8 * n + 2 * j + e][k * PER + m]; }
+                    qsum[n][e][k] = u;
+                    qoff[n][e][k] = v;
+                }
             }
         }
 
         float o[NT][Geo::MT][4];      // [.][channel pair][{first, second channel} x {row 2j, row 2j + 1}]
+        float oz[NT][4];              // sum of p z of the lane's channels (their group): rows 2j, 2j + 1; [2], [3] unused
         float m_run[NT][2], l_run[NT][2];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
@@ -337,18 +425,22 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 4 ? 2 : (NT == 2 ? 3 : 4)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) o[n][m][e] = 0.f;
 #pragma unroll
+            for (int e = 0; e < 4; ++e) oz[n][e] = 0.f;
+#pragma unroll
             for (int e = 0; e < 2; ++e) { m_run[n][e] = -CUDART_INF_F; l_run[n][e] = 0.f; }
         }
 
-        // Scores (log2 domain) of 32 tokens -> probabilities as B fragments.  s[u][n] = {token a: rows 2j, 2j+1; token a + 8: the
-        // same}, token a = 16 u + (g >> 1) + 4 (g & 1).
-        auto softmax_tile = [&](float (&s)[2][NT][4], uint32_t (&pb)[2][NT][2]) {
+        // Scores of 16 or 32 tokens (to be multiplied by the row's scale rs) -> probabilities as B fragments.  s[u][n] = {token a: rows
+        // 2j, 2j+1; token a + 8: the same}, token a = 16 u + (g >> 1) + 4 (g & 1).
+        auto softmax_tile = [&](auto &s, auto &pb) {
+            constexpr int U = sizeof(s) / sizeof(s[0]);
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
                 float x[2], base[2];
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    x[e] = fmaxf(fmaxf(s[0][n][e], s[0][n][2 + e]), fmaxf(s[1][n][e], s[1][n][2 + e]));
+                    x[e] = fmaxf(s[0][n][e], s[0][n][2 + e]);
+                    if constexpr (U == 2) x[e] = fmaxf(x[e], fmaxf(s[1][n][e], s[1][n][2 + e]));
 #pragma unroll
                     for (int d = 4; d < 32; d <<= 1) x[e] = fmaxf(x[e], __shfl_xor_sync(0xffffffffu, x[e], d));
                     x[e] = fmaxf(x[e], m_run[n][e]);
@@ -357,20 +449,22 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 4 ? 2 : (NT == 2 ? 3 : 4)
                     float down[2];
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        down[e] = x[e] > m_run[n][e] ? ex2_approx(m_run[n][e] - x[e]) : 1.f;
+                        down[e] = x[e] > m_run[n][e] ? ex2_approx((m_run[n][e] - x[e]) * rs[n][e]) : 1.f;
                         l_run[n][e] *= down[e];
                         m_run[n][e] = x[e];
                     }
 #pragma unroll
                     for (int m = 0; m < Geo::MT; ++m) { o[n][m][0] *= down[0]; o[n][m][1] *= down[1]; o[n][m][2] *= down[0]; o[n][m][3] *= down[1]; }
+                    oz[n][0] *= down[0];
+                    oz[n][1] *= down[1];
                 }
 #pragma unroll
-                for (int e = 0; e < 2; ++e) base[e] = (m_run[n][e] == -CUDART_INF_F ? 0.f : m_run[n][e]) - kPScaleLog2;
+                for (int e = 0; e < 2; ++e) base[e] = kPScaleLog2 - (m_run[n][e] == -CUDART_INF_F ? 0.f : m_run[n][e] * rs[n][e]);
 #pragma unroll
-                for (int u = 0; u < 2; ++u) {
+                for (int u = 0; u < U; ++u) {
                     float v[4];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) v[e] = ex2_approx(s[u][n][e] - base[e & 1]);
+                    for (int e = 0; e < 4; ++e) v[e] = ex2_approx(fmaf(s[u][n][e], rs[n][e & 1], base[e & 1]));
                     l_run[n][0] += v[0] + v[2];
                     l_run[n][1] += v[1] + v[3];
                     pb[u][n][0] = transpose8x8(pack_h2(v[0], v[1]));
@@ -379,50 +473,6 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 4 ? 2 : (NT == 2 ? 3 : 4)
             }
         };
 
-        // ---- quantized tokens
-        const uint32_t ring = smem_u32(smem) + warp * kStages * Geo::STAGE;
-        const uint8_t *ring_ptr = smem + warp * kStages * Geo::STAGE;
-        uint32_t bad = 0;      // bit 2 * stage + block: the block has no page
-        auto fetch = [&](int tile, int stage) {
-            if (tile < q1) {
-                if (tile * 2 >= pages_base + 32) {
-                    pages_base += 32;
-                    pages = pages_next;
-                    pages_next = load_pages(pages_base + 32);
-                }
-                const int ida = __shfl_sync(0xffffffffu, pages, tile * 2 - pages_base), idb = __shfl_sync(0xffffffffu, pages, tile * 2 + 1 - pages_base);
-                bad = (bad & ~(3u << (2 * stage))) | ((ida < 0 ? 1u : 0u) | (idb < 0 ? 2u : 0u)) << (2 * stage);
-                const uint32_t base = ring + stage * Geo::STAGE;
-                // first row of the two 16-token blocks in the pool
-                const int64_t ra = ((int64_t)ida * cfg.n_kv_heads + hk) * P + ((tile * kTile) & (P - 1));
-                const int64_t rb = ((int64_t)idb * cfg.n_kv_heads + hk) * P + ((tile * kTile + 16) & (P - 1));
-#pragma unroll
-                for (int k = 0; k < Geo::CHUNKS; ++k) {
-                    const int q = k * 32 + lane, t = q / Geo::CHUNKS, c = q % Geo::CHUNKS;
-                    const bool first = k < Geo::CHUNKS / 2;      // rows 0-15
-                    if ((first ? ida : idb) >= 0) {
-                        const int64_t at = ((first ? ra : rb) + (t & 15)) * Geo::ROW + c * 16;
-                        const uint32_t dst = base + t * Geo::ROW + piece_at<D>(t, c) * 16;
-                        cp16(dst, static_cast<const uint8_t *>(p.c.k_codes) + at);
-                        cp16(dst + Geo::CODES, static_cast<const uint8_t *>(p.c.v_codes) + at);
-                    }
-                }
-                constexpr int PIECES = kTile * NG / 4;      // 16-byte pieces of one tensor's parameters
-#pragma unroll
-                for (int k = 0; k < (2 * PIECES + 31) / 32; ++k) {
-                    const int q = k * 32 + lane, side = q >= PIECES, piece = q - side * PIECES;
-                    const int t = piece * 4 / NG;
-                    if (q < 2 * PIECES && (t < 16 ? ida : idb) >= 0) {
-                        const int64_t row = t < 16 ? ra : rb;
-                        const uint8_t *src = static_cast<const uint8_t *>(side ? p.c.v_meta : p.c.k_meta) + row * (NG * 4) + (piece - (t < 16 ? 0 : PIECES / 2)) * 16;
-                        cp16(base + 2 * Geo::CODES + side * Geo::META + piece * 16, src);
-                    }
-                }
-            }
-            cp_commit();
-        };
-#pragma unroll
-        for (int k = 0; k < kStages - 1; ++k) fetch(q0 + k, k);
         int stage = 0;
         const int tok = (g >> 1) + 4 * (g & 1);      // the token of row g of the score product, inside its 8
         const int end = min(lq, limit_lo);
@@ -441,27 +491,22 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 4 ? 2 : (NT == 2 ? 3 : 4)
                 const int t = 16 * u + tok;
                 float acc[NT][NG][4];
 #pragma unroll
-                for (int n = 0; n < NT; ++n)
-#pragma unroll
-                    for (int k = 0; k < NG; ++k)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) acc[n][k][e] = 0.f;
-#pragma unroll
                 for (int st = 0; st < Geo::SETS; ++st) {
                     uint32_t x[4], y[4];
-                    nibble_pairs(*reinterpret_cast<const uint32_t *>(buf + t * Geo::ROW + piece_at<D>(t, st) * 16 + j * 4), x);
-                    nibble_pairs(*reinterpret_cast<const uint32_t *>(buf + (t + 8) * Geo::ROW + piece_at<D>(t, st) * 16 + j * 4), y);
+                    raw_pairs(*reinterpret_cast<const uint32_t *>(buf + t * Geo::ROW + piece_at<D>(t, st) * 16 + j * 4), x);
+                    raw_pairs(*reinterpret_cast<const uint32_t *>(buf + (t + 8) * Geo::ROW + piece_at<D>(t, st) * 16 + j * 4), y);
+                    constexpr int PER = Geo::SETS / NG;      // sets per group
 #pragma unroll
                     for (int n = 0; n < NT; ++n) {
-                        float (&d)[4] = acc[n][st * NG / Geo::SETS];
-                        mma16816(d, x[0], y[0], x[1], y[1], bq[n][2 * st][0], bq[n][2 * st][1]);
+                        float (&d)[4] = acc[n][st / PER];
+                        if (st % PER == 0)
+                            mma16816_from(d, x[0], y[0], x[1], y[1], bq[n][2 * st][0], bq[n][2 * st][1], qoff[n][0][st / PER], qoff[n][1][st / PER],
+                                          qoff[n][0][st / PER], qoff[n][1][st / PER]);
+                        else
+                            mma16816(d, x[0], y[0], x[1], y[1], bq[n][2 * st][0], bq[n][2 * st][1]);
                         mma16816(d, x[2], y[2], x[3], y[3], bq[n][2 * st + 1][0], bq[n][2 * st + 1][1]);
                     }
                 }
-#pragma unroll
-                for (int n = 0; n < NT; ++n)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) s[u][n][e] = 0.f;
 #pragma unroll
                 for (int k = 0; k < NG; ++k) {
                     const uint32_t ma = km[t * NG + k], mb = km[(t + 8) * NG + k];
@@ -470,14 +515,11 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 4 ? 2 : (NT == 2 ? 3 : 4)
                     for (int n = 0; n < NT; ++n)
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
-                            s[u][n][e] = fmaf(ha.x, acc[n][k][e], fmaf(ha.y, qsum[n][e][k], s[u][n][e]));
-                            s[u][n][2 + e] = fmaf(hb.x, acc[n][k][2 + e], fmaf(hb.y, qsum[n][e][k], s[u][n][2 + e]));
+                            const float za = ha.y * qsum[n][e][k], zb = hb.y * qsum[n][e][k];
+                            s[u][n][e] = fmaf(ha.x, acc[n][k][e], k ? za + s[u][n][e] : za);
+                            s[u][n][2 + e] = fmaf(hb.x, acc[n][k][2 + e], k ? zb + s[u][n][2 + e] : zb);
                         }
                 }
-#pragma unroll
-                for (int n = 0; n < NT; ++n)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) s[u][n][e] *= rs[n][e & 1];
             }
             const bool edge = t0 + kTile > end || bad_here;      // some row or some token of the tile is masked
             if (edge) {
@@ -501,8 +543,11 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 4 ? 2 : (NT == 2 ? 3 : 4)
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
                     hz[k] = vm[(ta + 4 * k) * NG + g * NG / 8];
-                    // a row that holds nothing must not reach the product: 0 times what lies there need not be 0
-                    if (edge && (t0 + ta + 4 * k >= lq || ((bad_here >> u) & 1u))) hz[k] = 0u;
+                }
+                if (edge) {      // a row that holds nothing must not reach the product: 0 times what lies there need not be 0
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        if (t0 + ta + 4 * k >= lq || ((bad_here >> u) & 1u)) hz[k] = 0u;
                 }
                 const uint32_t h_a = __byte_perm(hz[0], hz[1], 0x5410), z_a = __byte_perm(hz[0], hz[1], 0x7632);
                 const uint32_t h_b = __byte_perm(hz[2], hz[3], 0x5410), z_b = __byte_perm(hz[2], hz[3], 0x7632);
@@ -520,15 +565,35 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 4 ? 2 : (NT == 2 ? 3 : 4)
                     }
                 }
 #pragma unroll
+                for (int n = 0; n < NT; ++n) mma16816(oz[n], z_a, 0u, z_b, 0u, pb[u][n][0], pb[u][n][1]);
+                // h c = h (1024 + c) - 1024 h, or h/16 (1024 + 16 c) - 64 h: one rounding, unless h is so large that 1024 h is not an
+                // fp16 number; then the code is formed first
+                constexpr uint32_t TOP = 0x53C053C0u;      // 62: h below it in both halves of both
+                const bool large = __any_sync(0xffffffffu, any_above(h_a, h_b, TOP));
+                const uint32_t hs_a = h2_mul(h_a, 0x2C002C00u), hs_b = h2_mul(h_b, 0x2C002C00u);      // h / 16
+                const uint32_t n_a = h2_mul(h_a, 0xE400E400u), n_b = h2_mul(h_b, 0xE400E400u);          // -1024 h
+                const uint32_t ns_a = h2_mul(h_a, 0xD400D400u), ns_b = h2_mul(h_b, 0xD400D400u);        // -64 h
+#pragma unroll
                 for (int q = 0; q < D / 64; ++q) {
 #pragma unroll
                     for (int hf = 0; hf < 2; ++hf) {
                         const uint32_t sel = hf ? 0x7632 : 0x5410;
                         uint32_t x[4], y[4];      // channels 4 hf .. 4 hf + 3 of the word, pairs (token, token + 4)
-                        nibble_pairs(__byte_perm(w[0][q], w[1][q], sel), x);
-                        nibble_pairs(__byte_perm(w[2][q], w[3][q], sel), y);
+                        raw_pairs(__byte_perm(w[0][q], w[1][q], sel), x);
+                        raw_pairs(__byte_perm(w[2][q], w[3][q], sel), y);
+                        if (!large) {
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) { x[k] = h2_fma(h_a, x[k], z_a); y[k] = h2_fma(h_b, y[k], z_b); }
+                            for (int k = 0; k < 4; ++k) {
+                                x[k] = h2_fma(x[k], k & 1 ? hs_a : h_a, k & 1 ? ns_a : n_a);
+                                y[k] = h2_fma(y[k], k & 1 ? hs_b : h_b, k & 1 ? ns_b : n_b);
+                            }
+                        } else {
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) {
+                                x[k] = h2_mul(k & 1 ? h2_fma(x[k], 0x2C002C00u, 0xD400D400u) : h2_sub(x[k], 0x64006400u), h_a);
+                                y[k] = h2_mul(k & 1 ? h2_fma(y[k], 0x2C002C00u, 0xD400D400u) : h2_sub(y[k], 0x64006400u), h_b);
+                            }
+                        }
 #pragma unroll
                         for (int k = 0; k < 2; ++k)
 #pragma unroll
@@ -542,64 +607,78 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 4 ? 2 : (NT == 2 ? 3 : 4)
         }
         cp_wait<0>();
 
-        // ---- the window: 16-bit rows straight from the ring; the warps take its tiles in turn
+        // ---- the window: 16-bit rows, 16 tokens at a time through the warp's whole ring; the warps take its tiles in turn
+        __syncwarp();
         const int r0 = max(seg0, sc.tiles_c), r1 = max(min(seg1, sc.tiles_c + sc.tiles_r), r0);
         const int64_t win_row0 = ((int64_t)seq.slot * cfg.n_kv_heads + hk) * cfg.ring_tokens;
-        auto ring_row = [&](int t) { return win_row0 + min(t, L - 1) % cfg.ring_tokens; };
 #pragma unroll 1
         for (int tile = r0 + warp; tile < r1; tile += kSplitWarps) {
-            const int t0 = lq + (tile - sc.tiles_c) * kTile;
+            const int t0 = lq + (tile - sc.tiles_c) * kRingTile;
             if (t0 >= limit_hi) break;
-            const T *kw = static_cast<const T *>(p.c.k_win), *vw = static_cast<const T *>(p.c.v_win);
-            float s[2][NT][4];
+            {
+                // lane: piece lane % RCHUNKS of every (32 / RCHUNKS)-th row; piece c of row t lies at c ^ (t & 7)
+                constexpr int STEP = 32 / Geo::RCHUNKS;
+                const int c = lane % Geo::RCHUNKS, first = t0 % cfg.ring_tokens;
+                const uint8_t *kw = static_cast<const uint8_t *>(p.c.k_win) + win_row0 * Geo::RROW + c * 16, *vw = static_cast<const uint8_t *>(p.c.v_win) + win_row0 * Geo::RROW + c * 16;
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const int ta = t0 + 16 * u + tok;
-                const T *src_a = kw + ring_row(ta) * D + 8 * j, *src_b = kw + ring_row(ta + 8) * D + 8 * j;
-#pragma unroll
-                for (int n = 0; n < NT; ++n)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) s[u][n][e] = 0.f;
-#pragma unroll
-                for (int st = 0; st < Geo::SETS; ++st) {
-                    uint4 x = *reinterpret_cast<const uint4 *>(src_a + 32 * st), y = *reinterpret_cast<const uint4 *>(src_b + 32 * st);
-                    x.x = as_h2<T>(x.x); x.y = as_h2<T>(x.y); x.z = as_h2<T>(x.z); x.w = as_h2<T>(x.w);
-                    y.x = as_h2<T>(y.x); y.y = as_h2<T>(y.y); y.z = as_h2<T>(y.z); y.w = as_h2<T>(y.w);
-#pragma unroll
-                    for (int n = 0; n < NT; ++n) {
-                        mma16816(s[u][n], __byte_perm(x.x, x.z, 0x5410), __byte_perm(y.x, y.z, 0x5410), __byte_perm(x.x, x.z, 0x7632),
-                                 __byte_perm(y.x, y.z, 0x7632), bq[n][2 * st][0], bq[n][2 * st][1]);
-                        mma16816(s[u][n], __byte_perm(x.y, x.w, 0x5410), __byte_perm(y.y, y.w, 0x5410), __byte_perm(x.y, x.w, 0x7632),
-                                 __byte_perm(y.y, y.w, 0x7632), bq[n][2 * st + 1][0], bq[n][2 * st + 1][1]);
+                for (int k = 0; k < kRingTile / STEP; ++k) {
+                    const int t = k * STEP + lane / Geo::RCHUNKS;
+                    const uint32_t at = t * Geo::RROW + (c ^ (t & 7)) * 16;
+                    if (t0 + t < L) {
+                        int row = first + t;      // the window is no longer than the ring: it wraps once at most
+                        if (row >= cfg.ring_tokens) row -= cfg.ring_tokens;
+                        cp16(ring + at, kw + (int64_t)row * Geo::RROW);
+                        cp16(ring + kRingTile * Geo::RROW + at, vw + (int64_t)row * Geo::RROW);
+                    } else {
+                        *reinterpret_cast<uint4 *>(smem + warp * kStages * Geo::STAGE + kRingTile * Geo::RROW + at) = make_uint4(0u, 0u, 0u, 0u);
                     }
                 }
-#pragma unroll
-                for (int n = 0; n < NT; ++n)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) s[u][n][e] = ta + 8 * (e >> 1) < lim[n][e & 1] ? s[u][n][e] * rs[n][e & 1] : -CUDART_INF_F;
+                cp_commit();
+                cp_wait<0>();
+                __syncwarp();
             }
-            uint32_t pb[2][NT][2];
+            float s[1][NT][4];
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[0][n][e] = 0.f;
+#pragma unroll
+            for (int st = 0; st < Geo::SETS; ++st) {
+                uint4 x = *reinterpret_cast<const uint4 *>(ring_ptr + tok * Geo::RROW + ((4 * st + j) ^ tok) * 16);
+                uint4 y = *reinterpret_cast<const uint4 *>(ring_ptr + (tok + 8) * Geo::RROW + ((4 * st + j) ^ tok) * 16);
+                x.x = as_h2<T>(x.x); x.y = as_h2<T>(x.y); x.z = as_h2<T>(x.z); x.w = as_h2<T>(x.w);
+                y.x = as_h2<T>(y.x); y.y = as_h2<T>(y.y); y.z = as_h2<T>(y.z); y.w = as_h2<T>(y.w);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    const uint4 q = *reinterpret_cast<const uint4 *>(qr + (8 * n + g) * Geo::QROW + 32 * st + 8 * j);
+                    mma16816(s[0][n], x.x, y.x, x.z, y.z, q.x, q.z);
+                    mma16816(s[0][n], x.y, y.y, x.w, y.w, q.y, q.w);
+                }
+            }
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (t0 + tok + 8 * (e >> 1) >= lim[n][e & 1]) s[0][n][e] = -CUDART_INF_F;
+            uint32_t pb[1][NT][2];
             softmax_tile(s, pb);
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
+            for (int q = 0; q < D / 64; ++q) {
+                uint32_t e[4][4];      // rows j, j + 4, j + 8, j + 12, eight of this lane's channels
 #pragma unroll
-                for (int q = 0; q < D / 64; ++q) {
-                    uint32_t e[4][4];      // rows ta, ta + 4, ta + 8, ta + 12, eight of this lane's channels
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const int t = t0 + 16 * u + j + 4 * k;
-                        uint4 x = make_uint4(0u, 0u, 0u, 0u);
-                        if (t < L) x = *reinterpret_cast<const uint4 *>(vw + ring_row(t) * D + g * Geo::CPT + 8 * q);
-                        e[k][0] = as_h2<T>(x.x); e[k][1] = as_h2<T>(x.y); e[k][2] = as_h2<T>(x.z); e[k][3] = as_h2<T>(x.w);
-                    }
-#pragma unroll
-                    for (int k = 0; k < 4; ++k)
-#pragma unroll
-                        for (int n = 0; n < NT; ++n)
-                            mma16816(o[n][4 * q + k], __byte_perm(e[0][k], e[1][k], 0x5410), __byte_perm(e[0][k], e[1][k], 0x7632),
-                                     __byte_perm(e[2][k], e[3][k], 0x5410), __byte_perm(e[2][k], e[3][k], 0x7632), pb[u][n][0], pb[u][n][1]);
+                for (int k = 0; k < 4; ++k) {
+                    const int t = j + 4 * k;
+                    const uint4 x = *reinterpret_cast<const uint4 *>(ring_ptr + kRingTile * Geo::RROW + t * Geo::RROW + ((g * (D / 64) + q) ^ (t & 7)) * 16);
+                    e[k][0] = as_h2<T>(x.x); e[k][1] = as_h2<T>(x.y); e[k][2] = as_h2<T>(x.z); e[k][3] = as_h2<T>(x.w);
                 }
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+                        mma16816(o[n][4 * q + k], __byte_perm(e[0][k], e[1][k], 0x5410), __byte_perm(e[0][k], e[1][k], 0x7632),
+                                 __byte_perm(e[2][k], e[3][k], 0x5410), __byte_perm(e[2][k], e[3][k], 0x7632), pb[0][n][0], pb[0][n][1]);
             }
+            __syncwarp();
         }
 
         // ---- join the four warps, in a fixed order
@@ -612,11 +691,11 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 4 ? 2 : (NT == 2 ? 3 : 4)
                 const int r = 8 * n + 2 * j + e;
 #pragma unroll
                 for (int d = 4; d < 32; d <<= 1) l_run[n][e] += __shfl_xor_sync(0xffffffffu, l_run[n][e], d);
-                if (g == 0) { ml_sh[warp][r][0] = m_run[n][e]; ml_sh[warp][r][1] = l_run[n][e]; }
+                if (g == 0) { ml_sh[warp][r][0] = m_run[n][e] * rs[n][e]; ml_sh[warp][r][1] = l_run[n][e]; }      // from here on in units of log2
                 if (r < R) {
                     float *row = join + (warp * ROWS + r) * Geo::JROW + g;
 #pragma unroll
-                    for (int m = 0; m < Geo::MT; ++m) { row[16 * m] = o[n][m][e]; row[16 * m + 8] = o[n][m][2 + e]; }
+                    for (int m = 0; m < Geo::MT; ++m) { row[16 * m] = o[n][m][e] + oz[n][e]; row[16 * m + 8] = o[n][m][2 + e] + oz[n][e]; }
                 }
             }
         }
@@ -675,17 +754,26 @@ __global__ void __launch_bounds__(D) paged_merge_kernel(const __grid_constant__ 
     constexpr int PS = partial_stride(D);
     const float *base = a.ws + (size_t)args.n_slots * kDescInts + ((size_t)slot * 2 * args.rows + r) * PS;
     auto partial = [&](int k) { return base + (size_t)(2 * k + (k == 0 ? 1 : 0)) * args.rows * PS; };
-    float m = -CUDART_INF_F;
-    for (int k = 0; k < n; ++k) m = fmaxf(m, partial(k)[D]);
-    float o = 0.f, l = 0.f;
-    if (m != -CUDART_INF_F) {
-#pragma unroll 4
-        for (int k = 0; k < n; ++k) {
-            const float *q = partial(k);
-            const float f = ex2_approx(q[D] - m);
-            l = fmaf(q[D + 1], f, l);
-            o = fmaf(q[c], f, o);
-        }
+    // 32 partials at a time: every warp has their maxima and sums in its lanes, each thread walks its channel
+    const int lane = threadIdx.x & 31;
+    float m = -CUDART_INF_F, o = 0.f, l = 0.f;
+    for (int k0 = 0; k0 < n; k0 += 32) {
+        const bool have = k0 + lane < n;
+        const float pm = have ? partial(k0 + lane)[D] : -CUDART_INF_F, pl = have ? partial(k0 + lane)[D + 1] : 0.f;
+        float top = fmaxf(pm, m);
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+        if (top == -CUDART_INF_F) continue;
+        const float down = ex2_approx(m - top), f = ex2_approx(pm - top);
+        float sum = pl * f;
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+        l = fmaf(l, down, sum);
+        o *= down;
+        m = top;
+        const int last = min(32, n - k0);
+#pragma unroll 8
+        for (int k = 0; k < last; ++k) o = fmaf(partial(k0 + k)[c], __shfl_sync(0xffffffffu, f, k), o);
     }
     const int i = row / rep, head = hk * rep + row % rep;
     const int dst = a.p.c.reorder_v ? a.p.c.reorder_v[hk * D + c] & (D - 1) : c;
@@ -706,7 +794,7 @@ int split_slots(const skvq_paged_config &cfg, const skvq_paged_batch &batch, int
     const int per = item_rows(cfg, batch);
     const long long rep = cfg.n_q_heads / cfg.n_kv_heads, m_tiles = (batch.max_new * rep + per - 1) / per;
     const long long lq = batch.max_len > cfg.window ? batch.max_len - cfg.window : 0;
-    const long long cost = (lq + kTile - 1) / kTile + kRingCost * ((batch.max_len - lq + kTile - 1) / kTile) + 1;
+    const long long cost = (lq + kTile - 1) / kTile + kRingCost * ((batch.max_len - lq + kRingTile - 1) / kRingTile) + 1;
     const long long items = (long long)batch.n_seqs * cfg.n_kv_heads * m_tiles;
     long long slots;
     if (n_splits > 0) slots = (long long)n_splits * items;
@@ -742,13 +830,14 @@ template <typename T, int D, int NG, int NT>
 cudaError_t launch_split(const PagedAttnArgs &a, cudaStream_t stream)
 {
     using Geo = Geometry<D, NG, NT>;
+    const long long most = (long long)a.p.batch.max_new * (a.p.cfg.n_q_heads / a.p.cfg.n_kv_heads);      // rows of a KV head
     const SplitArgs s{a, split_slots(a.p.cfg, a.p.batch, a.n_splits), Geo::ROWS};
     static unsigned long long done = 0;
     cudaError_t e = configure_smem_once(paged_split_kernel<T, D, NG, NT>, Geo::SMEM + (int)sizeof(long long) * (kMaxPagedSeqs + 1), done);
     if (e != cudaSuccess) return e;
     e = launch_chained(paged_split_kernel<T, D, NG, NT>, dim3(s.n_slots), kSplitThreads, Geo::SMEM + sizeof(long long) * (a.p.batch.n_seqs + 1), stream, s);
     if (e != cudaSuccess) return e;
-    return launch_chained(paged_merge_kernel<T, D>, dim3(s.n_slots, Geo::ROWS), D, 0, stream, s);
+    return launch_chained(paged_merge_kernel<T, D>, dim3(s.n_slots, (unsigned)(most < Geo::ROWS ? most : Geo::ROWS)), D, 0, stream, s);
 }
 
 template <typename T, int D, int NG> cudaError_t launch_by_rows(const PagedAttnArgs &a, cudaStream_t stream)
