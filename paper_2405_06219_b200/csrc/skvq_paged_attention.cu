@@ -25,7 +25,7 @@
 #include <math_constants.h>
 
 #include "skvq_mma_common.cuh"
-#include "skvq_paged.cuh"
+#include "skvq_paged_split.cuh"
 
 namespace skvq {
 namespace {
@@ -48,11 +48,6 @@ struct SplitArgs {
     int n_slots;
     int rows;      // rows per item: 8 NT
 };
-
-// Workspace: descriptor [n_slots][8] ints, then partials [n_slots][2][rows][D + 4] floats {o[D], m, l, pad}.  A run holds at
-// most one item that it continues (partial 0) and one that it begins and does not finish (partial 1).
-constexpr int kDescInts = 8;
-__host__ __device__ constexpr int partial_stride(int D) { return D + 4; }
 
 template <int D, int NG, int NT>
 struct Geometry {
@@ -168,7 +163,7 @@ __device__ __forceinline__ SeqCost seq_cost(const PagedArgs &p, const PagedSeq &
     c.tiles_c = (lq + kTile - 1) / kTile;
     c.tiles_r = (s.len - lq + kRingTile - 1) / kRingTile;
     c.cost = max(c.tiles_c + kRingCost * c.tiles_r, 1);
-    c.m_tiles = (s.n * rep + rows - 1) / rows;
+    c.m_tiles = s.n * rep <= kFewRows ? (s.n * rep + rows - 1) / rows : 0;      // the others are the tcgen05 kernel's
     return c;
 }
 
@@ -737,62 +732,74 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 4 ? 2 : (NT == 2 ? 3 : 4)
     }
 }
 
-// Joins the partials of an item that several runs share: one CTA per (run that begins the item, row).
+// Joins the partials of an item that several runs share: blockIdx.x is the run that begins it, blockIdx.y takes every
+// gridDim.y-th of its rows.
+struct MergeArgs {
+    PagedAttnArgs a;
+    int n_slots, rows;
+    float lse_offset;
+};
 template <typename T, int D>
-__global__ void __launch_bounds__(D) paged_merge_kernel(const __grid_constant__ SplitArgs args)
+__global__ void __launch_bounds__(D) paged_merge_kernel(const __grid_constant__ MergeArgs args)
 {
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;");
     const PagedAttnArgs &a = args.a;
     const skvq_paged_config &cfg = a.p.cfg;
-    const int slot = blockIdx.x, r = blockIdx.y, c = threadIdx.x;
+    const int slot = blockIdx.x, c = threadIdx.x, lane = threadIdx.x & 31;
     const int *desc = reinterpret_cast<const int *>(a.ws) + (size_t)slot * kDescInts;
     if (desc[0] == 0) return;
-    const int rep = cfg.n_q_heads / cfg.n_kv_heads, row = desc[4] * args.rows + r;
-    if (row >= desc[2] * rep) return;
-    const int n = desc[5], hk = desc[3];
+    const int rep = cfg.n_q_heads / cfg.n_kv_heads, n = desc[5], hk = desc[3];
     constexpr int PS = partial_stride(D);
-    const float *base = a.ws + (size_t)args.n_slots * kDescInts + ((size_t)slot * 2 * args.rows + r) * PS;
-    auto partial = [&](int k) { return base + (size_t)(2 * k + (k == 0 ? 1 : 0)) * args.rows * PS; };
-    // 32 partials at a time: every warp has their maxima and sums in its lanes, each thread walks its channel
-    const int lane = threadIdx.x & 31;
-    float m = -CUDART_INF_F, o = 0.f, l = 0.f;
-    for (int k0 = 0; k0 < n; k0 += 32) {
-        const bool have = k0 + lane < n;
-        const float pm = have ? partial(k0 + lane)[D] : -CUDART_INF_F, pl = have ? partial(k0 + lane)[D + 1] : 0.f;
-        float top = fmaxf(pm, m);
-#pragma unroll
-        for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-        if (top == -CUDART_INF_F) continue;
-        const float down = ex2_approx(m - top), f = ex2_approx(pm - top);
-        float sum = pl * f;
-#pragma unroll
-        for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-        l = fmaf(l, down, sum);
-        o *= down;
-        m = top;
-        const int last = min(32, n - k0);
-#pragma unroll 8
-        for (int k = 0; k < last; ++k) o = fmaf(partial(k0 + k)[c], __shfl_sync(0xffffffffu, f, k), o);
-    }
-    const int i = row / rep, head = hk * rep + row % rep;
     const int dst = a.p.c.reorder_v ? a.p.c.reorder_v[hk * D + c] & (D - 1) : c;
-    static_cast<T *>(a.out)[(int64_t)(desc[1] + i) * a.out_stride + head * D + dst] = Elem<T>::from_float(m == -CUDART_INF_F ? 0.f : o / l);
-    if (a.lse && c == 0)
-        a.lse[(int64_t)(desc[1] + i) * cfg.n_q_heads + head] = m == -CUDART_INF_F ? m : (m + log2f(l) - kPScaleLog2) * 0.6931471805599453f;
+    for (int r = blockIdx.y; r < args.rows; r += gridDim.y) {
+        const int row = desc[4] * args.rows + r;
+        if (row >= desc[2] * rep) return;
+        const float *base = a.ws + (size_t)args.n_slots * kDescInts + ((size_t)slot * 2 * args.rows + r) * PS;
+        auto partial = [&](int k) { return base + (size_t)(2 * k + (k == 0 ? 1 : 0)) * args.rows * PS; };
+        // 32 partials at a time: every warp has their maxima and sums in its lanes, each thread walks its channel
+        float m = -CUDART_INF_F, o = 0.f, l = 0.f;
+        for (int k0 = 0; k0 < n; k0 += 32) {
+            const bool have = k0 + lane < n;
+            const float pm = have ? partial(k0 + lane)[D] : -CUDART_INF_F, pl = have ? partial(k0 + lane)[D + 1] : 0.f;
+            float top = fmaxf(pm, m);
+#pragma unroll
+            for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+            if (top == -CUDART_INF_F) continue;
+            const float down = ex2_approx(m - top), f = ex2_approx(pm - top);
+            float sum = pl * f;
+#pragma unroll
+            for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+            l = fmaf(l, down, sum);
+            o *= down;
+            m = top;
+            const int last = min(32, n - k0);
+#pragma unroll 8
+            for (int k = 0; k < last; ++k) o = fmaf(partial(k0 + k)[c], __shfl_sync(0xffffffffu, f, k), o);
+        }
+        const int i = row / rep, head = hk * rep + row % rep;
+        static_cast<T *>(a.out)[(int64_t)(desc[1] + i) * a.out_stride + (int64_t)head * D + dst] = Elem<T>::from_float(m == -CUDART_INF_F ? 0.f : o / l);
+        if (a.lse && c == 0)
+            a.lse[(int64_t)(desc[1] + i) * cfg.n_q_heads + head] = m == -CUDART_INF_F ? m : (m + log2f(l) - args.lse_offset) * 0.6931471805599453f;
+    }
 }
 
-// Rows per item: 8, 16 or 32, by the most rows a KV head can have.
-int item_rows(const skvq_paged_config &cfg, const skvq_paged_batch &batch)
+// The most rows a KV head of this kernel can have, and the rows per item: 8, 16 or 32.
+long long few_rows(const skvq_paged_config &cfg, const skvq_paged_batch &batch)
 {
     const long long rows = (long long)batch.max_new * (cfg.n_q_heads / cfg.n_kv_heads);
+    return rows < kFewRows ? rows : kFewRows;
+}
+int item_rows(const skvq_paged_config &cfg, const skvq_paged_batch &batch)
+{
+    const long long rows = few_rows(cfg, batch);
     return rows <= 8 ? 8 : (rows <= 16 ? 16 : 32);
 }
 
 int split_slots(const skvq_paged_config &cfg, const skvq_paged_batch &batch, int n_splits)
 {
     const int per = item_rows(cfg, batch);
-    const long long rep = cfg.n_q_heads / cfg.n_kv_heads, m_tiles = (batch.max_new * rep + per - 1) / per;
+    const long long m_tiles = (few_rows(cfg, batch) + per - 1) / per;
     const long long lq = batch.max_len > cfg.window ? batch.max_len - cfg.window : 0;
     const long long cost = (lq + kTile - 1) / kTile + kRingCost * ((batch.max_len - lq + kRingTile - 1) / kRingTile) + 1;
     const long long items = (long long)batch.n_seqs * cfg.n_kv_heads * m_tiles;
@@ -808,36 +815,17 @@ int split_slots(const skvq_paged_config &cfg, const skvq_paged_batch &batch, int
     return slots < 1 ? 1 : (int)slots;
 }
 
-template <typename Kern, typename Args>
-cudaError_t launch_chained(Kern kern, dim3 grid, int threads, size_t smem, cudaStream_t stream, const Args &args)
-{
-    cudaLaunchConfig_t lc = {};
-    lc.gridDim = grid;
-    lc.blockDim = dim3(threads);
-    lc.dynamicSmemBytes = smem;
-    lc.stream = stream;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    lc.attrs = attr;
-    lc.numAttrs = 1;
-    const cudaError_t e = cudaLaunchKernelEx(&lc, kern, args);
-    if (e == cudaSuccess) count_launch();
-    return e;
-}
-
 template <typename T, int D, int NG, int NT>
 cudaError_t launch_split(const PagedAttnArgs &a, cudaStream_t stream)
 {
     using Geo = Geometry<D, NG, NT>;
-    const long long most = (long long)a.p.batch.max_new * (a.p.cfg.n_q_heads / a.p.cfg.n_kv_heads);      // rows of a KV head
     const SplitArgs s{a, split_slots(a.p.cfg, a.p.batch, a.n_splits), Geo::ROWS};
     static unsigned long long done = 0;
     cudaError_t e = configure_smem_once(paged_split_kernel<T, D, NG, NT>, Geo::SMEM + (int)sizeof(long long) * (kMaxPagedSeqs + 1), done);
     if (e != cudaSuccess) return e;
     e = launch_chained(paged_split_kernel<T, D, NG, NT>, dim3(s.n_slots), kSplitThreads, Geo::SMEM + sizeof(long long) * (a.p.batch.n_seqs + 1), stream, s);
     if (e != cudaSuccess) return e;
-    return launch_chained(paged_merge_kernel<T, D>, dim3(s.n_slots, (unsigned)(most < Geo::ROWS ? most : Geo::ROWS)), D, 0, stream, s);
+    return launch_paged_merge(a, s.n_slots, Geo::ROWS, (int)few_rows(a.p.cfg, a.p.batch), kPScaleLog2, stream);
 }
 
 template <typename T, int D, int NG> cudaError_t launch_by_rows(const PagedAttnArgs &a, cudaStream_t stream)
@@ -853,17 +841,46 @@ template <typename T> cudaError_t launch_by_shape(const PagedAttnArgs &a, cudaSt
     return a.p.ng == 1 ? launch_by_rows<T, 64, 1>(a, stream) : launch_by_rows<T, 64, 2>(a, stream);
 }
 
+size_t split_workspace_bytes(const skvq_paged_config &cfg, const skvq_paged_batch &batch, int n_splits)
+{
+    const size_t slots = split_slots(cfg, batch, n_splits);
+    return (slots * kDescInts * 4 + slots * 2 * item_rows(cfg, batch) * partial_stride(cfg.head_dim) * 4 + 15) / 16 * 16;
+}
+
+bool has_many_rows(const skvq_paged_config &cfg, const skvq_paged_batch &batch)
+{
+    return (long long)batch.max_new * (cfg.n_q_heads / cfg.n_kv_heads) > kFewRows;
+}
+
+template <typename T> cudaError_t merge_by_dim(const MergeArgs &m, int row_ctas, cudaStream_t stream)
+{
+    const dim3 grid(m.n_slots, row_ctas);
+    return m.a.p.cfg.head_dim == 128 ? launch_chained(paged_merge_kernel<T, 128>, grid, 128, 0, stream, m)
+                                     : launch_chained(paged_merge_kernel<T, 64>, grid, 64, 0, stream, m);
+}
+
 }  // namespace
+
+cudaError_t launch_paged_merge(const PagedAttnArgs &a, int n_slots, int rows, int row_ctas, float lse_offset, cudaStream_t stream)
+{
+    const MergeArgs m{a, n_slots, rows, lse_offset};
+    return a.p.cfg.dtype == SKVQ_F16 ? merge_by_dim<__half>(m, row_ctas, stream) : merge_by_dim<__nv_bfloat16>(m, row_ctas, stream);
+}
 
 size_t paged_workspace_bytes(const skvq_paged_config &cfg, const skvq_paged_batch &batch, int n_splits)
 {
-    const size_t slots = split_slots(cfg, batch, n_splits);
-    return slots * kDescInts * 4 + slots * 2 * item_rows(cfg, batch) * partial_stride(cfg.head_dim) * 4;
+    return split_workspace_bytes(cfg, batch, n_splits) + (has_many_rows(cfg, batch) ? prefill_workspace_bytes(cfg, batch) : 0);
 }
 
+// A step whose host bound allows many rows may still hold sequences with few: each kernel takes its own, by what the device arrays
+// say.
 cudaError_t launch_paged_attention(const PagedAttnArgs &a, cudaStream_t stream)
 {
-    return a.p.cfg.dtype == SKVQ_F16 ? launch_by_shape<__half>(a, stream) : launch_by_shape<__nv_bfloat16>(a, stream);
+    const cudaError_t e = a.p.cfg.dtype == SKVQ_F16 ? launch_by_shape<__half>(a, stream) : launch_by_shape<__nv_bfloat16>(a, stream);
+    if (e != cudaSuccess || !has_many_rows(a.p.cfg, a.p.batch)) return e;
+    PagedAttnArgs b = a;
+    b.ws = a.ws + split_workspace_bytes(a.p.cfg, a.p.batch, a.n_splits) / sizeof(float);
+    return launch_paged_prefill(b, stream);
 }
 
 }  // namespace skvq

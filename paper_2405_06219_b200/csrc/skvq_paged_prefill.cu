@@ -1,0 +1,745 @@
+// skvq_paged_attention for many query rows per (sequence, KV head): prompts and chunks of prompts, on tcgen05.
+//
+// One CTA per SM works on items of up to 256 packed rows (row = new token * (Hq/Hkv) + query head) of one KV head, as two row
+// blocks of 128, over 128-token tiles of the cache.  Four roles, ordered by mbarriers only:
+//   dequantizers  4 warps, a thread per token of the tile: codes and parameters come from the pages into registers one tile ahead,
+//                 leave as fp16(h c + z) (one rounding) in the 128-byte swizzle that both products read -- the key tile as the
+//                 K-major B operand of Q K^T, the value tile, same picture, as the MN-major B operand of P V; window tokens are
+//                 copied.  Two buffers of each.
+//   products      one thread issues S = Q K~^T (fp32 in tensor memory) and O += P V~ (P from tensor memory, in place of S).
+//   softmax       2 x 4 warps, a thread per row: S from tensor memory, probabilities back as fp16; the row sum in fp32.  The
+//                 reference of a row is raised, and O multiplied, only when a score exceeds it by more than 2^kLazy: O is
+//                 then read and written about once or twice per item.
+// While one block's scores become probabilities, the tensor core works for the other block.  Dequantizing costs about 450
+// instructions per thread and tile, shared by 256 rows; the exponentials (16 per clock and SM) and the products (2 x 1024 cycles
+// per tile and head dimension 128) bound the kernel about equally.
+//
+// A nibble pair (i, i + 4) of a code word becomes two neighbouring fp16, so the channels of each run of eight lie in the order
+// 0 4 1 5 2 6 3 7 in the operands; the queries are laid out the same way and the outputs put back.
+// Items are laid end to end, priced in tiles (causal limits included), and cut into equal runs, one per CTA; an item that several
+// runs share goes through the workspace to the merge kernel.
+#include <math_constants.h>
+
+#include "skvq_mma_common.cuh"
+#include "skvq_paged.cuh"
+#include "skvq_paged_split.cuh"
+#include "skvq_tcgen05.cuh"
+
+namespace skvq {
+namespace {
+
+using mmak::and_or;
+using mmak::ex2_approx;
+using mmak::mbar_init;
+using mmak::mbar_wait_bounded;
+using mmak::smem_u32;
+using namespace tc5;
+
+constexpr int kBlock = 128;                     // rows of a row block, tokens of a tile
+constexpr int kSoftmaxThreads = 2 * kBlock;     // warps 0-7
+constexpr int kDequantThreads = kBlock;         // warps 8-11
+constexpr int kPrefillThreads = kSoftmaxThreads + kDequantThreads + 32;      // warp 12 issues the products
+constexpr float kLazy = 8.f;                    // log2 of how far a score may exceed its row's reference
+constexpr float kPOffset = 6.f;                 // probabilities are held times 2^6: up to 2^14 in fp16, down to 2^-30 of the reference
+
+struct PrefillArgs {
+    PagedAttnArgs a;
+    int n_slots;
+};
+
+template <int D>
+struct PGeo {
+    static constexpr int HALVES = D / 64;                      // 64-channel halves of an operand tile: 128-byte rows
+    static constexpr int HALF_BYTES = kBlock * 128;
+    static constexpr int TILE_BYTES = HALVES * HALF_BYTES;      // one 128 x D fp16 operand
+    static constexpr int Q = 0;                                // 2 row blocks; at the end of an item its output rows
+    static constexpr int K = 2 * TILE_BYTES;                   // 2 buffers
+    static constexpr int V = 4 * TILE_BYTES;                   // 2 buffers
+    static constexpr int GATHER = 6 * TILE_BYTES;              // per softmax warp: two raw rows
+    static constexpr int SMEM = GATHER + 8 * 2 * D * 2 + 1024;  // and room to align to 1024 bytes
+    static constexpr int TMEM_S = 0, TMEM_O = 256;             // columns: S (P in place) 2 x 128, O 2 x D
+};
+
+// Shared-memory matrix descriptors in the 128-byte swizzle.  K-major: 8-row groups 1024 bytes apart.  MN-major: 64-element runs of
+// the MN dimension `mn_stride` bytes apart, groups of 8 along K 1024 bytes apart.
+__device__ __forceinline__ uint64_t desc_k_major(uint32_t addr)
+{
+    return (uint64_t)((addr >> 4) & 0x3FFFu) | ((uint64_t)1 << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
+}
+__device__ __forceinline__ uint64_t desc_mn_major(uint32_t addr, uint32_t mn_stride)
+{
+    return (uint64_t)((addr >> 4) & 0x3FFFu) | ((uint64_t)(mn_stride >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
+}
+// D (tensor memory) = A (tensor memory, fp16 pairs along the columns) B + D
+__device__ __forceinline__ void umma_f16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
+                 " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}"
+                 ::"r"(d_tmem), "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t (&r)[32])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,"
+                 "%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};"
+                 ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+                 "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
+                 "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
+                 "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]) : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t (&r)[16])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
+                 ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+                 "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
+}
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// Waits for this thread's tensor-memory loads; the registers that were in flight pass through the statement.
+__device__ __forceinline__ void tmem_wait_ld32(float (&r)[32])
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+f"(r[0]), "+f"(r[1]), "+f"(r[2]), "+f"(r[3]), "+f"(r[4]), "+f"(r[5]), "+f"(r[6]), "+f"(r[7]),
+                   "+f"(r[8]), "+f"(r[9]), "+f"(r[10]), "+f"(r[11]), "+f"(r[12]), "+f"(r[13]), "+f"(r[14]), "+f"(r[15]),
+                   "+f"(r[16]), "+f"(r[17]), "+f"(r[18]), "+f"(r[19]), "+f"(r[20]), "+f"(r[21]), "+f"(r[22]), "+f"(r[23]),
+                   "+f"(r[24]), "+f"(r[25]), "+f"(r[26]), "+f"(r[27]), "+f"(r[28]), "+f"(r[29]), "+f"(r[30]), "+f"(r[31])
+                 :: "memory");
+}
+__device__ __forceinline__ void mbar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
+__device__ __forceinline__ uint32_t h2(float lo, float hi)
+{
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+__device__ __forceinline__ uint32_t h2_sub(uint32_t a, uint32_t b)
+{
+    uint32_t r;
+    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+__device__ __forceinline__ uint32_t h2_fma(uint32_t a, uint32_t b, uint32_t c)
+{
+    uint32_t r;
+    asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
+    return r;
+}
+template <typename T> __device__ __forceinline__ uint32_t to_h2(uint32_t v);      // see as_h2 of the kernel for few rows
+template <> __device__ __forceinline__ uint32_t to_h2<__half>(uint32_t v) { return v; }
+template <> __device__ __forceinline__ uint32_t to_h2<__nv_bfloat16>(uint32_t v) { return h2(__uint_as_float(v << 16), __uint_as_float(v & 0xFFFF0000u)); }
+
+// Position 0..7 inside a run of eight operand channels -> stored channel.
+__device__ __forceinline__ int channel_at(int pos) { return (pos >> 1) + 4 * (pos & 1); }
+
+// The items of one sequence: per KV head, blocks of 256 rows; tiles that block m looks at.
+struct PItems {
+    int rep, n, len, lq, causal, tiles_c;
+    __device__ __forceinline__ void set(const PrefillArgs &a, const PagedSeq &s)
+    {
+        rep = a.a.p.cfg.n_q_heads / a.a.p.cfg.n_kv_heads;
+        n = s.n;
+        len = s.len;
+        lq = max(s.len - a.a.p.cfg.window, 0);
+        causal = a.a.causal;
+        tiles_c = (lq + kBlock - 1) / kBlock;
+    }
+    __device__ __forceinline__ int rows() const { return n * rep; }
+    __device__ __forceinline__ int blocks() const { return rows() > kFewRows ? (rows() + 2 * kBlock - 1) / (2 * kBlock) : 0; }      // the others are the other kernel's
+    __device__ __forceinline__ int limit(int row) const { return causal ? min(len, len - n + row / rep + 1) : len; }      // tokens below it are seen
+    __device__ __forceinline__ int tiles(int m) const
+    {
+        const int lim = limit(min((m + 1) * 2 * kBlock, rows()) - 1);
+        if (lim <= 0) return 0;
+        return lim <= lq ? (lim + kBlock - 1) / kBlock : tiles_c + (lim - lq + kBlock - 1) / kBlock;
+    }
+    __device__ __forceinline__ int cost(int m) const { return max(tiles(m), 1); }
+};
+
+// What a CTA works on next: block m of KV head hk of sequence b, tiles [t0, t1) of `total`.
+struct PSegment {
+    int b, hk, m, t0, t1, total;
+    long long item_end;      // end of the item on the common axis
+    PagedSeq seq;
+    PItems it;
+};
+
+// Every role walks the same segments.
+struct PWalk {
+    long long f, f1;
+    int b;
+    __device__ __forceinline__ bool next(const PrefillArgs &a, const long long *pre, PSegment &s)
+    {
+        if (f >= f1) return false;
+        while (pre[b + 1] <= f) ++b;
+        s.b = b;
+        paged_sequence(a.a.p, b, false, s.seq);
+        s.it.set(a, s.seq);
+        const long long per_head = (pre[b + 1] - pre[b]) / a.a.p.cfg.n_kv_heads;
+        long long at = f - pre[b];
+        s.hk = (int)(at / per_head);
+        at -= s.hk * per_head;
+        s.m = 0;
+        int c = s.it.cost(0);
+        while (at >= c) { at -= c; c = s.it.cost(++s.m); }
+        const int take = (int)min((long long)(c - at), f1 - f);
+        s.total = s.it.tiles(s.m);
+        s.t0 = (int)at;
+        s.t1 = min((int)at + take, s.total);
+        s.item_end = f - at + c;
+        f += take;
+        return true;
+    }
+};
+
+template <typename T, int D, int NG>
+__global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const __grid_constant__ PrefillArgs args)
+{
+    using Geo = PGeo<D>;
+    const PagedAttnArgs &a = args.a;
+    const PagedArgs &p = a.p;
+    const skvq_paged_config &cfg = p.cfg;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+    long long *pre = reinterpret_cast<long long *>(smem + Geo::SMEM - 1024);
+    __shared__ __align__(8) uint64_t bars[16];
+    __shared__ uint32_t tmem_sh;
+    __shared__ int fail_sh;
+    __shared__ long long scan_sh[16];
+    __shared__ float row_scale[2 * kBlock];
+    __shared__ uint16_t out_channel[2][D];      // source channel of every operand column, per row block
+    __shared__ uint32_t bad_sh[4];              // of the last four tiles: 16-token blocks without a page (a tile's is read until its
+                                                // probabilities are written, when the tile two further on may be in the making)
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, B = p.batch.n_seqs;
+
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;");
+
+    // ---- the flat partition
+    {
+        long long carry = 0;
+        for (int base = 0; base < B; base += kPrefillThreads) {
+            const int b = base + tid;
+            long long c = 0;
+            if (b < B) {
+                PagedSeq s;
+                if (paged_sequence(p, b, false, s)) {
+                    PItems it;
+                    it.set(args, s);
+                    const int blocks = it.blocks();
+                    for (int m = 0; m < blocks; ++m) c += it.cost(m);
+                    c *= cfg.n_kv_heads;
+                }      // the kernel for few rows reports the others
+            }
+            long long incl = c;
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const long long v = __shfl_up_sync(0xffffffffu, incl, d);
+                if (lane >= d) incl += v;
+            }
+            if (lane == 31) scan_sh[warp] = incl;
+            __syncthreads();
+            long long before = carry;
+            for (int w = 0; w < kPrefillThreads / 32; ++w) {
+                if (w < warp) before += scan_sh[w];
+                carry += scan_sh[w];
+            }
+            if (b < B) pre[b] = before + incl - c;
+            __syncthreads();
+        }
+        if (tid == 0) pre[B] = carry;
+    }
+    // ---- barriers, tensor memory
+    const uint32_t bar0 = smem_u32(bars);
+    const uint32_t k_full = bar0, k_empty = bar0 + 16, v_full = bar0 + 32, v_empty = bar0 + 48;      // + 8 * buffer
+    const uint32_t s_full = bar0 + 64, p_full = bar0 + 80, pv_done = bar0 + 96, q_full = bar0 + 112;  // + 8 * row block
+    if (tid == 0) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(k_full + 8 * i, kDequantThreads);
+            mbar_init(k_empty + 8 * i, 1);
+            mbar_init(v_full + 8 * i, kDequantThreads);
+            mbar_init(v_empty + 8 * i, 1);
+            mbar_init(s_full + 8 * i, 1);
+            mbar_init(p_full + 8 * i, kBlock);
+            mbar_init(pv_done + 8 * i, 1);
+            mbar_init(q_full + 8 * i, kBlock);
+        }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        fail_sh = 0;
+    }
+    if (warp == kPrefillThreads / 32 - 1) tmem_alloc(smem_u32(&tmem_sh), 512);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = tmem_sh;
+    const long long total = pre[B], ups = max((total + args.n_slots - 1) / args.n_slots, 1LL);
+    PWalk walk;
+    walk.f = blockIdx.x * ups;
+    walk.f1 = min(walk.f + ups, total);
+    walk.b = 0;
+    int *desc = reinterpret_cast<int *>(a.ws) + (size_t)blockIdx.x * kDescInts;
+    if (tid == 0) desc[0] = 0;
+    if (walk.f < walk.f1) {
+        int lo = 0, hi = B - 1;
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (pre[mid] <= walk.f) lo = mid; else hi = mid - 1;
+        }
+        walk.b = lo;
+    }
+    // A wait that runs out is reported; the thread then goes through its loops without waiting or storing.
+    bool alive = true;
+    volatile int *fail = &fail_sh;
+    auto wait = [&](uint32_t bar, uint32_t parity) {
+        if (alive && !mbar_wait_bounded(bar, parity)) {
+            alive = false;
+            *fail = 1;
+            set_status(p.c.status, SKVQ_STATUS_COPY_TIMEOUT);
+        }
+    };
+    PSegment s;
+
+    if (warp >= 8 && warp < 12) {
+        // ================================================================ dequantizers
+        const int row = tid - kSoftmaxThreads;      // token of the tile
+        const int P = cfg.page_tokens, page_shift = __ffs(P) - 1;
+        constexpr int PIECES = D / 32;              // 16-byte pieces of a code row
+        uint32_t n = 0;                             // tiles so far
+        while (walk.next(args, pre, s)) {
+            const int32_t *table = p.batch.page_table + (int64_t)s.b * p.batch.max_pages;
+            const int64_t win_row0 = ((int64_t)s.seq.slot * cfg.n_kv_heads + s.hk) * cfg.ring_tokens;
+            uint4 kc[PIECES], vc[PIECES];
+            uint32_t km[NG], vm[NG];
+            int page = -1;
+            // the page of this thread's token in tile t; -1: no such token, -2: no such page
+            auto page_of = [&](int t) {
+                const int tok = t * kBlock + row;
+                if (t >= min(s.t1, s.it.tiles_c) || tok >= s.it.lq) return -1;
+                const int id = table[tok >> page_shift];
+                if (id < 0 || id >= cfg.n_pages) { set_status(p.c.status, SKVQ_STATUS_BAD_PAGE); return -2; }
+                return id;
+            };
+            auto load_codes = [&](int t) {      // of tile t, with `page`
+                if (page >= 0) {
+                    const int64_t at = ((int64_t)page * cfg.n_kv_heads + s.hk) * P + ((t * kBlock + row) & (P - 1));
+#pragma unroll
+                    for (int i = 0; i < PIECES; ++i) {
+                        kc[i] = reinterpret_cast<const uint4 *>(static_cast<const uint8_t *>(p.c.k_codes) + at * (D / 2))[i];
+                        vc[i] = reinterpret_cast<const uint4 *>(static_cast<const uint8_t *>(p.c.v_codes) + at * (D / 2))[i];
+                    }
+#pragma unroll
+                    for (int g = 0; g < NG; ++g) {
+                        km[g] = static_cast<const uint32_t *>(p.c.k_meta)[at * NG + g];
+                        vm[g] = static_cast<const uint32_t *>(p.c.v_meta)[at * NG + g];
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < PIECES; ++i) kc[i] = vc[i] = make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+                    for (int g = 0; g < NG; ++g) km[g] = vm[g] = 0u;      // rows that hold nothing become zeros
+                }
+            };
+            page = page_of(s.t0);
+            load_codes(s.t0);
+            int page_next = page_of(s.t0 + 1);
+            for (int t = s.t0; t < s.t1; ++t, ++n) {
+                const uint32_t buf = n & 1, phase = (n >> 1) & 1;
+                if (*fail) alive = false;
+                uint8_t *kt = smem + Geo::K + buf * Geo::TILE_BYTES + row * 128, *vt = smem + Geo::V + buf * Geo::TILE_BYTES + row * 128;
+                // one code word -> one 16-byte piece of the operand row
+                auto piece = [&](uint8_t *base, int c8, uint32_t w, uint32_t hh, uint32_t zz) {
+                    constexpr uint32_t M = 0x64006400u, SIXTEENTH = 0x2C002C00u, MINUS64 = 0xD400D400u;
+                    const uint32_t u = w >> 8;
+                    uint4 r;
+                    r.x = h2_fma(h2_sub(and_or(w, 0x000F000Fu, M), M), hh, zz);
+                    r.y = h2_fma(h2_fma(and_or(w, 0x00F000F0u, M), SIXTEENTH, MINUS64), hh, zz);
+                    r.z = h2_fma(h2_sub(and_or(u, 0x000F000Fu, M), M), hh, zz);
+                    r.w = h2_fma(h2_fma(and_or(u, 0x00F000F0u, M), SIXTEENTH, MINUS64), hh, zz);
+                    *reinterpret_cast<uint4 *>(base + (c8 >> 3) * Geo::HALF_BYTES + (((c8 & 7) ^ (row & 7)) << 4)) = r;
+                };
+                auto expand = [&](uint8_t *base, const uint4 (&c)[PIECES], const uint32_t (&m)[NG]) {
+#pragma unroll
+                    for (int i = 0; i < PIECES; ++i) {      // 32 channels
+                        const uint32_t hz = m[i * NG / PIECES], hh = __byte_perm(hz, hz, 0x1010), zz = __byte_perm(hz, hz, 0x3232);
+                        piece(base, 4 * i, c[i].x, hh, zz);
+                        piece(base, 4 * i + 1, c[i].y, hh, zz);
+                        piece(base, 4 * i + 2, c[i].z, hh, zz);
+                        piece(base, 4 * i + 3, c[i].w, hh, zz);
+                    }
+                };
+                auto copy_row = [&](uint8_t *base, const void *pool, bool have, int64_t r) {
+#pragma unroll 4
+                    for (int i = 0; i < D / 8; ++i) {
+                        uint4 x = make_uint4(0u, 0u, 0u, 0u);
+                        if (have) x = reinterpret_cast<const uint4 *>(static_cast<const T *>(pool) + r * D)[i];
+                        x.x = to_h2<T>(x.x); x.y = to_h2<T>(x.y); x.z = to_h2<T>(x.z); x.w = to_h2<T>(x.w);
+                        *reinterpret_cast<uint4 *>(base + (i >> 3) * Geo::HALF_BYTES + (((i & 7) ^ (row & 7)) << 4)) =
+                            make_uint4(__byte_perm(x.x, x.z, 0x5410), __byte_perm(x.x, x.z, 0x7632), __byte_perm(x.y, x.w, 0x5410), __byte_perm(x.y, x.w, 0x7632));
+                    }
+                };
+                const bool quantized = t < s.it.tiles_c;
+                const int tok = s.it.lq + (t - s.it.tiles_c) * kBlock + row;      // of a window tile
+                const bool have = !quantized && tok < s.seq.len;
+                const int64_t r = have ? win_row0 + tok % cfg.ring_tokens : 0;
+                if (n >= 2) wait(k_empty + 8 * buf, phase ^ 1u);
+                {
+                    const uint32_t gone = __ballot_sync(0xffffffffu, page == -2);
+                    if (lane == 0) {      // this warp's two 16-token blocks
+                        const uint32_t two = (gone & 0xFFFFu ? 1u : 0u) | (gone >> 16 ? 2u : 0u);
+                        reinterpret_cast<uint8_t *>(&bad_sh[n & 3])[warp - 8] = (uint8_t)(quantized ? two : 0u);
+                    }
+                }
+                if (alive) {
+                    if (quantized) expand(kt, kc, km);
+                    else copy_row(kt, p.c.k_win, have, r);
+                }
+                proxy_fence();
+                mbar_arrive(k_full + 8 * buf);
+                if (n >= 2) wait(v_empty + 8 * buf, phase ^ 1u);
+                if (alive) {
+                    if (quantized) expand(vt, vc, vm);
+                    else copy_row(vt, p.c.v_win, have, r);
+                }
+                page = page_next;
+                load_codes(t + 1);      // in flight until the next tile's buffer is free
+                page_next = page_of(t + 2);
+                proxy_fence();
+                mbar_arrive(v_full + 8 * buf);
+            }
+        }
+    } else if (warp == 12) {
+        // ================================================================ products
+        if (lane == 0) {
+            constexpr uint32_t kIdescS = idesc_f16_f32(kBlock, kBlock);
+            constexpr uint32_t kIdescO = idesc_f16_f32(kBlock, D) | (1u << 16);      // B is MN-major
+            const uint32_t base = smem_u32(smem);
+            uint32_t n = 0, nq[2] = {0, 0}, np[2] = {0, 0};      // tiles so far; queries and probabilities taken, per row block
+            while (walk.next(args, pre, s)) {
+                const int rows = s.it.rows() - s.m * 2 * kBlock, blocks = rows > kBlock ? 2 : 1;
+                if (s.t0 >= s.t1) continue;      // nothing to see: the softmax warps write zeros on their own
+                auto scores = [&](int i, uint32_t buf) {
+#pragma unroll
+                    for (int ks = 0; ks < D / 16; ++ks)
+                        umma_f16(tmem + Geo::TMEM_S + i * kBlock, desc_k_major(base + Geo::Q + i * Geo::TILE_BYTES + (ks >> 2) * Geo::HALF_BYTES + (ks & 3) * 32),
+                                 desc_k_major(base + Geo::K + buf * Geo::TILE_BYTES + (ks >> 2) * Geo::HALF_BYTES + (ks & 3) * 32), kIdescS, ks > 0);
+                    umma_commit(s_full + 8 * i);
+                };
+                for (int i = 0; i < blocks; ++i) { wait(q_full + 8 * i, nq[i] & 1); ++nq[i]; }
+                wait(k_full + 8 * (n & 1), (n >> 1) & 1);
+                tc_fence_after();
+                for (int i = 0; i < blocks; ++i) scores(i, n & 1);
+                umma_commit(k_empty + 8 * (n & 1));
+                for (int t = s.t0; t < s.t1; ++t, ++n) {
+                    if (*fail) alive = false;
+                    const uint32_t buf = n & 1, next = buf ^ 1;
+                    const bool more = t + 1 < s.t1;
+                    wait(v_full + 8 * buf, (n >> 1) & 1);
+                    for (int i = 0; i < blocks; ++i) {
+                        wait(p_full + 8 * i, np[i] & 1);
+                        ++np[i];
+                        tc_fence_after();
+#pragma unroll
+                        for (int ks = 0; ks < kBlock / 16; ++ks)
+                            umma_f16_ts(tmem + Geo::TMEM_O + i * D, tmem + Geo::TMEM_S + i * kBlock + ks * 8,
+                                        desc_mn_major(base + Geo::V + buf * Geo::TILE_BYTES + ks * 2048, Geo::HALF_BYTES), kIdescO, t > s.t0 || ks > 0);
+                        umma_commit(pv_done + 8 * i);
+                        if (more) {
+                            if (i == 0) {
+                                wait(k_full + 8 * next, ((n + 1) >> 1) & 1);
+                                tc_fence_after();
+                            }
+                            scores(i, next);
+                        }
+                    }
+                    umma_commit(v_empty + 8 * buf);
+                    if (more) umma_commit(k_empty + 8 * next);
+                }
+            }
+        }
+        __syncwarp();
+    } else {
+        // ================================================================ softmax
+        const int blk = warp >> 2, row = tid & (kBlock - 1);                       // row block, row = lane of the tensor memory
+        const uint32_t quad = (uint32_t)((warp & 3) * 32) << 16;
+        const uint32_t s_addr = tmem + Geo::TMEM_S + blk * kBlock + quad, o_addr = tmem + Geo::TMEM_O + blk * D + quad;
+        const float sign = a.sm_scale < 0.f ? -1.f : (a.sm_scale == 0.f ? 0.f : 1.f);
+        uint8_t *q_tile = smem + Geo::Q + blk * Geo::TILE_BYTES;
+        T *raw = reinterpret_cast<T *>(smem + Geo::GATHER) + warp * 2 * D;
+        uint32_t n = 0, ns = 0;      // tiles so far (both blocks'), score tiles of this block so far
+        while (walk.next(args, pre, s)) {
+            const int rows = min(s.it.rows() - (s.m * 2 + blk) * kBlock, kBlock);      // of this block; may be <= 0
+            const int row_base = (s.m * 2 + blk) * kBlock;
+            const bool whole = s.t0 == 0 && s.t1 == s.total;
+            const bool work = s.t0 < s.t1 && rows > 0;
+            if (*fail) alive = false;
+            if (work) {
+                asm volatile("bar.sync %0, 128;" ::"r"(1 + blk) : "memory");      // every warp has sent off its rows of the item before
+                // ---- queries of the block: a warp per row; lane: operand positions C lane .. C lane + C - 1
+                constexpr int C = D / 32;
+                struct alignas(sizeof(T) * C) Piece { T v[C]; };
+                int from[C];
+#pragma unroll
+                for (int k = 0; k < C; ++k) {
+                    const int pos = lane * C + k, c = (pos & ~7) + channel_at(pos & 7);
+                    from[k] = p.c.reorder_k ? p.c.reorder_k[s.hk * D + c] & (D - 1) : c;
+                }
+                for (int c = row; c < D; c += kBlock) {
+                    const int st = (c & ~7) + channel_at(c & 7);
+                    out_channel[blk][c] = (uint16_t)(p.c.reorder_v ? p.c.reorder_v[s.hk * D + st] & (D - 1) : st);
+                }
+                const float2 *rope = static_cast<const float2 *>(p.rope.table);
+                const int half = p.rope.rot_dim / 2;
+#pragma unroll 2
+                for (int k = 0; k < 32; ++k) {
+                    const int r = (warp & 3) * 32 + k;
+                    float x[C], mx = 0.f;
+#pragma unroll
+                    for (int e = 0; e < C; ++e) x[e] = 0.f;
+                    if (r < rows && sign != 0.f) {
+                        const int i = (row_base + r) / s.it.rep, head = s.hk * s.it.rep + (row_base + r) % s.it.rep, pos = s.seq.len - s.seq.n + i;
+                        const T *src = static_cast<const T *>(a.q) + (int64_t)(s.seq.row0 + i) * a.q_stride + (int64_t)head * D;
+                        Piece own = *reinterpret_cast<const Piece *>(src + lane * C);
+                        T *buf = raw + (k & 1) * D;
+                        if (rope && pos >= 0) {
+                            *reinterpret_cast<Piece *>(buf + lane * C) = own;
+                            __syncwarp();
+#pragma unroll
+                            for (int e = 0; e < C; ++e) {
+                                const int c = lane * C + e;
+                                if (c < p.rope.rot_dim) {
+                                    const bool second = p.rope.interleaved ? c & 1 : c >= half;
+                                    const int pair = p.rope.interleaved ? c >> 1 : (second ? c - half : c);
+                                    const int partner = p.rope.interleaved ? c ^ 1 : (second ? c - half : c + half);
+                                    const float2 cs = rope[(int64_t)pos * half + pair];
+                                    const float mine = Elem<T>::to_float(own.v[e]), other = Elem<T>::to_float(buf[partner]);
+                                    own.v[e] = Elem<T>::from_float(second ? rotate_second(other, mine, cs.x, cs.y) : rotate_first(mine, other, cs.x, cs.y));
+                                }
+                            }
+                            __syncwarp();
+                        }
+                        *reinterpret_cast<Piece *>(buf + lane * C) = own;
+                        __syncwarp();
+#pragma unroll
+                        for (int e = 0; e < C; ++e) { x[e] = Elem<T>::to_float(buf[from[e]]); mx = fmaxf(mx, fabsf(x[e])); }
+                        __syncwarp();
+                    }
+                    mx = mmak::warp_max(mx);
+                    float up = 1.f;      // the row's largest to [2^4, 2^5): exact, and far from fp16's ends whatever the type's range
+                    if (mx > 0.f && mx < CUDART_INF_F) up = __int_as_float((127 + min(4 - (__float_as_int(mx) >> 23) + 127, 60)) << 23);
+                    if (lane == 0) row_scale[blk * kBlock + r] = (sign == 0.f ? 1.f : fabsf(a.sm_scale)) * 1.4426950408889634f / up;
+                    uint8_t *dst = q_tile + r * 128 + ((lane * C) >> 6) * Geo::HALF_BYTES + ((((lane * C) >> 3 & 7) ^ (r & 7)) << 4) + ((lane * C) & 7) * 2;
+                    const float f = up * sign;
+                    if constexpr (C == 4) *reinterpret_cast<uint2 *>(dst) = make_uint2(h2(x[0] * f, x[1] * f), h2(x[2] * f, x[3] * f));
+                    else *reinterpret_cast<uint32_t *>(dst) = h2(x[0] * f, x[1] * f);
+                }
+                proxy_fence();
+                mbar_arrive(q_full + 8 * blk);
+                asm volatile("bar.sync %0, 128;" ::"r"(1 + blk) : "memory");      // row_scale and out_channel of the whole block
+            }
+            const float rs = work ? row_scale[blk * kBlock + row] : 1.f;
+            const int lim = s.it.limit(row_base + min(row, max(rows, 1) - 1));
+            float ref = -CUDART_INF_F, l = 0.f;      // reference (unscaled score), sum of probabilities
+            for (int t = s.t0; t < s.t1; ++t, ++n) {
+                if (!work) continue;
+                if (*fail) alive = false;
+                wait(s_full + 8 * blk, ns & 1);
+                tc_fence_after();
+                const bool quantized = t < s.it.tiles_c;
+                const int tok0 = quantized ? t * kBlock : s.it.lq + (t - s.it.tiles_c) * kBlock;
+                const uint32_t bad = quantized ? bad_sh[n & 3] : 0u;      // two bits in each byte
+                const int seen = min(min(lim, quantized ? s.it.lq : s.seq.len) - tok0, kBlock);      // columns below it are seen
+                const bool edge = __any_sync(0xffffffffu, seen < kBlock || bad != 0u);
+                auto hidden = [&](int c) { return c >= seen || ((bad >> (8 * (c >> 5) + ((c >> 4) & 1))) & 1u); };
+                // ---- the row's maximum
+                float mx = -CUDART_INF_F;
+                {
+                    float x[32], y[32];
+#pragma unroll
+                    for (int c0 = 0; c0 < kBlock; c0 += 64) {
+                        tmem_ld32(s_addr + c0, x);
+                        tmem_ld32(s_addr + c0 + 32, y);
+                        tmem_wait_ld32(x);
+                        tmem_wait_ld32(y);
+                        if (edge) {
+#pragma unroll
+                            for (int c = 0; c < 32; ++c) {
+                                if (hidden(c0 + c)) x[c] = -CUDART_INF_F;
+                                if (hidden(c0 + 32 + c)) y[c] = -CUDART_INF_F;
+                            }
+                        }
+                        float m0 = fmaxf(x[0], y[0]), m1 = fmaxf(x[1], y[1]);
+#pragma unroll
+                        for (int c = 2; c < 32; c += 2) {
+                            m0 = fmaxf(fmaxf(m0, x[c]), y[c]);
+                            m1 = fmaxf(fmaxf(m1, x[c + 1]), y[c + 1]);
+                        }
+                        mx = fmaxf(mx, fmaxf(m0, m1));
+                    }
+                }
+                // ---- raise the reference: at first, then only when a score exceeds it by 2^kLazy
+                if (t > s.t0 && __any_sync(0xffffffffu, (mx - ref) * rs > kLazy)) {
+                    float down = 1.f;
+                    if (mx > ref) {
+                        down = ref == -CUDART_INF_F ? 0.f : ex2_approx((ref - mx) * rs);
+                        ref = mx;
+                    }
+                    l *= down;
+                    wait(pv_done + 8 * blk, (ns - 1) & 1);      // the products of the tile before have landed in O
+                    tc_fence_after();
+#pragma unroll 1
+                    for (int c0 = 0; c0 < D; c0 += 32) {
+                        float x[32];
+                        tmem_ld32(o_addr + c0, x);
+                        tmem_wait_ld32(x);
+                        uint32_t w[32];
+#pragma unroll
+                        for (int c = 0; c < 32; ++c) w[c] = __float_as_uint(x[c] * down);
+                        tmem_st32(o_addr + c0, w);
+                    }
+                } else if (t == s.t0) {
+                    ref = mx;
+                }
+                // ---- probabilities, in place of the scores
+                const float base = kPOffset - (ref == -CUDART_INF_F ? 0.f : ref * rs);
+#pragma unroll
+                for (int c0 = 0; c0 < kBlock; c0 += 32) {
+                    float x[32];
+                    tmem_ld32(s_addr + c0, x);
+                    tmem_wait_ld32(x);
+                    uint32_t w[16];
+                    float l0 = 0.f, l1 = 0.f;
+#pragma unroll
+                    for (int c = 0; c < 32; c += 2) {
+                        float e0 = ex2_approx(fmaf(x[c], rs, base)), e1 = ex2_approx(fmaf(x[c + 1], rs, base));
+                        if (edge) {
+                            if (hidden(c0 + c)) e0 = 0.f;
+                            if (hidden(c0 + c + 1)) e1 = 0.f;
+                        }
+                        l0 += e0;
+                        l1 += e1;
+                        w[c >> 1] = h2(e0, e1);
+                    }
+                    l += l0 + l1;
+                    tmem_st16(s_addr + c0 / 2, w);
+                }
+                tmem_wait_st();
+                tc_fence_before();
+                mbar_arrive(p_full + 8 * blk);
+                ++ns;
+            }
+            if (rows <= 0) continue;
+            // ---- the block's result
+            if (work) {
+                wait(pv_done + 8 * blk, (ns - 1) & 1);
+                tc_fence_after();
+            }
+            const int i = (row_base + row) / s.it.rep, head = s.hk * s.it.rep + (row_base + row) % s.it.rep;
+            if (whole) {
+                const float inv = ref == -CUDART_INF_F ? 0.f : 1.f / l;
+                T *rows_out = reinterpret_cast<T *>(q_tile);      // [128][D], 16-byte pieces of a row at piece ^ (row & 7); all products have been read
+#pragma unroll 1
+                for (int c0 = 0; c0 < D; c0 += 32) {
+                    float x[32];
+                    if (work) {
+                        tmem_ld32(o_addr + c0, x);
+                        tmem_wait_ld32(x);
+                    }
+#pragma unroll
+                    for (int c = 0; c < 32; ++c) {
+                        const int dst = work ? out_channel[blk][c0 + c] : c0 + c;
+                        rows_out[row * D + ((((dst >> 3) ^ (row & 7))) << 3) + (dst & 7)] = Elem<T>::from_float(work && ref != -CUDART_INF_F ? x[c] * inv : 0.f);
+                    }
+                }
+                if (a.lse && row < rows && alive)
+                    a.lse[(int64_t)(s.seq.row0 + i) * cfg.n_q_heads + head] = ref == -CUDART_INF_F ? ref : (ref * rs + log2f(l) - kPOffset) * 0.6931471805599453f;
+                __syncwarp();
+                constexpr int PER_ROW = D / 8;
+                for (int e = lane; e < 32 * PER_ROW; e += 32) {      // this warp's 32 rows, 16 bytes a lane
+                    const int r = (warp & 3) * 32 + e / PER_ROW, c8 = e % PER_ROW;
+                    if (r < rows && alive) {
+                        const int ri = (row_base + r) / s.it.rep, rh = s.hk * s.it.rep + (row_base + r) % s.it.rep;
+                        *reinterpret_cast<uint4 *>(static_cast<T *>(a.out) + (int64_t)(s.seq.row0 + ri) * a.out_stride + (int64_t)rh * D + c8 * 8) =
+                            *reinterpret_cast<const uint4 *>(rows_out + r * D + ((c8 ^ (r & 7)) << 3));
+                    }
+                }
+                __syncwarp();
+            } else if (alive) {
+                // a share of an item: unscaled sums, stored channels in order
+                float *part = a.ws + (size_t)args.n_slots * kDescInts +
+                              (((size_t)blockIdx.x * 2 + (s.t0 == 0 ? 1 : 0)) * 2 * kBlock + blk * kBlock + row) * partial_stride(D);
+#pragma unroll 1
+                for (int c0 = 0; c0 < D; c0 += 32) {
+                    float x[32];
+                    if (work) {
+                        tmem_ld32(o_addr + c0, x);
+                        tmem_wait_ld32(x);
+                    }
+                    if (row < rows) {
+#pragma unroll
+                        for (int c = 0; c < 32; c += 8) {
+                            const bool some = work && ref != -CUDART_INF_F;
+                            *reinterpret_cast<float4 *>(part + c0 + c) = some ? make_float4(x[c], x[c + 2], x[c + 4], x[c + 6]) : make_float4(0.f, 0.f, 0.f, 0.f);
+                            *reinterpret_cast<float4 *>(part + c0 + c + 4) = some ? make_float4(x[c + 1], x[c + 3], x[c + 5], x[c + 7]) : make_float4(0.f, 0.f, 0.f, 0.f);
+                        }
+                    }
+                }
+                if (row < rows) {
+                    part[D] = ref == -CUDART_INF_F ? ref : ref * rs;
+                    part[D + 1] = l;
+                }
+                if (s.t0 == 0 && blk == 0 && row == 0) {
+                    desc[1] = s.seq.row0; desc[2] = s.seq.n; desc[3] = s.hk; desc[4] = s.m;
+                    desc[5] = (int)((s.item_end - 1) / ups - blockIdx.x + 1);
+                    desc[0] = 1;
+                }
+            }
+            tc_fence_before();
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == 12) tmem_dealloc(tmem, 512);
+}
+
+int prefill_slots(const skvq_paged_config &cfg, const skvq_paged_batch &batch)
+{
+    const long long rows = (long long)batch.max_new * (cfg.n_q_heads / cfg.n_kv_heads);
+    const long long items = (long long)batch.n_seqs * cfg.n_kv_heads * ((rows + 2 * kBlock - 1) / (2 * kBlock));
+    const long long tiles = items * (((long long)batch.max_len + kBlock - 1) / kBlock + 1);
+    long long slots = sm_count();
+    if (slots > tiles / 2) slots = tiles / 2;
+    return slots < 1 ? 1 : (int)slots;
+}
+
+template <typename T, int D, int NG>
+cudaError_t launch_prefill(const PagedAttnArgs &a, cudaStream_t stream)
+{
+    const PrefillArgs s{a, prefill_slots(a.p.cfg, a.p.batch)};
+    static unsigned long long done = 0;
+    cudaError_t e = configure_smem_once(paged_prefill_kernel<T, D, NG>, PGeo<D>::SMEM + (int)sizeof(long long) * (kMaxPagedSeqs + 1), done);
+    if (e != cudaSuccess) return e;
+    e = launch_chained(paged_prefill_kernel<T, D, NG>, dim3(s.n_slots), kPrefillThreads, PGeo<D>::SMEM + sizeof(long long) * (a.p.batch.n_seqs + 1), stream, s);
+    if (e != cudaSuccess) return e;
+    return launch_paged_merge(a, s.n_slots, 2 * kBlock, 32, kPOffset, stream);
+}
+
+template <typename T> cudaError_t prefill_by_shape(const PagedAttnArgs &a, cudaStream_t stream)
+{
+    if (a.p.cfg.head_dim == 128)
+        return a.p.ng == 1 ? launch_prefill<T, 128, 1>(a, stream) : a.p.ng == 2 ? launch_prefill<T, 128, 2>(a, stream) : launch_prefill<T, 128, 4>(a, stream);
+    return a.p.ng == 1 ? launch_prefill<T, 64, 1>(a, stream) : launch_prefill<T, 64, 2>(a, stream);
+}
+
+}  // namespace
+
+size_t prefill_workspace_bytes(const skvq_paged_config &cfg, const skvq_paged_batch &batch)
+{
+    const size_t slots = prefill_slots(cfg, batch);
+    return slots * kDescInts * 4 + slots * 2 * (2 * kBlock) * partial_stride(cfg.head_dim) * 4;
+}
+
+cudaError_t launch_paged_prefill(const PagedAttnArgs &a, cudaStream_t stream)
+{
+    return a.p.cfg.dtype == SKVQ_F16 ? prefill_by_shape<__half>(a, stream) : prefill_by_shape<__nv_bfloat16>(a, stream);
+}
+
+}  // namespace skvq
