@@ -1,19 +1,16 @@
 // skvq_paged_attention for many query rows per (sequence, KV head): prompts and chunks of prompts, on tcgen05.
 //
 // One CTA per SM works on items of up to 256 packed rows (row = new token * (Hq/Hkv) + query head) of one KV head, as two row
-// blocks of 128, over 128-token tiles of the cache.  Four roles, ordered by mbarriers only:
+// blocks of 128, over 128-token tiles of the cache.  Two kinds of warps, ordered by mbarriers:
 //   dequantizers  4 warps, a thread per token of the tile: codes and parameters come from the pages into registers one tile ahead,
 //                 leave as fp16(h c + z) (one rounding) in the 128-byte swizzle that both products read -- the key tile as the
 //                 K-major B operand of Q K^T, the value tile, same picture, as the MN-major B operand of P V; window tokens are
 //                 copied.  Two buffers of each.
-//   products      one thread issues S = Q K~^T (fp32 in tensor memory) and O += P V~ (P from tensor memory, in place of S).
-//   softmax       2 x 4 warps, a thread per row: S from tensor memory, probabilities back as fp16; the row sum in fp32.  The
-//                 reference of a row is raised, and O multiplied, only when a score exceeds it by more than 2^kLazy: O is
-//                 then read and written about once or twice per item.
-// While one block's scores become probabilities, the tensor core works for the other block.  Dequantizing costs about 450
-// instructions per thread and tile, shared by 256 rows; the exponentials (16 per clock and SM) and the products (2 x 1024 cycles
-// per tile and head dimension 128) bound the kernel about equally.
-//
+//   softmax       2 x 4 warps, a thread per row: S from tensor memory, probabilities back, in place, as the fp16 A operand; the row sum in fp32.  One warp of each block issues the block's products: O += P V~, then, behind
+//                 it in the tensor core's queue, the next tile's S = Q K~^T.  The reference of a row is raised, and O multiplied,
+//                 only when a score exceeds it by more than 2^kLazy: O is then read and written about once or twice per item.
+// While one block's scores become probabilities, the tensor core works for the other block.  Twelve warps leave each thread 168
+// registers; a warp more would cut that to 128 (16 warps' worth).
 // A nibble pair (i, i + 4) of a code word becomes two neighbouring fp16, so the channels of each run of eight lie in the order
 // 0 4 1 5 2 6 3 7 in the operands; the queries are laid out the same way and the outputs put back.
 // Items are laid end to end, priced in tiles (causal limits included), and cut into equal runs, one per CTA; an item that several
@@ -31,14 +28,14 @@ namespace {
 using mmak::and_or;
 using mmak::ex2_approx;
 using mmak::mbar_init;
-using mmak::mbar_wait_bounded;
+using mmak::mbar_try_wait;
 using mmak::smem_u32;
 using namespace tc5;
 
 constexpr int kBlock = 128;                     // rows of a row block, tokens of a tile
 constexpr int kSoftmaxThreads = 2 * kBlock;     // warps 0-7
 constexpr int kDequantThreads = kBlock;         // warps 8-11
-constexpr int kPrefillThreads = kSoftmaxThreads + kDequantThreads + 32;      // warp 12 issues the products
+constexpr int kPrefillThreads = kSoftmaxThreads + kDequantThreads;
 constexpr float kLazy = 8.f;                    // log2 of how far a score may exceed its row's reference
 constexpr float kPOffset = 6.f;                 // probabilities are held times 2^6: up to 2^14 in fp16, down to 2^-30 of the reference
 
@@ -55,8 +52,8 @@ struct PGeo {
     static constexpr int Q = 0;                                // 2 row blocks; at the end of an item its output rows
     static constexpr int K = 2 * TILE_BYTES;                   // 2 buffers
     static constexpr int V = 4 * TILE_BYTES;                   // 2 buffers
-    static constexpr int GATHER = 6 * TILE_BYTES;              // per softmax warp: two raw rows
-    static constexpr int SMEM = GATHER + 8 * 2 * D * 2 + 1024;  // and room to align to 1024 bytes
+    static constexpr int GATHER = 6 * TILE_BYTES;              // per softmax warp: four rows of queries
+    static constexpr int SMEM = GATHER + 8 * 4 * D * 2 + 1024;  // and room to align to 1024 bytes
     static constexpr int TMEM_S = 0, TMEM_O = 256;             // columns: S (P in place) 2 x 128, O 2 x D
 };
 
@@ -103,6 +100,12 @@ __device__ __forceinline__ void tmem_wait_ld32(float (&r)[32])
                    "+f"(r[24]), "+f"(r[25]), "+f"(r[26]), "+f"(r[27]), "+f"(r[28]), "+f"(r[29]), "+f"(r[30]), "+f"(r[31])
                  :: "memory");
 }
+__device__ __forceinline__ bool elect_one()      // true in one lane of a converged warp
+{
+    uint32_t r;
+    asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(r));
+    return r != 0;
+}
 __device__ __forceinline__ void mbar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
 __device__ __forceinline__ uint32_t h2(float lo, float hi)
 {
@@ -125,6 +128,40 @@ __device__ __forceinline__ uint32_t h2_fma(uint32_t a, uint32_t b, uint32_t c)
 template <typename T> __device__ __forceinline__ uint32_t to_h2(uint32_t v);      // see as_h2 of the kernel for few rows
 template <> __device__ __forceinline__ uint32_t to_h2<__half>(uint32_t v) { return v; }
 template <> __device__ __forceinline__ uint32_t to_h2<__nv_bfloat16>(uint32_t v) { return h2(__uint_as_float(v << 16), __uint_as_float(v & 0xFFFF0000u)); }
+
+// Two fp32 in a 64-bit register: one instruction works on both.
+__device__ __forceinline__ uint64_t pair(float a, float b)
+{
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void unpair(uint64_t v, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ uint64_t pair_fma(uint64_t a, uint64_t b, uint64_t c)
+{
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t pair_add(uint64_t a, uint64_t b)
+{
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+
+// Poll with a limit in clock cycles (about a tenth of a second); false: it ran out.
+__device__ __forceinline__ bool mbar_wait_cycles(uint32_t bar, uint32_t parity)
+{
+    if (mbar_try_wait(bar, parity)) return true;
+    const long long t0 = clock64();
+    for (;;) {
+#pragma unroll 1
+        for (int i = 0; i < 64; ++i)
+            if (mbar_try_wait(bar, parity)) return true;
+        if (clock64() - t0 > 200000000ll) return false;
+    }
+}
 
 // Position 0..7 inside a run of eight operand channels -> stored channel.
 __device__ __forceinline__ int channel_at(int pos) { return (pos >> 1) + 4 * (pos & 1); }
@@ -153,41 +190,206 @@ struct PItems {
     __device__ __forceinline__ int cost(int m) const { return max(tiles(m), 1); }
 };
 
-// What a CTA works on next: block m of KV head hk of sequence b, tiles [t0, t1) of `total`.
+// What a role of the CTA works on: block m of KV head hk of sequence b, tiles [t0, t1) of `total`.  It lives in shared memory: kept in
+// registers it spilled, and with 220 KB of shared memory in use a spilled register comes back from the L2 cache, a thousand cycles
+// later.
 struct PSegment {
-    int b, hk, m, t0, t1, total;
-    long long item_end;      // end of the item on the common axis
+    long long f, f1;         // what is left of the CTA's run
+    int valid, b, hk, m, t0, t1, total, parts;      // parts: CTAs that share the rest of the item
     PagedSeq seq;
     PItems it;
 };
 
-// Every role walks the same segments.
-struct PWalk {
-    long long f, f1;
-    int b;
-    __device__ __forceinline__ bool next(const PrefillArgs &a, const long long *pre, PSegment &s)
-    {
-        if (f >= f1) return false;
-        while (pre[b + 1] <= f) ++b;
-        s.b = b;
-        paged_sequence(a.a.p, b, false, s.seq);
-        s.it.set(a, s.seq);
-        const long long per_head = (pre[b + 1] - pre[b]) / a.a.p.cfg.n_kv_heads;
-        long long at = f - pre[b];
-        s.hk = (int)(at / per_head);
-        at -= s.hk * per_head;
-        s.m = 0;
-        int c = s.it.cost(0);
-        while (at >= c) { at -= c; c = s.it.cost(++s.m); }
-        const int take = (int)min((long long)(c - at), f1 - f);
-        s.total = s.it.tiles(s.m);
-        s.t0 = (int)at;
-        s.t1 = min((int)at + take, s.total);
-        s.item_end = f - at + c;
-        f += take;
-        return true;
-    }
-};
+// The next segment, by one thread of the role.
+__device__ __noinline__ void next_segment(const PrefillArgs &a, const long long *pre, long long ups, PSegment &s)
+{
+    long long f = s.f;
+    if (f >= s.f1) { s.valid = 0; return; }
+    int b = s.b;
+    while (pre[b + 1] <= f) ++b;
+    PagedSeq seq;
+    PItems it;
+    paged_sequence(a.a.p, b, false, seq);
+    it.set(a, seq);
+    const long long per_head = (pre[b + 1] - pre[b]) / a.a.p.cfg.n_kv_heads;
+    long long at = f - pre[b];
+    const int hk = (int)(at / per_head);
+    at -= hk * per_head;
+    int m = 0, c = it.cost(0);
+    while (at >= c) { at -= c; c = it.cost(++m); }
+    const int take = (int)min((long long)(c - at), s.f1 - f);
+    s.b = b;
+    s.hk = hk;
+    s.m = m;
+    s.total = it.tiles(m);
+    s.t0 = (int)at;
+    s.t1 = min((int)at + take, s.total);
+    s.parts = (int)((f - at + c - 1) / ups - blockIdx.x + 1);
+    s.seq = seq;
+    s.it = it;
+    s.f = f + take;
+    s.valid = 1;
+}
+
+// The queries of a row block as the K-major A operand: rotated, rounded to T, reordered, scaled by a power of two per row; and the source
+// channel of every output column.  Not inlined, like write_rows: what these keep in registers would spill in the loop over tiles.
+template <typename T, int D>
+__device__ __noinline__ void prepare_queries(const PrefillArgs &args, const PSegment &s, int blk, int rows, int row_base, float sign, uint8_t *q_tile, T *raw,
+                                             float *row_scale, uint16_t *out_channel)
+{
+    using Geo = PGeo<D>;
+    const PagedAttnArgs &a = args.a;
+    const PagedArgs &p = a.p;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+        // ---- queries of the block: a warp per row; lane: operand positions C lane .. C lane + C - 1
+        constexpr int C = D / 32;
+        struct alignas(sizeof(T) * C) Piece { T v[C]; };
+        int from[C];
+#pragma unroll
+        for (int k = 0; k < C; ++k) {
+            const int pos = lane * C + k, c = (pos & ~7) + channel_at(pos & 7);
+            from[k] = p.c.reorder_k ? p.c.reorder_k[s.hk * D + c] & (D - 1) : c;
+        }
+        for (int c = threadIdx.x & (kBlock - 1); c < D; c += kBlock) {
+            const int st = (c & ~7) + channel_at(c & 7);
+            out_channel[c] = (uint16_t)(p.c.reorder_v ? p.c.reorder_v[s.hk * D + st] & (D - 1) : st);
+        }
+        const float2 *rope = static_cast<const float2 *>(p.rope.table);
+        const int half = p.rope.rot_dim / 2;
+        // four rows at a time: their loads are in flight together
+#pragma unroll 1
+        for (int r0 = (warp & 3) * 32; r0 < (warp & 3) * 32 + 32; r0 += 4) {
+            Piece own[4];
+            float2 cs[4][C];
+            bool turn[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int r = r0 + k, i = (row_base + r) / s.it.rep, head = s.hk * s.it.rep + (row_base + r) % s.it.rep, pos = s.seq.len - s.seq.n + i;
+                const bool have = r < rows && sign != 0.f;
+                turn[k] = have && rope && pos >= 0;
+#pragma unroll
+                for (int e = 0; e < C; ++e) own[k].v[e] = Elem<T>::from_float(0.f);
+                if (have) own[k] = *reinterpret_cast<const Piece *>(static_cast<const T *>(a.q) + (int64_t)(s.seq.row0 + i) * a.q_stride + (int64_t)head * D + lane * C);
+                if (turn[k]) {
+#pragma unroll
+                    for (int e = 0; e < C; ++e) {
+                        const int c = lane * C + e;
+                        if (c < p.rope.rot_dim) cs[k][e] = rope[(int64_t)pos * half + (p.rope.interleaved ? c >> 1 : (c >= half ? c - half : c))];
+                    }
+                }
+            }
+            if (rope) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) *reinterpret_cast<Piece *>(raw + k * D + lane * C) = own[k];
+                __syncwarp();
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    if (!turn[k]) continue;
+#pragma unroll
+                    for (int e = 0; e < C; ++e) {
+                        const int c = lane * C + e;
+                        if (c < p.rope.rot_dim) {
+                            const bool second = p.rope.interleaved ? c & 1 : c >= half;
+                            const int partner = p.rope.interleaved ? c ^ 1 : (second ? c - half : c + half);
+                            const float mine = Elem<T>::to_float(own[k].v[e]), other = Elem<T>::to_float(raw[k * D + partner]);
+                            own[k].v[e] = Elem<T>::from_float(second ? rotate_second(other, mine, cs[k][e].x, cs[k][e].y) : rotate_first(mine, other, cs[k][e].x, cs[k][e].y));
+                        }
+                    }
+                }
+                __syncwarp();
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) *reinterpret_cast<Piece *>(raw + k * D + lane * C) = own[k];
+            __syncwarp();
+            float x[4][C], mx[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                mx[k] = 0.f;
+#pragma unroll
+                for (int e = 0; e < C; ++e) { x[k][e] = Elem<T>::to_float(raw[k * D + from[e]]); mx[k] = fmaxf(mx[k], fabsf(x[k][e])); }
+            }
+            __syncwarp();
+#pragma unroll
+            for (int d = 16; d > 0; d >>= 1)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) mx[k] = fmaxf(mx[k], __shfl_xor_sync(0xffffffffu, mx[k], d));
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int r = r0 + k;
+                float up = 1.f;      // the row's largest to [2^4, 2^5): exact, and far from fp16's ends whatever the type's range
+                if (mx[k] > 0.f && mx[k] < CUDART_INF_F) up = __int_as_float((127 + min(4 - (__float_as_int(mx[k]) >> 23) + 127, 60)) << 23);
+                if (lane == 0) row_scale[r] = (sign == 0.f ? 1.f : fabsf(a.sm_scale)) * 1.4426950408889634f / up;
+                uint8_t *dst = q_tile + r * 128 + ((lane * C) >> 6) * Geo::HALF_BYTES + ((((lane * C) >> 3 & 7) ^ (r & 7)) << 4) + ((lane * C) & 7) * 2;
+                const float f = up * sign;
+                if constexpr (C == 4) *reinterpret_cast<uint2 *>(dst) = make_uint2(h2(x[k][0] * f, x[k][1] * f), h2(x[k][2] * f, x[k][3] * f));
+                else *reinterpret_cast<uint32_t *>(dst) = h2(x[k][0] * f, x[k][1] * f);
+            }
+        }
+}
+
+// The result of a row block: finished rows, or (a share of an item) sums that the merge kernel joins.
+template <typename T, int D>
+__device__ __noinline__ void write_rows(const PrefillArgs &args, const PSegment &s, int blk, int rows, int row_base, bool work, uint32_t o_addr, float ref, float l,
+                                        float rs, uint8_t *q_tile, const uint16_t *out_channel, bool whole, float *part)
+{
+    const PagedAttnArgs &a = args.a;
+    const skvq_paged_config &cfg = a.p.cfg;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, row = threadIdx.x & (kBlock - 1);
+    const int i = (row_base + row) / s.it.rep, head = s.hk * s.it.rep + (row_base + row) % s.it.rep;
+    if (whole) {
+        const float inv = ref == -CUDART_INF_F ? 0.f : 1.f / l;
+        T *rows_out = reinterpret_cast<T *>(q_tile);      // [128][D], 16-byte pieces of a row at piece ^ (row & 7); all products have been read
+#pragma unroll 1
+        for (int c0 = 0; c0 < D; c0 += 32) {
+            float x[32];
+            if (work) {
+                tmem_ld32(o_addr + c0, x);
+                tmem_wait_ld32(x);
+            }
+#pragma unroll
+            for (int c = 0; c < 32; ++c) {
+                const int dst = work ? out_channel[c0 + c] : c0 + c;
+                rows_out[row * D + ((((dst >> 3) ^ (row & 7))) << 3) + (dst & 7)] = Elem<T>::from_float(work && ref != -CUDART_INF_F ? x[c] * inv : 0.f);
+            }
+        }
+        if (a.lse && row < rows )
+            a.lse[(int64_t)(s.seq.row0 + i) * cfg.n_q_heads + head] = ref == -CUDART_INF_F ? ref : (ref * rs + log2f(l) - kPOffset) * 0.6931471805599453f;
+        __syncwarp();
+        constexpr int PER_ROW = D / 8;
+        for (int e = lane; e < 32 * PER_ROW; e += 32) {      // this warp's 32 rows, 16 bytes a lane
+            const int r = (warp & 3) * 32 + e / PER_ROW, c8 = e % PER_ROW;
+            if (r < rows ) {
+                const int ri = (row_base + r) / s.it.rep, rh = s.hk * s.it.rep + (row_base + r) % s.it.rep;
+                *reinterpret_cast<uint4 *>(static_cast<T *>(a.out) + (int64_t)(s.seq.row0 + ri) * a.out_stride + (int64_t)rh * D + c8 * 8) =
+                    *reinterpret_cast<const uint4 *>(rows_out + r * D + ((c8 ^ (r & 7)) << 3));
+            }
+        }
+        __syncwarp();
+    } else {
+        // a share of an item: unscaled sums, stored channels in order
+        part += row * partial_stride(D);
+#pragma unroll 1
+        for (int c0 = 0; c0 < D; c0 += 32) {
+            float x[32];
+            if (work) {
+                tmem_ld32(o_addr + c0, x);
+                tmem_wait_ld32(x);
+            }
+            if (row < rows) {
+#pragma unroll
+                for (int c = 0; c < 32; c += 8) {
+                    const bool some = work && ref != -CUDART_INF_F;
+                    *reinterpret_cast<float4 *>(part + c0 + c) = some ? make_float4(x[c], x[c + 2], x[c + 4], x[c + 6]) : make_float4(0.f, 0.f, 0.f, 0.f);
+                    *reinterpret_cast<float4 *>(part + c0 + c + 4) = some ? make_float4(x[c + 1], x[c + 3], x[c + 5], x[c + 7]) : make_float4(0.f, 0.f, 0.f, 0.f);
+                }
+            }
+        }
+        if (row < rows) {
+            part[D] = ref == -CUDART_INF_F ? ref : ref * rs;
+            part[D + 1] = l;
+        }
+                }
+}
 
 template <typename T, int D, int NG>
 __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const __grid_constant__ PrefillArgs args)
@@ -199,15 +401,17 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     long long *pre = reinterpret_cast<long long *>(smem + Geo::SMEM - 1024);
-    __shared__ __align__(8) uint64_t bars[16];
+    __shared__ __align__(8) uint64_t bars[12];
     __shared__ uint32_t tmem_sh;
     __shared__ int fail_sh;
     __shared__ long long scan_sh[16];
     __shared__ float row_scale[2 * kBlock];
     __shared__ uint16_t out_channel[2][D];      // source channel of every operand column, per row block
+    __shared__ PSegment seg_sh[3];              // of the two row blocks, of the dequantizers
     __shared__ uint32_t bad_sh[4];              // of the last four tiles: 16-token blocks without a page (a tile's is read until its
                                                 // probabilities are written, when the tile two further on may be in the making)
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, B = p.batch.n_seqs;
+    const int tid = threadIdx.x, lane = tid & 31, B = p.batch.n_seqs;
+    const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);      // one value per warp, and the compiler knows: descriptors stay in uniform registers
 
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;");
@@ -249,61 +453,75 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
     // ---- barriers, tensor memory
     const uint32_t bar0 = smem_u32(bars);
     const uint32_t k_full = bar0, k_empty = bar0 + 16, v_full = bar0 + 32, v_empty = bar0 + 48;      // + 8 * buffer
-    const uint32_t s_full = bar0 + 64, p_full = bar0 + 80, pv_done = bar0 + 96, q_full = bar0 + 112;  // + 8 * row block
+    const uint32_t s_full = bar0 + 64, pv_done = bar0 + 80;                                          // + 8 * row block
     if (tid == 0) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             mbar_init(k_full + 8 * i, kDequantThreads);
-            mbar_init(k_empty + 8 * i, 1);
+            mbar_init(k_empty + 8 * i, 2);      // both row blocks' products
             mbar_init(v_full + 8 * i, kDequantThreads);
-            mbar_init(v_empty + 8 * i, 1);
+            mbar_init(v_empty + 8 * i, 2);
             mbar_init(s_full + 8 * i, 1);
-            mbar_init(p_full + 8 * i, kBlock);
             mbar_init(pv_done + 8 * i, 1);
-            mbar_init(q_full + 8 * i, kBlock);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fail_sh = 0;
     }
-    if (warp == kPrefillThreads / 32 - 1) tmem_alloc(smem_u32(&tmem_sh), 512);
+    if (warp == 0) tmem_alloc(smem_u32(&tmem_sh), 512);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = tmem_sh;
     const long long total = pre[B], ups = max((total + args.n_slots - 1) / args.n_slots, 1LL);
-    PWalk walk;
-    walk.f = blockIdx.x * ups;
-    walk.f1 = min(walk.f + ups, total);
-    walk.b = 0;
     int *desc = reinterpret_cast<int *>(a.ws) + (size_t)blockIdx.x * kDescInts;
-    if (tid == 0) desc[0] = 0;
-    if (walk.f < walk.f1) {
-        int lo = 0, hi = B - 1;
-        while (lo < hi) {
-            const int mid = (lo + hi + 1) >> 1;
-            if (pre[mid] <= walk.f) lo = mid; else hi = mid - 1;
+    if (tid < 3) {
+        PSegment &first = seg_sh[tid];
+        first.f = blockIdx.x * ups;
+        first.f1 = min(first.f + ups, total);
+        first.b = 0;
+        if (first.f < first.f1) {
+            int lo = 0, hi = B - 1;
+            while (lo < hi) {
+                const int mid = (lo + hi + 1) >> 1;
+                if (pre[mid] <= first.f) lo = mid; else hi = mid - 1;
+            }
+            first.b = lo;
         }
-        walk.b = lo;
     }
+    if (tid == 0) desc[0] = 0;
+    __syncthreads();
     // A wait that runs out is reported; the thread then goes through its loops without waiting or storing.
     bool alive = true;
     volatile int *fail = &fail_sh;
+    // The whole warp calls this; one lane polls (32 lanes polling twelve warps over kept shared memory so busy that every access to it
+    // took several hundred cycles).
     auto wait = [&](uint32_t bar, uint32_t parity) {
-        if (alive && !mbar_wait_bounded(bar, parity)) {
+        bool ok = true;
+        if (alive && lane == 0) ok = mbar_wait_cycles(bar, parity);
+        if (!__shfl_sync(0xffffffffu, ok, 0)) {
             alive = false;
             *fail = 1;
-            set_status(p.c.status, SKVQ_STATUS_COPY_TIMEOUT);
+            if (lane == 0) set_status(p.c.status, SKVQ_STATUS_COPY_TIMEOUT);
         }
     };
-    PSegment s;
+    // A role is 128 threads: block 0, block 1, the dequantizers.
+    const int role = warp >> 2;
+    const PSegment &s = seg_sh[role];
+    auto role_sync = [&]() { asm volatile("bar.sync %0, 128;" ::"r"(1 + role) : "memory"); };
+    auto next = [&]() {
+        role_sync();
+        if ((tid & 127) == 0) next_segment(args, pre, ups, seg_sh[role]);
+        role_sync();
+        return s.valid != 0;
+    };
 
-    if (warp >= 8 && warp < 12) {
+    if (warp >= 8) {
         // ================================================================ dequantizers
         const int row = tid - kSoftmaxThreads;      // token of the tile
         const int P = cfg.page_tokens, page_shift = __ffs(P) - 1;
         constexpr int PIECES = D / 32;              // 16-byte pieces of a code row
         uint32_t n = 0;                             // tiles so far
-        while (walk.next(args, pre, s)) {
+        while (next()) {
             const int32_t *table = p.batch.page_table + (int64_t)s.b * p.batch.max_pages;
             const int64_t win_row0 = ((int64_t)s.seq.slot * cfg.n_kv_heads + s.hk) * cfg.ring_tokens;
             uint4 kc[PIECES], vc[PIECES];
@@ -342,7 +560,7 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
             int page_next = page_of(s.t0 + 1);
             for (int t = s.t0; t < s.t1; ++t, ++n) {
                 const uint32_t buf = n & 1, phase = (n >> 1) & 1;
-                if (*fail) alive = false;
+                if (__any_sync(0xffffffffu, *fail)) alive = false;
                 uint8_t *kt = smem + Geo::K + buf * Geo::TILE_BYTES + row * 128, *vt = smem + Geo::V + buf * Geo::TILE_BYTES + row * 128;
                 // one code word -> one 16-byte piece of the operand row
                 auto piece = [&](uint8_t *base, int c8, uint32_t w, uint32_t hh, uint32_t zz) {
@@ -398,63 +616,13 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
                     if (quantized) expand(vt, vc, vm);
                     else copy_row(vt, p.c.v_win, have, r);
                 }
-                page = page_next;
-                load_codes(t + 1);      // in flight until the next tile's buffer is free
-                page_next = page_of(t + 2);
                 proxy_fence();
                 mbar_arrive(v_full + 8 * buf);
+                page = page_next;
+                load_codes(t + 1);      // in flight until the next tile's buffer is free; behind the fence, which would wait for them
+                page_next = page_of(t + 2);
             }
         }
-    } else if (warp == 12) {
-        // ================================================================ products
-        if (lane == 0) {
-            constexpr uint32_t kIdescS = idesc_f16_f32(kBlock, kBlock);
-            constexpr uint32_t kIdescO = idesc_f16_f32(kBlock, D) | (1u << 16);      // B is MN-major
-            const uint32_t base = smem_u32(smem);
-            uint32_t n = 0, nq[2] = {0, 0}, np[2] = {0, 0};      // tiles so far; queries and probabilities taken, per row block
-            while (walk.next(args, pre, s)) {
-                const int rows = s.it.rows() - s.m * 2 * kBlock, blocks = rows > kBlock ? 2 : 1;
-                if (s.t0 >= s.t1) continue;      // nothing to see: the softmax warps write zeros on their own
-                auto scores = [&](int i, uint32_t buf) {
-#pragma unroll
-                    for (int ks = 0; ks < D / 16; ++ks)
-                        umma_f16(tmem + Geo::TMEM_S + i * kBlock, desc_k_major(base + Geo::Q + i * Geo::TILE_BYTES + (ks >> 2) * Geo::HALF_BYTES + (ks & 3) * 32),
-                                 desc_k_major(base + Geo::K + buf * Geo::TILE_BYTES + (ks >> 2) * Geo::HALF_BYTES + (ks & 3) * 32), kIdescS, ks > 0);
-                    umma_commit(s_full + 8 * i);
-                };
-                for (int i = 0; i < blocks; ++i) { wait(q_full + 8 * i, nq[i] & 1); ++nq[i]; }
-                wait(k_full + 8 * (n & 1), (n >> 1) & 1);
-                tc_fence_after();
-                for (int i = 0; i < blocks; ++i) scores(i, n & 1);
-                umma_commit(k_empty + 8 * (n & 1));
-                for (int t = s.t0; t < s.t1; ++t, ++n) {
-                    if (*fail) alive = false;
-                    const uint32_t buf = n & 1, next = buf ^ 1;
-                    const bool more = t + 1 < s.t1;
-                    wait(v_full + 8 * buf, (n >> 1) & 1);
-                    for (int i = 0; i < blocks; ++i) {
-                        wait(p_full + 8 * i, np[i] & 1);
-                        ++np[i];
-                        tc_fence_after();
-#pragma unroll
-                        for (int ks = 0; ks < kBlock / 16; ++ks)
-                            umma_f16_ts(tmem + Geo::TMEM_O + i * D, tmem + Geo::TMEM_S + i * kBlock + ks * 8,
-                                        desc_mn_major(base + Geo::V + buf * Geo::TILE_BYTES + ks * 2048, Geo::HALF_BYTES), kIdescO, t > s.t0 || ks > 0);
-                        umma_commit(pv_done + 8 * i);
-                        if (more) {
-                            if (i == 0) {
-                                wait(k_full + 8 * next, ((n + 1) >> 1) & 1);
-                                tc_fence_after();
-                            }
-                            scores(i, next);
-                        }
-                    }
-                    umma_commit(v_empty + 8 * buf);
-                    if (more) umma_commit(k_empty + 8 * next);
-                }
-            }
-        }
-        __syncwarp();
     } else {
         // ================================================================ softmax
         const int blk = warp >> 2, row = tid & (kBlock - 1);                       // row block, row = lane of the tensor memory
@@ -462,167 +630,188 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
         const uint32_t s_addr = tmem + Geo::TMEM_S + blk * kBlock + quad, o_addr = tmem + Geo::TMEM_O + blk * D + quad;
         const float sign = a.sm_scale < 0.f ? -1.f : (a.sm_scale == 0.f ? 0.f : 1.f);
         uint8_t *q_tile = smem + Geo::Q + blk * Geo::TILE_BYTES;
-        T *raw = reinterpret_cast<T *>(smem + Geo::GATHER) + warp * 2 * D;
+        T *raw = reinterpret_cast<T *>(smem + Geo::GATHER) + warp * 4 * D;
         uint32_t n = 0, ns = 0;      // tiles so far (both blocks'), score tiles of this block so far
-        while (walk.next(args, pre, s)) {
+        // ---- the block's products, issued by its first warp
+        constexpr uint32_t kIdescS = idesc_f16_f32(kBlock, kBlock);
+        constexpr uint32_t kIdescO = idesc_f16_f32(kBlock, D) | (1u << 16);      // B is MN-major
+        const uint32_t smem_base = smem_u32(smem);
+        // S = Q K~^T of tile number `tile`.  The whole warp runs these (addresses are warp-uniform), one lane issues.
+        auto issue_scores = [&](uint32_t tile) {
+            const uint32_t buf = tile & 1;
+            const uint64_t dq = desc_k_major(smem_base + Geo::Q + blk * Geo::TILE_BYTES), dk = desc_k_major(smem_base + Geo::K + buf * Geo::TILE_BYTES);
+            wait(k_full + 8 * buf, (tile >> 1) & 1);
+            tc_fence_after();
+            if (elect_one()) {
+#pragma unroll
+                for (int ks = 0; ks < D / 16; ++ks) {
+                    constexpr uint32_t half = Geo::HALF_BYTES >> 4;
+                    umma_f16(tmem + Geo::TMEM_S + blk * kBlock, dq + (ks >> 2) * half + (ks & 3) * 2, dk + (ks >> 2) * half + (ks & 3) * 2, kIdescS, ks > 0);
+                }
+                umma_commit(s_full + 8 * blk);
+                umma_commit(k_empty + 8 * buf);
+            }
+            __syncwarp();
+        };
+        auto issue_values = [&](uint32_t tile, bool first) {
+            const uint32_t buf = tile & 1;
+            const uint64_t dv = desc_mn_major(smem_base + Geo::V + buf * Geo::TILE_BYTES, Geo::HALF_BYTES);
+            wait(v_full + 8 * buf, (tile >> 1) & 1);
+            tc_fence_after();
+            if (elect_one()) {
+#pragma unroll
+                for (int ks = 0; ks < kBlock / 16; ++ks)
+                    umma_f16_ts(tmem + Geo::TMEM_O + blk * D, tmem + Geo::TMEM_S + blk * kBlock + ks * 8, dv + ks * (2048 >> 4), kIdescO, !first || ks > 0);
+                umma_commit(pv_done + 8 * blk);
+                umma_commit(v_empty + 8 * buf);
+            }
+            __syncwarp();
+        };
+        while (next()) {
             const int rows = min(s.it.rows() - (s.m * 2 + blk) * kBlock, kBlock);      // of this block; may be <= 0
             const int row_base = (s.m * 2 + blk) * kBlock;
             const bool whole = s.t0 == 0 && s.t1 == s.total;
             const bool work = s.t0 < s.t1 && rows > 0;
-            if (*fail) alive = false;
+            if (__any_sync(0xffffffffu, *fail)) alive = false;
             if (work) {
-                asm volatile("bar.sync %0, 128;" ::"r"(1 + blk) : "memory");      // every warp has sent off its rows of the item before
-                // ---- queries of the block: a warp per row; lane: operand positions C lane .. C lane + C - 1
-                constexpr int C = D / 32;
-                struct alignas(sizeof(T) * C) Piece { T v[C]; };
-                int from[C];
-#pragma unroll
-                for (int k = 0; k < C; ++k) {
-                    const int pos = lane * C + k, c = (pos & ~7) + channel_at(pos & 7);
-                    from[k] = p.c.reorder_k ? p.c.reorder_k[s.hk * D + c] & (D - 1) : c;
-                }
-                for (int c = row; c < D; c += kBlock) {
-                    const int st = (c & ~7) + channel_at(c & 7);
-                    out_channel[blk][c] = (uint16_t)(p.c.reorder_v ? p.c.reorder_v[s.hk * D + st] & (D - 1) : st);
-                }
-                const float2 *rope = static_cast<const float2 *>(p.rope.table);
-                const int half = p.rope.rot_dim / 2;
-#pragma unroll 2
-                for (int k = 0; k < 32; ++k) {
-                    const int r = (warp & 3) * 32 + k;
-                    float x[C], mx = 0.f;
-#pragma unroll
-                    for (int e = 0; e < C; ++e) x[e] = 0.f;
-                    if (r < rows && sign != 0.f) {
-                        const int i = (row_base + r) / s.it.rep, head = s.hk * s.it.rep + (row_base + r) % s.it.rep, pos = s.seq.len - s.seq.n + i;
-                        const T *src = static_cast<const T *>(a.q) + (int64_t)(s.seq.row0 + i) * a.q_stride + (int64_t)head * D;
-                        Piece own = *reinterpret_cast<const Piece *>(src + lane * C);
-                        T *buf = raw + (k & 1) * D;
-                        if (rope && pos >= 0) {
-                            *reinterpret_cast<Piece *>(buf + lane * C) = own;
-                            __syncwarp();
-#pragma unroll
-                            for (int e = 0; e < C; ++e) {
-                                const int c = lane * C + e;
-                                if (c < p.rope.rot_dim) {
-                                    const bool second = p.rope.interleaved ? c & 1 : c >= half;
-                                    const int pair = p.rope.interleaved ? c >> 1 : (second ? c - half : c);
-                                    const int partner = p.rope.interleaved ? c ^ 1 : (second ? c - half : c + half);
-                                    const float2 cs = rope[(int64_t)pos * half + pair];
-                                    const float mine = Elem<T>::to_float(own.v[e]), other = Elem<T>::to_float(buf[partner]);
-                                    own.v[e] = Elem<T>::from_float(second ? rotate_second(other, mine, cs.x, cs.y) : rotate_first(mine, other, cs.x, cs.y));
-                                }
-                            }
-                            __syncwarp();
-                        }
-                        *reinterpret_cast<Piece *>(buf + lane * C) = own;
-                        __syncwarp();
-#pragma unroll
-                        for (int e = 0; e < C; ++e) { x[e] = Elem<T>::to_float(buf[from[e]]); mx = fmaxf(mx, fabsf(x[e])); }
-                        __syncwarp();
-                    }
-                    mx = mmak::warp_max(mx);
-                    float up = 1.f;      // the row's largest to [2^4, 2^5): exact, and far from fp16's ends whatever the type's range
-                    if (mx > 0.f && mx < CUDART_INF_F) up = __int_as_float((127 + min(4 - (__float_as_int(mx) >> 23) + 127, 60)) << 23);
-                    if (lane == 0) row_scale[blk * kBlock + r] = (sign == 0.f ? 1.f : fabsf(a.sm_scale)) * 1.4426950408889634f / up;
-                    uint8_t *dst = q_tile + r * 128 + ((lane * C) >> 6) * Geo::HALF_BYTES + ((((lane * C) >> 3 & 7) ^ (r & 7)) << 4) + ((lane * C) & 7) * 2;
-                    const float f = up * sign;
-                    if constexpr (C == 4) *reinterpret_cast<uint2 *>(dst) = make_uint2(h2(x[0] * f, x[1] * f), h2(x[2] * f, x[3] * f));
-                    else *reinterpret_cast<uint32_t *>(dst) = h2(x[0] * f, x[1] * f);
-                }
+                prepare_queries<T, D>(args, s, blk, rows, row_base, sign, q_tile, raw, row_scale + blk * kBlock, out_channel[blk]);
                 proxy_fence();
-                mbar_arrive(q_full + 8 * blk);
-                asm volatile("bar.sync %0, 128;" ::"r"(1 + blk) : "memory");      // row_scale and out_channel of the whole block
+                role_sync();      // the operand, row_scale and out_channel of the whole block
+                if ((warp & 3) == 0) issue_scores(n);
             }
             const float rs = work ? row_scale[blk * kBlock + row] : 1.f;
             const int lim = s.it.limit(row_base + min(row, max(rows, 1) - 1));
             float ref = -CUDART_INF_F, l = 0.f;      // reference (unscaled score), sum of probabilities
-            for (int t = s.t0; t < s.t1; ++t, ++n) {
-                if (!work) continue;
-                if (*fail) alive = false;
-                wait(s_full + 8 * blk, ns & 1);
-                tc_fence_after();
+            if (!work) {
+                // A block without rows follows the tiles all the same: it frees the buffers on its side, and it must not reach a
+                // later item while a barrier is still two phases behind what it would wait for.
+                for (int t = s.t0; t < s.t1; ++t, ++n) {
+                    if ((warp & 3) != 0) continue;
+                    if (__any_sync(0xffffffffu, *fail)) alive = false;
+                    wait(k_full + 8 * (n & 1), (n >> 1) & 1);
+                    if (lane == 0) mbar_arrive(k_empty + 8 * (n & 1));
+                    wait(v_full + 8 * (n & 1), (n >> 1) & 1);
+                    if (lane == 0) mbar_arrive(v_empty + 8 * (n & 1));
+                }
+            }
+            for (int t = s.t0; work && t < s.t1; ++t, ++n) {
+                if (__any_sync(0xffffffffu, *fail)) alive = false;
                 const bool quantized = t < s.it.tiles_c;
                 const int tok0 = quantized ? t * kBlock : s.it.lq + (t - s.it.tiles_c) * kBlock;
-                const uint32_t bad = quantized ? bad_sh[n & 3] : 0u;      // two bits in each byte
                 const int seen = min(min(lim, quantized ? s.it.lq : s.seq.len) - tok0, kBlock);      // columns below it are seen
-                const bool edge = __any_sync(0xffffffffu, seen < kBlock || bad != 0u);
-                auto hidden = [&](int c) { return c >= seen || ((bad >> (8 * (c >> 5) + ((c >> 4) & 1))) & 1u); };
-                // ---- the row's maximum
-                float mx = -CUDART_INF_F;
-                {
-                    float x[32], y[32];
-#pragma unroll
-                    for (int c0 = 0; c0 < kBlock; c0 += 64) {
-                        tmem_ld32(s_addr + c0, x);
-                        tmem_ld32(s_addr + c0 + 32, y);
-                        tmem_wait_ld32(x);
-                        tmem_wait_ld32(y);
-                        if (edge) {
-#pragma unroll
-                            for (int c = 0; c < 32; ++c) {
-                                if (hidden(c0 + c)) x[c] = -CUDART_INF_F;
-                                if (hidden(c0 + 32 + c)) y[c] = -CUDART_INF_F;
-                            }
-                        }
-                        float m0 = fmaxf(x[0], y[0]), m1 = fmaxf(x[1], y[1]);
-#pragma unroll
-                        for (int c = 2; c < 32; c += 2) {
-                            m0 = fmaxf(fmaxf(m0, x[c]), y[c]);
-                            m1 = fmaxf(fmaxf(m1, x[c + 1]), y[c + 1]);
-                        }
-                        mx = fmaxf(mx, fmaxf(m0, m1));
-                    }
-                }
-                // ---- raise the reference: at first, then only when a score exceeds it by 2^kLazy
-                if (t > s.t0 && __any_sync(0xffffffffu, (mx - ref) * rs > kLazy)) {
-                    float down = 1.f;
-                    if (mx > ref) {
-                        down = ref == -CUDART_INF_F ? 0.f : ex2_approx((ref - mx) * rs);
-                        ref = mx;
-                    }
-                    l *= down;
-                    wait(pv_done + 8 * blk, (ns - 1) & 1);      // the products of the tile before have landed in O
-                    tc_fence_after();
+                wait(s_full + 8 * blk, ns & 1);
+                tc_fence_after();
+                const uint32_t bad = quantized ? bad_sh[n & 3] : 0u;      // two bits in each byte
+                if (__any_sync(0xffffffffu, seen < kBlock || bad != 0u)) {
+                    // hidden columns become -infinity in place; the code below then is the same for all tiles
 #pragma unroll 1
-                    for (int c0 = 0; c0 < D; c0 += 32) {
+                    for (int run = 0; run < 4; ++run) {
+                        const int left = seen - 32 * run;      // which of its 32 columns the row sees, one bit each
+                        uint32_t v = left >= 32 ? 0xFFFFFFFFu : (left <= 0 ? 0u : (1u << left) - 1u);
+                        const uint32_t two = (bad >> (8 * run)) & 3u;
+                        if (two & 1u) v &= 0xFFFF0000u;
+                        if (two & 2u) v &= 0x0000FFFFu;
                         float x[32];
-                        tmem_ld32(o_addr + c0, x);
+                        tmem_ld32(s_addr + 32 * run, x);
                         tmem_wait_ld32(x);
                         uint32_t w[32];
 #pragma unroll
-                        for (int c = 0; c < 32; ++c) w[c] = __float_as_uint(x[c] * down);
+                        for (int c = 0; c < 32; ++c) w[c] = (v >> c) & 1u ? __float_as_uint(x[c]) : 0xFF800000u;
+                        tmem_st32(s_addr + 32 * run, w);
+                    }
+                    tmem_wait_st();
+                }
+                auto largest = [&](const float (&x)[32], float m) {
+                    float m0 = fmaxf(fmaxf(m, x[0]), x[1]), m1 = fmaxf(x[2], x[3]), m2 = fmaxf(x[4], x[5]), m3 = fmaxf(x[6], x[7]);
+#pragma unroll
+                    for (int c = 8; c < 32; c += 8) {
+                        m0 = fmaxf(fmaxf(m0, x[c]), x[c + 1]);
+                        m1 = fmaxf(fmaxf(m1, x[c + 2]), x[c + 3]);
+                        m2 = fmaxf(fmaxf(m2, x[c + 4]), x[c + 5]);
+                        m3 = fmaxf(fmaxf(m3, x[c + 6]), x[c + 7]);
+                    }
+                    return fmaxf(fmaxf(m0, m1), fmaxf(m2, m3));
+                };
+                float down = 1.f;
+                bool raise = false;
+                // The row in four runs of 32 columns, twice: for the maximum, for the probabilities.  (Keeping runs in registers in between
+                // spilled.)
+                float x[32], y[32];
+                tmem_ld32(s_addr, x);
+                tmem_ld32(s_addr + 32, y);
+                tmem_wait_ld32(x);
+                tmem_wait_ld32(y);
+                float mx = largest(y, largest(x, -CUDART_INF_F));
+                tmem_ld32(s_addr + 64, x);
+                tmem_ld32(s_addr + 96, y);
+                tmem_wait_ld32(x);
+                tmem_wait_ld32(y);
+                mx = largest(y, largest(x, mx));
+                tmem_ld32(s_addr, x);
+                // ---- raise the reference: at first, then only when a score exceeds it by 2^kLazy
+                raise = t > s.t0 && __any_sync(0xffffffffu, (mx - ref) * rs > kLazy);
+                if (t == s.t0) ref = mx;
+                else if (raise && mx > ref) {
+                    down = ref == -CUDART_INF_F ? 0.f : ex2_approx((ref - mx) * rs);
+                    ref = mx;
+                    l *= down;
+                }
+                const float base = kPOffset - (ref == -CUDART_INF_F ? 0.f : ref * rs);
+                const uint64_t rs2 = pair(rs, rs), base2 = pair(base, base);
+                uint64_t l0 = 0ull, l1 = 0ull;      // pairs of sums
+                auto probabilities = [&](const float (&v)[32], int run) {
+                    uint32_t w[16];
+#pragma unroll
+                    for (int c = 0; c < 32; c += 4) {
+                        float e[4];
+                        unpair(pair_fma(pair(v[c], v[c + 1]), rs2, base2), e[0], e[1]);
+                        unpair(pair_fma(pair(v[c + 2], v[c + 3]), rs2, base2), e[2], e[3]);
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) e[k] = ex2_approx(e[k]);
+                        l0 = pair_add(l0, pair(e[0], e[1]));
+                        l1 = pair_add(l1, pair(e[2], e[3]));
+                        w[c >> 1] = h2(e[0], e[1]);
+                        w[(c >> 1) + 1] = h2(e[2], e[3]);
+                    }
+                    tmem_st16(s_addr + run * 16, w);      // over scores that are in registers or used up
+                };
+                tmem_wait_ld32(x);
+                tmem_ld32(s_addr + 32, y);
+                probabilities(x, 0);
+                tmem_wait_ld32(y);
+                tmem_ld32(s_addr + 64, x);
+                probabilities(y, 1);
+                tmem_wait_ld32(x);
+                tmem_ld32(s_addr + 96, y);
+                probabilities(x, 2);
+                tmem_wait_ld32(y);
+                probabilities(y, 3);
+                {
+                    float a0, a1;
+                    unpair(pair_add(l0, l1), a0, a1);
+                    l += a0 + a1;
+                }
+                if (raise) {      // O follows the reference, once the products of the tile before have landed in it
+                    wait(pv_done + 8 * blk, (ns - 1) & 1);
+                    tc_fence_after();
+#pragma unroll 1
+                    for (int c0 = 0; c0 < D; c0 += 32) {
+                        float y[32];
+                        tmem_ld32(o_addr + c0, y);
+                        tmem_wait_ld32(y);
+                        uint32_t w[32];
+#pragma unroll
+                        for (int c = 0; c < 32; ++c) w[c] = __float_as_uint(y[c] * down);
                         tmem_st32(o_addr + c0, w);
                     }
-                } else if (t == s.t0) {
-                    ref = mx;
-                }
-                // ---- probabilities, in place of the scores
-                const float base = kPOffset - (ref == -CUDART_INF_F ? 0.f : ref * rs);
-#pragma unroll
-                for (int c0 = 0; c0 < kBlock; c0 += 32) {
-                    float x[32];
-                    tmem_ld32(s_addr + c0, x);
-                    tmem_wait_ld32(x);
-                    uint32_t w[16];
-                    float l0 = 0.f, l1 = 0.f;
-#pragma unroll
-                    for (int c = 0; c < 32; c += 2) {
-                        float e0 = ex2_approx(fmaf(x[c], rs, base)), e1 = ex2_approx(fmaf(x[c + 1], rs, base));
-                        if (edge) {
-                            if (hidden(c0 + c)) e0 = 0.f;
-                            if (hidden(c0 + c + 1)) e1 = 0.f;
-                        }
-                        l0 += e0;
-                        l1 += e1;
-                        w[c >> 1] = h2(e0, e1);
-                    }
-                    l += l0 + l1;
-                    tmem_st16(s_addr + c0 / 2, w);
                 }
                 tmem_wait_st();
                 tc_fence_before();
-                mbar_arrive(p_full + 8 * blk);
+                role_sync();
+                if ((warp & 3) == 0) {
+                    issue_values(n, t == s.t0);
+                    if (t + 1 < s.t1) issue_scores(n + 1);
+                }
                 ++ns;
             }
             if (rows <= 0) continue;
@@ -631,65 +820,13 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
                 wait(pv_done + 8 * blk, (ns - 1) & 1);
                 tc_fence_after();
             }
-            const int i = (row_base + row) / s.it.rep, head = s.hk * s.it.rep + (row_base + row) % s.it.rep;
-            if (whole) {
-                const float inv = ref == -CUDART_INF_F ? 0.f : 1.f / l;
-                T *rows_out = reinterpret_cast<T *>(q_tile);      // [128][D], 16-byte pieces of a row at piece ^ (row & 7); all products have been read
-#pragma unroll 1
-                for (int c0 = 0; c0 < D; c0 += 32) {
-                    float x[32];
-                    if (work) {
-                        tmem_ld32(o_addr + c0, x);
-                        tmem_wait_ld32(x);
-                    }
-#pragma unroll
-                    for (int c = 0; c < 32; ++c) {
-                        const int dst = work ? out_channel[blk][c0 + c] : c0 + c;
-                        rows_out[row * D + ((((dst >> 3) ^ (row & 7))) << 3) + (dst & 7)] = Elem<T>::from_float(work && ref != -CUDART_INF_F ? x[c] * inv : 0.f);
-                    }
-                }
-                if (a.lse && row < rows && alive)
-                    a.lse[(int64_t)(s.seq.row0 + i) * cfg.n_q_heads + head] = ref == -CUDART_INF_F ? ref : (ref * rs + log2f(l) - kPOffset) * 0.6931471805599453f;
-                __syncwarp();
-                constexpr int PER_ROW = D / 8;
-                for (int e = lane; e < 32 * PER_ROW; e += 32) {      // this warp's 32 rows, 16 bytes a lane
-                    const int r = (warp & 3) * 32 + e / PER_ROW, c8 = e % PER_ROW;
-                    if (r < rows && alive) {
-                        const int ri = (row_base + r) / s.it.rep, rh = s.hk * s.it.rep + (row_base + r) % s.it.rep;
-                        *reinterpret_cast<uint4 *>(static_cast<T *>(a.out) + (int64_t)(s.seq.row0 + ri) * a.out_stride + (int64_t)rh * D + c8 * 8) =
-                            *reinterpret_cast<const uint4 *>(rows_out + r * D + ((c8 ^ (r & 7)) << 3));
-                    }
-                }
-                __syncwarp();
-            } else if (alive) {
-                // a share of an item: unscaled sums, stored channels in order
-                float *part = a.ws + (size_t)args.n_slots * kDescInts +
-                              (((size_t)blockIdx.x * 2 + (s.t0 == 0 ? 1 : 0)) * 2 * kBlock + blk * kBlock + row) * partial_stride(D);
-#pragma unroll 1
-                for (int c0 = 0; c0 < D; c0 += 32) {
-                    float x[32];
-                    if (work) {
-                        tmem_ld32(o_addr + c0, x);
-                        tmem_wait_ld32(x);
-                    }
-                    if (row < rows) {
-#pragma unroll
-                        for (int c = 0; c < 32; c += 8) {
-                            const bool some = work && ref != -CUDART_INF_F;
-                            *reinterpret_cast<float4 *>(part + c0 + c) = some ? make_float4(x[c], x[c + 2], x[c + 4], x[c + 6]) : make_float4(0.f, 0.f, 0.f, 0.f);
-                            *reinterpret_cast<float4 *>(part + c0 + c + 4) = some ? make_float4(x[c + 1], x[c + 3], x[c + 5], x[c + 7]) : make_float4(0.f, 0.f, 0.f, 0.f);
-                        }
-                    }
-                }
-                if (row < rows) {
-                    part[D] = ref == -CUDART_INF_F ? ref : ref * rs;
-                    part[D + 1] = l;
-                }
-                if (s.t0 == 0 && blk == 0 && row == 0) {
-                    desc[1] = s.seq.row0; desc[2] = s.seq.n; desc[3] = s.hk; desc[4] = s.m;
-                    desc[5] = (int)((s.item_end - 1) / ups - blockIdx.x + 1);
-                    desc[0] = 1;
-                }
+            if (alive)
+                write_rows<T, D>(args, s, blk, rows, row_base, work, o_addr, ref, l, rs, q_tile, out_channel[blk], whole,
+                                 a.ws + (size_t)args.n_slots * kDescInts + (((size_t)blockIdx.x * 2 + (s.t0 == 0 ? 1 : 0)) * 2 * kBlock + blk * kBlock) * partial_stride(D));
+            if (alive && !whole && s.t0 == 0 && tid == 0) {
+                desc[1] = s.seq.row0; desc[2] = s.seq.n; desc[3] = s.hk; desc[4] = s.m;
+                desc[5] = s.parts;
+                desc[0] = 1;
             }
             tc_fence_before();
         }
@@ -697,7 +834,7 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    if (warp == 12) tmem_dealloc(tmem, 512);
+    if (warp == 0) tmem_dealloc(tmem, 512);
 }
 
 int prefill_slots(const skvq_paged_config &cfg, const skvq_paged_batch &batch)
