@@ -163,6 +163,19 @@ __device__ __forceinline__ bool mbar_wait_cycles(uint32_t bar, uint32_t parity)
     }
 }
 
+// Two elements of the tensors' type in a register, as floats and back (rounded).
+template <typename T> __device__ __forceinline__ float2 unpack2(uint32_t v);
+template <> __device__ __forceinline__ float2 unpack2<__half>(uint32_t v) { return __half22float2(*reinterpret_cast<const __half2 *>(&v)); }
+template <> __device__ __forceinline__ float2 unpack2<__nv_bfloat16>(uint32_t v) { return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xFFFF0000u)); }
+template <typename T> __device__ __forceinline__ uint32_t pack2(float lo, float hi);
+template <> __device__ __forceinline__ uint32_t pack2<__half>(float lo, float hi) { return h2(lo, hi); }
+template <> __device__ __forceinline__ uint32_t pack2<__nv_bfloat16>(float lo, float hi)
+{
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+
 // Position 0..7 inside a run of eight operand channels -> stored channel.
 __device__ __forceinline__ int channel_at(int pos) { return (pos >> 1) + 4 * (pos & 1); }
 
@@ -231,111 +244,132 @@ __device__ __noinline__ void next_segment(const PrefillArgs &a, const long long 
     s.valid = 1;
 }
 
+// What the functions below need of the launch arguments, by value: read through a reference, every field is a memory access again after
+// every barrier.
+struct PContext {
+    const void *q;
+    void *out;
+    float *lse;
+    int64_t q_stride, out_stride;
+    const float2 *rope;
+    const int32_t *reorder_k, *reorder_v;
+    int rot_dim, interleaved, n_q_heads;
+    float sm_scale;
+};
+
 // The queries of a row block as the K-major A operand: rotated, rounded to T, reordered, scaled by a power of two per row; and the source
 // channel of every output column.  Not inlined, like write_rows: what these keep in registers would spill in the loop over tiles.
 template <typename T, int D>
-__device__ __noinline__ void prepare_queries(const PrefillArgs &args, const PSegment &s, int blk, int rows, int row_base, float sign, uint8_t *q_tile, T *raw,
+__device__ __noinline__ void prepare_queries(const PContext ctx, const PSegment &s, int rows, int row_base, float sign, uint8_t *q_tile, T *raw,
                                              float *row_scale, uint16_t *out_channel)
 {
     using Geo = PGeo<D>;
-    const PagedAttnArgs &a = args.a;
-    const PagedArgs &p = a.p;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-        // ---- queries of the block: a warp per row; lane: operand positions C lane .. C lane + C - 1
-        constexpr int C = D / 32;
-        struct alignas(sizeof(T) * C) Piece { T v[C]; };
-        int from[C];
+    const int rep = s.it.rep, hk = s.hk, row0 = s.seq.row0, first_pos = s.seq.len - s.seq.n;
+    // ---- queries of the block: a warp per row; lane: operand positions C lane .. C lane + C - 1
+    constexpr int C = D / 32;
+    int from[C];
 #pragma unroll
-        for (int k = 0; k < C; ++k) {
-            const int pos = lane * C + k, c = (pos & ~7) + channel_at(pos & 7);
-            from[k] = p.c.reorder_k ? p.c.reorder_k[s.hk * D + c] & (D - 1) : c;
-        }
-        for (int c = threadIdx.x & (kBlock - 1); c < D; c += kBlock) {
-            const int st = (c & ~7) + channel_at(c & 7);
-            out_channel[c] = (uint16_t)(p.c.reorder_v ? p.c.reorder_v[s.hk * D + st] & (D - 1) : st);
-        }
-        const float2 *rope = static_cast<const float2 *>(p.rope.table);
-        const int half = p.rope.rot_dim / 2;
-        // four rows at a time: their loads are in flight together
+    for (int k = 0; k < C; ++k) {
+        const int pos = lane * C + k, c = (pos & ~7) + channel_at(pos & 7);
+        from[k] = ctx.reorder_k ? ctx.reorder_k[hk * D + c] & (D - 1) : c;
+    }
+    for (int c = threadIdx.x & (kBlock - 1); c < D; c += kBlock) {
+        const int st = (c & ~7) + channel_at(c & 7);
+        out_channel[c] = (uint16_t)(ctx.reorder_v ? ctx.reorder_v[hk * D + st] & (D - 1) : st);
+    }
+    const float2 *rope = ctx.rope;
+    const int rot_dim = ctx.rot_dim, interleaved = ctx.interleaved, half = rot_dim / 2;
+    // four rows at a time: their loads are in flight together
 #pragma unroll 1
-        for (int r0 = (warp & 3) * 32; r0 < (warp & 3) * 32 + 32; r0 += 4) {
-            Piece own[4];
-            float2 cs[4][C];
-            bool turn[4];
+    for (int r0 = (warp & 3) * 32; r0 < (warp & 3) * 32 + 32; r0 += 4) {
+        float x[4][C], mx[4];
+        float2 cs[4][C];
+        bool turn[4];
+        auto put = [&]() {      // the four rows into shared memory, in the tensors' type
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                const int r = r0 + k, i = (row_base + r) / s.it.rep, head = s.hk * s.it.rep + (row_base + r) % s.it.rep, pos = s.seq.len - s.seq.n + i;
-                const bool have = r < rows && sign != 0.f;
-                turn[k] = have && rope && pos >= 0;
+                T *dst = raw + k * D + lane * C;
+                if constexpr (C == 4) *reinterpret_cast<uint2 *>(dst) = make_uint2(pack2<T>(x[k][0], x[k][1]), pack2<T>(x[k][2], x[k][3]));
+                else *reinterpret_cast<uint32_t *>(dst) = pack2<T>(x[k][0], x[k][1]);
+            }
+        };
 #pragma unroll
-                for (int e = 0; e < C; ++e) own[k].v[e] = Elem<T>::from_float(0.f);
-                if (have) own[k] = *reinterpret_cast<const Piece *>(static_cast<const T *>(a.q) + (int64_t)(s.seq.row0 + i) * a.q_stride + (int64_t)head * D + lane * C);
-                if (turn[k]) {
+        for (int k = 0; k < 4; ++k) {
+            const int r = r0 + k, i = (row_base + r) / rep, head = hk * rep + (row_base + r) - i * rep, pos = first_pos + i;
+            const bool have = r < rows && sign != 0.f;
+            turn[k] = have && rope && pos >= 0;
+            uint2 w = make_uint2(0u, 0u);
+            if (have) {
+                const T *src = static_cast<const T *>(ctx.q) + (int64_t)(row0 + i) * ctx.q_stride + (int64_t)head * D + lane * C;
+                if constexpr (C == 4) w = *reinterpret_cast<const uint2 *>(src);
+                else w.x = *reinterpret_cast<const uint32_t *>(src);
+            }
+            if (turn[k]) {
 #pragma unroll
-                    for (int e = 0; e < C; ++e) {
-                        const int c = lane * C + e;
-                        if (c < p.rope.rot_dim) cs[k][e] = rope[(int64_t)pos * half + (p.rope.interleaved ? c >> 1 : (c >= half ? c - half : c))];
-                    }
+                for (int e = 0; e < C; ++e) {
+                    const int c = lane * C + e;
+                    if (c < rot_dim) cs[k][e] = rope[(int64_t)pos * half + (interleaved ? c >> 1 : (c >= half ? c - half : c))];
                 }
             }
-            if (rope) {
-#pragma unroll
-                for (int k = 0; k < 4; ++k) *reinterpret_cast<Piece *>(raw + k * D + lane * C) = own[k];
-                __syncwarp();
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    if (!turn[k]) continue;
-#pragma unroll
-                    for (int e = 0; e < C; ++e) {
-                        const int c = lane * C + e;
-                        if (c < p.rope.rot_dim) {
-                            const bool second = p.rope.interleaved ? c & 1 : c >= half;
-                            const int partner = p.rope.interleaved ? c ^ 1 : (second ? c - half : c + half);
-                            const float mine = Elem<T>::to_float(own[k].v[e]), other = Elem<T>::to_float(raw[k * D + partner]);
-                            own[k].v[e] = Elem<T>::from_float(second ? rotate_second(other, mine, cs[k][e].x, cs[k][e].y) : rotate_first(mine, other, cs[k][e].x, cs[k][e].y));
-                        }
-                    }
-                }
-                __syncwarp();
-            }
-#pragma unroll
-            for (int k = 0; k < 4; ++k) *reinterpret_cast<Piece *>(raw + k * D + lane * C) = own[k];
-            __syncwarp();
-            float x[4][C], mx[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                mx[k] = 0.f;
-#pragma unroll
-                for (int e = 0; e < C; ++e) { x[k][e] = Elem<T>::to_float(raw[k * D + from[e]]); mx[k] = fmaxf(mx[k], fabsf(x[k][e])); }
-            }
-            __syncwarp();
-#pragma unroll
-            for (int d = 16; d > 0; d >>= 1)
-#pragma unroll
-                for (int k = 0; k < 4; ++k) mx[k] = fmaxf(mx[k], __shfl_xor_sync(0xffffffffu, mx[k], d));
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const int r = r0 + k;
-                float up = 1.f;      // the row's largest to [2^4, 2^5): exact, and far from fp16's ends whatever the type's range
-                if (mx[k] > 0.f && mx[k] < CUDART_INF_F) up = __int_as_float((127 + min(4 - (__float_as_int(mx[k]) >> 23) + 127, 60)) << 23);
-                if (lane == 0) row_scale[r] = (sign == 0.f ? 1.f : fabsf(a.sm_scale)) * 1.4426950408889634f / up;
-                uint8_t *dst = q_tile + r * 128 + ((lane * C) >> 6) * Geo::HALF_BYTES + ((((lane * C) >> 3 & 7) ^ (r & 7)) << 4) + ((lane * C) & 7) * 2;
-                const float f = up * sign;
-                if constexpr (C == 4) *reinterpret_cast<uint2 *>(dst) = make_uint2(h2(x[k][0] * f, x[k][1] * f), h2(x[k][2] * f, x[k][3] * f));
-                else *reinterpret_cast<uint32_t *>(dst) = h2(x[k][0] * f, x[k][1] * f);
-            }
+            const float2 u = unpack2<T>(w.x), v = unpack2<T>(w.y);
+            x[k][0] = u.x;
+            x[k][1] = u.y;
+            if constexpr (C == 4) { x[k][2] = v.x; x[k][3] = v.y; }
         }
+        put();
+        __syncwarp();
+        if (rope) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+#pragma unroll
+                for (int e = 0; e < C; ++e) {
+                    const int c = lane * C + e;
+                    if (turn[k] && c < rot_dim) {
+                        const bool second = interleaved ? c & 1 : c >= half;
+                        const int partner = interleaved ? c ^ 1 : (second ? c - half : c + half);
+                        const float mine = x[k][e], other = Elem<T>::to_float(raw[k * D + partner]);
+                        x[k][e] = second ? rotate_second(other, mine, cs[k][e].x, cs[k][e].y) : rotate_first(mine, other, cs[k][e].x, cs[k][e].y);
+                    }
+                }
+            }
+            __syncwarp();
+            put();
+            __syncwarp();
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            mx[k] = 0.f;
+#pragma unroll
+            for (int e = 0; e < C; ++e) { x[k][e] = Elem<T>::to_float(raw[k * D + from[e]]); mx[k] = fmaxf(mx[k], fabsf(x[k][e])); }
+        }
+        __syncwarp();
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) mx[k] = fmaxf(mx[k], __shfl_xor_sync(0xffffffffu, mx[k], d));
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int r = r0 + k;
+            float up = 1.f;      // the row's largest to [2^4, 2^5): exact, and far from fp16's ends whatever the type's range
+            if (mx[k] > 0.f && mx[k] < CUDART_INF_F) up = __int_as_float((127 + min(4 - (__float_as_int(mx[k]) >> 23) + 127, 60)) << 23);
+            if (lane == 0) row_scale[r] = (sign == 0.f ? 1.f : fabsf(ctx.sm_scale)) * 1.4426950408889634f / up;
+            uint8_t *dst = q_tile + r * 128 + ((lane * C) >> 6) * Geo::HALF_BYTES + ((((lane * C) >> 3 & 7) ^ (r & 7)) << 4) + ((lane * C) & 7) * 2;
+            const float f = up * sign;
+            if constexpr (C == 4) *reinterpret_cast<uint2 *>(dst) = make_uint2(h2(x[k][0] * f, x[k][1] * f), h2(x[k][2] * f, x[k][3] * f));
+            else *reinterpret_cast<uint32_t *>(dst) = h2(x[k][0] * f, x[k][1] * f);
+        }
+    }
 }
 
 // The result of a row block: finished rows, or (a share of an item) sums that the merge kernel joins.
 template <typename T, int D>
-__device__ __noinline__ void write_rows(const PrefillArgs &args, const PSegment &s, int blk, int rows, int row_base, bool work, uint32_t o_addr, float ref, float l,
+__device__ __noinline__ void write_rows(const PContext ctx, const PSegment &s, int rows, int row_base, bool work, uint32_t o_addr, float ref, float l,
                                         float rs, uint8_t *q_tile, const uint16_t *out_channel, bool whole, float *part)
 {
-    const PagedAttnArgs &a = args.a;
-    const skvq_paged_config &cfg = a.p.cfg;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, row = threadIdx.x & (kBlock - 1);
-    const int i = (row_base + row) / s.it.rep, head = s.hk * s.it.rep + (row_base + row) % s.it.rep;
+    const int rep = s.it.rep, hk = s.hk, row0 = s.seq.row0;
+    const int i = (row_base + row) / rep, head = hk * rep + (row_base + row) - i * rep;
     if (whole) {
         const float inv = ref == -CUDART_INF_F ? 0.f : 1.f / l;
         T *rows_out = reinterpret_cast<T *>(q_tile);      // [128][D], 16-byte pieces of a row at piece ^ (row & 7); all products have been read
@@ -352,15 +386,15 @@ __device__ __noinline__ void write_rows(const PrefillArgs &args, const PSegment 
                 rows_out[row * D + ((((dst >> 3) ^ (row & 7))) << 3) + (dst & 7)] = Elem<T>::from_float(work && ref != -CUDART_INF_F ? x[c] * inv : 0.f);
             }
         }
-        if (a.lse && row < rows )
-            a.lse[(int64_t)(s.seq.row0 + i) * cfg.n_q_heads + head] = ref == -CUDART_INF_F ? ref : (ref * rs + log2f(l) - kPOffset) * 0.6931471805599453f;
+        if (ctx.lse && row < rows )
+            ctx.lse[(int64_t)(row0 + i) * ctx.n_q_heads + head] = ref == -CUDART_INF_F ? ref : (ref * rs + log2f(l) - kPOffset) * 0.6931471805599453f;
         __syncwarp();
         constexpr int PER_ROW = D / 8;
         for (int e = lane; e < 32 * PER_ROW; e += 32) {      // this warp's 32 rows, 16 bytes a lane
             const int r = (warp & 3) * 32 + e / PER_ROW, c8 = e % PER_ROW;
             if (r < rows ) {
-                const int ri = (row_base + r) / s.it.rep, rh = s.hk * s.it.rep + (row_base + r) % s.it.rep;
-                *reinterpret_cast<uint4 *>(static_cast<T *>(a.out) + (int64_t)(s.seq.row0 + ri) * a.out_stride + (int64_t)rh * D + c8 * 8) =
+                const int ri = (row_base + r) / rep, rh = hk * rep + (row_base + r) - ri * rep;
+                *reinterpret_cast<uint4 *>(static_cast<T *>(ctx.out) + (int64_t)(row0 + ri) * ctx.out_stride + (int64_t)rh * D + c8 * 8) =
                     *reinterpret_cast<const uint4 *>(rows_out + r * D + ((c8 ^ (r & 7)) << 3));
             }
         }
@@ -631,6 +665,8 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
         const float sign = a.sm_scale < 0.f ? -1.f : (a.sm_scale == 0.f ? 0.f : 1.f);
         uint8_t *q_tile = smem + Geo::Q + blk * Geo::TILE_BYTES;
         T *raw = reinterpret_cast<T *>(smem + Geo::GATHER) + warp * 4 * D;
+        const PContext ctx{a.q, a.out, a.lse, a.q_stride, a.out_stride, static_cast<const float2 *>(p.rope.table), p.c.reorder_k, p.c.reorder_v,
+                           p.rope.rot_dim, p.rope.interleaved, cfg.n_q_heads, a.sm_scale};
         uint32_t n = 0, ns = 0;      // tiles so far (both blocks'), score tiles of this block so far
         // ---- the block's products, issued by its first warp
         constexpr uint32_t kIdescS = idesc_f16_f32(kBlock, kBlock);
@@ -674,7 +710,7 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
             const bool work = s.t0 < s.t1 && rows > 0;
             if (__any_sync(0xffffffffu, *fail)) alive = false;
             if (work) {
-                prepare_queries<T, D>(args, s, blk, rows, row_base, sign, q_tile, raw, row_scale + blk * kBlock, out_channel[blk]);
+                prepare_queries<T, D>(ctx, s, rows, row_base, sign, q_tile, raw, row_scale + blk * kBlock, out_channel[blk]);
                 proxy_fence();
                 role_sync();      // the operand, row_scale and out_channel of the whole block
                 if ((warp & 3) == 0) issue_scores(n);
@@ -821,7 +857,7 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
                 tc_fence_after();
             }
             if (alive)
-                write_rows<T, D>(args, s, blk, rows, row_base, work, o_addr, ref, l, rs, q_tile, out_channel[blk], whole,
+                write_rows<T, D>(ctx, s, rows, row_base, work, o_addr, ref, l, rs, q_tile, out_channel[blk], whole,
                                  a.ws + (size_t)args.n_slots * kDescInts + (((size_t)blockIdx.x * 2 + (s.t0 == 0 ? 1 : 0)) * 2 * kBlock + blk * kBlock) * partial_stride(D));
             if (alive && !whole && s.t0 == 0 && tid == 0) {
                 desc[1] = s.seq.row0; desc[2] = s.seq.n; desc[3] = s.hk; desc[4] = s.m;
