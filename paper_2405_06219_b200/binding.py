@@ -397,9 +397,25 @@ _DTYPES = {torch.float16: SKVQ_F16, torch.bfloat16: SKVQ_BF16, torch.float32: SK
 _HERE = contextlib.nullcontext()
 
 
-def _on(device: torch.device):
+def _on(index: int):
     """The calls launch on the current device: make it the tensors' own."""
-    return _HERE if torch.cuda.current_device() == device.index else torch.cuda.device(device)
+    return _HERE if torch.cuda.current_device() == index else torch.cuda.device(index)
+
+
+def _raw_stream(index: int, stream) -> int:
+    return torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream
+
+
+def _ref(struct):
+    return None if struct is None else ctypes.byref(struct)
+
+
+def _rope_operand(x, y, dtype, T: int, D: int, index: int) -> SkvqRopeTensor:
+    assert x.get_device() == y.get_device() == index and x.dtype == y.dtype == dtype, "tensors of one type on the table's device"
+    shape = x.shape
+    xs, ys = x.stride(), y.stride()
+    assert len(shape) == 3 and y.shape == shape and shape[0] == T and shape[2] == D and (D == 1 or (xs[2] == 1 and ys[2] == 1)), "rows [T, heads, D]"
+    return SkvqRopeTensor(x.data_ptr(), y.data_ptr(), xs[0], xs[1], ys[0], ys[1], shape[1])
 
 
 class RopeTable:
@@ -410,6 +426,7 @@ class RopeTable:
         assert table.dim() == 3 and tuple(table.shape[1:]) == (rot_dim // 2, 2), "table: [positions, rot_dim/2, 2]"
         self.table, self.rot_dim, self.interleaved, self.device = table, rot_dim, bool(interleaved), table.device
         self.struct = SkvqRope(table.data_ptr(), rot_dim, 1 if interleaved else 0, table.shape[0])
+        self.index = table.get_device()
 
     @classmethod
     def build(cls, rot_dim: int, n_positions: int, interleaved: bool = False, base: float = 10000.0,
@@ -418,25 +435,20 @@ class RopeTable:
         """The table of positions 0..n_positions-1 for one of the SKVQ_ROPE_* scalings."""
         f, amplitude = skvq_rope_frequencies(rot_dim, SkvqRopeScaling(kind, original_positions, base, factor, fast, slow))
         table = torch.empty((n_positions, rot_dim // 2, 2), dtype=torch.float32, device=device)
-        with _on(table.device):
+        with _on(table.get_device()):
             skvq_rope_table(f, amplitude, 0, n_positions, table)
         return cls(table, rot_dim, interleaved)
 
     def apply(self, positions, q, q_out=None, k=None, k_out=None, inverse: bool = False, status=None, stream=None) -> None:
         """Rotate q [T, heads, D] and, in the same launch, k: into q_out/k_out, in place without them.  positions: int32 [T]."""
-        q_out, k_out = (q if q_out is None else q_out), (k if k_out is None else k_out)
         T, _, D = q.shape
-        assert positions.dtype == torch.int32 and positions.is_contiguous() and positions.numel() == T
-        ops = []
-        for x, y in ((q, q_out), (k, k_out)):
-            if x is None:
-                ops.append(None)
-                continue
-            assert x.device == y.device == positions.device == self.device and x.dtype == y.dtype == q.dtype
-            assert x.shape == y.shape and x.shape[0] == T and x.shape[2] == D and (D == 1 or (x.stride(2) == 1 and y.stride(2) == 1))
-            ops.append(SkvqRopeTensor(x.data_ptr(), y.data_ptr(), x.stride(0), x.stride(1), y.stride(0), y.stride(1), x.shape[1]))
-        with _on(self.device):
-            skvq_rope_apply(self.struct, _DTYPES[q.dtype], D, ops[0], ops[1], positions, T, 1 if inverse else 0, status, stream)
+        index, dtype = self.index, q.dtype
+        assert positions.dtype == torch.int32 and positions.is_contiguous() and positions.numel() == T and positions.get_device() == index
+        a = _rope_operand(q, q if q_out is None else q_out, dtype, T, D, index)
+        b = None if k is None else _rope_operand(k, k if k_out is None else k_out, dtype, T, D, index)
+        with _on(index):
+            _check(lib().skvq_rope_apply(_ref(self.struct), _DTYPES[dtype], D, _ref(a), _ref(b), positions.data_ptr(), T,
+                                         1 if inverse else 0, _dptr(status), _raw_stream(index, stream)), "skvq_rope_apply")
 
 
 class SkvqPagedCache:
@@ -476,6 +488,7 @@ class SkvqPagedCache:
         self.struct = SkvqPagedCacheStruct(*[_dptr(t) if t is None or t.numel() else None for t in (
             self.k_codes, self.v_codes, self.k_meta, self.v_meta, self.k_win, self.v_win, self.reorder_k, self.reorder_v,
             self.alpha_k, self.alpha_v, self.status)])
+        self.index = self.k_codes.get_device()
 
     def batch(self, page_table, lens, starts, n_tokens: int, max_new: int, max_len: int, slots=None) -> SkvqPagedBatch:
         """The sequences of a step: page_table int32 [n, max_pages], lens int32 [n] (tokens including the new ones), starts
@@ -488,26 +501,34 @@ class SkvqPagedCache:
         b.keep = (page_table, lens, starts, slots)
         return b
 
-    def _rows(self, x, batch, heads):
-        assert x.device == self.device and x.dtype == self.dtype and x.dim() == 3 and x.shape[0] >= batch.n_tokens
+    def _rows(self, x, batch, heads) -> int:
+        """Checks packed rows [T, heads, D] and gives their token stride."""
+        shape, stride = x.shape, x.stride()
         D = self.cfg.head_dim
-        assert tuple(x.shape[1:]) == (heads, D) and x.stride(2) == 1 and (heads == 1 or x.stride(1) == D), "rows: heads and channels contiguous"
-        return x.stride(0) if x.shape[0] > 1 else heads * D
+        assert x.get_device() == self.index and x.dtype == self.dtype and len(shape) == 3 and shape[0] >= batch.n_tokens
+        assert shape[1] == heads and shape[2] == D and stride[2] == 1 and (heads == 1 or stride[1] == D), "rows: heads and channels contiguous"
+        return stride[0] if shape[0] > 1 else heads * D
 
     def append(self, batch, k, v, rope=None, stream=None) -> None:
         """k, v: [T, Hkv, D] in the cache's type, any token stride that is a multiple of 8."""
-        ks, vs = self._rows(k, batch, self.cfg.n_kv_heads), self._rows(v, batch, self.cfg.n_kv_heads)
-        with _on(self.device):
-            skvq_paged_append(self.cfg, self.struct, batch, None if rope is None else rope.struct, k, v, ks, vs, stream)
+        H, index = self.cfg.n_kv_heads, self.index
+        ks, vs = self._rows(k, batch, H), self._rows(v, batch, H)
+        with _on(index):
+            _check(lib().skvq_paged_append(_ref(self.cfg), _ref(self.struct), _ref(batch), None if rope is None else _ref(rope.struct), k.data_ptr(),
+                                           v.data_ptr(), ks, vs, _raw_stream(index, stream)), "skvq_paged_append")
 
     def read(self, batch, k=None, v=None, window: bool = True, stream=None):
         """The new tokens' rows of the cache as values [T, Hkv, D], in source order; into k and v where they are given."""
-        shape = (batch.n_tokens, self.cfg.n_kv_heads, self.cfg.head_dim)
-        with _on(self.device):
-            k = torch.empty(shape, dtype=self.dtype, device=self.device) if k is None else k
-            v = torch.empty(shape, dtype=self.dtype, device=self.device) if v is None else v
-            skvq_paged_read(self.cfg, self.struct, batch, 1 if window else 0, k, v, self._rows(k, batch, shape[1]),
-                            self._rows(v, batch, shape[1]), stream)
+        H, index = self.cfg.n_kv_heads, self.index
+        with _on(index), (_HERE if stream is None else torch.cuda.stream(stream)):
+            if k is None and v is None:
+                k, v = torch.empty((2, batch.n_tokens, H, self.cfg.head_dim), dtype=self.dtype, device=self.device).unbind(0)
+            elif k is None or v is None:
+                other = torch.empty((batch.n_tokens, H, self.cfg.head_dim), dtype=self.dtype, device=self.device)
+                k, v = (other, v) if k is None else (k, other)
+            ks, vs = self._rows(k, batch, H), self._rows(v, batch, H)
+            _check(lib().skvq_paged_read(_ref(self.cfg), _ref(self.struct), _ref(batch), 1 if window else 0, k.data_ptr(), v.data_ptr(), ks, vs,
+                                         _raw_stream(index, stream)), "skvq_paged_read")
         return k, v
 
     def attention(self, batch, q, sm_scale, out=None, causal: bool = True, rope=None, lse=None, n_splits: int = 0,
@@ -515,16 +536,22 @@ class SkvqPagedCache:
         """q [T, Hq, D] -> out [T, Hq, D]; lse: optional float32 [T, Hq].  Without a workspace (a tensor of at least
         skvq_paged_workspace_size bytes) each call takes one of its own from torch's allocator on the stream it runs on, so calls
         on several streams and captured graphs never share it."""
-        c = self.cfg
-        with _on(self.device), (_HERE if stream is None else torch.cuda.stream(stream)):
-            out = torch.empty((batch.n_tokens, c.n_q_heads, c.head_dim), dtype=self.dtype, device=self.device) if out is None else out
-            ws = workspace
-            if ws is None:
-                need = skvq_paged_workspace_size(c, batch, n_splits)
-                ws = torch.empty((need + 15) // 16 * 4, dtype=torch.float32, device=self.device)
-            assert ws.device == self.device and (lse is None or (lse.dtype == torch.float32 and lse.is_contiguous() and lse.device == self.device and
-                                                                 lse.numel() >= batch.n_tokens * c.n_q_heads))
-            args = SkvqPagedAttnArgs(sm_scale, 1 if causal else 0, n_splits, ws.data_ptr(), ws.numel() * ws.element_size())
-            skvq_paged_attention(c, self.struct, batch, None if rope is None else rope.struct, q, self._rows(q, batch, c.n_q_heads),
-                                 out, self._rows(out, batch, c.n_q_heads), lse, args, stream)
+        c, index = self.cfg, self.index
+        H = c.n_q_heads
+        qs = self._rows(q, batch, H)
+        with _on(index), (_HERE if stream is None else torch.cuda.stream(stream)):
+            if out is None:
+                out, os_ = torch.empty((batch.n_tokens, H, c.head_dim), dtype=self.dtype, device=self.device), H * c.head_dim
+            else:
+                os_ = self._rows(out, batch, H)
+            if workspace is None:
+                size = skvq_paged_workspace_size(c, batch, n_splits)
+                workspace = torch.empty(max(size, 16), dtype=torch.uint8, device=self.device)
+            else:
+                assert workspace.get_device() == index and workspace.is_contiguous()
+                size = workspace.numel() * workspace.element_size()
+            assert lse is None or (lse.dtype == torch.float32 and lse.is_contiguous() and lse.get_device() == index and lse.numel() >= batch.n_tokens * H)
+            args = SkvqPagedAttnArgs(sm_scale, 1 if causal else 0, n_splits, workspace.data_ptr(), size)
+            _check(lib().skvq_paged_attention(_ref(c), _ref(self.struct), _ref(batch), None if rope is None else _ref(rope.struct), q.data_ptr(), qs,
+                                              out.data_ptr(), os_, _dptr(lse), _ref(args), _raw_stream(index, stream)), "skvq_paged_attention")
         return out
