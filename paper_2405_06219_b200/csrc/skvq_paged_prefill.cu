@@ -1,16 +1,18 @@
 // skvq_paged_attention for many query rows per (sequence, KV head): prompts and chunks of prompts, on tcgen05.
 //
 // One CTA per SM works on items of up to 256 packed rows (row = new token * (Hq/Hkv) + query head) of one KV head, as two row
-// blocks of 128, over 128-token tiles of the cache.  Two kinds of warps, ordered by mbarriers:
+// blocks of 128, over 128-token tiles of the cache.  Three kinds of warps, ordered by mbarriers:
 //   dequantizers  4 warps, a thread per token of the tile: codes and parameters come from the pages into registers one tile ahead,
 //                 leave as fp16(h c + z) (one rounding) in the 128-byte swizzle that both products read -- the key tile as the
 //                 K-major B operand of Q K^T, the value tile, same picture, as the MN-major B operand of P V; window tokens are
 //                 copied.  Two buffers of each.
-//   softmax       2 x 4 warps, a thread per row: S from tensor memory, probabilities back, in place, as the fp16 A operand; the row sum in fp32.  One warp of each block issues the block's products: O += P V~, then, behind
-//                 it in the tensor core's queue, the next tile's S = Q K~^T.  The reference of a row is raised, and O multiplied,
-//                 only when a score exceeds it by more than 2^kLazy: O is then read and written about once or twice per item.
-// While one block's scores become probabilities, the tensor core works for the other block.  Twelve warps leave each thread 168
-// registers; a warp more would cut that to 128 (16 warps' worth).
+//   softmax       2 x 4 warps, a thread per row: S from tensor memory, probabilities back, in place, as the fp16 A operand; the row
+//                 sum in fp32.  The reference of a row is raised, and O multiplied, only when a score exceeds it by more than
+//                 2^kLazy: O is then read and written about once or twice per item.
+//   issuers       a warp per row block: O += P V~, then, behind it in the tensor core's queue, the next tile's S = Q K~^T.  (Issuing
+//                 blocks while the queue is full: from a softmax warp it cost the whole block that time.)
+// A tile's scores come as two halves of 64 tokens with a buffer each: while one half becomes probabilities, the products of the other
+// half and of the other block run, so a softmax warp finds its next scores waiting.
 // A nibble pair (i, i + 4) of a code word becomes two neighbouring fp16, so the channels of each run of eight lie in the order
 // 0 4 1 5 2 6 3 7 in the operands; the queries are laid out the same way and the outputs put back.
 // Items are laid end to end, priced in tiles (causal limits included), and cut into equal runs, one per CTA; an item that several
@@ -35,7 +37,7 @@ using namespace tc5;
 constexpr int kBlock = 128;                     // rows of a row block, tokens of a tile
 constexpr int kSoftmaxThreads = 2 * kBlock;     // warps 0-7
 constexpr int kDequantThreads = kBlock;         // warps 8-11
-constexpr int kPrefillThreads = kSoftmaxThreads + kDequantThreads;
+constexpr int kPrefillThreads = kSoftmaxThreads + kDequantThreads + 128;      // warps 12, 13 issue the products of a row block each
 constexpr float kLazy = 8.f;                    // log2 of how far a score may exceed its row's reference
 constexpr float kPOffset = 6.f;                 // probabilities are held times 2^6: up to 2^14 in fp16, down to 2^-30 of the reference
 
@@ -54,7 +56,7 @@ struct PGeo {
     static constexpr int V = 4 * TILE_BYTES;                   // 2 buffers
     static constexpr int GATHER = 6 * TILE_BYTES;              // per softmax warp: four rows of queries
     static constexpr int SMEM = GATHER + 8 * 4 * D * 2 + 1024;  // and room to align to 1024 bytes
-    static constexpr int TMEM_S = 0, TMEM_O = 256;             // columns: S (P in place) 2 x 128, O 2 x D
+    static constexpr int TMEM_S = 0, TMEM_O = 256;             // columns: S (P in place) 2 blocks x 2 halves x 64, O 2 x D
 };
 
 // Shared-memory matrix descriptors in the 128-byte swizzle.  K-major: 8-row groups 1024 bytes apart.  MN-major: 64-element runs of
@@ -244,8 +246,8 @@ __device__ __noinline__ void next_segment(const PrefillArgs &a, const long long 
     s.valid = 1;
 }
 
-// What the functions below need of the launch arguments, by value: read through a reference, every field is a memory access again after
-// every barrier.
+// What the functions below need of the launch arguments: copied once, in one trip, because a field read through the reference is a memory
+// access again after every barrier; and inside, because held by the caller the copies would spill in the loop over tiles.
 struct PContext {
     const void *q;
     void *out;
@@ -256,15 +258,21 @@ struct PContext {
     int rot_dim, interleaved, n_q_heads;
     float sm_scale;
 };
+__device__ __forceinline__ PContext context(const PagedAttnArgs &a)
+{
+    return PContext{a.q, a.out, a.lse, a.q_stride, a.out_stride, static_cast<const float2 *>(a.p.rope.table), a.p.c.reorder_k, a.p.c.reorder_v,
+                    a.p.rope.rot_dim, a.p.rope.interleaved, a.p.cfg.n_q_heads, a.sm_scale};
+}
 
 // The queries of a row block as the K-major A operand: rotated, rounded to T, reordered, scaled by a power of two per row; and the source
 // channel of every output column.  Not inlined, like write_rows: what these keep in registers would spill in the loop over tiles.
 template <typename T, int D>
-__device__ __noinline__ void prepare_queries(const PContext ctx, const PSegment &s, int rows, int row_base, float sign, uint8_t *q_tile, T *raw,
+__device__ __noinline__ void prepare_queries(const PagedAttnArgs &args, const PSegment &s, int rows, int row_base, float sign, uint8_t *q_tile, T *raw,
                                              float *row_scale, uint16_t *out_channel)
 {
     using Geo = PGeo<D>;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const PContext ctx = context(args);
     const int rep = s.it.rep, hk = s.hk, row0 = s.seq.row0, first_pos = s.seq.len - s.seq.n;
     // ---- queries of the block: a warp per row; lane: operand positions C lane .. C lane + C - 1
     constexpr int C = D / 32;
@@ -364,24 +372,25 @@ __device__ __noinline__ void prepare_queries(const PContext ctx, const PSegment 
 
 // The result of a row block: finished rows, or (a share of an item) sums that the merge kernel joins.
 template <typename T, int D>
-__device__ __noinline__ void write_rows(const PContext ctx, const PSegment &s, int rows, int row_base, bool work, uint32_t o_addr, float ref, float l,
+__device__ __noinline__ void write_rows(const PagedAttnArgs &args, const PSegment &s, int rows, int row_base, bool work, uint32_t o_addr, float ref, float l,
                                         float rs, uint8_t *q_tile, const uint16_t *out_channel, bool whole, float *part)
 {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, row = threadIdx.x & (kBlock - 1);
+    const PContext ctx = context(args);
     const int rep = s.it.rep, hk = s.hk, row0 = s.seq.row0;
     const int i = (row_base + row) / rep, head = hk * rep + (row_base + row) - i * rep;
     if (whole) {
         const float inv = ref == -CUDART_INF_F ? 0.f : 1.f / l;
         T *rows_out = reinterpret_cast<T *>(q_tile);      // [128][D], 16-byte pieces of a row at piece ^ (row & 7); all products have been read
 #pragma unroll 1
-        for (int c0 = 0; c0 < D; c0 += 32) {
-            float x[32];
+        for (int c0 = 0; c0 < D; c0 += 16) {
+            float x[16];
             if (work) {
-                tmem_ld32(o_addr + c0, x);
-                tmem_wait_ld32(x);
+                tmem_ld16f(o_addr + c0, x);
+                tmem_wait_ld16f(x);
             }
 #pragma unroll
-            for (int c = 0; c < 32; ++c) {
+            for (int c = 0; c < 16; ++c) {
                 const int dst = work ? out_channel[c0 + c] : c0 + c;
                 rows_out[row * D + ((((dst >> 3) ^ (row & 7))) << 3) + (dst & 7)] = Elem<T>::from_float(work && ref != -CUDART_INF_F ? x[c] * inv : 0.f);
             }
@@ -403,15 +412,15 @@ __device__ __noinline__ void write_rows(const PContext ctx, const PSegment &s, i
         // a share of an item: unscaled sums, stored channels in order
         part += row * partial_stride(D);
 #pragma unroll 1
-        for (int c0 = 0; c0 < D; c0 += 32) {
-            float x[32];
+        for (int c0 = 0; c0 < D; c0 += 16) {
+            float x[16];
             if (work) {
-                tmem_ld32(o_addr + c0, x);
-                tmem_wait_ld32(x);
+                tmem_ld16f(o_addr + c0, x);
+                tmem_wait_ld16f(x);
             }
             if (row < rows) {
 #pragma unroll
-                for (int c = 0; c < 32; c += 8) {
+                for (int c = 0; c < 16; c += 8) {
                     const bool some = work && ref != -CUDART_INF_F;
                     *reinterpret_cast<float4 *>(part + c0 + c) = some ? make_float4(x[c], x[c + 2], x[c + 4], x[c + 6]) : make_float4(0.f, 0.f, 0.f, 0.f);
                     *reinterpret_cast<float4 *>(part + c0 + c + 4) = some ? make_float4(x[c + 1], x[c + 3], x[c + 5], x[c + 7]) : make_float4(0.f, 0.f, 0.f, 0.f);
@@ -435,13 +444,13 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     long long *pre = reinterpret_cast<long long *>(smem + Geo::SMEM - 1024);
-    __shared__ __align__(8) uint64_t bars[12];
+    __shared__ __align__(8) uint64_t bars[22];
     __shared__ uint32_t tmem_sh;
     __shared__ int fail_sh;
     __shared__ long long scan_sh[16];
     __shared__ float row_scale[2 * kBlock];
     __shared__ uint16_t out_channel[2][D];      // source channel of every operand column, per row block
-    __shared__ PSegment seg_sh[3];              // of the two row blocks, of the dequantizers
+    __shared__ PSegment seg_sh[5];              // of the two row blocks' softmax, of the dequantizers, of the two issuers
     __shared__ uint32_t bad_sh[4];              // of the last four tiles: 16-token blocks without a page (a tile's is read until its
                                                 // probabilities are written, when the tile two further on may be in the making)
     const int tid = threadIdx.x, lane = tid & 31, B = p.batch.n_seqs;
@@ -487,7 +496,8 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
     // ---- barriers, tensor memory
     const uint32_t bar0 = smem_u32(bars);
     const uint32_t k_full = bar0, k_empty = bar0 + 16, v_full = bar0 + 32, v_empty = bar0 + 48;      // + 8 * buffer
-    const uint32_t s_full = bar0 + 64, pv_done = bar0 + 80;                                          // + 8 * row block
+    const uint32_t s_full = bar0 + 64, pv_done = bar0 + 96;                                          // + 16 * row block + 8 * half
+    const uint32_t p_full = bar0 + 128, q_full = bar0 + 160;                                        // the same; + 8 * row block
     if (tid == 0) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
@@ -495,8 +505,13 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
             mbar_init(k_empty + 8 * i, 2);      // both row blocks' products
             mbar_init(v_full + 8 * i, kDequantThreads);
             mbar_init(v_empty + 8 * i, 2);
-            mbar_init(s_full + 8 * i, 1);
-            mbar_init(pv_done + 8 * i, 1);
+            mbar_init(s_full + 16 * i, 1);
+            mbar_init(s_full + 16 * i + 8, 1);
+            mbar_init(pv_done + 16 * i, 1);
+            mbar_init(pv_done + 16 * i + 8, 1);
+            mbar_init(p_full + 16 * i, 4);      // an arrival per warp
+            mbar_init(p_full + 16 * i + 8, 4);
+            mbar_init(q_full + 8 * i, 4);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fail_sh = 0;
@@ -508,7 +523,7 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
     const uint32_t tmem = tmem_sh;
     const long long total = pre[B], ups = max((total + args.n_slots - 1) / args.n_slots, 1LL);
     int *desc = reinterpret_cast<int *>(a.ws) + (size_t)blockIdx.x * kDescInts;
-    if (tid < 3) {
+    if (tid < 5) {
         PSegment &first = seg_sh[tid];
         first.f = blockIdx.x * ups;
         first.f1 = min(first.f + ups, total);
@@ -527,29 +542,28 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
     // A wait that runs out is reported; the thread then goes through its loops without waiting or storing.
     bool alive = true;
     volatile int *fail = &fail_sh;
-    // The whole warp calls this; one lane polls (32 lanes polling twelve warps over kept shared memory so busy that every access to it
-    // took several hundred cycles).
-    auto wait = [&](uint32_t bar, uint32_t parity) {
-        bool ok = true;
-        if (alive && lane == 0) ok = mbar_wait_cycles(bar, parity);
-        if (!__shfl_sync(0xffffffffu, ok, 0)) {
+    auto wait = [&](uint32_t bar, uint32_t parity) {      // by whole warps
+        if (alive && !mbar_wait_cycles(bar, parity)) {
             alive = false;
             *fail = 1;
-            if (lane == 0) set_status(p.c.status, SKVQ_STATUS_COPY_TIMEOUT);
+            set_status(p.c.status, SKVQ_STATUS_COPY_TIMEOUT);
         }
     };
-    // A role is 128 threads: block 0, block 1, the dequantizers.
-    const int role = warp >> 2;
+    // A role is 128 threads (block 0, block 1, the dequantizers) or a warp (an issuer).
+    const int role = warp < 12 ? warp >> 2 : 3 + (warp & 1);
     const PSegment &s = seg_sh[role];
-    auto role_sync = [&]() { asm volatile("bar.sync %0, 128;" ::"r"(1 + role) : "memory"); };
+    auto role_sync = [&]() {
+        if (warp < 12) asm volatile("bar.sync %0, 128;" ::"r"(1 + role) : "memory");
+        else __syncwarp();
+    };
     auto next = [&]() {
         role_sync();
-        if ((tid & 127) == 0) next_segment(args, pre, ups, seg_sh[role]);
+        if ((warp < 12 ? tid & 127 : lane) == 0) next_segment(args, pre, ups, seg_sh[role]);
         role_sync();
         return s.valid != 0;
     };
 
-    if (warp >= 8) {
+    if (warp >= 8 && warp < 12) {
         // ================================================================ dequantizers
         const int row = tid - kSoftmaxThreads;      // token of the tile
         const int P = cfg.page_tokens, page_shift = __ffs(P) - 1;
@@ -594,7 +608,7 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
             int page_next = page_of(s.t0 + 1);
             for (int t = s.t0; t < s.t1; ++t, ++n) {
                 const uint32_t buf = n & 1, phase = (n >> 1) & 1;
-                if (__any_sync(0xffffffffu, *fail)) alive = false;
+                if (*fail) alive = false;
                 uint8_t *kt = smem + Geo::K + buf * Geo::TILE_BYTES + row * 128, *vt = smem + Geo::V + buf * Geo::TILE_BYTES + row * 128;
                 // one code word -> one 16-byte piece of the operand row
                 auto piece = [&](uint8_t *base, int c8, uint32_t w, uint32_t hh, uint32_t zz) {
@@ -657,6 +671,73 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
                 page_next = page_of(t + 2);
             }
         }
+    } else if (warp >= 12) {
+        // ================================================================ products of a row block
+        if (warp < 14) {
+        const int blk = warp & 1;
+        constexpr uint32_t kIdescS = idesc_f16_f32(kBlock, kBlock / 2);
+        constexpr uint32_t kIdescO = idesc_f16_f32(kBlock, D) | (1u << 16);      // B is MN-major
+        const uint32_t smem_base = smem_u32(smem);
+        // S = Q K~^T of half `hf` of tile number `tile`.  The whole warp runs these (addresses are warp-uniform), one lane issues.
+        auto issue_scores = [&](uint32_t tile, int hf) {
+            const uint32_t buf = tile & 1;
+            const uint64_t dq = desc_k_major(smem_base + Geo::Q + blk * Geo::TILE_BYTES), dk = desc_k_major(smem_base + Geo::K + buf * Geo::TILE_BYTES + hf * 64 * 128);
+            if (hf == 0) wait(k_full + 8 * buf, (tile >> 1) & 1);
+            tc_fence_after();
+            if (elect_one()) {
+#pragma unroll
+                for (int ks = 0; ks < D / 16; ++ks) {
+                    constexpr uint32_t half = Geo::HALF_BYTES >> 4;
+                    umma_f16(tmem + Geo::TMEM_S + blk * kBlock + hf * 64, dq + (ks >> 2) * half + (ks & 3) * 2, dk + (ks >> 2) * half + (ks & 3) * 2, kIdescS, ks > 0);
+                }
+                umma_commit(s_full + 16 * blk + 8 * hf);
+                if (hf) umma_commit(k_empty + 8 * buf);
+            }
+            __syncwarp();
+        };
+        auto issue_values = [&](uint32_t tile, int hf, bool first) {
+            const uint32_t buf = tile & 1;
+            const uint64_t dv = desc_mn_major(smem_base + Geo::V + buf * Geo::TILE_BYTES + hf * 64 * 128, Geo::HALF_BYTES);
+            if (hf == 0) wait(v_full + 8 * buf, (tile >> 1) & 1);
+            tc_fence_after();
+            if (elect_one()) {
+#pragma unroll
+                for (int ks = 0; ks < kBlock / 32; ++ks)
+                    umma_f16_ts(tmem + Geo::TMEM_O + blk * D, tmem + Geo::TMEM_S + blk * kBlock + hf * 64 + ks * 8, dv + ks * (2048 >> 4), kIdescO, !first || ks > 0);
+                umma_commit(pv_done + 16 * blk + 8 * hf);
+                if (hf) umma_commit(v_empty + 8 * buf);
+            }
+            __syncwarp();
+        };
+        uint32_t n = 0, ns = 0, nq = 0;      // tiles so far (both blocks'), of this block, items of this block
+        while (next()) {
+            if (*fail) alive = false;
+            if (s.it.rows() <= (s.m * 2 + blk) * kBlock) {
+                // A block without rows follows the tiles all the same: it frees the buffers on its side, and it must not reach a
+                // later item while a barrier is still two phases behind what it would wait for.
+                for (int t = s.t0; t < s.t1; ++t, ++n) {
+                    wait(k_full + 8 * (n & 1), (n >> 1) & 1);
+                    if (lane == 0) mbar_arrive(k_empty + 8 * (n & 1));
+                    wait(v_full + 8 * (n & 1), (n >> 1) & 1);
+                    if (lane == 0) mbar_arrive(v_empty + 8 * (n & 1));
+                }
+                continue;
+            }
+            if (s.t0 >= s.t1) continue;
+            wait(q_full + 8 * blk, nq & 1);
+            ++nq;
+            issue_scores(n, 0);
+            issue_scores(n, 1);
+            for (int t = s.t0; t < s.t1; ++t, ++n, ++ns) {
+#pragma unroll 1
+                for (int hf = 0; hf < 2; ++hf) {
+                    wait(p_full + 16 * blk + 8 * hf, ns & 1);
+                    issue_values(n, hf, t == s.t0 && hf == 0);
+                    if (t + 1 < s.t1) issue_scores(n + 1, hf);
+                }
+            }
+        }
+        }
     } else {
         // ================================================================ softmax
         const int blk = warp >> 2, row = tid & (kBlock - 1);                       // row block, row = lane of the tensor memory
@@ -665,128 +746,80 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
         const float sign = a.sm_scale < 0.f ? -1.f : (a.sm_scale == 0.f ? 0.f : 1.f);
         uint8_t *q_tile = smem + Geo::Q + blk * Geo::TILE_BYTES;
         T *raw = reinterpret_cast<T *>(smem + Geo::GATHER) + warp * 4 * D;
-        const PContext ctx{a.q, a.out, a.lse, a.q_stride, a.out_stride, static_cast<const float2 *>(p.rope.table), p.c.reorder_k, p.c.reorder_v,
-                           p.rope.rot_dim, p.rope.interleaved, cfg.n_q_heads, a.sm_scale};
-        uint32_t n = 0, ns = 0;      // tiles so far (both blocks'), score tiles of this block so far
-        // ---- the block's products, issued by its first warp
-        constexpr uint32_t kIdescS = idesc_f16_f32(kBlock, kBlock);
-        constexpr uint32_t kIdescO = idesc_f16_f32(kBlock, D) | (1u << 16);      // B is MN-major
-        const uint32_t smem_base = smem_u32(smem);
-        // S = Q K~^T of tile number `tile`.  The whole warp runs these (addresses are warp-uniform), one lane issues.
-        auto issue_scores = [&](uint32_t tile) {
-            const uint32_t buf = tile & 1;
-            const uint64_t dq = desc_k_major(smem_base + Geo::Q + blk * Geo::TILE_BYTES), dk = desc_k_major(smem_base + Geo::K + buf * Geo::TILE_BYTES);
-            wait(k_full + 8 * buf, (tile >> 1) & 1);
-            tc_fence_after();
-            if (elect_one()) {
-#pragma unroll
-                for (int ks = 0; ks < D / 16; ++ks) {
-                    constexpr uint32_t half = Geo::HALF_BYTES >> 4;
-                    umma_f16(tmem + Geo::TMEM_S + blk * kBlock, dq + (ks >> 2) * half + (ks & 3) * 2, dk + (ks >> 2) * half + (ks & 3) * 2, kIdescS, ks > 0);
-                }
-                umma_commit(s_full + 8 * blk);
-                umma_commit(k_empty + 8 * buf);
-            }
-            __syncwarp();
-        };
-        auto issue_values = [&](uint32_t tile, bool first) {
-            const uint32_t buf = tile & 1;
-            const uint64_t dv = desc_mn_major(smem_base + Geo::V + buf * Geo::TILE_BYTES, Geo::HALF_BYTES);
-            wait(v_full + 8 * buf, (tile >> 1) & 1);
-            tc_fence_after();
-            if (elect_one()) {
-#pragma unroll
-                for (int ks = 0; ks < kBlock / 16; ++ks)
-                    umma_f16_ts(tmem + Geo::TMEM_O + blk * D, tmem + Geo::TMEM_S + blk * kBlock + ks * 8, dv + ks * (2048 >> 4), kIdescO, !first || ks > 0);
-                umma_commit(pv_done + 8 * blk);
-                umma_commit(v_empty + 8 * buf);
-            }
-            __syncwarp();
-        };
+        uint32_t n = 0, ns = 0;      // tiles so far (both blocks'), tiles of this block so far
         while (next()) {
             const int rows = min(s.it.rows() - (s.m * 2 + blk) * kBlock, kBlock);      // of this block; may be <= 0
             const int row_base = (s.m * 2 + blk) * kBlock;
             const bool whole = s.t0 == 0 && s.t1 == s.total;
             const bool work = s.t0 < s.t1 && rows > 0;
-            if (__any_sync(0xffffffffu, *fail)) alive = false;
+            if (*fail) alive = false;
             if (work) {
-                prepare_queries<T, D>(ctx, s, rows, row_base, sign, q_tile, raw, row_scale + blk * kBlock, out_channel[blk]);
+                prepare_queries<T, D>(a, s, rows, row_base, sign, q_tile, raw, row_scale + blk * kBlock, out_channel[blk]);
                 proxy_fence();
-                role_sync();      // the operand, row_scale and out_channel of the whole block
-                if ((warp & 3) == 0) issue_scores(n);
+                __syncwarp();
+                if (lane == 0) mbar_arrive(q_full + 8 * blk);
+                role_sync();      // row_scale and out_channel of the whole block
             }
             const float rs = work ? row_scale[blk * kBlock + row] : 1.f;
             const int lim = s.it.limit(row_base + min(row, max(rows, 1) - 1));
             float ref = -CUDART_INF_F, l = 0.f;      // reference (unscaled score), sum of probabilities
-            if (!work) {
-                // A block without rows follows the tiles all the same: it frees the buffers on its side, and it must not reach a
-                // later item while a barrier is still two phases behind what it would wait for.
-                for (int t = s.t0; t < s.t1; ++t, ++n) {
-                    if ((warp & 3) != 0) continue;
-                    if (__any_sync(0xffffffffu, *fail)) alive = false;
-                    wait(k_full + 8 * (n & 1), (n >> 1) & 1);
-                    if (lane == 0) mbar_arrive(k_empty + 8 * (n & 1));
-                    wait(v_full + 8 * (n & 1), (n >> 1) & 1);
-                    if (lane == 0) mbar_arrive(v_empty + 8 * (n & 1));
-                }
-            }
+            if (!work) n += max(s.t1 - s.t0, 0);
             for (int t = s.t0; work && t < s.t1; ++t, ++n) {
-                if (__any_sync(0xffffffffu, *fail)) alive = false;
                 const bool quantized = t < s.it.tiles_c;
                 const int tok0 = quantized ? t * kBlock : s.it.lq + (t - s.it.tiles_c) * kBlock;
-                const int seen = min(min(lim, quantized ? s.it.lq : s.seq.len) - tok0, kBlock);      // columns below it are seen
-                wait(s_full + 8 * blk, ns & 1);
+                const int seen_tile = min(lim, quantized ? s.it.lq : s.seq.len) - tok0;      // tokens of the tile below it are seen
+#pragma unroll 1
+                for (int hf = 0; hf < 2; ++hf) {
+                const uint32_t h_addr = s_addr + hf * 64;
+                const int seen = seen_tile - hf * 64;
+                const bool first = t == s.t0 && hf == 0;
+                wait(s_full + 16 * blk + 8 * hf, ns & 1);
                 tc_fence_after();
-                const uint32_t bad = quantized ? bad_sh[n & 3] : 0u;      // two bits in each byte
-                if (__any_sync(0xffffffffu, seen < kBlock || bad != 0u)) {
+                float x[32], y[32];
+                tmem_ld32(h_addr, x);
+                tmem_ld32(h_addr + 32, y);
+                const uint32_t bad = quantized ? (bad_sh[n & 3] >> (16 * hf)) & 0x303u : 0u;      // two bits in each byte
+                const bool edge = __any_sync(0xffffffffu, seen < 64 || bad != 0u);
+                tmem_wait_ld32(x);
+                tmem_wait_ld32(y);
+                if (edge) {
                     // hidden columns become -infinity in place; the code below then is the same for all tiles
 #pragma unroll 1
-                    for (int run = 0; run < 4; ++run) {
+                    for (int run = 0; run < 2; ++run) {
                         const int left = seen - 32 * run;      // which of its 32 columns the row sees, one bit each
                         uint32_t v = left >= 32 ? 0xFFFFFFFFu : (left <= 0 ? 0u : (1u << left) - 1u);
                         const uint32_t two = (bad >> (8 * run)) & 3u;
                         if (two & 1u) v &= 0xFFFF0000u;
                         if (two & 2u) v &= 0x0000FFFFu;
-                        float x[32];
-                        tmem_ld32(s_addr + 32 * run, x);
+                        tmem_ld32(h_addr + 32 * run, x);
                         tmem_wait_ld32(x);
                         uint32_t w[32];
 #pragma unroll
                         for (int c = 0; c < 32; ++c) w[c] = (v >> c) & 1u ? __float_as_uint(x[c]) : 0xFF800000u;
-                        tmem_st32(s_addr + 32 * run, w);
+                        tmem_st32(h_addr + 32 * run, w);
                     }
                     tmem_wait_st();
+                    tmem_ld32(h_addr, x);
+                    tmem_ld32(h_addr + 32, y);
+                    tmem_wait_ld32(x);
+                    tmem_wait_ld32(y);
                 }
-                auto largest = [&](const float (&x)[32], float m) {
-                    float m0 = fmaxf(fmaxf(m, x[0]), x[1]), m1 = fmaxf(x[2], x[3]), m2 = fmaxf(x[4], x[5]), m3 = fmaxf(x[6], x[7]);
+                float mx;
+                {
+                    float m0 = fmaxf(x[0], y[0]), m1 = fmaxf(x[1], y[1]), m2 = fmaxf(x[2], y[2]), m3 = fmaxf(x[3], y[3]);
 #pragma unroll
-                    for (int c = 8; c < 32; c += 8) {
-                        m0 = fmaxf(fmaxf(m0, x[c]), x[c + 1]);
-                        m1 = fmaxf(fmaxf(m1, x[c + 2]), x[c + 3]);
-                        m2 = fmaxf(fmaxf(m2, x[c + 4]), x[c + 5]);
-                        m3 = fmaxf(fmaxf(m3, x[c + 6]), x[c + 7]);
+                    for (int c = 4; c < 32; c += 4) {
+                        m0 = fmaxf(fmaxf(m0, x[c]), y[c]);
+                        m1 = fmaxf(fmaxf(m1, x[c + 1]), y[c + 1]);
+                        m2 = fmaxf(fmaxf(m2, x[c + 2]), y[c + 2]);
+                        m3 = fmaxf(fmaxf(m3, x[c + 3]), y[c + 3]);
                     }
-                    return fmaxf(fmaxf(m0, m1), fmaxf(m2, m3));
-                };
-                float down = 1.f;
-                bool raise = false;
-                // The row in four runs of 32 columns, twice: for the maximum, for the probabilities.  (Keeping runs in registers in between
-                // spilled.)
-                float x[32], y[32];
-                tmem_ld32(s_addr, x);
-                tmem_ld32(s_addr + 32, y);
-                tmem_wait_ld32(x);
-                tmem_wait_ld32(y);
-                float mx = largest(y, largest(x, -CUDART_INF_F));
-                tmem_ld32(s_addr + 64, x);
-                tmem_ld32(s_addr + 96, y);
-                tmem_wait_ld32(x);
-                tmem_wait_ld32(y);
-                mx = largest(y, largest(x, mx));
-                tmem_ld32(s_addr, x);
+                    mx = fmaxf(fmaxf(m0, m1), fmaxf(m2, m3));
+                }
                 // ---- raise the reference: at first, then only when a score exceeds it by 2^kLazy
-                raise = t > s.t0 && __any_sync(0xffffffffu, (mx - ref) * rs > kLazy);
-                if (t == s.t0) ref = mx;
+                float down = 1.f;
+                const bool raise = !first && __any_sync(0xffffffffu, (mx - ref) * rs > kLazy);
+                if (first) ref = mx;
                 else if (raise && mx > ref) {
                     down = ref == -CUDART_INF_F ? 0.f : ex2_approx((ref - mx) * rs);
                     ref = mx;
@@ -809,55 +842,44 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
                         w[c >> 1] = h2(e[0], e[1]);
                         w[(c >> 1) + 1] = h2(e[2], e[3]);
                     }
-                    tmem_st16(s_addr + run * 16, w);      // over scores that are in registers or used up
+                    tmem_st16(h_addr + run * 16, w);      // over scores that are in registers
                 };
-                tmem_wait_ld32(x);
-                tmem_ld32(s_addr + 32, y);
                 probabilities(x, 0);
-                tmem_wait_ld32(y);
-                tmem_ld32(s_addr + 64, x);
                 probabilities(y, 1);
-                tmem_wait_ld32(x);
-                tmem_ld32(s_addr + 96, y);
-                probabilities(x, 2);
-                tmem_wait_ld32(y);
-                probabilities(y, 3);
                 {
                     float a0, a1;
                     unpair(pair_add(l0, l1), a0, a1);
                     l += a0 + a1;
                 }
-                if (raise) {      // O follows the reference, once the products of the tile before have landed in it
-                    wait(pv_done + 8 * blk, (ns - 1) & 1);
+                if (raise) {      // O follows the reference, once the products of the half before have landed in it
+                    if (hf) wait(pv_done + 16 * blk, ns & 1);
+                    else wait(pv_done + 16 * blk + 8, (ns - 1) & 1);
                     tc_fence_after();
 #pragma unroll 1
                     for (int c0 = 0; c0 < D; c0 += 32) {
-                        float y[32];
-                        tmem_ld32(o_addr + c0, y);
-                        tmem_wait_ld32(y);
+                        tmem_ld32(o_addr + c0, x);
+                        tmem_wait_ld32(x);
                         uint32_t w[32];
 #pragma unroll
-                        for (int c = 0; c < 32; ++c) w[c] = __float_as_uint(y[c] * down);
+                        for (int c = 0; c < 32; ++c) w[c] = __float_as_uint(x[c] * down);
                         tmem_st32(o_addr + c0, w);
                     }
                 }
                 tmem_wait_st();
                 tc_fence_before();
-                role_sync();
-                if ((warp & 3) == 0) {
-                    issue_values(n, t == s.t0);
-                    if (t + 1 < s.t1) issue_scores(n + 1);
+                __syncwarp();
+                if (lane == 0) mbar_arrive(p_full + 16 * blk + 8 * hf);
                 }
                 ++ns;
             }
             if (rows <= 0) continue;
             // ---- the block's result
             if (work) {
-                wait(pv_done + 8 * blk, (ns - 1) & 1);
+                wait(pv_done + 16 * blk + 8, (ns - 1) & 1);
                 tc_fence_after();
             }
             if (alive)
-                write_rows<T, D>(ctx, s, rows, row_base, work, o_addr, ref, l, rs, q_tile, out_channel[blk], whole,
+                write_rows<T, D>(a, s, rows, row_base, work, o_addr, ref, l, rs, q_tile, out_channel[blk], whole,
                                  a.ws + (size_t)args.n_slots * kDescInts + (((size_t)blockIdx.x * 2 + (s.t0 == 0 ? 1 : 0)) * 2 * kBlock + blk * kBlock) * partial_stride(D));
             if (alive && !whole && s.t0 == 0 && tid == 0) {
                 desc[1] = s.seq.row0; desc[2] = s.seq.n; desc[3] = s.hk; desc[4] = s.m;

@@ -547,3 +547,33 @@ def test_many_sequences():
     p.append([r.randint(0, 40) for _ in range(n)])
     p.append([r.randint(0, 1) for _ in range(n)])
     p.check_attention([min(1, L) for L in p.lens()])
+
+
+def test_prompts_of_one_and_two_row_blocks_in_turn():
+    """Items of fewer than 128 packed rows beside items of more, many tiles of both for every CTA: the second row block is idle for
+    several tiles and has to stay in step.  (One that ran ahead waited on a barrier two phases behind and got through at once.)"""
+    p = Paged(n_seqs=8, Hq=32, H=32, D=64, G=32, W=16, P=64, seed=161, max_len=1300, dtype=BF16, outliers=False)
+    p.append([1100, 1200] * 4)
+    new = [100, 200, 40, 129, 128, 300, 60, 140]
+    q = torch.randn(sum(new), 32, 64, generator=p.g).to(BF16)
+    b = p.batch(new, p.lens())
+    out = p.cache.attention(b, q.cuda(), 0.125)
+    assert int(p.cache.status[0]) == 0
+    got, at = out.cpu().double(), 0
+    for i, n in enumerate(new):
+        rows = sorted({0, 1, n // 2, n - 1})
+        for r in rows:      # a row and all behind it taken away: the same tokens seen
+            L = len(p.ref.rows[i])
+            K, V = p.ref.values(i, "k"), p.ref.values(i, "v")
+            off, hc = p.ref.score_error(i), p.ref.value_parts(i)
+            lim = L - n + r + 1
+            for h in (0, 13, 31):
+                qr = q[at + r, h].double()[p.ref.rk[h]]
+                s = 0.125 * (K[:lim, h] @ qr)
+                w = torch.softmax(s, 0)
+                o = w @ V[:lim, h]
+                ds = 0.125 * float((off[:lim, h] @ qr.abs()).max())
+                err = (w @ V[:lim, h].abs()) * (2.0 ** -11 + 2 * ds + 2.0 ** -21 + lim * 2.0 ** -23) + (w @ hc[:lim, h]) * (2.0 ** -11 + lim * 2.0 ** -23)
+                err = err + o.abs() * 2.0 ** -8 * 1.01 + 1e-7
+                assert ((got[at + r, h][p.ref.rv[h]] - o).abs() <= err).all(), (i, r, h)
+        at += n
