@@ -39,6 +39,82 @@ template <> struct Elem<float> {
 __device__ __forceinline__ float rotate_first(float x1, float x2, float c, float s) { return __fsub_rn(__fmul_rn(x1, c), __fmul_rn(x2, s)); }
 __device__ __forceinline__ float rotate_second(float x1, float x2, float c, float s) { return __fadd_rn(__fmul_rn(x2, c), __fmul_rn(x1, s)); }
 
+// D/16 elements of the tensors' type: a lane's share of a row that sixteen lanes own.
+template <typename T, int D> struct Row {
+    static constexpr int C = D / 16;
+    static constexpr int WORDS = C / 2;
+    uint32_t w[WORDS];
+    __device__ __forceinline__ void load(const T *p)
+    {
+        if constexpr (C == 8) { const uint4 v = *reinterpret_cast<const uint4 *>(p); w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w; }
+        else { const uint2 v = *reinterpret_cast<const uint2 *>(p); w[0] = v.x; w[1] = v.y; }
+    }
+    __device__ __forceinline__ void store(T *p) const
+    {
+        if constexpr (C == 8) *reinterpret_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+        else *reinterpret_cast<uint2 *>(p) = make_uint2(w[0], w[1]);
+    }
+};
+// Two elements in a register, as floats and back (rounded).
+template <typename T> __device__ __forceinline__ float2 floats(uint32_t v);
+template <> __device__ __forceinline__ float2 floats<__half>(uint32_t v) { return __half22float2(*reinterpret_cast<const __half2 *>(&v)); }
+template <> __device__ __forceinline__ float2 floats<__nv_bfloat16>(uint32_t v) { return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xFFFF0000u)); }
+template <typename T> __device__ __forceinline__ uint32_t packed(float lo, float hi);
+template <> __device__ __forceinline__ uint32_t packed<__half>(float lo, float hi)
+{
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+template <> __device__ __forceinline__ uint32_t packed<__nv_bfloat16>(float lo, float hi)
+{
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+// Rotates a lane's channels c0 .. c0 + C - 1 of a row; cs[j] = {cos, sin} of channel c0 + j.  `raw` is the row in shared memory, as read, for
+// the partners of the half layout (interleaved pairs lie in one lane).  Rounded to T.
+template <typename T, int D>
+__device__ __forceinline__ void rotate_row(Row<T, D> &row, int c0, const float2 *cs, const T *raw, int rot_dim, bool interleaved)
+{
+    const int half = rot_dim / 2;
+#pragma unroll
+    for (int j = 0; j < Row<T, D>::C; j += 2) {
+        const float2 x = floats<T>(row.w[j / 2]);
+        float y0 = x.x, y1 = x.y;
+        const int ca = c0 + j, cb = ca + 1;
+        if (interleaved) {
+            if (ca < rot_dim) {
+                y0 = rotate_first(x.x, x.y, cs[j].x, cs[j].y);
+                y1 = rotate_second(x.x, x.y, cs[j].x, cs[j].y);
+            }
+        } else {
+            if (ca < rot_dim) {
+                const float o = Elem<T>::to_float(raw[ca >= half ? ca - half : ca + half]);
+                y0 = ca >= half ? rotate_second(o, x.x, cs[j].x, cs[j].y) : rotate_first(x.x, o, cs[j].x, cs[j].y);
+            }
+            if (cb < rot_dim) {
+                const float o = Elem<T>::to_float(raw[cb >= half ? cb - half : cb + half]);
+                y1 = cb >= half ? rotate_second(o, x.y, cs[j + 1].x, cs[j + 1].y) : rotate_first(x.y, o, cs[j + 1].x, cs[j + 1].y);
+            }
+        }
+        row.w[j / 2] = packed<T>(y0, y1);
+    }
+}
+// cos and sin of a lane's channels at position t ({1, 0} behind rot_dim).
+template <int C>
+__device__ __forceinline__ void load_angles(float2 (&cs)[C], const skvq_rope &rope, int t, int c0)
+{
+    const int half = rope.rot_dim / 2;
+    const float2 *table = static_cast<const float2 *>(rope.table) + (int64_t)t * half;
+#pragma unroll
+    for (int j = 0; j < C; ++j) {
+        const int c = c0 + j;
+        cs[j] = make_float2(1.f, 0.f);
+        if (c < rope.rot_dim) cs[j] = table[rope.interleaved ? c >> 1 : (c >= half ? c - half : c)];
+    }
+}
+
 __device__ __forceinline__ void set_status(int32_t *status, int bits)
 {
     if (status) atomicOr(status, bits);

@@ -26,38 +26,6 @@ struct AppendIo {
     int bulk;        // 1: half-warps take tokens; 0: heads of one token
 };
 
-// D/16 elements of the tensors' type, and a row of them in shared memory.
-template <typename T, int D> struct Row {
-    static constexpr int C = D / 16;
-    static constexpr int WORDS = C / 2;
-    uint32_t w[WORDS];
-    __device__ __forceinline__ void load(const T *p)
-    {
-        if constexpr (C == 8) { const uint4 v = *reinterpret_cast<const uint4 *>(p); w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w; }
-        else { const uint2 v = *reinterpret_cast<const uint2 *>(p); w[0] = v.x; w[1] = v.y; }
-    }
-    __device__ __forceinline__ void store(T *p) const
-    {
-        if constexpr (C == 8) *reinterpret_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]);
-        else *reinterpret_cast<uint2 *>(p) = make_uint2(w[0], w[1]);
-    }
-};
-template <typename T> __device__ __forceinline__ float2 floats(uint32_t v);
-template <> __device__ __forceinline__ float2 floats<__half>(uint32_t v) { return __half22float2(*reinterpret_cast<const __half2 *>(&v)); }
-template <> __device__ __forceinline__ float2 floats<__nv_bfloat16>(uint32_t v) { return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xFFFF0000u)); }
-template <typename T> __device__ __forceinline__ uint32_t packed(float lo, float hi);
-template <> __device__ __forceinline__ uint32_t packed<__half>(float lo, float hi)
-{
-    uint32_t r;
-    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-    return r;
-}
-template <> __device__ __forceinline__ uint32_t packed<__nv_bfloat16>(float lo, float hi)
-{
-    uint32_t r;
-    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-    return r;
-}
 template <typename T> __device__ __forceinline__ uint32_t min2(uint32_t a, uint32_t b);
 template <> __device__ __forceinline__ uint32_t min2<__half>(uint32_t a, uint32_t b)
 {
@@ -97,19 +65,11 @@ __device__ __forceinline__ void append_rows(const AppendIo &io, const PagedSeq &
         }
     }
     const bool rot = !IS_V && a.rope.table;
-    const int half = a.rope.rot_dim / 2, c0 = sub * C;
+    const int c0 = sub * C;
     const bool inter = a.rope.interleaved;
     float2 cs[IS_V ? 1 : C];
     if constexpr (!IS_V) {
-        if (rot && have) {
-            const float2 *table = static_cast<const float2 *>(a.rope.table) + (int64_t)t * half;
-#pragma unroll
-            for (int j = 0; j < C; ++j) {
-                const int c = c0 + j;
-                cs[j] = make_float2(1.f, 0.f);
-                if (c < a.rope.rot_dim) cs[j] = table[inter ? c >> 1 : (c >= half ? c - half : c)];
-            }
-        }
+        if (rot && have) load_angles(cs, a.rope, t, c0);
     }
     const T *src = static_cast<const T *>(IS_V ? io.v : io.k) + (int64_t)(seq.row0 + i) * (IS_V ? io.v_stride : io.k_stride) + c0;
     const int32_t *reorder = IS_V ? a.c.reorder_v : a.c.reorder_k;
@@ -147,30 +107,7 @@ __device__ __forceinline__ void append_rows(const AppendIo &io, const PagedSeq &
                     row.store(raw + c0);
                     __syncwarp();
                 }
-                if (here) {
-#pragma unroll
-                    for (int j = 0; j < C; j += 2) {
-                        const float2 x = floats<T>(row.w[j / 2]);
-                        float y0 = x.x, y1 = x.y;
-                        if (inter) {
-                            if (c0 + j < a.rope.rot_dim) {
-                                y0 = rotate_first(x.x, x.y, cs[j].x, cs[j].y);
-                                y1 = rotate_second(x.x, x.y, cs[j].x, cs[j].y);
-                            }
-                        } else {
-                            const int ca = c0 + j, cb = ca + 1;
-                            if (ca < a.rope.rot_dim) {
-                                const float o = Elem<T>::to_float(raw[ca >= half ? ca - half : ca + half]);
-                                y0 = ca >= half ? rotate_second(o, x.x, cs[j].x, cs[j].y) : rotate_first(x.x, o, cs[j].x, cs[j].y);
-                            }
-                            if (cb < a.rope.rot_dim) {
-                                const float o = Elem<T>::to_float(raw[cb >= half ? cb - half : cb + half]);
-                                y1 = cb >= half ? rotate_second(o, x.y, cs[j + 1].x, cs[j + 1].y) : rotate_first(x.y, o, cs[j + 1].x, cs[j + 1].y);
-                            }
-                        }
-                        row.w[j / 2] = packed<T>(y0, y1);
-                    }
-                }
+                if (here) rotate_row<T, D>(row, c0, cs, raw, a.rope.rot_dim, inter);
             }
         }
         row.store(turned + c0);

@@ -44,6 +44,8 @@ constexpr float kPOffset = 6.f;                 // probabilities are held times 
 struct PrefillArgs {
     PagedAttnArgs a;
     int n_slots;
+    __half *queries;      // [Hkv][T * Hq/Hkv][D], by paged_queries_kernel
+    float *scales;        // [Hkv][T * Hq/Hkv]
 };
 
 template <int D>
@@ -54,8 +56,7 @@ struct PGeo {
     static constexpr int Q = 0;                                // 2 row blocks; at the end of an item its output rows
     static constexpr int K = 2 * TILE_BYTES;                   // 2 buffers
     static constexpr int V = 4 * TILE_BYTES;                   // 2 buffers
-    static constexpr int GATHER = 6 * TILE_BYTES;              // per softmax warp: four rows of queries
-    static constexpr int SMEM = GATHER + 8 * 4 * D * 2 + 1024;  // and room to align to 1024 bytes
+    static constexpr int SMEM = 6 * TILE_BYTES + 1024;         // and room to align to 1024 bytes
     static constexpr int TMEM_S = 0, TMEM_O = 256;             // columns: S (P in place) 2 blocks x 2 halves x 64, O 2 x D
 };
 
@@ -165,17 +166,25 @@ __device__ __forceinline__ bool mbar_wait_cycles(uint32_t bar, uint32_t parity)
     }
 }
 
-// Two elements of the tensors' type in a register, as floats and back (rounded).
-template <typename T> __device__ __forceinline__ float2 unpack2(uint32_t v);
-template <> __device__ __forceinline__ float2 unpack2<__half>(uint32_t v) { return __half22float2(*reinterpret_cast<const __half2 *>(&v)); }
-template <> __device__ __forceinline__ float2 unpack2<__nv_bfloat16>(uint32_t v) { return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xFFFF0000u)); }
-template <typename T> __device__ __forceinline__ uint32_t pack2(float lo, float hi);
-template <> __device__ __forceinline__ uint32_t pack2<__half>(float lo, float hi) { return h2(lo, hi); }
-template <> __device__ __forceinline__ uint32_t pack2<__nv_bfloat16>(float lo, float hi)
+// 2^a and 2^b by multiply-adds: x = n + f with n the nearest integer, a polynomial of degree 4 for 2^f on [-1/2, 1/2] (fitted for the
+// smallest relative error: 3e-6, a hundredth of the fp16 step that the result is rounded to), n added to the exponent.  Arguments below
+// -126, -infinity among them, give 2^-126.
+constexpr int kPolynomial = 2;
+__device__ __forceinline__ void exp2_pair(float &a, float &b)
 {
-    uint32_t r;
-    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-    return r;
+    constexpr float MAGIC = 12582912.0f;      // 1.5 2^23: the sum's low bits hold the rounded integer
+    const uint64_t x = pair(fmaxf(a, -126.0f), fmaxf(b, -126.0f));
+    const uint64_t t = pair_add(x, pair(MAGIC, MAGIC));
+    const uint64_t f = pair_fma(pair_add(t, pair(-MAGIC, -MAGIC)), pair(-1.f, -1.f), x);
+    uint64_t p = pair_fma(f, pair(0.00957010f, 0.00957010f), pair(0.05591786f, 0.05591786f));
+    p = pair_fma(f, p, pair(0.24024744f, 0.24024744f));
+    p = pair_fma(f, p, pair(0.69312179f, 0.69312179f));
+    p = pair_fma(f, p, pair(0.99999928f, 0.99999928f));
+    float p0, p1, t0, t1;
+    unpair(p, p0, p1);
+    unpair(t, t0, t1);
+    a = __int_as_float(__float_as_int(p0) + (__float_as_int(t0) << 23));
+    b = __int_as_float(__float_as_int(p1) + (__float_as_int(t1) << 23));
 }
 
 // Position 0..7 inside a run of eight operand channels -> stored channel.
@@ -246,127 +255,111 @@ __device__ __noinline__ void next_segment(const PrefillArgs &a, const long long 
     s.valid = 1;
 }
 
-// What the functions below need of the launch arguments: copied once, in one trip, because a field read through the reference is a memory
-// access again after every barrier; and inside, because held by the caller the copies would spill in the loop over tiles.
-struct PContext {
-    const void *q;
-    void *out;
-    float *lse;
-    int64_t q_stride, out_stride;
-    const float2 *rope;
-    const int32_t *reorder_k, *reorder_v;
-    int rot_dim, interleaved, n_q_heads;
-    float sm_scale;
+// The queries as rows of the A operand, for all row blocks at once: rotated, rounded to T, reordered, in the operand's channel order, fp16
+// times a power of two per row; packed row (token * Hq/Hkv + query head of the KV head) of KV head h in row h * T * Hq/Hkv + it.  Sixteen
+// lanes own a row; a half-warp takes a token and walks over the heads with the token's angles in registers.  (Prepared by the softmax
+// warps, item by item, this took 35,000 cycles per item of 256 rows.)
+constexpr int kQueryThreads = 128;
+constexpr int kQueryTokens = kQueryThreads / 16;
+struct QueryArgs {
+    PrefillArgs f;
+    int heads;      // query heads a CTA walks over
 };
-__device__ __forceinline__ PContext context(const PagedAttnArgs &a)
+template <typename T, int D>
+__global__ void __launch_bounds__(kQueryThreads) paged_queries_kernel(const __grid_constant__ QueryArgs args)
 {
-    return PContext{a.q, a.out, a.lse, a.q_stride, a.out_stride, static_cast<const float2 *>(a.p.rope.table), a.p.c.reorder_k, a.p.c.reorder_v,
-                    a.p.rope.rot_dim, a.p.rope.interleaved, a.p.cfg.n_q_heads, a.sm_scale};
+    using R = Row<T, D>;
+    constexpr int C = R::C;
+    __shared__ __align__(16) T rows[kQueryTokens][2][D + 8];
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;");
+    const PagedAttnArgs &a = args.f.a;
+    const PagedArgs &p = a.p;
+    const int unit = threadIdx.x >> 4, sub = threadIdx.x & 15, c0 = sub * C, rep = p.cfg.n_q_heads / p.cfg.n_kv_heads;
+    PagedSeq seq;
+    if (!paged_sequence(p, blockIdx.z, false, seq) || seq.n * rep <= kFewRows) return;
+    if ((int)blockIdx.x * kQueryTokens >= seq.n) return;
+    const int i = blockIdx.x * kQueryTokens + unit, pos = seq.len - seq.n + i;
+    const int h0 = blockIdx.y * args.heads, h1 = min(h0 + args.heads, p.cfg.n_q_heads);
+    const bool have = i < seq.n, turn = p.rope.table && have && pos >= 0;
+    const int64_t tok = seq.row0 + i, all = (int64_t)p.batch.n_tokens * rep;
+    float2 cs[C];
+    if (turn) load_angles(cs, p.rope, pos, c0);
+    const T *src = static_cast<const T *>(a.q) + tok * a.q_stride + c0;
+    T *raw = rows[unit][0], *turned = rows[unit][1];
+    const float sign = a.sm_scale < 0.f ? -1.f : (a.sm_scale == 0.f ? 0.f : 1.f);      // the rows' scale is positive
+    const float scale = (sign == 0.f ? 1.f : fabsf(a.sm_scale)) * 1.4426950408889634f;
+    int from[C], hk = -1;
+    for (int h = h0; h < h1; ++h) {
+        if (h / rep != hk) {
+            hk = h / rep;
+#pragma unroll
+            for (int j = 0; j < C; ++j) {
+                const int c = (c0 & ~7) + channel_at((c0 + j) & 7);
+                from[j] = p.c.reorder_k ? p.c.reorder_k[hk * D + c] & (D - 1) : c;
+            }
+        }
+        R row;
+#pragma unroll
+        for (int k = 0; k < R::WORDS; ++k) row.w[k] = 0u;
+        if (have) row.load(src + (int64_t)h * D);
+        if (p.rope.table) {
+            if (!p.rope.interleaved) {
+                row.store(raw + c0);
+                __syncwarp();
+            }
+            if (turn) rotate_row<T, D>(row, c0, cs, raw, p.rope.rot_dim, p.rope.interleaved);
+        }
+        row.store(turned + c0);
+        __syncwarp();
+        float x[C], mx = 0.f;
+#pragma unroll
+        for (int j = 0; j < C; ++j) { x[j] = Elem<T>::to_float(turned[from[j]]); mx = fmaxf(mx, fabsf(x[j])); }
+        __syncwarp();
+#pragma unroll
+        for (int d = 1; d < 16; d <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
+        float up = 1.f;      // the row's largest to [2^4, 2^5): exact, and far from fp16's ends whatever the type's range
+        if (mx > 0.f && mx < CUDART_INF_F) up = __int_as_float((127 + min(4 - (__float_as_int(mx) >> 23) + 127, 60)) << 23);
+        if (!have) continue;
+        const float f = sign == 0.f ? 0.f : up * sign;
+        const int64_t at = hk * all + tok * rep + (h - hk * rep);
+        __half *dst = args.f.queries + at * D + c0;
+        if constexpr (C == 8)
+            *reinterpret_cast<uint4 *>(dst) = make_uint4(h2(x[0] * f, x[1] * f), h2(x[2] * f, x[3] * f), h2(x[4] * f, x[5] * f), h2(x[6] * f, x[7] * f));
+        else *reinterpret_cast<uint2 *>(dst) = make_uint2(h2(x[0] * f, x[1] * f), h2(x[2] * f, x[3] * f));
+        if (sub == 0) args.f.scales[at] = scale / up;
+    }
 }
 
-// The queries of a row block as the K-major A operand: rotated, rounded to T, reordered, scaled by a power of two per row; and the source
-// channel of every output column.  Not inlined, like write_rows: what these keep in registers would spill in the loop over tiles.
-template <typename T, int D>
-__device__ __noinline__ void prepare_queries(const PagedAttnArgs &args, const PSegment &s, int rows, int row_base, float sign, uint8_t *q_tile, T *raw,
-                                             float *row_scale, uint16_t *out_channel)
+// A row block's queries and their scales into shared memory, and the source channel of every output column.  Not inlined, like write_rows:
+// what they keep in registers would spill in the loop over tiles.
+template <int D>
+__device__ __noinline__ void load_queries(const PrefillArgs &args, const PSegment &s, int rows, int row_base, uint8_t *q_tile, float *row_scale, uint16_t *out_channel)
 {
     using Geo = PGeo<D>;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const PContext ctx = context(args);
-    const int rep = s.it.rep, hk = s.hk, row0 = s.seq.row0, first_pos = s.seq.len - s.seq.n;
-    // ---- queries of the block: a warp per row; lane: operand positions C lane .. C lane + C - 1
-    constexpr int C = D / 32;
-    int from[C];
+    const int row = threadIdx.x & (kBlock - 1), hk = s.hk;
+    const int32_t *reorder_v = args.a.p.c.reorder_v;
+    const int64_t at = (int64_t)hk * args.a.p.batch.n_tokens * s.it.rep + (int64_t)s.seq.row0 * s.it.rep + row_base;
+    const uint4 *src = reinterpret_cast<const uint4 *>(args.queries + at * D);
 #pragma unroll
-    for (int k = 0; k < C; ++k) {
-        const int pos = lane * C + k, c = (pos & ~7) + channel_at(pos & 7);
-        from[k] = ctx.reorder_k ? ctx.reorder_k[hk * D + c] & (D - 1) : c;
+    for (int e0 = 0; e0 < kBlock * D / 8; e0 += 8 * kBlock) {      // 8 loads in flight
+        uint4 v[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int e = e0 + k * kBlock + row;
+            v[k] = make_uint4(0u, 0u, 0u, 0u);
+            if (e / (D / 8) < rows) v[k] = src[e];
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int e = e0 + k * kBlock + row, r = e / (D / 8), c8 = e % (D / 8);
+            *reinterpret_cast<uint4 *>(q_tile + (c8 >> 3) * Geo::HALF_BYTES + r * 128 + (((c8 & 7) ^ (r & 7)) << 4)) = v[k];
+        }
     }
-    for (int c = threadIdx.x & (kBlock - 1); c < D; c += kBlock) {
+    row_scale[row] = row < rows ? args.scales[at + row] : 0.f;
+    for (int c = row; c < D; c += kBlock) {
         const int st = (c & ~7) + channel_at(c & 7);
-        out_channel[c] = (uint16_t)(ctx.reorder_v ? ctx.reorder_v[hk * D + st] & (D - 1) : st);
-    }
-    const float2 *rope = ctx.rope;
-    const int rot_dim = ctx.rot_dim, interleaved = ctx.interleaved, half = rot_dim / 2;
-    // four rows at a time: their loads are in flight together
-#pragma unroll 1
-    for (int r0 = (warp & 3) * 32; r0 < (warp & 3) * 32 + 32; r0 += 4) {
-        float x[4][C], mx[4];
-        float2 cs[4][C];
-        bool turn[4];
-        auto put = [&]() {      // the four rows into shared memory, in the tensors' type
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                T *dst = raw + k * D + lane * C;
-                if constexpr (C == 4) *reinterpret_cast<uint2 *>(dst) = make_uint2(pack2<T>(x[k][0], x[k][1]), pack2<T>(x[k][2], x[k][3]));
-                else *reinterpret_cast<uint32_t *>(dst) = pack2<T>(x[k][0], x[k][1]);
-            }
-        };
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const int r = r0 + k, i = (row_base + r) / rep, head = hk * rep + (row_base + r) - i * rep, pos = first_pos + i;
-            const bool have = r < rows && sign != 0.f;
-            turn[k] = have && rope && pos >= 0;
-            uint2 w = make_uint2(0u, 0u);
-            if (have) {
-                const T *src = static_cast<const T *>(ctx.q) + (int64_t)(row0 + i) * ctx.q_stride + (int64_t)head * D + lane * C;
-                if constexpr (C == 4) w = *reinterpret_cast<const uint2 *>(src);
-                else w.x = *reinterpret_cast<const uint32_t *>(src);
-            }
-            if (turn[k]) {
-#pragma unroll
-                for (int e = 0; e < C; ++e) {
-                    const int c = lane * C + e;
-                    if (c < rot_dim) cs[k][e] = rope[(int64_t)pos * half + (interleaved ? c >> 1 : (c >= half ? c - half : c))];
-                }
-            }
-            const float2 u = unpack2<T>(w.x), v = unpack2<T>(w.y);
-            x[k][0] = u.x;
-            x[k][1] = u.y;
-            if constexpr (C == 4) { x[k][2] = v.x; x[k][3] = v.y; }
-        }
-        put();
-        __syncwarp();
-        if (rope) {
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-#pragma unroll
-                for (int e = 0; e < C; ++e) {
-                    const int c = lane * C + e;
-                    if (turn[k] && c < rot_dim) {
-                        const bool second = interleaved ? c & 1 : c >= half;
-                        const int partner = interleaved ? c ^ 1 : (second ? c - half : c + half);
-                        const float mine = x[k][e], other = Elem<T>::to_float(raw[k * D + partner]);
-                        x[k][e] = second ? rotate_second(other, mine, cs[k][e].x, cs[k][e].y) : rotate_first(mine, other, cs[k][e].x, cs[k][e].y);
-                    }
-                }
-            }
-            __syncwarp();
-            put();
-            __syncwarp();
-        }
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            mx[k] = 0.f;
-#pragma unroll
-            for (int e = 0; e < C; ++e) { x[k][e] = Elem<T>::to_float(raw[k * D + from[e]]); mx[k] = fmaxf(mx[k], fabsf(x[k][e])); }
-        }
-        __syncwarp();
-#pragma unroll
-        for (int d = 16; d > 0; d >>= 1)
-#pragma unroll
-            for (int k = 0; k < 4; ++k) mx[k] = fmaxf(mx[k], __shfl_xor_sync(0xffffffffu, mx[k], d));
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const int r = r0 + k;
-            float up = 1.f;      // the row's largest to [2^4, 2^5): exact, and far from fp16's ends whatever the type's range
-            if (mx[k] > 0.f && mx[k] < CUDART_INF_F) up = __int_as_float((127 + min(4 - (__float_as_int(mx[k]) >> 23) + 127, 60)) << 23);
-            if (lane == 0) row_scale[r] = (sign == 0.f ? 1.f : fabsf(ctx.sm_scale)) * 1.4426950408889634f / up;
-            uint8_t *dst = q_tile + r * 128 + ((lane * C) >> 6) * Geo::HALF_BYTES + ((((lane * C) >> 3 & 7) ^ (r & 7)) << 4) + ((lane * C) & 7) * 2;
-            const float f = up * sign;
-            if constexpr (C == 4) *reinterpret_cast<uint2 *>(dst) = make_uint2(h2(x[k][0] * f, x[k][1] * f), h2(x[k][2] * f, x[k][3] * f));
-            else *reinterpret_cast<uint32_t *>(dst) = h2(x[k][0] * f, x[k][1] * f);
-        }
+        out_channel[c] = (uint16_t)(reorder_v ? reorder_v[hk * D + st] & (D - 1) : st);
     }
 }
 
@@ -376,7 +369,11 @@ __device__ __noinline__ void write_rows(const PagedAttnArgs &args, const PSegmen
                                         float rs, uint8_t *q_tile, const uint16_t *out_channel, bool whole, float *part)
 {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, row = threadIdx.x & (kBlock - 1);
-    const PContext ctx = context(args);
+    // read once, together: through the reference every field is a memory access
+    void *const out = args.out;
+    float *const lse = args.lse;
+    const int64_t out_stride = args.out_stride;
+    const int n_q_heads = args.p.cfg.n_q_heads;
     const int rep = s.it.rep, hk = s.hk, row0 = s.seq.row0;
     const int i = (row_base + row) / rep, head = hk * rep + (row_base + row) - i * rep;
     if (whole) {
@@ -395,15 +392,15 @@ __device__ __noinline__ void write_rows(const PagedAttnArgs &args, const PSegmen
                 rows_out[row * D + ((((dst >> 3) ^ (row & 7))) << 3) + (dst & 7)] = Elem<T>::from_float(work && ref != -CUDART_INF_F ? x[c] * inv : 0.f);
             }
         }
-        if (ctx.lse && row < rows )
-            ctx.lse[(int64_t)(row0 + i) * ctx.n_q_heads + head] = ref == -CUDART_INF_F ? ref : (ref * rs + log2f(l) - kPOffset) * 0.6931471805599453f;
+        if (lse && row < rows )
+            lse[(int64_t)(row0 + i) * n_q_heads + head] = ref == -CUDART_INF_F ? ref : (ref * rs + log2f(l) - kPOffset) * 0.6931471805599453f;
         __syncwarp();
         constexpr int PER_ROW = D / 8;
         for (int e = lane; e < 32 * PER_ROW; e += 32) {      // this warp's 32 rows, 16 bytes a lane
             const int r = (warp & 3) * 32 + e / PER_ROW, c8 = e % PER_ROW;
             if (r < rows ) {
                 const int ri = (row_base + r) / rep, rh = hk * rep + (row_base + r) - ri * rep;
-                *reinterpret_cast<uint4 *>(static_cast<T *>(ctx.out) + (int64_t)(row0 + ri) * ctx.out_stride + (int64_t)rh * D + c8 * 8) =
+                *reinterpret_cast<uint4 *>(static_cast<T *>(out) + (int64_t)(row0 + ri) * out_stride + (int64_t)rh * D + c8 * 8) =
                     *reinterpret_cast<const uint4 *>(rows_out + r * D + ((c8 ^ (r & 7)) << 3));
             }
         }
@@ -743,9 +740,7 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
         const int blk = warp >> 2, row = tid & (kBlock - 1);                       // row block, row = lane of the tensor memory
         const uint32_t quad = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t s_addr = tmem + Geo::TMEM_S + blk * kBlock + quad, o_addr = tmem + Geo::TMEM_O + blk * D + quad;
-        const float sign = a.sm_scale < 0.f ? -1.f : (a.sm_scale == 0.f ? 0.f : 1.f);
         uint8_t *q_tile = smem + Geo::Q + blk * Geo::TILE_BYTES;
-        T *raw = reinterpret_cast<T *>(smem + Geo::GATHER) + warp * 4 * D;
         uint32_t n = 0, ns = 0;      // tiles so far (both blocks'), tiles of this block so far
         while (next()) {
             const int rows = min(s.it.rows() - (s.m * 2 + blk) * kBlock, kBlock);      // of this block; may be <= 0
@@ -754,7 +749,7 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
             const bool work = s.t0 < s.t1 && rows > 0;
             if (*fail) alive = false;
             if (work) {
-                prepare_queries<T, D>(a, s, rows, row_base, sign, q_tile, raw, row_scale + blk * kBlock, out_channel[blk]);
+                load_queries<D>(args, s, rows, row_base, q_tile, row_scale + blk * kBlock, out_channel[blk]);
                 proxy_fence();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(q_full + 8 * blk);
@@ -828,19 +823,21 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
                 const float base = kPOffset - (ref == -CUDART_INF_F ? 0.f : ref * rs);
                 const uint64_t rs2 = pair(rs, rs), base2 = pair(base, base);
                 uint64_t l0 = 0ull, l1 = 0ull;      // pairs of sums
-                auto probabilities = [&](const float (&v)[32], int run) {
+                // Of every eight exponentials the last kPolynomial are computed with multiply-adds: the special-function unit, at 16 a
+                // clock for the SM, would alone take as long as the tensor core.
+                auto probabilities = [&](float (&v)[32], int run) {
                     uint32_t w[16];
 #pragma unroll
-                    for (int c = 0; c < 32; c += 4) {
-                        float e[4];
-                        unpair(pair_fma(pair(v[c], v[c + 1]), rs2, base2), e[0], e[1]);
-                        unpair(pair_fma(pair(v[c + 2], v[c + 3]), rs2, base2), e[2], e[3]);
+                    for (int c = 0; c < 32; c += 8) {
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) e[k] = ex2_approx(e[k]);
-                        l0 = pair_add(l0, pair(e[0], e[1]));
-                        l1 = pair_add(l1, pair(e[2], e[3]));
-                        w[c >> 1] = h2(e[0], e[1]);
-                        w[(c >> 1) + 1] = h2(e[2], e[3]);
+                        for (int k = c; k < c + 8; k += 2) {
+                            unpair(pair_fma(pair(v[k], v[k + 1]), rs2, base2), v[k], v[k + 1]);
+                            if (k % 8 < 8 - kPolynomial) { v[k] = ex2_approx(v[k]); v[k + 1] = ex2_approx(v[k + 1]); }
+                            else exp2_pair(v[k], v[k + 1]);
+                            if (k & 2) l1 = pair_add(l1, pair(v[k], v[k + 1]));
+                            else l0 = pair_add(l0, pair(v[k], v[k + 1]));
+                            w[k / 2] = h2(v[k], v[k + 1]);
+                        }
                     }
                     tmem_st16(h_addr + run * 16, w);      // over scores that are in registers
                 };
@@ -905,14 +902,28 @@ int prefill_slots(const skvq_paged_config &cfg, const skvq_paged_batch &batch)
     return slots < 1 ? 1 : (int)slots;
 }
 
+size_t partials_bytes(const skvq_paged_config &cfg, const skvq_paged_batch &batch)
+{
+    const size_t slots = prefill_slots(cfg, batch);
+    return slots * kDescInts * 4 + slots * 2 * (2 * kBlock) * partial_stride(cfg.head_dim) * 4;      // a multiple of 16
+}
+
 template <typename T, int D, int NG>
 cudaError_t launch_prefill(const PagedAttnArgs &a, cudaStream_t stream)
 {
-    const PrefillArgs s{a, prefill_slots(a.p.cfg, a.p.batch)};
-    static unsigned long long done = 0;
-    cudaError_t e = configure_smem_once(paged_prefill_kernel<T, D, NG>, PGeo<D>::SMEM + (int)sizeof(long long) * (kMaxPagedSeqs + 1), done);
+    const skvq_paged_config &cfg = a.p.cfg;
+    const skvq_paged_batch &batch = a.p.batch;
+    char *ws = reinterpret_cast<char *>(a.ws) + partials_bytes(cfg, batch);
+    const PrefillArgs s{a, prefill_slots(cfg, batch), reinterpret_cast<__half *>(ws), reinterpret_cast<float *>(ws + (size_t)batch.n_tokens * cfg.n_q_heads * D * 2)};
+    QueryArgs q{s, cfg.n_q_heads};
+    const long long tokens = (batch.max_new + kQueryTokens - 1) / kQueryTokens;
+    while (q.heads > 4 && tokens * batch.n_seqs * ((cfg.n_q_heads + q.heads - 1) / q.heads) < 32LL * sm_count()) q.heads = (q.heads + 1) / 2;
+    cudaError_t e = launch_chained(paged_queries_kernel<T, D>, dim3((unsigned)tokens, (cfg.n_q_heads + q.heads - 1) / q.heads, batch.n_seqs), kQueryThreads, 0, stream, q);
     if (e != cudaSuccess) return e;
-    e = launch_chained(paged_prefill_kernel<T, D, NG>, dim3(s.n_slots), kPrefillThreads, PGeo<D>::SMEM + sizeof(long long) * (a.p.batch.n_seqs + 1), stream, s);
+    static unsigned long long done = 0;
+    e = configure_smem_once(paged_prefill_kernel<T, D, NG>, PGeo<D>::SMEM + (int)sizeof(long long) * (kMaxPagedSeqs + 1), done);
+    if (e != cudaSuccess) return e;
+    e = launch_chained(paged_prefill_kernel<T, D, NG>, dim3(s.n_slots), kPrefillThreads, PGeo<D>::SMEM + sizeof(long long) * (batch.n_seqs + 1), stream, s);
     if (e != cudaSuccess) return e;
     return launch_paged_merge(a, s.n_slots, 2 * kBlock, 32, kPOffset, stream);
 }
@@ -928,8 +939,7 @@ template <typename T> cudaError_t prefill_by_shape(const PagedAttnArgs &a, cudaS
 
 size_t prefill_workspace_bytes(const skvq_paged_config &cfg, const skvq_paged_batch &batch)
 {
-    const size_t slots = prefill_slots(cfg, batch);
-    return slots * kDescInts * 4 + slots * 2 * (2 * kBlock) * partial_stride(cfg.head_dim) * 4;
+    return partials_bytes(cfg, batch) + (size_t)batch.n_tokens * cfg.n_q_heads * (cfg.head_dim * 2 + 4);
 }
 
 cudaError_t launch_paged_prefill(const PagedAttnArgs &a, cudaStream_t stream)
