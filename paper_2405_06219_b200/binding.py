@@ -546,12 +546,12 @@ class SkvqPagedCache:
                 os_ = self._rows(out, batch, H)
             if workspace is None:
                 size = skvq_paged_workspace_size(c, batch, n_splits)
-                workspace = torch.empty(max(size, 16), dtype=torch.uint8, device=self.device)
+                workspace = torch.empty(size, dtype=torch.uint8, device=self.device) if size else None
             else:
                 assert workspace.get_device() == index and workspace.is_contiguous()
                 size = workspace.numel() * workspace.element_size()
             assert lse is None or (lse.dtype == torch.float32 and lse.is_contiguous() and lse.get_device() == index and lse.numel() >= batch.n_tokens * H)
-            args = SkvqPagedAttnArgs(sm_scale, 1 if causal else 0, n_splits, workspace.data_ptr(), size)
+            args = SkvqPagedAttnArgs(sm_scale, 1 if causal else 0, n_splits, _dptr(workspace), size)
             _check(lib().skvq_paged_attention(_ref(c), _ref(self.struct), _ref(batch), None if rope is None else _ref(rope.struct), q.data_ptr(), qs,
                                               out.data_ptr(), os_, _dptr(lse), _ref(args), _raw_stream(index, stream)), "skvq_paged_attention")
         return out

@@ -1,11 +1,12 @@
 // skvq_paged_append and skvq_paged_read: rotated, reordered, 4-bit quantized rows into pages, and back.
 //
-// Sixteen lanes own a row (one token of one KV head, keys or values), D/16 neighbouring channels a lane; a warp works on two rows at
-// a time: two tokens of the same head (bulk), or two heads of the same token (steps of few tokens, where latency counts), and walks
-// over heads, so a token's angles stay in registers.  The row is read coalesced, rotated (partner channels come through shared
-// memory), and gathered from shared memory in stored order; a group's extremes are reduced by shuffles.
-// What bounds it is instructions, not bytes (about 90 per key row and lane group, 65 per value row): so min and max travel as one
-// packed pair, and the code is formed without a division,
+// Sixteen lanes own the rows of two neighbouring tokens (of one KV head, keys or values), D/16 neighbouring channels a lane; the half-warps
+// of a CTA take token pairs (bulk) or heads of the same pair (steps of few tokens, where latency counts) and walk over heads, so a token's
+// angles stay in registers.  The rows are read coalesced and put into shared memory interleaved, a 32-bit word holding one channel
+// of both tokens: partner channels of the rotation, and the gather in stored order, then take one shared-memory access for
+// two rows, and minimum and maximum one packed instruction for both.  A group's extremes are reduced by shuffles.
+// What bounds it is instructions, not bytes (a row at a time: 420 us for the append of a 32k-token prompt of 32 heads, 267 for reading it back,
+// floors of 105 each), so the code is formed without a division,
 //   code = rint(d / h): t = fma(d, RN(1/h), 1.5 2^23) holds rint(d RN(1/h)); the remainder d - code h tells whether the quotient can be
 //   near k + 0.5 (|remainder| >= h/2 (1 - 2^-18)); only then (ties included) the rows concerned divide.
 // The quantizer arithmetic is explicitly rounded fp32: codes and parameters do not depend on compiler contraction.
@@ -16,7 +17,7 @@ namespace {
 
 constexpr int kRowWarps = 4;
 constexpr int kRowThreads = kRowWarps * 32;
-constexpr int kBulkTokens = 2 * kRowWarps;      // tokens of a CTA when they lie side by side
+constexpr int kBulkTokens = 4 * kRowWarps;      // tokens of a CTA when they lie side by side
 
 struct AppendIo {
     PagedArgs p;
@@ -27,10 +28,17 @@ struct AppendIo {
 };
 
 template <typename T> __device__ __forceinline__ uint32_t min2(uint32_t a, uint32_t b);
+template <typename T> __device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b);
 template <> __device__ __forceinline__ uint32_t min2<__half>(uint32_t a, uint32_t b)
 {
     uint32_t r;
     asm("min.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+template <> __device__ __forceinline__ uint32_t max2<__half>(uint32_t a, uint32_t b)
+{
+    uint32_t r;
+    asm("max.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
     return r;
 }
 template <> __device__ __forceinline__ uint32_t min2<__nv_bfloat16>(uint32_t a, uint32_t b)
@@ -39,139 +47,209 @@ template <> __device__ __forceinline__ uint32_t min2<__nv_bfloat16>(uint32_t a, 
     asm("min.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
     return r;
 }
+template <> __device__ __forceinline__ uint32_t max2<__nv_bfloat16>(uint32_t a, uint32_t b)
+{
+    uint32_t r;
+    asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
 
-// The row's position and place, or valid = false.
-struct RowPlace {
-    bool valid;
-    int t, page;
-};
+// Two rows <-> words {channel of the first, channel of the second}.
+template <typename T, int D> __device__ __forceinline__ void interleave(const Row<T, D> (&row)[2], uint32_t (&w)[Row<T, D>::C])
+{
+#pragma unroll
+    for (int k = 0; k < Row<T, D>::WORDS; ++k) {
+        w[2 * k] = __byte_perm(row[0].w[k], row[1].w[k], 0x5410);
+        w[2 * k + 1] = __byte_perm(row[0].w[k], row[1].w[k], 0x7632);
+    }
+}
+template <typename T, int D> __device__ __forceinline__ void separate(const uint32_t (&w)[Row<T, D>::C], Row<T, D> (&row)[2])
+{
+#pragma unroll
+    for (int k = 0; k < Row<T, D>::WORDS; ++k) {
+        row[0].w[k] = __byte_perm(w[2 * k], w[2 * k + 1], 0x5410);
+        row[1].w[k] = __byte_perm(w[2 * k], w[2 * k + 1], 0x7632);
+    }
+}
+template <int C> __device__ __forceinline__ void put_words(uint32_t *p, const uint32_t (&w)[C])
+{
+#pragma unroll
+    for (int k = 0; k < C; k += 4) *reinterpret_cast<uint4 *>(p + k) = make_uint4(w[k], w[k + 1], w[k + 2], w[k + 3]);
+}
+template <int C> __device__ __forceinline__ void get_words(const uint32_t *p, uint32_t (&w)[C])
+{
+#pragma unroll
+    for (int k = 0; k < C; k += 4) {
+        const uint4 v = *reinterpret_cast<const uint4 *>(p + k);
+        w[k] = v.x; w[k + 1] = v.y; w[k + 2] = v.z; w[k + 3] = v.w;
+    }
+}
+// A lane's C gather indices of a head (identity without a reorder index).
+template <int C, int D> __device__ __forceinline__ void load_index(int (&idx)[C], const int32_t *reorder, int h, int c0)
+{
+#pragma unroll
+    for (int j = 0; j < C; j += 4) {
+        int4 v = make_int4(c0 + j, c0 + j + 1, c0 + j + 2, c0 + j + 3);
+        if (reorder) {
+            const int32_t *r = reorder + h * D + c0 + j;
+            v = make_int4(r[0], r[1], r[2], r[3]);
+        }
+        idx[j] = v.x & (D - 1); idx[j + 1] = v.y & (D - 1); idx[j + 2] = v.z & (D - 1); idx[j + 3] = v.w & (D - 1);
+    }
+}
 
 template <typename T, int D, int NG, bool IS_V>
-__device__ __forceinline__ void append_rows(const AppendIo &io, const PagedSeq &seq, int b, int i, int h_first, int h_step, int h_end, bool any, T *raw, T *turned)
+__device__ __forceinline__ void append_rows(const AppendIo &io, const PagedSeq &seq, int b, int i, int h_first, int h_step, int h_end, uint32_t *raw, uint32_t *turned)
 {
     using R = Row<T, D>;
     constexpr int C = R::C, LANES = 16 / NG;      // lanes of a group
     const PagedArgs &a = io.p;
     const skvq_paged_config &cfg = a.cfg;
-    const int sub = threadIdx.x & 15, P = cfg.page_tokens;
-    const bool have = any && i < seq.n;
-    const int t = seq.len - seq.n + i;
-    int page = -1;
-    if (have) {
-        page = a.batch.page_table[(int64_t)b * a.batch.max_pages + t / P];
-        if (page < 0 || page >= cfg.n_pages) {
-            page = -1;
-            if (sub == 0) set_status(a.c.status, SKVQ_STATUS_BAD_PAGE);
+    const int sub = threadIdx.x & 15, P = cfg.page_tokens, c0 = sub * C;
+    const bool rot = !IS_V && a.rope.table, inter = a.rope.interleaved;
+    bool have[2], keep[2];
+    int page[2], ring[2];
+    int64_t page_row[2];
+    float2 cs[2][IS_V ? 1 : C];
+    const T *src[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const int t = seq.len - seq.n + i + k;
+        have[k] = i + k < seq.n;
+        page[k] = -1;
+        if (have[k]) {
+            page[k] = a.batch.page_table[(int64_t)b * a.batch.max_pages + t / P];
+            if (page[k] < 0 || page[k] >= cfg.n_pages) {
+                page[k] = -1;
+                if (sub == 0) set_status(a.c.status, SKVQ_STATUS_BAD_PAGE);
+            }
         }
+        if constexpr (!IS_V) {
+            if (rot && have[k]) load_angles(cs[k], a.rope, t, c0);
+        }
+        src[k] = static_cast<const T *>(IS_V ? io.v : io.k) + (int64_t)(seq.row0 + i + k) * (IS_V ? io.v_stride : io.k_stride) + c0;
+        page_row[k] = ((int64_t)page[k] * cfg.n_kv_heads) * P + t % P;
+        keep[k] = cfg.window > 0 && have[k] && page[k] >= 0 && t >= seq.len - cfg.ring_tokens;
+        ring[k] = cfg.ring_tokens > 0 ? t % cfg.ring_tokens : 0;
     }
-    const bool rot = !IS_V && a.rope.table;
-    const int c0 = sub * C;
-    const bool inter = a.rope.interleaved;
-    float2 cs[IS_V ? 1 : C];
-    if constexpr (!IS_V) {
-        if (rot && have) load_angles(cs, a.rope, t, c0);
-    }
-    const T *src = static_cast<const T *>(IS_V ? io.v : io.k) + (int64_t)(seq.row0 + i) * (IS_V ? io.v_stride : io.k_stride) + c0;
     const int32_t *reorder = IS_V ? a.c.reorder_v : a.c.reorder_k;
     const float *alphas = IS_V ? a.c.alpha_v : a.c.alpha_k;
-    const int64_t page_row = ((int64_t)page * cfg.n_kv_heads) * P + t % P;
     uint8_t *codes_pool = static_cast<uint8_t *>(IS_V ? a.c.v_codes : a.c.k_codes);
     uint32_t *meta_pool = static_cast<uint32_t *>(IS_V ? a.c.v_meta : a.c.k_meta);
-    const bool keep = cfg.window > 0 && t >= seq.len - cfg.ring_tokens;
-    const int ring = cfg.ring_tokens > 0 ? t % cfg.ring_tokens : 0;
     T *win = static_cast<T *>(IS_V ? a.c.v_win : a.c.k_win);
 
-    R next;
+    R next[2];
 #pragma unroll
-    for (int k = 0; k < R::WORDS; ++k) next.w[k] = 0u;
-    if (have && h_first < h_end) next.load(src + (int64_t)h_first * D);
+    for (int k = 0; k < 2; ++k) {
+#pragma unroll
+        for (int m = 0; m < R::WORDS; ++m) next[k].w[m] = 0u;
+        if (have[k] && h_first < h_end) next[k].load(src[k] + (int64_t)h_first * D);
+    }
     for (int h0 = h_first; __any_sync(0xffffffffu, h0 < h_end); h0 += h_step) {
-        const bool here = have && h0 < h_end;
+        const bool here = h0 < h_end;
         const int h = min(h0, h_end - 1);
         int idx[C];
-#pragma unroll
-        for (int j = 0; j < C; j += 4) {
-            int4 v = make_int4(c0 + j, c0 + j + 1, c0 + j + 2, c0 + j + 3);
-            if (reorder) {
-                const int32_t *r = reorder + h * D + c0 + j;
-                v = make_int4(r[0], r[1], r[2], r[3]);
-            }
-            idx[j] = v.x & (D - 1); idx[j + 1] = v.y & (D - 1); idx[j + 2] = v.z & (D - 1); idx[j + 3] = v.w & (D - 1);
-        }
+        load_index<C, D>(idx, reorder, h, c0);
         const float alpha = alphas ? alphas[h * NG + sub / LANES] : 1.0f;
-        R row = next;
-        if (have && h0 + h_step < h_end) next.load(src + (int64_t)(h0 + h_step) * D);
+        uint32_t w[C];
+        interleave<T, D>(next, w);
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+            if (have[k] && h0 + h_step < h_end) next[k].load(src[k] + (int64_t)(h0 + h_step) * D);
         if constexpr (!IS_V) {
             if (rot) {
+                const int rot_dim = a.rope.rot_dim, half = rot_dim / 2;
                 if (!inter) {
-                    row.store(raw + c0);
+                    put_words(raw + c0, w);
                     __syncwarp();
                 }
-                if (here) rotate_row<T, D>(row, c0, cs, raw, a.rope.rot_dim, inter);
+#pragma unroll
+                for (int j = 0; j < C; ++j) {
+                    const int c = c0 + j;
+                    if (c < rot_dim && (!inter || !(j & 1))) {
+                        const float2 x = floats<T>(w[j]);
+                        if (inter) {
+                            const float2 o = floats<T>(w[j + 1]);
+                            w[j] = packed<T>(rotate_first(x.x, o.x, cs[0][j].x, cs[0][j].y), rotate_first(x.y, o.y, cs[1][j].x, cs[1][j].y));
+                            w[j + 1] = packed<T>(rotate_second(x.x, o.x, cs[0][j].x, cs[0][j].y), rotate_second(x.y, o.y, cs[1][j].x, cs[1][j].y));
+                        } else if (c < half) {
+                            const float2 o = floats<T>(raw[c + half]);
+                            w[j] = packed<T>(rotate_first(x.x, o.x, cs[0][j].x, cs[0][j].y), rotate_first(x.y, o.y, cs[1][j].x, cs[1][j].y));
+                        } else {
+                            const float2 o = floats<T>(raw[c - half]);
+                            w[j] = packed<T>(rotate_second(o.x, x.x, cs[0][j].x, cs[0][j].y), rotate_second(o.y, x.y, cs[1][j].x, cs[1][j].y));
+                        }
+                    }
+                }
             }
         }
-        row.store(turned + c0);
+        put_words(turned + c0, w);
         __syncwarp();
-        const uint16_t *from = reinterpret_cast<const uint16_t *>(turned);
 #pragma unroll
-        for (int j = 0; j < C; j += 2) row.w[j / 2] = (uint32_t)from[idx[j]] | (uint32_t)from[idx[j + 1]] << 16;
+        for (int j = 0; j < C; ++j) w[j] = turned[idx[j]];
         __syncwarp();
 
-        // extremes as the pair {min, -max}: min serves both
-        uint32_t mn = row.w[0], ng = row.w[0] ^ 0x80008000u;
+        uint32_t mn = w[0], mx = w[0];
 #pragma unroll
-        for (int k = 1; k < R::WORDS; ++k) { mn = min2<T>(mn, row.w[k]); ng = min2<T>(ng, row.w[k] ^ 0x80008000u); }
-        uint32_t ext = min2<T>(__byte_perm(mn, ng, 0x5410), __byte_perm(mn, ng, 0x7632));
+        for (int j = 1; j < C; ++j) { mn = min2<T>(mn, w[j]); mx = max2<T>(mx, w[j]); }
 #pragma unroll
-        for (int m = 1; m < LANES; m <<= 1) ext = min2<T>(ext, __shfl_xor_sync(0xffffffffu, ext, m));
-        const float2 e = floats<T>(ext);
-        const float lo = __fadd_rn(__fmul_rn(alpha, e.x), 0.0f), hi = __fadd_rn(__fmul_rn(alpha, -e.y), 0.0f);
-        const __half2 hz = __halves2half2(__float2half_rn(__fmul_rn(__fsub_rn(hi, lo), 1.0f / 15.0f)), __float2half_rn(lo));
-        const float hf = __low2float(hz), zf = __high2float(hz);
-        constexpr float MAGIC = 12582912.0f;      // 1.5 2^23: a sum with it is rounded to an integer, ties to even
-        const float r = hf != 0.0f ? __frcp_rn(hf) : 0.0f;
-        float far = 0.f, p[C / 4];      // largest remainder; four codes in a sum
+        for (int m = 1; m < LANES; m <<= 1) {
+            mn = min2<T>(mn, __shfl_xor_sync(0xffffffffu, mn, m));
+            mx = max2<T>(mx, __shfl_xor_sync(0xffffffffu, mx, m));
+        }
+        const float2 mnf = floats<T>(mn), mxf = floats<T>(mx);
 #pragma unroll
-        for (int j = 0; j < C; j += 2) {
-            const float2 x = floats<T>(row.w[j / 2]);
+        for (int k = 0; k < 2; ++k) {
+            const float lo = __fadd_rn(__fmul_rn(alpha, k ? mnf.y : mnf.x), 0.0f), hi = __fadd_rn(__fmul_rn(alpha, k ? mxf.y : mxf.x), 0.0f);
+            const __half2 hz = __halves2half2(__float2half_rn(__fmul_rn(__fsub_rn(hi, lo), 1.0f / 15.0f)), __float2half_rn(lo));
+            const float hf = __low2float(hz), zf = __high2float(hz);
+            constexpr float MAGIC = 12582912.0f;      // 1.5 2^23: a sum with it is rounded to an integer, ties to even
+            const float r = hf != 0.0f ? __frcp_rn(hf) : 0.0f;
+            float far = 0.f, p[C / 4];      // largest remainder; four codes in a sum
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
+            for (int j = 0; j < C; ++j) {
+                const float2 x = floats<T>(w[j]);
                 const float d = __fsub_rn(k ? x.y : x.x, zf);
                 const float c = __fsub_rn(__fmaf_rn(d, r, MAGIC), MAGIC);
                 far = fmaxf(far, fabsf(__fmaf_rn(-c, hf, d)));
                 const float q = fminf(fmaxf(c, 0.0f), 15.0f);
-                const int n = j + k;
-                p[n / 4] = n % 4 == 0 ? q : __fmaf_rn(q, (float)(1 << (4 * (n % 4))), p[n / 4]);
+                p[j / 4] = j % 4 == 0 ? q : __fmaf_rn(q, (float)(1 << (4 * (j % 4))), p[j / 4]);
             }
-        }
-        uint32_t codes = (uint32_t)(int)p[0];
-        if constexpr (C == 8) codes |= (uint32_t)(int)p[1] << 16;
-        // (also taken for quotients beyond 2^22, which the sum with MAGIC cannot round, and for infinities)
-        if (!(far < 0.5f * hf * (1.0f - 3.814697265625e-06f)) && hf != 0.0f) {
-            codes = 0u;
+            uint32_t codes = (uint32_t)(int)p[0];
+            if constexpr (C == 8) codes |= (uint32_t)(int)p[1] << 16;
+            // (also taken for quotients beyond 2^22, which the sum with MAGIC cannot round, and for infinities)
+            if (!(far < 0.5f * hf * (1.0f - 3.814697265625e-06f)) && hf != 0.0f) {
+                codes = 0u;
 #pragma unroll
-            for (int j = 0; j < C; ++j) {
-                const float2 x = floats<T>(row.w[j / 2]);
-                const float c = fminf(fmaxf(rintf(__fdiv_rn(__fsub_rn(j & 1 ? x.y : x.x, zf), hf)), 0.0f), 15.0f);
-                codes |= (uint32_t)(int)c << (4 * j);
+                for (int j = 0; j < C; ++j) {
+                    const float2 x = floats<T>(w[j]);
+                    const float c = fminf(fmaxf(rintf(__fdiv_rn(__fsub_rn(k ? x.y : x.x, zf), hf)), 0.0f), 15.0f);
+                    codes |= (uint32_t)(int)c << (4 * j);
+                }
+            }
+            if (hf == 0.0f) codes = 0u;
+            if (here && page[k] >= 0) {
+                const int64_t at = page_row[k] + (int64_t)h * P;
+                if constexpr (C == 8) reinterpret_cast<uint32_t *>(codes_pool + at * (D / 2))[sub] = codes;
+                else reinterpret_cast<uint16_t *>(codes_pool + at * (D / 2))[sub] = (uint16_t)codes;
+                if (sub % LANES == 0) meta_pool[at * NG + sub / LANES] = *reinterpret_cast<const uint32_t *>(&hz);
             }
         }
-        if (hf == 0.0f) codes = 0u;
-        if (here && page >= 0) {
-            const int64_t at = page_row + (int64_t)h * P;
-            if constexpr (C == 8) reinterpret_cast<uint32_t *>(codes_pool + at * (D / 2))[sub] = codes;
-            else reinterpret_cast<uint16_t *>(codes_pool + at * (D / 2))[sub] = (uint16_t)codes;
-            if (sub % LANES == 0) meta_pool[at * NG + sub / LANES] = *reinterpret_cast<const uint32_t *>(&hz);
-            if (keep) row.store(win + (((int64_t)seq.slot * cfg.n_kv_heads + h) * cfg.ring_tokens + ring) * D + c0);
+        if (here && (keep[0] || keep[1])) {
+            R out[2];
+            separate<T, D>(w, out);
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+                if (keep[k]) out[k].store(win + (((int64_t)seq.slot * cfg.n_kv_heads + h) * cfg.ring_tokens + ring[k]) * D + c0);
         }
     }
 }
 
-// blockIdx: x = tokens of a sequence, y = runs of heads, keys and values in turn, z = sequences.
+// blockIdx: x = tokens of a sequence (16, or a pair), y = runs of heads, keys and values in turn, z = sequences.
 template <typename T, int D, int NG>
 __global__ void __launch_bounds__(kRowThreads) paged_append_kernel(const __grid_constant__ AppendIo io)
 {
-    __shared__ __align__(16) T rows[2 * kRowWarps][2][D + 8];      // a half-warp each: as read, rotated; the two rows of a warp start 4 banks apart
+    __shared__ __align__(16) uint32_t rows[2 * kRowWarps][2][D + 4];      // a half-warp each: as read, rotated
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;");
     const PagedArgs &a = io.p;
@@ -181,12 +259,12 @@ __global__ void __launch_bounds__(kRowThreads) paged_append_kernel(const __grid_
         if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) set_status(a.c.status, SKVQ_STATUS_BAD_BATCH);
         return;
     }
-    const int i0 = io.bulk ? blockIdx.x * kBulkTokens : blockIdx.x;
+    const int i0 = blockIdx.x * (io.bulk ? kBulkTokens : 2);
     if (i0 >= seq.n) return;
-    const int i = io.bulk ? i0 + unit : i0, h0 = (blockIdx.y >> 1) * io.heads, h1 = min(h0 + io.heads, a.cfg.n_kv_heads);
+    const int i = io.bulk ? i0 + 2 * unit : i0, h0 = (blockIdx.y >> 1) * io.heads, h1 = min(h0 + io.heads, a.cfg.n_kv_heads);
     const int first = io.bulk ? h0 : h0 + unit, step = io.bulk ? 1 : 2 * kRowWarps;
-    if (blockIdx.y & 1) append_rows<T, D, NG, true>(io, seq, b, i, first, step, h1, true, rows[unit][0], rows[unit][1]);
-    else append_rows<T, D, NG, false>(io, seq, b, i, first, step, h1, true, rows[unit][0], rows[unit][1]);
+    if (blockIdx.y & 1) append_rows<T, D, NG, true>(io, seq, b, i, first, step, h1, rows[unit][0], rows[unit][1]);
+    else append_rows<T, D, NG, false>(io, seq, b, i, first, step, h1, rows[unit][0], rows[unit][1]);
 }
 
 struct ReadIo {
@@ -201,7 +279,7 @@ __global__ void __launch_bounds__(kRowThreads) paged_read_kernel(const __grid_co
 {
     using R = Row<T, D>;
     constexpr int C = R::C, LANES = 16 / NG;
-    __shared__ __align__(16) T rows[2 * kRowWarps][D + 8];
+    __shared__ __align__(16) uint32_t rows[2 * kRowWarps][D + 4];
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;");
     const PagedArgs &a = io.p;
@@ -214,75 +292,93 @@ __global__ void __launch_bounds__(kRowThreads) paged_read_kernel(const __grid_co
     }
     const bool is_v = blockIdx.y & 1;
     T *dst = static_cast<T *>(is_v ? io.v : io.k);
-    const int i0 = io.bulk ? blockIdx.x * kBulkTokens : blockIdx.x;
+    const int i0 = blockIdx.x * (io.bulk ? kBulkTokens : 2);
     if (i0 >= seq.n || !dst) return;
-    const int i = io.bulk ? i0 + unit : i0, h_begin = (blockIdx.y >> 1) * io.heads, h_end = min(h_begin + io.heads, cfg.n_kv_heads);
+    const int i = io.bulk ? i0 + 2 * unit : i0, h_begin = (blockIdx.y >> 1) * io.heads, h_end = min(h_begin + io.heads, cfg.n_kv_heads);
     const int first = io.bulk ? h_begin : h_begin + unit, step = io.bulk ? 1 : 2 * kRowWarps;
-    const int P = cfg.page_tokens, t = seq.len - seq.n + i, c0 = sub * C;
-    bool have = i < seq.n;
-    const bool recent = io.window && cfg.window > 0 && t >= seq.len - cfg.window;
-    int page = 0;
-    if (have && !recent) {
-        page = a.batch.page_table[(int64_t)b * a.batch.max_pages + t / P];
-        if (page < 0 || page >= cfg.n_pages) {
-            have = false;
-            if (sub == 0) set_status(a.c.status, SKVQ_STATUS_BAD_PAGE);
+    const int P = cfg.page_tokens, c0 = sub * C;
+    bool have[2], recent[2];
+    int64_t page_row[2], win_row[2];
+    T *out[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const int t = seq.len - seq.n + i + k;
+        have[k] = i + k < seq.n;
+        recent[k] = io.window && cfg.window > 0 && t >= seq.len - cfg.window;
+        int page = 0;
+        if (have[k] && !recent[k]) {
+            page = a.batch.page_table[(int64_t)b * a.batch.max_pages + t / P];
+            if (page < 0 || page >= cfg.n_pages) {
+                have[k] = false;
+                if (sub == 0) set_status(a.c.status, SKVQ_STATUS_BAD_PAGE);
+            }
         }
+        page_row[k] = ((int64_t)page * cfg.n_kv_heads) * P + t % P;
+        win_row[k] = recent[k] ? (int64_t)seq.slot * cfg.n_kv_heads * cfg.ring_tokens + t % cfg.ring_tokens : 0;
+        out[k] = dst + (int64_t)(seq.row0 + i + k) * (is_v ? io.v_stride : io.k_stride) + c0;
     }
     const int32_t *reorder = is_v ? a.c.reorder_v : a.c.reorder_k;
-    const int64_t page_row = ((int64_t)page * cfg.n_kv_heads) * P + t % P;
     const uint8_t *codes_pool = static_cast<const uint8_t *>(is_v ? a.c.v_codes : a.c.k_codes);
     const uint32_t *meta_pool = static_cast<const uint32_t *>(is_v ? a.c.v_meta : a.c.k_meta);
     const T *win = static_cast<const T *>(is_v ? a.c.v_win : a.c.k_win);
-    dst += (int64_t)(seq.row0 + i) * (is_v ? io.v_stride : io.k_stride) + c0;
-    uint16_t *mine = reinterpret_cast<uint16_t *>(rows[unit]);
-    auto load = [&](int h, uint32_t &codes, uint32_t &hz) {
-        const int64_t at = page_row + (int64_t)h * P;
-        codes = C == 8 ? reinterpret_cast<const uint32_t *>(codes_pool + at * (D / 2))[sub] : reinterpret_cast<const uint16_t *>(codes_pool + at * (D / 2))[sub];
-        hz = meta_pool[at * NG + sub / LANES];
-    };
-    uint32_t codes_next = 0u, hz_next = 0u;
-    if (have && !recent && first < h_end) load(first, codes_next, hz_next);
-    for (int h0 = first; __any_sync(0xffffffffu, h0 < h_end); h0 += step) {
-        const bool here = have && h0 < h_end;
-        const int h = min(h0, h_end - 1);
-        const uint32_t codes = codes_next;
-        const __half2 hz = *reinterpret_cast<const __half2 *>(&hz_next);
-        if (have && !recent && h0 + step < h_end) load(h0 + step, codes_next, hz_next);
-        R row;
-        if (recent) {
-            if (here) row.load(win + (((int64_t)seq.slot * cfg.n_kv_heads + h) * cfg.ring_tokens + t % cfg.ring_tokens) * D + c0);
-        } else {
-            const float hf = __low2float(hz), zf = __high2float(hz);
-            float v[C];
+    uint32_t *mine = rows[unit];
+    uint32_t codes_next[2] = {0u, 0u}, hz_next[2] = {0u, 0u};
+    auto load = [&](int h) {
 #pragma unroll
-            for (int j = 0; j < C; ++j)      // 2^23 + code, minus 2^23
-                v[j] = __fadd_rn(__fmul_rn(hf, __fsub_rn(__uint_as_float(0x4B000000u | ((codes >> (4 * j)) & 15u)), 8388608.0f)), zf);
-#pragma unroll
-            for (int k = 0; k < R::WORDS; ++k) row.w[k] = packed<T>(v[2 * k], v[2 * k + 1]);
-        }
-        if (reorder) {
-            const int32_t *idx = reorder + h * D + c0;
-#pragma unroll
-            for (int k = 0; k < R::WORDS; ++k) {
-                mine[idx[2 * k] & (D - 1)] = (uint16_t)row.w[k];
-                mine[idx[2 * k + 1] & (D - 1)] = (uint16_t)(row.w[k] >> 16);
+        for (int k = 0; k < 2; ++k) {
+            if (have[k] && !recent[k] && h < h_end) {
+                const int64_t at = page_row[k] + (int64_t)h * P;
+                codes_next[k] = C == 8 ? reinterpret_cast<const uint32_t *>(codes_pool + at * (D / 2))[sub] : reinterpret_cast<const uint16_t *>(codes_pool + at * (D / 2))[sub];
+                hz_next[k] = meta_pool[at * NG + sub / LANES];
             }
-            __syncwarp();
-            row.load(rows[unit] + c0);
-            __syncwarp();
         }
-        if (here) row.store(dst + (int64_t)h * D);
+    };
+    load(first);
+    for (int h0 = first; __any_sync(0xffffffffu, h0 < h_end); h0 += step) {
+        const bool here = h0 < h_end;
+        const int h = min(h0, h_end - 1);
+        R row[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const uint32_t codes = codes_next[k];
+            const __half2 hz = *reinterpret_cast<const __half2 *>(&hz_next[k]);
+            const float hf = __low2float(hz), zf = __high2float(hz);
+#pragma unroll
+            for (int m = 0; m < R::WORDS; ++m) {
+                float v[2];
+#pragma unroll
+                for (int e = 0; e < 2; ++e)      // 2^23 + code, minus 2^23
+                    v[e] = __fadd_rn(__fmul_rn(hf, __fsub_rn(__uint_as_float(0x4B000000u | ((codes >> (8 * m + 4 * e)) & 15u)), 8388608.0f)), zf);
+                row[k].w[m] = packed<T>(v[0], v[1]);
+            }
+            if (recent[k] && have[k] && here) row[k].load(win + (win_row[k] + (int64_t)h * cfg.ring_tokens) * D + c0);
+        }
+        load(h0 + step);
+        if (reorder) {
+            uint32_t w[C];
+            int idx[C];
+            load_index<C, D>(idx, reorder, h, c0);
+            interleave<T, D>(row, w);
+#pragma unroll
+            for (int j = 0; j < C; ++j) mine[idx[j]] = w[j];
+            __syncwarp();
+            get_words(mine + c0, w);
+            __syncwarp();
+            separate<T, D>(w, row);
+        }
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+            if (here && have[k]) row[k].store(out[k] + (int64_t)h * D);
     }
 }
 
-// Grid: tokens of the longest sequence, runs of heads for keys and for values, sequences.  Side-by-side tokens need at least two; a run
+// Grid: tokens of the longest sequence, runs of heads for keys and for values, sequences.  A run
 // is as long as keeps several waves of CTAs (the angles are loaded once per run).
 template <typename Io> dim3 row_grid(const PagedArgs &a, Io &io)
 {
     const int H = a.cfg.n_kv_heads;
-    io.bulk = a.batch.max_new >= 4 ? 1 : 0;
-    const long long tokens = io.bulk ? (a.batch.max_new + kBulkTokens - 1) / kBulkTokens : a.batch.max_new;
+    io.bulk = a.batch.max_new >= 8 ? 1 : 0;
+    const long long tokens = io.bulk ? (a.batch.max_new + kBulkTokens - 1) / kBulkTokens : (a.batch.max_new + 1) / 2;
     if (io.bulk) {
         io.heads = H;
         while (io.heads > 4 && tokens * a.batch.n_seqs * 2 * ((H + io.heads - 1) / io.heads) < 32LL * sm_count()) io.heads = (io.heads + 1) / 2;

@@ -1,6 +1,6 @@
 // skvq_paged_attention for few query rows per (sequence, KV head): single-token decode, drafted tokens.
 //
-// The rows of a KV head are packed: row = new token * (Hq/Hkv) + query head, 8 NT rows per item (NT = 1, 2 or 4).  Items of
+// The rows of a KV head are packed: row = new token * (Hq/Hkv) + query head, 8 NT rows per item (NT = 1 or 2).  Items of
 // the whole batch are laid end to end, priced in 32-token tiles (a tile of the unquantized window costs kRingCost), and cut
 // into equal runs, one per CTA: ragged batches and long single sequences load the GPU alike.  The four warps of a CTA take
 // quarters of a run, stream their tiles through private shared-memory rings, and join their softmax states at the end; an item
@@ -47,6 +47,7 @@ struct SplitArgs {
     PagedAttnArgs a;
     int n_slots;
     int rows;      // rows per item: 8 NT
+    int whole;     // a CTA takes a whole item: nothing to join
 };
 
 template <int D, int NG, int NT>
@@ -155,20 +156,20 @@ struct SeqCost {
     int cost;                  // of one item, at least 1
     int m_tiles;               // items per KV head
 };
-__device__ __forceinline__ SeqCost seq_cost(const PagedArgs &p, const PagedSeq &s, int rows)
+__device__ __forceinline__ SeqCost seq_cost(const PagedArgs &p, const PagedSeq &s, int rows, int whole)
 {
     SeqCost c;
     const int rep = p.cfg.n_q_heads / p.cfg.n_kv_heads;
     const int lq = max(s.len - p.cfg.window, 0);
     c.tiles_c = (lq + kTile - 1) / kTile;
     c.tiles_r = (s.len - lq + kRingTile - 1) / kRingTile;
-    c.cost = max(c.tiles_c + kRingCost * c.tiles_r, 1);
+    c.cost = whole ? 1 : max(c.tiles_c + kRingCost * c.tiles_r, 1);
     c.m_tiles = s.n * rep <= kFewRows ? (s.n * rep + rows - 1) / rows : 0;      // the others are the tcgen05 kernel's
     return c;
 }
 
 template <typename T, int D, int NG, int NT>
-__global__ void __launch_bounds__(kSplitThreads, NT == 4 ? 2 : (NT == 2 ? 3 : 4)) paged_split_kernel(const __grid_constant__ SplitArgs args)
+__global__ void __launch_bounds__(kSplitThreads, NT == 2 ? 2 : 3) paged_split_kernel(const __grid_constant__ SplitArgs args)
 {
     using Geo = Geometry<D, NG, NT>;
     constexpr int ROWS = Geo::ROWS;
@@ -197,7 +198,7 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 4 ? 2 : (NT == 2 ? 3 : 4)
             if (b < B) {
                 PagedSeq s;
                 if (paged_sequence(p, b, false, s)) {
-                    const SeqCost sc = seq_cost(p, s, ROWS);
+                    const SeqCost sc = seq_cost(p, s, ROWS, args.whole);
                     c = (long long)sc.cost * sc.m_tiles * cfg.n_kv_heads;
                 } else if (blockIdx.x == 0) {
                     set_status(p.c.status, SKVQ_STATUS_BAD_BATCH);
@@ -226,7 +227,7 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 4 ? 2 : (NT == 2 ? 3 : 4)
     long long f = blockIdx.x * ups;
     const long long f1 = min(f + ups, total);
     int *desc = reinterpret_cast<int *>(a.ws) + (size_t)blockIdx.x * kDescInts;
-    if (tid == 0) desc[0] = 0;
+    if (tid == 0 && !args.whole) desc[0] = 0;
     if (f >= f1) return;
     int b;
     {
@@ -243,7 +244,7 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 4 ? 2 : (NT == 2 ? 3 : 4)
         while (pre[b + 1] <= f) ++b;
         PagedSeq seq;
         paged_sequence(p, b, false, seq);
-        const SeqCost sc = seq_cost(p, seq, ROWS);
+        const SeqCost sc = seq_cost(p, seq, ROWS, args.whole);
         const long long item = (f - pre[b]) / sc.cost;
         const int off = (int)((f - pre[b]) - item * sc.cost);
         const int take = (int)min((long long)(sc.cost - off), f1 - f);
@@ -259,7 +260,7 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 4 ? 2 : (NT == 2 ? 3 : 4)
 
         // ---- this warp's quarter of the run; its first pages are on their way while the queries are prepared
         auto tile_of = [&](int x) { return x <= sc.tiles_c ? x : sc.tiles_c + (x - sc.tiles_c + kRingCost - 1) / kRingCost; };
-        const int seg0 = tile_of(off), seg1 = tile_of(off + take);
+        const int seg0 = tile_of(off), seg1 = args.whole ? sc.tiles_c + sc.tiles_r : tile_of(off + take);
         const int c0 = min(seg0, sc.tiles_c), c1 = max(min(min(seg1, sc.tiles_c), (limit_hi + kTile - 1) / kTile), c0);
         const int q0 = c0 + (int)((long long)(c1 - c0) * warp / kSplitWarps), q1 = c0 + (int)((long long)(c1 - c0) * (warp + 1) / kSplitWarps);
         const int P = cfg.page_tokens, page_shift = __ffs(P) - 1;
@@ -784,7 +785,7 @@ __global__ void __launch_bounds__(D) paged_merge_kernel(const __grid_constant__ 
     }
 }
 
-// The most rows a KV head of this kernel can have, and the rows per item: 8, 16 or 32.
+// The most rows a KV head of this kernel can have, and the rows per item: 8 or 16.
 long long few_rows(const skvq_paged_config &cfg, const skvq_paged_batch &batch)
 {
     const long long rows = (long long)batch.max_new * (cfg.n_q_heads / cfg.n_kv_heads);
@@ -793,25 +794,45 @@ long long few_rows(const skvq_paged_config &cfg, const skvq_paged_batch &batch)
 int item_rows(const skvq_paged_config &cfg, const skvq_paged_batch &batch)
 {
     const long long rows = few_rows(cfg, batch);
-    return rows <= 8 ? 8 : (rows <= 16 ? 16 : 32);
+    return rows <= 8 ? 8 : 16;
+}
+
+// Contexts so short that a CTA per item is done sooner than several and a merge (512 tokens, window 128, 16 or 64 sequences of 8 KV heads:
+// 24 us split, 16 whole; 40 and 31).
+constexpr int kWholeCost = 48;
+constexpr long long kMaxSlots = 16384;
+
+// Price of an item at most, and the items of a step at most.
+long long item_cost(const skvq_paged_config &cfg, const skvq_paged_batch &batch)
+{
+    const long long lq = batch.max_len > cfg.window ? batch.max_len - cfg.window : 0;
+    return (lq + kTile - 1) / kTile + kRingCost * ((batch.max_len - lq + kRingTile - 1) / kRingTile) + 1;
+}
+long long item_count(const skvq_paged_config &cfg, const skvq_paged_batch &batch)
+{
+    const int per = item_rows(cfg, batch);
+    return (long long)batch.n_seqs * cfg.n_kv_heads * ((few_rows(cfg, batch) + per - 1) / per);
+}
+bool whole_items(const skvq_paged_config &cfg, const skvq_paged_batch &batch, int n_splits)
+{
+    return n_splits == 0 && item_cost(cfg, batch) <= kWholeCost && item_count(cfg, batch) <= kMaxSlots;
 }
 
 int split_slots(const skvq_paged_config &cfg, const skvq_paged_batch &batch, int n_splits)
 {
     const int per = item_rows(cfg, batch);
-    const long long m_tiles = (few_rows(cfg, batch) + per - 1) / per;
-    const long long lq = batch.max_len > cfg.window ? batch.max_len - cfg.window : 0;
-    const long long cost = (lq + kTile - 1) / kTile + kRingCost * ((batch.max_len - lq + kRingTile - 1) / kRingTile) + 1;
-    const long long items = (long long)batch.n_seqs * cfg.n_kv_heads * m_tiles;
+    const long long items = item_count(cfg, batch), cost = item_cost(cfg, batch);
+    if (whole_items(cfg, batch, n_splits)) return (int)items;
     long long slots;
     if (n_splits > 0) slots = (long long)n_splits * items;
     else {
-        // one wave of resident CTAs, each with two tiles per warp at least: a shorter run costs more to join than it saves
-        slots = (per == 8 ? 4LL : (per == 16 ? 3LL : 2LL)) * sm_count();
+        // one wave of resident CTAs (a CTA more per SM spills: serving mix 597 us against 580), each with two tiles per warp at least: a
+        // shorter run costs more to join than it saves
+        slots = (per == 8 ? 3LL : 2LL) * sm_count();
         if (slots > items * cost / 8) slots = items * cost / 8;
     }
     if (slots > items * cost) slots = items * cost;
-    if (slots > 16384) slots = 16384;
+    if (slots > kMaxSlots) slots = kMaxSlots;
     return slots < 1 ? 1 : (int)slots;
 }
 
@@ -819,19 +840,20 @@ template <typename T, int D, int NG, int NT>
 cudaError_t launch_split(const PagedAttnArgs &a, cudaStream_t stream)
 {
     using Geo = Geometry<D, NG, NT>;
-    const SplitArgs s{a, split_slots(a.p.cfg, a.p.batch, a.n_splits), Geo::ROWS};
+    const bool whole = whole_items(a.p.cfg, a.p.batch, a.n_splits);
+    const SplitArgs s{a, split_slots(a.p.cfg, a.p.batch, a.n_splits), Geo::ROWS, whole};
     static unsigned long long done = 0;
     cudaError_t e = configure_smem_once(paged_split_kernel<T, D, NG, NT>, Geo::SMEM + (int)sizeof(long long) * (kMaxPagedSeqs + 1), done);
     if (e != cudaSuccess) return e;
     e = launch_chained(paged_split_kernel<T, D, NG, NT>, dim3(s.n_slots), kSplitThreads, Geo::SMEM + sizeof(long long) * (a.p.batch.n_seqs + 1), stream, s);
-    if (e != cudaSuccess) return e;
+    if (e != cudaSuccess || whole) return e;
     return launch_paged_merge(a, s.n_slots, Geo::ROWS, (int)few_rows(a.p.cfg, a.p.batch), kPScaleLog2, stream);
 }
 
 template <typename T, int D, int NG> cudaError_t launch_by_rows(const PagedAttnArgs &a, cudaStream_t stream)
 {
     const int rows = item_rows(a.p.cfg, a.p.batch);
-    return rows == 8 ? launch_split<T, D, NG, 1>(a, stream) : rows == 16 ? launch_split<T, D, NG, 2>(a, stream) : launch_split<T, D, NG, 4>(a, stream);
+    return rows == 8 ? launch_split<T, D, NG, 1>(a, stream) : launch_split<T, D, NG, 2>(a, stream);
 }
 
 template <typename T> cudaError_t launch_by_shape(const PagedAttnArgs &a, cudaStream_t stream)
@@ -843,6 +865,7 @@ template <typename T> cudaError_t launch_by_shape(const PagedAttnArgs &a, cudaSt
 
 size_t split_workspace_bytes(const skvq_paged_config &cfg, const skvq_paged_batch &batch, int n_splits)
 {
+    if (whole_items(cfg, batch, n_splits)) return 0;
     const size_t slots = split_slots(cfg, batch, n_splits);
     return (slots * kDescInts * 4 + slots * 2 * item_rows(cfg, batch) * partial_stride(cfg.head_dim) * 4 + 15) / 16 * 16;
 }

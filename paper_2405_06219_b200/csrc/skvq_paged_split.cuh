@@ -6,8 +6,9 @@
 namespace skvq {
 
 // Sequences with at most this many packed rows (new tokens * Hq/Hkv) per KV head go to the kernel for few rows, the others to the
-// tcgen05 kernel.
-constexpr int kFewRows = 32;
+// tcgen05 kernel.  Measured on 16 sequences of 1024 to 16384 tokens, 8 KV heads: 16 rows 114 us here, 237 there; 20 rows 209 here (a
+// second item per KV head, or wider ones), 198 there; 32 rows 256 and 235.
+constexpr int kFewRows = 16;
 
 // Workspace of a kernel: descriptor [n_slots][8] ints, then partials [n_slots][2][rows per item][D + 4] floats {o[D], m (log2
 // units), l, pad}.  A CTA's run holds at most one item that it continues (partial 0) and one that it begins and does not finish

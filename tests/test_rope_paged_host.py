@@ -182,8 +182,10 @@ def test_paged_calls_refuse_bad_arguments_before_any_launch(lib):
     assert call("read", x=None, y=None) == B.SKVQ_OK
     assert call("attention", args=dict(causal=2)) == B.SKVQ_ERR_INVALID_ARG
     assert call("attention", args=dict(n_splits=-1)) == B.SKVQ_ERR_INVALID_ARG
-    assert call("attention", args=dict(workspace=None)) == B.SKVQ_ERR_WORKSPACE
-    assert call("attention", args=dict(workspace_bytes=64)) == B.SKVQ_ERR_WORKSPACE
+    assert call("attention", args=dict(workspace=None, n_splits=2)) == B.SKVQ_ERR_WORKSPACE
+    assert call("attention", args=dict(workspace_bytes=64, n_splits=2)) == B.SKVQ_ERR_WORKSPACE
+    long = dict(max_pages=100, max_len=6400)      # (contexts as short as the others' here need no workspace)
+    assert call("attention", batch=long, args=dict(workspace=None)) == B.SKVQ_ERR_WORKSPACE
     assert call("attention", args=dict(workspace=fake + 4)) == B.SKVQ_ERR_MISALIGNED
     assert call("attention", lse=fake + 2) == B.SKVQ_ERR_MISALIGNED
     assert B.skvq_launch_count() == before
