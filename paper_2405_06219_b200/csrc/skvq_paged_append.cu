@@ -8,7 +8,7 @@
 // What bounds it is instructions, not bytes (a row at a time: 420 us for the append of a 32k-token prompt of 32 heads, 267 for reading it back,
 // floors of 105 each), so the code is formed without a division,
 //   code = rint(d / h): t = fma(d, RN(1/h), 1.5 2^23) holds rint(d RN(1/h)); the remainder d - code h tells whether the quotient can be
-//   near k + 0.5 (|remainder| >= h/2 (1 - 2^-18)); only then (ties included) the rows concerned divide.
+//   near k + 0.5 (|remainder| >= h/2 (1 - 2^-18)); only then is more done.
 // The quantizer arithmetic is explicitly rounded fp32: codes and parameters do not depend on compiler contraction.
 #include "skvq_paged_split.cuh"
 
@@ -107,6 +107,8 @@ __device__ __forceinline__ void append_rows(const AppendIo &io, const PagedSeq &
     const skvq_paged_config &cfg = a.cfg;
     const int sub = threadIdx.x & 15, P = cfg.page_tokens, c0 = sub * C;
     const bool rot = !IS_V && a.rope.table, inter = a.rope.interleaved;
+    const int rot_dim = a.rope.rot_dim, half = rot_dim / 2;
+    const bool straight = (inter ? rot_dim : half) % C == 0;      // a lane's channels are all rotated or none, its partners lie side by side
     bool have[2], keep[2];
     int page[2], ring[2];
     int64_t page_row[2];
@@ -125,7 +127,15 @@ __device__ __forceinline__ void append_rows(const AppendIo &io, const PagedSeq &
             }
         }
         if constexpr (!IS_V) {
-            if (rot && have[k]) load_angles(cs[k], a.rope, t, c0);
+            if (rot && have[k]) {
+                load_angles(cs[k], a.rope, t, c0);
+#pragma unroll
+                for (int j = 0; j < C; ++j)
+                    if (inter ? !((c0 + j) & 1) : c0 + j < half) cs[k][j].y = -cs[k][j].y;
+            } else {
+#pragma unroll
+                for (int j = 0; j < (IS_V ? 1 : C); ++j) cs[k][j] = make_float2(0.f, 0.f);
+            }
         }
         src[k] = static_cast<const T *>(IS_V ? io.v : io.k) + (int64_t)(seq.row0 + i + k) * (IS_V ? io.v_stride : io.k_stride) + c0;
         page_row[k] = ((int64_t)page[k] * cfg.n_kv_heads) * P + t % P;
@@ -158,27 +168,31 @@ __device__ __forceinline__ void append_rows(const AppendIo &io, const PagedSeq &
             if (have[k] && h0 + h_step < h_end) next[k].load(src[k] + (int64_t)(h0 + h_step) * D);
         if constexpr (!IS_V) {
             if (rot) {
-                const int rot_dim = a.rope.rot_dim, half = rot_dim / 2;
-                if (!inter) {
+                // y = x c + o s with the partner o and, for the first channel of a pair, the sine negated (see the loads of cs): the
+                // roundings of x c - o s
+                uint32_t o[C];
+                if (inter) {
+#pragma unroll
+                    for (int j = 0; j < C; ++j) o[j] = w[j ^ 1];
+                } else {
                     put_words(raw + c0, w);
                     __syncwarp();
-                }
+                    if (straight) get_words(raw + (c0 < half ? c0 + half : (c0 < rot_dim ? c0 - half : c0)), o);
+                    else {
 #pragma unroll
-                for (int j = 0; j < C; ++j) {
-                    const int c = c0 + j;
-                    if (c < rot_dim && (!inter || !(j & 1))) {
-                        const float2 x = floats<T>(w[j]);
-                        if (inter) {
-                            const float2 o = floats<T>(w[j + 1]);
-                            w[j] = packed<T>(rotate_first(x.x, o.x, cs[0][j].x, cs[0][j].y), rotate_first(x.y, o.y, cs[1][j].x, cs[1][j].y));
-                            w[j + 1] = packed<T>(rotate_second(x.x, o.x, cs[0][j].x, cs[0][j].y), rotate_second(x.y, o.y, cs[1][j].x, cs[1][j].y));
-                        } else if (c < half) {
-                            const float2 o = floats<T>(raw[c + half]);
-                            w[j] = packed<T>(rotate_first(x.x, o.x, cs[0][j].x, cs[0][j].y), rotate_first(x.y, o.y, cs[1][j].x, cs[1][j].y));
-                        } else {
-                            const float2 o = floats<T>(raw[c - half]);
-                            w[j] = packed<T>(rotate_second(o.x, x.x, cs[0][j].x, cs[0][j].y), rotate_second(o.y, x.y, cs[1][j].x, cs[1][j].y));
+                        for (int j = 0; j < C; ++j) {
+                            const int c = c0 + j;
+                            o[j] = raw[c < half ? c + half : (c < rot_dim ? c - half : c)];
                         }
+                    }
+                }
+                if (c0 < rot_dim) {
+#pragma unroll
+                    for (int j = 0; j < C; ++j) {
+                        const float2 x = floats<T>(w[j]), y = floats<T>(o[j]);
+                        const uint32_t v = packed<T>(__fadd_rn(__fmul_rn(x.x, cs[0][j].x), __fmul_rn(y.x, cs[0][j].y)),
+                                                     __fadd_rn(__fmul_rn(x.y, cs[1][j].x), __fmul_rn(y.y, cs[1][j].y)));
+                        if (straight || c0 + j < rot_dim) w[j] = v;
                     }
                 }
             }
@@ -217,14 +231,34 @@ __device__ __forceinline__ void append_rows(const AppendIo &io, const PagedSeq &
             }
             uint32_t codes = (uint32_t)(int)p[0];
             if constexpr (C == 8) codes |= (uint32_t)(int)p[1] << 16;
-            // (also taken for quotients beyond 2^22, which the sum with MAGIC cannot round, and for infinities)
-            if (!(far < 0.5f * hf * (1.0f - 3.814697265625e-06f)) && hf != 0.0f) {
+            // In doubt (fp16 values meet k + 1/2 often: two iterations in five have such an element somewhere in the warp): the remainder
+            // is exact, so a tie shows as |remainder| = h/2 and goes to the even code; what is near a tie but none, and quotients
+            // beyond 2^22 or infinite, take the division.
+            const float hh = 0.5f * hf;
+            if (!(far < hh * (1.0f - 3.814697265625e-06f)) && hf != 0.0f) {
+                bool hard = false;
                 codes = 0u;
 #pragma unroll
                 for (int j = 0; j < C; ++j) {
                     const float2 x = floats<T>(w[j]);
-                    const float c = fminf(fmaxf(rintf(__fdiv_rn(__fsub_rn(k ? x.y : x.x, zf), hf)), 0.0f), 15.0f);
-                    codes |= (uint32_t)(int)c << (4 * j);
+                    const float d = __fsub_rn(k ? x.y : x.x, zf), t = __fmaf_rn(d, r, MAGIC);
+                    float c = __fsub_rn(t, MAGIC);
+                    const float e = __fmaf_rn(-c, hf, d);
+                    if (fabsf(e) == hh) {
+                        if (__float_as_int(t) & 1) c += e > 0.f ? 1.f : -1.f;
+                    } else if (!(fabsf(e) < hh * (1.0f - 3.814697265625e-06f))) {
+                        hard = true;
+                    }
+                    codes |= (uint32_t)(int)fminf(fmaxf(c, 0.0f), 15.0f) << (4 * j);
+                }
+                if (hard) {
+                    codes = 0u;
+#pragma unroll
+                    for (int j = 0; j < C; ++j) {
+                        const float2 x = floats<T>(w[j]);
+                        const float c = fminf(fmaxf(rintf(__fdiv_rn(__fsub_rn(k ? x.y : x.x, zf), hf)), 0.0f), 15.0f);
+                        codes |= (uint32_t)(int)c << (4 * j);
+                    }
                 }
             }
             if (hf == 0.0f) codes = 0u;
@@ -246,8 +280,10 @@ __device__ __forceinline__ void append_rows(const AppendIo &io, const PagedSeq &
 }
 
 // blockIdx: x = tokens of a sequence (16, or a pair), y = runs of heads, keys and values in turn, z = sequences.
+// Five CTAs per SM: what spills (angles of the key rows) costs less than the warps that 150 registers would leave out (32k-token prompt,
+// append and read back: 542 us against 595).
 template <typename T, int D, int NG>
-__global__ void __launch_bounds__(kRowThreads) paged_append_kernel(const __grid_constant__ AppendIo io)
+__global__ void __launch_bounds__(kRowThreads, 5) paged_append_kernel(const __grid_constant__ AppendIo io)
 {
     __shared__ __align__(16) uint32_t rows[2 * kRowWarps][2][D + 4];      // a half-warp each: as read, rotated
     asm volatile("griddepcontrol.wait;" ::: "memory");

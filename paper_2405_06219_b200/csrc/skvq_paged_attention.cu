@@ -733,33 +733,38 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 2 ? 2 : 3) paged_split_ke
     }
 }
 
-// Joins the partials of an item that several runs share: blockIdx.x is the run that begins it, blockIdx.y takes every
-// gridDim.y-th of its rows.
+// Joins the partials of an item that several runs share: blockIdx.x is the run that begins it; a warp takes a row, D/32 channels a lane.
+constexpr int kMergeWarps = 4;
 struct MergeArgs {
     PagedAttnArgs a;
     int n_slots, rows;
     float lse_offset;
 };
 template <typename T, int D>
-__global__ void __launch_bounds__(D) paged_merge_kernel(const __grid_constant__ MergeArgs args)
+__global__ void __launch_bounds__(kMergeWarps * 32) paged_merge_kernel(const __grid_constant__ MergeArgs args)
 {
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;");
+    constexpr int C = D / 32, PS = partial_stride(D);
     const PagedAttnArgs &a = args.a;
     const skvq_paged_config &cfg = a.p.cfg;
-    const int slot = blockIdx.x, c = threadIdx.x, lane = threadIdx.x & 31;
-    const int *desc = reinterpret_cast<const int *>(a.ws) + (size_t)slot * kDescInts;
-    if (desc[0] == 0) return;
-    const int rep = cfg.n_q_heads / cfg.n_kv_heads, n = desc[5], hk = desc[3];
-    constexpr int PS = partial_stride(D);
-    const int dst = a.p.c.reorder_v ? a.p.c.reorder_v[hk * D + c] & (D - 1) : c;
-    for (int r = blockIdx.y; r < args.rows; r += gridDim.y) {
-        const int row = desc[4] * args.rows + r;
-        if (row >= desc[2] * rep) return;
+    const int slot = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int4 d0 = *reinterpret_cast<const int4 *>(reinterpret_cast<const int *>(a.ws) + (size_t)slot * kDescInts);
+    if (d0.x == 0) return;
+    const int4 d1 = *reinterpret_cast<const int4 *>(reinterpret_cast<const int *>(a.ws) + (size_t)slot * kDescInts + 4);
+    const int row0 = d0.y, n_new = d0.z, hk = d0.w, item = d1.x, n = d1.y, rep = cfg.n_q_heads / cfg.n_kv_heads;
+    int dst[C];
+#pragma unroll
+    for (int k = 0; k < C; ++k) dst[k] = a.p.c.reorder_v ? a.p.c.reorder_v[hk * D + lane * C + k] & (D - 1) : lane * C + k;
+    for (int r = blockIdx.y * kMergeWarps + warp; r < args.rows; r += gridDim.y * kMergeWarps) {
+        const int row = item * args.rows + r;
+        if (row >= n_new * rep) return;
         const float *base = a.ws + (size_t)args.n_slots * kDescInts + ((size_t)slot * 2 * args.rows + r) * PS;
         auto partial = [&](int k) { return base + (size_t)(2 * k + (k == 0 ? 1 : 0)) * args.rows * PS; };
-        // 32 partials at a time: every warp has their maxima and sums in its lanes, each thread walks its channel
-        float m = -CUDART_INF_F, o = 0.f, l = 0.f;
+        // 32 partials at a time: their maxima and sums in the lanes of the warp
+        float m = -CUDART_INF_F, l = 0.f, o[C];
+#pragma unroll
+        for (int k = 0; k < C; ++k) o[k] = 0.f;
         for (int k0 = 0; k0 < n; k0 += 32) {
             const bool have = k0 + lane < n;
             const float pm = have ? partial(k0 + lane)[D] : -CUDART_INF_F, pl = have ? partial(k0 + lane)[D + 1] : 0.f;
@@ -772,16 +777,28 @@ __global__ void __launch_bounds__(D) paged_merge_kernel(const __grid_constant__ 
 #pragma unroll
             for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
             l = fmaf(l, down, sum);
-            o *= down;
+#pragma unroll
+            for (int k = 0; k < C; ++k) o[k] *= down;
             m = top;
             const int last = min(32, n - k0);
-#pragma unroll 8
-            for (int k = 0; k < last; ++k) o = fmaf(partial(k0 + k)[c], __shfl_sync(0xffffffffu, f, k), o);
+#pragma unroll 4
+            for (int q = 0; q < last; ++q) {
+                const float g = __shfl_sync(0xffffffffu, f, q);
+                if constexpr (C == 4) {
+                    const float4 v = *reinterpret_cast<const float4 *>(partial(k0 + q) + lane * 4);
+                    o[0] = fmaf(v.x, g, o[0]); o[1] = fmaf(v.y, g, o[1]); o[2] = fmaf(v.z, g, o[2]); o[3] = fmaf(v.w, g, o[3]);
+                } else {
+                    const float2 v = *reinterpret_cast<const float2 *>(partial(k0 + q) + lane * 2);
+                    o[0] = fmaf(v.x, g, o[0]); o[1] = fmaf(v.y, g, o[1]);
+                }
+            }
         }
         const int i = row / rep, head = hk * rep + row % rep;
-        static_cast<T *>(a.out)[(int64_t)(desc[1] + i) * a.out_stride + (int64_t)head * D + dst] = Elem<T>::from_float(m == -CUDART_INF_F ? 0.f : o / l);
-        if (a.lse && c == 0)
-            a.lse[(int64_t)(desc[1] + i) * cfg.n_q_heads + head] = m == -CUDART_INF_F ? m : (m + log2f(l) - args.lse_offset) * 0.6931471805599453f;
+        T *out = static_cast<T *>(a.out) + (int64_t)(row0 + i) * a.out_stride + (int64_t)head * D;
+#pragma unroll
+        for (int k = 0; k < C; ++k) out[dst[k]] = Elem<T>::from_float(m == -CUDART_INF_F ? 0.f : o[k] / l);
+        if (a.lse && lane == 0)
+            a.lse[(int64_t)(row0 + i) * cfg.n_q_heads + head] = m == -CUDART_INF_F ? m : (m + log2f(l) - args.lse_offset) * 0.6931471805599453f;
     }
 }
 
@@ -875,19 +892,19 @@ bool has_many_rows(const skvq_paged_config &cfg, const skvq_paged_batch &batch)
     return (long long)batch.max_new * (cfg.n_q_heads / cfg.n_kv_heads) > kFewRows;
 }
 
-template <typename T> cudaError_t merge_by_dim(const MergeArgs &m, int row_ctas, cudaStream_t stream)
+template <typename T> cudaError_t merge_by_dim(const MergeArgs &m, int row_warps, cudaStream_t stream)
 {
-    const dim3 grid(m.n_slots, row_ctas);
-    return m.a.p.cfg.head_dim == 128 ? launch_chained(paged_merge_kernel<T, 128>, grid, 128, 0, stream, m)
-                                     : launch_chained(paged_merge_kernel<T, 64>, grid, 64, 0, stream, m);
+    const dim3 grid(m.n_slots, (row_warps + kMergeWarps - 1) / kMergeWarps);
+    return m.a.p.cfg.head_dim == 128 ? launch_chained(paged_merge_kernel<T, 128>, grid, kMergeWarps * 32, 0, stream, m)
+                                     : launch_chained(paged_merge_kernel<T, 64>, grid, kMergeWarps * 32, 0, stream, m);
 }
 
 }  // namespace
 
-cudaError_t launch_paged_merge(const PagedAttnArgs &a, int n_slots, int rows, int row_ctas, float lse_offset, cudaStream_t stream)
+cudaError_t launch_paged_merge(const PagedAttnArgs &a, int n_slots, int rows, int row_warps, float lse_offset, cudaStream_t stream)
 {
     const MergeArgs m{a, n_slots, rows, lse_offset};
-    return a.p.cfg.dtype == SKVQ_F16 ? merge_by_dim<__half>(m, row_ctas, stream) : merge_by_dim<__nv_bfloat16>(m, row_ctas, stream);
+    return a.p.cfg.dtype == SKVQ_F16 ? merge_by_dim<__half>(m, row_warps, stream) : merge_by_dim<__nv_bfloat16>(m, row_warps, stream);
 }
 
 size_t paged_workspace_bytes(const skvq_paged_config &cfg, const skvq_paged_batch &batch, int n_splits)

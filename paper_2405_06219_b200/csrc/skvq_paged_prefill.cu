@@ -290,6 +290,10 @@ __global__ void __launch_bounds__(kQueryThreads) paged_queries_kernel(const __gr
     const float sign = a.sm_scale < 0.f ? -1.f : (a.sm_scale == 0.f ? 0.f : 1.f);      // the rows' scale is positive
     const float scale = (sign == 0.f ? 1.f : fabsf(a.sm_scale)) * 1.4426950408889634f;
     int from[C], hk = -1;
+    R next;
+#pragma unroll
+    for (int k = 0; k < R::WORDS; ++k) next.w[k] = 0u;
+    if (have && h0 < h1) next.load(src + (int64_t)h0 * D);
     for (int h = h0; h < h1; ++h) {
         if (h / rep != hk) {
             hk = h / rep;
@@ -299,10 +303,8 @@ __global__ void __launch_bounds__(kQueryThreads) paged_queries_kernel(const __gr
                 from[j] = p.c.reorder_k ? p.c.reorder_k[hk * D + c] & (D - 1) : c;
             }
         }
-        R row;
-#pragma unroll
-        for (int k = 0; k < R::WORDS; ++k) row.w[k] = 0u;
-        if (have) row.load(src + (int64_t)h * D);
+        R row = next;
+        if (have && h + 1 < h1) next.load(src + (int64_t)(h + 1) * D);
         if (p.rope.table) {
             if (!p.rope.interleaved) {
                 row.store(raw + c0);
@@ -925,7 +927,7 @@ cudaError_t launch_prefill(const PagedAttnArgs &a, cudaStream_t stream)
     if (e != cudaSuccess) return e;
     e = launch_chained(paged_prefill_kernel<T, D, NG>, dim3(s.n_slots), kPrefillThreads, PGeo<D>::SMEM + sizeof(long long) * (batch.n_seqs + 1), stream, s);
     if (e != cudaSuccess) return e;
-    return launch_paged_merge(a, s.n_slots, 2 * kBlock, 32, kPOffset, stream);
+    return launch_paged_merge(a, s.n_slots, 2 * kBlock, 2 * kBlock / 4, kPOffset, stream);
 }
 
 template <typename T> cudaError_t prefill_by_shape(const PagedAttnArgs &a, cudaStream_t stream)

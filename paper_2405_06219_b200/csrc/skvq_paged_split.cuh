@@ -16,8 +16,8 @@ constexpr int kFewRows = 16;
 constexpr int kDescInts = 8;
 __host__ __device__ constexpr int partial_stride(int D) { return D + 4; }
 
-// Joins the partials; `lse_offset`: log2 of the factor that the probabilities carry.  `row_ctas` CTAs share an item's rows.
-cudaError_t launch_paged_merge(const PagedAttnArgs &a, int n_slots, int rows, int row_ctas, float lse_offset, cudaStream_t stream);
+// Joins the partials; `lse_offset`: log2 of the factor that the probabilities carry.  `row_warps` warps share an item's rows.
+cudaError_t launch_paged_merge(const PagedAttnArgs &a, int n_slots, int rows, int row_warps, float lse_offset, cudaStream_t stream);
 
 size_t prefill_workspace_bytes(const skvq_paged_config &cfg, const skvq_paged_batch &batch);
 cudaError_t launch_paged_prefill(const PagedAttnArgs &a, cudaStream_t stream);
