@@ -125,7 +125,7 @@ struct PagedSeq {
 };
 
 // What sequence b asks for; false when its entries are out of range (the caller reports and skips it).
-// `causal_only`: attention may have more rows than tokens.
+// `rows_within_len`: no more new tokens than the sequence is long (attention may have more rows).
 __device__ __forceinline__ bool paged_sequence(const PagedArgs &a, int b, bool rows_within_len, PagedSeq &q)
 {
     const skvq_paged_batch &p = a.batch;

@@ -13,9 +13,11 @@
 // the 8 columns.  A code goes in as 1024 + c (one instruction: its nibble under the bits of 1024) or, where the nibble lies four
 // bits higher, as 1024 + 16 c against q'/16; the accumulators start at minus 1024 times the sum of the operand's q', so they end at
 // sum q' c.  On the way they reach 1024 |q'| per term: of fp32's 24 bits that leaves 17 for the sum of codes, an error of h 2^-9
-// sum |q'| at the very most (16 truncated additions of 2^-23).  Values enter the transposed product (V~^T P^T) as fp16(h c)
-// (one rounding, 2^-11 at most: h times 1024 + c, minus 1024 h, in one multiply-add) and the zero points as one more row tile of
-// it, exact, so nothing is added per element; probabilities are rounded to fp16.  A probability is held times 2^14
+// sum |q'| at the very most (16 truncated additions of 2^-23).  Values enter the transposed product (V~^T P^T) as
+// fp16(h c + z): one rounding, 2^-11 of the value at most; probabilities are rounded to fp16.  (h c alone as the operand and the zero
+// points as one more row tile of the product is an instruction less per pair, but rounds h c, twice to three times the value:
+// outputs 6e-4 instead of 3e-4 off in fp16, and measured no faster, 595 and 589 us for the serving mix.)
+// A probability is held times 2^14
 // relative to the running maximum: fp16 then resolves 2^-38 of the largest, so a million small ones still add up; their
 // sum is kept in fp32.
 // Fragments: the channels of a k-step and the tokens of a row are free to choose as long as both operands agree.  A lane's
@@ -47,7 +49,7 @@ struct SplitArgs {
     PagedAttnArgs a;
     int n_slots;
     int rows;      // rows per item: 8 NT
-    int whole;     // a CTA takes a whole item: nothing to join
+    int pieces;    // > 0: a CTA takes one of so many pieces of an item; 0: an equal share of the whole step
 };
 
 template <int D, int NG, int NT>
@@ -109,19 +111,6 @@ __device__ __forceinline__ void raw_pairs(uint32_t w, uint32_t (&r)[4])      // 
     r[2] = and_or(u, 0x000F000Fu, M);
     r[3] = and_or(u, 0x00F000F0u, M);
 }
-// Is one of the four halves above `top`?
-__device__ __forceinline__ bool any_above(uint32_t a, uint32_t b, uint32_t top)
-{
-    uint32_t m;
-    asm("max.f16x2 %0, %1, %2;" : "=r"(m) : "r"(a), "r"(b));
-    return (m & 0x7FFFu) > (top & 0x7FFFu) || ((m >> 16) & 0x7FFFu) > (top >> 16);
-}
-__device__ __forceinline__ uint32_t h2_mul(uint32_t a, uint32_t b)
-{
-    uint32_t r;
-    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-    return r;
-}
 // d = a b + c with an accumulator of its own
 __device__ __forceinline__ void mma16816_from(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1, float c0,
                                               float c1, float c2, float c3)
@@ -156,14 +145,14 @@ struct SeqCost {
     int cost;                  // of one item, at least 1
     int m_tiles;               // items per KV head
 };
-__device__ __forceinline__ SeqCost seq_cost(const PagedArgs &p, const PagedSeq &s, int rows, int whole)
+__device__ __forceinline__ SeqCost seq_cost(const PagedArgs &p, const PagedSeq &s, int rows, int pieces)
 {
     SeqCost c;
     const int rep = p.cfg.n_q_heads / p.cfg.n_kv_heads;
     const int lq = max(s.len - p.cfg.window, 0);
     c.tiles_c = (lq + kTile - 1) / kTile;
     c.tiles_r = (s.len - lq + kRingTile - 1) / kRingTile;
-    c.cost = whole ? 1 : max(c.tiles_c + kRingCost * c.tiles_r, 1);
+    c.cost = pieces ? pieces : max(c.tiles_c + kRingCost * c.tiles_r, 1);
     c.m_tiles = s.n * rep <= kFewRows ? (s.n * rep + rows - 1) / rows : 0;      // the others are the tcgen05 kernel's
     return c;
 }
@@ -198,7 +187,7 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 2 ? 2 : 3) paged_split_ke
             if (b < B) {
                 PagedSeq s;
                 if (paged_sequence(p, b, false, s)) {
-                    const SeqCost sc = seq_cost(p, s, ROWS, args.whole);
+                    const SeqCost sc = seq_cost(p, s, ROWS, args.pieces);
                     c = (long long)sc.cost * sc.m_tiles * cfg.n_kv_heads;
                 } else if (blockIdx.x == 0) {
                     set_status(p.c.status, SKVQ_STATUS_BAD_BATCH);
@@ -227,7 +216,7 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 2 ? 2 : 3) paged_split_ke
     long long f = blockIdx.x * ups;
     const long long f1 = min(f + ups, total);
     int *desc = reinterpret_cast<int *>(a.ws) + (size_t)blockIdx.x * kDescInts;
-    if (tid == 0 && !args.whole) desc[0] = 0;
+    if (tid == 0 && args.pieces != 1) desc[0] = 0;
     if (f >= f1) return;
     int b;
     {
@@ -244,7 +233,7 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 2 ? 2 : 3) paged_split_ke
         while (pre[b + 1] <= f) ++b;
         PagedSeq seq;
         paged_sequence(p, b, false, seq);
-        const SeqCost sc = seq_cost(p, seq, ROWS, args.whole);
+        const SeqCost sc = seq_cost(p, seq, ROWS, args.pieces);
         const long long item = (f - pre[b]) / sc.cost;
         const int off = (int)((f - pre[b]) - item * sc.cost);
         const int take = (int)min((long long)(sc.cost - off), f1 - f);
@@ -260,7 +249,8 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 2 ? 2 : 3) paged_split_ke
 
         // ---- this warp's quarter of the run; its first pages are on their way while the queries are prepared
         auto tile_of = [&](int x) { return x <= sc.tiles_c ? x : sc.tiles_c + (x - sc.tiles_c + kRingCost - 1) / kRingCost; };
-        const int seg0 = tile_of(off), seg1 = args.whole ? sc.tiles_c + sc.tiles_r : tile_of(off + take);
+        const int full = sc.tiles_c + kRingCost * sc.tiles_r;
+        const int seg0 = tile_of(args.pieces ? full * off / args.pieces : off), seg1 = tile_of(args.pieces ? full * (off + take) / args.pieces : off + take);
         const int c0 = min(seg0, sc.tiles_c), c1 = max(min(min(seg1, sc.tiles_c), (limit_hi + kTile - 1) / kTile), c0);
         const int q0 = c0 + (int)((long long)(c1 - c0) * warp / kSplitWarps), q1 = c0 + (int)((long long)(c1 - c0) * (warp + 1) / kSplitWarps);
         const int P = cfg.page_tokens, page_shift = __ffs(P) - 1;
@@ -412,7 +402,6 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 2 ? 2 : 3) paged_split_ke
         }
 
         float o[NT][Geo::MT][4];      // [.][channel pair][{first, second channel} x {row 2j, row 2j + 1}]
-        float oz[NT][4];              // sum of p z of the lane's channels (their group): rows 2j, 2j + 1; [2], [3] unused
         float m_run[NT][2], l_run[NT][2];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
@@ -420,8 +409,6 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 2 ? 2 : 3) paged_split_ke
             for (int m = 0; m < Geo::MT; ++m)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) o[n][m][e] = 0.f;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) oz[n][e] = 0.f;
 #pragma unroll
             for (int e = 0; e < 2; ++e) { m_run[n][e] = -CUDART_INF_F; l_run[n][e] = 0.f; }
         }
@@ -451,8 +438,6 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 2 ? 2 : 3) paged_split_ke
                     }
 #pragma unroll
                     for (int m = 0; m < Geo::MT; ++m) { o[n][m][0] *= down[0]; o[n][m][1] *= down[1]; o[n][m][2] *= down[0]; o[n][m][3] *= down[1]; }
-                    oz[n][0] *= down[0];
-                    oz[n][1] *= down[1];
                 }
 #pragma unroll
                 for (int e = 0; e < 2; ++e) base[e] = kPScaleLog2 - (m_run[n][e] == -CUDART_INF_F ? 0.f : m_run[n][e] * rs[n][e]);
@@ -561,15 +546,6 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 2 ? 2 : 3) paged_split_ke
                     }
                 }
 #pragma unroll
-                for (int n = 0; n < NT; ++n) mma16816(oz[n], z_a, 0u, z_b, 0u, pb[u][n][0], pb[u][n][1]);
-                // h c = h (1024 + c) - 1024 h, or h/16 (1024 + 16 c) - 64 h: one rounding, unless h is so large that 1024 h is not an
-                // fp16 number; then the code is formed first
-                constexpr uint32_t TOP = 0x53C053C0u;      // 62: h below it in both halves of both
-                const bool large = __any_sync(0xffffffffu, any_above(h_a, h_b, TOP));
-                const uint32_t hs_a = h2_mul(h_a, 0x2C002C00u), hs_b = h2_mul(h_b, 0x2C002C00u);      // h / 16
-                const uint32_t n_a = h2_mul(h_a, 0xE400E400u), n_b = h2_mul(h_b, 0xE400E400u);          // -1024 h
-                const uint32_t ns_a = h2_mul(h_a, 0xD400D400u), ns_b = h2_mul(h_b, 0xD400D400u);        // -64 h
-#pragma unroll
                 for (int q = 0; q < D / 64; ++q) {
 #pragma unroll
                     for (int hf = 0; hf < 2; ++hf) {
@@ -577,18 +553,10 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 2 ? 2 : 3) paged_split_ke
                         uint32_t x[4], y[4];      // channels 4 hf .. 4 hf + 3 of the word, pairs (token, token + 4)
                         raw_pairs(__byte_perm(w[0][q], w[1][q], sel), x);
                         raw_pairs(__byte_perm(w[2][q], w[3][q], sel), y);
-                        if (!large) {
 #pragma unroll
-                            for (int k = 0; k < 4; ++k) {
-                                x[k] = h2_fma(x[k], k & 1 ? hs_a : h_a, k & 1 ? ns_a : n_a);
-                                y[k] = h2_fma(y[k], k & 1 ? hs_b : h_b, k & 1 ? ns_b : n_b);
-                            }
-                        } else {
-#pragma unroll
-                            for (int k = 0; k < 4; ++k) {
-                                x[k] = h2_mul(k & 1 ? h2_fma(x[k], 0x2C002C00u, 0xD400D400u) : h2_sub(x[k], 0x64006400u), h_a);
-                                y[k] = h2_mul(k & 1 ? h2_fma(y[k], 0x2C002C00u, 0xD400D400u) : h2_sub(y[k], 0x64006400u), h_b);
-                            }
+                        for (int k = 0; k < 4; ++k) {      // 1024 + c - 1024, (1024 + 16 c) / 16 - 64: the code, exact
+                            x[k] = h2_fma(k & 1 ? h2_fma(x[k], 0x2C002C00u, 0xD400D400u) : h2_sub(x[k], 0x64006400u), h_a, z_a);
+                            y[k] = h2_fma(k & 1 ? h2_fma(y[k], 0x2C002C00u, 0xD400D400u) : h2_sub(y[k], 0x64006400u), h_b, z_b);
                         }
 #pragma unroll
                         for (int k = 0; k < 2; ++k)
@@ -691,7 +659,7 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 2 ? 2 : 3) paged_split_ke
                 if (r < R) {
                     float *row = join + (warp * ROWS + r) * Geo::JROW + g;
 #pragma unroll
-                    for (int m = 0; m < Geo::MT; ++m) { row[16 * m] = o[n][m][e] + oz[n][e]; row[16 * m + 8] = o[n][m][2 + e] + oz[n][e]; }
+                    for (int m = 0; m < Geo::MT; ++m) { row[16 * m] = o[n][m][e]; row[16 * m + 8] = o[n][m][2 + e]; }
                 }
             }
         }
@@ -830,40 +798,38 @@ long long item_count(const skvq_paged_config &cfg, const skvq_paged_batch &batch
     const int per = item_rows(cfg, batch);
     return (long long)batch.n_seqs * cfg.n_kv_heads * ((few_rows(cfg, batch) + per - 1) / per);
 }
-bool whole_items(const skvq_paged_config &cfg, const skvq_paged_batch &batch, int n_splits)
+// How a step is cut: pieces of items (1: whole ones, nothing to join), or, pieces = 0, equal shares of everything.
+struct SplitShape {
+    int pieces, slots;
+};
+SplitShape split_plan(const skvq_paged_config &cfg, const skvq_paged_batch &batch, int n_splits)
 {
-    return n_splits == 0 && item_cost(cfg, batch) <= kWholeCost && item_count(cfg, batch) <= kMaxSlots;
-}
-
-int split_slots(const skvq_paged_config &cfg, const skvq_paged_batch &batch, int n_splits)
-{
-    const int per = item_rows(cfg, batch);
     const long long items = item_count(cfg, batch), cost = item_cost(cfg, batch);
-    if (whole_items(cfg, batch, n_splits)) return (int)items;
-    long long slots;
-    if (n_splits > 0) slots = (long long)n_splits * items;
-    else {
-        // one wave of resident CTAs (a CTA more per SM spills: serving mix 597 us against 580), each with two tiles per warp at least: a
-        // shorter run costs more to join than it saves
-        slots = (per == 8 ? 3LL : 2LL) * sm_count();
-        if (slots > items * cost / 8) slots = items * cost / 8;
-    }
+    if (n_splits == 0 && cost <= kWholeCost && items <= kMaxSlots) return {1, (int)items};
+    // one wave of resident CTAs (a CTA more per SM spills: serving mix 597 us against 580), each with two tiles per warp at least: a shorter run
+    // costs more to join than it saves
+    const long long wave = (item_rows(cfg, batch) == 8 ? 3LL : 2LL) * sm_count();
+    long long slots = n_splits > 0 ? n_splits * items : (wave < items * cost / 8 ? wave : items * cost / 8);
     if (slots > items * cost) slots = items * cost;
     if (slots > kMaxSlots) slots = kMaxSlots;
-    return slots < 1 ? 1 : (int)slots;
+    if (slots < 1) slots = 1;
+    // Few items and little work: equal pieces of every item.  A share that ends one item and begins the next prepares two sets of
+    // queries and joins twice, which such short shares do not hide (one query over 4096 tokens, 32 heads: 21.8 us in equal shares, 17.9 so).
+    if (n_splits == 0 && items * 2 <= slots && items * cost <= slots * 32) return {(int)(slots / items), (int)(slots / items * items)};
+    return {0, (int)slots};
 }
 
 template <typename T, int D, int NG, int NT>
 cudaError_t launch_split(const PagedAttnArgs &a, cudaStream_t stream)
 {
     using Geo = Geometry<D, NG, NT>;
-    const bool whole = whole_items(a.p.cfg, a.p.batch, a.n_splits);
-    const SplitArgs s{a, split_slots(a.p.cfg, a.p.batch, a.n_splits), Geo::ROWS, whole};
+    const SplitShape shape = split_plan(a.p.cfg, a.p.batch, a.n_splits);
+    const SplitArgs s{a, shape.slots, Geo::ROWS, shape.pieces};
     static unsigned long long done = 0;
     cudaError_t e = configure_smem_once(paged_split_kernel<T, D, NG, NT>, Geo::SMEM + (int)sizeof(long long) * (kMaxPagedSeqs + 1), done);
     if (e != cudaSuccess) return e;
     e = launch_chained(paged_split_kernel<T, D, NG, NT>, dim3(s.n_slots), kSplitThreads, Geo::SMEM + sizeof(long long) * (a.p.batch.n_seqs + 1), stream, s);
-    if (e != cudaSuccess || whole) return e;
+    if (e != cudaSuccess || shape.pieces == 1) return e;
     return launch_paged_merge(a, s.n_slots, Geo::ROWS, (int)few_rows(a.p.cfg, a.p.batch), kPScaleLog2, stream);
 }
 
@@ -882,8 +848,9 @@ template <typename T> cudaError_t launch_by_shape(const PagedAttnArgs &a, cudaSt
 
 size_t split_workspace_bytes(const skvq_paged_config &cfg, const skvq_paged_batch &batch, int n_splits)
 {
-    if (whole_items(cfg, batch, n_splits)) return 0;
-    const size_t slots = split_slots(cfg, batch, n_splits);
+    const SplitShape shape = split_plan(cfg, batch, n_splits);
+    if (shape.pieces == 1) return 0;
+    const size_t slots = shape.slots;
     return (slots * kDescInts * 4 + slots * 2 * item_rows(cfg, batch) * partial_stride(cfg.head_dim) * 4 + 15) / 16 * 16;
 }
 

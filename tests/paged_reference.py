@@ -104,31 +104,17 @@ class Reference:
                 out[t] = (mag * (self.D * 2.0 ** -23 + 2.0 ** -11) + h * (16 * 1024 * 2.0 ** -23)).flatten(-2)
         return out
 
-    def value_parts(self, b):
-        """float64 [L, H, D]: h code, the part of a value that is rounded to fp16 before the product (the value itself in the
-        window, where nothing is rounded beyond the type)."""
-        L = len(self.rows[b])
-        out = torch.zeros(L, self.H, self.D, dtype=torch.float64)
-        for t, row in enumerate(self.rows[b]):
-            if t >= L - self.W:
-                out[t] = row[1].double().abs()
-            else:
-                out[t] = (row[4].double().unflatten(-1, (-1, self.G)) * row[5].double()[..., :1]).flatten(-2)
-        return out
-
     def attention(self, b, q, sm_scale, causal=True, length=None):
         """q [n, Hq, D] -> (out float64 [n, Hq, D] in source order, lse [n, Hq], allowed error [n, Hq, D], of lse [n, Hq]).
 
-        The error bound counts: the scores' (score_error), probabilities rounded to fp16 (2^-11 of the value each), h code rounded to
-        fp16 (2^-11 of it; the zero point is added exactly, so the rounding is relative to h code and not to the value), fp32 sums
-        of L probabilities with truncating adders, ex2 to 2^-22."""
+        The error bound counts: the scores' (score_error), probabilities and values rounded to fp16 (2^-11 each), fp32 sums of L
+        probabilities with truncating adders, ex2 to 2^-22."""
         n, L = q.shape[0], len(self.rows[b])
         if self.rot_dim and n:
             pos = torch.arange(L - n, L)
             turned = rotate32(q, self.table[pos.clamp(min=0)], self.rot_dim, self.interleaved)
             q = torch.where((pos >= 0)[:, None, None], turned, q)
         K, V, off = self.values(b, "k"), self.values(b, "v"), self.score_error(b)
-        hc = self.value_parts(b)
         out = torch.zeros(n, self.Hq, self.D, dtype=torch.float64)
         lse = torch.full((n, self.Hq), -math.inf, dtype=torch.float64)
         err, err_lse = torch.zeros_like(out), torch.zeros(n, self.Hq, dtype=torch.float64)
@@ -147,12 +133,12 @@ class Reference:
                 l = p.sum()
                 p = p / l
                 o = p @ V[:lim, h]
-                a, a_hc = p @ V[:lim, h].abs(), p @ hc[:lim, h]
+                a = p @ V[:lim, h].abs()
                 ds = abs(sm_scale) * float((off[:lim, h] @ qr.abs()).max())
                 # a probability far below the largest is held to 2^-39 of it (fp16 steps of 2^-24 under a factor 2^14, half of one)
                 floor = float((V[:lim, h].abs().sum(0) / l).max()) * 2.0 ** -39
                 out[i, hq, self.rv[h]] = o
-                err[i, hq, self.rv[h]] = a * (2.0 ** -11 + 2 * ds + 2.0 ** -21 + lim * 2.0 ** -23) + a_hc * (2.0 ** -11 + lim * 2.0 ** -23) + o.abs() * half_step * 1.01 + floor + 1e-7
+                err[i, hq, self.rv[h]] = a * (2.0 ** -10 + 2 * ds + 2.0 ** -21 + lim * 2.0 ** -23) + o.abs() * half_step * 1.01 + floor + 1e-7
                 lse[i, hq] = m + torch.log(l)
                 err_lse[i, hq] = ds + 2.0 ** -21 + lim * 2.0 ** -23 + abs(float(lse[i, hq])) * 2.0 ** -22
         return out, lse, err, err_lse
