@@ -767,107 +767,107 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
                 const int seen_tile = min(lim, quantized ? s.it.lq : s.seq.len) - tok0;      // tokens of the tile below it are seen
 #pragma unroll 1
                 for (int hf = 0; hf < 2; ++hf) {
-                const uint32_t h_addr = s_addr + hf * 64;
-                const int seen = seen_tile - hf * 64;
-                const bool first = t == s.t0 && hf == 0;
-                wait(s_full + 16 * blk + 8 * hf, ns & 1);
-                tc_fence_after();
-                float x[32], y[32];
-                tmem_ld32(h_addr, x);
-                tmem_ld32(h_addr + 32, y);
-                const uint32_t bad = quantized ? (bad_sh[n & 3] >> (16 * hf)) & 0x303u : 0u;      // two bits in each byte
-                const bool edge = __any_sync(0xffffffffu, seen < 64 || bad != 0u);
-                tmem_wait_ld32(x);
-                tmem_wait_ld32(y);
-                if (edge) {
-                    // hidden columns become -infinity in place; the code below then is the same for all tiles
-#pragma unroll 1
-                    for (int run = 0; run < 2; ++run) {
-                        const int left = seen - 32 * run;      // which of its 32 columns the row sees, one bit each
-                        uint32_t v = left >= 32 ? 0xFFFFFFFFu : (left <= 0 ? 0u : (1u << left) - 1u);
-                        const uint32_t two = (bad >> (8 * run)) & 3u;
-                        if (two & 1u) v &= 0xFFFF0000u;
-                        if (two & 2u) v &= 0x0000FFFFu;
-                        tmem_ld32(h_addr + 32 * run, x);
-                        tmem_wait_ld32(x);
-                        uint32_t w[32];
-#pragma unroll
-                        for (int c = 0; c < 32; ++c) w[c] = (v >> c) & 1u ? __float_as_uint(x[c]) : 0xFF800000u;
-                        tmem_st32(h_addr + 32 * run, w);
-                    }
-                    tmem_wait_st();
+                    const uint32_t h_addr = s_addr + hf * 64;
+                    const int seen = seen_tile - hf * 64;
+                    const bool first = t == s.t0 && hf == 0;
+                    wait(s_full + 16 * blk + 8 * hf, ns & 1);
+                    tc_fence_after();
+                    float x[32], y[32];
                     tmem_ld32(h_addr, x);
                     tmem_ld32(h_addr + 32, y);
+                    const uint32_t bad = quantized ? (bad_sh[n & 3] >> (16 * hf)) & 0x303u : 0u;      // two bits in each byte
+                    const bool edge = __any_sync(0xffffffffu, seen < 64 || bad != 0u);
                     tmem_wait_ld32(x);
                     tmem_wait_ld32(y);
-                }
-                float mx;
-                {
-                    float m0 = fmaxf(x[0], y[0]), m1 = fmaxf(x[1], y[1]), m2 = fmaxf(x[2], y[2]), m3 = fmaxf(x[3], y[3]);
+                    if (edge) {
+                        // hidden columns become -infinity in place; the code below then is the same for all tiles
+#pragma unroll 1
+                        for (int run = 0; run < 2; ++run) {
+                            const int left = seen - 32 * run;      // which of its 32 columns the row sees, one bit each
+                            uint32_t v = left >= 32 ? 0xFFFFFFFFu : (left <= 0 ? 0u : (1u << left) - 1u);
+                            const uint32_t two = (bad >> (8 * run)) & 3u;
+                            if (two & 1u) v &= 0xFFFF0000u;
+                            if (two & 2u) v &= 0x0000FFFFu;
+                            tmem_ld32(h_addr + 32 * run, x);
+                            tmem_wait_ld32(x);
+                            uint32_t w[32];
 #pragma unroll
-                    for (int c = 4; c < 32; c += 4) {
-                        m0 = fmaxf(fmaxf(m0, x[c]), y[c]);
-                        m1 = fmaxf(fmaxf(m1, x[c + 1]), y[c + 1]);
-                        m2 = fmaxf(fmaxf(m2, x[c + 2]), y[c + 2]);
-                        m3 = fmaxf(fmaxf(m3, x[c + 3]), y[c + 3]);
+                            for (int c = 0; c < 32; ++c) w[c] = (v >> c) & 1u ? __float_as_uint(x[c]) : 0xFF800000u;
+                            tmem_st32(h_addr + 32 * run, w);
+                        }
+                        tmem_wait_st();
+                        tmem_ld32(h_addr, x);
+                        tmem_ld32(h_addr + 32, y);
+                        tmem_wait_ld32(x);
+                        tmem_wait_ld32(y);
                     }
-                    mx = fmaxf(fmaxf(m0, m1), fmaxf(m2, m3));
-                }
-                // ---- raise the reference: at first, then only when a score exceeds it by 2^kLazy
-                float down = 1.f;
-                const bool raise = !first && __any_sync(0xffffffffu, (mx - ref) * rs > kLazy);
-                if (first) ref = mx;
-                else if (raise && mx > ref) {
-                    down = ref == -CUDART_INF_F ? 0.f : ex2_approx((ref - mx) * rs);
-                    ref = mx;
-                    l *= down;
-                }
-                const float base = kPOffset - (ref == -CUDART_INF_F ? 0.f : ref * rs);
-                const uint64_t rs2 = pair(rs, rs), base2 = pair(base, base);
-                uint64_t l0 = 0ull, l1 = 0ull;      // pairs of sums
-                // Of every eight exponentials the last kPolynomial are computed with multiply-adds: the special-function unit, at 16 a
-                // clock for the SM, would alone take as long as the tensor core.
-                auto probabilities = [&](float (&v)[32], int run) {
-                    uint32_t w[16];
+                    float mx;
+                    {
+                        float m0 = fmaxf(x[0], y[0]), m1 = fmaxf(x[1], y[1]), m2 = fmaxf(x[2], y[2]), m3 = fmaxf(x[3], y[3]);
 #pragma unroll
-                    for (int c = 0; c < 32; c += 8) {
+                        for (int c = 4; c < 32; c += 4) {
+                            m0 = fmaxf(fmaxf(m0, x[c]), y[c]);
+                            m1 = fmaxf(fmaxf(m1, x[c + 1]), y[c + 1]);
+                            m2 = fmaxf(fmaxf(m2, x[c + 2]), y[c + 2]);
+                            m3 = fmaxf(fmaxf(m3, x[c + 3]), y[c + 3]);
+                        }
+                        mx = fmaxf(fmaxf(m0, m1), fmaxf(m2, m3));
+                    }
+                    // ---- raise the reference: at first, then only when a score exceeds it by 2^kLazy
+                    float down = 1.f;
+                    const bool raise = !first && __any_sync(0xffffffffu, (mx - ref) * rs > kLazy);
+                    if (first) ref = mx;
+                    else if (raise && mx > ref) {
+                        down = ref == -CUDART_INF_F ? 0.f : ex2_approx((ref - mx) * rs);
+                        ref = mx;
+                        l *= down;
+                    }
+                    const float base = kPOffset - (ref == -CUDART_INF_F ? 0.f : ref * rs);
+                    const uint64_t rs2 = pair(rs, rs), base2 = pair(base, base);
+                    uint64_t l0 = 0ull, l1 = 0ull;      // pairs of sums
+                    // Of every eight exponentials the last kPolynomial are computed with multiply-adds: the special-function unit, at 16 a
+                    // clock for the SM, would alone take as long as the tensor core.
+                    auto probabilities = [&](float (&v)[32], int run) {
+                        uint32_t w[16];
 #pragma unroll
-                        for (int k = c; k < c + 8; k += 2) {
-                            unpair(pair_fma(pair(v[k], v[k + 1]), rs2, base2), v[k], v[k + 1]);
-                            if (k % 8 < 8 - kPolynomial) { v[k] = ex2_approx(v[k]); v[k + 1] = ex2_approx(v[k + 1]); }
-                            else exp2_pair(v[k], v[k + 1]);
-                            if (k & 2) l1 = pair_add(l1, pair(v[k], v[k + 1]));
-                            else l0 = pair_add(l0, pair(v[k], v[k + 1]));
-                            w[k / 2] = h2(v[k], v[k + 1]);
+                        for (int c = 0; c < 32; c += 8) {
+#pragma unroll
+                            for (int k = c; k < c + 8; k += 2) {
+                                unpair(pair_fma(pair(v[k], v[k + 1]), rs2, base2), v[k], v[k + 1]);
+                                if (k % 8 < 8 - kPolynomial) { v[k] = ex2_approx(v[k]); v[k + 1] = ex2_approx(v[k + 1]); }
+                                else exp2_pair(v[k], v[k + 1]);
+                                if (k & 2) l1 = pair_add(l1, pair(v[k], v[k + 1]));
+                                else l0 = pair_add(l0, pair(v[k], v[k + 1]));
+                                w[k / 2] = h2(v[k], v[k + 1]);
+                            }
+                        }
+                        tmem_st16(h_addr + run * 16, w);      // over scores that are in registers
+                    };
+                    probabilities(x, 0);
+                    probabilities(y, 1);
+                    {
+                        float a0, a1;
+                        unpair(pair_add(l0, l1), a0, a1);
+                        l += a0 + a1;
+                    }
+                    if (raise) {      // O follows the reference, once the products of the half before have landed in it
+                        if (hf) wait(pv_done + 16 * blk, ns & 1);
+                        else wait(pv_done + 16 * blk + 8, (ns - 1) & 1);
+                        tc_fence_after();
+#pragma unroll 1
+                        for (int c0 = 0; c0 < D; c0 += 32) {
+                            tmem_ld32(o_addr + c0, x);
+                            tmem_wait_ld32(x);
+                            uint32_t w[32];
+#pragma unroll
+                            for (int c = 0; c < 32; ++c) w[c] = __float_as_uint(x[c] * down);
+                            tmem_st32(o_addr + c0, w);
                         }
                     }
-                    tmem_st16(h_addr + run * 16, w);      // over scores that are in registers
-                };
-                probabilities(x, 0);
-                probabilities(y, 1);
-                {
-                    float a0, a1;
-                    unpair(pair_add(l0, l1), a0, a1);
-                    l += a0 + a1;
-                }
-                if (raise) {      // O follows the reference, once the products of the half before have landed in it
-                    if (hf) wait(pv_done + 16 * blk, ns & 1);
-                    else wait(pv_done + 16 * blk + 8, (ns - 1) & 1);
-                    tc_fence_after();
-#pragma unroll 1
-                    for (int c0 = 0; c0 < D; c0 += 32) {
-                        tmem_ld32(o_addr + c0, x);
-                        tmem_wait_ld32(x);
-                        uint32_t w[32];
-#pragma unroll
-                        for (int c = 0; c < 32; ++c) w[c] = __float_as_uint(x[c] * down);
-                        tmem_st32(o_addr + c0, w);
-                    }
-                }
-                tmem_wait_st();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(p_full + 16 * blk + 8 * hf);
+                    tmem_wait_st();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(p_full + 16 * blk + 8 * hf);
                 }
                 ++ns;
             }
