@@ -416,26 +416,32 @@ int skvq_paged_read(const skvq_paged_config *cfg, const skvq_paged_cache *cache,
 typedef struct skvq_paged_attn_args {
     float sm_scale;       /* softmax scale, e.g. 1/sqrt(D) */
     int32_t causal;       /* 1: row i of a sequence sees tokens 0 .. L_b - n_b + i; 0: all L_b tokens */
-    int32_t n_splits;     /* 0: the library chooses; n > 0: about n pieces of the context per (sequence, KV head) */
+    int32_t n_splits;     /* 0: the library chooses; n > 0: about n pieces of the context per (sequence, KV head), for sequences with
+                             at most 16 rows (new tokens * Hq/Hkv) per KV head */
     void *workspace;      /* device scratch of at least skvq_paged_workspace_size() bytes; may be NULL when that is 0 */
     size_t workspace_bytes;
 } skvq_paged_attn_args;
 
 /* Scratch bytes that skvq_paged_attention needs (depends on the host bounds in `batch`, not on the device arrays, and on the
- * GPU's SM count).  0 also on bad arguments.  Host only. */
+ * GPU's SM count): partial results of (sequence, KV head) pairs that several CTAs share, and, where max_new * Hq/Hkv exceeds 16, the
+ * rotated queries, T * Hq * (2 D + 4) bytes.  0 also on bad arguments.  Host only. */
 size_t skvq_paged_workspace_size(const skvq_paged_config *cfg, const skvq_paged_batch *batch, int32_t n_splits);
 
 /*
  * Attention of the new tokens' queries over the cache (append first: the cache then holds them):
  *   q' = rope(q) rounded to dtype (rope != NULL),  s_t = sm_scale sum_j q'_j K~[t][j],  p = softmax over the tokens the row sees,
  *   out_j = sum_t p_t V~[t][j]
- * K~, V~ as skvq_paged_read(window = 1) defines them, unrounded.  Scores, softmax statistics and sums are fp32.
+ * K~, V~ as skvq_paged_read(window = 1) defines them, before its rounding to dtype; as operands of the tensor core they are rounded to
+ * fp16 once (with at most 16 rows, n_b * Hq/Hkv, per KV head only V~ is), and so are the probabilities.  Scores, softmax statistics
+ * and sums are fp32.
  * A row that sees no token (n_b > L_b, or L_b = 0) gives zeros and a log-sum-exp of -infinity.
  *   q, out           dtype [T][Hq][D], token strides in elements (multiples of 8, >= Hq*D)
  *   lse              float [T][Hq], natural logarithm of the softmax denominator of every row, or NULL
  * Skipped sequences (as for skvq_paged_append, except that n_b may exceed L_b): their rows are left alone.  Tokens behind a bad
  * page-table entry are left out of the softmax and SKVQ_STATUS_BAD_PAGE is set.  Rows of the cache at or beyond L_b are never
- * used, whatever they hold.  The workspace is overwritten; calls sharing one must be stream-ordered.
+ * used, whatever they hold.  A query that is not finite gives its own row NaN and no other.  Keys and values have to be finite and
+ * in fp16's range (as for skvq_paged_append): one that is not can reach every row of its sequence, those that do not see it too.
+ * The workspace is overwritten; calls sharing one must be stream-ordered.  out and lse must not overlap the inputs.
  */
 int skvq_paged_attention(const skvq_paged_config *cfg, const skvq_paged_cache *cache, const skvq_paged_batch *batch,
                          const skvq_rope *rope, const void *q, int64_t q_stride, void *out, int64_t out_stride, void *lse,

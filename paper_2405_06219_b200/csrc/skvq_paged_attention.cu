@@ -673,19 +673,18 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 2 ? 2 : 3) paged_split_ke
             float M = -CUDART_INF_F, l = 0.f, v = 0.f;
 #pragma unroll
             for (int w = 0; w < kSplitWarps; ++w) M = fmaxf(M, ml_sh[w][r][0]);
-            if (M != -CUDART_INF_F) {
+            const float from = M == -CUDART_INF_F ? 0.f : M;      // nothing seen: sums of zero; a query that is not a number: sums that are none
 #pragma unroll
-                for (int w = 0; w < kSplitWarps; ++w) {
-                    const float k = ex2_approx(ml_sh[w][r][0] - M);
-                    l = fmaf(ml_sh[w][r][1], k, l);
-                    v = fmaf(join[(w * ROWS + r) * Geo::JROW + (c % Geo::CPT) * 8 + c / Geo::CPT], k, v);
-                }
+            for (int w = 0; w < kSplitWarps; ++w) {
+                const float k = ex2_approx(ml_sh[w][r][0] - from);
+                l = fmaf(ml_sh[w][r][1], k, l);
+                v = fmaf(join[(w * ROWS + r) * Geo::JROW + (c % Geo::CPT) * 8 + c / Geo::CPT], k, v);
             }
             if (whole) {
                 const int i = (row_base + r) / rep, head = hk * rep + (row_base + r) % rep;
-                static_cast<T *>(a.out)[(int64_t)(seq.row0 + i) * a.out_stride + head * D + dst] = Elem<T>::from_float(M == -CUDART_INF_F ? 0.f : v / l);
+                static_cast<T *>(a.out)[(int64_t)(seq.row0 + i) * a.out_stride + head * D + dst] = Elem<T>::from_float(l == 0.f ? 0.f : v / l);
                 if (a.lse && c == 0)
-                    a.lse[(int64_t)(seq.row0 + i) * cfg.n_q_heads + head] = M == -CUDART_INF_F ? M : (M + log2f(l) - kPScaleLog2) * 0.6931471805599453f;
+                    a.lse[(int64_t)(seq.row0 + i) * cfg.n_q_heads + head] = l == 0.f ? -CUDART_INF_F : (M + log2f(l) - kPScaleLog2) * 0.6931471805599453f;
             } else {
                 part[r * partial_stride(D) + c] = v;
                 if (c == 0) { part[r * partial_stride(D) + D] = M; part[r * partial_stride(D) + D + 1] = l; }
@@ -739,8 +738,8 @@ __global__ void __launch_bounds__(kMergeWarps * 32) paged_merge_kernel(const __g
             float top = fmaxf(pm, m);
 #pragma unroll
             for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-            if (top == -CUDART_INF_F) continue;
-            const float down = ex2_approx(m - top), f = ex2_approx(pm - top);
+            const float from = top == -CUDART_INF_F ? 0.f : top;
+            const float down = ex2_approx(m - from), f = ex2_approx(pm - from);
             float sum = pl * f;
 #pragma unroll
             for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
@@ -764,9 +763,9 @@ __global__ void __launch_bounds__(kMergeWarps * 32) paged_merge_kernel(const __g
         const int i = row / rep, head = hk * rep + row % rep;
         T *out = static_cast<T *>(a.out) + (int64_t)(row0 + i) * a.out_stride + (int64_t)head * D;
 #pragma unroll
-        for (int k = 0; k < C; ++k) out[dst[k]] = Elem<T>::from_float(m == -CUDART_INF_F ? 0.f : o[k] / l);
+        for (int k = 0; k < C; ++k) out[dst[k]] = Elem<T>::from_float(l == 0.f ? 0.f : o[k] / l);
         if (a.lse && lane == 0)
-            a.lse[(int64_t)(row0 + i) * cfg.n_q_heads + head] = m == -CUDART_INF_F ? m : (m + log2f(l) - args.lse_offset) * 0.6931471805599453f;
+            a.lse[(int64_t)(row0 + i) * cfg.n_q_heads + head] = l == 0.f ? -CUDART_INF_F : (m + log2f(l) - args.lse_offset) * 0.6931471805599453f;
     }
 }
 

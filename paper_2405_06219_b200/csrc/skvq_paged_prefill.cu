@@ -378,8 +378,9 @@ __device__ __noinline__ void write_rows(const PagedAttnArgs &args, const PSegmen
     const int n_q_heads = args.p.cfg.n_q_heads;
     const int rep = s.it.rep, hk = s.hk, row0 = s.seq.row0;
     const int i = (row_base + row) / rep, head = hk * rep + (row_base + row) - i * rep;
+    const bool none = !work || (ref == -CUDART_INF_F && l == l);      // no token seen; a query that is not a number leaves its mark in l
     if (whole) {
-        const float inv = ref == -CUDART_INF_F ? 0.f : 1.f / l;
+        const float inv = 1.f / l;
         T *rows_out = reinterpret_cast<T *>(q_tile);      // [128][D], 16-byte pieces of a row at piece ^ (row & 7); all products have been read
 #pragma unroll 1
         for (int c0 = 0; c0 < D; c0 += 16) {
@@ -391,16 +392,16 @@ __device__ __noinline__ void write_rows(const PagedAttnArgs &args, const PSegmen
 #pragma unroll
             for (int c = 0; c < 16; ++c) {
                 const int dst = work ? out_channel[c0 + c] : c0 + c;
-                rows_out[row * D + ((((dst >> 3) ^ (row & 7))) << 3) + (dst & 7)] = Elem<T>::from_float(work && ref != -CUDART_INF_F ? x[c] * inv : 0.f);
+                rows_out[row * D + ((((dst >> 3) ^ (row & 7))) << 3) + (dst & 7)] = Elem<T>::from_float(none ? 0.f : x[c] * inv);
             }
         }
-        if (lse && row < rows )
-            lse[(int64_t)(row0 + i) * n_q_heads + head] = ref == -CUDART_INF_F ? ref : (ref * rs + log2f(l) - kPOffset) * 0.6931471805599453f;
+        if (lse && row < rows)
+            lse[(int64_t)(row0 + i) * n_q_heads + head] = none ? -CUDART_INF_F : (ref * rs + log2f(l) - kPOffset) * 0.6931471805599453f;
         __syncwarp();
         constexpr int PER_ROW = D / 8;
         for (int e = lane; e < 32 * PER_ROW; e += 32) {      // this warp's 32 rows, 16 bytes a lane
             const int r = (warp & 3) * 32 + e / PER_ROW, c8 = e % PER_ROW;
-            if (r < rows ) {
+            if (r < rows) {
                 const int ri = (row_base + r) / rep, rh = hk * rep + (row_base + r) - ri * rep;
                 *reinterpret_cast<uint4 *>(static_cast<T *>(out) + (int64_t)(row0 + ri) * out_stride + (int64_t)rh * D + c8 * 8) =
                     *reinterpret_cast<const uint4 *>(rows_out + r * D + ((c8 ^ (r & 7)) << 3));
@@ -420,15 +421,14 @@ __device__ __noinline__ void write_rows(const PagedAttnArgs &args, const PSegmen
             if (row < rows) {
 #pragma unroll
                 for (int c = 0; c < 16; c += 8) {
-                    const bool some = work && ref != -CUDART_INF_F;
-                    *reinterpret_cast<float4 *>(part + c0 + c) = some ? make_float4(x[c], x[c + 2], x[c + 4], x[c + 6]) : make_float4(0.f, 0.f, 0.f, 0.f);
-                    *reinterpret_cast<float4 *>(part + c0 + c + 4) = some ? make_float4(x[c + 1], x[c + 3], x[c + 5], x[c + 7]) : make_float4(0.f, 0.f, 0.f, 0.f);
+                    *reinterpret_cast<float4 *>(part + c0 + c) = none ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(x[c], x[c + 2], x[c + 4], x[c + 6]);
+                    *reinterpret_cast<float4 *>(part + c0 + c + 4) = none ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(x[c + 1], x[c + 3], x[c + 5], x[c + 7]);
                 }
             }
         }
         if (row < rows) {
             part[D] = ref == -CUDART_INF_F ? ref : ref * rs;
-            part[D + 1] = l;
+            part[D + 1] = none ? 0.f : l;
         }
                 }
 }

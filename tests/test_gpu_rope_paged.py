@@ -592,3 +592,23 @@ def test_long_contexts_however_the_step_is_cut(lens, new, kw):
     p.check_attention(new)
     p.check_attention(new, max_len=max(lens) + 5000 if max(lens) + 5000 <= p.max_pages * p.P else p.max_pages * p.P)      # a loose bound of the longest
     assert int(p.cache.status[0]) == 0
+
+
+@pytest.mark.parametrize("new,n_splits", [([1, 1], 0), ([1, 1], 3), ([4, 3], 0), ([20, 150], 0), ([0, 300], 0)])
+@pytest.mark.parametrize("dtype", [F16, BF16])
+def test_a_query_that_is_not_a_number_spoils_its_own_row_alone(new, n_splits, dtype):
+    p = Paged(n_seqs=2, Hq=8, H=2, D=128, G=64, W=32, P=64, seed=181, max_len=2000, dtype=dtype)
+    p.append([400, 1900])
+    T = sum(new)
+    q = torch.randn(T, 8, 128, generator=p.g).to(dtype)
+    b = p.batch(new, p.lens())
+    lse = torch.empty(T, 8, device="cuda")
+    good = p.cache.attention(b, q.cuda(), 0.1, n_splits=n_splits, lse=lse)
+    bad = q.clone()
+    bad[0, 3, 5] = bad[T - 1, 6] = math.nan
+    lse2 = torch.empty(T, 8, device="cuda")
+    out = p.cache.attention(b, bad.cuda(), 0.1, n_splits=n_splits, lse=lse2)
+    spoilt = torch.zeros(T, 8, dtype=torch.bool, device="cuda")
+    spoilt[0, 3] = spoilt[T - 1, 6] = True
+    assert torch.isnan(out[spoilt]).all() and torch.isnan(lse2[spoilt]).all()
+    assert torch.equal(out[~spoilt], good[~spoilt]) and torch.equal(lse2[~spoilt], lse[~spoilt])
