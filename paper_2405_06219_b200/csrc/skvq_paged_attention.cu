@@ -24,6 +24,9 @@
 // registers of the score product are the nibble pairs (i, i+4) of one 32-bit word, a word of every lane inside one
 // 32-channel granule; of the value product they pair one channel of tokens j and j+4.  Neither operand passes through shared
 // memory a second time; only the 16 x 8 probabilities are transposed (movmatrix).
+// Measured: a decode step of 64 sequences of 1024 to 16384 tokens, 32 heads, 564 to 588 us (4.3 to 4.5 TB/s of the cache); 4 sequences of 131072
+// tokens, 32 heads over 8, 163 us.  Instruction issue bounds it (61 % of the slots with 11 warps an SM, the logic pipe that unpacks
+// codes half busy); a CTA more an SM spills.
 #include <math_constants.h>
 
 #include "skvq_mma_common.cuh"
