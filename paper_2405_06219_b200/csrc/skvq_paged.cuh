@@ -72,6 +72,46 @@ template <> __device__ __forceinline__ uint32_t packed<__nv_bfloat16>(float lo, 
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
 }
+// Two fp32 in a 64-bit register: one instruction works on both, rounding each as the scalar form does.
+__device__ __forceinline__ uint64_t pair(float a, float b)
+{
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void unpair(uint64_t v, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ uint64_t pair_fma(uint64_t a, uint64_t b, uint64_t c)
+{
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t pair_add(uint64_t a, uint64_t b)
+{
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+// For products that are exact: the compiler contracts it with a sum that follows.
+__device__ __forceinline__ uint64_t pair_mul(uint64_t a, uint64_t b)
+{
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+// The two elements of a register as a pair of floats, and back (rounded).
+template <typename T> __device__ __forceinline__ uint64_t pair_of(uint32_t v)
+{
+    const float2 f = floats<T>(v);
+    return pair(f.x, f.y);
+}
+template <typename T> __device__ __forceinline__ uint32_t packed(uint64_t v)
+{
+    float lo, hi;
+    unpair(v, lo, hi);
+    return packed<T>(lo, hi);
+}
+
 // Rotates a lane's channels c0 .. c0 + C - 1 of a row; cs[j] = {cos, sin} of channel c0 + j.  `raw` is the row in shared memory, as read, for
 // the partners of the half layout (interleaved pairs lie in one lane).  Rounded to T.
 template <typename T, int D>

@@ -26,6 +26,8 @@ struct AppendIo {
     int64_t k_stride, v_stride;
     int heads;       // heads a CTA walks over
     int bulk;        // 1: half-warps take tokens; 0: heads of one token
+    uint64_t nothing = 0x8000000080000000ull;      // a pair of -0: a product with it added is the rounded product (a plain paired product before
+                                                  // a paired sum is contracted with it; a value from outside is not)
 };
 
 template <typename T> __device__ __forceinline__ uint32_t min2(uint32_t a, uint32_t b);
@@ -113,7 +115,7 @@ __device__ __forceinline__ void append_rows(const AppendIo &io, const PagedSeq &
     bool have[2], keep[2];
     int page[2], ring[2];
     int64_t page_row[2];
-    float2 cs[2][IS_V ? 1 : C];
+    uint64_t cosine[IS_V ? 1 : C], sine[IS_V ? 1 : C];      // of both tokens
     const T *src[2];
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
@@ -127,21 +129,25 @@ __device__ __forceinline__ void append_rows(const AppendIo &io, const PagedSeq &
                 if (sub == 0) set_status(a.c.status, SKVQ_STATUS_BAD_PAGE);
             }
         }
-        if constexpr (!IS_V) {
-            if (rot && have[k]) {
-                load_angles(cs[k], a.rope, t, c0);
-#pragma unroll
-                for (int j = 0; j < C; ++j)
-                    if (inter ? !((c0 + j) & 1) : c0 + j < half) cs[k][j].y = -cs[k][j].y;
-            } else {
-#pragma unroll
-                for (int j = 0; j < (IS_V ? 1 : C); ++j) cs[k][j] = make_float2(0.f, 0.f);
-            }
-        }
         src[k] = static_cast<const T *>(IS_V ? io.v : io.k) + (int64_t)(seq.row0 + i + k) * (IS_V ? io.v_stride : io.k_stride) + c0;
         page_row[k] = ((int64_t)page[k] * cfg.n_kv_heads) * P + t % P;
         keep[k] = cfg.window > 0 && have[k] && page[k] >= 0 && t >= seq.len - cfg.ring_tokens;
         ring[k] = cfg.ring_tokens > 0 ? t % cfg.ring_tokens : 0;
+    }
+    if constexpr (!IS_V) {
+        float2 cs[2][C];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+#pragma unroll
+            for (int j = 0; j < C; ++j) cs[k][j] = make_float2(0.f, 0.f);
+            if (rot && have[k]) load_angles(cs[k], a.rope, seq.len - seq.n + i + k, c0);
+        }
+#pragma unroll
+        for (int j = 0; j < C; ++j) {
+            const float sign = (inter ? !((c0 + j) & 1) : c0 + j < half) ? -1.f : 1.f;
+            cosine[j] = pair(cs[0][j].x, cs[1][j].x);
+            sine[j] = pair(sign * cs[0][j].y, sign * cs[1][j].y);
+        }
     }
     const int32_t *reorder = IS_V ? a.c.reorder_v : a.c.reorder_k;
     const float *alphas = IS_V ? a.c.alpha_v : a.c.alpha_k;
@@ -169,8 +175,7 @@ __device__ __forceinline__ void append_rows(const AppendIo &io, const PagedSeq &
             if (have[k] && h0 + h_step < h_end) next[k].load(src[k] + (int64_t)(h0 + h_step) * D);
         if constexpr (!IS_V) {
             if (rot) {
-                // y = x c + o s with the partner o and, for the first channel of a pair, the sine negated (see the loads of cs): the
-                // roundings of x c - o s
+                // y = x c + o s with the partner o and, for the first channel of a pair, the sine negated: the roundings of x c - o s
                 uint32_t o[C];
                 if (inter) {
 #pragma unroll
@@ -190,9 +195,7 @@ __device__ __forceinline__ void append_rows(const AppendIo &io, const PagedSeq &
                 if (c0 < rot_dim) {
 #pragma unroll
                     for (int j = 0; j < C; ++j) {
-                        const float2 x = floats<T>(w[j]), y = floats<T>(o[j]);
-                        const uint32_t v = packed<T>(__fadd_rn(__fmul_rn(x.x, cs[0][j].x), __fmul_rn(y.x, cs[0][j].y)),
-                                                     __fadd_rn(__fmul_rn(x.y, cs[1][j].x), __fmul_rn(y.y, cs[1][j].y)));
+                        const uint32_t v = packed<T>(pair_add(pair_fma(pair_of<T>(w[j]), cosine[j], io.nothing), pair_fma(pair_of<T>(o[j]), sine[j], io.nothing)));
                         if (straight || c0 + j < rot_dim) w[j] = v;
                     }
                 }
@@ -213,25 +216,52 @@ __device__ __forceinline__ void append_rows(const AppendIo &io, const PagedSeq &
             mx = max2<T>(mx, __shfl_xor_sync(0xffffffffu, mx, m));
         }
         const float2 mnf = floats<T>(mn), mxf = floats<T>(mx);
+        constexpr float MAGIC = 12582912.0f;      // 1.5 2^23: a sum with it is rounded to an integer, ties to even
+        __half2 hz2[2];
+        float h2[2], z2[2], r2[2], far2[2] = {0.f, 0.f};      // far2: largest remainder
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
             const float lo = __fadd_rn(__fmul_rn(alpha, k ? mnf.y : mnf.x), 0.0f), hi = __fadd_rn(__fmul_rn(alpha, k ? mxf.y : mxf.x), 0.0f);
-            const __half2 hz = __halves2half2(__float2half_rn(__fmul_rn(__fsub_rn(hi, lo), 1.0f / 15.0f)), __float2half_rn(lo));
-            const float hf = __low2float(hz), zf = __high2float(hz);
-            constexpr float MAGIC = 12582912.0f;      // 1.5 2^23: a sum with it is rounded to an integer, ties to even
-            const float r = hf != 0.0f ? __frcp_rn(hf) : 0.0f;
-            float far = 0.f, p[C / 4];      // largest remainder; four codes in a sum
+            hz2[k] = __halves2half2(__float2half_rn(__fmul_rn(__fsub_rn(hi, lo), 1.0f / 15.0f)), __float2half_rn(lo));
+            h2[k] = __low2float(hz2[k]);
+            z2[k] = __high2float(hz2[k]);
+            r2[k] = h2[k] != 0.0f ? __frcp_rn(h2[k]) : 0.0f;
+        }
+        uint32_t code[2];
+        {
+            const uint64_t neg_z = pair(-z2[0], -z2[1]), neg_h = pair(-h2[0], -h2[1]), inverse = pair(r2[0], r2[1]);
+            const uint64_t magic = pair(MAGIC, MAGIC), neg_magic = pair(-MAGIC, -MAGIC);
+            uint32_t q[C];      // both tokens' codes as fp16, clamped
 #pragma unroll
             for (int j = 0; j < C; ++j) {
-                const float2 x = floats<T>(w[j]);
-                const float d = __fsub_rn(k ? x.y : x.x, zf);
-                const float c = __fsub_rn(__fmaf_rn(d, r, MAGIC), MAGIC);
-                far = fmaxf(far, fabsf(__fmaf_rn(-c, hf, d)));
-                const float q = fminf(fmaxf(c, 0.0f), 15.0f);
-                p[j / 4] = j % 4 == 0 ? q : __fmaf_rn(q, (float)(1 << (4 * (j % 4))), p[j / 4]);
+                const uint64_t d = pair_add(pair_of<T>(w[j]), neg_z), c = pair_add(pair_fma(d, inverse, magic), neg_magic);
+                float e0, e1, c0f, c1f;
+                unpair(pair_fma(c, neg_h, d), e0, e1);
+                unpair(c, c0f, c1f);
+                far2[0] = fmaxf(far2[0], fabsf(e0));
+                far2[1] = fmaxf(far2[1], fabsf(e1));
+                asm("{\n .reg .b32 t;\n cvt.rn.relu.f16x2.f32 t, %1, %2;\n min.f16x2 %0, t, %3;\n}" : "=r"(q[j]) : "f"(c1f), "f"(c0f), "r"(0x4B804B80u));      // 15
             }
-            uint32_t codes = (uint32_t)(int)p[0];
-            if constexpr (C == 8) codes |= (uint32_t)(int)p[1] << 16;
+            // 1024 + first + 16 second: exact, and the fp16's low byte is the codes' byte
+            uint32_t u[C / 2];
+#pragma unroll
+            for (int j = 0; j < C / 2; ++j)
+                asm("{\n .reg .b32 t;\n add.rn.f16x2 t, %1, %3;\n fma.rn.f16x2 %0, %2, %4, t;\n}" : "=r"(u[j]) : "r"(q[2 * j]), "r"(q[2 * j + 1]), "r"(0x64006400u), "r"(0x4C004C00u));
+            const uint32_t lo = __byte_perm(u[0], u[1], 0x6240);      // bytes: first token's two, second token's two
+            if constexpr (C == 8) {
+                const uint32_t hi = __byte_perm(u[2], u[3], 0x6240);
+                code[0] = __byte_perm(lo, hi, 0x5410);
+                code[1] = __byte_perm(lo, hi, 0x7632);
+            } else {
+                code[0] = lo & 0xFFFFu;
+                code[1] = lo >> 16;
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const float hf = h2[k], zf = z2[k], r = r2[k], far = far2[k];
+            const __half2 hz = hz2[k];
+            uint32_t codes = code[k];
             // In doubt (fp16 values meet k + 1/2 often: two iterations in five have such an element somewhere in the warp): the remainder
             // is exact, so a tie shows as |remainder| = h/2 and goes to the even code; what is near a tie but none, and quotients
             // beyond 2^22 or infinite, take the division.
@@ -374,35 +404,42 @@ __global__ void __launch_bounds__(kRowThreads) paged_read_kernel(const __grid_co
     for (int h0 = first; __any_sync(0xffffffffu, h0 < h_end); h0 += step) {
         const bool here = h0 < h_end;
         const int h = min(h0, h_end - 1);
-        R row[2];
+        // 2^23 + 16^p code, minus 2^23, times h / 16^p (all exact but the product), for nibbles p = 0 .. 4 in place, then from bit 20 on
+        uint32_t w[C];
+        {
+            const float2 par0 = __half22float2(*reinterpret_cast<const __half2 *>(&hz_next[0])), par1 = __half22float2(*reinterpret_cast<const __half2 *>(&hz_next[1]));
+            const uint64_t z = pair(par0.y, par1.y), neg = pair(-8388608.0f, -8388608.0f), down = pair(0.0625f, 0.0625f);
+            uint64_t h = pair(par0.x, par1.x);
+            uint64_t hs[5];
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const uint32_t codes = codes_next[k];
-            const __half2 hz = *reinterpret_cast<const __half2 *>(&hz_next[k]);
-            const float hf = __low2float(hz), zf = __high2float(hz);
+            for (int p = 0; p < 5; ++p) { hs[p] = h; h = pair_mul(h, down); }
 #pragma unroll
-            for (int m = 0; m < R::WORDS; ++m) {
-                float v[2];
-#pragma unroll
-                for (int e = 0; e < 2; ++e)      // 2^23 + code, minus 2^23
-                    v[e] = __fadd_rn(__fmul_rn(hf, __fsub_rn(__uint_as_float(0x4B000000u | ((codes >> (8 * m + 4 * e)) & 15u)), 8388608.0f)), zf);
-                row[k].w[m] = packed<T>(v[0], v[1]);
+            for (int j = 0; j < C; ++j) {
+                const int p = j < 5 ? j : j - 5;
+                const uint32_t a0 = j < 5 ? codes_next[0] : codes_next[0] >> 20, a1 = j < 5 ? codes_next[1] : codes_next[1] >> 20;
+                const uint64_t c = pair_add(pair(__uint_as_float(0x4B000000u | (a0 & (15u << (4 * p)))), __uint_as_float(0x4B000000u | (a1 & (15u << (4 * p))))), neg);
+                w[j] = packed<T>(pair_add(pair_mul(hs[p], c), z));
             }
-            if (recent[k] && have[k] && here) row[k].load(win + (win_row[k] + (int64_t)h * cfg.ring_tokens) * D + c0);
+        }
+        R row[2];
+        if ((recent[0] && have[0]) || (recent[1] && have[1])) {
+            separate<T, D>(w, row);
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+                if (recent[k] && have[k] && here) row[k].load(win + (win_row[k] + (int64_t)h * cfg.ring_tokens) * D + c0);
+            interleave<T, D>(row, w);
         }
         load(h0 + step);
         if (reorder) {
-            uint32_t w[C];
             int idx[C];
             load_index<C, D>(idx, reorder, h, c0);
-            interleave<T, D>(row, w);
 #pragma unroll
             for (int j = 0; j < C; ++j) mine[idx[j]] = w[j];
             __syncwarp();
             get_words(mine + c0, w);
             __syncwarp();
-            separate<T, D>(w, row);
         }
+        separate<T, D>(w, row);
 #pragma unroll
         for (int k = 0; k < 2; ++k)
             if (here && have[k]) row[k].store(out[k] + (int64_t)h * D);

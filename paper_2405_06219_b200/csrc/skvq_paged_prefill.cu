@@ -136,27 +136,6 @@ template <typename T> __device__ __forceinline__ uint32_t to_h2(uint32_t v);    
 template <> __device__ __forceinline__ uint32_t to_h2<__half>(uint32_t v) { return v; }
 template <> __device__ __forceinline__ uint32_t to_h2<__nv_bfloat16>(uint32_t v) { return h2(__uint_as_float(v << 16), __uint_as_float(v & 0xFFFF0000u)); }
 
-// Two fp32 in a 64-bit register: one instruction works on both.
-__device__ __forceinline__ uint64_t pair(float a, float b)
-{
-    uint64_t r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
-    return r;
-}
-__device__ __forceinline__ void unpair(uint64_t v, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
-__device__ __forceinline__ uint64_t pair_fma(uint64_t a, uint64_t b, uint64_t c)
-{
-    uint64_t r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-    return r;
-}
-__device__ __forceinline__ uint64_t pair_add(uint64_t a, uint64_t b)
-{
-    uint64_t r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
-
 // Poll with a limit in clock cycles (about a tenth of a second); false: it ran out.
 __device__ __forceinline__ bool mbar_wait_cycles(uint32_t bar, uint32_t parity)
 {
