@@ -357,7 +357,9 @@ typedef struct skvq_paged_config {
  *   alpha_k/_v       float  [Hkv][ng]                 clip factors; NULL = 1
  *   status           int32  [1] or NULL               SKVQ_STATUS_* bits are OR-ed in
  * EVERY token is quantized into its page when it is appended, and the newest are kept in the ring as well: a page is
- * complete at any time (it can be shared, moved or kept for another request with the same prefix).
+ * complete at any time (it can be shared, moved or kept for another request with the same prefix).  The ring is not: a
+ * sequence that begins on kept pages, or comes back in another slot, says in skvq_paged_batch::ring_from where its slot's
+ * rows begin.
  */
 typedef struct skvq_paged_cache {
     void *k_codes, *v_codes;
@@ -379,6 +381,11 @@ typedef struct skvq_paged_batch {
     int32_t n_tokens;          /* T: rows that k, v, q and outputs have */
     int32_t max_new;           /* host upper bound on n_b; max_new * Hq/Hkv <= 2^30 */
     int32_t max_len;           /* host upper bound on lens[], <= max_pages * P */
+    const int32_t *ring_from;  /* [n_seqs] or NULL: the slot's ring holds the sequence's tokens from ring_from[b] on -- the first
+                                  token appended since the sequence has had this slot; older tokens of the window are read from
+                                  their pages, quantized.  (After more than R - W tokens were taken back it is the longest length
+                                  reached minus R.)  Values below 0 count as 0, values above L_b as L_b.  NULL: 0, every token of
+                                  the window was appended to this slot, by this sequence */
 } skvq_paged_batch;
 
 /* Validate a paged configuration (host only). */
@@ -405,7 +412,7 @@ int skvq_paged_append(const skvq_paged_config *cfg, const skvq_paged_cache *cach
 
 /*
  * The last n_b tokens of every sequence as values, channels back in source order: h*code + z in fp32, rounded to dtype; with
- * window = 1 the newest W tokens of a sequence come from the ring instead (what attention sees).  Keys come out rotated, as
+ * window = 1 those of the newest W tokens of a sequence that its ring holds (ring_from) come from the ring instead (what attention sees).  Keys come out rotated, as
  * they are held.  Rows of skipped sequences and tokens (see skvq_paged_append) are left alone.
  *   k, v             dtype [T][Hkv][D], token strides as for skvq_paged_append; either may be NULL
  */

@@ -83,7 +83,7 @@ class SkvqPagedCacheStruct(ctypes.Structure):
 
 class SkvqPagedBatch(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("page_table", "lens", "starts", "slots")] + \
-        [(n, ctypes.c_int32) for n in ("n_seqs", "max_pages", "n_tokens", "max_new", "max_len")]
+        [(n, ctypes.c_int32) for n in ("n_seqs", "max_pages", "n_tokens", "max_new", "max_len")] + [("ring_from", ctypes.c_void_p)]
 
 
 class SkvqPagedAttnArgs(ctypes.Structure):
@@ -490,15 +490,17 @@ class SkvqPagedCache:
             self.alpha_k, self.alpha_v, self.status)])
         self.index = self.k_codes.get_device()
 
-    def batch(self, page_table, lens, starts, n_tokens: int, max_new: int, max_len: int, slots=None) -> SkvqPagedBatch:
+    def batch(self, page_table, lens, starts, n_tokens: int, max_new: int, max_len: int, slots=None, ring_from=None) -> SkvqPagedBatch:
         """The sequences of a step: page_table int32 [n, max_pages], lens int32 [n] (tokens including the new ones), starts
-        int32 [n + 1] (their rows among the n_tokens packed ones), slots int32 [n] or None; max_new and max_len bound them."""
+        int32 [n + 1] (their rows among the n_tokens packed ones), slots int32 [n] or None; max_new and max_len bound them.  ring_from int32
+        [n] or None: the first token that was appended to the sequence's present slot, for sequences that begin on kept pages or came
+        back in another slot; the window's older tokens are then read from their pages."""
         n = page_table.shape[0]
-        for t, count in ((page_table, page_table.numel()), (lens, n), (starts, n + 1), (slots, n)):
+        for t, count in ((page_table, page_table.numel()), (lens, n), (starts, n + 1), (slots, n), (ring_from, n)):
             assert t is None or (t.device == self.device and t.dtype == torch.int32 and t.is_contiguous() and t.numel() == count)
         b = SkvqPagedBatch(page_table.data_ptr(), lens.data_ptr(), starts.data_ptr(), _dptr(slots), n, page_table.shape[1],
-                           n_tokens, max_new, max_len)
-        b.keep = (page_table, lens, starts, slots)
+                           n_tokens, max_new, max_len, _dptr(ring_from))
+        b.keep = (page_table, lens, starts, slots, ring_from)
         return b
 
     def _rows(self, x, batch, heads) -> int:

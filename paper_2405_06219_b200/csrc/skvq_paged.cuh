@@ -162,6 +162,7 @@ __device__ __forceinline__ void set_status(int32_t *status, int bits)
 
 struct PagedSeq {
     int len, n, row0, slot;     // tokens including the new ones, new ones, first packed row, ring slot
+    int lq;                     // tokens below it are read from the pages, the others from the ring
 };
 
 // What sequence b asks for; false when its entries are out of range (the caller reports and skips it).
@@ -174,6 +175,8 @@ __device__ __forceinline__ bool paged_sequence(const PagedArgs &a, int b, bool r
     q.row0 = s0;
     q.n = s1 - s0;
     q.slot = p.slots ? p.slots[b] : b;
+    q.lq = max(q.len - a.cfg.window, 0);
+    if (p.ring_from) q.lq = max(q.lq, min(p.ring_from[b], q.len));
     bool ok = s0 >= 0 && s1 >= s0 && s1 <= p.n_tokens && q.n <= p.max_new && q.len >= 0 && q.len <= p.max_len;
     if (rows_within_len) ok = ok && q.n <= q.len;
     if (a.rope.table) ok = ok && q.len <= a.rope.n_positions;

@@ -37,7 +37,7 @@ int check_batch(const skvq_paged_config *cfg, const skvq_paged_batch *b)
     if (b->n_seqs > kMaxPagedSeqs) return SKVQ_ERR_UNSUPPORTED;
     if ((int64_t)b->max_new * (cfg->n_q_heads / cfg->n_kv_heads) > (1 << 30)) return SKVQ_ERR_UNSUPPORTED;      // packed rows of a KV head
     if (b->max_len > (int64_t)b->max_pages * cfg->page_tokens) return SKVQ_ERR_CAPACITY;
-    if (off(b->page_table, 4) || off(b->lens, 4) || off(b->starts, 4) || off(b->slots, 4)) return SKVQ_ERR_MISALIGNED;
+    if (off(b->page_table, 4) || off(b->lens, 4) || off(b->starts, 4) || off(b->slots, 4) || off(b->ring_from, 4)) return SKVQ_ERR_MISALIGNED;
     if (!b->slots && cfg->window > 0 && b->n_seqs > cfg->n_slots) return SKVQ_ERR_CAPACITY;
     return SKVQ_OK;
 }

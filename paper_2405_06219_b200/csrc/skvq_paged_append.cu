@@ -371,7 +371,7 @@ __global__ void __launch_bounds__(kRowThreads) paged_read_kernel(const __grid_co
     for (int k = 0; k < 2; ++k) {
         const int t = seq.len - seq.n + i + k;
         have[k] = i + k < seq.n;
-        recent[k] = io.window && cfg.window > 0 && t >= seq.len - cfg.window;
+        recent[k] = io.window && t >= seq.lq;
         int page = 0;
         if (have[k] && !recent[k]) {
             page = a.batch.page_table[(int64_t)b * a.batch.max_pages + t / P];

@@ -152,9 +152,8 @@ __device__ __forceinline__ SeqCost seq_cost(const PagedArgs &p, const PagedSeq &
 {
     SeqCost c;
     const int rep = p.cfg.n_q_heads / p.cfg.n_kv_heads;
-    const int lq = max(s.len - p.cfg.window, 0);
-    c.tiles_c = (lq + kTile - 1) / kTile;
-    c.tiles_r = (s.len - lq + kRingTile - 1) / kRingTile;
+    c.tiles_c = (s.lq + kTile - 1) / kTile;
+    c.tiles_r = (s.len - s.lq + kRingTile - 1) / kRingTile;
     c.cost = pieces ? pieces : max(c.tiles_c + kRingCost * c.tiles_r, 1);
     c.m_tiles = s.n * rep <= kFewRows ? (s.n * rep + rows - 1) / rows : 0;      // the others are the tcgen05 kernel's
     return c;
@@ -242,7 +241,7 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 2 ? 2 : 3) paged_split_ke
         const int take = (int)min((long long)(sc.cost - off), f1 - f);
         const int hk = (int)(item / sc.m_tiles), mt = (int)(item - (long long)hk * sc.m_tiles);
         const int row_base = mt * ROWS, R = min(ROWS, seq.n * rep - row_base);
-        const int L = seq.len, lq = max(L - cfg.window, 0);
+        const int L = seq.len, lq = seq.lq;
         // rows see tokens below their limit
         auto row_limit = [&](int r) { return a.causal ? min(L, L - seq.n + (row_base + min(r, R - 1)) / rep + 1) : L; };
         const int limit_lo = row_limit(0), limit_hi = row_limit(R - 1);

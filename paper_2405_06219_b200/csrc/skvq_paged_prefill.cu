@@ -181,7 +181,7 @@ struct PItems {
         rep = a.a.p.cfg.n_q_heads / a.a.p.cfg.n_kv_heads;
         n = s.n;
         len = s.len;
-        lq = max(s.len - a.a.p.cfg.window, 0);
+        lq = s.lq;
         causal = a.a.causal;
         tiles_c = (lq + kBlock - 1) / kBlock;
     }

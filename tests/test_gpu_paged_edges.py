@@ -1,0 +1,141 @@
+"""The paged cache where it meets an engine's own bookkeeping: kept prefixes, sequences that change their slot, page-table entries
+that are no pages, queries that are not finite.  Against the plain 64-bit forms of paged_reference, with their counted bounds."""
+import math
+
+import pytest
+import torch
+
+import paged_reference as ref
+import test_gpu_rope_paged as base
+from paper_2405_06219_b200 import binding as B
+from paper_2405_06219_b200 import build
+
+pytestmark = pytest.mark.gpu
+F16, BF16 = torch.float16, torch.bfloat16
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _lib():
+    build.build_library()
+    B.lib()
+
+
+# ------------------------------------------------------------------------------------------------ a window that reaches back behind the ring
+class FromPages(ref.Reference):
+    """The plain cache with a first ring token per sequence: tokens before it are read from their pages, inside the window too."""
+
+    def __init__(self, plain, n):
+        self.__dict__.update(plain.__dict__)
+        self.ring_from = [0] * n
+
+    def ring_rows(self, b):
+        L = len(self.rows[b])
+        return min(self.W, L - min(max(self.ring_from[b], 0), L))
+
+    def values(self, b, which, window=True):
+        whole, self.W = self.W, self.ring_rows(b)
+        try:
+            return super().values(b, which, window)
+        finally:
+            self.W = whole
+
+    def score_error(self, b):
+        whole, self.W = self.W, self.ring_rows(b)
+        try:
+            return super().score_error(b)
+        finally:
+            self.W = whole
+
+
+class Engine(base.Paged):
+    """A cache whose sequences say where their ring begins; ring rows that nobody wrote are NaN."""
+
+    def __init__(self, n_seqs, **kw):
+        super().__init__(n_seqs=n_seqs, **kw)
+        self.ref = FromPages(self.ref, n_seqs)
+
+    def batch(self, new, lens, pad=0, max_new=None, max_len=None):
+        b = super().batch(new, lens, pad, max_new, max_len)
+        first = torch.tensor(self.ref.ring_from, dtype=torch.int32, device="cuda")
+        return self.cache.batch(*b.keep[:3], b.n_tokens, b.max_new, b.max_len, slots=b.keep[3], ring_from=first)
+
+    def check_read(self, new):
+        """The last rows of every sequence as attention sees them."""
+        T = sum(new)
+        k, v = self.cache.read(self.batch(new, self.lens()))
+        at = 0
+        for i, n in enumerate(new):
+            L = len(self.ref.rows[i])
+            for got, which, idx in ((k, "k", self.ref.rk), (v, "v", self.ref.rv)):
+                val = self.ref.values(i, which)[L - n:].float().to(self.dtype)
+                want = torch.empty(n, self.H, self.D, dtype=self.dtype)
+                for h in range(self.H):
+                    want[:, h, idx[h]] = val[:, h]
+                assert torch.equal(base.bits(got[at:at + n].cpu()), base.bits(want)), (i, which)
+            at += n
+        assert at == T
+
+
+RINGS = [dict(W=32, P=32, D=128, G=64, rot=64), dict(W=20, R=33, P=16, D=64, G=32, H=3, Hq=9, dtype=BF16), dict(W=150, P=16, D=128, G=32, H=1, Hq=4, rot=128, inter=True)]
+
+
+@pytest.mark.parametrize("kw", RINGS)
+def test_a_kept_prefix_under_a_window(kw):
+    """A second sequence begins on the first one's pages: the prefix tokens of its window are read from there, until the window has
+    passed them."""
+    p = Engine(2, seed=71, **kw)
+    p.append([96, 0])
+    shared = 96 // p.P
+    p.page_table[1, :shared] = p.page_table[0, :shared]
+    p.ref.rows[1] = list(p.ref.rows[0])
+    p.ref.ring_from[1] = 96
+    p.check_attention([1, 1])                    # nothing appended yet: the whole window lies in shared pages
+    p.check_attention([90, 60])
+    for new in ([1, 1], [3, 2], [10, 14], [1, 1], [40, 60], [1, 1], [90, 100]):
+        p.append(new)
+        p.check_attention(new)
+        p.check_attention([1, 1], n_splits=2)
+        p.check_attention([30, 50], causal=False)
+        p.check_read([min(60, n) for n in p.lens()])
+    assert int(p.cache.status[0]) == 0
+
+
+@pytest.mark.parametrize("kw", RINGS)
+@pytest.mark.parametrize("length", [1, 15, 37, 130])
+def test_a_sequence_that_comes_back_in_another_slot(kw, length):
+    p = Engine(2, seed=72, slots=[0, 1, 2, 3], **kw)
+    p.slots = torch.tensor([0, 1], dtype=torch.int32, device="cuda")
+    p.append([length, 50])
+    p.slots = torch.tensor([3, 1], dtype=torch.int32, device="cuda")      # slot 3 was never written
+    p.ref.ring_from[0] = length
+    p.check_attention([1, 1])
+    for new in ([1, 1], [17, 1], [64, 30]):
+        p.append(new)
+        p.check_attention(new)
+        p.check_attention([1, 4])
+        p.check_read([min(5, n) for n in p.lens()])
+    assert int(p.cache.status[0]) == 0
+
+
+def test_first_ring_tokens_outside_the_sequence():
+    p = Engine(3, W=32, seed=73)
+    p.append([100, 40, 0])
+    p.cache.k_win[1].fill_(math.nan)             # all of this one comes from its pages
+    p.cache.v_win[1].fill_(math.nan)
+    p.ref.ring_from = [-7, 2 ** 31 - 1, 5]
+    p.check_attention([1, 1, 1])
+    p.check_attention([50, 40, 0])
+    p.check_read([60, 40, 0])
+    assert int(p.cache.status[0]) == 0
+
+
+def test_taking_back_more_than_the_ring_holds():
+    """The ring is as long as the window: tokens that were refused took the rows of older ones, which then come from their pages."""
+    p = Engine(1, W=32, seed=74, max_len=200)
+    p.append([100])
+    p.append([8])
+    p.ref.truncate(0, 102)
+    p.ref.ring_from = [108 - 32]
+    p.check_attention([1])
+    p.check_attention([40])
+    p.check_read([40])
