@@ -445,7 +445,7 @@ size_t skvq_paged_workspace_size(const skvq_paged_config *cfg, const skvq_paged_
  *   q, out           dtype [T][Hq][D], token strides in elements (multiples of 8, >= Hq*D)
  *   lse              float [T][Hq], natural logarithm of the softmax denominator of every row, or NULL
  * Skipped sequences (as for skvq_paged_append, except that n_b may exceed L_b): their rows are left alone.  Tokens behind a bad
- * page-table entry are left out of the softmax and SKVQ_STATUS_BAD_PAGE is set.  Rows of the cache at or beyond L_b are never
+ * page-table entry, those of the window too, are left out of the softmax and SKVQ_STATUS_BAD_PAGE is set.  Rows of the cache at or beyond L_b are never
  * used, whatever they hold.  A query that is not finite gives its own row NaN and no other.  Keys and values have to be finite and
  * in fp16's range (as for skvq_paged_append): one that is not can reach every row of its sequence, those that do not see it too.
  * The workspace is overwritten; calls sharing one must be stream-ordered.  out and lse must not overlap the inputs.

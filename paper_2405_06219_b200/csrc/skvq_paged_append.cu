@@ -373,7 +373,7 @@ __global__ void __launch_bounds__(kRowThreads) paged_read_kernel(const __grid_co
         have[k] = i + k < seq.n;
         recent[k] = io.window && t >= seq.lq;
         int page = 0;
-        if (have[k] && !recent[k]) {
+        if (have[k]) {
             page = a.batch.page_table[(int64_t)b * a.batch.max_pages + t / P];
             if (page < 0 || page >= cfg.n_pages) {
                 have[k] = false;

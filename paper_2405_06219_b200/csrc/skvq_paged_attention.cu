@@ -581,7 +581,10 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 2 ? 2 : 3) paged_split_ke
         for (int tile = r0 + warp; tile < r1; tile += kSplitWarps) {
             const int t0 = lq + (tile - sc.tiles_c) * kRingTile;
             if (t0 >= limit_hi) break;
+            uint32_t gone;      // tokens of the tile whose page-table entry is no page of the pool
             {
+                int id = 0;
+                if (lane < kRingTile && t0 + lane < L) id = table[(t0 + lane) >> page_shift];
                 // lane: piece lane % RCHUNKS of every (32 / RCHUNKS)-th row; piece c of row t lies at c ^ (t & 7)
                 constexpr int STEP = 32 / Geo::RCHUNKS;
                 const int c = lane % Geo::RCHUNKS, first = t0 % cfg.ring_tokens;
@@ -600,8 +603,17 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 2 ? 2 : 3) paged_split_ke
                     }
                 }
                 cp_commit();
+                const bool none = id < 0 || id >= cfg.n_pages;
+                if (none) set_status(p.c.status, SKVQ_STATUS_BAD_PAGE);
+                gone = __ballot_sync(0xffffffffu, none);
                 cp_wait<0>();
                 __syncwarp();
+                if (gone) {      // their value rows hold nothing that may reach the product
+                    for (int e = lane; e < kRingTile * Geo::RCHUNKS; e += 32)
+                        if ((gone >> (e / Geo::RCHUNKS)) & 1u)
+                            *reinterpret_cast<uint4 *>(smem + warp * kStages * Geo::STAGE + kRingTile * Geo::RROW + e * 16) = make_uint4(0u, 0u, 0u, 0u);
+                    __syncwarp();
+                }
             }
             float s[1][NT][4];
 #pragma unroll
@@ -625,7 +637,7 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 2 ? 2 : 3) paged_split_ke
             for (int n = 0; n < NT; ++n)
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    if (t0 + tok + 8 * (e >> 1) >= lim[n][e & 1]) s[0][n][e] = -CUDART_INF_F;
+                    if (t0 + tok + 8 * (e >> 1) >= lim[n][e & 1] || ((gone >> (tok + 8 * (e >> 1))) & 1u)) s[0][n][e] = -CUDART_INF_F;
             uint32_t pb[1][NT][2];
             softmax_tile(s, pb);
 #pragma unroll

@@ -433,7 +433,7 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
     __shared__ float row_scale[2 * kBlock];
     __shared__ uint16_t out_channel[2][D];      // source channel of every operand column, per row block
     __shared__ PSegment seg_sh[5];              // of the two row blocks' softmax, of the dequantizers, of the two issuers
-    __shared__ uint32_t bad_sh[4];              // of the last four tiles: 16-token blocks without a page (a tile's is read until its
+    __shared__ uint32_t bad_sh[4][4];           // of the last four tiles: tokens without a page, a bit each (a tile's are read until its
                                                 // probabilities are written, when the tile two further on may be in the making)
     const int tid = threadIdx.x, lane = tid & 31, B = p.batch.n_seqs;
     const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);      // one value per warp, and the compiler knows: descriptors stay in uniform registers
@@ -557,16 +557,18 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
             uint4 kc[PIECES], vc[PIECES];
             uint32_t km[NG], vm[NG];
             int page = -1;
-            // the page of this thread's token in tile t; -1: no such token, -2: no such page
+            // this thread's token in tile t
+            auto token_of = [&](int t) { return (t < s.it.tiles_c ? t * kBlock : s.it.lq + (t - s.it.tiles_c) * kBlock) + row; };
+            // its page (of a window token too: one without a page is left out); -1: no such token, -2: no such page
             auto page_of = [&](int t) {
-                const int tok = t * kBlock + row;
-                if (t >= min(s.t1, s.it.tiles_c) || tok >= s.it.lq) return -1;
+                const int tok = token_of(t);
+                if (t >= s.t1 || tok >= (t < s.it.tiles_c ? s.it.lq : s.seq.len)) return -1;
                 const int id = table[tok >> page_shift];
                 if (id < 0 || id >= cfg.n_pages) { set_status(p.c.status, SKVQ_STATUS_BAD_PAGE); return -2; }
                 return id;
             };
             auto load_codes = [&](int t) {      // of tile t, with `page`
-                if (page >= 0) {
+                if (page >= 0 && t < s.it.tiles_c) {
                     const int64_t at = ((int64_t)page * cfg.n_kv_heads + s.hk) * P + ((t * kBlock + row) & (P - 1));
 #pragma unroll
                     for (int i = 0; i < PIECES; ++i) {
@@ -624,16 +626,12 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
                     }
                 };
                 const bool quantized = t < s.it.tiles_c;
-                const int tok = s.it.lq + (t - s.it.tiles_c) * kBlock + row;      // of a window tile
-                const bool have = !quantized && tok < s.seq.len;
-                const int64_t r = have ? win_row0 + tok % cfg.ring_tokens : 0;
+                const bool have = !quantized && page >= 0;      // a window token
+                const int64_t r = have ? win_row0 + token_of(t) % cfg.ring_tokens : 0;
                 if (n >= 2) wait(k_empty + 8 * buf, phase ^ 1u);
                 {
                     const uint32_t gone = __ballot_sync(0xffffffffu, page == -2);
-                    if (lane == 0) {      // this warp's two 16-token blocks
-                        const uint32_t two = (gone & 0xFFFFu ? 1u : 0u) | (gone >> 16 ? 2u : 0u);
-                        reinterpret_cast<uint8_t *>(&bad_sh[n & 3])[warp - 8] = (uint8_t)(quantized ? two : 0u);
-                    }
+                    if (lane == 0) bad_sh[n & 3][warp - 8] = gone;
                 }
                 if (alive) {
                     if (quantized) expand(kt, kc, km);
@@ -758,8 +756,7 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
                     float x[32], y[32];
                     tmem_ld32(h_addr, x);
                     tmem_ld32(h_addr + 32, y);
-                    const uint32_t bad = quantized ? (bad_sh[n & 3] >> (16 * hf)) & 0x303u : 0u;      // two bits in each byte
-                    const bool edge = __any_sync(0xffffffffu, seen < 64 || bad != 0u);
+                    const bool edge = __any_sync(0xffffffffu, seen < 64 || (bad_sh[n & 3][2 * hf] | bad_sh[n & 3][2 * hf + 1]) != 0u);
                     tmem_wait_ld32(x);
                     tmem_wait_ld32(y);
                     if (edge) {
@@ -768,9 +765,7 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
                         for (int run = 0; run < 2; ++run) {
                             const int left = seen - 32 * run;      // which of its 32 columns the row sees, one bit each
                             uint32_t v = left >= 32 ? 0xFFFFFFFFu : (left <= 0 ? 0u : (1u << left) - 1u);
-                            const uint32_t two = (bad >> (8 * run)) & 3u;
-                            if (two & 1u) v &= 0xFFFF0000u;
-                            if (two & 2u) v &= 0x0000FFFFu;
+                            v &= ~bad_sh[n & 3][2 * hf + run];
                             tmem_ld32(h_addr + 32 * run, x);
                             tmem_wait_ld32(x);
                             uint32_t w[32];

@@ -139,3 +139,48 @@ def test_taking_back_more_than_the_ring_holds():
     p.check_attention([1])
     p.check_attention([40])
     p.check_read([40])
+
+
+# ------------------------------------------------------------------------------------------------ a window token without a page
+@pytest.mark.parametrize("kw", [dict(D=128, G=64), dict(D=64, G=32, H=1, Hq=4, dtype=BF16)])
+@pytest.mark.parametrize("entry", [-1, 2 ** 31 - 1])
+@pytest.mark.parametrize("appended", [True, False])
+def test_a_bad_page_under_the_window(kw, entry, appended):
+    """Tokens 64..79 lose their page, after they were appended or before (then their ring rows were never written): attention leaves
+    them out, read leaves their rows alone, both report them.  The window begins inside a page, its tiles straddle the bad one."""
+    p = base.Paged(n_seqs=1, W=41, P=16, seed=111, max_len=128, **kw)
+    good = p.page_table.clone()
+    if appended:
+        p.append([100])
+    p.page_table[0, 4] = entry
+    if not appended:
+        p.append([100])
+        assert int(p.cache.status[0]) == B.SKVQ_STATUS_BAD_PAGE
+        p.cache.status.zero_()
+    without = ref.Reference(1, p.Hq, p.H, p.D, kw["G"], 41 - 16, p.dtype, p.ref.rk, p.ref.rv, p.ref.ak, p.ref.av)
+    without.rows[0] = p.ref.rows[0][:64] + p.ref.rows[0][80:]
+    for new in (1, 3, 100):
+        for causal in (False, True):
+            p.cache.status.zero_()
+            q = torch.randn(new, p.Hq, p.D, generator=p.g).to(p.dtype)
+            lse = torch.empty(new, p.Hq, device="cuda")
+            out = p.cache.attention(p.batch([new], [100]), q.cuda(), 0.1, causal=causal, lse=lse)
+            assert int(p.cache.status[0]) == B.SKVQ_STATUS_BAD_PAGE
+            for i in {0, min(70, new - 1), new - 1}:
+                limit = 100 - new + i + 1 if causal else 100
+                kept = limit - max(0, min(limit, 80) - 64)      # of the tokens that are left
+                few = ref.Reference(1, p.Hq, p.H, p.D, kw["G"], max(0, kept - (84 - 25)), p.dtype, p.ref.rk, p.ref.rv, p.ref.ak, p.ref.av)
+                few.rows[0] = without.rows[0][:kept]
+                want, wl, err, el = few.attention(0, q[i:i + 1], 0.1, causal=False)
+                assert ((out.cpu().double()[i:i + 1] - want).abs() <= err).all()
+                assert ((lse.cpu().double()[i:i + 1] - wl).abs() <= el).all()
+    p.cache.status.zero_()
+    got, _ = p.cache.read(p.batch([100], [100]), torch.full((100, p.H, p.D), 9.0, dtype=p.dtype, device="cuda"))
+    assert int(p.cache.status[0]) == B.SKVQ_STATUS_BAD_PAGE
+    assert (got[64:80] == 9).all() and torch.isfinite(got.float()).all() and not (got[:64] == 9).all(-1).any() and not (got[80:] == 9).all(-1).any()
+    p.cache.status.zero_()
+    p.page_table.copy_(good)
+    if appended:
+        p.check_attention([1])
+        p.check_attention([100])
+        assert int(p.cache.status[0]) == 0
