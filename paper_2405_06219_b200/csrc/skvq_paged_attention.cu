@@ -358,13 +358,14 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 2 ? 2 : 3) paged_split_ke
             for (int r = r_first; r < ROWS; r += STEP) {
                 __half v = __float2half_rn(0.f), w = v;
                 float sum = 0.f, off_sum = 0.f, up = 1.f;
-                if (r < R && sign != 0.f) {
+                if (r < R) {
                     float mx = q_max[r][0];
 #pragma unroll
                     for (int k = 1; k < PARTS; ++k) mx = fmaxf(mx, q_max[r][k]);
                     // bring the row's largest to [2^13, 2^14): exact, whatever the range of the type
                     if (mx > 0.f && mx < CUDART_INF_F) up = __int_as_float((127 + min(13 - (__float_as_int(mx) >> 23) + 127, 60)) << 23);
-                    v = __float2half_rn(Elem<T>::to_float(raw[r * Geo::QROW + from]) * (up * sign));
+                    // an infinite query: infinities would leave scores of -infinity, which mean masked
+                    v = __float2half_rn(Elem<T>::to_float(raw[r * Geo::QROW + from]) * (mx < CUDART_INF_F ? up * sign : CUDART_NAN_F));
                     w = c & 1 ? __hmul(v, __float2half_rn(0.0625f)) : v;
                     sum = mmak::warp_sum(__half2float(v));
                     off_sum = mmak::warp_sum(__half2float(w));

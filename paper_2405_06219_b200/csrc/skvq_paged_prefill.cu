@@ -306,7 +306,7 @@ __global__ void __launch_bounds__(kQueryThreads) paged_queries_kernel(const __gr
         float up = 1.f;      // the row's largest to [2^4, 2^5): exact, and far from fp16's ends whatever the type's range
         if (mx > 0.f && mx < CUDART_INF_F) up = __int_as_float((127 + min(4 - (__float_as_int(mx) >> 23) + 127, 60)) << 23);
         if (!have) continue;
-        const float f = sign == 0.f ? 0.f : up * sign;
+        const float f = mx < CUDART_INF_F ? up * sign : CUDART_NAN_F;      // an infinite query: see the kernel for few rows
         const int64_t at = hk * all + tok * rep + (h - hk * rep);
         __half *dst = args.f.queries + at * D + c0;
         if constexpr (C == 8)

@@ -184,3 +184,38 @@ def test_a_bad_page_under_the_window(kw, entry, appended):
         p.check_attention([1])
         p.check_attention([100])
         assert int(p.cache.status[0]) == 0
+
+
+# ------------------------------------------------------------------------------------------------ queries that are not finite
+@pytest.mark.parametrize("length,window,new", [(40, 64, 1), (40, 64, 3), (40, 64, 40), (90, 0, 2), (90, 0, 60), (200, 32, 1), (200, 32, 100)])
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("scale", [0.1, -0.1, 0.0])
+@pytest.mark.parametrize("value", [math.inf, -math.inf, math.nan])
+def test_an_infinite_query_gives_its_row_nan(length, window, new, dtype, scale, value):
+    """Keys of one sign: the scores of an infinite query are all of one sign too, -infinity among them, which means masked elsewhere."""
+    p = base.Paged(n_seqs=1, W=window, P=64, seed=191, dtype=dtype)
+    k, v = p.keys(length)
+    k = k.abs() + 0.25
+    p.cache.append(p.batch([length], [length]), k.cuda(), v.cuda())
+    p.ref.append(0, k, v)
+    q = torch.randn(new, 4, 128, generator=p.g).to(dtype)
+    lse = [torch.empty(new, 4, device="cuda") for _ in range(2)]
+    good = p.cache.attention(p.batch([new], [length]), q.cuda(), scale, lse=lse[0])
+    assert torch.isfinite(good.float()).all()
+    q[new - 1, 2, 7] = value
+    out = p.cache.attention(p.batch([new], [length]), q.cuda(), scale, lse=lse[1])
+    spoilt = torch.zeros(new, 4, dtype=torch.bool, device="cuda")
+    spoilt[new - 1, 2] = True
+    assert torch.isnan(out[spoilt]).all() and torch.isnan(lse[1][spoilt]).all()
+    assert torch.equal(out[~spoilt], good[~spoilt]) and torch.equal(lse[1][~spoilt], lse[0][~spoilt])
+
+
+def test_an_infinite_query_that_sees_nothing_gives_zeros():
+    p = base.Paged(n_seqs=1, seed=192)
+    p.append([2])
+    for new in (5, 40):
+        q = torch.randn(new, 4, 128, generator=p.g).half()
+        q[0, 1, 3] = math.inf
+        lse = torch.empty(new, 4, device="cuda")
+        out = p.cache.attention(p.batch([new], [2]), q.cuda(), 0.1, lse=lse)
+        assert (out[0, 1] == 0).all() and float(lse[0, 1]) == -math.inf
