@@ -431,7 +431,7 @@ typedef struct skvq_paged_attn_args {
 
 /* Scratch bytes that skvq_paged_attention needs (depends on the host bounds in `batch`, not on the device arrays, and on the
  * GPU's SM count): partial results of (sequence, KV head) pairs that several CTAs share, and, where max_new * Hq/Hkv exceeds 16, the
- * rotated queries, T * Hq * (2 D + 4) bytes.  0 also on bad arguments.  Host only. */
+ * rotated queries, T * Hq * (2 D + 4) bytes.  0 also for a step without new tokens (n_tokens or max_new 0) and on bad arguments.  Host only. */
 size_t skvq_paged_workspace_size(const skvq_paged_config *cfg, const skvq_paged_batch *batch, int32_t n_splits);
 
 /*

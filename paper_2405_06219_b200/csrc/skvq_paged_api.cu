@@ -127,8 +127,8 @@ int skvq_paged_read(const skvq_paged_config *cfg, const skvq_paged_cache *cache,
 
 size_t skvq_paged_workspace_size(const skvq_paged_config *cfg, const skvq_paged_batch *batch, int32_t n_splits)
 {
-    if (check_paged_cfg(cfg) != SKVQ_OK || !batch || batch->n_seqs < 1 || batch->n_seqs > kMaxPagedSeqs || batch->max_new < 0 ||
-        batch->max_len < 0 || n_splits < 0)
+    if (check_paged_cfg(cfg) != SKVQ_OK || !batch || batch->n_seqs < 1 || batch->n_seqs > kMaxPagedSeqs || batch->max_new < 1 ||
+        batch->n_tokens < 1 || batch->max_len < 0 || n_splits < 0)
         return 0;
     return paged_workspace_bytes(*cfg, *batch, n_splits);
 }

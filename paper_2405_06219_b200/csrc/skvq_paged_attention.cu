@@ -819,6 +819,7 @@ struct SplitShape {
 SplitShape split_plan(const skvq_paged_config &cfg, const skvq_paged_batch &batch, int n_splits)
 {
     const long long items = item_count(cfg, batch), cost = item_cost(cfg, batch);
+    if (items == 0) return {1, 0};      // no new tokens: the entry points return before a launch
     if (n_splits == 0 && cost <= kWholeCost && items <= kMaxSlots) return {1, (int)items};
     // one wave of resident CTAs (a CTA more per SM spills: serving mix 597 us against 580), each with two tiles per warp at least: a shorter run
     // costs more to join than it saves

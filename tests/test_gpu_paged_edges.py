@@ -219,3 +219,21 @@ def test_an_infinite_query_that_sees_nothing_gives_zeros():
         lse = torch.empty(new, 4, device="cuda")
         out = p.cache.attention(p.batch([new], [2]), q.cuda(), 0.1, lse=lse)
         assert (out[0, 1] == 0).all() and float(lse[0, 1]) == -math.inf
+
+
+def test_a_step_without_new_tokens():
+    """A batch over long contexts in which nobody has a new token: nothing to do, in every call."""
+    p = base.Paged(n_seqs=2, W=16, P=64, seed=201, max_len=4096)
+    p.append([40, 3])
+    before = [getattr(p.cache, n).clone() for n in ("k_codes", "v_codes", "k_meta", "v_meta", "k_win", "v_win")]
+    none = torch.zeros(0, 2, 128, dtype=F16, device="cuda")
+    for max_len in (100, 4096):
+        b = p.batch([0, 0], p.lens(), max_len=max_len)
+        for n_splits in (0, 4):
+            assert p.cache.attention(b, torch.zeros(0, 4, 128, dtype=F16, device="cuda"), 0.1, n_splits=n_splits).shape == (0, 4, 128)
+        p.cache.append(b, none, none)
+        assert p.cache.read(b)[0].shape == (0, 2, 128)
+    torch.cuda.synchronize()
+    for x, n in zip(before, ("k_codes", "v_codes", "k_meta", "v_meta", "k_win", "v_win")):
+        assert torch.equal(x.view(torch.uint8), getattr(p.cache, n).view(torch.uint8)), n
+    assert int(p.cache.status[0]) == 0

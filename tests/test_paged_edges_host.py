@@ -1,5 +1,8 @@
 """Sizing and refusals of the paged and rotary calls at the ends of their ranges: host only, nothing is launched."""
 import ctypes
+import os
+import subprocess
+import sys
 
 import pytest
 
@@ -8,6 +11,7 @@ from paper_2405_06219_b200 import binding as B
 from paper_2405_06219_b200 import build
 
 FAKE = 0x1000
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 
 @pytest.fixture(scope="module")
@@ -36,3 +40,29 @@ def test_first_ring_tokens_are_checked(lib):
     before = B.skvq_launch_count()
     assert three_calls(lib, batch(ring_from=FAKE + 2)) == [B.SKVQ_ERR_MISALIGNED] * 3
     assert B.skvq_launch_count() == before
+
+
+def run(code):
+    return subprocess.run([sys.executable, "-c", "from paper_2405_06219_b200 import binding as B\n" + code], cwd=ROOT, capture_output=True, text=True)
+
+
+@pytest.mark.parametrize("kw", [dict(max_new=0, n_tokens=0), dict(max_new=0, n_tokens=7), dict(max_new=4, n_tokens=0)])
+def test_a_step_without_new_tokens_needs_no_workspace(lib, kw):
+    """In a process of its own: the sizing once divided by the number of items."""
+    code = """
+cfg = B.SkvqPagedConfig(32, 8, 128, 64, 128, 128, 64, 4000, 4, 0)
+for max_len in (0, 128, 4096, 200000):
+    for n_splits in (0, 1, 5):
+        assert B.skvq_paged_workspace_size(cfg, B.SkvqPagedBatch(n_seqs=1, max_pages=4000, max_len=max_len, **%r), n_splits) == 0
+""" % kw
+    r = run(code)
+    assert r.returncode == 0, (r.returncode, r.stderr)
+
+
+def test_sizing_refuses_what_the_calls_refuse(lib):
+    cfg = base.pcfg()
+    long = dict(max_pages=5000, max_len=300000)
+    assert B.skvq_paged_workspace_size(cfg, batch(**long)) > 0
+    for kw in (dict(max_new=-1), dict(n_tokens=-1), dict(max_len=-1), dict(n_seqs=0), dict(n_seqs=2049)):
+        assert B.skvq_paged_workspace_size(cfg, batch(**{**long, **kw})) == 0, kw
+    assert B.skvq_paged_workspace_size(cfg, batch(**long), -1) == 0
