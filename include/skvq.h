@@ -380,7 +380,7 @@ typedef struct skvq_paged_batch {
     int32_t max_pages;         /* row length of page_table */
     int32_t n_tokens;          /* T: rows that k, v, q and outputs have */
     int32_t max_new;           /* host upper bound on n_b; max_new * Hq/Hkv <= 2^30 */
-    int32_t max_len;           /* host upper bound on lens[], <= max_pages * P */
+    int32_t max_len;           /* host upper bound on lens[], <= max_pages * P and <= 2^30 */
     const int32_t *ring_from;  /* [n_seqs] or NULL: the slot's ring holds the sequence's tokens from ring_from[b] on -- the first
                                   token appended since the sequence has had this slot; older tokens of the window are read from
                                   their pages, quantized.  (After more than R - W tokens were taken back it is the longest length

@@ -8,6 +8,7 @@
 namespace skvq {
 
 constexpr int kMaxPagedSeqs = 2048;
+constexpr int kMaxPagedLen = 1 << 30;      // token numbers are ints, and kernels look some tiles past a sequence's end
 
 // Everything the paged kernels need, by value.
 struct PagedArgs {

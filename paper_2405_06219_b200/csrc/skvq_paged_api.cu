@@ -34,7 +34,7 @@ int check_batch(const skvq_paged_config *cfg, const skvq_paged_batch *b)
 {
     if (!b || !b->page_table || !b->lens || !b->starts) return SKVQ_ERR_INVALID_ARG;
     if (b->n_seqs < 1 || b->max_pages < 1 || b->n_tokens < 0 || b->max_new < 0 || b->max_len < 0) return SKVQ_ERR_INVALID_ARG;
-    if (b->n_seqs > kMaxPagedSeqs) return SKVQ_ERR_UNSUPPORTED;
+    if (b->n_seqs > kMaxPagedSeqs || b->max_len > kMaxPagedLen) return SKVQ_ERR_UNSUPPORTED;
     if ((int64_t)b->max_new * (cfg->n_q_heads / cfg->n_kv_heads) > (1 << 30)) return SKVQ_ERR_UNSUPPORTED;      // packed rows of a KV head
     if (b->max_len > (int64_t)b->max_pages * cfg->page_tokens) return SKVQ_ERR_CAPACITY;
     if (off(b->page_table, 4) || off(b->lens, 4) || off(b->starts, 4) || off(b->slots, 4) || off(b->ring_from, 4)) return SKVQ_ERR_MISALIGNED;
@@ -128,7 +128,7 @@ int skvq_paged_read(const skvq_paged_config *cfg, const skvq_paged_cache *cache,
 size_t skvq_paged_workspace_size(const skvq_paged_config *cfg, const skvq_paged_batch *batch, int32_t n_splits)
 {
     if (check_paged_cfg(cfg) != SKVQ_OK || !batch || batch->n_seqs < 1 || batch->n_seqs > kMaxPagedSeqs || batch->max_new < 1 ||
-        batch->n_tokens < 1 || batch->max_len < 0 || n_splits < 0)
+        batch->n_tokens < 1 || batch->max_len < 0 || batch->max_len > kMaxPagedLen || n_splits < 0)
         return 0;
     return paged_workspace_bytes(*cfg, *batch, n_splits);
 }

@@ -66,3 +66,15 @@ def test_sizing_refuses_what_the_calls_refuse(lib):
     for kw in (dict(max_new=-1), dict(n_tokens=-1), dict(max_len=-1), dict(n_seqs=0), dict(n_seqs=2049)):
         assert B.skvq_paged_workspace_size(cfg, batch(**{**long, **kw})) == 0, kw
     assert B.skvq_paged_workspace_size(cfg, batch(**long), -1) == 0
+
+
+def test_lengths_whose_token_numbers_would_pass_32_bits_are_refused(lib):
+    """Kernels look some 64 blocks of 16 tokens past the length: near 2^31 those numbers would wrap."""
+    before = B.skvq_launch_count()
+    most = 1 << 30
+    for max_len in (most + 1, 2 ** 31 - 1):
+        b = batch(max_len=max_len, max_pages=2 ** 31 // 64)
+        assert three_calls(lib, b) == [B.SKVQ_ERR_UNSUPPORTED] * 3
+        assert B.skvq_paged_workspace_size(base.pcfg(), b) == 0
+    assert B.skvq_paged_workspace_size(base.pcfg(), batch(max_len=most, max_pages=most // 64)) > 0
+    assert B.skvq_launch_count() == before
