@@ -192,7 +192,7 @@ int skvq_rope_table(const double *frequencies_host, int32_t n_freq, double ampli
                     int32_t n_positions, void *table, void *cuda_stream)
 {
     if (!frequencies_host || n_freq < 1 || n_positions < 0 || first_position < 0 || !std::isfinite(amplitude)) return SKVQ_ERR_INVALID_ARG;
-    if (n_freq > kMaxFreq || first_position + n_positions > 0x7fffffffLL) return SKVQ_ERR_UNSUPPORTED;
+    if (n_freq > kMaxFreq || first_position > 0x7fffffffLL - n_positions) return SKVQ_ERR_UNSUPPORTED;
     if (n_positions == 0) return SKVQ_OK;
     if (!table) return SKVQ_ERR_INVALID_ARG;
     if (!plain_pointer(table, 8)) return SKVQ_ERR_MISALIGNED;

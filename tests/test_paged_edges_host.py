@@ -78,3 +78,11 @@ def test_lengths_whose_token_numbers_would_pass_32_bits_are_refused(lib):
         assert B.skvq_paged_workspace_size(base.pcfg(), b) == 0
     assert B.skvq_paged_workspace_size(base.pcfg(), batch(max_len=most, max_pages=most // 64)) > 0
     assert B.skvq_launch_count() == before
+
+
+def test_a_table_that_begins_beyond_64_bits_is_refused(lib):
+    f = (ctypes.c_double * 4)(*[0.5] * 4)
+    before = B.skvq_launch_count()
+    for first, n in ((2 ** 63 - 1, 1), (2 ** 63 - 10, 100), (2 ** 31 - 1, 1), (2 ** 31 - 5, 5)):
+        assert lib.skvq_rope_table(f, 4, 1.0, first, n, FAKE, None) == B.SKVQ_ERR_UNSUPPORTED, (first, n)
+    assert B.skvq_launch_count() == before
