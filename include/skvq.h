@@ -308,7 +308,8 @@ typedef struct skvq_rope {
 } skvq_rope;
 
 /* One operand of skvq_rope_apply (host struct).  Strides are in elements, between tokens and between heads; the channels of
- * a head are contiguous.  y may be x itself (same pointer and strides); other overlaps are not allowed. */
+ * a head are contiguous.  x may be broadcast (a stride of 0); rows of y that share elements are refused.  y may be x itself (same
+ * pointer and strides); other overlaps are not allowed. */
 typedef struct skvq_rope_tensor {
     const void *x;
     void *y;

@@ -152,6 +152,21 @@ cudaError_t launch_rope(RopeArgs a, bool interleaved, cudaStream_t stream)
     return cudaGetLastError();
 }
 
+// Rows t * ts + h * hs (dim elements each) that share an element would be written by several threads, in an order that nobody knows.
+bool rows_overlap(int n_tokens, int n_heads, int64_t ts, int64_t hs, int dim)
+{
+    using Wide = __int128;
+    const Wide t = ts < 0 ? -(Wide)ts : ts, h = hs < 0 ? -(Wide)hs : hs;
+    if ((n_tokens > 1 && t < dim) || (n_heads > 1 && h < dim)) return true;
+    if (n_tokens == 1 || n_heads == 1 || t >= (n_heads - 1) * h + dim || h >= (n_tokens - 1) * t + dim) return false;
+    for (int dh = 1; dh < n_heads; ++dh) {      // neither lies within the other: the tokens nearest to dh heads away
+        const Wide near = dh * h / t;
+        for (Wide dt = near; dt <= near + 1; ++dt)
+            if (dt < n_tokens && (dh * h > dt * t ? dh * h - dt * t : dt * t - dh * h) < dim) return true;
+    }
+    return false;
+}
+
 bool plain_pointer(const void *p, int elt) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(elt - 1)) == 0; }
 
 }  // namespace
@@ -235,6 +250,12 @@ int skvq_rope_apply(const skvq_rope *rope, int32_t dtype, int32_t head_dim, cons
         if (t[i]->n_heads > 65535) return SKVQ_ERR_UNSUPPORTED;
         if (t[i]->n_heads > 0 && n_tokens > 0 && (!t[i]->x || !t[i]->y)) return SKVQ_ERR_INVALID_ARG;
         if (!plain_pointer(t[i]->x, elt) || !plain_pointer(t[i]->y, elt)) return SKVQ_ERR_MISALIGNED;
+        if (n_tokens > 0 && t[i]->n_heads > 0) {
+            if (rows_overlap(n_tokens, t[i]->n_heads, t[i]->y_token_stride, t[i]->y_head_stride, head_dim)) return SKVQ_ERR_INVALID_ARG;
+            if (t[i]->x == t[i]->y && ((n_tokens > 1 && t[i]->x_token_stride != t[i]->y_token_stride) ||
+                                       (t[i]->n_heads > 1 && t[i]->x_head_stride != t[i]->y_head_stride)))
+                return SKVQ_ERR_INVALID_ARG;
+        }
         a.op[i] = RopeOperand{t[i]->x, t[i]->y, t[i]->x_token_stride, t[i]->x_head_stride, t[i]->y_token_stride, t[i]->y_head_stride, t[i]->n_heads};
         a.heads += t[i]->n_heads;
         wide = wide && plain_pointer(t[i]->x, 16) && plain_pointer(t[i]->y, 16) &&

@@ -237,3 +237,29 @@ def test_a_step_without_new_tokens():
     for x, n in zip(before, ("k_codes", "v_codes", "k_meta", "v_meta", "k_win", "v_win")):
         assert torch.equal(x.view(torch.uint8), getattr(p.cache, n).view(torch.uint8)), n
     assert int(p.cache.status[0]) == 0
+
+
+# ------------------------------------------------------------------------------------------------ rotation of broadcast and strided rows
+@pytest.mark.parametrize("inter", [False, True])
+def test_rotation_of_a_broadcast_input_and_of_odd_layouts(inter):
+    """One head or one token broadcast to many; outputs head by head, backwards, and with rows that interleave without touching."""
+    T, H, D, rot = 3, 3, 8, 8
+    g = torch.Generator().manual_seed(7)
+    cs = ref.table64(rot, 50).float()
+    rope = B.RopeTable(cs.cuda(), rot, inter)
+    pos = torch.tensor([4, 49, 0], dtype=torch.int32)
+    for x in (torch.randn(T, 1, D, generator=g).expand(T, H, D), torch.randn(1, H, D, generator=g).expand(T, H, D), torch.randn(T, H, D, generator=g)):
+        want = ref.rotate32(x.contiguous(), cs[pos.long()], rot, inter)
+        src = x[:, :1].cuda().expand(T, H, D) if x.stride(1) == 0 else x[:1].cuda().expand(T, H, D) if x.stride(0) == 0 else x.cuda()
+        assert src.stride() == x.stride()
+        for strides in ((H * D, D, 1), (D, T * D, 1), (16, 24, 1), (40, 16, 1)):
+            pool = torch.full((200,), 5.0, device="cuda")
+            out = pool.as_strided((T, H, D), strides, 3)
+            rope.apply(pos.cuda(), src, out)
+            assert torch.equal(base.bits(out.cpu()), base.bits(want)), strides
+            written = torch.zeros(200, dtype=torch.bool)
+            written.as_strided((T, H, D), strides, 3).fill_(True)
+            assert (pool.cpu()[~written] == 5).all(), strides
+    with pytest.raises(B.SkvqError) as e:
+        rope.apply(pos.cuda(), torch.zeros(T, 1, D, device="cuda").expand(T, H, D))
+    assert e.value.code == B.SKVQ_ERR_INVALID_ARG

@@ -86,3 +86,29 @@ def test_a_table_that_begins_beyond_64_bits_is_refused(lib):
     for first, n in ((2 ** 63 - 1, 1), (2 ** 63 - 10, 100), (2 ** 31 - 1, 1), (2 ** 31 - 5, 5)):
         assert lib.skvq_rope_table(f, 4, 1.0, first, n, FAKE, None) == B.SKVQ_ERR_UNSUPPORTED, (first, n)
     assert B.skvq_launch_count() == before
+
+
+def test_outputs_whose_rows_overlap_are_refused(lib):
+    """Heads or tokens that share a row of y: broadcast outputs, and tensors rotated in place through other strides than x's."""
+    before = B.skvq_launch_count()
+
+    def call(x, y, xs, ys, heads=8, T=4, D=128):
+        rope = B.SkvqRope(FAKE, 64, 0, 8)
+        a = B.SkvqRopeTensor(x, y, *xs, *ys, heads)
+        ok = B.SkvqRopeTensor(FAKE, FAKE + (1 << 20), 1024, 128, 1024, 128, 8)
+        return [lib.skvq_rope_apply(ctypes.byref(rope), B.SKVQ_F16, D, ctypes.byref(p), ctypes.byref(q), FAKE, T, 0, None, None) for p, q in ((a, ok), (ok, a))]
+
+    bad = [B.SKVQ_ERR_INVALID_ARG] * 2
+    far = FAKE + (1 << 24)
+    assert call(FAKE, far, (1024, 128), (1024, 0)) == bad             # every head into one row
+    assert call(FAKE, far, (1024, 128), (0, 128)) == bad              # every token into one row
+    assert call(FAKE, far, (1024, 128), (1024, 64)) == bad            # heads that reach into each other
+    assert call(FAKE, far, (1024, 128), (1024, -64)) == bad
+    assert call(FAKE, far, (1024, 128), (127, 128), heads=1) == bad
+    assert call(FAKE, far, (1024, 128), (128, 128)) == bad            # a token's second head is the next token's first
+    assert call(FAKE, far, (1024, 128), (-384, 128)) == bad
+    assert call(FAKE, far, (1024, 128), (2 ** 62, 2 ** 62 + 64)) == bad
+    assert call(FAKE, FAKE, (1024, 0), (1024, 0)) == bad              # a broadcast input in place
+    assert call(FAKE, FAKE, (1024, 128), (1024, 256)) == bad          # in place, other strides
+    assert call(FAKE, FAKE, (1024, 128), (2048, 128)) == bad
+    assert B.skvq_launch_count() == before
