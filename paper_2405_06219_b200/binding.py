@@ -444,6 +444,7 @@ class RopeTable:
         T, _, D = q.shape
         index, dtype = self.index, q.dtype
         assert positions.dtype == torch.int32 and positions.is_contiguous() and positions.numel() == T and positions.get_device() == index
+        assert status is None or (status.dtype == torch.int32 and status.numel() >= 1 and status.get_device() == index), "status: int32 on the table's device"
         a = _rope_operand(q, q if q_out is None else q_out, dtype, T, D, index)
         b = None if k is None else _rope_operand(k, k if k_out is None else k_out, dtype, T, D, index)
         with _on(index):
@@ -501,6 +502,7 @@ class SkvqPagedCache:
         b = SkvqPagedBatch(page_table.data_ptr(), lens.data_ptr(), starts.data_ptr(), _dptr(slots), n, page_table.shape[1],
                            n_tokens, max_new, max_len, _dptr(ring_from))
         b.keep = (page_table, lens, starts, slots, ring_from)
+        b.index = self.index
         return b
 
     def _rows(self, x, batch, heads) -> int:
@@ -511,17 +513,26 @@ class SkvqPagedCache:
         assert shape[1] == heads and shape[2] == D and stride[2] == 1 and (heads == 1 or stride[1] == D), "rows: heads and channels contiguous"
         return stride[0] if shape[0] > 1 else heads * D
 
+    def _operands(self, batch, rope=None):
+        """Batch and rotation have to lie on the cache's device; the rotation's struct."""
+        assert getattr(batch, "index", self.index) == self.index, "a batch on the cache's device"
+        if rope is None:
+            return None
+        assert rope.index == self.index, "a rotation on the cache's device"
+        return _ref(rope.struct)
+
     def append(self, batch, k, v, rope=None, stream=None) -> None:
         """k, v: [T, Hkv, D] in the cache's type, any token stride that is a multiple of 8."""
-        H, index = self.cfg.n_kv_heads, self.index
+        H, index, rotation = self.cfg.n_kv_heads, self.index, self._operands(batch, rope)
         ks, vs = self._rows(k, batch, H), self._rows(v, batch, H)
         with _on(index):
-            _check(lib().skvq_paged_append(_ref(self.cfg), _ref(self.struct), _ref(batch), None if rope is None else _ref(rope.struct), k.data_ptr(),
+            _check(lib().skvq_paged_append(_ref(self.cfg), _ref(self.struct), _ref(batch), rotation, k.data_ptr(),
                                            v.data_ptr(), ks, vs, _raw_stream(index, stream)), "skvq_paged_append")
 
     def read(self, batch, k=None, v=None, window: bool = True, stream=None):
         """The new tokens' rows of the cache as values [T, Hkv, D], in source order; into k and v where they are given."""
         H, index = self.cfg.n_kv_heads, self.index
+        self._operands(batch)
         with _on(index), (_HERE if stream is None else torch.cuda.stream(stream)):
             if k is None and v is None:
                 k, v = torch.empty((2, batch.n_tokens, H, self.cfg.head_dim), dtype=self.dtype, device=self.device).unbind(0)
@@ -538,7 +549,7 @@ class SkvqPagedCache:
         """q [T, Hq, D] -> out [T, Hq, D]; lse: optional float32 [T, Hq].  Without a workspace (a tensor of at least
         skvq_paged_workspace_size bytes) each call takes one of its own from torch's allocator on the stream it runs on, so calls
         on several streams and captured graphs never share it."""
-        c, index = self.cfg, self.index
+        c, index, rotation = self.cfg, self.index, self._operands(batch, rope)
         H = c.n_q_heads
         qs = self._rows(q, batch, H)
         with _on(index), (_HERE if stream is None else torch.cuda.stream(stream)):
@@ -554,6 +565,6 @@ class SkvqPagedCache:
                 size = workspace.numel() * workspace.element_size()
             assert lse is None or (lse.dtype == torch.float32 and lse.is_contiguous() and lse.get_device() == index and lse.numel() >= batch.n_tokens * H)
             args = SkvqPagedAttnArgs(sm_scale, 1 if causal else 0, n_splits, _dptr(workspace), size)
-            _check(lib().skvq_paged_attention(_ref(c), _ref(self.struct), _ref(batch), None if rope is None else _ref(rope.struct), q.data_ptr(), qs,
+            _check(lib().skvq_paged_attention(_ref(c), _ref(self.struct), _ref(batch), rotation, q.data_ptr(), qs,
                                               out.data_ptr(), os_, _dptr(lse), _ref(args), _raw_stream(index, stream)), "skvq_paged_attention")
         return out

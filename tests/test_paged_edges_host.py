@@ -5,6 +5,7 @@ import subprocess
 import sys
 
 import pytest
+import torch
 
 import test_rope_paged_host as base
 from paper_2405_06219_b200 import binding as B
@@ -112,3 +113,69 @@ def test_outputs_whose_rows_overlap_are_refused(lib):
     assert call(FAKE, FAKE, (1024, 128), (1024, 256)) == bad          # in place, other strides
     assert call(FAKE, FAKE, (1024, 128), (2048, 128)) == bad
     assert B.skvq_launch_count() == before
+
+
+# ------------------------------------------------------------------------------------------------ tensors of another GPU, in the binding
+class OnGpu:
+    """What the binding asks of a tensor, on a GPU that need not exist."""
+
+    def __init__(self, index, shape, dtype):
+        self.index, self.shape, self.dtype = index, shape, dtype
+
+    def get_device(self):
+        return self.index
+
+    def stride(self):
+        out = [1]
+        for n in self.shape[:0:-1]:
+            out.insert(0, out[0] * n)
+        return tuple(out)
+
+    def data_ptr(self):
+        return FAKE
+
+    def is_contiguous(self):
+        return True
+
+    def numel(self):
+        n = 1
+        for m in self.shape:
+            n *= m
+        return n
+
+
+def fake_cache(index):
+    c = B.SkvqPagedCache.__new__(B.SkvqPagedCache)
+    c.cfg, c.struct, c.dtype, c.index, c.device = base.pcfg(), B.SkvqPagedCacheStruct(), torch.float16, index, torch.device("cuda", index)
+    return c
+
+
+def fake_rope(index):
+    r = B.RopeTable.__new__(B.RopeTable)
+    r.struct, r.rot_dim, r.interleaved, r.index = B.SkvqRope(FAKE, 64, 0, 8), 64, False, index
+    return r
+
+
+def test_a_rotation_of_another_gpu_is_refused():
+    c = fake_cache(1)
+    k, q = OnGpu(1, (7, 2, 128), torch.float16), OnGpu(1, (7, 8, 128), torch.float16)
+    for call in (lambda rope: c.append(batch(), k, k, rope=rope),
+                 lambda rope: c.attention(batch(), q, 0.1, out=q, rope=rope)):
+        with pytest.raises(AssertionError, match="rotation"):
+            call(fake_rope(0))
+
+
+def test_a_batch_of_another_gpu_is_refused():
+    c, b = fake_cache(1), batch()
+    b.index = 0
+    k, q = OnGpu(1, (7, 2, 128), torch.float16), OnGpu(1, (7, 8, 128), torch.float16)
+    for call in (lambda: c.append(b, k, k), lambda: c.read(b, k, k), lambda: c.attention(b, q, 0.1, out=q)):
+        with pytest.raises(AssertionError, match="batch"):
+            call()
+
+
+@pytest.mark.parametrize("status", [OnGpu(1, (1,), torch.int32), OnGpu(0, (1,), torch.int64), OnGpu(0, (0,), torch.int32)])
+def test_a_status_word_that_is_none_is_refused(status):
+    pos, x = OnGpu(0, (7,), torch.int32), OnGpu(0, (7, 2, 128), torch.float16)
+    with pytest.raises(AssertionError, match="status"):
+        fake_rope(0).apply(pos, x, status=status)
