@@ -49,7 +49,8 @@ extern "C" {
 
 #define SKVQ_STATUS_OVERFLOW 1    /* bit set in *status when a sequence would have exceeded max_tokens */
 #define SKVQ_STATUS_COPY_TIMEOUT 2 /* bit set when a shared-memory copy inside decode attention never completed (bounded
-                                     wait ran out); the affected tokens contribute nothing to the result */
+                                     wait ran out); the affected tokens contribute nothing to the result;
+                                     skvq_paged_attention: the affected rows are NaN */
 #define SKVQ_STATUS_BOUNDS 4       /* only from a library built with -DSKVQ_CHECKED (a debugging build): a kernel was about to
                                      use a row, slot or partial index outside its buffer; the access was skipped */
 
@@ -445,6 +446,7 @@ size_t skvq_paged_workspace_size(const skvq_paged_config *cfg, const skvq_paged_
  * A row that sees no token (n_b > L_b, or L_b = 0) gives zeros and a log-sum-exp of -infinity.
  *   q, out           dtype [T][Hq][D], token strides in elements (multiples of 8, >= Hq*D)
  *   lse              float [T][Hq], natural logarithm of the softmax denominator of every row, or NULL
+ * Waits inside are bounded: one that runs out (it never should) sets SKVQ_STATUS_COPY_TIMEOUT, and the rows that it concerns are NaN.
  * Skipped sequences (as for skvq_paged_append, except that n_b may exceed L_b): their rows are left alone.  Tokens behind a bad
  * page-table entry, those of the window too, are left out of the softmax and SKVQ_STATUS_BAD_PAGE is set.  Rows of the cache at or beyond L_b are never
  * used, whatever they hold.  A query that is not finite gives its own row NaN and no other.  Keys and values have to be finite and

@@ -348,9 +348,10 @@ __device__ __noinline__ void load_queries(const PrefillArgs &args, const PSegmen
     }
 }
 
-// The result of a row block: finished rows, or (a share of an item) sums that the merge kernel joins.
+// The result of a row block: finished rows, or (a share of an item) sums that the merge kernel joins.  `failed`: a wait ran out, what the
+// block holds is worth nothing; its rows become NaN, and so does what a share is joined with.
 template <typename T, int D>
-__device__ __noinline__ void write_rows(const PagedAttnArgs &args, const PSegment &s, int rows, int row_base, bool work, uint32_t o_addr, float ref, float l,
+__device__ __noinline__ void write_rows(const PagedAttnArgs &args, const PSegment &s, int rows, int row_base, bool work, bool failed, uint32_t o_addr, float ref, float l,
                                         float rs, uint8_t *q_tile, const uint16_t *out_channel, bool whole, float *part)
 {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, row = threadIdx.x & (kBlock - 1);
@@ -361,7 +362,9 @@ __device__ __noinline__ void write_rows(const PagedAttnArgs &args, const PSegmen
     const int n_q_heads = args.p.cfg.n_q_heads;
     const int rep = s.it.rep, hk = s.hk, row0 = s.seq.row0;
     const int i = (row_base + row) / rep, head = hk * rep + (row_base + row) - i * rep;
+    if (failed) work = false;
     const bool none = !work || (ref == -CUDART_INF_F && l == l);      // no token seen; a query that is not a number leaves its mark in l
+    const float blank = failed ? CUDART_NAN_F : 0.f;
     if (whole) {
         const float inv = 1.f / l;
         T *rows_out = reinterpret_cast<T *>(q_tile);      // [128][D], 16-byte pieces of a row at piece ^ (row & 7); all products have been read
@@ -375,11 +378,11 @@ __device__ __noinline__ void write_rows(const PagedAttnArgs &args, const PSegmen
 #pragma unroll
             for (int c = 0; c < 16; ++c) {
                 const int dst = work ? out_channel[c0 + c] : c0 + c;
-                rows_out[row * D + ((((dst >> 3) ^ (row & 7))) << 3) + (dst & 7)] = Elem<T>::from_float(none ? 0.f : x[c] * inv);
+                rows_out[row * D + ((((dst >> 3) ^ (row & 7))) << 3) + (dst & 7)] = Elem<T>::from_float(none ? blank : x[c] * inv);
             }
         }
         if (lse && row < rows)
-            lse[(int64_t)(row0 + i) * n_q_heads + head] = none ? -CUDART_INF_F : (ref * rs + log2f(l) - kPOffset) * 0.6931471805599453f;
+            lse[(int64_t)(row0 + i) * n_q_heads + head] = failed ? blank : none ? -CUDART_INF_F : (ref * rs + log2f(l) - kPOffset) * 0.6931471805599453f;
         __syncwarp();
         constexpr int PER_ROW = D / 8;
         for (int e = lane; e < 32 * PER_ROW; e += 32) {      // this warp's 32 rows, 16 bytes a lane
@@ -404,16 +407,16 @@ __device__ __noinline__ void write_rows(const PagedAttnArgs &args, const PSegmen
             if (row < rows) {
 #pragma unroll
                 for (int c = 0; c < 16; c += 8) {
-                    *reinterpret_cast<float4 *>(part + c0 + c) = none ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(x[c], x[c + 2], x[c + 4], x[c + 6]);
-                    *reinterpret_cast<float4 *>(part + c0 + c + 4) = none ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(x[c + 1], x[c + 3], x[c + 5], x[c + 7]);
+                    *reinterpret_cast<float4 *>(part + c0 + c) = none ? make_float4(blank, blank, blank, blank) : make_float4(x[c], x[c + 2], x[c + 4], x[c + 6]);
+                    *reinterpret_cast<float4 *>(part + c0 + c + 4) = none ? make_float4(blank, blank, blank, blank) : make_float4(x[c + 1], x[c + 3], x[c + 5], x[c + 7]);
                 }
             }
         }
         if (row < rows) {
-            part[D] = ref == -CUDART_INF_F ? ref : ref * rs;
-            part[D + 1] = none ? 0.f : l;
+            part[D] = failed || ref == -CUDART_INF_F ? -CUDART_INF_F : ref * rs;
+            part[D + 1] = none ? blank : l;
         }
-                }
+    }
 }
 
 template <typename T, int D, int NG>
@@ -426,7 +429,7 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     long long *pre = reinterpret_cast<long long *>(smem + Geo::SMEM - 1024);
-    __shared__ __align__(8) uint64_t bars[22];
+    __shared__ __align__(8) uint64_t bars[24];
     __shared__ uint32_t tmem_sh;
     __shared__ int fail_sh;
     __shared__ long long scan_sh[16];
@@ -479,7 +482,7 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
     const uint32_t bar0 = smem_u32(bars);
     const uint32_t k_full = bar0, k_empty = bar0 + 16, v_full = bar0 + 32, v_empty = bar0 + 48;      // + 8 * buffer
     const uint32_t s_full = bar0 + 64, pv_done = bar0 + 96;                                          // + 16 * row block + 8 * half
-    const uint32_t p_full = bar0 + 128, q_full = bar0 + 160;                                        // the same; + 8 * row block
+    const uint32_t p_full = bar0 + 128, q_full = bar0 + 160, drained = bar0 + 176;                  // the same; + 8 * row block
     if (tid == 0) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
@@ -494,6 +497,7 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
             mbar_init(p_full + 16 * i, 4);      // an arrival per warp
             mbar_init(p_full + 16 * i + 8, 4);
             mbar_init(q_full + 8 * i, 4);
+            mbar_init(drained + 8 * i, 1);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fail_sh = 0;
@@ -521,7 +525,8 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
     }
     if (tid == 0) desc[0] = 0;
     __syncthreads();
-    // A wait that runs out is reported; the thread then goes through its loops without waiting or storing.
+    // A wait that runs out is reported; the thread then goes through its loops without waiting.  The flag is set before anything that
+    // follows from it, so that a row block that has read spoilt operands finds it set when it comes to write its rows.
     bool alive = true;
     volatile int *fail = &fail_sh;
     auto wait = [&](uint32_t bar, uint32_t parity) {      // by whole warps
@@ -717,6 +722,10 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
                 }
             }
         }
+        if (__any_sync(0xffffffffu, *fail != 0)) {      // nobody may have waited for the last products: they must not outlive the CTA
+            if (elect_one()) umma_commit(drained + 8 * blk);
+            mbar_wait_cycles(drained + 8 * blk, 0);
+        }
         }
     } else {
         // ================================================================ softmax
@@ -855,10 +864,10 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
                 wait(pv_done + 16 * blk + 8, (ns - 1) & 1);
                 tc_fence_after();
             }
-            if (alive)
-                write_rows<T, D>(a, s, rows, row_base, work, o_addr, ref, l, rs, q_tile, out_channel[blk], whole,
-                                 a.ws + (size_t)args.n_slots * kDescInts + (((size_t)blockIdx.x * 2 + (s.t0 == 0 ? 1 : 0)) * 2 * kBlock + blk * kBlock) * partial_stride(D));
-            if (alive && !whole && s.t0 == 0 && tid == 0) {
+            alive = __all_sync(0xffffffffu, alive && !*fail);
+            write_rows<T, D>(a, s, rows, row_base, work, !alive, o_addr, ref, l, rs, q_tile, out_channel[blk], whole,
+                             a.ws + (size_t)args.n_slots * kDescInts + (((size_t)blockIdx.x * 2 + (s.t0 == 0 ? 1 : 0)) * 2 * kBlock + blk * kBlock) * partial_stride(D));
+            if (!whole && s.t0 == 0 && tid == 0) {
                 desc[1] = s.seq.row0; desc[2] = s.seq.n; desc[3] = s.hk; desc[4] = s.m;
                 desc[5] = s.parts;
                 desc[0] = 1;
