@@ -406,7 +406,8 @@ int skvq_paged_cache_sizes(const skvq_paged_config *cfg, size_t bytes_out[6]);
  * A sequence is skipped and SKVQ_STATUS_BAD_BATCH set when its starts are not 0 <= starts[b] <= starts[b+1] <= T, n_b exceeds
  * max_new or L_b, L_b exceeds max_len or the table's rows, or its slot is not in [0, n_slots); a token whose page-table entry is
  * not in [0, n_pages) is skipped and sets SKVQ_STATUS_BAD_PAGE.  Two tokens of one call must not share a page row, two sequences
- * with new tokens no slot.  Magnitudes beyond the fp16 range (and NaN) give unspecified rows: the parameters are fp16.
+ * with new tokens no slot.  Magnitudes above 65440 (and NaN) give unspecified rows: the parameters are
+ * fp16, and the highest code's value can lie a rounding of 15 steps above the group's maximum, where fp16 ends.
  * Repeating a call with the same arguments gives the same cache.
  */
 int skvq_paged_append(const skvq_paged_config *cfg, const skvq_paged_cache *cache, const skvq_paged_batch *batch,
@@ -440,6 +441,9 @@ size_t skvq_paged_workspace_size(const skvq_paged_config *cfg, const skvq_paged_
  * Attention of the new tokens' queries over the cache (append first: the cache then holds them):
  *   q' = rope(q) rounded to dtype (rope != NULL),  s_t = sm_scale sum_j q'_j K~[t][j],  p = softmax over the tokens the row sees,
  *   out_j = sum_t p_t V~[t][j]
+ * The window is the sequence's: all rows of a call read the same W newest tokens of L_b unquantized, and what lies before those
+ * quantized, even where a row's own W newest tokens reach further back.  So rows of a chunk, or of several drafted tokens, differ
+ * by the quantization of those tokens from what single-token steps give.
  * K~, V~ as skvq_paged_read(window = 1) defines them, before its rounding to dtype; as operands of the tensor core they are rounded to
  * fp16 once (with at most 16 rows, n_b * Hq/Hkv, per KV head only V~ is), and so are the probabilities.  Scores, softmax statistics
  * and sums are fp32.
@@ -449,8 +453,8 @@ size_t skvq_paged_workspace_size(const skvq_paged_config *cfg, const skvq_paged_
  * Waits inside are bounded: one that runs out (it never should) sets SKVQ_STATUS_COPY_TIMEOUT, and the rows that it concerns are NaN.
  * Skipped sequences (as for skvq_paged_append, except that n_b may exceed L_b): their rows are left alone.  Tokens behind a bad
  * page-table entry, those of the window too, are left out of the softmax and SKVQ_STATUS_BAD_PAGE is set.  Rows of the cache at or beyond L_b are never
- * used, whatever they hold.  A query that is not finite gives its own row NaN and no other.  Keys and values have to be finite and
- * in fp16's range (as for skvq_paged_append): one that is not can reach every row of its sequence, those that do not see it too.
+ * used, whatever they hold.  A query that is not finite gives its own row NaN and no other.  Keys and values have to be finite,
+ * at most 65440 (as for skvq_paged_append): one that is not can reach every row of its sequence, those that do not see it too.
  * The workspace is overwritten; calls sharing one must be stream-ordered.  out and lse must not overlap the inputs.
  */
 int skvq_paged_attention(const skvq_paged_config *cfg, const skvq_paged_cache *cache, const skvq_paged_batch *batch,

@@ -263,3 +263,18 @@ def test_rotation_of_a_broadcast_input_and_of_odd_layouts(inter):
     with pytest.raises(B.SkvqError) as e:
         rope.apply(pos.cuda(), torch.zeros(T, 1, D, device="cuda").expand(T, H, D))
     assert e.value.code == B.SKVQ_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("new", [1, 3, 60])
+def test_the_largest_magnitudes(new):
+    """Groups that span +-65440: every value of theirs, and of the operands, still is a finite fp16."""
+    p = base.Paged(n_seqs=1, W=16, P=64, seed=231, reorder=False, outliers=False)
+    k, v = p.keys(120)
+    for x in (k, v):
+        x[:, :, 3::32], x[:, :, 5::32] = 65440.0, -65440.0
+    p.cache.append(p.batch([120], [120]), k.cuda(), v.cuda())
+    p.ref.append(0, k, v)
+    p.check_rows()
+    ko, vo = p.cache.read(p.batch([120], [120]), window=False)
+    assert torch.isfinite(ko.float()).all() and torch.isfinite(vo.float()).all()
+    p.check_attention([new], sm_scale=1e-7)
