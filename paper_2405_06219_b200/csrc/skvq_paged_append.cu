@@ -5,9 +5,10 @@
 // angles stay in registers.  The rows are read coalesced and put into shared memory interleaved, a 32-bit word holding one channel
 // of both tokens: partner channels of the rotation, and the gather in stored order, then take one shared-memory access for
 // two rows, the arithmetic is on pairs of fp32, and minimum and maximum are one packed instruction for both.  A group's extremes are reduced by
-// shuffles.  Measured: a 32k-token prompt of 32 heads, rotated, appended and read back 506 us (538 with an instruction per row and value).
-// What bounds it is instructions, not bytes (68 % of the issue slots at a quarter of the DRAM rate; a row at a time: 420 us for the append of a 32k-token prompt of 32 heads, 267 for reading it back,
-// floors of 105 each), so the code is formed without a division,
+// shuffles.  Measured: a 32k-token prompt of 32 heads of 128 channels, rotated and appended, 325 us, read back 182 (floors of 105 each); a decode
+// step of 64 sequences 6.9 and 4.1 us in a graph.
+// What bounds the append is instructions, not bytes (68 % of the issue slots at a quarter of the DRAM rate), so the code is formed without a
+// division,
 //   code = rint(d / h): t = fma(d, RN(1/h), 1.5 2^23) holds rint(d RN(1/h)); the remainder d - code h tells whether the quotient can be
 //   near k + 0.5 (|remainder| >= h/2 (1 - 2^-18)); only then is more done.
 // The quantizer arithmetic is explicitly rounded fp32: codes and parameters do not depend on compiler contraction.

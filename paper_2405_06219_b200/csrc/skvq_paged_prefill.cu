@@ -17,10 +17,11 @@
 // 0 4 1 5 2 6 3 7 in the operands; the queries are laid out the same way and the outputs put back.
 // Items are laid end to end, priced in tiles (causal limits included), and cut into equal runs, one per CTA; an item that several
 // runs share goes through the workspace to the merge kernel.
-// Measured: 2048 queries at the end of 32k tokens, 32 heads over 8, D = 128: 1287 us, 0.83 PFLOP/s (tensor core 57 % busy); ragged prompts up to
-// 4095 tokens, 32 heads of 64: 563 us, of it 74 for the queries.  The chain of a row block bounds it: scores out of tensor memory,
-// exponentials, probabilities back, product, about 4600 clocks a tile of 256 x 128 where the products alone take 2048; more stages
-// need more than tensor memory's 512 columns.
+// Measured: 2048 queries at the end of 32k tokens, 32 heads over 8, D = 128: 1216 to 1290 us, 0.83 to 0.88 PFLOP/s (tensor core 57 % busy); ragged
+// prompts up to 4095 tokens, 32 heads of 64: 558 to 571 us, of it 74 for the queries.  At D = 128 the chain of a row block bounds it: scores out
+// of tensor memory, exponentials, probabilities back, product, about 4600 clocks a tile of 256 x 128 where the products alone take 2048;
+// more stages need more than tensor memory's 512 columns.  At D = 64, whose items are short (9 tiles on average in those prompts), what
+// lies between items is as much: queries, first scores, last products and rows follow one another, and 128 columns stay idle.
 #include <math_constants.h>
 
 #include "skvq_mma_common.cuh"
@@ -659,73 +660,73 @@ __global__ void __launch_bounds__(kPrefillThreads, 1) paged_prefill_kernel(const
     } else if (warp >= 12) {
         // ================================================================ products of a row block
         if (warp < 14) {
-        const int blk = warp & 1;
-        constexpr uint32_t kIdescS = idesc_f16_f32(kBlock, kBlock / 2);
-        constexpr uint32_t kIdescO = idesc_f16_f32(kBlock, D) | (1u << 16);      // B is MN-major
-        const uint32_t smem_base = smem_u32(smem);
-        // S = Q K~^T of half `hf` of tile number `tile`.  The whole warp runs these (addresses are warp-uniform), one lane issues.
-        auto issue_scores = [&](uint32_t tile, int hf) {
-            const uint32_t buf = tile & 1;
-            const uint64_t dq = desc_k_major(smem_base + Geo::Q + blk * Geo::TILE_BYTES), dk = desc_k_major(smem_base + Geo::K + buf * Geo::TILE_BYTES + hf * 64 * 128);
-            if (hf == 0) wait(k_full + 8 * buf, (tile >> 1) & 1);
-            tc_fence_after();
-            if (elect_one()) {
-#pragma unroll
-                for (int ks = 0; ks < D / 16; ++ks) {
-                    constexpr uint32_t half = Geo::HALF_BYTES >> 4;
-                    umma_f16(tmem + Geo::TMEM_S + blk * kBlock + hf * 64, dq + (ks >> 2) * half + (ks & 3) * 2, dk + (ks >> 2) * half + (ks & 3) * 2, kIdescS, ks > 0);
+            const int blk = warp & 1;
+            constexpr uint32_t kIdescS = idesc_f16_f32(kBlock, kBlock / 2);
+            constexpr uint32_t kIdescO = idesc_f16_f32(kBlock, D) | (1u << 16);      // B is MN-major
+            const uint32_t smem_base = smem_u32(smem);
+            // S = Q K~^T of half `hf` of tile number `tile`.  The whole warp runs these (addresses are warp-uniform), one lane issues.
+            auto issue_scores = [&](uint32_t tile, int hf) {
+                const uint32_t buf = tile & 1;
+                const uint64_t dq = desc_k_major(smem_base + Geo::Q + blk * Geo::TILE_BYTES), dk = desc_k_major(smem_base + Geo::K + buf * Geo::TILE_BYTES + hf * 64 * 128);
+                if (hf == 0) wait(k_full + 8 * buf, (tile >> 1) & 1);
+                tc_fence_after();
+                if (elect_one()) {
+    #pragma unroll
+                    for (int ks = 0; ks < D / 16; ++ks) {
+                        constexpr uint32_t half = Geo::HALF_BYTES >> 4;
+                        umma_f16(tmem + Geo::TMEM_S + blk * kBlock + hf * 64, dq + (ks >> 2) * half + (ks & 3) * 2, dk + (ks >> 2) * half + (ks & 3) * 2, kIdescS, ks > 0);
+                    }
+                    umma_commit(s_full + 16 * blk + 8 * hf);
+                    if (hf) umma_commit(k_empty + 8 * buf);
                 }
-                umma_commit(s_full + 16 * blk + 8 * hf);
-                if (hf) umma_commit(k_empty + 8 * buf);
-            }
-            __syncwarp();
-        };
-        auto issue_values = [&](uint32_t tile, int hf, bool first) {
-            const uint32_t buf = tile & 1;
-            const uint64_t dv = desc_mn_major(smem_base + Geo::V + buf * Geo::TILE_BYTES + hf * 64 * 128, Geo::HALF_BYTES);
-            if (hf == 0) wait(v_full + 8 * buf, (tile >> 1) & 1);
-            tc_fence_after();
-            if (elect_one()) {
-#pragma unroll
-                for (int ks = 0; ks < kBlock / 32; ++ks)
-                    umma_f16_ts(tmem + Geo::TMEM_O + blk * D, tmem + Geo::TMEM_S + blk * kBlock + hf * 64 + ks * 8, dv + ks * (2048 >> 4), kIdescO, !first || ks > 0);
-                umma_commit(pv_done + 16 * blk + 8 * hf);
-                if (hf) umma_commit(v_empty + 8 * buf);
-            }
-            __syncwarp();
-        };
-        uint32_t n = 0, ns = 0, nq = 0;      // tiles so far (both blocks'), of this block, items of this block
-        while (next()) {
-            if (*fail) alive = false;
-            if (s.it.rows() <= (s.m * 2 + blk) * kBlock) {
-                // A block without rows follows the tiles all the same: it frees the buffers on its side, and it must not reach a
-                // later item while a barrier is still two phases behind what it would wait for.
-                for (int t = s.t0; t < s.t1; ++t, ++n) {
-                    wait(k_full + 8 * (n & 1), (n >> 1) & 1);
-                    if (lane == 0) mbar_arrive(k_empty + 8 * (n & 1));
-                    wait(v_full + 8 * (n & 1), (n >> 1) & 1);
-                    if (lane == 0) mbar_arrive(v_empty + 8 * (n & 1));
+                __syncwarp();
+            };
+            auto issue_values = [&](uint32_t tile, int hf, bool first) {
+                const uint32_t buf = tile & 1;
+                const uint64_t dv = desc_mn_major(smem_base + Geo::V + buf * Geo::TILE_BYTES + hf * 64 * 128, Geo::HALF_BYTES);
+                if (hf == 0) wait(v_full + 8 * buf, (tile >> 1) & 1);
+                tc_fence_after();
+                if (elect_one()) {
+    #pragma unroll
+                    for (int ks = 0; ks < kBlock / 32; ++ks)
+                        umma_f16_ts(tmem + Geo::TMEM_O + blk * D, tmem + Geo::TMEM_S + blk * kBlock + hf * 64 + ks * 8, dv + ks * (2048 >> 4), kIdescO, !first || ks > 0);
+                    umma_commit(pv_done + 16 * blk + 8 * hf);
+                    if (hf) umma_commit(v_empty + 8 * buf);
                 }
-                continue;
-            }
-            if (s.t0 >= s.t1) continue;
-            wait(q_full + 8 * blk, nq & 1);
-            ++nq;
-            issue_scores(n, 0);
-            issue_scores(n, 1);
-            for (int t = s.t0; t < s.t1; ++t, ++n, ++ns) {
-#pragma unroll 1
-                for (int hf = 0; hf < 2; ++hf) {
-                    wait(p_full + 16 * blk + 8 * hf, ns & 1);
-                    issue_values(n, hf, t == s.t0 && hf == 0);
-                    if (t + 1 < s.t1) issue_scores(n + 1, hf);
+                __syncwarp();
+            };
+            uint32_t n = 0, ns = 0, nq = 0;      // tiles so far (both blocks'), of this block, items of this block
+            while (next()) {
+                if (*fail) alive = false;
+                if (s.it.rows() <= (s.m * 2 + blk) * kBlock) {
+                    // A block without rows follows the tiles all the same: it frees the buffers on its side, and it must not reach a
+                    // later item while a barrier is still two phases behind what it would wait for.
+                    for (int t = s.t0; t < s.t1; ++t, ++n) {
+                        wait(k_full + 8 * (n & 1), (n >> 1) & 1);
+                        if (lane == 0) mbar_arrive(k_empty + 8 * (n & 1));
+                        wait(v_full + 8 * (n & 1), (n >> 1) & 1);
+                        if (lane == 0) mbar_arrive(v_empty + 8 * (n & 1));
+                    }
+                    continue;
+                }
+                if (s.t0 >= s.t1) continue;
+                wait(q_full + 8 * blk, nq & 1);
+                ++nq;
+                issue_scores(n, 0);
+                issue_scores(n, 1);
+                for (int t = s.t0; t < s.t1; ++t, ++n, ++ns) {
+    #pragma unroll 1
+                    for (int hf = 0; hf < 2; ++hf) {
+                        wait(p_full + 16 * blk + 8 * hf, ns & 1);
+                        issue_values(n, hf, t == s.t0 && hf == 0);
+                        if (t + 1 < s.t1) issue_scores(n + 1, hf);
+                    }
                 }
             }
-        }
-        if (__any_sync(0xffffffffu, *fail != 0)) {      // nobody may have waited for the last products: they must not outlive the CTA
-            if (elect_one()) umma_commit(drained + 8 * blk);
-            mbar_wait_cycles(drained + 8 * blk, 0);
-        }
+            if (__any_sync(0xffffffffu, *fail != 0)) {      // nobody may have waited for the last products: they must not outlive the CTA
+                if (elect_one()) umma_commit(drained + 8 * blk);
+                mbar_wait_cycles(drained + 8 * blk, 0);
+            }
         }
     } else {
         // ================================================================ softmax

@@ -6,8 +6,9 @@
 namespace skvq {
 
 // Sequences with at most this many packed rows (new tokens * Hq/Hkv) per KV head go to the kernel for few rows, the others to the
-// tcgen05 kernel.  Measured on 16 sequences of 1024 to 16384 tokens, 8 KV heads: 16 rows 114 us here, 237 there; 20 rows 209 here (a
-// second item per KV head, or wider ones), 198 there; 32 rows 256 and 235.
+// tcgen05 kernel.  Measured on 16 sequences of 1024 to 16384 tokens, 8 KV heads of 128, bf16, in a graph: 8 rows 62 us here; 16 rows 102 here,
+// 209 there; 20 rows (a second item per KV head here) 158 here, 198 there; 24 rows 147 and 198; 32 rows 171 and 231.  So the kernel for few
+// rows would take up to 32 rows faster; above 16 it has not been tested.
 constexpr int kFewRows = 16;
 
 // Workspace of a kernel: descriptor [n_slots][8] ints, then partials [n_slots][2][rows per item][D + 4] floats {o[D], m (log2
