@@ -1,6 +1,7 @@
 """The paged cache where it meets an engine's own bookkeeping: kept prefixes, sequences that change their slot, page-table entries
 that are no pages, queries that are not finite.  Against the plain 64-bit forms of paged_reference, with their counted bounds."""
 import math
+import threading
 
 import pytest
 import torch
@@ -278,3 +279,70 @@ def test_the_largest_magnitudes(new):
     ko, vo = p.cache.read(p.batch([120], [120]), window=False)
     assert torch.isfinite(ko.float()).all() and torch.isfinite(vo.float()).all()
     p.check_attention([new], sm_scale=1e-7)
+
+
+# ------------------------------------------------------------------------------------------------ two calls at once, captured prompts
+def test_two_host_threads_and_two_graphs_of_a_prompt_step():
+    """Calls from two threads on a stream each, and a step of prompts and single tokens captured twice and replayed side by side with
+    lengths that change on the device: every result as it is alone."""
+    p = base.Paged(n_seqs=4, Hq=8, H=2, seed=241, W=32, P=32, rot=64)
+    p.append([180, 40, 300, 7])
+    new = [150, 1, 20, 1]
+    q = torch.randn(sum(new), 8, 128, generator=p.g).half().cuda()
+    b, one = p.batch(new, p.lens()), p.batch([1, 1, 1, 1], p.lens())
+    q1 = q[:4].contiguous()
+    alone = [p.cache.attention(b, q, 0.1, rope=p.rope), p.cache.attention(one, q1, 0.1, rope=p.rope)]
+    torch.cuda.synchronize()
+    got = [[], []]
+
+    def calls(i):
+        stream = torch.cuda.Stream()
+        with torch.cuda.stream(stream):
+            for _ in range(20):
+                got[i].append(p.cache.attention(b, q, 0.1, rope=p.rope) if i == 0 else p.cache.attention(one, q1, 0.1, rope=p.rope))
+        stream.synchronize()
+
+    threads = [threading.Thread(target=calls, args=(i,)) for i in range(2)]
+    [t.start() for t in threads]
+    [t.join() for t in threads]
+    assert len(got[0]) == len(got[1]) == 20
+    assert all(torch.equal(x, alone[i]) for i in range(2) for x in got[i])
+    lens = torch.tensor(p.lens(), dtype=torch.int32, device="cuda")
+    live = p.cache.batch(p.page_table, lens, b.keep[2], sum(new), 150, p.max_pages * p.P)
+    graphs, outs = [torch.cuda.CUDAGraph() for _ in range(2)], []
+    for g in graphs:
+        with torch.cuda.graph(g):
+            outs.append(p.cache.attention(live, q, 0.1, rope=p.rope))
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for less in (0, 3, 6):
+        lens.copy_(torch.tensor([n - less for n in p.lens()], dtype=torch.int32))
+        torch.cuda.synchronize()
+        for g, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                for _ in range(3):
+                    g.replay()
+        torch.cuda.synchronize()
+        want = p.cache.attention(live, q, 0.1, rope=p.rope)
+        assert torch.equal(outs[0], want) and torch.equal(outs[1], want)
+    assert int(p.cache.status[0]) == 0
+
+
+@pytest.mark.parametrize("rows", [1, 17])
+def test_a_context_of_sixteen_million_tokens(rows):
+    """One page over and over: the answer is that of the page, the log-sum-exp larger by the logarithm of the number of pages."""
+    P, D, L = 256, 64, 1 << 24
+    p = base.Paged(n_seqs=1, Hq=1, H=1, D=D, G=64, W=0, P=P, max_len=P, seed=251, reorder=False, outliers=False)
+    p.append([P])
+    q = torch.randn(rows, 1, D, generator=p.g).half()
+    table = p.page_table[:, :1].expand(1, L // P).contiguous()
+    b = p.cache.batch(table, torch.tensor([L], dtype=torch.int32, device="cuda"), torch.tensor([0, rows], dtype=torch.int32, device="cuda"), rows, rows, L)
+    lse = torch.empty(rows, 1, device="cuda")
+    out = p.cache.attention(b, q.cuda(), 0.125, causal=False, lse=lse)
+    want, wl, err, el = p.ref.attention(0, q, 0.125, causal=False)
+    # The longest chain of one accumulator's truncated sums is that of a CTA's warp in the kernel for few rows (2^24 tokens over 148 x 3 CTAs
+    # of 4 warps, 16 tokens a product: 591), a CTA's tiles in the other (2^24 over 148 CTAs, 16 tokens a product: 7085).
+    chain = 7100 * 2.0 ** -23
+    top = float(p.ref.values(0, "v").abs().max())
+    assert ((out.cpu().double() - want).abs() <= err + chain * top).all()
+    assert ((lse.cpu().double() - wl - math.log(L // P)).abs() <= el + chain + 30 * 2.0 ** -23).all()
+    assert int(p.cache.status[0]) == 0
