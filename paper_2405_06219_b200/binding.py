@@ -457,7 +457,8 @@ class SkvqPagedCache:
 
     dtype: torch.float16 or torch.bfloat16; reorder_k/_v: int32 [Hkv, D] or None; alpha_k/_v: float32 [Hkv, D/G] or None;
     ring_tokens: rows per ring slot (default: window); buffers: an engine's own tensors for any of k_codes, v_codes, k_meta,
-    v_meta, k_win, v_win instead of new ones."""
+    v_meta, k_win, v_win instead of new ones.  status[0] (int32, on the GPU) collects the SKVQ_STATUS_* bits of all calls: sequences
+    and tokens that a call skipped are reported there and nowhere else; the caller reads and clears it."""
 
     def __init__(self, n_q_heads, n_kv_heads, head_dim, group_size, window, page_tokens, n_pages, n_slots, dtype=torch.float16,
                  reorder_k=None, reorder_v=None, alpha_k=None, alpha_v=None, ring_tokens=None, buffers=None, device="cuda:0"):
@@ -530,7 +531,9 @@ class SkvqPagedCache:
                                            v.data_ptr(), ks, vs, _raw_stream(index, stream)), "skvq_paged_append")
 
     def read(self, batch, k=None, v=None, window: bool = True, stream=None):
-        """The new tokens' rows of the cache as values [T, Hkv, D], in source order; into k and v where they are given."""
+        """The new tokens' rows of the cache as values [T, Hkv, D], in source order; into k and v where they are given.
+        Rows of skipped sequences and tokens, and rows behind the last sequence, are not written: in tensors made here they hold
+        whatever lay in that memory.  What was skipped shows in the cache's `status`."""
         H, index = self.cfg.n_kv_heads, self.index
         self._operands(batch)
         with _on(index), (_HERE if stream is None else torch.cuda.stream(stream)):
@@ -548,7 +551,8 @@ class SkvqPagedCache:
                   workspace=None, stream=None):
         """q [T, Hq, D] -> out [T, Hq, D]; lse: optional float32 [T, Hq].  Without a workspace (a tensor of at least
         skvq_paged_workspace_size bytes) each call takes one of its own from torch's allocator on the stream it runs on, so calls
-        on several streams and captured graphs never share it."""
+        on several streams and captured graphs never share it.  Rows of skipped sequences, and rows behind the last sequence, are not
+        written: without `out` they hold whatever lay in that memory.  What was skipped shows in the cache's `status`."""
         c, index, rotation = self.cfg, self.index, self._operands(batch, rope)
         H = c.n_q_heads
         qs = self._rows(q, batch, H)
