@@ -17,7 +17,7 @@
 // 0 4 1 5 2 6 3 7 in the operands; the queries are laid out the same way and the outputs put back.
 // Items are laid end to end, priced in tiles (causal limits included), and cut into equal runs, one per CTA; an item that several
 // runs share goes through the workspace to the merge kernel.
-// Measured: 2048 queries at the end of 32k tokens, 32 heads over 8, D = 128: 1216 to 1290 us, 0.83 to 0.88 PFLOP/s (tensor core 57 % busy); ragged
+// Measured: 2048 queries at the end of 32k tokens, 32 heads over 8, D = 128: 1216 to 1290 us, 0.83 to 0.88 PFLOP/s (tensor core 61 % busy); ragged
 // prompts up to 4095 tokens, 32 heads of 64: 558 to 571 us, of it 74 for the queries.  At D = 128 the chain of a row block bounds it: scores out
 // of tensor memory, exponentials, probabilities back, product, about 4600 clocks a tile of 256 x 128 where the products alone take 2048;
 // more stages need more than tensor memory's 512 columns.  At D = 64, whose items are short (9 tiles on average in those prompts), what
