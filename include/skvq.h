@@ -56,7 +56,7 @@ extern "C" {
 
 #define SKVQ_STATUS_BAD_BATCH 8    /* paged calls: a sequence's lens/starts/slots entry is out of range; that sequence was skipped */
 #define SKVQ_STATUS_BAD_PAGE 16    /* paged calls: a page-table entry is not a page of the pool; its tokens were skipped */
-#define SKVQ_STATUS_BAD_POSITION 32 /* skvq_rope_apply: a position lies outside the table; that token's rows were not written */
+#define SKVQ_STATUS_BAD_POSITION 32 /* skvq_rope_apply, skvq_rope_apply_axes: a position lies outside the table; that token's rows were not written */
 
 /* Rows of the quantized segment are allocated in multiples of this many tokens so
  * that a kernel may stage whole tiles; see skvq_quant_capacity(). */
@@ -334,6 +334,28 @@ int skvq_rope_apply(const skvq_rope *rope, int32_t dtype, int32_t head_dim, cons
                     const skvq_rope_tensor *b, const int32_t *positions, int32_t n_tokens, int32_t inverse, int32_t *status,
                     void *cuda_stream);
 
+/* Which axis of a position turns which pair (host struct): for tokens with several coordinates, e.g. time, height and width. */
+typedef struct skvq_rope_axes {
+    int32_t n_axes;    /* 1..4 */
+    uint8_t axis[128]; /* axis of pair j, below n_axes, for j < rot_dim/2; any assignment (runs of pairs, taking turns, ...) */
+} skvq_rope_axes;
+
+/*
+ * skvq_rope_apply for tokens with several positions each: pair j of token t turns by {c, s} = table[p][j], p the token's position
+ * on axis[j].  All axes read the one table; its frequencies are the caller's (skvq_rope_table takes any list, so axes may begin at
+ * the highest frequency each, or share one sequence of them).  With one axis this is skvq_rope_apply, bit for bit.
+ * inverse = 1 is the gradient with respect to x.
+ *   positions   device int32; token t's position on axis i is positions[i * axis_stride + t * token_stride] (strides in elements,
+ *               any, 0 included).  A token with a position outside the table on any axis is not written and sets
+ *               SKVQ_STATUS_BAD_POSITION
+ *   rot_dim     at most 256; everything else as for skvq_rope_apply
+ * For keys and queries whose positions are not their token numbers in the cache (images; sequences that skvq_paged_evict has
+ * shortened): rotate here, then call skvq_paged_append and skvq_paged_attention without a rotation.
+ */
+int skvq_rope_apply_axes(const skvq_rope *rope, const skvq_rope_axes *axes, int32_t dtype, int32_t head_dim,
+                         const skvq_rope_tensor *a, const skvq_rope_tensor *b, const int32_t *positions, int64_t axis_stride,
+                         int64_t token_stride, int32_t n_tokens, int32_t inverse, int32_t *status, void *cuda_stream);
+
 /* Shape of a paged cache (host struct). */
 typedef struct skvq_paged_config {
     int32_t n_q_heads;   /* Hq, a multiple of Hkv, Hq/Hkv <= 16 */
@@ -460,6 +482,92 @@ size_t skvq_paged_workspace_size(const skvq_paged_config *cfg, const skvq_paged_
 int skvq_paged_attention(const skvq_paged_config *cfg, const skvq_paged_cache *cache, const skvq_paged_batch *batch,
                          const skvq_rope *rope, const void *q, int64_t q_stride, void *out, int64_t out_stride, void *lse,
                          const skvq_paged_attn_args *args, void *cuda_stream);
+
+/* ------------------------------------------------------------------------------------------------------------------
+ * Shrinking a paged cache by what attention looked at: every step adds the probabilities that its rows gave each token to the
+ * token's weight (skvq_paged_weights, after skvq_paged_attention with an lse); when a sequence is too long, every KV head keeps
+ * its oldest, its newest and its heaviest tokens (skvq_paged_evict).  Weights are the caller's: float [n_slots][Hkv][capacity],
+ * token t of the sequence in slot s and KV head h at [s][h][t]; slots are those of the batch (without `slots` sequence b uses slot b).
+ * After an eviction a token's number in the cache is no longer its position: rotate by positions with skvq_rope_apply_axes (or
+ * skvq_rope_apply) and append and attend without a rotation.
+ * ------------------------------------------------------------------------------------------------------------------ */
+
+/* Options of one skvq_paged_weights call (host struct). */
+typedef struct skvq_paged_weights_args {
+    float sm_scale;       /* as for the attention that gave lse */
+    int32_t causal;       /* the same */
+    int32_t last;         /* 0: every new token's rows count; n > 0: those of a sequence's last n new tokens alone */
+    int32_t capacity;     /* tokens per row of the weights, >= max_len */
+    const float *weights; /* [n_slots][Hkv][capacity], or NULL: zeros */
+    float *weights_out;   /* the same shape; may be `weights` itself, other overlaps are not allowed */
+    void *workspace;      /* device scratch of at least skvq_paged_weights_workspace_size() bytes; may be NULL when that is 0 */
+    size_t workspace_bytes;
+} skvq_paged_weights_args;
+
+/* Scratch bytes that skvq_paged_weights needs (from the host bounds in `batch`): the counted queries, rotated, in the tensor
+ * core's layout.  0 without new tokens and on bad arguments.  Host only. */
+size_t skvq_paged_weights_workspace_size(const skvq_paged_config *cfg, const skvq_paged_batch *batch, int32_t last);
+
+/*
+ * Attention weights of a step, added up per token and KV head:
+ *   weights_out[s][h][t] = (t < L_b - n_b ? weights[s][h][t] : 0) + sum over the counted rows r of KV head h that see token t of
+ *                          exp(sm_scale q'_r . K~_t - lse_r)
+ * for t < L_b; entries at or beyond L_b are left alone, and a new token's old entry is not read (a slot needs no clearing).  q' and K~ are
+ * those of skvq_paged_attention; here the keys are not rounded to fp16: scores carry fp32's error.  Rows: the Hq/Hkv query heads of
+ * KV head h for each counted token; row i of a sequence sees tokens as attention's `causal` says.  A row whose lse is not finite, or
+ * whose query is not, adds nothing.  Sums are fp32, in an order that does not change from run to run.
+ *   q                dtype [T][Hq][D], token stride in elements (a multiple of 8, >= Hq*D), 16-byte aligned; not rotated when rope is
+ *                    given, as for attention
+ *   lse              float [T][Hq], as skvq_paged_attention wrote it
+ * A sequence without new tokens is copied (nothing is done when weights_out is weights).  Skipped sequences (as for
+ * skvq_paged_attention; here a slot outside [0, n_slots) always skips): their entries are left alone, SKVQ_STATUS_BAD_BATCH is set.  A token behind a bad page-table
+ * entry gains nothing and sets SKVQ_STATUS_BAD_PAGE.  Values need not lie in the cache (v_codes, v_meta, v_win are not read).
+ * Two sequences of a call must not share a slot.  Waits inside are bounded: one that runs out (it never should) sets
+ * SKVQ_STATUS_COPY_TIMEOUT, and the weights that it concerns are NaN.
+ */
+int skvq_paged_weights(const skvq_paged_config *cfg, const skvq_paged_cache *cache, const skvq_paged_batch *batch,
+                       const skvq_rope *rope, const void *q, int64_t q_stride, const void *lse,
+                       const skvq_paged_weights_args *args, void *cuda_stream);
+
+/* Options of one skvq_paged_evict call (host struct of device pointers and host numbers). */
+typedef struct skvq_paged_evict_args {
+    int32_t keep;          /* tokens that a sequence has afterwards at most, >= 1 */
+    int32_t first;         /* its oldest tokens that always stay, >= 0 */
+    int32_t recent;        /* its newest tokens that always stay, >= window; first + recent <= keep */
+    int32_t capacity;      /* tokens per row of the weights, >= max_len */
+    const float *weights;  /* [n_slots][Hkv][capacity] */
+    float *weights_out;    /* the same shape: the kept tokens' weights, in the destination slot; may be `weights` itself */
+    const int32_t *page_table_out; /* [n_seqs][max_pages_out]: pages that receive the kept rows, or NULL: the batch's page table */
+    int32_t max_pages_out;
+    const int32_t *slots_out;      /* [n_seqs] ring and weight slots afterwards, or NULL: the batch's */
+    int32_t *lens_out;             /* [n_seqs] lengths afterwards; may be the batch's lens */
+    int32_t *ring_from_out;        /* [n_seqs] ring_from afterwards, or NULL; may be the batch's ring_from */
+    int32_t *kept;                 /* [n_seqs][Hkv][keep]: the old number of every token, increasing; -1 behind the last */
+    void *workspace;               /* device scratch of at least skvq_paged_evict_workspace_size() bytes */
+    size_t workspace_bytes;
+} skvq_paged_evict_args;
+
+/* Scratch bytes that skvq_paged_evict needs.  0 on bad arguments.  Host only. */
+size_t skvq_paged_evict_workspace_size(const skvq_paged_config *cfg, const skvq_paged_batch *batch);
+
+/*
+ * Shorten sequences to `keep` tokens.  Of a sequence with L_b > keep every KV head keeps tokens 0 .. first-1, the last `recent` ones, and
+ * of those between them the keep - first - recent with the largest weights: at equal weights the lower token number, -0 equal to
+ * +0, a weight that is not a number below all others.  The kept rows of keys, values and weights become tokens 0 .. keep-1, in the order they
+ * had (heads differ in which tokens these are), and the ring's rows of the `recent` tokens follow (8192 of them at most).  Sequences with L_b <= keep
+ * stay as they are, and are copied where the destination is another.
+ *   batch            page_table, lens, slots, ring_from, max_len; starts (may be NULL), n_tokens and max_new are not looked at
+ * A destination page is the source's page of the same place in the table, or one that no sequence of the call reads; a destination slot is
+ * the sequence's own or one that no sequence of the call has.  So pages that sequences share must not be shortened in place: give
+ * page_table_out.  Pages behind the new length are the caller's to free.
+ * Pass ring_from_out to later batches if ring_from was given or tokens may be taken back (it tells which tokens the ring still
+ * holds); otherwise, since recent >= window, the ring holds what the window needs.
+ * A sequence is skipped and SKVQ_STATUS_BAD_BATCH set when its length is not in [0, max_len] or a slot of it is not in [0, n_slots): it keeps its
+ * length and ring_from, its kept numbers are -1.  A row whose source or destination page is not in [0, n_pages) is not moved and
+ * sets SKVQ_STATUS_BAD_PAGE.  SKVQ_ERR_UNSUPPORTED for a window beyond 8192.
+ */
+int skvq_paged_evict(const skvq_paged_config *cfg, const skvq_paged_cache *cache, const skvq_paged_batch *batch,
+                     const skvq_paged_evict_args *args, void *cuda_stream);
 
 #ifdef __cplusplus
 }

@@ -36,7 +36,8 @@ EXPORTS = ["skvq_version", "skvq_strerror", "skvq_launch_count", "skvq_check_con
            "skvq_cache_sizes", "skvq_sink_bytes", "skvq_quantize_append", "skvq_workspace_size", "skvq_decode_attention",
            "skvq_step_staging_size", "skvq_decode_step_host", "skvq_decode_attention_noalloc", "skvq_check_group_bounds",
            "skvq_rope_frequencies", "skvq_rope_table", "skvq_rope_apply", "skvq_check_paged_config", "skvq_paged_cache_sizes",
-           "skvq_paged_append", "skvq_paged_read", "skvq_paged_workspace_size", "skvq_paged_attention"]
+           "skvq_paged_append", "skvq_paged_read", "skvq_paged_workspace_size", "skvq_paged_attention", "skvq_rope_apply_axes",
+           "skvq_paged_weights_workspace_size", "skvq_paged_weights", "skvq_paged_evict_workspace_size", "skvq_paged_evict"]
 
 
 class SkvqConfig(ctypes.Structure):
@@ -71,6 +72,10 @@ class SkvqRopeTensor(ctypes.Structure):
         [("n_heads", ctypes.c_int32)]
 
 
+class SkvqRopeAxes(ctypes.Structure):
+    _fields_ = [("n_axes", ctypes.c_int32), ("axis", ctypes.c_uint8 * 128)]
+
+
 class SkvqPagedConfig(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("n_q_heads", "n_kv_heads", "head_dim", "group_size", "window", "ring_tokens",
                                               "page_tokens", "n_pages", "n_slots", "dtype")]
@@ -89,6 +94,18 @@ class SkvqPagedBatch(ctypes.Structure):
 class SkvqPagedAttnArgs(ctypes.Structure):
     _fields_ = [("sm_scale", ctypes.c_float), ("causal", ctypes.c_int32), ("n_splits", ctypes.c_int32),
                 ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t)]
+
+
+class SkvqPagedWeightsArgs(ctypes.Structure):
+    _fields_ = [("sm_scale", ctypes.c_float), ("causal", ctypes.c_int32), ("last", ctypes.c_int32), ("capacity", ctypes.c_int32),
+                ("weights", ctypes.c_void_p), ("weights_out", ctypes.c_void_p), ("workspace", ctypes.c_void_p),
+                ("workspace_bytes", ctypes.c_size_t)]
+
+
+class SkvqPagedEvictArgs(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("keep", "first", "recent", "capacity")] + \
+        [(n, ctypes.c_void_p) for n in ("weights", "weights_out", "page_table_out")] + [("max_pages_out", ctypes.c_int32)] + \
+        [(n, ctypes.c_void_p) for n in ("slots_out", "lens_out", "ring_from_out", "kept", "workspace")] + [("workspace_bytes", ctypes.c_size_t)]
 
 
 class SkvqError(RuntimeError):
@@ -161,6 +178,17 @@ def lib() -> ctypes.CDLL:
         L.skvq_paged_workspace_size.argtypes = [P(SkvqPagedConfig), P(SkvqPagedBatch), i32]
         L.skvq_paged_attention.restype = c_int
         L.skvq_paged_attention.argtypes = [*paged, P(SkvqRope), vp, i64, vp, i64, vp, P(SkvqPagedAttnArgs), vp]
+        L.skvq_rope_apply_axes.restype = c_int
+        L.skvq_rope_apply_axes.argtypes = [P(SkvqRope), P(SkvqRopeAxes), i32, i32, P(SkvqRopeTensor), P(SkvqRopeTensor), vp, i64, i64, i32, i32,
+                                           vp, vp]
+        L.skvq_paged_weights_workspace_size.restype = c_sz
+        L.skvq_paged_weights_workspace_size.argtypes = [P(SkvqPagedConfig), P(SkvqPagedBatch), i32]
+        L.skvq_paged_weights.restype = c_int
+        L.skvq_paged_weights.argtypes = [*paged, P(SkvqRope), vp, i64, vp, P(SkvqPagedWeightsArgs), vp]
+        L.skvq_paged_evict_workspace_size.restype = c_sz
+        L.skvq_paged_evict_workspace_size.argtypes = [P(SkvqPagedConfig), P(SkvqPagedBatch)]
+        L.skvq_paged_evict.restype = c_int
+        L.skvq_paged_evict.argtypes = [*paged, P(SkvqPagedEvictArgs), vp]
         _lib = L
     return _lib
 
@@ -297,6 +325,31 @@ def skvq_paged_attention(cfg, cache, batch, rope, q, q_stride: int, out, out_str
                                       _dptr(lse), ctypes.byref(args), _stream(stream)), "skvq_paged_attention")
 
 
+def skvq_rope_apply_axes(rope: SkvqRope, axes: SkvqRopeAxes, dtype: int, head_dim: int, a: SkvqRopeTensor, b, positions, axis_stride: int,
+                         token_stride: int, n_tokens: int, inverse: int = 0, status=None, stream=None) -> None:
+    _check(lib().skvq_rope_apply_axes(ctypes.byref(rope), ctypes.byref(axes), dtype, head_dim, ctypes.byref(a),
+                                      None if b is None else ctypes.byref(b), _dptr(positions), axis_stride, token_stride, n_tokens,
+                                      inverse, _dptr(status), _stream(stream)), "skvq_rope_apply_axes")
+
+
+def skvq_paged_weights_workspace_size(cfg, batch, last: int = 0) -> int:
+    return int(lib().skvq_paged_weights_workspace_size(ctypes.byref(cfg), ctypes.byref(batch), last))
+
+
+def skvq_paged_weights(cfg, cache, batch, rope, q, q_stride: int, lse, args, stream=None) -> None:
+    _check(lib().skvq_paged_weights(ctypes.byref(cfg), ctypes.byref(cache), ctypes.byref(batch), None if rope is None else ctypes.byref(rope),
+                                    _dptr(q), q_stride, _dptr(lse), ctypes.byref(args), _stream(stream)), "skvq_paged_weights")
+
+
+def skvq_paged_evict_workspace_size(cfg, batch) -> int:
+    return int(lib().skvq_paged_evict_workspace_size(ctypes.byref(cfg), ctypes.byref(batch)))
+
+
+def skvq_paged_evict(cfg, cache, batch, args, stream=None) -> None:
+    _check(lib().skvq_paged_evict(ctypes.byref(cfg), ctypes.byref(cache), ctypes.byref(batch), ctypes.byref(args), _stream(stream)),
+           "skvq_paged_evict")
+
+
 # ---------------------------------------------------------------- device-memory holder
 class SkvqCache:
     """Allocates the cache buffers as torch tensors (device memory only) and keeps the C structs.
@@ -418,6 +471,22 @@ def _rope_operand(x, y, dtype, T: int, D: int, index: int) -> SkvqRopeTensor:
     return SkvqRopeTensor(x.data_ptr(), y.data_ptr(), xs[0], xs[1], ys[0], ys[1], shape[1])
 
 
+class RopeAxes:
+    """Which axis of a position turns which pair of a head: ``of_pair[j]`` is the axis of pair j (0..3), one entry per pair.
+
+    RopeAxes.runs([16, 24, 24]) gives the first 16 pairs to axis 0, the next 24 to axis 1, the last 24 to axis 2."""
+
+    def __init__(self, of_pair):
+        of_pair = [int(a) for a in of_pair]
+        assert 1 <= len(of_pair) <= 128 and 0 <= min(of_pair) and max(of_pair) < 4, "an axis below 4 for each of up to 128 pairs"
+        self.pairs, self.n_axes = len(of_pair), max(of_pair) + 1
+        self.struct = SkvqRopeAxes(self.n_axes, (ctypes.c_uint8 * 128)(*of_pair))
+
+    @classmethod
+    def runs(cls, lengths):
+        return cls([a for a, n in enumerate(lengths) for _ in range(n)])
+
+
 class RopeTable:
     """A rotation: its cos/sin table (fp32 [positions, rot_dim/2, 2] on the GPU) and the pairing of channels."""
 
@@ -450,6 +519,22 @@ class RopeTable:
         with _on(index):
             _check(lib().skvq_rope_apply(_ref(self.struct), _DTYPES[dtype], D, _ref(a), _ref(b), positions.data_ptr(), T,
                                          1 if inverse else 0, _dptr(status), _raw_stream(index, stream)), "skvq_rope_apply")
+
+
+    def apply_axes(self, axes: RopeAxes, positions, q, q_out=None, k=None, k_out=None, inverse: bool = False, status=None, stream=None) -> None:
+        """apply() for tokens with a position on each of several axes.  positions: int32 [n_axes, T], any strides (a transposed [T, n_axes]
+        tensor does); pair j of a head turns by the table's row positions[axis of j].  inverse=True is the gradient of the rotation."""
+        T, _, D = q.shape
+        index, dtype = self.index, q.dtype
+        assert axes.pairs == self.rot_dim // 2, "axes: one entry per pair of the rotation"
+        assert positions.dtype == torch.int32 and tuple(positions.shape) == (axes.n_axes, T) and positions.get_device() == index, "positions: int32 [n_axes, T]"
+        assert status is None or (status.dtype == torch.int32 and status.numel() >= 1 and status.get_device() == index), "status: int32 on the table's device"
+        a = _rope_operand(q, q if q_out is None else q_out, dtype, T, D, index)
+        b = None if k is None else _rope_operand(k, k if k_out is None else k_out, dtype, T, D, index)
+        ps = positions.stride()
+        with _on(index):
+            _check(lib().skvq_rope_apply_axes(_ref(self.struct), _ref(axes.struct), _DTYPES[dtype], D, _ref(a), _ref(b), positions.data_ptr(), ps[0],
+                                              ps[1], T, 1 if inverse else 0, _dptr(status), _raw_stream(index, stream)), "skvq_rope_apply_axes")
 
 
 class SkvqPagedCache:
@@ -572,3 +657,65 @@ class SkvqPagedCache:
             _check(lib().skvq_paged_attention(_ref(c), _ref(self.struct), _ref(batch), rotation, q.data_ptr(), qs,
                                               out.data_ptr(), os_, _dptr(lse), _ref(args), _raw_stream(index, stream)), "skvq_paged_attention")
         return out
+
+    def new_weights(self, capacity: int):
+        """Attention weights of every slot, for accumulate_weights and evict: float32 [n_slots, Hkv, capacity], capacity >= the longest
+        sequence."""
+        return torch.zeros((self.cfg.n_slots, self.cfg.n_kv_heads, capacity), dtype=torch.float32, device=self.device)
+
+    def _weights(self, w) -> int:
+        shape = w.shape
+        assert w.get_device() == self.index and w.dtype == torch.float32 and w.is_contiguous() and len(shape) == 3
+        assert shape[0] == self.cfg.n_slots and shape[1] == self.cfg.n_kv_heads, "weights: [n_slots, Hkv, capacity]"
+        return shape[2]
+
+    def accumulate_weights(self, batch, q, lse, weights, sm_scale, out=None, causal: bool = True, rope=None, last: int = 0, workspace=None,
+                           stream=None):
+        """Adds to the weight of every token what this step's rows gave it: exp(score - lse) over the query heads of its KV head.
+        q [T, Hq, D] and lse [T, Hq] float32 as attention(..., lse=lse) had them, with the same sm_scale, causal and rope; weights float32
+        [n_slots, Hkv, capacity] (None: zeros), updated in place or into `out`.  last: only the last so many new tokens of a sequence
+        count.  Entries at or beyond a sequence's length are left alone.  Without a workspace each call takes one of its own."""
+        c, index, rotation = self.cfg, self.index, self._operands(batch, rope)
+        out = weights if out is None else out
+        capacity = self._weights(out)
+        assert weights is None or self._weights(weights) == capacity, "weights and out of one capacity"
+        qs = self._rows(q, batch, c.n_q_heads)
+        assert lse.dtype == torch.float32 and lse.is_contiguous() and lse.get_device() == index and lse.numel() >= batch.n_tokens * c.n_q_heads
+        with _on(index), (_HERE if stream is None else torch.cuda.stream(stream)):
+            if workspace is None:
+                size = skvq_paged_weights_workspace_size(c, batch, last)
+                workspace = torch.empty(size, dtype=torch.uint8, device=self.device) if size else None
+            else:
+                assert workspace.get_device() == index and workspace.is_contiguous()
+                size = workspace.numel() * workspace.element_size()
+            args = SkvqPagedWeightsArgs(sm_scale, 1 if causal else 0, last, capacity, _dptr(weights), out.data_ptr(), _dptr(workspace), size)
+            _check(lib().skvq_paged_weights(_ref(c), _ref(self.struct), _ref(batch), rotation, q.data_ptr(), qs, lse.data_ptr(), _ref(args),
+                                            _raw_stream(index, stream)), "skvq_paged_weights")
+        return out
+
+    def evict(self, batch, weights, keep: int, first: int = 0, recent=None, weights_out=None, page_table_out=None, slots_out=None, lens_out=None,
+              ring_from_out=None, kept=None, stream=None):
+        """Shortens every sequence of the batch to `keep` tokens: per KV head the `first` oldest, the `recent` newest (default: the
+        window) and the heaviest of those between.  Gives (kept int32 [n, Hkv, keep]: the old number of every token, -1 behind the last;
+        the lengths int32 [n]; ring_from int32 [n] for later batches).  In place, or into other pages (page_table_out int32
+        [n, max_pages]), slots (slots_out int32 [n]) and weights (weights_out).  lens_out and ring_from_out may be the batch's own."""
+        c, index = self.cfg, self.index
+        self._operands(batch)
+        n, H = batch.n_seqs, c.n_kv_heads
+        capacity = self._weights(weights)
+        assert weights_out is None or self._weights(weights_out) == capacity, "weights of one capacity"
+        for t, count in ((page_table_out, None), (slots_out, n), (lens_out, n), (ring_from_out, n), (kept, n * H * keep)):
+            assert t is None or (t.get_device() == index and t.dtype == torch.int32 and t.is_contiguous() and (count is None or t.numel() == count))
+        assert page_table_out is None or (page_table_out.dim() == 2 and page_table_out.shape[0] == n), "page_table_out: [n, max_pages]"
+        with _on(index), (_HERE if stream is None else torch.cuda.stream(stream)):
+            size = skvq_paged_evict_workspace_size(c, batch)
+            workspace = torch.empty(size // 4, dtype=torch.int32, device=self.device)
+            kept = torch.empty((n, H, keep), dtype=torch.int32, device=self.device) if kept is None else kept
+            lens_out = torch.empty(n, dtype=torch.int32, device=self.device) if lens_out is None else lens_out
+            ring_from_out = torch.empty(n, dtype=torch.int32, device=self.device) if ring_from_out is None else ring_from_out
+            args = SkvqPagedEvictArgs(keep, first, c.window if recent is None else recent, capacity, weights.data_ptr(),
+                                      (weights if weights_out is None else weights_out).data_ptr(), _dptr(page_table_out),
+                                      0 if page_table_out is None else page_table_out.shape[1], _dptr(slots_out), lens_out.data_ptr(),
+                                      ring_from_out.data_ptr(), kept.data_ptr(), workspace.data_ptr(), size)
+            _check(lib().skvq_paged_evict(_ref(c), _ref(self.struct), _ref(batch), _ref(args), _raw_stream(index, stream)), "skvq_paged_evict")
+        return kept, lens_out, ring_from_out

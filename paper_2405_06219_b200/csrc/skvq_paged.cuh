@@ -202,4 +202,27 @@ struct PagedAttnArgs {
 size_t paged_workspace_bytes(const skvq_paged_config &cfg, const skvq_paged_batch &batch, int n_splits);
 cudaError_t launch_paged_attention(const PagedAttnArgs &a, cudaStream_t stream);
 
+struct PagedWeightArgs {
+    PagedArgs p;
+    const void *q;
+    const float *lse;
+    const float *w_in;      // NULL: zeros
+    float *w_out;
+    int64_t q_stride;
+    float sm_scale;
+    int causal, last, capacity;
+    uint8_t *ws;
+};
+size_t paged_weights_workspace_bytes(const skvq_paged_config &cfg, const skvq_paged_batch &batch, int last);
+cudaError_t launch_paged_weights(const PagedWeightArgs &a, cudaStream_t stream);
+
+constexpr int kMaxRingMoved = 8192;      // ring rows of a sequence that an eviction moves at most
+struct PagedEvictArgs {
+    PagedArgs p;
+    skvq_paged_evict_args e;
+    int max_kept;      // min(keep, max_len)
+};
+size_t paged_evict_workspace_bytes(const skvq_paged_batch &batch);
+cudaError_t launch_paged_evict(const PagedEvictArgs &a, cudaStream_t stream);
+
 }  // namespace skvq

@@ -69,6 +69,12 @@ PagedArgs make_args(const skvq_paged_config *cfg, const skvq_paged_cache *cache,
     return a;
 }
 
+// Weights have a row per slot whatever the window is.
+int check_slots(const skvq_paged_config *cfg, const skvq_paged_batch *b)
+{
+    return !b->slots && b->n_seqs > cfg->n_slots ? SKVQ_ERR_CAPACITY : SKVQ_OK;
+}
+
 }  // namespace
 }  // namespace skvq
 
@@ -164,6 +170,94 @@ int skvq_paged_attention(const skvq_paged_config *cfg, const skvq_paged_cache *c
     a.n_splits = args->n_splits;
     a.ws = static_cast<float *>(args->workspace);
     const cudaError_t e = launch_paged_attention(a, static_cast<cudaStream_t>(cuda_stream));
+    return e == cudaSuccess ? SKVQ_OK : SKVQ_ERR_CUDA;
+}
+
+size_t skvq_paged_weights_workspace_size(const skvq_paged_config *cfg, const skvq_paged_batch *batch, int32_t last)
+{
+    if (check_paged_cfg(cfg) != SKVQ_OK || !batch || batch->n_seqs < 1 || batch->n_seqs > kMaxPagedSeqs || batch->max_new < 1 ||
+        batch->n_tokens < 1 || batch->max_len < 0 || batch->max_len > kMaxPagedLen || last < 0 ||
+        (int64_t)batch->max_new * (cfg->n_q_heads / cfg->n_kv_heads) > (1 << 30))
+        return 0;
+    return paged_weights_workspace_bytes(*cfg, *batch, last);
+}
+
+int skvq_paged_weights(const skvq_paged_config *cfg, const skvq_paged_cache *cache, const skvq_paged_batch *batch,
+                       const skvq_rope *rope, const void *q, int64_t q_stride, const void *lse,
+                       const skvq_paged_weights_args *args, void *cuda_stream)
+{
+    int rc = check_paged_cfg(cfg);
+    if (rc == SKVQ_OK) rc = check_pool(cfg, cache);
+    if (rc == SKVQ_OK) rc = check_batch(cfg, batch);
+    if (rc == SKVQ_OK) rc = check_slots(cfg, batch);
+    if (rc == SKVQ_OK) rc = check_rope(cfg, rope);
+    if (rc != SKVQ_OK) return rc;
+    if (!args || args->last < 0 || (args->causal != 0 && args->causal != 1) || args->capacity < 1 || !args->weights_out) return SKVQ_ERR_INVALID_ARG;
+    if (batch->max_len > args->capacity) return SKVQ_ERR_CAPACITY;
+    if (off(args->weights, 4) || off(args->weights_out, 4) || off(args->workspace, 16)) return SKVQ_ERR_MISALIGNED;
+    const bool rows = batch->n_tokens > 0 && batch->max_new > 0;
+    if (!rows && args->weights == args->weights_out) return SKVQ_OK;
+    if (rows) {
+        if (!q || !lse) return SKVQ_ERR_INVALID_ARG;
+        rc = check_rows(q, q_stride, (int64_t)cfg->n_q_heads * cfg->head_dim);
+        if (rc != SKVQ_OK) return rc;
+        if (off(lse, 4)) return SKVQ_ERR_MISALIGNED;
+        const size_t need = paged_weights_workspace_bytes(*cfg, *batch, args->last);
+        if (need && (!args->workspace || args->workspace_bytes < need)) return SKVQ_ERR_WORKSPACE;
+    }
+    PagedWeightArgs a;
+    a.p = make_args(cfg, cache, batch, rope);
+    a.q = q;
+    a.lse = static_cast<const float *>(lse);
+    a.w_in = args->weights;
+    a.w_out = args->weights_out;
+    a.q_stride = q_stride;
+    a.sm_scale = args->sm_scale;
+    a.causal = args->causal;
+    a.last = args->last;
+    a.capacity = args->capacity;
+    a.ws = static_cast<uint8_t *>(args->workspace);
+    const cudaError_t e = launch_paged_weights(a, static_cast<cudaStream_t>(cuda_stream));
+    return e == cudaSuccess ? SKVQ_OK : SKVQ_ERR_CUDA;
+}
+
+size_t skvq_paged_evict_workspace_size(const skvq_paged_config *cfg, const skvq_paged_batch *batch)
+{
+    if (check_paged_cfg(cfg) != SKVQ_OK || !batch || batch->n_seqs < 1 || batch->n_seqs > kMaxPagedSeqs) return 0;
+    return paged_evict_workspace_bytes(*batch);
+}
+
+int skvq_paged_evict(const skvq_paged_config *cfg, const skvq_paged_cache *cache, const skvq_paged_batch *batch,
+                     const skvq_paged_evict_args *args, void *cuda_stream)
+{
+    int rc = check_paged_cfg(cfg);
+    if (rc == SKVQ_OK) rc = check_pool(cfg, cache);
+    if (rc != SKVQ_OK) return rc;
+    if (!batch) return SKVQ_ERR_INVALID_ARG;
+    skvq_paged_batch b = *batch;      // what the call does not look at is not checked either
+    b.starts = b.lens;
+    b.n_tokens = b.max_new = 0;
+    rc = check_batch(cfg, &b);
+    if (rc == SKVQ_OK) rc = check_slots(cfg, &b);
+    if (rc != SKVQ_OK) return rc;
+    if (!args || args->keep < 1 || args->first < 0 || args->recent < 0 || args->recent < cfg->window || args->capacity < 1) return SKVQ_ERR_INVALID_ARG;
+    if ((int64_t)args->first + args->recent > args->keep) return SKVQ_ERR_INVALID_ARG;
+    if (!args->weights || !args->weights_out || !args->lens_out || !args->kept) return SKVQ_ERR_INVALID_ARG;
+    if (cfg->window > kMaxRingMoved) return SKVQ_ERR_UNSUPPORTED;
+    if (batch->max_len > args->capacity) return SKVQ_ERR_CAPACITY;
+    const int64_t most = batch->max_len < args->keep ? batch->max_len : args->keep;
+    if (args->page_table_out && args->max_pages_out < 1) return SKVQ_ERR_INVALID_ARG;
+    if (args->page_table_out && most > (int64_t)args->max_pages_out * cfg->page_tokens) return SKVQ_ERR_CAPACITY;
+    const void *words[] = {args->weights, args->weights_out, args->page_table_out, args->slots_out, args->lens_out, args->ring_from_out, args->kept};
+    for (const void *p : words)
+        if (off(p, 4)) return SKVQ_ERR_MISALIGNED;
+    if (off(args->workspace, 16)) return SKVQ_ERR_MISALIGNED;
+    if (!args->workspace || args->workspace_bytes < paged_evict_workspace_bytes(b)) return SKVQ_ERR_WORKSPACE;
+    PagedEvictArgs a;
+    a.p = make_args(cfg, cache, &b, nullptr);
+    a.e = *args;
+    a.max_kept = (int)most;
+    const cudaError_t e = launch_paged_evict(a, static_cast<cudaStream_t>(cuda_stream));
     return e == cudaSuccess ? SKVQ_OK : SKVQ_ERR_CUDA;
 }
 

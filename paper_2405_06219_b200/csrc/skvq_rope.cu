@@ -55,44 +55,15 @@ struct RopeArgs {
 
 template <typename T, int V> struct alignas(sizeof(T) * V) Vec { T v[V]; };
 
-// A task is V pairs of the rotated part (half layout: V channels and their V partners; interleaved: 2V neighbouring channels)
-// or 2V channels behind it.
+// What a thread does to its channels of its heads.  A task is V pairs of the rotated part (half layout: V channels and their V partners;
+// interleaved: 2V neighbouring channels) or 2V channels behind it.
 template <typename T, int V, bool INTERLEAVED>
-__global__ void __launch_bounds__(kRopeThreads) rope_kernel(const __grid_constant__ RopeArgs a)
+__device__ __forceinline__ void rotate_heads(const RopeArgs &a, long long tok, int group, int task, bool rot, const float (&cs)[V], const float (&sn)[V])
 {
-    const long long i = (long long)blockIdx.x * kRopeThreads + threadIdx.x;
-    const int task = (int)(i % a.tasks);
-    const long long rest = i / a.tasks;
-    const int group = (int)(rest % a.groups);
-    const long long tok = rest / a.groups;
-    if (tok >= a.n_tokens) return;
-    const int p = a.positions[tok];
-    if (p < 0 || p >= a.n_positions) {
-        if (task == 0 && group == 0) set_status(a.status, SKVQ_STATUS_BAD_POSITION);
-        return;
-    }
     using VecT = Vec<T, V>;
-    const bool rot = task < a.pair_tasks;
-    const int half = a.rot_dim / 2;
-    int c1, c2;             // first channels of the task's two vectors
-    float cs[V], sn[V];
-    if (rot) {
-        const int j = task * V;
-        c1 = INTERLEAVED ? 2 * j : j;
-        c2 = INTERLEAVED ? 2 * j + V : j + half;
-        const float *row = a.table + ((int64_t)p * half + j) * 2;
-        Vec<float, V >= 2 ? 4 : 2> e;
-        constexpr int PER = V >= 2 ? 2 : 1;       // pairs per load
-#pragma unroll
-        for (int k = 0; k < V; k += PER) {
-            e = *reinterpret_cast<const decltype(e) *>(row + 2 * k);
-#pragma unroll
-            for (int m = 0; m < PER; ++m) { cs[k + m] = e.v[2 * m]; sn[k + m] = a.sign * e.v[2 * m + 1]; }
-        }
-    } else {
-        c1 = a.rot_dim + (task - a.pair_tasks) * 2 * V;
-        c2 = c1 + V;
-    }
+    const int j = task * V;
+    const int c1 = rot ? (INTERLEAVED ? 2 * j : j) : a.rot_dim + (task - a.pair_tasks) * 2 * V;      // first channels of the task's two vectors
+    const int c2 = rot && !INTERLEAVED ? j + a.rot_dim / 2 : c1 + V;
     const bool second = c2 < a.head_dim;      // the copied part may end inside a task
 #pragma unroll 2
     for (int hh = 0; hh < a.per_thread; ++hh) {
@@ -134,8 +105,39 @@ __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const __grid_constan
     }
 }
 
-template <typename T, int V>
-cudaError_t launch_rope(RopeArgs a, bool interleaved, cudaStream_t stream)
+template <typename T, int V, bool INTERLEAVED>
+__global__ void __launch_bounds__(kRopeThreads) rope_kernel(const __grid_constant__ RopeArgs a)
+{
+    const long long i = (long long)blockIdx.x * kRopeThreads + threadIdx.x;
+    const int task = (int)(i % a.tasks);
+    const long long rest = i / a.tasks;
+    const int group = (int)(rest % a.groups);
+    const long long tok = rest / a.groups;
+    if (tok >= a.n_tokens) return;
+    const int p = a.positions[tok];
+    if (p < 0 || p >= a.n_positions) {
+        if (task == 0 && group == 0) set_status(a.status, SKVQ_STATUS_BAD_POSITION);
+        return;
+    }
+    const bool rot = task < a.pair_tasks;
+    float cs[V], sn[V];
+    if (rot) {
+        const int j = task * V;
+        const float *row = a.table + ((int64_t)p * (a.rot_dim / 2) + j) * 2;
+        Vec<float, V >= 2 ? 4 : 2> e;
+        constexpr int PER = V >= 2 ? 2 : 1;       // pairs per load
+#pragma unroll
+        for (int k = 0; k < V; k += PER) {
+            e = *reinterpret_cast<const decltype(e) *>(row + 2 * k);
+#pragma unroll
+            for (int m = 0; m < PER; ++m) { cs[k + m] = e.v[2 * m]; sn[k + m] = a.sign * e.v[2 * m + 1]; }
+        }
+    }
+    rotate_heads<T, V, INTERLEAVED>(a, tok, group, task, rot, cs, sn);
+}
+
+// Tasks, heads per thread; the blocks of the launch.
+template <int V> long long rope_shape(RopeArgs &a)
 {
     a.pair_tasks = a.rot_dim / 2 / V;
     a.tasks = a.pair_tasks + (a.head_dim - a.rot_dim + 2 * V - 1) / (2 * V);
@@ -144,10 +146,81 @@ cudaError_t launch_rope(RopeArgs a, bool interleaved, cudaStream_t stream)
     long long per = all / want;
     a.per_thread = (int)(per < 1 ? 1 : (per > 8 ? 8 : per));
     a.groups = (a.heads + a.per_thread - 1) / a.per_thread;
-    const long long threads = (long long)a.n_tokens * a.groups * a.tasks, blocks = (threads + kRopeThreads - 1) / kRopeThreads;
+    return ((long long)a.n_tokens * a.groups * a.tasks + kRopeThreads - 1) / kRopeThreads;
+}
+
+template <typename T, int V>
+cudaError_t launch_rope(RopeArgs a, bool interleaved, cudaStream_t stream)
+{
+    const long long blocks = rope_shape<V>(a);
     if (blocks > 0x7fffffffLL) return cudaErrorInvalidValue;
     if (interleaved) rope_kernel<T, V, true><<<(unsigned)blocks, kRopeThreads, 0, stream>>>(a);
     else rope_kernel<T, V, false><<<(unsigned)blocks, kRopeThreads, 0, stream>>>(a);
+    count_launch();
+    return cudaGetLastError();
+}
+
+// The rotation with several axes: pair j turns by the angle that the table's row of the token's position on axis[j] has.  A thread
+// differs from the kernel above in what it does once: it reads the token's positions on all axes and picks a row per pair; then it
+// walks over heads with its angles in registers just so.
+constexpr int kMaxAxes = 4;
+struct RopeAxesArgs {
+    RopeArgs r;
+    int64_t axis_stride, token_stride;
+    int n_axes;
+    unsigned long long axis_of[4];      // two bits per pair, pair j in bits 2 (j % 32) of word j / 32
+};
+
+template <typename T, int V, bool INTERLEAVED>
+__global__ void __launch_bounds__(kRopeThreads) rope_axes_kernel(const __grid_constant__ RopeAxesArgs args)
+{
+    const RopeArgs &a = args.r;
+    const long long i = (long long)blockIdx.x * kRopeThreads + threadIdx.x;
+    const int task = (int)(i % a.tasks);
+    const long long rest = i / a.tasks;
+    const int group = (int)(rest % a.groups);
+    const long long tok = rest / a.groups;
+    if (tok >= a.n_tokens) return;
+    int p[kMaxAxes];
+    bool inside = true;
+#pragma unroll
+    for (int x = 0; x < kMaxAxes; ++x) {
+        p[x] = 0;
+        if (x < args.n_axes) {
+            p[x] = a.positions[tok * args.token_stride + x * args.axis_stride];
+            inside = inside && p[x] >= 0 && p[x] < a.n_positions;
+        }
+    }
+    if (!inside) {
+        if (task == 0 && group == 0) set_status(a.status, SKVQ_STATUS_BAD_POSITION);
+        return;
+    }
+    float cs[V], sn[V];
+    const bool rot = task < a.pair_tasks;
+    if (rot) {
+        const int j = task * V, half = a.rot_dim / 2;
+        const unsigned long long word = j < 64 ? (j < 32 ? args.axis_of[0] : args.axis_of[1]) : (j < 96 ? args.axis_of[2] : args.axis_of[3]);
+        const uint32_t axes = (uint32_t)(word >> (2 * (j & 31)));      // V divides 32: a task's pairs lie in one word
+        const float2 *table = reinterpret_cast<const float2 *>(a.table) + j;
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+            const int x = (axes >> (2 * k)) & 3;
+            const int row = x & 2 ? (x & 1 ? p[3] : p[2]) : (x & 1 ? p[1] : p[0]);
+            const float2 e = table[(int64_t)row * half + k];
+            cs[k] = e.x;
+            sn[k] = a.sign * e.y;
+        }
+    }
+    rotate_heads<T, V, INTERLEAVED>(a, tok, group, task, rot, cs, sn);
+}
+
+template <typename T, int V>
+cudaError_t launch_rope_axes(RopeAxesArgs a, bool interleaved, cudaStream_t stream)
+{
+    const long long blocks = rope_shape<V>(a.r);
+    if (blocks > 0x7fffffffLL) return cudaErrorInvalidValue;
+    if (interleaved) rope_axes_kernel<T, V, true><<<(unsigned)blocks, kRopeThreads, 0, stream>>>(a);
+    else rope_axes_kernel<T, V, false><<<(unsigned)blocks, kRopeThreads, 0, stream>>>(a);
     count_launch();
     return cudaGetLastError();
 }
@@ -168,6 +241,55 @@ bool rows_overlap(int n_tokens, int n_heads, int64_t ts, int64_t hs, int dim)
 }
 
 bool plain_pointer(const void *p, int elt) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(elt - 1)) == 0; }
+
+// The checks that both rotations make, and their common arguments; a.n_tokens = 0: nothing to do.  `wide`: vectors of 16 bytes.
+int rope_args(const skvq_rope *rope, int32_t dtype, int32_t head_dim, const skvq_rope_tensor *ta, const skvq_rope_tensor *tb,
+              const int32_t *positions, int32_t n_tokens, int32_t inverse, int32_t *status, RopeArgs &a, bool &wide)
+{
+    if (!rope || !ta || n_tokens < 0 || head_dim < 1 || (inverse != 0 && inverse != 1)) return SKVQ_ERR_INVALID_ARG;
+    if (dtype != SKVQ_F16 && dtype != SKVQ_BF16 && dtype != SKVQ_F32) return SKVQ_ERR_UNSUPPORTED;
+    if (rope->rot_dim < 2 || (rope->rot_dim & 1) || rope->rot_dim > head_dim || rope->n_positions < 0 ||
+        (rope->interleaved != 0 && rope->interleaved != 1))
+        return SKVQ_ERR_INVALID_ARG;
+    if (head_dim > 512) return SKVQ_ERR_UNSUPPORTED;
+    const int elt = dtype == SKVQ_F32 ? 4 : 2;
+    const skvq_rope_tensor *t[2] = {ta, tb};
+    wide = head_dim * elt % 16 == 0;      // 16-byte vectors everywhere
+    a.heads = 0;
+    for (int i = 0; i < 2; ++i) {
+        a.op[i] = RopeOperand{};
+        if (!t[i]) continue;
+        if (t[i]->n_heads < 0) return SKVQ_ERR_INVALID_ARG;
+        if (t[i]->n_heads > 65535) return SKVQ_ERR_UNSUPPORTED;
+        if (t[i]->n_heads > 0 && n_tokens > 0 && (!t[i]->x || !t[i]->y)) return SKVQ_ERR_INVALID_ARG;
+        if (!plain_pointer(t[i]->x, elt) || !plain_pointer(t[i]->y, elt)) return SKVQ_ERR_MISALIGNED;
+        if (n_tokens > 0 && t[i]->n_heads > 0) {
+            if (rows_overlap(n_tokens, t[i]->n_heads, t[i]->y_token_stride, t[i]->y_head_stride, head_dim)) return SKVQ_ERR_INVALID_ARG;
+            if (t[i]->x == t[i]->y && ((n_tokens > 1 && t[i]->x_token_stride != t[i]->y_token_stride) ||
+                                       (t[i]->n_heads > 1 && t[i]->x_head_stride != t[i]->y_head_stride)))
+                return SKVQ_ERR_INVALID_ARG;
+        }
+        a.op[i] = RopeOperand{t[i]->x, t[i]->y, t[i]->x_token_stride, t[i]->x_head_stride, t[i]->y_token_stride, t[i]->y_head_stride, t[i]->n_heads};
+        a.heads += t[i]->n_heads;
+        wide = wide && plain_pointer(t[i]->x, 16) && plain_pointer(t[i]->y, 16) &&
+               ((t[i]->x_token_stride | t[i]->x_head_stride | t[i]->y_token_stride | t[i]->y_head_stride) * elt) % 16 == 0;
+    }
+    a.n_tokens = a.heads == 0 ? 0 : n_tokens;
+    if (a.n_tokens == 0) return SKVQ_OK;
+    if (!rope->table || !positions) return SKVQ_ERR_INVALID_ARG;
+    if (!plain_pointer(rope->table, 16) || !plain_pointer(positions, 4) || !plain_pointer(status, 4)) return SKVQ_ERR_MISALIGNED;
+    a.table = static_cast<const float *>(rope->table);
+    a.positions = positions;
+    a.status = status;
+    a.n_positions = rope->n_positions;
+    a.rot_dim = rope->rot_dim;
+    a.head_dim = head_dim;
+    a.sign = inverse ? -1.0f : 1.0f;
+    // Vectors of 16 bytes where rows, heads and the halves of the rotated part start on 16-byte boundaries; single elements else.
+    const int v = 16 / elt;
+    wide = wide && (rope->interleaved ? rope->rot_dim % (2 * v) : rope->rot_dim / 2 % v) == 0;
+    return SKVQ_OK;
+}
 
 }  // namespace
 }  // namespace skvq
@@ -232,54 +354,43 @@ int skvq_rope_apply(const skvq_rope *rope, int32_t dtype, int32_t head_dim, cons
                     const skvq_rope_tensor *tb, const int32_t *positions, int32_t n_tokens, int32_t inverse, int32_t *status,
                     void *cuda_stream)
 {
-    if (!rope || !ta || n_tokens < 0 || head_dim < 1 || (inverse != 0 && inverse != 1)) return SKVQ_ERR_INVALID_ARG;
-    if (dtype != SKVQ_F16 && dtype != SKVQ_BF16 && dtype != SKVQ_F32) return SKVQ_ERR_UNSUPPORTED;
-    if (rope->rot_dim < 2 || (rope->rot_dim & 1) || rope->rot_dim > head_dim || rope->n_positions < 0 ||
-        (rope->interleaved != 0 && rope->interleaved != 1))
-        return SKVQ_ERR_INVALID_ARG;
-    if (head_dim > 512) return SKVQ_ERR_UNSUPPORTED;
-    const int elt = dtype == SKVQ_F32 ? 4 : 2;
     RopeArgs a;
-    const skvq_rope_tensor *t[2] = {ta, tb};
-    bool wide = head_dim * elt % 16 == 0;      // 16-byte vectors everywhere
-    a.heads = 0;
-    for (int i = 0; i < 2; ++i) {
-        a.op[i] = RopeOperand{};
-        if (!t[i]) continue;
-        if (t[i]->n_heads < 0) return SKVQ_ERR_INVALID_ARG;
-        if (t[i]->n_heads > 65535) return SKVQ_ERR_UNSUPPORTED;
-        if (t[i]->n_heads > 0 && n_tokens > 0 && (!t[i]->x || !t[i]->y)) return SKVQ_ERR_INVALID_ARG;
-        if (!plain_pointer(t[i]->x, elt) || !plain_pointer(t[i]->y, elt)) return SKVQ_ERR_MISALIGNED;
-        if (n_tokens > 0 && t[i]->n_heads > 0) {
-            if (rows_overlap(n_tokens, t[i]->n_heads, t[i]->y_token_stride, t[i]->y_head_stride, head_dim)) return SKVQ_ERR_INVALID_ARG;
-            if (t[i]->x == t[i]->y && ((n_tokens > 1 && t[i]->x_token_stride != t[i]->y_token_stride) ||
-                                       (t[i]->n_heads > 1 && t[i]->x_head_stride != t[i]->y_head_stride)))
-                return SKVQ_ERR_INVALID_ARG;
-        }
-        a.op[i] = RopeOperand{t[i]->x, t[i]->y, t[i]->x_token_stride, t[i]->x_head_stride, t[i]->y_token_stride, t[i]->y_head_stride, t[i]->n_heads};
-        a.heads += t[i]->n_heads;
-        wide = wide && plain_pointer(t[i]->x, 16) && plain_pointer(t[i]->y, 16) &&
-               ((t[i]->x_token_stride | t[i]->x_head_stride | t[i]->y_token_stride | t[i]->y_head_stride) * elt) % 16 == 0;
-    }
-    if (n_tokens == 0 || a.heads == 0) return SKVQ_OK;
-    if (!rope->table || !positions) return SKVQ_ERR_INVALID_ARG;
-    if (!plain_pointer(rope->table, 16) || !plain_pointer(positions, 4) || !plain_pointer(status, 4)) return SKVQ_ERR_MISALIGNED;
-    a.table = static_cast<const float *>(rope->table);
-    a.positions = positions;
-    a.status = status;
-    a.n_tokens = n_tokens;
-    a.n_positions = rope->n_positions;
-    a.rot_dim = rope->rot_dim;
-    a.head_dim = head_dim;
-    a.sign = inverse ? -1.0f : 1.0f;
-    // Vectors of 16 bytes where rows, heads and the halves of the rotated part start on 16-byte boundaries; single elements else.
-    const int v = 16 / elt;
-    wide = wide && (rope->interleaved ? rope->rot_dim % (2 * v) : rope->rot_dim / 2 % v) == 0;
+    bool wide;
+    const int rc = rope_args(rope, dtype, head_dim, ta, tb, positions, n_tokens, inverse, status, a, wide);
+    if (rc != SKVQ_OK || a.n_tokens == 0) return rc;
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     cudaError_t e;
     if (dtype == SKVQ_F16) e = wide ? launch_rope<__half, 8>(a, rope->interleaved, stream) : launch_rope<__half, 1>(a, rope->interleaved, stream);
     else if (dtype == SKVQ_BF16) e = wide ? launch_rope<__nv_bfloat16, 8>(a, rope->interleaved, stream) : launch_rope<__nv_bfloat16, 1>(a, rope->interleaved, stream);
     else e = wide ? launch_rope<float, 4>(a, rope->interleaved, stream) : launch_rope<float, 1>(a, rope->interleaved, stream);
+    return e == cudaSuccess ? SKVQ_OK : SKVQ_ERR_CUDA;
+}
+
+int skvq_rope_apply_axes(const skvq_rope *rope, const skvq_rope_axes *axes, int32_t dtype, int32_t head_dim, const skvq_rope_tensor *ta,
+                         const skvq_rope_tensor *tb, const int32_t *positions, int64_t axis_stride, int64_t token_stride, int32_t n_tokens,
+                         int32_t inverse, int32_t *status, void *cuda_stream)
+{
+    if (!axes || axes->n_axes < 1) return SKVQ_ERR_INVALID_ARG;
+    if (axes->n_axes > kMaxAxes) return SKVQ_ERR_UNSUPPORTED;
+    RopeAxesArgs a;
+    bool wide;
+    const int rc = rope_args(rope, dtype, head_dim, ta, tb, positions, n_tokens, inverse, status, a.r, wide);
+    if (rc != SKVQ_OK) return rc;
+    if (rope->rot_dim > 2 * kMaxFreq) return SKVQ_ERR_UNSUPPORTED;
+    for (unsigned long long &w : a.axis_of) w = 0;
+    for (int j = 0; j < rope->rot_dim / 2; ++j) {
+        if (axes->axis[j] >= axes->n_axes) return SKVQ_ERR_INVALID_ARG;
+        a.axis_of[j >> 5] |= (unsigned long long)axes->axis[j] << (2 * (j & 31));
+    }
+    if (a.r.n_tokens == 0) return SKVQ_OK;
+    a.axis_stride = axis_stride;
+    a.token_stride = token_stride;
+    a.n_axes = axes->n_axes;
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    cudaError_t e;
+    if (dtype == SKVQ_F16) e = wide ? launch_rope_axes<__half, 8>(a, rope->interleaved, stream) : launch_rope_axes<__half, 1>(a, rope->interleaved, stream);
+    else if (dtype == SKVQ_BF16) e = wide ? launch_rope_axes<__nv_bfloat16, 8>(a, rope->interleaved, stream) : launch_rope_axes<__nv_bfloat16, 1>(a, rope->interleaved, stream);
+    else e = wide ? launch_rope_axes<float, 4>(a, rope->interleaved, stream) : launch_rope_axes<float, 1>(a, rope->interleaved, stream);
     return e == cudaSuccess ? SKVQ_OK : SKVQ_ERR_CUDA;
 }
 
