@@ -9,26 +9,31 @@
 // since a key rounded to fp16 would put an error of 2^-11 of its largest terms into the exponent.
 #include <math_constants.h>
 
+#include "skvq_mma_common.cuh"
 #include "skvq_paged.cuh"
 #include "skvq_paged_split.cuh"
 
 namespace skvq {
 namespace {
 
+using mmak::ex2_approx;
+using mmak::mma16816;
+using mmak::smem_u32;
+
+constexpr float kSubnormal = 1.f / 16777216.f;      // 2^-24: the least fp16 subnormal, what a code's lowest bit stands for as an operand
 constexpr int kQueryThreads = 128;
 constexpr int kQueryTokens = kQueryThreads / 16;
-constexpr int kTileRows = 128;      // rows of a query tile where sequences may have many
+constexpr int kTileRows = 128;      // rows of a query tile
 
-// A query tile: `rows` rows of D fp16, 64-channel halves one after the other, a half's rows 128 bytes each with 16-byte piece c of row r
-// at c ^ (r & 7) (the 128-byte swizzle of the tensor core's operands); then floats [rows] factor of a score in units of log2, [rows]
-// minus the lse in units of log2 (minus infinity: the row adds nothing), [NG][rows] sums of the row over a group's channels.
+// A query tile: kTileRows rows of D fp16, 64-channel halves one after the other, a half's rows 128 bytes each with 16-byte piece c of row r
+// at c ^ (r & 7) (the 128-byte swizzle of the tensor core's operands); then floats [kTileRows] factor of a score in units of log2,
+// [kTileRows] minus the lse in units of log2 (minus infinity: the row adds nothing), [NG][kTileRows] sums of the row over a group's channels.
 struct WeightPlan {
     PagedWeightArgs a;
-    int tile_rows;        // 16 or kTileRows
-    int seq_tiles;        // > 0: sequence b's tiles begin at b * seq_tiles; 0: at starts[b] * Hq/Hkv / tile_rows + b
+    int seq_tiles;        // > 0: sequence b's tiles begin at b * seq_tiles; 0: at starts[b] * Hq/Hkv / kTileRows + b
     int heads;            // query heads that a CTA of the first kernel walks over
 };
-__host__ __device__ inline int tile_bytes(int rows, int D, int ng) { return rows * (D * 2 + (2 + ng) * 4); }
+__host__ __device__ constexpr int tile_bytes(int D, int ng) { return kTileRows * (D * 2 + (2 + ng) * 4); }
 
 // What a sequence contributes.
 struct WeightSeq {
@@ -45,13 +50,463 @@ __device__ __forceinline__ void weight_sequence(const PagedWeightArgs &a, int b,
 }
 __device__ __forceinline__ const uint8_t *query_tile(const WeightPlan &p, const WeightSeq &w, int b, int h, int tile)
 {
-    const int64_t base = p.seq_tiles ? (int64_t)b * p.seq_tiles : (int64_t)w.s.row0 * w.rep / p.tile_rows + b;
-    return p.a.ws + ((base + tile) * p.a.p.cfg.n_kv_heads + h) * tile_bytes(p.tile_rows, p.a.p.cfg.head_dim, p.a.p.ng);
+    const int64_t base = p.seq_tiles ? (int64_t)b * p.seq_tiles : (int64_t)w.s.row0 * w.rep / kTileRows + b;
+    return p.a.ws + ((base + tile) * p.a.p.cfg.n_kv_heads + h) * tile_bytes(p.a.p.cfg.head_dim, p.a.p.ng);
 }
 
 // Position 0..7 inside a run of eight operand channels -> stored channel: nibbles i and i + 4 of a code word become neighbours.
 __device__ __forceinline__ int channel_at(int pos) { return (pos >> 1) + 4 * (pos & 1); }
 
+// The power of two that brings a row's largest magnitude to [2^13, 2^14): exact, whatever the type's range.
+__device__ __forceinline__ float row_factor(float mx)
+{
+    return mx > 0.f ? __int_as_float((127 + min(13 - (__float_as_int(mx) >> 23) + 127, 60)) << 23) : 1.f;
+}
+__device__ __forceinline__ uint32_t sixteenth(uint32_t v)      // of two fp16
+{
+    uint32_t r;
+    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(v), "r"(0x2C002C00u));
+    return r;
+}
+__device__ __forceinline__ void load_matrices(uint32_t (&r)[4], uint32_t addr)      // four 8 x 8 matrices of 16-bit elements
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void cp16(uint32_t dst, const void *src)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+// A pair of elements of the cache's type as fp16 (bf16: exact between 2^-14 and 65504, off by 2^-25 at most below).
+template <typename T> __device__ __forceinline__ uint32_t as_h2(uint32_t v);
+template <> __device__ __forceinline__ uint32_t as_h2<__half>(uint32_t v) { return v; }
+template <> __device__ __forceinline__ uint32_t as_h2<__nv_bfloat16>(uint32_t v)
+{
+    return packed<__half>(__uint_as_float(v << 16), __uint_as_float(v & 0xFFFF0000u));
+}
+
+// ------------------------------------------------------------------------------------------------ few rows: single tokens, drafts
+// Sequences with at most 16 rows per KV head.  What bounds it is reading the keys' codes once; every warp works for itself.
+// The (sequence, KV head) pairs are laid end to end, priced in 32-token tiles (16 tokens of the unquantized window: kRingCost), and cut into
+// equal runs, one per warp.  A warp streams its tiles through a ring of its own in shared memory; 16 tokens' codes are the A
+// operand of mma.m16n8k16, 8 rows the B operand, one accumulator per group.  A nibble under zeros is an fp16 subnormal, c 2^-24 (or
+// 16 c 2^-24, against q/16), so codes enter the product as they are, exactly; the parameters' factor 2^24 goes to h.  The
+// accumulators start at minus 8 times the sum of the group's q' (and z becomes z + 8 h): sums of codes about their middle, which are as small as the score.
+constexpr int kFewRowTile = 8;
+constexpr int kTile = 32;
+constexpr int kRingTile = 16;
+constexpr int kRingCost = 2;
+constexpr int kFewWarps = 4;
+constexpr int kFewThreads = kFewWarps * 32;
+constexpr int kFewStages = 3;
+
+template <int D, int NG, int NT> struct FewGeo {
+    static constexpr int ROW = D / 2, CHUNKS = ROW / 16;
+    static constexpr int CODES = kTile * ROW, META = kTile * NG * 4, STAGE = CODES + META;
+    static constexpr int SETS = D / 32;                      // 32-channel granules: 16-byte pieces of a code row
+    static constexpr int RROW = D * 2, RCHUNKS = RROW / 16;
+    static constexpr int RING = kFewStages * STAGE;
+    static constexpr int ROWS = kFewRowTile * NT, QROW = D + 8;
+    static constexpr int QUERIES = RING, RAW = QUERIES + ROWS * QROW * 2, CONSTANTS = RAW + D * 2;
+    static constexpr int WARP = CONSTANTS + ROWS * (2 + NG) * 4;
+    static constexpr int SMEM = kFewWarps * WARP;
+    static_assert(kRingTile * RROW <= RING, "a window tile fits the warp's ring");
+    static_assert(WARP % 16 == 0 && QUERIES % 16 == 0 && RAW % 16 == 0, "16-byte pieces");
+};
+// Position of 16-byte piece c of row t: the eight rows that a matrix load touches lie in different banks.
+template <int D> __device__ __forceinline__ int piece_at(int t, int c) { return D == 128 ? c ^ ((t >> 1) & 3) : c ^ ((t >> 2) & 1); }
+
+struct FewCost {
+    int tiles_c, tiles_r, cost;
+};
+__device__ __forceinline__ FewCost few_cost(const PagedWeightArgs &a, const WeightSeq &w)
+{
+    FewCost c;
+    c.tiles_c = (w.s.lq + kTile - 1) / kTile;
+    c.tiles_r = (w.s.len - w.s.lq + kRingTile - 1) / kRingTile;
+    c.cost = w.rows > kFewRows || (w.rows == 0 && a.w_in == a.w_out) ? 0 : c.tiles_c + kRingCost * c.tiles_r;
+    return c;
+}
+
+template <typename T, int D, int NG, int NT>
+__global__ void __launch_bounds__(kFewThreads, NT == 1 ? 5 : 4) weight_few_kernel(const __grid_constant__ WeightPlan plan)
+{
+    using Geo = FewGeo<D, NG, NT>;
+    const PagedWeightArgs &a = plan.a;
+    const PagedArgs &p = a.p;
+    const skvq_paged_config &cfg = p.cfg;
+    extern __shared__ __align__(128) uint8_t smem[];
+    long long *pre = reinterpret_cast<long long *>(smem + Geo::SMEM);      // [n_seqs + 1] cost of the sequences before b
+    __shared__ long long scan_sh[kFewWarps];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, j = lane & 3, B = p.batch.n_seqs, H = cfg.n_kv_heads;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;");
+    // ---- the flat partition: exclusive prefix of the sequences' costs
+    {
+        long long carry = 0;
+        for (int base = 0; base < B; base += kFewThreads) {
+            const int b = base + tid;
+            long long c = 0;
+            if (b < B) {
+                WeightSeq w;
+                weight_sequence(a, b, w);
+                if (w.ok) c = (long long)few_cost(a, w).cost * H;
+                else if (blockIdx.x == 0) set_status(p.c.status, SKVQ_STATUS_BAD_BATCH);
+            }
+            long long incl = c;
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const long long v = __shfl_up_sync(0xffffffffu, incl, d);
+                if (lane >= d) incl += v;
+            }
+            if (lane == 31) scan_sh[warp] = incl;
+            __syncthreads();
+            long long before = carry;
+            for (int k = 0; k < kFewWarps; ++k) {
+                if (k < warp) before += scan_sh[k];
+                carry += scan_sh[k];
+            }
+            if (b < B) pre[b] = before + incl - c;
+            __syncthreads();
+        }
+        if (tid == 0) pre[B] = carry;
+        __syncthreads();
+    }
+    const long long total = pre[B], runs = (long long)gridDim.x * kFewWarps, per = max((total + runs - 1) / runs, 1LL);
+    long long f = ((long long)blockIdx.x * kFewWarps + warp) * per;
+    const long long f1 = min(f + per, total);
+    if (f >= f1) return;
+    int b;
+    {
+        int lo = 0, hi = B - 1;
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (pre[mid] <= f) lo = mid; else hi = mid - 1;
+        }
+        b = lo;
+    }
+    uint8_t *mine = smem + warp * Geo::WARP;
+    const uint32_t ring = smem_u32(mine);
+    __half *queries = reinterpret_cast<__half *>(mine + Geo::QUERIES);      // [ROWS][QROW], runs of eight in the order 0 4 1 5 2 6 3 7
+    T *raw = reinterpret_cast<T *>(mine + Geo::RAW);
+    float *constants = reinterpret_cast<float *>(mine + Geo::CONSTANTS);    // [ROWS][2 + NG]: factor, minus lse, sums of the groups
+    const int P = cfg.page_tokens, page_shift = __ffs(P) - 1;
+
+    while (f < f1) {
+        while (pre[b + 1] <= f) ++b;
+        WeightSeq w;
+        weight_sequence(a, b, w);
+        const FewCost fc = few_cost(a, w);
+        const int item = (int)((f - pre[b]) / fc.cost), off = (int)(f - pre[b] - (long long)item * fc.cost), hk = item;
+        const int take = (int)min((long long)(fc.cost - off), f1 - f);
+        f += take;
+        const int L = w.s.len, lq = w.s.lq, R = w.rows, fresh = L - w.s.n;      // tokens at or beyond `fresh` are new
+        auto tile_of = [&](int x) { return x <= fc.tiles_c ? x : fc.tiles_c + (x - fc.tiles_c + kRingCost - 1) / kRingCost; };
+        const int seg0 = tile_of(off), seg1 = tile_of(off + take);
+        const int q0 = min(seg0, fc.tiles_c), q1 = min(seg1, fc.tiles_c), r0 = max(seg0, fc.tiles_c), r1 = max(seg1, fc.tiles_c);
+        const int64_t weight_row = ((int64_t)w.s.slot * H + hk) * a.capacity;
+        const float *w_in = a.w_in ? a.w_in + weight_row : nullptr;
+        float *w_out = a.w_out + weight_row;
+        auto old_weight = [&](int t) { return w_in && t < fresh ? w_in[t] : 0.f; };
+        if (R == 0) {
+            for (int t = q0 * kTile + lane; t < min(q1 * kTile, lq); t += 32) w_out[t] = old_weight(t);
+            for (int t = lq + (r0 - fc.tiles_c) * kRingTile + lane; t < min(lq + (r1 - fc.tiles_c) * kRingTile, L); t += 32) w_out[t] = old_weight(t);
+            continue;
+        }
+        const int32_t *table = p.batch.page_table + (int64_t)b * p.batch.max_pages;
+        // Page ids of 32 consecutive 16-token blocks, one per lane; -1 past the quantized tokens, -2 for an id outside the pool.
+        auto load_pages = [&](int block) {
+            const int t = (block + lane) * 16;
+            int id = -1;
+            if (t < lq) {
+                id = table[t >> page_shift];
+                if (id < 0 || id >= cfg.n_pages) { id = -2; set_status(p.c.status, SKVQ_STATUS_BAD_PAGE); }
+            }
+            return id;
+        };
+        int pages_base = q0 * 2, pages = q0 < q1 ? load_pages(pages_base) : -1, pages_next = q0 < q1 ? load_pages(pages_base + 32) : -1;
+        uint32_t bad = 0;      // bit 2 * stage + block: the block has no page
+        const uint32_t codes_dst = (lane / Geo::CHUNKS) * Geo::ROW;
+        auto fetch = [&](int tile, int stage) {
+            if (tile < q1) {
+                if (tile * 2 >= pages_base + 32) {
+                    pages_base += 32;
+                    pages = pages_next;
+                    pages_next = load_pages(pages_base + 32);
+                }
+                const uint32_t base = ring + stage * Geo::STAGE;
+                uint32_t none = 0;
+                constexpr int HALF = Geo::CHUNKS / 2, STEP = 32 / Geo::CHUNKS;      // copies of a block; rows that one covers
+#pragma unroll
+                for (int blk = 0; blk < 2; ++blk) {
+                    const int id = __shfl_sync(0xffffffffu, pages, tile * 2 + blk - pages_base);
+                    const int64_t at = ((int64_t)id * H + hk) * P + ((tile * kTile + 16 * blk) & (P - 1));
+                    if (id < 0) { none |= 1u << blk; continue; }
+                    const uint8_t *src = static_cast<const uint8_t *>(p.c.k_codes) + at * Geo::ROW + lane * 16;
+#pragma unroll
+                    for (int k = 0; k < HALF; ++k) {
+                        const int row = 16 * blk + k * STEP + lane / Geo::CHUNKS;
+                        cp16(base + codes_dst + (16 * blk + k * STEP) * Geo::ROW + piece_at<D>(row, lane % Geo::CHUNKS) * 16, src + k * 512);
+                    }
+                    if (lane < 4 * NG) cp16(base + Geo::CODES + blk * (64 * NG) + lane * 16, static_cast<const uint8_t *>(p.c.k_meta) + at * (NG * 4) + lane * 16);
+                }
+                bad = (bad & ~(3u << (2 * stage))) | none << (2 * stage);
+            }
+            cp_commit();
+        };
+#pragma unroll
+        for (int k = 0; k < kFewStages - 1; ++k) fetch(q0 + k, k);
+
+        // ---- the rows: rotate, round to T, reorder, fp16 times a power of two; the sums of the groups
+        {
+            constexpr int C = D / 32;
+            const float2 *rope = static_cast<const float2 *>(p.rope.table);
+            const int half = p.rope.rot_dim / 2;
+            int from[C];
+#pragma unroll
+            for (int k = 0; k < C; ++k) {
+                const int pos = lane * C + k, c = (pos & ~7) + channel_at(pos & 7);
+                from[k] = p.c.reorder_k ? p.c.reorder_k[hk * D + c] & (D - 1) : c;
+            }
+#pragma unroll 1
+            for (int r = 0; r < Geo::ROWS; ++r) {
+                if (r >= R) {
+                    if constexpr (C == 4) *reinterpret_cast<uint2 *>(queries + r * Geo::QROW + lane * C) = make_uint2(0u, 0u);
+                    else *reinterpret_cast<uint32_t *>(queries + r * Geo::QROW + lane * C) = 0u;
+                    if (lane < 2 + NG) constants[r * (2 + NG) + lane] = lane == 1 ? -CUDART_INF_F : 0.f;
+                    continue;
+                }
+                const int i = r / w.rep, head = hk * w.rep + r - i * w.rep, pos = L - w.m + i;
+                const int64_t tok = w.s.row0 + w.s.n - w.m + i;
+                const T *src = static_cast<const T *>(a.q) + tok * a.q_stride + (int64_t)head * D;
+                const float lse = a.lse[tok * cfg.n_q_heads + head];
+                __syncwarp();
+#pragma unroll
+                for (int k = 0; k < C; ++k) {
+                    const int c = lane + 32 * k;
+                    T x = src[c];
+                    if (rope && c < p.rope.rot_dim && pos >= 0) {
+                        const bool second = p.rope.interleaved ? c & 1 : c >= half;
+                        const int at = p.rope.interleaved ? c >> 1 : (second ? c - half : c), partner = p.rope.interleaved ? c ^ 1 : (second ? c - half : c + half);
+                        const float2 cs = rope[(int64_t)pos * half + at];
+                        const float own = Elem<T>::to_float(x), other = Elem<T>::to_float(src[partner]);
+                        x = Elem<T>::from_float(second ? rotate_second(other, own, cs.x, cs.y) : rotate_first(own, other, cs.x, cs.y));
+                    }
+                    raw[c] = x;
+                }
+                __syncwarp();
+                float x[C], mx = 0.f, sum = 0.f;
+                bool finite = fabsf(lse) < CUDART_INF_F;
+#pragma unroll
+                for (int k = 0; k < C; ++k) {
+                    x[k] = Elem<T>::to_float(raw[from[k]]);
+                    mx = fmaxf(mx, fabsf(x[k]));
+                    finite = finite && fabsf(x[k]) < CUDART_INF_F;
+                }
+                const bool counts = __all_sync(0xffffffffu, finite);
+#pragma unroll
+                for (int d = 1; d < 32; d <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
+                const float up = counts ? row_factor(mx) : 0.f;
+                uint32_t v[C / 2];
+#pragma unroll
+                for (int k = 0; k < C; k += 2) {
+                    v[k / 2] = counts ? packed<__half>(x[k] * up, x[k + 1] * up) : 0u;
+                    const float2 q = floats<__half>(v[k / 2]);
+                    sum += q.x + q.y;
+                }
+#pragma unroll
+                for (int d = 1; d < 32 / NG; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+                if constexpr (C == 4) *reinterpret_cast<uint2 *>(queries + r * Geo::QROW + lane * C) = make_uint2(v[0], v[1]);
+                else *reinterpret_cast<uint32_t *>(queries + r * Geo::QROW + lane * C) = v[0];
+                if (lane == 0) {
+                    constants[r * (2 + NG)] = counts ? a.sm_scale * 1.4426950408889634f / up : 0.f;
+                    constants[r * (2 + NG) + 1] = counts ? lse * -1.4426950408889634f : -CUDART_INF_F;
+                }
+                if (lane % (32 / NG) == 0) constants[r * (2 + NG) + 2 + lane / (32 / NG)] = sum;
+            }
+            __syncwarp();
+        }
+        uint32_t bq[NT][Geo::SETS * 2][2];
+        float rs[NT][2], nl[NT][2], qsum[NT][2][NG];
+        int lim[NT][2];      // of this lane's rows 8 n + 2 j and 8 n + 2 j + 1: they see tokens below it
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+#pragma unroll
+            for (int st = 0; st < Geo::SETS; ++st) {
+                const uint4 x = *reinterpret_cast<const uint4 *>(queries + (8 * n + g) * Geo::QROW + 32 * st + 8 * j);
+                bq[n][2 * st][0] = x.x;
+                bq[n][2 * st][1] = sixteenth(x.y);
+                bq[n][2 * st + 1][0] = x.z;
+                bq[n][2 * st + 1][1] = sixteenth(x.w);
+            }
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int r = 8 * n + 2 * j + e;
+                rs[n][e] = constants[r * (2 + NG)];
+                nl[n][e] = constants[r * (2 + NG) + 1];
+#pragma unroll
+                for (int k = 0; k < NG; ++k) qsum[n][e][k] = constants[r * (2 + NG) + 2 + k];
+                lim[n][e] = a.causal ? min(L, L - w.m + min(r, R - 1) / w.rep + 1) : L;
+            }
+        }
+        const int lowest = a.causal ? min(L, L - w.m + 1) : L;      // the first row's limit
+
+        // ---- quantized tokens
+        int stage = 0;
+        const uint32_t matrix_row = (lane & 7) + ((lane >> 3) & 1) * 8, matrix_piece = lane >> 4;      // what this lane's address stands for in a load of four matrices
+        float old_next = q0 < q1 && q0 * kTile + 8 * j + g < lq ? old_weight(q0 * kTile + 8 * j + g) : 0.f;
+#pragma unroll 1
+        for (int tile = q0; tile < q1; ++tile) {
+            fetch(tile + kFewStages - 1, stage == 0 ? kFewStages - 1 : stage - 1);
+            const int t0 = tile * kTile, own = t0 + 8 * j + g;
+            const float old = old_next;
+            if (tile + 1 < q1) old_next = own + kTile < lq ? old_weight(own + kTile) : 0.f;
+            cp_wait<kFewStages - 1>();
+            __syncwarp();
+            const uint32_t buf = ring + stage * Geo::STAGE;
+            const uint32_t *km = reinterpret_cast<const uint32_t *>(mine + stage * Geo::STAGE + Geo::CODES);
+            const uint32_t bad_here = (bad >> (2 * stage)) & 3u;
+            const bool edge = t0 + kTile > min(lq, lowest) || bad_here;      // some row or some token of the tile is masked
+            float sums[2][2];      // tokens 16 u + g and 16 u + 8 + g
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                float acc[NT][NG][4];
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int k = 0; k < NG; ++k)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[n][k][e] = qsum[n][e & 1][k] * (-8.f * kSubnormal);
+#pragma unroll
+                for (int s2 = 0; s2 < Geo::SETS; s2 += 2) {
+                    const int row = 16 * u + matrix_row;
+                    uint32_t c[4];      // words of tokens g and g + 8, granule s2; the same of granule s2 + 1
+                    load_matrices(c, buf + row * Geo::ROW + piece_at<D>(row, s2 + matrix_piece) * 16);
+#pragma unroll
+                    for (int h2 = 0; h2 < 2; ++h2) {
+                        const int st = s2 + h2;
+                        constexpr int PER = Geo::SETS / NG;      // granules per group
+                        const uint32_t x = c[2 * h2], y = c[2 * h2 + 1], xs = x >> 8, ys = y >> 8;
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) {
+                            float (&d)[4] = acc[n][st / PER];
+                            mma16816(d, x & 0x000F000Fu, y & 0x000F000Fu, x & 0x00F000F0u, y & 0x00F000F0u, bq[n][2 * st][0], bq[n][2 * st][1]);
+                            mma16816(d, xs & 0x000F000Fu, ys & 0x000F000Fu, xs & 0x00F000F0u, ys & 0x00F000F0u, bq[n][2 * st + 1][0], bq[n][2 * st + 1][1]);
+                        }
+                    }
+                }
+                float h[2][NG], z[2][NG];
+#pragma unroll
+                for (int half = 0; half < 2; ++half)
+#pragma unroll
+                    for (int k = 0; k < NG; ++k) {
+                        const float2 m = floats<__half>(km[(16 * u + 8 * half + g) * NG + k]);
+                        z[half][k] = fmaf(8.f, m.x, m.y);
+                        h[half][k] = m.x * (1.f / kSubnormal);
+                    }
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    float sum = 0.f;
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            float s = z[half][0] * qsum[n][e][0];
+#pragma unroll
+                            for (int k = 1; k < NG; ++k) s = fmaf(z[half][k], qsum[n][e][k], s);
+#pragma unroll
+                            for (int k = 0; k < NG; ++k) s = fmaf(h[half][k], acc[n][k][2 * half + e], s);
+                            s = fmaf(s, rs[n][e], nl[n][e]);
+                            if (edge && (t0 + 16 * u + 8 * half + g >= min(lq, lim[n][e]) || ((bad_here >> u) & 1u))) s = -CUDART_INF_F;
+                            sum += ex2_approx(s);
+                        }
+                    sums[u][half] = sum;
+                }
+            }
+            // lane (g, j) gets token 8 j + g, added up over the lanes that hold the other rows
+            {
+                const bool hi = j & 2, odd = j & 1;
+                float x0 = hi ? sums[1][0] : sums[0][0], x1 = hi ? sums[1][1] : sums[0][1];
+                x0 += __shfl_xor_sync(0xffffffffu, hi ? sums[0][0] : sums[1][0], 2);
+                x1 += __shfl_xor_sync(0xffffffffu, hi ? sums[0][1] : sums[1][1], 2);
+                const float x = (odd ? x1 : x0) + __shfl_xor_sync(0xffffffffu, odd ? x0 : x1, 1);
+                if (own < lq) w_out[own] = old + x;
+            }
+            __syncwarp();
+            stage = stage + 1 == kFewStages ? 0 : stage + 1;
+        }
+        cp_wait<0>();
+        __syncwarp();
+
+        // ---- the window: 16-bit rows, 16 tokens at a time through the warp's ring
+        const int64_t win_row0 = ((int64_t)w.s.slot * H + hk) * cfg.ring_tokens;
+#pragma unroll 1
+        for (int tile = r0; tile < r1; ++tile) {
+            const int t0 = lq + (tile - fc.tiles_c) * kRingTile;
+            int id = 0;
+            if (lane < kRingTile && t0 + lane < L) id = table[(t0 + lane) >> page_shift];
+            constexpr int STEP = 32 / Geo::RCHUNKS;
+            const int c = lane % Geo::RCHUNKS, first = t0 % cfg.ring_tokens;
+            const uint8_t *kw = static_cast<const uint8_t *>(p.c.k_win) + win_row0 * Geo::RROW + c * 16;
+#pragma unroll
+            for (int k = 0; k < kRingTile / STEP; ++k) {
+                const int t = k * STEP + lane / Geo::RCHUNKS;
+                if (t0 + t < L) {
+                    int row = first + t;      // the window is no longer than the ring: it wraps once at most
+                    if (row >= cfg.ring_tokens) row -= cfg.ring_tokens;
+                    cp16(ring + t * Geo::RROW + (c ^ (t & 7)) * 16, kw + (int64_t)row * Geo::RROW);
+                }
+            }
+            cp_commit();
+            const int tok = t0 + g + 8 * (j & 1);      // of lanes j = 0 and 1
+            const float old = j < 2 && tok < L ? old_weight(tok) : 0.f;
+            const bool none = id < 0 || id >= cfg.n_pages;
+            if (none) set_status(p.c.status, SKVQ_STATUS_BAD_PAGE);
+            const uint32_t gone = __ballot_sync(0xffffffffu, none);
+            cp_wait<0>();
+            __syncwarp();
+            float s[NT][4];
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[n][e] = 0.f;
+#pragma unroll
+            for (int st = 0; st < Geo::SETS; ++st) {
+                uint32_t x[2][4];
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    uint4 v = *reinterpret_cast<const uint4 *>(mine + (g + 8 * half) * Geo::RROW + ((4 * st + j) ^ g) * 16);
+                    v.x = as_h2<T>(v.x); v.y = as_h2<T>(v.y); v.z = as_h2<T>(v.z); v.w = as_h2<T>(v.w);
+                    x[half][0] = __byte_perm(v.x, v.z, 0x5410); x[half][1] = __byte_perm(v.x, v.z, 0x7632);
+                    x[half][2] = __byte_perm(v.y, v.w, 0x5410); x[half][3] = __byte_perm(v.y, v.w, 0x7632);
+                }
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    const uint4 q = *reinterpret_cast<const uint4 *>(queries + (8 * n + g) * Geo::QROW + 32 * st + 8 * j);
+                    mma16816(s[n], x[0][0], x[1][0], x[0][1], x[1][1], q.x, q.y);
+                    mma16816(s[n], x[0][2], x[1][2], x[0][3], x[1][3], q.z, q.w);
+                }
+            }
+            float sums[2] = {0.f, 0.f};
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int at = g + 8 * (e >> 1);
+                    const bool hidden = t0 + at >= lim[n][e & 1] || ((gone >> at) & 1u);      // rows behind the last token were not copied
+                    sums[e >> 1] += hidden ? 0.f : ex2_approx(fmaf(s[n][e], rs[n][e & 1], nl[n][e & 1]));
+                }
+            const bool odd = j & 1;
+            float x = (odd ? sums[1] : sums[0]) + __shfl_xor_sync(0xffffffffu, odd ? sums[0] : sums[1], 1);
+            x += __shfl_xor_sync(0xffffffffu, x, 2);
+            if (j < 2 && tok < L) w_out[tok] = old + x;
+            __syncwarp();
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ many rows: prompts and chunks
 // Sixteen lanes own a row; a half-warp takes a token and walks over heads with the token's angles in registers.
 template <typename T, int D, int NG>
 __global__ void __launch_bounds__(kQueryThreads) weight_queries_kernel(const __grid_constant__ WeightPlan plan)
@@ -66,9 +521,8 @@ __global__ void __launch_bounds__(kQueryThreads) weight_queries_kernel(const __g
     const int unit = threadIdx.x >> 4, sub = threadIdx.x & 15, c0 = sub * C, b = blockIdx.z;
     WeightSeq w;
     weight_sequence(a, b, w);
-    if (!w.ok) return;
-    // a tile that is read whole has zeros behind its last row
-    const int filled = plan.tile_rows == kTileRows ? (w.rows + kTileRows - 1) / kTileRows * kTileRows : w.rows;
+    if (!w.ok || w.rows <= kFewRows) return;
+    const int filled = (w.rows + kTileRows - 1) / kTileRows * kTileRows;      // zeros behind the last row: tiles are read whole
     if ((int)blockIdx.x * kQueryTokens * w.rep >= filled) return;
     const int i = blockIdx.x * kQueryTokens + unit, pos = w.s.len - w.m + i;
     const int h0 = blockIdx.y * plan.heads, h1 = min(h0 + plan.heads, p.cfg.n_q_heads);
@@ -116,8 +570,7 @@ __global__ void __launch_bounds__(kQueryThreads) weight_queries_kernel(const __g
         const bool counts = odd == 0u && fabsf(lse) < CUDART_INF_F;
 #pragma unroll
         for (int d = 1; d < 16; d <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
-        float up = 1.f;      // the row's largest to [2^13, 2^14): exact, whatever the type's range
-        if (mx > 0.f && counts) up = __int_as_float((127 + min(13 - (__float_as_int(mx) >> 23) + 127, 60)) << 23);
+        const float up = counts ? row_factor(mx) : 1.f;
         float sum = 0.f;
 #pragma unroll
         for (int j = 0; j < C; ++j) {
@@ -129,18 +582,18 @@ __global__ void __launch_bounds__(kQueryThreads) weight_queries_kernel(const __g
         for (int d = 1; d < 16 / NG; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
         const int r = i * w.rep + h - hk * w.rep;
         if (r >= filled) continue;
-        uint8_t *tile = const_cast<uint8_t *>(query_tile(plan, w, b, hk, r / plan.tile_rows));
-        const int tr = r % plan.tile_rows;
-        uint8_t *dst = tile + (c0 >> 6) * plan.tile_rows * 128 + tr * 128 + (((((c0 >> 3) & 7) ^ (tr & 7)) << 4)) + (c0 & 7) * 2;
+        uint8_t *tile = const_cast<uint8_t *>(query_tile(plan, w, b, hk, r / kTileRows));
+        const int tr = r % kTileRows;
+        uint8_t *dst = tile + (c0 >> 6) * kTileRows * 128 + tr * 128 + (((((c0 >> 3) & 7) ^ (tr & 7)) << 4)) + (c0 & 7) * 2;
         if constexpr (C == 8)
             *reinterpret_cast<uint4 *>(dst) = make_uint4(packed<__half>(x[0], x[1]), packed<__half>(x[2], x[3]), packed<__half>(x[4], x[5]), packed<__half>(x[6], x[7]));
         else *reinterpret_cast<uint2 *>(dst) = make_uint2(packed<__half>(x[0], x[1]), packed<__half>(x[2], x[3]));
-        float *constants = reinterpret_cast<float *>(tile + plan.tile_rows * D * 2) + tr;
+        float *constants = reinterpret_cast<float *>(tile + kTileRows * D * 2) + tr;
         if (sub == 0) {
             constants[0] = a.sm_scale * 1.4426950408889634f / up;
-            constants[plan.tile_rows] = counts ? lse * -1.4426950408889634f : -CUDART_INF_F;
+            constants[kTileRows] = counts ? lse * -1.4426950408889634f : -CUDART_INF_F;
         }
-        if (sub % (16 / NG) == 0) constants[(2 + sub / (16 / NG)) * plan.tile_rows] = sum;
+        if (sub % (16 / NG) == 0) constants[(2 + sub / (16 / NG)) * kTileRows] = sum;
     }
 }
 
@@ -160,13 +613,9 @@ __global__ void __launch_bounds__(kThreads) weight_tokens_kernel(const __grid_co
     const int b = blockIdx.z, h = blockIdx.y, token = threadIdx.x % kTokens, quarter = threadIdx.x / kTokens, t = blockIdx.x * kTokens + token;
     WeightSeq w;
     weight_sequence(a, b, w);
-    if (!w.ok) {
-        if (threadIdx.x == 0) set_status(a.p.c.status, SKVQ_STATUS_BAD_BATCH);
-        return;
-    }
-    if ((int)blockIdx.x * kTokens >= w.s.len) return;
+    if (!w.ok || w.rows <= kFewRows || (int)blockIdx.x * kTokens >= w.s.len) return;
     const int P = cfg.page_tokens;
-    bool have = t < w.s.len && w.rows > 0;
+    bool have = t < w.s.len;
     if (have) {
         const int page = a.p.batch.page_table[(int64_t)b * a.p.batch.max_pages + t / P];
         if (page < 0 || page >= cfg.n_pages) {
@@ -194,12 +643,12 @@ __global__ void __launch_bounds__(kThreads) weight_tokens_kernel(const __grid_co
     for (int r0 = 0; r0 < w.rows; r0 += 8) {
         __syncthreads();
         for (int e = threadIdx.x; e < 8 * D; e += kThreads) {
-            const int r = r0 + e / D, c = e % D, tr = r % plan.tile_rows;
+            const int r = r0 + e / D, c = e % D, tr = r % kTileRows;
             if (r >= w.rows) break;
-            const uint8_t *tile = query_tile(plan, w, b, h, r / plan.tile_rows);
+            const uint8_t *tile = query_tile(plan, w, b, h, r / kTileRows);
             query[e / D][(c & ~7) + channel_at(c & 7)] = __half2float(*reinterpret_cast<const __half *>(
-                tile + (c >> 6) * plan.tile_rows * 128 + tr * 128 + ((((c >> 3) & 7) ^ (tr & 7)) << 4) + (c & 7) * 2));
-            if (c < 2 + NG) constants[e / D][c] = reinterpret_cast<const float *>(tile + plan.tile_rows * D * 2)[c * plan.tile_rows + tr];
+                tile + (c >> 6) * kTileRows * 128 + tr * 128 + ((((c >> 3) & 7) ^ (tr & 7)) << 4) + (c & 7) * 2));
+            if (c < 2 + NG) constants[e / D][c] = reinterpret_cast<const float *>(tile + kTileRows * D * 2)[c * kTileRows + tr];
         }
         __syncthreads();
         for (int k = quarter; k < min(8, w.rows - r0); k += 4) {
@@ -219,15 +668,36 @@ __global__ void __launch_bounds__(kThreads) weight_tokens_kernel(const __grid_co
     }
 }
 
-// The layout of the query tiles.
-void plan_tiles(const skvq_paged_config &cfg, const skvq_paged_batch &batch, int last, WeightPlan &p, int64_t &tiles)
+// The most counted rows that a KV head of a sequence can have.
+int64_t most_rows(const skvq_paged_config &cfg, const skvq_paged_batch &batch, int last)
 {
-    const int64_t rep = cfg.n_q_heads / cfg.n_kv_heads, most = last && last < batch.max_new ? last : batch.max_new;
-    p.tile_rows = most * rep <= 16 ? 16 : kTileRows;
-    const int64_t uniform = (most * rep + p.tile_rows - 1) / p.tile_rows, together = batch.n_tokens * rep / p.tile_rows + batch.n_seqs;
-    const bool by_seq = uniform * batch.n_seqs <= together || (last && last < batch.max_new);
-    p.seq_tiles = by_seq ? (int)uniform : 0;
-    tiles = by_seq ? uniform * batch.n_seqs : together;
+    return (int64_t)(last && last < batch.max_new ? last : batch.max_new) * (cfg.n_q_heads / cfg.n_kv_heads);
+}
+// The layout of the query tiles: the smaller of a fixed number per sequence and one after the other.
+int64_t query_tiles(const skvq_paged_config &cfg, const skvq_paged_batch &batch, int last, int &seq_tiles)
+{
+    const int64_t rows = most_rows(cfg, batch, last), uniform = (rows + kTileRows - 1) / kTileRows * batch.n_seqs;
+    const int64_t together = (int64_t)batch.n_tokens * (cfg.n_q_heads / cfg.n_kv_heads) / kTileRows + batch.n_seqs;
+    seq_tiles = 0;
+    if (rows <= kFewRows) return 0;
+    if (uniform <= together || (last && last < batch.max_new)) seq_tiles = (int)(uniform / batch.n_seqs);
+    return seq_tiles ? uniform : together;
+}
+
+template <typename T, int D, int NG, int NT> cudaError_t launch_few(const WeightPlan &p, cudaStream_t stream)
+{
+    using Geo = FewGeo<D, NG, NT>;
+    const skvq_paged_config &cfg = p.a.p.cfg;
+    const skvq_paged_batch &batch = p.a.p.batch;
+    static unsigned long long done = 0;
+    const cudaError_t e = configure_smem_once(weight_few_kernel<T, D, NG, NT>, Geo::SMEM + (int)sizeof(long long) * (kMaxPagedSeqs + 1), done);
+    if (e != cudaSuccess) return e;
+    // one wave of resident CTAs, no more warps than tiles
+    const long long lq = batch.max_len > cfg.window ? batch.max_len - cfg.window : 0;
+    const long long tiles = (lq + kTile - 1) / kTile + kRingCost * ((batch.max_len - lq + kRingTile - 1) / kRingTile);
+    const long long wave = (NT == 1 ? 5LL : 4LL) * sm_count(), useful = ((long long)batch.n_seqs * cfg.n_kv_heads * tiles + kFewWarps - 1) / kFewWarps;
+    return launch_chained(weight_few_kernel<T, D, NG, NT>, dim3((unsigned)(useful < wave ? useful : wave)), kFewThreads,
+                          Geo::SMEM + sizeof(long long) * (batch.n_seqs + 1), stream, p);
 }
 
 template <typename T, int D, int NG> cudaError_t launch_weights(const PagedWeightArgs &a, cudaStream_t stream)
@@ -236,18 +706,15 @@ template <typename T, int D, int NG> cudaError_t launch_weights(const PagedWeigh
     const skvq_paged_batch &batch = a.p.batch;
     WeightPlan p{};
     p.a = a;
-    int64_t tiles;
-    plan_tiles(cfg, batch, a.last, p, tiles);
-    cudaError_t e;
-    const int64_t rep = cfg.n_q_heads / cfg.n_kv_heads, most = a.last && a.last < batch.max_new ? a.last : batch.max_new;
-    if (batch.n_tokens > 0 && most > 0) {
-        const int64_t rows = p.tile_rows == kTileRows ? (most * rep + kTileRows - 1) / kTileRows * kTileRows : most * rep;
-        const int64_t chunks = ((rows + rep - 1) / rep + kQueryTokens - 1) / kQueryTokens;
-        p.heads = cfg.n_q_heads;
-        while (p.heads > 4 && chunks * batch.n_seqs * ((cfg.n_q_heads + p.heads - 1) / p.heads) < 32LL * sm_count()) p.heads = (p.heads + 1) / 2;
-        e = launch_chained(weight_queries_kernel<T, D, NG>, dim3((unsigned)chunks, (cfg.n_q_heads + p.heads - 1) / p.heads, batch.n_seqs), kQueryThreads, 0, stream, p);
-        if (e != cudaSuccess) return e;
-    }
+    query_tiles(cfg, batch, a.last, p.seq_tiles);
+    const int64_t rows = batch.n_tokens > 0 ? most_rows(cfg, batch, a.last) : 0, rep = cfg.n_q_heads / cfg.n_kv_heads;
+    cudaError_t e = rows <= kFewRowTile ? launch_few<T, D, NG, 1>(p, stream) : launch_few<T, D, NG, 2>(p, stream);
+    if (e != cudaSuccess || rows <= kFewRows) return e;
+    const int64_t padded = (rows + kTileRows - 1) / kTileRows * kTileRows, chunks = ((padded + rep - 1) / rep + kQueryTokens - 1) / kQueryTokens;
+    p.heads = cfg.n_q_heads;
+    while (p.heads > 4 && chunks * batch.n_seqs * ((cfg.n_q_heads + p.heads - 1) / p.heads) < 32LL * sm_count()) p.heads = (p.heads + 1) / 2;
+    e = launch_chained(weight_queries_kernel<T, D, NG>, dim3((unsigned)chunks, (cfg.n_q_heads + p.heads - 1) / p.heads, batch.n_seqs), kQueryThreads, 0, stream, p);
+    if (e != cudaSuccess) return e;
     return launch_chained(weight_tokens_kernel<T, D, NG>, dim3((batch.max_len + kTokens - 1) / kTokens, cfg.n_kv_heads, batch.n_seqs), kThreads, 0, stream, p);
 }
 
@@ -262,10 +729,8 @@ template <typename T> cudaError_t launch_by_shape(const PagedWeightArgs &a, cuda
 
 size_t paged_weights_workspace_bytes(const skvq_paged_config &cfg, const skvq_paged_batch &batch, int last)
 {
-    WeightPlan p{};
-    int64_t tiles;
-    plan_tiles(cfg, batch, last, p, tiles);
-    return (size_t)tiles * cfg.n_kv_heads * tile_bytes(p.tile_rows, cfg.head_dim, cfg.head_dim / cfg.group_size);
+    int seq_tiles;
+    return (size_t)query_tiles(cfg, batch, last, seq_tiles) * cfg.n_kv_heads * tile_bytes(cfg.head_dim, cfg.head_dim / cfg.group_size);
 }
 
 cudaError_t launch_paged_weights(const PagedWeightArgs &a, cudaStream_t stream)

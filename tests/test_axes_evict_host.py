@@ -110,8 +110,9 @@ def test_common_refusals(lib, call):
     for name in ("weights", "weights_out"):
         assert call(lib, args={name: FAKE + 2}) == B.SKVQ_ERR_MISALIGNED, name
     assert call(lib, args=dict(workspace=FAKE + 8)) == B.SKVQ_ERR_MISALIGNED
-    assert call(lib, args=dict(workspace=None)) == B.SKVQ_ERR_WORKSPACE
-    assert call(lib, args=dict(workspace_bytes=8)) == B.SKVQ_ERR_WORKSPACE
+    rows = dict(n_tokens=70, max_new=40)      # (few rows need no workspace)
+    assert call(lib, batch=rows, args=dict(workspace=None)) == B.SKVQ_ERR_WORKSPACE
+    assert call(lib, batch=rows, args=dict(workspace_bytes=8)) == B.SKVQ_ERR_WORKSPACE
 
 
 def test_weights_refusals(lib):
@@ -143,7 +144,7 @@ def test_evict_refusals(lib):
 
 
 def test_workspace_sizes(lib):
-    cfg, _, batch = structs()
+    cfg, _, batch = structs(batch=dict(n_tokens=70, max_new=40))
     assert B.skvq_paged_evict_workspace_size(cfg, batch) > 0
     for bad in (dict(n_seqs=0), dict(n_seqs=2049)):
         assert B.skvq_paged_evict_workspace_size(cfg, structs(batch=bad)[2]) == 0
