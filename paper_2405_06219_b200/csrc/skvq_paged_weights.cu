@@ -21,6 +21,7 @@ using mmak::mma16816;
 using mmak::smem_u32;
 
 constexpr float kSubnormal = 1.f / 16777216.f;      // 2^-24: the least fp16 subnormal, what a code's lowest bit stands for as an operand
+constexpr float kZeroScale = 1.f / 1024.f;           // brings 8 times a sum of 128 operands below 2^14 into fp16's range
 constexpr int kQueryThreads = 128;
 constexpr int kQueryTokens = kQueryThreads / 16;
 constexpr int kTileRows = 128;      // rows of a query tile
@@ -68,6 +69,14 @@ __device__ __forceinline__ uint32_t sixteenth(uint32_t v)      // of two fp16
     asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(v), "r"(0x2C002C00u));
     return r;
 }
+// d = a b + c with an accumulator of its own
+__device__ __forceinline__ void mma16816_from(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1, float c0,
+                                              float c1, float c2, float c3)
+{
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%12,%13};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c0), "f"(c1), "f"(c2), "f"(c3));
+}
 __device__ __forceinline__ void load_matrices(uint32_t (&r)[4], uint32_t addr)      // four 8 x 8 matrices of 16-bit elements
 {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
@@ -91,8 +100,10 @@ template <> __device__ __forceinline__ uint32_t as_h2<__nv_bfloat16>(uint32_t v)
 // The (sequence, KV head) pairs are laid end to end, priced in 32-token tiles (16 tokens of the unquantized window: kRingCost), and cut into
 // equal runs, one per warp.  A warp streams its tiles through a ring of its own in shared memory; 16 tokens' codes are the A
 // operand of mma.m16n8k16, 8 rows the B operand, one accumulator per group.  A nibble under zeros is an fp16 subnormal, c 2^-24 (or
-// 16 c 2^-24, against q/16), so codes enter the product as they are, exactly; the parameters' factor 2^24 goes to h.  The
-// accumulators start at minus 8 times the sum of the group's q' (and z becomes z + 8 h): sums of codes about their middle, which are as small as the score.
+// 16 c 2^-24, against q/16), so codes enter the product as they are, exactly.  The accumulators start at minus 8 times the sum of the
+// group's q', so they end at sums of codes about their middle, which are as small as the score; what that leaves, the sum over groups of
+// (z + 8 h) sum q', is one more product: the parameters' words are its A operand as they lie in memory, 8 sum q' and sum q' in two fp16
+// parts (22 bits) the B operand.  With at most 4 rows they take every other column, and a lane has one row instead of two.
 constexpr int kFewRowTile = 8;
 constexpr int kTile = 32;
 constexpr int kRingTile = 16;
@@ -101,13 +112,13 @@ constexpr int kFewWarps = 4;
 constexpr int kFewThreads = kFewWarps * 32;
 constexpr int kFewStages = 3;
 
-template <int D, int NG, int NT> struct FewGeo {
+template <int D, int NG, int NT, int E> struct FewGeo {
     static constexpr int ROW = D / 2, CHUNKS = ROW / 16;
     static constexpr int CODES = kTile * ROW, META = kTile * NG * 4, STAGE = CODES + META;
     static constexpr int SETS = D / 32;                      // 32-channel granules: 16-byte pieces of a code row
     static constexpr int RROW = D * 2, RCHUNKS = RROW / 16;
     static constexpr int RING = kFewStages * STAGE;
-    static constexpr int ROWS = kFewRowTile * NT, QROW = D + 8;
+    static constexpr int ROWS = kFewRowTile * NT * E / 2, QROW = D + 8;      // E rows per lane and tile: 2, or 1
     static constexpr int QUERIES = RING, RAW = QUERIES + ROWS * QROW * 2, CONSTANTS = RAW + D * 2;
     static constexpr int WARP = CONSTANTS + ROWS * (2 + NG) * 4;
     static constexpr int SMEM = kFewWarps * WARP;
@@ -129,10 +140,10 @@ __device__ __forceinline__ FewCost few_cost(const PagedWeightArgs &a, const Weig
     return c;
 }
 
-template <typename T, int D, int NG, int NT>
+template <typename T, int D, int NG, int NT, int E>
 __global__ void __launch_bounds__(kFewThreads, NT == 1 ? 5 : 4) weight_few_kernel(const __grid_constant__ WeightPlan plan)
 {
-    using Geo = FewGeo<D, NG, NT>;
+    using Geo = FewGeo<D, NG, NT, E>;
     const PagedWeightArgs &a = plan.a;
     const PagedArgs &p = a.p;
     const skvq_paged_config &cfg = p.cfg;
@@ -327,27 +338,35 @@ __global__ void __launch_bounds__(kFewThreads, NT == 1 ? 5 : 4) weight_few_kerne
             }
             __syncwarp();
         }
-        uint32_t bq[NT][Geo::SETS * 2][2];
-        float rs[NT][2], nl[NT][2], qsum[NT][2][NG];
-        int lim[NT][2];      // of this lane's rows 8 n + 2 j and 8 n + 2 j + 1: they see tokens below it
+        // column g of tile n is row 8 n + g, or, E = 1, row g / 2 where g is even; a lane's columns of the result are 2 j and 2 j + 1
+        uint32_t bq[NT][Geo::SETS * 2][2], bz[NT][2];
+        float rs[NT][E], nl[NT][E], qoff[NT][E][NG];
+        int lim[NT][E];      // this lane's rows see tokens below it
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
+            const int r = E == 2 ? 8 * n + g : g >> 1;
+            const bool column = E == 2 || g % 2 == 0;
 #pragma unroll
             for (int st = 0; st < Geo::SETS; ++st) {
-                const uint4 x = *reinterpret_cast<const uint4 *>(queries + (8 * n + g) * Geo::QROW + 32 * st + 8 * j);
+                uint4 x = *reinterpret_cast<const uint4 *>(queries + r * Geo::QROW + 32 * st + 8 * j);
+                if (!column) x = make_uint4(0u, 0u, 0u, 0u);
                 bq[n][2 * st][0] = x.x;
                 bq[n][2 * st][1] = sixteenth(x.y);
                 bq[n][2 * st + 1][0] = x.z;
                 bq[n][2 * st + 1][1] = sixteenth(x.w);
             }
+            const float q = column && j < NG ? constants[r * (2 + NG) + 2 + j] * kZeroScale : 0.f;      // of group j
+            const float high = __half2float(__float2half_rn(q));
+            bz[n][0] = packed<__half>(8.f * high, high);
+            bz[n][1] = packed<__half>(8.f * (q - high), q - high);
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const int r = 8 * n + 2 * j + e;
-                rs[n][e] = constants[r * (2 + NG)];
-                nl[n][e] = constants[r * (2 + NG) + 1];
+            for (int e = 0; e < E; ++e) {
+                const int own = E == 2 ? 8 * n + 2 * j + e : j;
+                rs[n][e] = constants[own * (2 + NG)] * (1.f / kZeroScale);
+                nl[n][e] = constants[own * (2 + NG) + 1];
 #pragma unroll
-                for (int k = 0; k < NG; ++k) qsum[n][e][k] = constants[r * (2 + NG) + 2 + k];
-                lim[n][e] = a.causal ? min(L, L - w.m + min(r, R - 1) / w.rep + 1) : L;
+                for (int k = 0; k < NG; ++k) qoff[n][e][k] = constants[own * (2 + NG) + 2 + k] * (-8.f * kSubnormal);
+                lim[n][e] = a.causal ? min(L, L - w.m + min(own, R - 1) / w.rep + 1) : L;
             }
         }
         const int lowest = a.causal ? min(L, L - w.m + 1) : L;      // the first row's limit
@@ -371,13 +390,13 @@ __global__ void __launch_bounds__(kFewThreads, NT == 1 ? 5 : 4) weight_few_kerne
             float sums[2][2];      // tokens 16 u + g and 16 u + 8 + g
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-                float acc[NT][NG][4];
+                float acc[NT][NG][4], zero[NT][4];
+                {
+                    const int group = NG == 4 ? j : j % NG;
+                    const uint32_t x = km[(16 * u + g) * NG + group], y = km[(16 * u + 8 + g) * NG + group];
 #pragma unroll
-                for (int n = 0; n < NT; ++n)
-#pragma unroll
-                    for (int k = 0; k < NG; ++k)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) acc[n][k][e] = qsum[n][e & 1][k] * (-8.f * kSubnormal);
+                    for (int n = 0; n < NT; ++n) mma16816_from(zero[n], x, y, x, y, bz[n][0], bz[n][1], 0.f, 0.f, 0.f, 0.f);
+                }
 #pragma unroll
                 for (int s2 = 0; s2 < Geo::SETS; s2 += 2) {
                     const int row = 16 * u + matrix_row;
@@ -391,37 +410,47 @@ __global__ void __launch_bounds__(kFewThreads, NT == 1 ? 5 : 4) weight_few_kerne
 #pragma unroll
                         for (int n = 0; n < NT; ++n) {
                             float (&d)[4] = acc[n][st / PER];
-                            mma16816(d, x & 0x000F000Fu, y & 0x000F000Fu, x & 0x00F000F0u, y & 0x00F000F0u, bq[n][2 * st][0], bq[n][2 * st][1]);
+                            const uint32_t x0 = x & 0x000F000Fu, y0 = y & 0x000F000Fu, x1 = x & 0x00F000F0u, y1 = y & 0x00F000F0u;
+                            if (st % PER == 0)
+                                mma16816_from(d, x0, y0, x1, y1, bq[n][2 * st][0], bq[n][2 * st][1], qoff[n][0][st / PER], E == 2 ? qoff[n][E - 1][st / PER] : 0.f,
+                                              qoff[n][0][st / PER], E == 2 ? qoff[n][E - 1][st / PER] : 0.f);
+                            else mma16816(d, x0, y0, x1, y1, bq[n][2 * st][0], bq[n][2 * st][1]);
                             mma16816(d, xs & 0x000F000Fu, ys & 0x000F000Fu, xs & 0x00F000F0u, ys & 0x00F000F0u, bq[n][2 * st + 1][0], bq[n][2 * st + 1][1]);
                         }
                     }
                 }
-                float h[2][NG], z[2][NG];
-#pragma unroll
-                for (int half = 0; half < 2; ++half)
-#pragma unroll
-                    for (int k = 0; k < NG; ++k) {
-                        const float2 m = floats<__half>(km[(16 * u + 8 * half + g) * NG + k]);
-                        z[half][k] = fmaf(8.f, m.x, m.y);
-                        h[half][k] = m.x * (1.f / kSubnormal);
-                    }
+                float s[2][NT][E];
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
-                    float sum = 0.f;
+                    float h[NG];
+#pragma unroll
+                    for (int k = 0; k < NG; ++k) h[k] = floats<__half>(km[(16 * u + 8 * half + g) * NG + k]).x;
 #pragma unroll
                     for (int n = 0; n < NT; ++n)
 #pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            float s = z[half][0] * qsum[n][e][0];
+                        for (int e = 0; e < E; ++e) {
+                            float x = h[0] * acc[n][0][2 * half + e];
 #pragma unroll
-                            for (int k = 1; k < NG; ++k) s = fmaf(z[half][k], qsum[n][e][k], s);
-#pragma unroll
-                            for (int k = 0; k < NG; ++k) s = fmaf(h[half][k], acc[n][k][2 * half + e], s);
-                            s = fmaf(s, rs[n][e], nl[n][e]);
-                            if (edge && (t0 + 16 * u + 8 * half + g >= min(lq, lim[n][e]) || ((bad_here >> u) & 1u))) s = -CUDART_INF_F;
-                            sum += ex2_approx(s);
+                            for (int k = 1; k < NG; ++k) x = fmaf(h[k], acc[n][k][2 * half + e], x);
+                            s[half][n][e] = fmaf(fmaf(x, kZeroScale / kSubnormal, zero[n][2 * half + e]), rs[n][e], nl[n][e]);
                         }
-                    sums[u][half] = sum;
+                }
+                if (edge) {
+#pragma unroll
+                    for (int half = 0; half < 2; ++half)
+#pragma unroll
+                        for (int n = 0; n < NT; ++n)
+#pragma unroll
+                            for (int e = 0; e < E; ++e)
+                                if (t0 + 16 * u + 8 * half + g >= min(lq, lim[n][e]) || ((bad_here >> u) & 1u)) s[half][n][e] = -CUDART_INF_F;
+                }
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    sums[u][half] = 0.f;
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int e = 0; e < E; ++e) sums[u][half] += ex2_approx(s[half][n][e]);
                 }
             }
             // lane (g, j) gets token 8 j + g, added up over the lanes that hold the other rows
@@ -483,7 +512,8 @@ __global__ void __launch_bounds__(kFewThreads, NT == 1 ? 5 : 4) weight_few_kerne
                 }
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
-                    const uint4 q = *reinterpret_cast<const uint4 *>(queries + (8 * n + g) * Geo::QROW + 32 * st + 8 * j);
+                    uint4 q = *reinterpret_cast<const uint4 *>(queries + (E == 2 ? 8 * n + g : g >> 1) * Geo::QROW + 32 * st + 8 * j);
+                    if (E == 1 && g % 2) q = make_uint4(0u, 0u, 0u, 0u);
                     mma16816(s[n], x[0][0], x[1][0], x[0][1], x[1][1], q.x, q.y);
                     mma16816(s[n], x[0][2], x[1][2], x[0][3], x[1][3], q.z, q.w);
                 }
@@ -492,11 +522,13 @@ __global__ void __launch_bounds__(kFewThreads, NT == 1 ? 5 : 4) weight_few_kerne
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int at = g + 8 * (e >> 1);
-                    const bool hidden = t0 + at >= lim[n][e & 1] || ((gone >> at) & 1u);      // rows behind the last token were not copied
-                    sums[e >> 1] += hidden ? 0.f : ex2_approx(fmaf(s[n][e], rs[n][e & 1], nl[n][e & 1]));
-                }
+                for (int half = 0; half < 2; ++half)
+#pragma unroll
+                    for (int e = 0; e < E; ++e) {
+                        const int at = g + 8 * half;
+                        const bool hidden = t0 + at >= lim[n][e] || ((gone >> at) & 1u);      // rows behind the last token were not copied
+                        sums[half] += hidden ? 0.f : ex2_approx(fmaf(s[n][2 * half + e], rs[n][e] * kZeroScale, nl[n][e]));
+                    }
             const bool odd = j & 1;
             float x = (odd ? sums[1] : sums[0]) + __shfl_xor_sync(0xffffffffu, odd ? sums[0] : sums[1], 1);
             x += __shfl_xor_sync(0xffffffffu, x, 2);
@@ -684,19 +716,19 @@ int64_t query_tiles(const skvq_paged_config &cfg, const skvq_paged_batch &batch,
     return seq_tiles ? uniform : together;
 }
 
-template <typename T, int D, int NG, int NT> cudaError_t launch_few(const WeightPlan &p, cudaStream_t stream)
+template <typename T, int D, int NG, int NT, int E> cudaError_t launch_few(const WeightPlan &p, cudaStream_t stream)
 {
-    using Geo = FewGeo<D, NG, NT>;
+    using Geo = FewGeo<D, NG, NT, E>;
     const skvq_paged_config &cfg = p.a.p.cfg;
     const skvq_paged_batch &batch = p.a.p.batch;
     static unsigned long long done = 0;
-    const cudaError_t e = configure_smem_once(weight_few_kernel<T, D, NG, NT>, Geo::SMEM + (int)sizeof(long long) * (kMaxPagedSeqs + 1), done);
+    const cudaError_t e = configure_smem_once(weight_few_kernel<T, D, NG, NT, E>, Geo::SMEM + (int)sizeof(long long) * (kMaxPagedSeqs + 1), done);
     if (e != cudaSuccess) return e;
     // one wave of resident CTAs, no more warps than tiles
     const long long lq = batch.max_len > cfg.window ? batch.max_len - cfg.window : 0;
     const long long tiles = (lq + kTile - 1) / kTile + kRingCost * ((batch.max_len - lq + kRingTile - 1) / kRingTile);
     const long long wave = (NT == 1 ? 5LL : 4LL) * sm_count(), useful = ((long long)batch.n_seqs * cfg.n_kv_heads * tiles + kFewWarps - 1) / kFewWarps;
-    return launch_chained(weight_few_kernel<T, D, NG, NT>, dim3((unsigned)(useful < wave ? useful : wave)), kFewThreads,
+    return launch_chained(weight_few_kernel<T, D, NG, NT, E>, dim3((unsigned)(useful < wave ? useful : wave)), kFewThreads,
                           Geo::SMEM + sizeof(long long) * (batch.n_seqs + 1), stream, p);
 }
 
@@ -708,7 +740,7 @@ template <typename T, int D, int NG> cudaError_t launch_weights(const PagedWeigh
     p.a = a;
     query_tiles(cfg, batch, a.last, p.seq_tiles);
     const int64_t rows = batch.n_tokens > 0 ? most_rows(cfg, batch, a.last) : 0, rep = cfg.n_q_heads / cfg.n_kv_heads;
-    cudaError_t e = rows <= kFewRowTile ? launch_few<T, D, NG, 1>(p, stream) : launch_few<T, D, NG, 2>(p, stream);
+    cudaError_t e = rows <= kFewRowTile / 2 ? launch_few<T, D, NG, 1, 1>(p, stream) : rows <= kFewRowTile ? launch_few<T, D, NG, 1, 2>(p, stream) : launch_few<T, D, NG, 2, 2>(p, stream);
     if (e != cudaSuccess || rows <= kFewRows) return e;
     const int64_t padded = (rows + kTileRows - 1) / kTileRows * kTileRows, chunks = ((padded + rep - 1) / rep + kQueryTokens - 1) / kQueryTokens;
     p.heads = cfg.n_q_heads;
