@@ -21,7 +21,7 @@ using mmak::mma16816;
 using mmak::smem_u32;
 
 constexpr float kSubnormal = 1.f / 16777216.f;      // 2^-24: the least fp16 subnormal, what a code's lowest bit stands for as an operand
-constexpr float kZeroScale = 1.f / 1024.f;           // brings 8 times a sum of 128 operands below 2^14 into fp16's range
+constexpr float kZeroScale = 1.f / 1024.f;           // brings a sum of 128 operands below 2^14 into fp16's range
 constexpr int kQueryThreads = 128;
 constexpr int kQueryTokens = kQueryThreads / 16;
 constexpr int kTileRows = 128;      // rows of a query tile
@@ -100,10 +100,9 @@ template <> __device__ __forceinline__ uint32_t as_h2<__nv_bfloat16>(uint32_t v)
 // The (sequence, KV head) pairs are laid end to end, priced in 32-token tiles (16 tokens of the unquantized window: kRingCost), and cut into
 // equal runs, one per warp.  A warp streams its tiles through a ring of its own in shared memory; 16 tokens' codes are the A
 // operand of mma.m16n8k16, 8 rows the B operand, one accumulator per group.  A nibble under zeros is an fp16 subnormal, c 2^-24 (or
-// 16 c 2^-24, against q/16), so codes enter the product as they are, exactly.  The accumulators start at minus 8 times the sum of the
-// group's q', so they end at sums of codes about their middle, which are as small as the score; what that leaves, the sum over groups of
-// (z + 8 h) sum q', is one more product: the parameters' words are its A operand as they lie in memory, 8 sum q' and sum q' in two fp16
-// parts (22 bits) the B operand.  With at most 4 rows they take every other column, and a lane has one row instead of two.
+// 16 c 2^-24, against q/16), so codes enter the product as they are, exactly.  The zero points' share, the sum over groups of z sum q',
+// is one more product: the parameters' words {h, z} are its A operand as they lie in memory, {0, sum q'} in two fp16 parts (22 bits)
+// the B operand.  With at most 4 rows they take every other column, and a lane has one row instead of two.
 constexpr int kFewRowTile = 8;
 constexpr int kTile = 32;
 constexpr int kRingTile = 16;
@@ -226,43 +225,50 @@ __global__ void __launch_bounds__(kFewThreads, NT == 1 ? 5 : 4) weight_few_kerne
             continue;
         }
         const int32_t *table = p.batch.page_table + (int64_t)b * p.batch.max_pages;
-        // Page ids of 32 consecutive 16-token blocks, one per lane; -1 past the quantized tokens, -2 for an id outside the pool.
+        // The pool's row of the first token of 32 consecutive 16-token blocks, one per lane; negative past the quantized tokens and
+        // for an id outside the pool.
         auto load_pages = [&](int block) {
             const int t = (block + lane) * 16;
-            int id = -1;
+            long long row = -1;
             if (t < lq) {
-                id = table[t >> page_shift];
-                if (id < 0 || id >= cfg.n_pages) { id = -2; set_status(p.c.status, SKVQ_STATUS_BAD_PAGE); }
+                const int id = table[t >> page_shift];
+                if (id >= 0 && id < cfg.n_pages) row = ((long long)id * H + hk) * P + (t & (P - 1));
+                else set_status(p.c.status, SKVQ_STATUS_BAD_PAGE);
             }
-            return id;
+            return row;
         };
-        int pages_base = q0 * 2, pages = q0 < q1 ? load_pages(pages_base) : -1, pages_next = q0 < q1 ? load_pages(pages_base + 32) : -1;
+        int block = q0 * 2 & 31;      // the next tile's first block among the 32
+        long long pages = -1, pages_next = -1;
+        if (q0 < q1) {
+            pages = load_pages(q0 * 2 - block);
+            pages_next = load_pages(q0 * 2 - block + 32);
+        }
         uint32_t bad = 0;      // bit 2 * stage + block: the block has no page
-        const uint32_t codes_dst = (lane / Geo::CHUNKS) * Geo::ROW;
+        const uint8_t *codes_src = static_cast<const uint8_t *>(p.c.k_codes) + lane * 16, *meta_src = static_cast<const uint8_t *>(p.c.k_meta) + lane * 16;
+        const uint32_t codes_dst = ring + (lane / Geo::CHUNKS) * Geo::ROW + piece_at<D>(lane / Geo::CHUNKS, lane % Geo::CHUNKS) * 16, meta_dst = ring + Geo::CODES + lane * 16;
         auto fetch = [&](int tile, int stage) {
             if (tile < q1) {
-                if (tile * 2 >= pages_base + 32) {
-                    pages_base += 32;
+                if (block == 32) {
+                    block = 0;
                     pages = pages_next;
-                    pages_next = load_pages(pages_base + 32);
+                    pages_next = load_pages(tile * 2 + 32);
                 }
-                const uint32_t base = ring + stage * Geo::STAGE;
-                uint32_t none = 0;
+                bad &= ~(3u << (2 * stage));
                 constexpr int HALF = Geo::CHUNKS / 2, STEP = 32 / Geo::CHUNKS;      // copies of a block; rows that one covers
+                static_assert(STEP % 8 == 0, "the pieces' places repeat every eight rows");
 #pragma unroll
                 for (int blk = 0; blk < 2; ++blk) {
-                    const int id = __shfl_sync(0xffffffffu, pages, tile * 2 + blk - pages_base);
-                    const int64_t at = ((int64_t)id * H + hk) * P + ((tile * kTile + 16 * blk) & (P - 1));
-                    if (id < 0) { none |= 1u << blk; continue; }
-                    const uint8_t *src = static_cast<const uint8_t *>(p.c.k_codes) + at * Geo::ROW + lane * 16;
+                    const long long row = __shfl_sync(0xffffffffu, pages, block + blk);
+                    if (row >= 0) {
 #pragma unroll
-                    for (int k = 0; k < HALF; ++k) {
-                        const int row = 16 * blk + k * STEP + lane / Geo::CHUNKS;
-                        cp16(base + codes_dst + (16 * blk + k * STEP) * Geo::ROW + piece_at<D>(row, lane % Geo::CHUNKS) * 16, src + k * 512);
+                        for (int k = 0; k < HALF; ++k)
+                            cp16(codes_dst + stage * Geo::STAGE + (16 * blk + k * STEP) * Geo::ROW, codes_src + row * Geo::ROW + k * 512);
+                        if (lane < 4 * NG) cp16(meta_dst + stage * Geo::STAGE + blk * (64 * NG), meta_src + row * (NG * 4));
+                    } else {
+                        bad |= 1u << (2 * stage + blk);
                     }
-                    if (lane < 4 * NG) cp16(base + Geo::CODES + blk * (64 * NG) + lane * 16, static_cast<const uint8_t *>(p.c.k_meta) + at * (NG * 4) + lane * 16);
                 }
-                bad = (bad & ~(3u << (2 * stage))) | none << (2 * stage);
+                block += 2;
             }
             cp_commit();
         };
@@ -340,7 +346,7 @@ __global__ void __launch_bounds__(kFewThreads, NT == 1 ? 5 : 4) weight_few_kerne
         }
         // column g of tile n is row 8 n + g, or, E = 1, row g / 2 where g is even; a lane's columns of the result are 2 j and 2 j + 1
         uint32_t bq[NT][Geo::SETS * 2][2], bz[NT][2];
-        float rs[NT][E], nl[NT][E], qoff[NT][E][NG];
+        float rs[NT][E], nl[NT][E];
         int lim[NT][E];      // this lane's rows see tokens below it
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
@@ -357,15 +363,13 @@ __global__ void __launch_bounds__(kFewThreads, NT == 1 ? 5 : 4) weight_few_kerne
             }
             const float q = column && j < NG ? constants[r * (2 + NG) + 2 + j] * kZeroScale : 0.f;      // of group j
             const float high = __half2float(__float2half_rn(q));
-            bz[n][0] = packed<__half>(8.f * high, high);
-            bz[n][1] = packed<__half>(8.f * (q - high), q - high);
+            bz[n][0] = packed<__half>(0.f, high);
+            bz[n][1] = packed<__half>(0.f, q - high);
 #pragma unroll
             for (int e = 0; e < E; ++e) {
                 const int own = E == 2 ? 8 * n + 2 * j + e : j;
                 rs[n][e] = constants[own * (2 + NG)] * (1.f / kZeroScale);
                 nl[n][e] = constants[own * (2 + NG) + 1];
-#pragma unroll
-                for (int k = 0; k < NG; ++k) qoff[n][e][k] = constants[own * (2 + NG) + 2 + k] * (-8.f * kSubnormal);
                 lim[n][e] = a.causal ? min(L, L - w.m + min(own, R - 1) / w.rep + 1) : L;
             }
         }
@@ -411,9 +415,7 @@ __global__ void __launch_bounds__(kFewThreads, NT == 1 ? 5 : 4) weight_few_kerne
                         for (int n = 0; n < NT; ++n) {
                             float (&d)[4] = acc[n][st / PER];
                             const uint32_t x0 = x & 0x000F000Fu, y0 = y & 0x000F000Fu, x1 = x & 0x00F000F0u, y1 = y & 0x00F000F0u;
-                            if (st % PER == 0)
-                                mma16816_from(d, x0, y0, x1, y1, bq[n][2 * st][0], bq[n][2 * st][1], qoff[n][0][st / PER], E == 2 ? qoff[n][E - 1][st / PER] : 0.f,
-                                              qoff[n][0][st / PER], E == 2 ? qoff[n][E - 1][st / PER] : 0.f);
+                            if (st % PER == 0) mma16816_from(d, x0, y0, x1, y1, bq[n][2 * st][0], bq[n][2 * st][1], 0.f, 0.f, 0.f, 0.f);
                             else mma16816(d, x0, y0, x1, y1, bq[n][2 * st][0], bq[n][2 * st][1]);
                             mma16816(d, xs & 0x000F000Fu, ys & 0x000F000Fu, xs & 0x00F000F0u, ys & 0x00F000F0u, bq[n][2 * st + 1][0], bq[n][2 * st + 1][1]);
                         }
