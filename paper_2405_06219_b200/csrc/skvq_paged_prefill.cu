@@ -35,7 +35,8 @@ namespace {
 using mmak::and_or;
 using mmak::ex2_approx;
 using mmak::mbar_init;
-using mmak::mbar_try_wait;
+using mmak::mbar_arrive;
+using mmak::mbar_wait_cycles;
 using mmak::smem_u32;
 using namespace tc5;
 
@@ -65,56 +66,6 @@ struct PGeo {
     static constexpr int TMEM_S = 0, TMEM_O = 256;             // columns: S (P in place) 2 blocks x 2 halves x 64, O 2 x D
 };
 
-// Shared-memory matrix descriptors in the 128-byte swizzle.  K-major: 8-row groups 1024 bytes apart.  MN-major: 64-element runs of
-// the MN dimension `mn_stride` bytes apart, groups of 8 along K 1024 bytes apart.
-__device__ __forceinline__ uint64_t desc_k_major(uint32_t addr)
-{
-    return (uint64_t)((addr >> 4) & 0x3FFFu) | ((uint64_t)1 << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
-}
-__device__ __forceinline__ uint64_t desc_mn_major(uint32_t addr, uint32_t mn_stride)
-{
-    return (uint64_t)((addr >> 4) & 0x3FFFu) | ((uint64_t)(mn_stride >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
-}
-// D (tensor memory) = A (tensor memory, fp16 pairs along the columns) B + D
-__device__ __forceinline__ void umma_f16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc, uint32_t accumulate)
-{
-    asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
-                 " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}"
-                 ::"r"(d_tmem), "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
-}
-__device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t (&r)[32])
-{
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,"
-                 "%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};"
-                 ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
-                 "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
-                 "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
-                 "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]) : "memory");
-}
-__device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t (&r)[16])
-{
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
-                 ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
-                 "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
-}
-__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-// Waits for this thread's tensor-memory loads; the registers that were in flight pass through the statement.
-__device__ __forceinline__ void tmem_wait_ld32(float (&r)[32])
-{
-    asm volatile("tcgen05.wait::ld.sync.aligned;"
-                 : "+f"(r[0]), "+f"(r[1]), "+f"(r[2]), "+f"(r[3]), "+f"(r[4]), "+f"(r[5]), "+f"(r[6]), "+f"(r[7]),
-                   "+f"(r[8]), "+f"(r[9]), "+f"(r[10]), "+f"(r[11]), "+f"(r[12]), "+f"(r[13]), "+f"(r[14]), "+f"(r[15]),
-                   "+f"(r[16]), "+f"(r[17]), "+f"(r[18]), "+f"(r[19]), "+f"(r[20]), "+f"(r[21]), "+f"(r[22]), "+f"(r[23]),
-                   "+f"(r[24]), "+f"(r[25]), "+f"(r[26]), "+f"(r[27]), "+f"(r[28]), "+f"(r[29]), "+f"(r[30]), "+f"(r[31])
-                 :: "memory");
-}
-__device__ __forceinline__ bool elect_one()      // true in one lane of a converged warp
-{
-    uint32_t r;
-    asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(r));
-    return r != 0;
-}
-__device__ __forceinline__ void mbar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
 __device__ __forceinline__ uint32_t h2(float lo, float hi)
 {
     uint32_t r;
@@ -136,19 +87,6 @@ __device__ __forceinline__ uint32_t h2_fma(uint32_t a, uint32_t b, uint32_t c)
 template <typename T> __device__ __forceinline__ uint32_t to_h2(uint32_t v);      // see as_h2 of the kernel for few rows
 template <> __device__ __forceinline__ uint32_t to_h2<__half>(uint32_t v) { return v; }
 template <> __device__ __forceinline__ uint32_t to_h2<__nv_bfloat16>(uint32_t v) { return h2(__uint_as_float(v << 16), __uint_as_float(v & 0xFFFF0000u)); }
-
-// Poll with a limit in clock cycles (about a tenth of a second); false: it ran out.
-__device__ __forceinline__ bool mbar_wait_cycles(uint32_t bar, uint32_t parity)
-{
-    if (mbar_try_wait(bar, parity)) return true;
-    const long long t0 = clock64();
-    for (;;) {
-#pragma unroll 1
-        for (int i = 0; i < 64; ++i)
-            if (mbar_try_wait(bar, parity)) return true;
-        if (clock64() - t0 > 200000000ll) return false;
-    }
-}
 
 // 2^a and 2^b by multiply-adds: x = n + f with n the nearest integer, a polynomial of degree 4 for 2^f on [-1/2, 1/2] (fitted for the
 // smallest relative error: 3e-6, a hundredth of the fp16 step that the result is rounded to), n added to the exponent.  Arguments below

@@ -12,13 +12,20 @@
 #include "skvq_mma_common.cuh"
 #include "skvq_paged.cuh"
 #include "skvq_paged_split.cuh"
+#include "skvq_tcgen05.cuh"
 
 namespace skvq {
 namespace {
 
+using mmak::bulk_g2s;
 using mmak::ex2_approx;
+using mmak::mbar_arrive;
+using mmak::mbar_expect_tx;
+using mmak::mbar_init;
+using mmak::mbar_wait_cycles;
 using mmak::mma16816;
 using mmak::smem_u32;
+using namespace tc5;
 
 constexpr float kSubnormal = 1.f / 16777216.f;      // 2^-24: the least fp16 subnormal, what a code's lowest bit stands for as an operand
 constexpr float kZeroScale = 1.f / 1024.f;           // brings a sum of 128 operands below 2^14 into fp16's range
@@ -27,14 +34,14 @@ constexpr int kQueryTokens = kQueryThreads / 16;
 constexpr int kTileRows = 128;      // rows of a query tile
 
 // A query tile: kTileRows rows of D fp16, 64-channel halves one after the other, a half's rows 128 bytes each with 16-byte piece c of row r
-// at c ^ (r & 7) (the 128-byte swizzle of the tensor core's operands); then floats [kTileRows] factor of a score in units of log2,
-// [kTileRows] minus the lse in units of log2 (minus infinity: the row adds nothing), [NG][kTileRows] sums of the row over a group's channels.
+// at c ^ (r & 7) (the 128-byte swizzle of the tensor core's operands); then for every two rows four floats: the factors of their scores in
+// units of log2, minus their lse in units of log2 (minus infinity: the row adds nothing).
 struct WeightPlan {
     PagedWeightArgs a;
     int seq_tiles;        // > 0: sequence b's tiles begin at b * seq_tiles; 0: at starts[b] * Hq/Hkv / kTileRows + b
     int heads;            // query heads that a CTA of the first kernel walks over
 };
-__host__ __device__ constexpr int tile_bytes(int D, int ng) { return kTileRows * (D * 2 + (2 + ng) * 4); }
+__host__ __device__ constexpr int tile_bytes(int D) { return kTileRows * (D * 2 + 8); }
 
 // What a sequence contributes.
 struct WeightSeq {
@@ -52,7 +59,14 @@ __device__ __forceinline__ void weight_sequence(const PagedWeightArgs &a, int b,
 __device__ __forceinline__ const uint8_t *query_tile(const WeightPlan &p, const WeightSeq &w, int b, int h, int tile)
 {
     const int64_t base = p.seq_tiles ? (int64_t)b * p.seq_tiles : (int64_t)w.s.row0 * w.rep / kTileRows + b;
-    return p.a.ws + ((base + tile) * p.a.p.cfg.n_kv_heads + h) * tile_bytes(p.a.p.cfg.head_dim, p.a.p.ng);
+    return p.a.ws + ((base + tile) * p.a.p.cfg.n_kv_heads + h) * tile_bytes(p.a.p.cfg.head_dim);
+}
+
+// Token t of KV head h gains `sum`; an old entry of a new token is not read.
+__device__ __forceinline__ void write_weight(const PagedWeightArgs &a, const WeightSeq &w, int h, int t, float sum)
+{
+    const int64_t at = ((int64_t)w.s.slot * a.p.cfg.n_kv_heads + h) * a.capacity + t;
+    a.w_out[at] = (a.w_in && t < w.s.len - w.s.n ? a.w_in[at] : 0.f) + sum;
 }
 
 // Position 0..7 inside a run of eight operand channels -> stored channel: nibbles i and i + 4 of a code word become neighbours.
@@ -139,8 +153,12 @@ __device__ __forceinline__ FewCost few_cost(const PagedWeightArgs &a, const Weig
     return c;
 }
 
+template <int N> struct alignas(4 * N) Words { uint32_t w[N]; };
+
+constexpr int kFewCtas = 4;      // per SM: 128 registers a thread; with 5 (spills) the serving mix took 301 us against 306, 4 x 131072 tokens 91 against 88
+
 template <typename T, int D, int NG, int NT, int E>
-__global__ void __launch_bounds__(kFewThreads, NT == 1 ? 5 : 4) weight_few_kernel(const __grid_constant__ WeightPlan plan)
+__global__ void __launch_bounds__(kFewThreads, kFewCtas) weight_few_kernel(const __grid_constant__ WeightPlan plan)
 {
     using Geo = FewGeo<D, NG, NT, E>;
     const PagedWeightArgs &a = plan.a;
@@ -425,8 +443,11 @@ __global__ void __launch_bounds__(kFewThreads, NT == 1 ? 5 : 4) weight_few_kerne
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
                     float h[NG];
+                    {
+                        const Words<NG> m = reinterpret_cast<const Words<NG> *>(km)[16 * u + 8 * half + g];
 #pragma unroll
-                    for (int k = 0; k < NG; ++k) h[k] = floats<__half>(km[(16 * u + 8 * half + g) * NG + k]).x;
+                        for (int k = 0; k < NG; ++k) h[k] = floats<__half>(m.w[k]).x;
+                    }
 #pragma unroll
                     for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -542,7 +563,7 @@ __global__ void __launch_bounds__(kFewThreads, NT == 1 ? 5 : 4) weight_few_kerne
 
 // ------------------------------------------------------------------------------------------------ many rows: prompts and chunks
 // Sixteen lanes own a row; a half-warp takes a token and walks over heads with the token's angles in registers.
-template <typename T, int D, int NG>
+template <typename T, int D>
 __global__ void __launch_bounds__(kQueryThreads) weight_queries_kernel(const __grid_constant__ WeightPlan plan)
 {
     using R = Row<T, D>;
@@ -605,15 +626,8 @@ __global__ void __launch_bounds__(kQueryThreads) weight_queries_kernel(const __g
 #pragma unroll
         for (int d = 1; d < 16; d <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
         const float up = counts ? row_factor(mx) : 1.f;
-        float sum = 0.f;
 #pragma unroll
-        for (int j = 0; j < C; ++j) {
-            x[j] = counts ? x[j] * up : 0.f;
-            sum += __half2float(__float2half_rn(x[j]));
-        }
-        // sums of a group's channels: a group is the channels of 16 / NG lanes
-#pragma unroll
-        for (int d = 1; d < 16 / NG; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+        for (int j = 0; j < C; ++j) x[j] = counts ? x[j] * up : 0.f;
         const int r = i * w.rep + h - hk * w.rep;
         if (r >= filled) continue;
         uint8_t *tile = const_cast<uint8_t *>(query_tile(plan, w, b, hk, r / kTileRows));
@@ -622,84 +636,493 @@ __global__ void __launch_bounds__(kQueryThreads) weight_queries_kernel(const __g
         if constexpr (C == 8)
             *reinterpret_cast<uint4 *>(dst) = make_uint4(packed<__half>(x[0], x[1]), packed<__half>(x[2], x[3]), packed<__half>(x[4], x[5]), packed<__half>(x[6], x[7]));
         else *reinterpret_cast<uint2 *>(dst) = make_uint2(packed<__half>(x[0], x[1]), packed<__half>(x[2], x[3]));
-        float *constants = reinterpret_cast<float *>(tile + kTileRows * D * 2) + tr;
         if (sub == 0) {
+            float *constants = reinterpret_cast<float *>(tile + kTileRows * D * 2) + (tr >> 1) * 4 + (tr & 1);
             constants[0] = a.sm_scale * 1.4426950408889634f / up;
-            constants[kTileRows] = counts ? lse * -1.4426950408889634f : -CUDART_INF_F;
+            constants[2] = counts ? lse * -1.4426950408889634f : -CUDART_INF_F;
         }
-        if (sub % (16 / NG) == 0) constants[(2 + sub / (16 / NG)) * kTileRows] = sum;
     }
 }
 
-// A CTA per 64 tokens of a KV head: its keys in shared memory as fp32, a token and a quarter of the rows per thread.
-constexpr int kTokens = 64;
-constexpr int kThreads = 256;
-template <typename T, int D, int NG>
-__global__ void __launch_bounds__(kThreads) weight_tokens_kernel(const __grid_constant__ WeightPlan plan)
+// One CTA per SM works on items: 256 tokens of a KV head (two blocks of 128, a token per lane of the tensor memory) and the query tiles
+// that see them.  Transposed scores, S^T = K~ Q^T: a token's sum over the rows then stays in one thread.  Roles, ordered by mbarriers:
+//   dequantizers  4 warps, two tokens per thread: the key as fp32 h c + z, split into fp16 high and low parts (2^-22 together), both
+//                 into tensor memory as the A operand: 2 D columns of K for a product whose B operand, the queries, is read from
+//                 shared memory alone.
+//   loader        a thread brings query tiles with their rows' constants into a ring, one bulk copy each (they are laid out for it).
+//   issuer        a warp: for each half of a tile (64 rows) and block, S = (high + low) Q^T; a buffer each, so the products run while the
+//                 other half and the other block become probabilities.
+//   exponentials  2 x 4 warps, a block each: scores from tensor memory, exp2(rs s - lse), their sum.
+// Items are laid end to end, priced in query tiles (causal limits included), and cut into equal runs, one per CTA; partial sums of an
+// item that several runs share are added in order by a last kernel.
+constexpr int kBlock = 128;                            // tokens of a block, rows of a query tile
+constexpr int kItemTokens = 2 * kBlock;
+constexpr int kExpThreads = 2 * kBlock;                // warps 0-7
+constexpr int kManyThreads = kExpThreads + kBlock + 64;      // warps 8-11 dequantize, 12 issues, 13 loads
+constexpr int kManyDesc = 8;                           // ints of a run's descriptor
+
+struct ManyArgs {
+    WeightPlan plan;
+    int n_slots;
+    uint8_t *shares;      // [n_slots][kManyDesc] ints, then [n_slots][2][kItemTokens] floats: a run's share of an item it continues (0), of one it begins (1)
+};
+
+template <int D> struct ManyGeo {
+    static constexpr int TILE = tile_bytes(D);
+    static constexpr int STAGES = D == 128 ? 4 : 6;
+    static constexpr int SMEM = STAGES * TILE + 1024;            // and room to align to 1024 bytes
+    static constexpr int HALF_BYTES = kBlock * 128;              // 64 channels of a tile
+    static constexpr int A_COLUMNS = D;                          // of a block: high parts, low parts, two to a column
+    static constexpr int A_BUFFERS = D == 128 ? 1 : 2;           // what 512 columns leave room for
+    static constexpr int TMEM_S = 0, TMEM_A = 256;               // columns: S 2 blocks x 2 halves x 64
+};
+
+// The items of one sequence: per KV head, 256 tokens each; query tiles that they look at.
+struct ManyItems {
+    int rep, m, len, base, rows, steps, causal, tiles;
+    __device__ __forceinline__ void set(const PagedWeightArgs &a, const WeightSeq &w)
+    {
+        rep = w.rep;
+        m = w.m;
+        len = w.s.len;
+        base = len - m;
+        rows = w.rows;
+        steps = (rows + kTileRows - 1) / kTileRows;
+        causal = a.causal;
+        tiles = rows > kFewRows ? (len + kItemTokens - 1) / kItemTokens : 0;      // the others are the other kernel's
+    }
+    // the first row that sees token t (of a causal step)
+    __device__ __forceinline__ int first_row(int t) const { return causal ? max(t - base, 0) * rep : 0; }
+    __device__ __forceinline__ int first_step(int tile) const { return first_row(tile * kItemTokens) / kTileRows; }
+    __device__ __forceinline__ int cost(int tile) const { return steps - first_step(tile); }
+    // tiles that all steps look at
+    __device__ __forceinline__ int whole() const { return !causal ? tiles : base < 0 ? 0 : min(tiles, base / kItemTokens + 1); }
+    __device__ __forceinline__ long long total() const
+    {
+        long long c = (long long)whole() * steps;
+        for (int tile = whole(); tile < tiles; ++tile) c += cost(tile);
+        return c;
+    }
+};
+
+// What a role works on: steps [s0, s1) of tile `tile` of KV head h of sequence b.  In shared memory: in registers it would spill.
+struct ManySegment {
+    long long f, f1;      // what is left of the CTA's run
+    int valid, b, h, tile, s0, s1, whole, begins, parts;
+    WeightSeq w;
+    ManyItems it;
+};
+__device__ __noinline__ void next_segment(const ManyArgs &args, const long long *pre, long long per, ManySegment &s)
 {
-    __shared__ float key[kTokens][D + 1];
-    __shared__ float zero[kTokens][NG];
-    __shared__ float query[8][D], constants[8][2 + NG], part[4][kTokens];
+    const PagedWeightArgs &a = args.plan.a;
+    const long long f = s.f;
+    if (f >= s.f1) { s.valid = 0; return; }
+    int b = s.b;
+    while (pre[b + 1] <= f) ++b;
+    WeightSeq w;
+    ManyItems it;
+    weight_sequence(a, b, w);
+    it.set(a, w);
+    const long long per_head = (pre[b + 1] - pre[b]) / a.p.cfg.n_kv_heads;
+    long long at = f - pre[b];
+    const int h = (int)(at / per_head);
+    at -= h * per_head;
+    const int full = it.whole();
+    int tile = (int)min(at / it.steps, (long long)full);
+    at -= (long long)tile * it.steps;
+    int c = it.steps;
+    if (tile >= full) {
+        c = it.cost(tile);
+        while (at >= c) { at -= c; c = it.cost(++tile); }
+    }
+    const int take = (int)min((long long)(c - at), s.f1 - f);
+    s.b = b;
+    s.h = h;
+    s.tile = tile;
+    s.s0 = it.steps - c + (int)at;
+    s.s1 = s.s0 + take;
+    s.begins = at == 0;
+    s.whole = at == 0 && take == c;
+    s.parts = (int)((f - at + c - 1) / per - blockIdx.x + 1);
+    s.w = w;
+    s.it = it;
+    s.f = f + take;
+    s.valid = 1;
+}
+
+// Thirty-two scores of a thread's token -> their probabilities' sum.  `constants`: {factor, factor, -lse, -lse} of two rows.  EDGE: rows
+// below `hidden` do not see the token.
+template <bool EDGE> __device__ __forceinline__ float sum_probabilities(const float (&x)[32], const float4 *constants, int hidden)
+{
+    uint64_t l0 = 0ull, l1 = 0ull;
+#pragma unroll
+    for (int c = 0; c < 32; c += 2) {
+        const float4 k = constants[c / 2];
+        float a, b;
+        unpair(pair_fma(pair(x[c], x[c + 1]), pair(k.x, k.y), pair(k.z, k.w)), a, b);
+        a = ex2_approx(a);
+        b = ex2_approx(b);
+        if (EDGE && c < hidden) a = 0.f;
+        if (EDGE && c + 1 < hidden) b = 0.f;
+        if (c & 2) l1 = pair_add(l1, pair(a, b));
+        else l0 = pair_add(l0, pair(a, b));
+    }
+    float a, b;
+    unpair(pair_add(l0, l1), a, b);
+    return a + b;
+}
+
+template <typename T, int D, int NG>
+__global__ void __launch_bounds__(kManyThreads, 1) weight_many_kernel(const __grid_constant__ ManyArgs args)
+{
+    using Geo = ManyGeo<D>;
+    const PagedWeightArgs &a = args.plan.a;
+    const PagedArgs &p = a.p;
+    const skvq_paged_config &cfg = p.cfg;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+    long long *pre = reinterpret_cast<long long *>(smem + Geo::STAGES * Geo::TILE);
+    __shared__ __align__(8) uint64_t bars[2 * Geo::STAGES + 12];
+    __shared__ uint32_t tmem_sh;
+    __shared__ int fail_sh;
+    __shared__ long long scan_sh[16];
+    __shared__ ManySegment seg_sh[5];      // of the two blocks' exponentials, of the dequantizers, the issuer, the loader
+    const int tid = threadIdx.x, lane = tid & 31, B = p.batch.n_seqs, H = cfg.n_kv_heads;
+    const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
+
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;");
-    const PagedWeightArgs &a = plan.a;
-    const skvq_paged_config &cfg = a.p.cfg;
-    const int b = blockIdx.z, h = blockIdx.y, token = threadIdx.x % kTokens, quarter = threadIdx.x / kTokens, t = blockIdx.x * kTokens + token;
+
+    // ---- the flat partition
+    {
+        long long carry = 0;
+        for (int base = 0; base < B; base += kManyThreads) {
+            const int b = base + tid;
+            long long c = 0;
+            if (b < B) {
+                WeightSeq w;
+                weight_sequence(a, b, w);
+                if (w.ok) {      // the kernel for few rows reports the others
+                    ManyItems it;
+                    it.set(a, w);
+                    c = it.total() * H;
+                }
+            }
+            long long incl = c;
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const long long v = __shfl_up_sync(0xffffffffu, incl, d);
+                if (lane >= d) incl += v;
+            }
+            if (lane == 31) scan_sh[warp] = incl;
+            __syncthreads();
+            long long before = carry;
+            for (int w = 0; w < kManyThreads / 32; ++w) {
+                if (w < warp) before += scan_sh[w];
+                carry += scan_sh[w];
+            }
+            if (b < B) pre[b] = before + incl - c;
+            __syncthreads();
+        }
+        if (tid == 0) pre[B] = carry;
+    }
+    // ---- barriers, tensor memory
+    const uint32_t bar0 = smem_u32(bars);
+    const uint32_t q_full = bar0, q_empty = bar0 + 8 * Geo::STAGES;      // + 8 * stage
+    const uint32_t s_full = bar0 + 16 * Geo::STAGES, s_empty = s_full + 32;      // + 16 * block + 8 * half
+    const uint32_t a_full = s_full + 64, a_empty = s_full + 80;          // + 8 * buffer
+    __shared__ __align__(8) uint64_t drained_sh;
+    const uint32_t drained = smem_u32(&drained_sh);
+    if (tid == 0) {
+#pragma unroll
+        for (int i = 0; i < Geo::STAGES; ++i) {
+            mbar_init(q_full + 8 * i, 1);
+            mbar_init(q_empty + 8 * i, 1 + kExpThreads / 32);      // the products, and a warp each that has read its constants
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            mbar_init(s_full + 8 * i, 1);
+            mbar_init(s_empty + 8 * i, 4);
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(a_full + 8 * i, kBlock);
+            mbar_init(a_empty + 8 * i, 1);
+        }
+        mbar_init(drained, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        fail_sh = 0;
+    }
+    if (warp == 0) tmem_alloc(smem_u32(&tmem_sh), 512);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = tmem_sh;
+    const long long total = pre[B], per = max((total + args.n_slots - 1) / args.n_slots, 1LL);
+    int *desc = reinterpret_cast<int *>(args.shares) + (size_t)blockIdx.x * kManyDesc;
+    if (tid < 5) {
+        ManySegment &first = seg_sh[tid];
+        first.f = blockIdx.x * per;
+        first.f1 = min(first.f + per, total);
+        first.b = 0;
+        if (first.f < first.f1) {
+            int lo = 0, hi = B - 1;
+            while (lo < hi) {
+                const int mid = (lo + hi + 1) >> 1;
+                if (pre[mid] <= first.f) lo = mid; else hi = mid - 1;
+            }
+            first.b = lo;
+        }
+    }
+    if (tid == 0) desc[0] = 0;
+    __syncthreads();
+    // A wait that runs out is reported; the thread then goes through its loops without waiting.  The flag is set before anything that
+    // follows from it, so that who has read spoilt operands finds it set when it comes to write its sums.
+    bool alive = true;
+    volatile int *fail = &fail_sh;
+    auto wait = [&](uint32_t bar, uint32_t parity) {      // by whole warps
+        if (alive && !mbar_wait_cycles(bar, parity)) {
+            alive = false;
+            *fail = 1;
+            set_status(p.c.status, SKVQ_STATUS_COPY_TIMEOUT);
+        }
+    };
+    // A role is 128 threads (block 0, block 1, the dequantizers) or a warp (issuer, loader).
+    const int role = warp < 12 ? warp >> 2 : warp - 9;
+    const ManySegment &s = seg_sh[role];
+    auto role_sync = [&]() {
+        if (warp < 12) asm volatile("bar.sync %0, 128;" ::"r"(1 + role) : "memory");
+        else __syncwarp();
+    };
+    auto next = [&]() {
+        role_sync();
+        if ((warp < 12 ? tid & 127 : lane) == 0) next_segment(args, pre, per, seg_sh[role]);
+        role_sync();
+        return s.valid != 0;
+    };
+    // rows of step `step` come as one or two halves
+    auto halves = [&](int step) { return s.it.rows - step * kTileRows > 64 ? 2 : 1; };
+
+    if (warp >= 8 && warp < 12) {
+        // ================================================================ dequantizers
+        const int row = tid - kExpThreads, P = cfg.page_tokens, page_shift = __ffs(P) - 1;
+        const uint32_t quad = (uint32_t)((warp & 3) * 32) << 16;
+        uint32_t n = 0;      // segments so far
+        while (next()) {
+            if (*fail) alive = false;
+            const uint32_t buf = n % Geo::A_BUFFERS, use = n / Geo::A_BUFFERS;
+            if (use) wait(a_empty + 8 * buf, (use - 1) & 1);
+            tc_fence_after();
+            const int32_t *table = p.batch.page_table + (int64_t)s.b * p.batch.max_pages;
+#pragma unroll 1
+            for (int blk = 0; blk < 2; ++blk) {
+                const int t = s.tile * kItemTokens + blk * kBlock + row;
+                const uint32_t dst = tmem + Geo::TMEM_A + (buf * 2 + blk) * Geo::A_COLUMNS + quad;
+                int page = -1;
+                if (t < s.w.s.len) {
+                    page = table[t >> page_shift];
+                    if (page < 0 || page >= cfg.n_pages) { page = -1; set_status(p.c.status, SKVQ_STATUS_BAD_PAGE); }
+                }
+                const bool codes = page >= 0 && t < s.w.s.lq, window = page >= 0 && !codes;
+                const int64_t at = codes ? ((int64_t)page * H + s.h) * P + (t & (P - 1)) : 0;
+                const int64_t ring = window ? ((int64_t)s.w.s.slot * H + s.h) * cfg.ring_tokens + t % cfg.ring_tokens : 0;
+                const uint4 *code_row = reinterpret_cast<const uint4 *>(static_cast<const uint8_t *>(p.c.k_codes) + at * (D / 2));
+                const uint4 *ring_row = reinterpret_cast<const uint4 *>(static_cast<const T *>(p.c.k_win) + ring * D);
+                uint4 c[D / 32];
+                uint32_t meta[NG];
+#pragma unroll
+                for (int i = 0; i < D / 32; ++i) c[i] = codes ? code_row[i] : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+                for (int g = 0; g < NG; ++g) meta[g] = codes ? static_cast<const uint32_t *>(p.c.k_meta)[at * NG + g] : 0u;
+                // 32 channels at a time, operand order 0 4 1 5 2 6 3 7 in every run of eight: 16 columns of high parts, 16 of low ones
+#pragma unroll
+                for (int i = 0; i < D / 32; ++i) {
+                    const float2 hz = floats<__half>(meta[i * NG / (D / 32)]);
+                    uint32_t high[16], low[16];
+                    const uint32_t words[4] = {c[i].x, c[i].y, c[i].z, c[i].w};
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        float x[8];
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {      // 2^23 + code, minus 2^23
+                            const int nibble = (e >> 1) + 4 * (e & 1);
+                            x[e] = fmaf(hz.x, __uint_as_float(0x4B000000u | (words[k] >> (4 * nibble) & 15u)) - 8388608.f, hz.y);
+                        }
+                        if (window) {
+                            const uint4 v = ring_row[i * 4 + k];
+                            const uint32_t pairs[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) {
+                                const int ch = (e >> 1) + 4 * (e & 1);
+                                const float2 f = floats<T>(pairs[ch / 2]);
+                                x[e] = ch & 1 ? f.y : f.x;
+                            }
+                        }
+#pragma unroll
+                        for (int e = 0; e < 8; e += 2) {
+                            const uint32_t hi = packed<__half>(x[e], x[e + 1]);
+                            const float2 f = floats<__half>(hi);
+                            high[k * 4 + e / 2] = hi;
+                            low[k * 4 + e / 2] = packed<__half>(x[e] - f.x, x[e + 1] - f.y);
+                        }
+                    }
+                    tmem_st16(dst + i * 16, high);
+                    tmem_st16(dst + D / 2 + i * 16, low);
+                }
+            }
+            tmem_wait_st();
+            tc_fence_before();
+            mbar_arrive(a_full + 8 * buf);
+            ++n;
+        }
+    } else if (warp == 12) {
+        // ================================================================ products
+        constexpr uint32_t kIdesc = idesc_f16_f32(kBlock, 64);
+        const uint32_t smem_base = smem_u32(smem);
+        uint32_t n = 0, nq = 0, n0 = 0, n1 = 0;      // segments, query tiles, uses of the halves' buffers
+        while (next()) {
+            if (*fail) alive = false;
+            const uint32_t buf = n % Geo::A_BUFFERS;
+            wait(a_full + 8 * buf, (n / Geo::A_BUFFERS) & 1);
+            for (int step = s.s0; step < s.s1; ++step, ++nq) {
+                const uint32_t stage = nq % Geo::STAGES;
+                wait(q_full + 8 * stage, (nq / Geo::STAGES) & 1);
+                const int parts = halves(step);
+#pragma unroll 1
+                for (int hf = 0; hf < parts; ++hf) {
+                    const uint64_t dq = desc_k_major(smem_base + stage * Geo::TILE + hf * 64 * 128);
+                    const uint32_t uses = hf ? n1 : n0;
+#pragma unroll 1
+                    for (int blk = 0; blk < 2; ++blk) {
+                        if (uses) wait(s_empty + 16 * blk + 8 * hf, (uses - 1) & 1);
+                        tc_fence_after();
+                        if (elect_one()) {
+                            const uint32_t d = tmem + Geo::TMEM_S + blk * 128 + hf * 64, ka = tmem + Geo::TMEM_A + (buf * 2 + blk) * Geo::A_COLUMNS;
+#pragma unroll
+                            for (int part = 0; part < 2; ++part)
+#pragma unroll
+                                for (int ks = 0; ks < D / 16; ++ks)
+                                    umma_f16_ts(d, ka + part * (D / 2) + ks * 8, dq + (ks >> 2) * (Geo::HALF_BYTES >> 4) + (ks & 3) * 2, kIdesc, part + ks > 0);
+                            umma_commit(s_full + 16 * blk + 8 * hf);
+                        }
+                        __syncwarp();
+                    }
+                    if (hf) ++n1;
+                    else ++n0;
+                }
+                if (elect_one()) umma_commit(q_empty + 8 * stage);
+                __syncwarp();
+            }
+            if (elect_one()) umma_commit(a_empty + 8 * buf);
+            __syncwarp();
+            ++n;
+        }
+        // the last products must not outlive the CTA, whoever waited for them
+        if (n) {
+            if (elect_one()) umma_commit(drained);
+            __syncwarp();
+            mbar_wait_cycles(drained, 0);
+        }
+    } else if (warp == 13) {
+        // ================================================================ query tiles
+        const uint32_t smem_base = smem_u32(smem);
+        uint32_t nq = 0;
+        while (next()) {
+            if (*fail) alive = false;
+            for (int step = s.s0; step < s.s1; ++step, ++nq) {
+                const uint32_t stage = nq % Geo::STAGES, use = nq / Geo::STAGES;
+                if (use) wait(q_empty + 8 * stage, (use - 1) & 1);
+                alive = __all_sync(0xffffffffu, alive && !*fail);
+                if (lane == 0 && alive) {      // once a wait has run out nothing is copied any more
+                    mbar_expect_tx(q_full + 8 * stage, Geo::TILE);
+                    bulk_g2s(smem_base + stage * Geo::TILE, query_tile(args.plan, s.w, s.b, s.h, step), Geo::TILE, q_full + 8 * stage);
+                }
+                __syncwarp();
+            }
+        }
+        // copies in flight end before the CTA does
+        for (uint32_t i = nq > Geo::STAGES ? nq - Geo::STAGES : 0; i < nq; ++i) mbar_wait_cycles(q_full + 8 * (i % Geo::STAGES), (i / Geo::STAGES) & 1);
+    } else {
+        // ================================================================ exponentials
+        const int blk = warp >> 2, row = tid & (kBlock - 1);
+        const uint32_t s_addr = tmem + Geo::TMEM_S + blk * 128 + ((uint32_t)((warp & 3) * 32) << 16);
+        uint32_t nq = 0, n0 = 0, n1 = 0;      // query tiles, uses of the halves' buffers
+        while (next()) {
+            if (*fail) alive = false;
+            const int t = s.tile * kItemTokens + blk * kBlock + row;
+            const int hidden_rows = t < s.w.s.len ? s.it.first_row(t) : 0;      // rows below it do not see the token
+            float sum = 0.f;
+            for (int step = s.s0; step < s.s1; ++step, ++nq) {
+                const uint32_t stage = nq % Geo::STAGES;
+                wait(q_full + 8 * stage, (nq / Geo::STAGES) & 1);
+                const float4 *constants = reinterpret_cast<const float4 *>(smem + stage * Geo::TILE + kTileRows * D * 2);
+                const int parts = halves(step);
+#pragma unroll 1
+                for (int hf = 0; hf < parts; ++hf) {
+                    wait(s_full + 16 * blk + 8 * hf, (hf ? n1 : n0) & 1);
+                    if (hf) ++n1;
+                    else ++n0;
+                    tc_fence_after();
+                    float x[32], y[32];
+                    tmem_ld32(s_addr + hf * 64, x);
+                    tmem_ld32(s_addr + hf * 64 + 32, y);
+                    tmem_wait_ld32(x);
+                    tmem_wait_ld32(y);
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(s_empty + 16 * blk + 8 * hf);
+                    const int hidden = hidden_rows - step * kTileRows - hf * 64;      // columns below it
+                    if (__any_sync(0xffffffffu, hidden > 0)) {
+                        sum += sum_probabilities<true>(x, constants + hf * 32, hidden);
+                        sum += sum_probabilities<true>(y, constants + hf * 32 + 16, hidden - 32);
+                    } else {
+                        sum += sum_probabilities<false>(x, constants + hf * 32, 0);
+                        sum += sum_probabilities<false>(y, constants + hf * 32 + 16, 0);
+                    }
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(q_empty + 8 * stage);
+            }
+            if (t < s.w.s.len) {      // a token without a page gains nothing
+                const int page = p.batch.page_table[(int64_t)s.b * p.batch.max_pages + t / cfg.page_tokens];
+                if (page < 0 || page >= cfg.n_pages) sum = 0.f;
+            }
+            alive = __all_sync(0xffffffffu, alive && !*fail);
+            if (!alive) sum = CUDART_NAN_F;
+            if (s.whole) {
+                if (t < s.w.s.len) write_weight(a, s.w, s.h, t, sum);
+            } else {
+                float *shares = reinterpret_cast<float *>(args.shares + (size_t)args.n_slots * kManyDesc * 4);
+                shares[((size_t)blockIdx.x * 2 + (s.begins ? 1 : 0)) * kItemTokens + blk * kBlock + row] = sum;
+                if (s.begins && tid == 0) {
+                    desc[1] = s.b; desc[2] = s.h; desc[3] = s.tile; desc[4] = s.parts;
+                    desc[0] = 1;
+                }
+            }
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == 0) tmem_dealloc(tmem, 512);
+}
+
+// Adds up the shares of an item that several runs have: blockIdx.x is the run that begins it.
+__global__ void __launch_bounds__(kItemTokens) weight_join_kernel(const __grid_constant__ ManyArgs args)
+{
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;");
+    const int *desc = reinterpret_cast<const int *>(args.shares) + (size_t)blockIdx.x * kManyDesc;
+    if (desc[0] == 0) return;
+    const PagedWeightArgs &a = args.plan.a;
+    const int b = desc[1], h = desc[2], n = desc[4], t = desc[3] * kItemTokens + threadIdx.x;
     WeightSeq w;
     weight_sequence(a, b, w);
-    if (!w.ok || w.rows <= kFewRows || (int)blockIdx.x * kTokens >= w.s.len) return;
-    const int P = cfg.page_tokens;
-    bool have = t < w.s.len;
-    if (have) {
-        const int page = a.p.batch.page_table[(int64_t)b * a.p.batch.max_pages + t / P];
-        if (page < 0 || page >= cfg.n_pages) {
-            set_status(a.p.c.status, SKVQ_STATUS_BAD_PAGE);
-            have = false;
-        } else if (t < w.s.lq) {
-            const int64_t at = ((int64_t)page * cfg.n_kv_heads + h) * P + t % P;
-            for (int c = quarter * (D / 4); c < (quarter + 1) * (D / 4); ++c) {
-                const int code = static_cast<const uint8_t *>(a.p.c.k_codes)[at * (D / 2) + c / 2] >> (c % 2 * 4) & 15;
-                const __half2 m = static_cast<const __half2 *>(a.p.c.k_meta)[at * NG + c / (D / NG)];
-                key[token][c] = __low2float(m) * code;
-                zero[token][c / (D / NG)] = __high2float(m);
-            }
-        } else {
-            const int64_t row = ((int64_t)w.s.slot * cfg.n_kv_heads + h) * cfg.ring_tokens + t % cfg.ring_tokens;
-            for (int c = quarter * (D / 4); c < (quarter + 1) * (D / 4); ++c) {
-                key[token][c] = Elem<T>::to_float(static_cast<const T *>(a.p.c.k_win)[row * D + c]);
-                zero[token][c / (D / NG)] = 0.f;
-            }
-        }
-    }
-    // rows below it do not see the token
-    const int64_t first_row = a.causal ? (int64_t)max(t - (w.s.len - w.m), 0) * w.rep : 0;
+    if (t >= w.s.len) return;
+    const float *shares = reinterpret_cast<const float *>(args.shares + (size_t)args.n_slots * kManyDesc * 4) + threadIdx.x;
     float sum = 0.f;
-    for (int r0 = 0; r0 < w.rows; r0 += 8) {
-        __syncthreads();
-        for (int e = threadIdx.x; e < 8 * D; e += kThreads) {
-            const int r = r0 + e / D, c = e % D, tr = r % kTileRows;
-            if (r >= w.rows) break;
-            const uint8_t *tile = query_tile(plan, w, b, h, r / kTileRows);
-            query[e / D][(c & ~7) + channel_at(c & 7)] = __half2float(*reinterpret_cast<const __half *>(
-                tile + (c >> 6) * kTileRows * 128 + tr * 128 + ((((c >> 3) & 7) ^ (tr & 7)) << 4) + (c & 7) * 2));
-            if (c < 2 + NG) constants[e / D][c] = reinterpret_cast<const float *>(tile + kTileRows * D * 2)[c * kTileRows + tr];
-        }
-        __syncthreads();
-        for (int k = quarter; k < min(8, w.rows - r0); k += 4) {
-            if (!have || r0 + k < first_row) continue;
-            float s = 0.f;
-            for (int c = 0; c < D; ++c) s = fmaf(query[k][c], key[token][c], s);
-            for (int g = 0; g < NG; ++g) s = fmaf(constants[k][2 + g], zero[token][g], s);
-            sum += exp2f(fmaf(s, constants[k][0], constants[k][1]));
-        }
-    }
-    part[quarter][token] = sum;
-    __syncthreads();
-    if (quarter == 0 && t < w.s.len) {
-        const int64_t at = ((int64_t)w.s.slot * cfg.n_kv_heads + h) * a.capacity + t;
-        const float old = a.w_in && t < w.s.len - w.s.n ? a.w_in[at] : 0.f;
-        a.w_out[at] = old + ((part[0][token] + part[1][token]) + (part[2][token] + part[3][token]));
-    }
+    for (int k = 0; k < n; ++k) sum += shares[((size_t)(blockIdx.x + k) * 2 + (k == 0 ? 1 : 0)) * kItemTokens];
+    write_weight(a, w, h, t, sum);
 }
 
 // The most counted rows that a KV head of a sequence can have.
@@ -718,6 +1141,13 @@ int64_t query_tiles(const skvq_paged_config &cfg, const skvq_paged_batch &batch,
     return seq_tiles ? uniform : together;
 }
 
+// Runs that the work is cut into: a CTA per SM, a query tile each at least.
+int many_slots(const skvq_paged_config &cfg, const skvq_paged_batch &batch, int64_t rows)
+{
+    const int64_t units = (int64_t)batch.n_seqs * cfg.n_kv_heads * ((batch.max_len + kItemTokens - 1) / kItemTokens) * ((rows + kTileRows - 1) / kTileRows);
+    return (int)(units < sm_count() ? (units < 1 ? 1 : units) : sm_count());
+}
+
 template <typename T, int D, int NG, int NT, int E> cudaError_t launch_few(const WeightPlan &p, cudaStream_t stream)
 {
     using Geo = FewGeo<D, NG, NT, E>;
@@ -729,7 +1159,7 @@ template <typename T, int D, int NG, int NT, int E> cudaError_t launch_few(const
     // one wave of resident CTAs, no more warps than tiles
     const long long lq = batch.max_len > cfg.window ? batch.max_len - cfg.window : 0;
     const long long tiles = (lq + kTile - 1) / kTile + kRingCost * ((batch.max_len - lq + kRingTile - 1) / kRingTile);
-    const long long wave = (NT == 1 ? 5LL : 4LL) * sm_count(), useful = ((long long)batch.n_seqs * cfg.n_kv_heads * tiles + kFewWarps - 1) / kFewWarps;
+    const long long wave = (long long)kFewCtas * sm_count(), useful = ((long long)batch.n_seqs * cfg.n_kv_heads * tiles + kFewWarps - 1) / kFewWarps;
     return launch_chained(weight_few_kernel<T, D, NG, NT, E>, dim3((unsigned)(useful < wave ? useful : wave)), kFewThreads,
                           Geo::SMEM + sizeof(long long) * (batch.n_seqs + 1), stream, p);
 }
@@ -747,9 +1177,16 @@ template <typename T, int D, int NG> cudaError_t launch_weights(const PagedWeigh
     const int64_t padded = (rows + kTileRows - 1) / kTileRows * kTileRows, chunks = ((padded + rep - 1) / rep + kQueryTokens - 1) / kQueryTokens;
     p.heads = cfg.n_q_heads;
     while (p.heads > 4 && chunks * batch.n_seqs * ((cfg.n_q_heads + p.heads - 1) / p.heads) < 32LL * sm_count()) p.heads = (p.heads + 1) / 2;
-    e = launch_chained(weight_queries_kernel<T, D, NG>, dim3((unsigned)chunks, (cfg.n_q_heads + p.heads - 1) / p.heads, batch.n_seqs), kQueryThreads, 0, stream, p);
+    e = launch_chained(weight_queries_kernel<T, D>, dim3((unsigned)chunks, (cfg.n_q_heads + p.heads - 1) / p.heads, batch.n_seqs), kQueryThreads, 0, stream, p);
     if (e != cudaSuccess) return e;
-    return launch_chained(weight_tokens_kernel<T, D, NG>, dim3((batch.max_len + kTokens - 1) / kTokens, cfg.n_kv_heads, batch.n_seqs), kThreads, 0, stream, p);
+    int seq_tiles;
+    const ManyArgs m{p, many_slots(cfg, batch, rows), a.ws + query_tiles(cfg, batch, a.last, seq_tiles) * cfg.n_kv_heads * tile_bytes(D)};
+    static unsigned long long done = 0;
+    e = configure_smem_once(weight_many_kernel<T, D, NG>, ManyGeo<D>::SMEM + (int)sizeof(long long) * (kMaxPagedSeqs + 1), done);
+    if (e != cudaSuccess) return e;
+    e = launch_chained(weight_many_kernel<T, D, NG>, dim3(m.n_slots), kManyThreads, ManyGeo<D>::SMEM + sizeof(long long) * (batch.n_seqs + 1), stream, m);
+    if (e != cudaSuccess) return e;
+    return launch_chained(weight_join_kernel, dim3(m.n_slots), kItemTokens, 0, stream, m);
 }
 
 template <typename T> cudaError_t launch_by_shape(const PagedWeightArgs &a, cudaStream_t stream)
@@ -764,7 +1201,9 @@ template <typename T> cudaError_t launch_by_shape(const PagedWeightArgs &a, cuda
 size_t paged_weights_workspace_bytes(const skvq_paged_config &cfg, const skvq_paged_batch &batch, int last)
 {
     int seq_tiles;
-    return (size_t)query_tiles(cfg, batch, last, seq_tiles) * cfg.n_kv_heads * tile_bytes(cfg.head_dim, cfg.head_dim / cfg.group_size);
+    const int64_t rows = most_rows(cfg, batch, last), tiles = query_tiles(cfg, batch, last, seq_tiles);
+    if (tiles == 0) return 0;
+    return (size_t)tiles * cfg.n_kv_heads * tile_bytes(cfg.head_dim) + many_slots(cfg, batch, rows) * (size_t)(kManyDesc * 4 + 2 * kItemTokens * 4);
 }
 
 cudaError_t launch_paged_weights(const PagedWeightArgs &a, cudaStream_t stream)
