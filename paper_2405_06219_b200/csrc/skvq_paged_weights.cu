@@ -28,14 +28,15 @@ using mmak::smem_u32;
 using namespace tc5;
 
 constexpr float kSubnormal = 1.f / 16777216.f;      // 2^-24: the least fp16 subnormal, what a code's lowest bit stands for as an operand
+constexpr float kLog2E = 1.4426950408889634f;      // applied to score - lse, which is small where it matters: their own products with it would lose 2^-24 of 20 or 30
 constexpr float kZeroScale = 1.f / 1024.f;           // brings a sum of 128 operands below 2^14 into fp16's range
 constexpr int kQueryThreads = 128;
 constexpr int kQueryTokens = kQueryThreads / 16;
 constexpr int kTileRows = 128;      // rows of a query tile
 
 // A query tile: kTileRows rows of D fp16, 64-channel halves one after the other, a half's rows 128 bytes each with 16-byte piece c of row r
-// at c ^ (r & 7) (the 128-byte swizzle of the tensor core's operands); then for every two rows four floats: the factors of their scores in
-// units of log2, minus their lse in units of log2 (minus infinity: the row adds nothing).
+// at c ^ (r & 7) (the 128-byte swizzle of the tensor core's operands); then for every two rows four floats: the factors of their scores, minus their
+// lse (minus infinity: the row adds nothing).
 struct WeightPlan {
     PagedWeightArgs a;
     int seq_tiles;        // > 0: sequence b's tiles begin at b * seq_tiles; 0: at starts[b] * Hq/Hkv / kTileRows + b
@@ -355,8 +356,8 @@ __global__ void __launch_bounds__(kFewThreads, kFewCtas) weight_few_kernel(const
                 if constexpr (C == 4) *reinterpret_cast<uint2 *>(queries + r * Geo::QROW + lane * C) = make_uint2(v[0], v[1]);
                 else *reinterpret_cast<uint32_t *>(queries + r * Geo::QROW + lane * C) = v[0];
                 if (lane == 0) {
-                    constants[r * (2 + NG)] = counts ? a.sm_scale * 1.4426950408889634f / up : 0.f;
-                    constants[r * (2 + NG) + 1] = counts ? lse * -1.4426950408889634f : -CUDART_INF_F;
+                    constants[r * (2 + NG)] = counts ? a.sm_scale / up : 0.f;
+                    constants[r * (2 + NG) + 1] = counts ? -lse : -CUDART_INF_F;
                 }
                 if (lane % (32 / NG) == 0) constants[r * (2 + NG) + 2 + lane / (32 / NG)] = sum;
             }
@@ -455,7 +456,7 @@ __global__ void __launch_bounds__(kFewThreads, kFewCtas) weight_few_kernel(const
                             float x = h[0] * acc[n][0][2 * half + e];
 #pragma unroll
                             for (int k = 1; k < NG; ++k) x = fmaf(h[k], acc[n][k][2 * half + e], x);
-                            s[half][n][e] = fmaf(fmaf(x, kZeroScale / kSubnormal, zero[n][2 * half + e]), rs[n][e], nl[n][e]);
+                            s[half][n][e] = fmaf(fmaf(x, kZeroScale / kSubnormal, zero[n][2 * half + e]), rs[n][e], nl[n][e]) * kLog2E;
                         }
                 }
                 if (edge) {
@@ -550,7 +551,7 @@ __global__ void __launch_bounds__(kFewThreads, kFewCtas) weight_few_kernel(const
                     for (int e = 0; e < E; ++e) {
                         const int at = g + 8 * half;
                         const bool hidden = t0 + at >= lim[n][e] || ((gone >> at) & 1u);      // rows behind the last token were not copied
-                        sums[half] += hidden ? 0.f : ex2_approx(fmaf(s[n][2 * half + e], rs[n][e] * kZeroScale, nl[n][e]));
+                        sums[half] += hidden ? 0.f : ex2_approx(fmaf(s[n][2 * half + e], rs[n][e] * kZeroScale, nl[n][e]) * kLog2E);
                     }
             const bool odd = j & 1;
             float x = (odd ? sums[1] : sums[0]) + __shfl_xor_sync(0xffffffffu, odd ? sums[0] : sums[1], 1);
@@ -638,8 +639,8 @@ __global__ void __launch_bounds__(kQueryThreads) weight_queries_kernel(const __g
         else *reinterpret_cast<uint2 *>(dst) = make_uint2(packed<__half>(x[0], x[1]), packed<__half>(x[2], x[3]));
         if (sub == 0) {
             float *constants = reinterpret_cast<float *>(tile + kTileRows * D * 2) + (tr >> 1) * 4 + (tr & 1);
-            constants[0] = a.sm_scale * 1.4426950408889634f / up;
-            constants[2] = counts ? lse * -1.4426950408889634f : -CUDART_INF_F;
+            constants[0] = a.sm_scale / up;
+            constants[2] = counts ? -lse : -CUDART_INF_F;
         }
     }
 }
@@ -652,7 +653,7 @@ __global__ void __launch_bounds__(kQueryThreads) weight_queries_kernel(const __g
 //   loader        a thread brings query tiles with their rows' constants into a ring, one bulk copy each (they are laid out for it).
 //   issuer        a warp: for each half of a tile (64 rows) and block, S = (high + low) Q^T; a buffer each, so the products run while the
 //                 other half and the other block become probabilities.
-//   exponentials  2 x 4 warps, a block each: scores from tensor memory, exp2(rs s - lse), their sum.
+//   exponentials  2 x 4 warps, a block each: scores from tensor memory, exp(factor s - lse), their sum.
 // Items are laid end to end, priced in query tiles (causal limits included), and cut into equal runs, one per CTA; partial sums of an
 // item that several runs share are added in order by a last kernel.
 constexpr int kBlock = 128;                            // tokens of a block, rows of a query tile
@@ -759,7 +760,7 @@ template <bool EDGE> __device__ __forceinline__ float sum_probabilities(const fl
     for (int c = 0; c < 32; c += 2) {
         const float4 k = constants[c / 2];
         float a, b;
-        unpair(pair_fma(pair(x[c], x[c + 1]), pair(k.x, k.y), pair(k.z, k.w)), a, b);
+        unpair(pair_mul(pair_fma(pair(x[c], x[c + 1]), pair(k.x, k.y), pair(k.z, k.w)), pair(kLog2E, kLog2E)), a, b);
         a = ex2_approx(a);
         b = ex2_approx(b);
         if (EDGE && c < hidden) a = 0.f;
@@ -999,10 +1000,10 @@ __global__ void __launch_bounds__(kManyThreads, 1) weight_many_kernel(const __gr
                         if (elect_one()) {
                             const uint32_t d = tmem + Geo::TMEM_S + blk * 128 + hf * 64, ka = tmem + Geo::TMEM_A + (buf * 2 + blk) * Geo::A_COLUMNS;
 #pragma unroll
-                            for (int part = 0; part < 2; ++part)
+                            for (int part = 1; part >= 0; --part)      // the low parts first: the accumulator's truncations are of small sums then
 #pragma unroll
                                 for (int ks = 0; ks < D / 16; ++ks)
-                                    umma_f16_ts(d, ka + part * (D / 2) + ks * 8, dq + (ks >> 2) * (Geo::HALF_BYTES >> 4) + (ks & 3) * 2, kIdesc, part + ks > 0);
+                                    umma_f16_ts(d, ka + part * (D / 2) + ks * 8, dq + (ks >> 2) * (Geo::HALF_BYTES >> 4) + (ks & 3) * 2, kIdesc, part == 0 || ks > 0);
                             umma_commit(s_full + 16 * blk + 8 * hf);
                         }
                         __syncwarp();
