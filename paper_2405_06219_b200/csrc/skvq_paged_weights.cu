@@ -651,8 +651,8 @@ __global__ void __launch_bounds__(kQueryThreads) weight_queries_kernel(const __g
 //                 into tensor memory as the A operand: 2 D columns of K for a product whose B operand, the queries, is read from
 //                 shared memory alone.
 //   loader        a thread brings query tiles with their rows' constants into a ring, one bulk copy each (they are laid out for it).
-//   issuer        a warp: for each half of a tile (64 rows) and block, S = (high + low) Q^T; a buffer each, so the products run while the
-//                 other half and the other block become probabilities.
+//   issuer        a warp: S = (low + high) Q^T of a block and a tile; the products of one block run while the other's scores become
+//                 probabilities.
 //   exponentials  2 x 4 warps, a block each: scores from tensor memory, exp(factor s - lse), their sum.
 // Items are laid end to end, priced in query tiles (causal limits included), and cut into equal runs, one per CTA; partial sums of an
 // item that several runs share are added in order by a last kernel.
@@ -675,7 +675,7 @@ template <int D> struct ManyGeo {
     static constexpr int HALF_BYTES = kBlock * 128;              // 64 channels of a tile
     static constexpr int A_COLUMNS = D;                          // of a block: high parts, low parts, two to a column
     static constexpr int A_BUFFERS = D == 128 ? 1 : 2;           // what 512 columns leave room for
-    static constexpr int TMEM_S = 0, TMEM_A = 256;               // columns: S 2 blocks x 2 halves x 64
+    static constexpr int TMEM_S = 0, TMEM_A = 256;               // columns: S 2 blocks x 128 rows
 };
 
 // The items of one sequence: per KV head, 256 tokens each; query tiles that they look at.
@@ -783,7 +783,7 @@ __global__ void __launch_bounds__(kManyThreads, 1) weight_many_kernel(const __gr
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     long long *pre = reinterpret_cast<long long *>(smem + Geo::STAGES * Geo::TILE);
-    __shared__ __align__(8) uint64_t bars[2 * Geo::STAGES + 12];
+    __shared__ __align__(8) uint64_t bars[2 * Geo::STAGES + 8];
     __shared__ uint32_t tmem_sh;
     __shared__ int fail_sh;
     __shared__ long long scan_sh[16];
@@ -830,8 +830,8 @@ __global__ void __launch_bounds__(kManyThreads, 1) weight_many_kernel(const __gr
     // ---- barriers, tensor memory
     const uint32_t bar0 = smem_u32(bars);
     const uint32_t q_full = bar0, q_empty = bar0 + 8 * Geo::STAGES;      // + 8 * stage
-    const uint32_t s_full = bar0 + 16 * Geo::STAGES, s_empty = s_full + 32;      // + 16 * block + 8 * half
-    const uint32_t a_full = s_full + 64, a_empty = s_full + 80;          // + 8 * buffer
+    const uint32_t s_full = bar0 + 16 * Geo::STAGES, s_empty = s_full + 16;      // + 8 * block
+    const uint32_t a_full = s_full + 32, a_empty = s_full + 48;          // + 8 * buffer
     __shared__ __align__(8) uint64_t drained_sh;
     const uint32_t drained = smem_u32(&drained_sh);
     if (tid == 0) {
@@ -841,12 +841,9 @@ __global__ void __launch_bounds__(kManyThreads, 1) weight_many_kernel(const __gr
             mbar_init(q_empty + 8 * i, 1 + kExpThreads / 32);      // the products, and a warp each that has read its constants
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < 2; ++i) {
             mbar_init(s_full + 8 * i, 1);
             mbar_init(s_empty + 8 * i, 4);
-        }
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
             mbar_init(a_full + 8 * i, kBlock);
             mbar_init(a_empty + 8 * i, 1);
         }
@@ -901,7 +898,7 @@ __global__ void __launch_bounds__(kManyThreads, 1) weight_many_kernel(const __gr
         role_sync();
         return s.valid != 0;
     };
-    // rows of step `step` come as one or two halves
+    // rows of step `step` come as one or two halves of 64
     auto halves = [&](int step) { return s.it.rows - step * kTileRows > 64 ? 2 : 1; };
 
     if (warp >= 8 && warp < 12) {
@@ -978,38 +975,31 @@ __global__ void __launch_bounds__(kManyThreads, 1) weight_many_kernel(const __gr
         }
     } else if (warp == 12) {
         // ================================================================ products
-        constexpr uint32_t kIdesc = idesc_f16_f32(kBlock, 64);
+        constexpr uint32_t kWhole = idesc_f16_f32(kBlock, kTileRows), kHalf = idesc_f16_f32(kBlock, kTileRows / 2);
         const uint32_t smem_base = smem_u32(smem);
-        uint32_t n = 0, nq = 0, n0 = 0, n1 = 0;      // segments, query tiles, uses of the halves' buffers
+        uint32_t n = 0, nq = 0;      // segments, query tiles
         while (next()) {
             if (*fail) alive = false;
             const uint32_t buf = n % Geo::A_BUFFERS;
             wait(a_full + 8 * buf, (n / Geo::A_BUFFERS) & 1);
             for (int step = s.s0; step < s.s1; ++step, ++nq) {
-                const uint32_t stage = nq % Geo::STAGES;
+                const uint32_t stage = nq % Geo::STAGES, idesc = halves(step) == 2 ? kWhole : kHalf;
                 wait(q_full + 8 * stage, (nq / Geo::STAGES) & 1);
-                const int parts = halves(step);
+                const uint64_t dq = desc_k_major(smem_base + stage * Geo::TILE);
 #pragma unroll 1
-                for (int hf = 0; hf < parts; ++hf) {
-                    const uint64_t dq = desc_k_major(smem_base + stage * Geo::TILE + hf * 64 * 128);
-                    const uint32_t uses = hf ? n1 : n0;
-#pragma unroll 1
-                    for (int blk = 0; blk < 2; ++blk) {
-                        if (uses) wait(s_empty + 16 * blk + 8 * hf, (uses - 1) & 1);
-                        tc_fence_after();
-                        if (elect_one()) {
-                            const uint32_t d = tmem + Geo::TMEM_S + blk * 128 + hf * 64, ka = tmem + Geo::TMEM_A + (buf * 2 + blk) * Geo::A_COLUMNS;
+                for (int blk = 0; blk < 2; ++blk) {
+                    if (nq) wait(s_empty + 8 * blk, (nq - 1) & 1);
+                    tc_fence_after();
+                    if (elect_one()) {
+                        const uint32_t d = tmem + Geo::TMEM_S + blk * kTileRows, ka = tmem + Geo::TMEM_A + (buf * 2 + blk) * Geo::A_COLUMNS;
 #pragma unroll
-                            for (int part = 1; part >= 0; --part)      // the low parts first: the accumulator's truncations are of small sums then
+                        for (int part = 1; part >= 0; --part)      // the low parts first: the accumulator's truncations are of small sums then
 #pragma unroll
-                                for (int ks = 0; ks < D / 16; ++ks)
-                                    umma_f16_ts(d, ka + part * (D / 2) + ks * 8, dq + (ks >> 2) * (Geo::HALF_BYTES >> 4) + (ks & 3) * 2, kIdesc, part == 0 || ks > 0);
-                            umma_commit(s_full + 16 * blk + 8 * hf);
-                        }
-                        __syncwarp();
+                            for (int ks = 0; ks < D / 16; ++ks)
+                                umma_f16_ts(d, ka + part * (D / 2) + ks * 8, dq + (ks >> 2) * (Geo::HALF_BYTES >> 4) + (ks & 3) * 2, idesc, part == 0 || ks > 0);
+                        umma_commit(s_full + 8 * blk);
                     }
-                    if (hf) ++n1;
-                    else ++n0;
+                    __syncwarp();
                 }
                 if (elect_one()) umma_commit(q_empty + 8 * stage);
                 __syncwarp();
@@ -1046,8 +1036,8 @@ __global__ void __launch_bounds__(kManyThreads, 1) weight_many_kernel(const __gr
     } else {
         // ================================================================ exponentials
         const int blk = warp >> 2, row = tid & (kBlock - 1);
-        const uint32_t s_addr = tmem + Geo::TMEM_S + blk * 128 + ((uint32_t)((warp & 3) * 32) << 16);
-        uint32_t nq = 0, n0 = 0, n1 = 0;      // query tiles, uses of the halves' buffers
+        const uint32_t s_addr = tmem + Geo::TMEM_S + blk * kTileRows + ((uint32_t)((warp & 3) * 32) << 16);
+        uint32_t nq = 0;      // query tiles
         while (next()) {
             if (*fail) alive = false;
             const int t = s.tile * kItemTokens + blk * kBlock + row;
@@ -1058,20 +1048,20 @@ __global__ void __launch_bounds__(kManyThreads, 1) weight_many_kernel(const __gr
                 wait(q_full + 8 * stage, (nq / Geo::STAGES) & 1);
                 const float4 *constants = reinterpret_cast<const float4 *>(smem + stage * Geo::TILE + kTileRows * D * 2);
                 const int parts = halves(step);
+                wait(s_full + 8 * blk, nq & 1);
+                tc_fence_after();
 #pragma unroll 1
                 for (int hf = 0; hf < parts; ++hf) {
-                    wait(s_full + 16 * blk + 8 * hf, (hf ? n1 : n0) & 1);
-                    if (hf) ++n1;
-                    else ++n0;
-                    tc_fence_after();
                     float x[32], y[32];
                     tmem_ld32(s_addr + hf * 64, x);
                     tmem_ld32(s_addr + hf * 64 + 32, y);
                     tmem_wait_ld32(x);
                     tmem_wait_ld32(y);
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(s_empty + 16 * blk + 8 * hf);
+                    if (hf == parts - 1) {      // the scores are in registers: the next product may overwrite them
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(s_empty + 8 * blk);
+                    }
                     const int hidden = hidden_rows - step * kTileRows - hf * 64;      // columns below it
                     if (__any_sync(0xffffffffu, hidden > 0)) {
                         sum += sum_probabilities<true>(x, constants + hf * 32, hidden);
