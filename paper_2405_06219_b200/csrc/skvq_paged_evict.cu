@@ -3,16 +3,23 @@
 //
 // Two kernels.  The first finds, per (sequence, KV head), the threshold of the middle's weights by a radix selection (three digits
 // of 11, 11 and 10 bits of the order-preserving integer of a float) and writes the kept tokens' numbers in order: those above the
-// threshold, and of those at it the lowest-numbered.  The second moves rows: row i of the shortened sequence comes from token
-// kept[i] >= i.  Rows of one pass are read before any of them is written, passes go upwards, and the sources of later passes lie
-// behind what earlier passes write: so a sequence may be shortened inside its own pages.
+// threshold, and of those at it the lowest-numbered.  A CTA, or a cluster of up to eight that add their histograms up over
+// distributed shared memory, holds the weights in registers: they are read once.  The second kernel moves rows: row i of the shortened
+// sequence comes from token kept[i] >= i.  A CTA, or a cluster, has the keys or values of a pair; the rows of one pass are read before any of
+// them is written, passes go upwards, and the sources of later passes lie behind what earlier passes write: so a sequence may be
+// shortened inside its own pages.
+#include <cooperative_groups.h>
+
 #include "skvq_paged.cuh"
 #include "skvq_paged_split.cuh"
 
 namespace skvq {
 namespace {
 
-constexpr int kSelectThreads = 1024;
+namespace cg = cooperative_groups;
+
+constexpr int kSelectThreads = 512;
+constexpr int kMaxCluster = 8;      // the portable size
 constexpr int kMoveThreads = 256;
 constexpr int kUnroll = 4;
 constexpr int kBins = 2048;
@@ -42,48 +49,98 @@ __device__ __forceinline__ uint32_t weight_key(float w)
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-__global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(const __grid_constant__ PagedEvictArgs a)
+struct SelectArgs {
+    PagedEvictArgs a;
+    int ctas;      // of a cluster: they share the middle of a (sequence, KV head)
+};
+
+// ITEMS > 0: a CTA's share of the middle has at most kSelectThreads * ITEMS weights, which stay in registers; ITEMS = 0: any length, the weights
+// are read again for every digit and for the result.
+template <int ITEMS>
+__global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(const __grid_constant__ SelectArgs args)
 {
-    __shared__ int hist[kBins];
-    __shared__ int warp_sum[32], found_bin, found_above;
+    constexpr int WARPS = kSelectThreads / 32, KEYS = ITEMS ? ITEMS : 1;
+    __shared__ int hist[3][kBins];
+    __shared__ int warp_sum[WARPS], found[2], totals[2];
+    __shared__ int2 warp_count[WARPS];
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;");
-    const int H = a.p.cfg.n_kv_heads, b = blockIdx.x / H, h = blockIdx.x % H;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const PagedEvictArgs &a = args.a;
+    cg::cluster_group cluster = cg::this_cluster();
+    const int H = a.p.cfg.n_kv_heads, C = args.ctas, pair = blockIdx.x / C, rank = blockIdx.x % C, b = pair / H, h = pair % H;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, all = rank * kSelectThreads + tid, step = C * kSelectThreads;
     EvictSeq s;
     const bool ok = evict_sequence(a, b, s);
-    if (h == 0 && tid == 0) {
+    if (h == 0 && all == 0) {
         static_cast<EvictSeq *>(a.e.workspace)[b] = s;
         if (!ok) set_status(a.p.c.status, SKVQ_STATUS_BAD_BATCH);
     }
     int32_t *kept = a.e.kept + ((int64_t)b * H + h) * a.e.keep;
     if (!ok) s.left = 0;
-    for (int64_t i = (int64_t)s.left + tid; i < a.e.keep; i += kSelectThreads) kept[i] = -1;
+    for (int64_t i = (int64_t)s.left + all; i < a.e.keep; i += step) kept[i] = -1;
     if (s.left == s.len || !ok) {
-        for (int i = tid; i < s.left; i += kSelectThreads) kept[i] = i;
+        for (int i = all; i < s.left; i += step) kept[i] = i;
         return;
     }
     const int first = a.e.first, end = s.len - a.e.recent, want = a.e.keep - first - a.e.recent;
-    for (int i = tid; i < first; i += kSelectThreads) kept[i] = i;
-    for (int i = tid; i < a.e.recent; i += kSelectThreads) kept[first + want + i] = end + i;
+    for (int i = all; i < first; i += step) kept[i] = i;
+    for (int i = all; i < a.e.recent; i += step) kept[first + want + i] = end + i;
     if (want == 0) return;
     const float *w = a.e.weights + ((int64_t)(a.p.batch.slots ? a.p.batch.slots[b] : b) * H + h) * a.e.capacity;
+    // this CTA's share: tokens [lo, hi), a warp's run of it is contiguous
+    const int span = (end - first + C - 1) / C, lo = min(first + rank * span, end), hi = min(lo + span, end);
+    const int warp_span = ITEMS ? ITEMS * 32 : (span + WARPS * 32 - 1) / (WARPS * 32) * 32, warp_lo = lo + warp * warp_span;
+    uint32_t keys[KEYS];
+    if constexpr (ITEMS > 0) {
+#pragma unroll
+        for (int k = 0; k < ITEMS; ++k) {
+            const int t = warp_lo + k * 32 + lane;
+            keys[k] = t < hi ? weight_key(w[t]) : 0u;
+        }
+    }
+    // calls f(token, key, is there one) for every place of the warp's run, the lanes side by side
+    auto each = [&](auto &&f) {
+        if constexpr (ITEMS > 0) {
+#pragma unroll
+            for (int k = 0; k < ITEMS; ++k) {
+                const int t = warp_lo + k * 32 + lane;
+                f(t, keys[k], t < hi);
+            }
+        } else {
+            for (int t = warp_lo + lane; t - lane < min(warp_lo + warp_span, hi); t += 32) {
+                const bool have = t < min(warp_lo + warp_span, hi);
+                f(t, have ? weight_key(w[t]) : 0u, have);
+            }
+        }
+    };
     // ---- the threshold: the want-th largest key
+    for (int i = tid; i < 3 * kBins; i += kSelectThreads) hist[0][i] = 0;
+    __syncthreads();
     uint32_t prefix = 0u;
     int left = want;      // still to be found among the keys that begin with `prefix`
 #pragma unroll 1
     for (int round = 0; round < 3; ++round) {
         const int shift = round == 0 ? 21 : (round == 1 ? 10 : 0), bits = round == 2 ? 10 : 11;
-        for (int i = tid; i < kBins; i += kSelectThreads) hist[i] = 0;
-        __syncthreads();
-        for (int t = first + tid; t < end; t += kSelectThreads) {
-            const uint32_t key = weight_key(w[t]);
-            if (round == 0 || (key >> (shift + bits)) == prefix) atomicAdd(&hist[(key >> shift) & ((1u << bits) - 1u)], 1);
+        int *bins = hist[round];
+        each([&](int, uint32_t key, bool have) {
+            if (have && (round == 0 || (key >> (shift + bits)) == prefix)) atomicAdd(&bins[(key >> shift) & ((1u << bits) - 1u)], 1);
+        });
+        if (C > 1) cluster.sync();
+        else __syncthreads();
+        // bins from the top: thread i owns the four below kBins - 4 i
+        constexpr int OWN = kBins / kSelectThreads;
+        int n[OWN], incl = 0;
+#pragma unroll
+        for (int k = 0; k < OWN; ++k) n[k] = 0;
+        for (int r = 0; r < C; ++r) {
+            const int *other = C > 1 ? cluster.map_shared_rank(bins, r) : bins;
+            const int4 v = *reinterpret_cast<const int4 *>(other + kBins - OWN * (tid + 1));
+            n[0] += v.w; n[1] += v.z; n[2] += v.y; n[3] += v.x;
         }
-        __syncthreads();
-        // bins from the top: thread i owns bins kBins - 1 - 2 i and the one below
-        const int hi = hist[kBins - 1 - 2 * tid], lo = hist[kBins - 2 - 2 * tid];
-        int incl = hi + lo;
+        static_assert(OWN == 4, "a 16-byte read of four bins");
+#pragma unroll
+        for (int k = 0; k < OWN; ++k) incl += n[k];
+        const int own = incl;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
             const int v = __shfl_up_sync(0xffffffffu, incl, d);
@@ -91,45 +148,63 @@ __global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(const __gr
         }
         if (lane == 31) warp_sum[warp] = incl;
         __syncthreads();
-        int before = incl - hi - lo;
+        int before = incl - own;
         for (int k = 0; k < warp; ++k) before += warp_sum[k];
-        if (before < left && before + hi >= left) { found_bin = kBins - 1 - 2 * tid; found_above = before; }
-        else if (before + hi < left && before + hi + lo >= left) { found_bin = kBins - 2 - 2 * tid; found_above = before + hi; }
-        __syncthreads();
-        prefix = prefix << bits | (uint32_t)found_bin;
-        left -= found_above;
-        __syncthreads();
-    }
-    // ---- the kept tokens in order: all above the threshold, the first `left` at it
-    int above = 0, equal = 0;      // so far
-    for (int base = first; base < end; base += kSelectThreads) {
-        const int t = base + tid;
-        const uint32_t key = t < end ? weight_key(w[t]) : 0u;
-        const bool gt = t < end && key > prefix, eq = t < end && key == prefix;
-        const uint32_t gts = __ballot_sync(0xffffffffu, gt), eqs = __ballot_sync(0xffffffffu, eq);
-        if (lane == 0) warp_sum[warp] = __popc(gts) << 16 | __popc(eqs);
-        __syncthreads();
-        int g = above, e = equal;
-        for (int k = 0; k < 32; ++k) {
-            const int v = warp_sum[k];
-            if (k < warp) { g += v >> 16; e += v & 0xFFFF; }
-            above += v >> 16;
-            equal += v & 0xFFFF;
+#pragma unroll
+        for (int k = 0; k < OWN; ++k) {
+            if (before < left && before + n[k] >= left) { found[0] = kBins - 1 - OWN * tid - k; found[1] = before; }
+            before += n[k];
         }
-        const uint32_t below = (1u << lane) - 1u;
-        g += __popc(gts & below);
-        e += __popc(eqs & below);
-        if (gt || (eq && e < left)) kept[first + g + min(e, left)] = t;
         __syncthreads();
+        prefix = prefix << bits | (uint32_t)found[0];
+        left -= found[1];
     }
+    // ---- the kept tokens in order: all above the threshold, the first `left` at it.  How many of each lie before this warp's?
+    int above = 0, equal = 0;
+    each([&](int, uint32_t key, bool have) {
+        above += __popc(__ballot_sync(0xffffffffu, have && key > prefix));
+        equal += __popc(__ballot_sync(0xffffffffu, have && key == prefix));
+    });
+    if (lane == 0) warp_count[warp] = make_int2(above, equal);
+    __syncthreads();
+    int g = 0, e = 0, all_g = 0, all_e = 0;
+#pragma unroll
+    for (int k = 0; k < WARPS; ++k) {
+        const int2 v = warp_count[k];
+        if (k < warp) { g += v.x; e += v.y; }
+        all_g += v.x;
+        all_e += v.y;
+    }
+    if (C > 1) {
+        if (tid == 0) { totals[0] = all_g; totals[1] = all_e; }
+        cluster.sync();
+        for (int r = 0; r < rank; ++r) {
+            const int *other = cluster.map_shared_rank(totals, r);
+            g += other[0];
+            e += other[1];
+        }
+    }
+    const uint32_t below = (1u << lane) - 1u;
+    each([&](int t, uint32_t key, bool have) {
+        const bool gt = have && key > prefix, eq = have && key == prefix;
+        const uint32_t gts = __ballot_sync(0xffffffffu, gt), eqs = __ballot_sync(0xffffffffu, eq);
+        const int eb = e + __popc(eqs & below);
+        if (gt || (eq && eb < left)) kept[first + g + __popc(gts & below) + min(eb, left)] = t;
+        g += __popc(gts);
+        e += __popc(eqs);
+    });
+    if (C > 1) cluster.sync();      // nobody leaves while another may still read its shared memory
 }
 
 struct MoveArgs {
     PagedEvictArgs a;
     int strip;      // bytes of a ring row that a CTA moves at a time
+    int ctas;       // of a cluster: they share a unit
 };
 
-// blockIdx.x = 2 * (sequence * KV heads + KV head) + side (0 keys, 1 values), first for the pages, then again for the rings.
+// Unit 2 * (sequence * KV heads + KV head) + side (0 keys, 1 values), first for the pages, then again for the rings.
+template <int NG> struct alignas(4 * NG) Parameters { uint32_t w[NG]; };      // of a row
+
 template <int D, int NG>
 __global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(const __grid_constant__ MoveArgs args)
 {
@@ -138,16 +213,16 @@ __global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(const __grid_c
     asm volatile("griddepcontrol.launch_dependents;");
     const PagedEvictArgs &a = args.a;
     const skvq_paged_config &cfg = a.p.cfg;
-    const int H = cfg.n_kv_heads, units = 2 * H * a.p.batch.n_seqs, tid = threadIdx.x;
-    const bool pages = (int)blockIdx.x < units;
-    const int unit = pages ? blockIdx.x : blockIdx.x - units;
+    const int H = cfg.n_kv_heads, units = 2 * H * a.p.batch.n_seqs, tid = threadIdx.x, C = args.ctas, rank = blockIdx.x % C;
+    const bool pages = (int)(blockIdx.x / C) < units;
+    const int unit = pages ? blockIdx.x / C : blockIdx.x / C - units;
     const int side = unit & 1, h = (unit >> 1) % H, b = (unit >> 1) / H;
     const EvictSeq s = static_cast<const EvictSeq *>(a.e.workspace)[b];
     const int slot = s.ok ? (a.p.batch.slots ? a.p.batch.slots[b] : b) : 0, slot_out = s.ok && a.e.slots_out ? a.e.slots_out[b] : slot;
     const int gone = s.len - s.left, R = cfg.ring_tokens;
     // ring rows that stay: of a sequence that lost tokens those of the recent ones, whose numbers all shift alike
     const int t0 = cfg.window > 0 ? max(s.len - min(min(R, kMaxRingMoved), gone ? a.e.recent : R), s.ring_from) : 0;
-    if (pages && h == 0 && side == 0 && tid == 0) {
+    if (pages && h == 0 && side == 0 && rank == 0 && tid == 0) {
         a.e.lens_out[b] = s.ok ? s.left : s.len;
         if (a.e.ring_from_out) a.e.ring_from_out[b] = s.ok && cfg.window > 0 ? max(t0, 0) - gone : s.ring_from;
     }
@@ -159,44 +234,58 @@ __global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(const __grid_c
         const int32_t *from = a.p.batch.page_table + (int64_t)b * a.p.batch.max_pages;
         const int32_t *to = a.e.page_table_out ? a.e.page_table_out + (int64_t)b * a.e.max_pages_out : from;
         uint4 *codes = static_cast<uint4 *>(side ? a.p.c.v_codes : a.p.c.k_codes);
-        uint32_t *meta = static_cast<uint32_t *>(side ? a.p.c.v_meta : a.p.c.k_meta);
+        Parameters<NG> *meta = static_cast<Parameters<NG> *>(side ? a.p.c.v_meta : a.p.c.k_meta);
         const float *w = a.e.weights + ((int64_t)slot * H + h) * a.e.capacity;
         float *w_out = a.e.weights_out + ((int64_t)slot_out * H + h) * a.e.capacity;
-        const int lane = tid % LANES, row = tid / LANES;
-        for (int base = 0; base < s.left; base += PER_PASS * kUnroll) {
+        const int lane = tid % LANES, row = rank * PER_PASS * kUnroll + tid / LANES, pass = C * PER_PASS * kUnroll;
+        int next[kUnroll];      // the sources of the next pass: their numbers are read a pass ahead
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            const int i = u * PER_PASS + row;
+            next[u] = i < s.left ? kept[i] : 0;
+        }
+        for (int base = 0; base < s.left; base += pass) {
             uint4 c[kUnroll];
-            uint32_t m[kUnroll][NG];
+            Parameters<NG> m[kUnroll];
             float x[kUnroll];
-            int64_t dst[kUnroll];
+            int64_t dst[kUnroll], src[kUnroll];
 #pragma unroll
             for (int u = 0; u < kUnroll; ++u) {
-                const int i = base + u * PER_PASS + row;
-                dst[u] = -1;
-                if (i >= s.left) continue;
-                const int t = kept[i], src_page = from[t >> shift], dst_page = to[i >> shift];
-                if (src_page < 0 || src_page >= cfg.n_pages || dst_page < 0 || dst_page >= cfg.n_pages) set_status(a.p.c.status, SKVQ_STATUS_BAD_PAGE);
-                else if (src_page != dst_page || t != i) {
-                    const int64_t src = ((int64_t)src_page * H + h) * P + (t & (P - 1));
-                    dst[u] = ((int64_t)dst_page * H + h) * P + (i & (P - 1));
-                    c[u] = codes[src * LANES + lane];
-                    if (lane == 0) {
-#pragma unroll
-                        for (int g = 0; g < NG; ++g) m[u][g] = meta[src * NG + g];
+                const int i = base + u * PER_PASS + row, t = next[u];
+                dst[u] = src[u] = -1;
+                if (i < s.left) {
+                    const int src_page = from[t >> shift], dst_page = to[i >> shift];
+                    if (src_page < 0 || src_page >= cfg.n_pages || dst_page < 0 || dst_page >= cfg.n_pages) set_status(a.p.c.status, SKVQ_STATUS_BAD_PAGE);
+                    else if (src_page != dst_page || t != i) {
+                        src[u] = ((int64_t)src_page * H + h) * P + (t & (P - 1));
+                        dst[u] = ((int64_t)dst_page * H + h) * P + (i & (P - 1));
                     }
                 }
-                if (lane == 0 && side == 0) x[u] = w[t];
             }
-            __syncthreads();
 #pragma unroll
             for (int u = 0; u < kUnroll; ++u) {
                 const int i = base + u * PER_PASS + row;
-                if (i >= s.left) continue;
-                if (lane == 0 && side == 0) w_out[i] = x[u];
-                if (dst[u] < 0) continue;
-                codes[dst[u] * LANES + lane] = c[u];
-                if (lane == 0) {
+                if (src[u] >= 0) {
+                    c[u] = codes[src[u] * LANES + lane];
+                    if (lane == 0) m[u] = meta[src[u]];
+                }
+                if (side == 0 && lane == 1 && i < s.left) x[u] = w[next[u]];
+                next[u] = i + pass < s.left ? kept[i + pass] : 0;
+            }
+            // every row of the pass is in registers before one is written
+            if (C > 1) {
+                asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+                asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+            } else {
+                __syncthreads();
+            }
 #pragma unroll
-                    for (int g = 0; g < NG; ++g) meta[dst[u] * NG + g] = m[u][g];
+            for (int u = 0; u < kUnroll; ++u) {
+                const int i = base + u * PER_PASS + row;
+                if (side == 0 && lane == 1 && i < s.left) w_out[i] = x[u];
+                if (dst[u] >= 0) {
+                    codes[dst[u] * LANES + lane] = c[u];
+                    if (lane == 0) meta[dst[u]] = m[u];
                 }
             }
         }
@@ -208,7 +297,7 @@ __global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(const __grid_c
         const uint8_t *src = win + ((int64_t)slot * H + h) * R * (D * 2);
         uint8_t *dst = win + ((int64_t)slot_out * H + h) * R * (D * 2);
         uint4 *held = reinterpret_cast<uint4 *>(ring_rows);
-        for (int c0 = 0; c0 < D * 2; c0 += args.strip) {
+        for (int c0 = rank * args.strip; c0 < D * 2; c0 += C * args.strip) {
             for (int e = tid; e < rows * pieces; e += kMoveThreads)
                 held[e] = *reinterpret_cast<const uint4 *>(src + (int64_t)((first + e / pieces) % R) * (D * 2) + c0 + e % pieces * 16);
             __syncthreads();
@@ -219,15 +308,59 @@ __global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(const __grid_c
     }
 }
 
+// A launch in clusters that may start while its predecessor on the stream drains.
+template <typename Kern, typename Args>
+cudaError_t launch_clusters(Kern kern, int clusters, int ctas, int threads, size_t smem, cudaStream_t stream, const Args &args)
+{
+    cudaLaunchConfig_t lc = {};
+    lc.gridDim = dim3((unsigned)clusters * ctas);
+    lc.blockDim = dim3(threads);
+    lc.dynamicSmemBytes = smem;
+    lc.stream = stream;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = ctas;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    lc.attrs = attr;
+    lc.numAttrs = 2;
+    const cudaError_t e = cudaLaunchKernelEx(&lc, kern, args);
+    if (e == cudaSuccess) count_launch();
+    return e;
+}
+
+// A cluster's size: twice as many CTAs as long as the GPU has room for them (`room` per SM) and each keeps `least` of the `items`.
+int cluster_size(long long units, long long items, long long least, int room)
+{
+    int c = 1;
+    while (c < kMaxCluster && units * c * 2 <= (long long)room * sm_count() && items >= least * c * 2) c *= 2;
+    return c;
+}
+
+cudaError_t launch_select(const PagedEvictArgs &a, cudaStream_t stream)
+{
+    const int pairs = a.p.cfg.n_kv_heads * a.p.batch.n_seqs;
+    const long long most = a.p.batch.max_len - (long long)a.e.first - a.e.recent;      // of a middle
+    constexpr int SMALL = 8, LARGE = 32;
+    SelectArgs s{a, cluster_size(pairs, most, kSelectThreads * SMALL / 2, 4)};
+    while (s.ctas < kMaxCluster && most > (long long)s.ctas * kSelectThreads * LARGE) s.ctas *= 2;      // what fits the registers is read once
+    const long long share = (most + s.ctas - 1) / s.ctas;
+    if (share <= kSelectThreads * SMALL) return launch_clusters(evict_select_kernel<SMALL>, pairs, s.ctas, kSelectThreads, 0, stream, s);
+    if (share <= kSelectThreads * LARGE) return launch_clusters(evict_select_kernel<LARGE>, pairs, s.ctas, kSelectThreads, 0, stream, s);
+    return launch_clusters(evict_select_kernel<0>, pairs, s.ctas, kSelectThreads, 0, stream, s);
+}
+
 template <int D, int NG> cudaError_t launch_move(const PagedEvictArgs &a, cudaStream_t stream)
 {
     const skvq_paged_config &cfg = a.p.cfg;
     const int units = 2 * cfg.n_kv_heads * a.p.batch.n_seqs, rows = cfg.ring_tokens < kMaxRingMoved ? cfg.ring_tokens : kMaxRingMoved;
-    MoveArgs m{a, rows <= 1024 ? 64 : (rows <= 2048 ? 32 : 16)};
+    constexpr int PASS = kMoveThreads / (D / 32) * kUnroll;
+    MoveArgs m{a, rows <= 1024 ? 64 : (rows <= 2048 ? 32 : 16), cluster_size(units, a.max_kept, PASS / 2, 6)};
     static unsigned long long done = 0;
     const cudaError_t e = configure_smem_once(evict_move_kernel<D, NG>, kMaxRingMoved * 16, done);
     if (e != cudaSuccess) return e;
-    return launch_chained(evict_move_kernel<D, NG>, dim3(cfg.window > 0 ? 2 * units : units), kMoveThreads, cfg.window > 0 ? (size_t)rows * m.strip : 0, stream, m);
+    return launch_clusters(evict_move_kernel<D, NG>, cfg.window > 0 ? 2 * units : units, m.ctas, kMoveThreads, cfg.window > 0 ? (size_t)rows * m.strip : 0, stream, m);
 }
 
 }  // namespace
@@ -236,7 +369,7 @@ size_t paged_evict_workspace_bytes(const skvq_paged_batch &batch) { return batch
 
 cudaError_t launch_paged_evict(const PagedEvictArgs &a, cudaStream_t stream)
 {
-    const cudaError_t e = launch_chained(evict_select_kernel, dim3(a.p.cfg.n_kv_heads * a.p.batch.n_seqs), kSelectThreads, 0, stream, a);
+    const cudaError_t e = launch_select(a, stream);
     if (e != cudaSuccess) return e;
     if (a.p.cfg.head_dim == 128) return a.p.ng == 1 ? launch_move<128, 1>(a, stream) : a.p.ng == 2 ? launch_move<128, 2>(a, stream) : launch_move<128, 4>(a, stream);
     return a.p.ng == 1 ? launch_move<64, 1>(a, stream) : launch_move<64, 2>(a, stream);
