@@ -10,6 +10,7 @@
 // shortened inside its own pages.
 #include <cooperative_groups.h>
 
+#include "skvq_mma_common.cuh"
 #include "skvq_paged.cuh"
 #include "skvq_paged_split.cuh"
 
@@ -17,6 +18,7 @@ namespace skvq {
 namespace {
 
 namespace cg = cooperative_groups;
+using mmak::smem_u32;
 
 constexpr int kSelectThreads = 512;
 constexpr int kMaxCluster = 8;      // the portable size
@@ -49,6 +51,10 @@ __device__ __forceinline__ uint32_t weight_key(float w)
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
+// An increment of a word in shared memory.  `one` is 1, which the compiler must not know: increments by a constant become a loop over the
+// distinct addresses of the warp (32 pairs of 131k weights: 121 us so).
+__device__ __forceinline__ void count(uint32_t word, uint32_t one) { asm volatile("red.shared.add.u32 [%0], %1;" ::"r"(word), "r"(one) : "memory"); }
+
 struct SelectArgs {
     PagedEvictArgs a;
     int ctas;      // of a cluster: they share the middle of a (sequence, KV head)
@@ -57,7 +63,7 @@ struct SelectArgs {
 // ITEMS > 0: a CTA's share of the middle has at most kSelectThreads * ITEMS weights, which stay in registers; ITEMS = 0: any length, the weights
 // are read again for every digit and for the result.
 template <int ITEMS>
-__global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(const __grid_constant__ SelectArgs args)
+__global__ void __launch_bounds__(kSelectThreads, 2) evict_select_kernel(const __grid_constant__ SelectArgs args)
 {
     constexpr int WARPS = kSelectThreads / 32, KEYS = ITEMS ? ITEMS : 1;
     __shared__ int hist[3][kBins];
@@ -116,14 +122,15 @@ __global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(const __gr
     // ---- the threshold: the want-th largest key
     for (int i = tid; i < 3 * kBins; i += kSelectThreads) hist[0][i] = 0;
     __syncthreads();
-    uint32_t prefix = 0u;
+    uint32_t prefix = 0u, one;
+    asm volatile("mov.u32 %0, 1;" : "=r"(one));
     int left = want;      // still to be found among the keys that begin with `prefix`
 #pragma unroll 1
     for (int round = 0; round < 3; ++round) {
         const int shift = round == 0 ? 21 : (round == 1 ? 10 : 0), bits = round == 2 ? 10 : 11;
         int *bins = hist[round];
         each([&](int, uint32_t key, bool have) {
-            if (have && (round == 0 || (key >> (shift + bits)) == prefix)) atomicAdd(&bins[(key >> shift) & ((1u << bits) - 1u)], 1);
+            if (have && (round == 0 || (key >> (shift + bits)) == prefix)) count(smem_u32(bins + ((key >> shift) & ((1u << bits) - 1u))), one);
         });
         if (C > 1) cluster.sync();
         else __syncthreads();

@@ -31,7 +31,6 @@ constexpr float kSubnormal = 1.f / 16777216.f;      // 2^-24: the least fp16 sub
 constexpr float kLog2E = 1.4426950408889634f;      // applied to score - lse, which is small where it matters: their own products with it would lose 2^-24 of 20 or 30
 constexpr float kZeroScale = 1.f / 1024.f;           // brings a sum of 128 operands below 2^14 into fp16's range
 constexpr int kQueryThreads = 128;
-constexpr int kQueryTokens = kQueryThreads / 16;
 constexpr int kTileRows = 128;      // rows of a query tile
 
 // A query tile: kTileRows rows of D fp16, 64-channel halves one after the other, a half's rows 128 bytes each with 16-byte piece c of row r
@@ -563,24 +562,24 @@ __global__ void __launch_bounds__(kFewThreads, kFewCtas) weight_few_kernel(const
 }
 
 // ------------------------------------------------------------------------------------------------ many rows: prompts and chunks
-// Sixteen lanes own a row; a half-warp takes a token and walks over heads with the token's angles in registers.
+// D / 8 lanes own a row; they take a token and walk over heads with the token's angles in registers.
 template <typename T, int D>
 __global__ void __launch_bounds__(kQueryThreads) weight_queries_kernel(const __grid_constant__ WeightPlan plan)
 {
-    using R = Row<T, D>;
-    constexpr int C = R::C;
-    __shared__ __align__(16) T rows[kQueryTokens][2][D + 8];
+    using R = Row<T, 128>;      // 8 channels a lane, whatever D is
+    constexpr int C = R::C, LANES = D / C, TOKENS = kQueryThreads / LANES;
+    __shared__ __align__(16) T rows[TOKENS][2][D + 8];
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;");
     const PagedWeightArgs &a = plan.a;
     const PagedArgs &p = a.p;
-    const int unit = threadIdx.x >> 4, sub = threadIdx.x & 15, c0 = sub * C, b = blockIdx.z;
+    const int unit = threadIdx.x / LANES, sub = threadIdx.x % LANES, c0 = sub * C, b = blockIdx.z;
     WeightSeq w;
     weight_sequence(a, b, w);
     if (!w.ok || w.rows <= kFewRows) return;
     const int filled = (w.rows + kTileRows - 1) / kTileRows * kTileRows;      // zeros behind the last row: tiles are read whole
-    if ((int)blockIdx.x * kQueryTokens * w.rep >= filled) return;
-    const int i = blockIdx.x * kQueryTokens + unit, pos = w.s.len - w.m + i;
+    if ((int)blockIdx.x * TOKENS * w.rep >= filled) return;
+    const int i = blockIdx.x * TOKENS + unit, pos = w.s.len - w.m + i;
     const int h0 = blockIdx.y * plan.heads, h1 = min(h0 + plan.heads, p.cfg.n_q_heads);
     const bool have = i < w.m, turn = p.rope.table && have && pos >= 0;
     const int64_t tok = w.s.row0 + w.s.n - w.m + i;
@@ -590,56 +589,59 @@ __global__ void __launch_bounds__(kQueryThreads) weight_queries_kernel(const __g
     T *raw = rows[unit][0], *turned = rows[unit][1];
     int from[C], hk = -1;
     R next;
+    float lse_next = CUDART_INF_F;
 #pragma unroll
     for (int k = 0; k < R::WORDS; ++k) next.w[k] = 0u;
-    if (have && h0 < h1) next.load(src + (int64_t)h0 * D);
+    if (have && h0 < h1) {
+        next.load(src + (int64_t)h0 * D);
+        lse_next = a.lse[tok * p.cfg.n_q_heads + h0];
+    }
     for (int h = h0; h < h1; ++h) {
         if (h / w.rep != hk) {
             hk = h / w.rep;
 #pragma unroll
             for (int j = 0; j < C; ++j) {
-                const int c = (c0 & ~7) + channel_at((c0 + j) & 7);
+                const int c = c0 + channel_at(j);
                 from[j] = p.c.reorder_k ? p.c.reorder_k[hk * D + c] & (D - 1) : c;
             }
         }
         R row = next;
-        if (have && h + 1 < h1) next.load(src + (int64_t)(h + 1) * D);
+        const float lse = lse_next;
+        if (have && h + 1 < h1) {
+            next.load(src + (int64_t)(h + 1) * D);
+            lse_next = a.lse[tok * p.cfg.n_q_heads + h + 1];
+        }
         if (p.rope.table) {
             if (!p.rope.interleaved) {
                 row.store(raw + c0);
                 __syncwarp();
             }
-            if (turn) rotate_row<T, D>(row, c0, cs, raw, p.rope.rot_dim, p.rope.interleaved);
+            if (turn) rotate_row<T, 128>(row, c0, cs, raw, p.rope.rot_dim, p.rope.interleaved);
         }
         row.store(turned + c0);
         __syncwarp();
-        float x[C], mx = 0.f;
-        bool finite = true;
+        float x[C];
+        uint32_t mx = 0u;      // the largest magnitude's bits: those of infinities and of what is no number are larger still
 #pragma unroll
         for (int j = 0; j < C; ++j) {
             x[j] = Elem<T>::to_float(turned[from[j]]);
-            mx = fmaxf(mx, fabsf(x[j]));
-            finite = finite && fabsf(x[j]) < CUDART_INF_F;
+            mx = max(mx, __float_as_uint(x[j]) & 0x7FFFFFFFu);
         }
-        const float lse = have ? a.lse[tok * p.cfg.n_q_heads + h] : CUDART_INF_F;
-        const uint32_t odd = __ballot_sync(0xffffffffu, !finite) & (0xFFFFu << (threadIdx.x & 16));
-        const bool counts = odd == 0u && fabsf(lse) < CUDART_INF_F;
 #pragma unroll
-        for (int d = 1; d < 16; d <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
-        const float up = counts ? row_factor(mx) : 1.f;
+        for (int d = 1; d < LANES; d <<= 1) mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, d));
+        const bool counts = mx < 0x7F800000u && fabsf(lse) < CUDART_INF_F;
+        const float up = counts ? row_factor(__uint_as_float(mx)) : 1.f;
 #pragma unroll
         for (int j = 0; j < C; ++j) x[j] = counts ? x[j] * up : 0.f;
         const int r = i * w.rep + h - hk * w.rep;
         if (r >= filled) continue;
         uint8_t *tile = const_cast<uint8_t *>(query_tile(plan, w, b, hk, r / kTileRows));
         const int tr = r % kTileRows;
-        uint8_t *dst = tile + (c0 >> 6) * kTileRows * 128 + tr * 128 + (((((c0 >> 3) & 7) ^ (tr & 7)) << 4)) + (c0 & 7) * 2;
-        if constexpr (C == 8)
-            *reinterpret_cast<uint4 *>(dst) = make_uint4(packed<__half>(x[0], x[1]), packed<__half>(x[2], x[3]), packed<__half>(x[4], x[5]), packed<__half>(x[6], x[7]));
-        else *reinterpret_cast<uint2 *>(dst) = make_uint2(packed<__half>(x[0], x[1]), packed<__half>(x[2], x[3]));
+        *reinterpret_cast<uint4 *>(tile + (c0 >> 6) * kTileRows * 128 + tr * 128 + ((((c0 >> 3) & 7) ^ (tr & 7)) << 4)) =
+            make_uint4(packed<__half>(x[0], x[1]), packed<__half>(x[2], x[3]), packed<__half>(x[4], x[5]), packed<__half>(x[6], x[7]));
         if (sub == 0) {
             float *constants = reinterpret_cast<float *>(tile + kTileRows * D * 2) + (tr >> 1) * 4 + (tr & 1);
-            constants[0] = a.sm_scale / up;
+            constants[0] = a.sm_scale * __uint_as_float((254u << 23) - __float_as_uint(up));      // divided by the power of two
             constants[2] = counts ? -lse : -CUDART_INF_F;
         }
     }
@@ -675,6 +677,7 @@ template <int D> struct ManyGeo {
     static constexpr int HALF_BYTES = kBlock * 128;              // 64 channels of a tile
     static constexpr int A_COLUMNS = D;                          // of a block: high parts, low parts, two to a column
     static constexpr int A_BUFFERS = D == 128 ? 1 : 2;           // what 512 columns leave room for
+    static constexpr int POLY = D == 128 ? 2 : 2;
     static constexpr int TMEM_S = 0, TMEM_A = 256;               // columns: S 2 blocks x 128 rows
 };
 
@@ -751,18 +754,46 @@ __device__ __noinline__ void next_segment(const ManyArgs &args, const long long 
     s.valid = 1;
 }
 
+// 2^a and 2^b by multiply-adds: x = n + f with n the nearest integer, a polynomial of degree 5 for 2^f on [-1/2, 1/2] (fitted for the
+// smallest relative error with 1 as its constant term: 9.1e-08, with fp32's roundings 1.6e-07, about ex2.approx's own error), n added to the
+// exponent.  Arguments at or below -127, -infinity among them, give exactly 0: 1's bits and -127 in the exponent cancel.
+__device__ __forceinline__ void exp2_by_polynomial(uint64_t v, float &a, float &b)
+{
+    constexpr float MAGIC = 12582912.0f;      // 1.5 2^23: the sum's low bits hold the rounded integer
+    unpair(v, a, b);
+    const uint64_t x = pair(fmaxf(a, -127.0f), fmaxf(b, -127.0f));
+    const uint64_t t = pair_add(x, pair(MAGIC, MAGIC));
+    const uint64_t f = pair_fma(pair_add(t, pair(-MAGIC, -MAGIC)), pair(-1.f, -1.f), x);
+    uint64_t p = pair_fma(f, pair(0.0013264727f, 0.0013264727f), pair(0.0096715130f, 0.0096715130f));
+    p = pair_fma(f, p, pair(0.0555073358f, 0.0555073358f));
+    p = pair_fma(f, p, pair(0.2402224243f, 0.2402224243f));
+    p = pair_fma(f, p, pair(0.6931470037f, 0.6931470037f));
+    p = pair_fma(f, p, pair(1.0f, 1.0f));
+    float p0, p1, t0, t1;
+    unpair(p, p0, p1);
+    unpair(t, t0, t1);
+    a = __int_as_float(__float_as_int(p0) + (__float_as_int(t0) << 23));
+    b = __int_as_float(__float_as_int(p1) + (__float_as_int(t1) << 23));
+}
+
 // Thirty-two scores of a thread's token -> their probabilities' sum.  `constants`: {factor, factor, -lse, -lse} of two rows.  EDGE: rows
-// below `hidden` do not see the token.
-template <bool EDGE> __device__ __forceinline__ float sum_probabilities(const float (&x)[32], const float4 *constants, int hidden)
+// below `hidden` do not see the token.  POLY of every eight exponentials are computed with multiply-adds: the special-function unit, at 16
+// a clock for the SM, would alone take 2048 clocks for a tile of 128 rows and both blocks.
+template <bool EDGE, int POLY> __device__ __forceinline__ float sum_probabilities(const float (&x)[32], const float4 *constants, int hidden)
 {
     uint64_t l0 = 0ull, l1 = 0ull;
 #pragma unroll
     for (int c = 0; c < 32; c += 2) {
         const float4 k = constants[c / 2];
+        const uint64_t v = pair_mul(pair_fma(pair(x[c], x[c + 1]), pair(k.x, k.y), pair(k.z, k.w)), pair(kLog2E, kLog2E));
         float a, b;
-        unpair(pair_mul(pair_fma(pair(x[c], x[c + 1]), pair(k.x, k.y), pair(k.z, k.w)), pair(kLog2E, kLog2E)), a, b);
-        a = ex2_approx(a);
-        b = ex2_approx(b);
+        if (c % 8 < 8 - POLY) {
+            unpair(v, a, b);
+            a = ex2_approx(a);
+            b = ex2_approx(b);
+        } else {
+            exp2_by_polynomial(v, a, b);
+        }
         if (EDGE && c < hidden) a = 0.f;
         if (EDGE && c + 1 < hidden) b = 0.f;
         if (c & 2) l1 = pair_add(l1, pair(a, b));
@@ -1050,26 +1081,30 @@ __global__ void __launch_bounds__(kManyThreads, 1) weight_many_kernel(const __gr
                 const int parts = halves(step);
                 wait(s_full + 8 * blk, nq & 1);
                 tc_fence_after();
+                const int hidden = hidden_rows - step * kTileRows;      // columns below it
+                const bool edge = __any_sync(0xffffffffu, hidden > 0);
+                auto probabilities = [&](const float (&v)[32], int c) {
+                    sum += edge ? sum_probabilities<true, Geo::POLY>(v, constants + c / 2, hidden - c) : sum_probabilities<false, Geo::POLY>(v, constants + c / 2, 0);
+                };
+                // 32 columns become probabilities while the next 32 are on their way from tensor memory
+                float x[32], y[32];
+                tmem_ld32(s_addr, x);
+                tmem_wait_ld32(x);
 #pragma unroll 1
                 for (int hf = 0; hf < parts; ++hf) {
-                    float x[32], y[32];
-                    tmem_ld32(s_addr + hf * 64, x);
                     tmem_ld32(s_addr + hf * 64 + 32, y);
-                    tmem_wait_ld32(x);
+                    probabilities(x, hf * 64);
                     tmem_wait_ld32(y);
-                    if (hf == parts - 1) {      // the scores are in registers: the next product may overwrite them
+                    const bool last = hf == parts - 1;
+                    if (last) {      // the scores are in registers: the next product may overwrite them
                         tc_fence_before();
                         __syncwarp();
                         if (lane == 0) mbar_arrive(s_empty + 8 * blk);
-                    }
-                    const int hidden = hidden_rows - step * kTileRows - hf * 64;      // columns below it
-                    if (__any_sync(0xffffffffu, hidden > 0)) {
-                        sum += sum_probabilities<true>(x, constants + hf * 32, hidden);
-                        sum += sum_probabilities<true>(y, constants + hf * 32 + 16, hidden - 32);
                     } else {
-                        sum += sum_probabilities<false>(x, constants + hf * 32, 0);
-                        sum += sum_probabilities<false>(y, constants + hf * 32 + 16, 0);
+                        tmem_ld32(s_addr + hf * 64 + 64, x);
                     }
+                    probabilities(y, hf * 64 + 32);
+                    if (!last) tmem_wait_ld32(x);
                 }
                 __syncwarp();
                 if (lane == 0) mbar_arrive(q_empty + 8 * stage);
@@ -1165,7 +1200,7 @@ template <typename T, int D, int NG> cudaError_t launch_weights(const PagedWeigh
     const int64_t rows = batch.n_tokens > 0 ? most_rows(cfg, batch, a.last) : 0, rep = cfg.n_q_heads / cfg.n_kv_heads;
     cudaError_t e = rows <= kFewRowTile / 2 ? launch_few<T, D, NG, 1, 1>(p, stream) : rows <= kFewRowTile ? launch_few<T, D, NG, 1, 2>(p, stream) : launch_few<T, D, NG, 2, 2>(p, stream);
     if (e != cudaSuccess || rows <= kFewRows) return e;
-    const int64_t padded = (rows + kTileRows - 1) / kTileRows * kTileRows, chunks = ((padded + rep - 1) / rep + kQueryTokens - 1) / kQueryTokens;
+    const int64_t padded = (rows + kTileRows - 1) / kTileRows * kTileRows, per = kQueryThreads / (D / 8), chunks = ((padded + rep - 1) / rep + per - 1) / per;
     p.heads = cfg.n_q_heads;
     while (p.heads > 4 && chunks * batch.n_seqs * ((cfg.n_q_heads + p.heads - 1) / p.heads) < 32LL * sm_count()) p.heads = (p.heads + 1) / 2;
     e = launch_chained(weight_queries_kernel<T, D>, dim3((unsigned)chunks, (cfg.n_q_heads + p.heads - 1) / p.heads, batch.n_seqs), kQueryThreads, 0, stream, p);
