@@ -46,9 +46,9 @@ __device__ __forceinline__ bool evict_sequence(const PagedEvictArgs &a, int b, E
 // Larger weights have larger keys; -0 and +0 share one, and what is not a number has the smallest.
 __device__ __forceinline__ uint32_t weight_key(float w)
 {
-    if (w != w) return 0u;
     const uint32_t u = __float_as_uint(w + 0.f);
-    return u & 0x80000000u ? ~u : u | 0x80000000u;
+    const uint32_t key = u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+    return w == w ? key : 0u;
 }
 
 // An increment of a word in shared memory.  `one` is 1, which the compiler must not know: increments by a constant become a loop over the
@@ -95,14 +95,18 @@ __global__ void __launch_bounds__(kSelectThreads, 2) evict_select_kernel(const _
     const float *w = a.e.weights + ((int64_t)(a.p.batch.slots ? a.p.batch.slots[b] : b) * H + h) * a.e.capacity;
     // this CTA's share: tokens [lo, hi), a warp's run of it is contiguous
     const int span = (end - first + C - 1) / C, lo = min(first + rank * span, end), hi = min(lo + span, end);
-    const int warp_span = ITEMS ? ITEMS * 32 : (span + WARPS * 32 - 1) / (WARPS * 32) * 32, warp_lo = lo + warp * warp_span;
+    const int items = (span + kSelectThreads - 1) / kSelectThreads, warp_span = items * 32, warp_lo = min(lo + warp * warp_span, hi);
     uint32_t keys[KEYS];
     if constexpr (ITEMS > 0) {
+        float x[KEYS];      // all loads first: with the conversions between them they went one after the other, 8 us for 32
 #pragma unroll
         for (int k = 0; k < ITEMS; ++k) {
             const int t = warp_lo + k * 32 + lane;
-            keys[k] = t < hi ? weight_key(w[t]) : 0u;
+            x[k] = 0.f;
+            if (k < items && t < hi) x[k] = w[t];
         }
+#pragma unroll
+        for (int k = 0; k < ITEMS; ++k) keys[k] = weight_key(x[k]);
     }
     // calls f(token, key, is there one) for every place of the warp's run, the lanes side by side
     auto each = [&](auto &&f) {
@@ -110,7 +114,7 @@ __global__ void __launch_bounds__(kSelectThreads, 2) evict_select_kernel(const _
 #pragma unroll
             for (int k = 0; k < ITEMS; ++k) {
                 const int t = warp_lo + k * 32 + lane;
-                f(t, keys[k], t < hi);
+                if (k < items) f(t, keys[k], t < hi);
             }
         } else {
             for (int t = warp_lo + lane; t - lane < min(warp_lo + warp_span, hi); t += 32) {
@@ -139,10 +143,16 @@ __global__ void __launch_bounds__(kSelectThreads, 2) evict_select_kernel(const _
         int n[OWN], incl = 0;
 #pragma unroll
         for (int k = 0; k < OWN; ++k) n[k] = 0;
-        for (int r = 0; r < C; ++r) {
-            const int *other = C > 1 ? cluster.map_shared_rank(bins, r) : bins;
-            const int4 v = *reinterpret_cast<const int4 *>(other + kBins - OWN * (tid + 1));
-            n[0] += v.w; n[1] += v.z; n[2] += v.y; n[3] += v.x;
+        if (C > 1) {
+#pragma unroll
+            for (int r = 0; r < kMaxCluster; ++r) {      // all on their way together
+                if (r >= C) continue;
+                const int4 v = *reinterpret_cast<const int4 *>(cluster.map_shared_rank(bins, (rank + r) & (C - 1)) + kBins - OWN * (tid + 1));      // each begins with its own
+                n[0] += v.w; n[1] += v.z; n[2] += v.y; n[3] += v.x;
+            }
+        } else {
+            const int4 v = *reinterpret_cast<const int4 *>(bins + kBins - OWN * (tid + 1));
+            n[0] = v.w; n[1] = v.z; n[2] = v.y; n[3] = v.x;
         }
         static_assert(OWN == 4, "a 16-byte read of four bins");
 #pragma unroll
@@ -156,7 +166,8 @@ __global__ void __launch_bounds__(kSelectThreads, 2) evict_select_kernel(const _
         if (lane == 31) warp_sum[warp] = incl;
         __syncthreads();
         int before = incl - own;
-        for (int k = 0; k < warp; ++k) before += warp_sum[k];
+#pragma unroll
+        for (int k = 0; k < WARPS; ++k) before += k < warp ? warp_sum[k] : 0;
 #pragma unroll
         for (int k = 0; k < OWN; ++k) {
             if (before < left && before + n[k] >= left) { found[0] = kBins - 1 - OWN * tid - k; found[1] = before; }
@@ -209,21 +220,34 @@ struct MoveArgs {
     int ctas;       // of a cluster: they share a unit
 };
 
-// Unit 2 * (sequence * KV heads + KV head) + side (0 keys, 1 values), first for the pages, then again for the rings.
+// Everybody in the cluster has loaded what it stores next.  Across a cluster: `seen` is made of the loaded values, so the loads are done;
+// the arrival itself is relaxed, for a releasing one would wait for the stores of the pass before as well.
+__device__ __forceinline__ void all_loaded(int ctas, uint32_t seen)
+{
+    if (ctas > 1) {
+        asm volatile("{\n .reg .pred p;\n setp.eq.u32 p, %0, 0x5EED5EED;\n @p nanosleep.u32 0;\n}" ::"r"(seen) : "memory");
+        asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    } else {
+        __syncthreads();
+    }
+}
+
+// Units: for every (sequence, KV head) its keys, its values and its weights; then for each the rings of keys and of values.  (With the
+// weights read beside the keys, four bytes a row, the keys took twice the values' time.)
 template <int NG> struct alignas(4 * NG) Parameters { uint32_t w[NG]; };      // of a row
 
 template <int D, int NG>
-__global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(const __grid_constant__ MoveArgs args)
+__global__ void __launch_bounds__(kMoveThreads, 4) evict_move_kernel(const __grid_constant__ MoveArgs args)
 {
     extern __shared__ __align__(16) uint8_t ring_rows[];
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;");
     const PagedEvictArgs &a = args.a;
     const skvq_paged_config &cfg = a.p.cfg;
-    const int H = cfg.n_kv_heads, units = 2 * H * a.p.batch.n_seqs, tid = threadIdx.x, C = args.ctas, rank = blockIdx.x % C;
-    const bool pages = (int)(blockIdx.x / C) < units;
-    const int unit = pages ? blockIdx.x / C : blockIdx.x / C - units;
-    const int side = unit & 1, h = (unit >> 1) % H, b = (unit >> 1) / H;
+    const int H = cfg.n_kv_heads, pairs = H * a.p.batch.n_seqs, tid = threadIdx.x, C = args.ctas, rank = blockIdx.x % C, unit = blockIdx.x / C;
+    const bool pages = unit < 3 * pairs;
+    const int pair = pages ? unit / 3 : (unit - 3 * pairs) >> 1, side = pages ? unit % 3 : (unit - 3 * pairs) & 1, h = pair % H, b = pair / H;
     const EvictSeq s = static_cast<const EvictSeq *>(a.e.workspace)[b];
     const int slot = s.ok ? (a.p.batch.slots ? a.p.batch.slots[b] : b) : 0, slot_out = s.ok && a.e.slots_out ? a.e.slots_out[b] : slot;
     const int gone = s.len - s.left, R = cfg.ring_tokens;
@@ -234,64 +258,101 @@ __global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(const __grid_c
         if (a.e.ring_from_out) a.e.ring_from_out[b] = s.ok && cfg.window > 0 ? max(t0, 0) - gone : s.ring_from;
     }
     if (!s.ok) return;
-    if (pages) {
+    if (pages && s.left == 0) return;
+    const int32_t *kept = a.e.kept + ((int64_t)b * H + h) * a.e.keep;
+    if (pages && side == 2) {
+        const float *w = a.e.weights + ((int64_t)slot * H + h) * a.e.capacity;
+        float *w_out = a.e.weights_out + ((int64_t)slot_out * H + h) * a.e.capacity;
+        const int mine = rank * kMoveThreads * kUnroll + tid, pass = C * kMoveThreads * kUnroll;
+        int next[kUnroll];
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) next[u] = kept[min(mine + u * kMoveThreads, s.left - 1)];
+        for (int base = 0; base < s.left; base += pass) {
+            float x[kUnroll];
+            uint32_t seen = 0u;
+#pragma unroll
+            for (int u = 0; u < kUnroll; ++u) x[u] = w[next[u]];
+#pragma unroll
+            for (int u = 0; u < kUnroll; ++u) {
+                next[u] = kept[min(base + pass + mine + u * kMoveThreads, s.left - 1)];
+                seen |= __float_as_uint(x[u]);
+            }
+            all_loaded(C, seen);
+#pragma unroll
+            for (int u = 0; u < kUnroll; ++u) {
+                const int i = base + mine + u * kMoveThreads;
+                if (i < s.left) w_out[i] = x[u];
+            }
+        }
+    } else if (pages) {
         constexpr int LANES = D / 32, PER_PASS = kMoveThreads / LANES;      // lanes of a row, 16 bytes each
         const int P = cfg.page_tokens, shift = __ffs(P) - 1;
-        const int32_t *kept = a.e.kept + ((int64_t)b * H + h) * a.e.keep;
         const int32_t *from = a.p.batch.page_table + (int64_t)b * a.p.batch.max_pages;
         const int32_t *to = a.e.page_table_out ? a.e.page_table_out + (int64_t)b * a.e.max_pages_out : from;
         uint4 *codes = static_cast<uint4 *>(side ? a.p.c.v_codes : a.p.c.k_codes);
         Parameters<NG> *meta = static_cast<Parameters<NG> *>(side ? a.p.c.v_meta : a.p.c.k_meta);
-        const float *w = a.e.weights + ((int64_t)slot * H + h) * a.e.capacity;
-        float *w_out = a.e.weights_out + ((int64_t)slot_out * H + h) * a.e.capacity;
         const int lane = tid % LANES, row = rank * PER_PASS * kUnroll + tid / LANES, pass = C * PER_PASS * kUnroll;
-        int next[kUnroll];      // the sources of the next pass: their numbers are read a pass ahead
+        // Rows of the pool fit 32 bits: of one, keys and values take 72 bytes at least.  The pages that a row comes from and goes to are read a
+        // pass ahead, the number of the token it is two passes ahead.
+        constexpr uint32_t NONE = 0xFFFFFFFFu;
+        int token[kUnroll], next[kUnroll], src_page[kUnroll], dst_page[kUnroll];
+        uint32_t src[kUnroll], dst[kUnroll];
+        // All of these load without a condition, from places that exist: behind branches the loads would wait for one another.
+        auto numbers = [&](int base) {
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
-            const int i = u * PER_PASS + row;
-            next[u] = i < s.left ? kept[i] : 0;
-        }
+            for (int u = 0; u < kUnroll; ++u) next[u] = kept[min(base + u * PER_PASS + row, s.left - 1)];
+        };
+        auto pages_of = [&](int base) {      // of the tokens in `next`
+#pragma unroll
+            for (int u = 0; u < kUnroll; ++u) {
+                token[u] = next[u];
+                src_page[u] = from[next[u] >> shift];
+                dst_page[u] = to[min(base + u * PER_PASS + row, s.left - 1) >> shift];
+            }
+        };
+        auto places = [&](int base) {
+#pragma unroll
+            for (int u = 0; u < kUnroll; ++u) {
+                const int i = base + u * PER_PASS + row;
+                const bool pages_exist = src_page[u] >= 0 && src_page[u] < cfg.n_pages && dst_page[u] >= 0 && dst_page[u] < cfg.n_pages;
+                const bool moves = i < s.left && pages_exist && (src_page[u] != dst_page[u] || token[u] != i);
+                src[u] = moves ? ((uint32_t)src_page[u] * H + h) * P + (token[u] & (P - 1)) : NONE;
+                dst[u] = ((uint32_t)dst_page[u] * H + h) * P + (i & (P - 1));
+                if (i < s.left && !pages_exist) set_status(a.p.c.status, SKVQ_STATUS_BAD_PAGE);
+            }
+        };
+        numbers(0);
+        pages_of(0);
+        numbers(pass);
         for (int base = 0; base < s.left; base += pass) {
             uint4 c[kUnroll];
             Parameters<NG> m[kUnroll];
-            float x[kUnroll];
-            int64_t dst[kUnroll], src[kUnroll];
+            places(base);
 #pragma unroll
             for (int u = 0; u < kUnroll; ++u) {
-                const int i = base + u * PER_PASS + row, t = next[u];
-                dst[u] = src[u] = -1;
-                if (i < s.left) {
-                    const int src_page = from[t >> shift], dst_page = to[i >> shift];
-                    if (src_page < 0 || src_page >= cfg.n_pages || dst_page < 0 || dst_page >= cfg.n_pages) set_status(a.p.c.status, SKVQ_STATUS_BAD_PAGE);
-                    else if (src_page != dst_page || t != i) {
-                        src[u] = ((int64_t)src_page * H + h) * P + (t & (P - 1));
-                        dst[u] = ((int64_t)dst_page * H + h) * P + (i & (P - 1));
+                if (src[u] != NONE) {
+                    c[u] = codes[(int64_t)src[u] * LANES + lane];
+                    if (lane == 0) m[u] = meta[src[u]];
+                }
+            }
+            pages_of(base + pass);
+            numbers(base + 2 * pass);
+            uint32_t seen = 0u;
+            if (C > 1) {
+#pragma unroll
+                for (int u = 0; u < kUnroll; ++u) {
+                    if (src[u] != NONE) seen |= c[u].x | c[u].y | c[u].z | c[u].w;
+                    if (src[u] != NONE && lane == 0) {
+#pragma unroll
+                        for (int g = 0; g < NG; ++g) seen |= m[u].w[g];
                     }
                 }
             }
+            all_loaded(C, seen);
 #pragma unroll
             for (int u = 0; u < kUnroll; ++u) {
-                const int i = base + u * PER_PASS + row;
-                if (src[u] >= 0) {
-                    c[u] = codes[src[u] * LANES + lane];
-                    if (lane == 0) m[u] = meta[src[u]];
-                }
-                if (side == 0 && lane == 1 && i < s.left) x[u] = w[next[u]];
-                next[u] = i + pass < s.left ? kept[i + pass] : 0;
-            }
-            // every row of the pass is in registers before one is written
-            if (C > 1) {
-                asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-                asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-            } else {
-                __syncthreads();
-            }
-#pragma unroll
-            for (int u = 0; u < kUnroll; ++u) {
-                const int i = base + u * PER_PASS + row;
-                if (side == 0 && lane == 1 && i < s.left) w_out[i] = x[u];
-                if (dst[u] >= 0) {
-                    codes[dst[u] * LANES + lane] = c[u];
+                if (src[u] != NONE) {
+                    codes[(int64_t)dst[u] * LANES + lane] = c[u];
                     if (lane == 0) meta[dst[u]] = m[u];
                 }
             }
@@ -361,13 +422,13 @@ cudaError_t launch_select(const PagedEvictArgs &a, cudaStream_t stream)
 template <int D, int NG> cudaError_t launch_move(const PagedEvictArgs &a, cudaStream_t stream)
 {
     const skvq_paged_config &cfg = a.p.cfg;
-    const int units = 2 * cfg.n_kv_heads * a.p.batch.n_seqs, rows = cfg.ring_tokens < kMaxRingMoved ? cfg.ring_tokens : kMaxRingMoved;
+    const int pairs = cfg.n_kv_heads * a.p.batch.n_seqs, rows = cfg.ring_tokens < kMaxRingMoved ? cfg.ring_tokens : kMaxRingMoved;
     constexpr int PASS = kMoveThreads / (D / 32) * kUnroll;
-    MoveArgs m{a, rows <= 1024 ? 64 : (rows <= 2048 ? 32 : 16), cluster_size(units, a.max_kept, PASS / 2, 6)};
+    MoveArgs m{a, rows <= 1024 ? 64 : (rows <= 2048 ? 32 : 16), cluster_size(2LL * pairs, a.max_kept, PASS / 2, 6)};
     static unsigned long long done = 0;
     const cudaError_t e = configure_smem_once(evict_move_kernel<D, NG>, kMaxRingMoved * 16, done);
     if (e != cudaSuccess) return e;
-    return launch_clusters(evict_move_kernel<D, NG>, cfg.window > 0 ? 2 * units : units, m.ctas, kMoveThreads, cfg.window > 0 ? (size_t)rows * m.strip : 0, stream, m);
+    return launch_clusters(evict_move_kernel<D, NG>, (cfg.window > 0 ? 5 : 3) * pairs, m.ctas, kMoveThreads, cfg.window > 0 ? (size_t)rows * m.strip : 0, stream, m);
 }
 
 }  // namespace
