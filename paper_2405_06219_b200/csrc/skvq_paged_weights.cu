@@ -677,7 +677,6 @@ template <int D> struct ManyGeo {
     static constexpr int HALF_BYTES = kBlock * 128;              // 64 channels of a tile
     static constexpr int A_COLUMNS = D;                          // of a block: high parts, low parts, two to a column
     static constexpr int A_BUFFERS = D == 128 ? 1 : 2;           // what 512 columns leave room for
-    static constexpr int POLY = D == 128 ? 2 : 2;
     static constexpr int TMEM_S = 0, TMEM_A = 256;               // columns: S 2 blocks x 128 rows
 };
 
@@ -754,46 +753,18 @@ __device__ __noinline__ void next_segment(const ManyArgs &args, const long long 
     s.valid = 1;
 }
 
-// 2^a and 2^b by multiply-adds: x = n + f with n the nearest integer, a polynomial of degree 5 for 2^f on [-1/2, 1/2] (fitted for the
-// smallest relative error with 1 as its constant term: 9.1e-08, with fp32's roundings 1.6e-07, about ex2.approx's own error), n added to the
-// exponent.  Arguments at or below -127, -infinity among them, give exactly 0: 1's bits and -127 in the exponent cancel.
-__device__ __forceinline__ void exp2_by_polynomial(uint64_t v, float &a, float &b)
-{
-    constexpr float MAGIC = 12582912.0f;      // 1.5 2^23: the sum's low bits hold the rounded integer
-    unpair(v, a, b);
-    const uint64_t x = pair(fmaxf(a, -127.0f), fmaxf(b, -127.0f));
-    const uint64_t t = pair_add(x, pair(MAGIC, MAGIC));
-    const uint64_t f = pair_fma(pair_add(t, pair(-MAGIC, -MAGIC)), pair(-1.f, -1.f), x);
-    uint64_t p = pair_fma(f, pair(0.0013264727f, 0.0013264727f), pair(0.0096715130f, 0.0096715130f));
-    p = pair_fma(f, p, pair(0.0555073358f, 0.0555073358f));
-    p = pair_fma(f, p, pair(0.2402224243f, 0.2402224243f));
-    p = pair_fma(f, p, pair(0.6931470037f, 0.6931470037f));
-    p = pair_fma(f, p, pair(1.0f, 1.0f));
-    float p0, p1, t0, t1;
-    unpair(p, p0, p1);
-    unpair(t, t0, t1);
-    a = __int_as_float(__float_as_int(p0) + (__float_as_int(t0) << 23));
-    b = __int_as_float(__float_as_int(p1) + (__float_as_int(t1) << 23));
-}
-
 // Thirty-two scores of a thread's token -> their probabilities' sum.  `constants`: {factor, factor, -lse, -lse} of two rows.  EDGE: rows
-// below `hidden` do not see the token.  POLY of every eight exponentials are computed with multiply-adds: the special-function unit, at 16
-// a clock for the SM, would alone take 2048 clocks for a tile of 128 rows and both blocks.
-template <bool EDGE, int POLY> __device__ __forceinline__ float sum_probabilities(const float (&x)[32], const float4 *constants, int hidden)
+// below `hidden` do not see the token.
+template <bool EDGE> __device__ __forceinline__ float sum_probabilities(const float (&x)[32], const float4 *constants, int hidden)
 {
     uint64_t l0 = 0ull, l1 = 0ull;
 #pragma unroll
     for (int c = 0; c < 32; c += 2) {
         const float4 k = constants[c / 2];
-        const uint64_t v = pair_mul(pair_fma(pair(x[c], x[c + 1]), pair(k.x, k.y), pair(k.z, k.w)), pair(kLog2E, kLog2E));
         float a, b;
-        if (c % 8 < 8 - POLY) {
-            unpair(v, a, b);
-            a = ex2_approx(a);
-            b = ex2_approx(b);
-        } else {
-            exp2_by_polynomial(v, a, b);
-        }
+        unpair(pair_mul(pair_fma(pair(x[c], x[c + 1]), pair(k.x, k.y), pair(k.z, k.w)), pair(kLog2E, kLog2E)), a, b);
+        a = ex2_approx(a);
+        b = ex2_approx(b);
         if (EDGE && c < hidden) a = 0.f;
         if (EDGE && c + 1 < hidden) b = 0.f;
         if (c & 2) l1 = pair_add(l1, pair(a, b));
@@ -1081,30 +1052,26 @@ __global__ void __launch_bounds__(kManyThreads, 1) weight_many_kernel(const __gr
                 const int parts = halves(step);
                 wait(s_full + 8 * blk, nq & 1);
                 tc_fence_after();
-                const int hidden = hidden_rows - step * kTileRows;      // columns below it
-                const bool edge = __any_sync(0xffffffffu, hidden > 0);
-                auto probabilities = [&](const float (&v)[32], int c) {
-                    sum += edge ? sum_probabilities<true, Geo::POLY>(v, constants + c / 2, hidden - c) : sum_probabilities<false, Geo::POLY>(v, constants + c / 2, 0);
-                };
-                // 32 columns become probabilities while the next 32 are on their way from tensor memory
-                float x[32], y[32];
-                tmem_ld32(s_addr, x);
-                tmem_wait_ld32(x);
 #pragma unroll 1
                 for (int hf = 0; hf < parts; ++hf) {
+                    float x[32], y[32];
+                    tmem_ld32(s_addr + hf * 64, x);
                     tmem_ld32(s_addr + hf * 64 + 32, y);
-                    probabilities(x, hf * 64);
+                    tmem_wait_ld32(x);
                     tmem_wait_ld32(y);
-                    const bool last = hf == parts - 1;
-                    if (last) {      // the scores are in registers: the next product may overwrite them
+                    if (hf == parts - 1) {      // the scores are in registers: the next product may overwrite them
                         tc_fence_before();
                         __syncwarp();
                         if (lane == 0) mbar_arrive(s_empty + 8 * blk);
-                    } else {
-                        tmem_ld32(s_addr + hf * 64 + 64, x);
                     }
-                    probabilities(y, hf * 64 + 32);
-                    if (!last) tmem_wait_ld32(x);
+                    const int hidden = hidden_rows - step * kTileRows - hf * 64;      // columns below it
+                    if (__any_sync(0xffffffffu, hidden > 0)) {
+                        sum += sum_probabilities<true>(x, constants + hf * 32, hidden);
+                        sum += sum_probabilities<true>(y, constants + hf * 32 + 16, hidden - 32);
+                    } else {
+                        sum += sum_probabilities<false>(x, constants + hf * 32, 0);
+                        sum += sum_probabilities<false>(y, constants + hf * 32 + 16, 0);
+                    }
                 }
                 __syncwarp();
                 if (lane == 0) mbar_arrive(q_empty + 8 * stage);
