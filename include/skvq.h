@@ -50,7 +50,8 @@ extern "C" {
 #define SKVQ_STATUS_OVERFLOW 1    /* bit set in *status when a sequence would have exceeded max_tokens */
 #define SKVQ_STATUS_COPY_TIMEOUT 2 /* bit set when a shared-memory copy inside decode attention never completed (bounded
                                      wait ran out); the affected tokens contribute nothing to the result;
-                                     skvq_paged_attention: the affected rows are NaN */
+                                     skvq_paged_attention: the affected rows are NaN; skvq_paged_weights: the
+                                     affected weights are NaN */
 #define SKVQ_STATUS_BOUNDS 4       /* only from a library built with -DSKVQ_CHECKED (a debugging build): a kernel was about to
                                      use a row, slot or partial index outside its buffer; the access was skipped */
 
@@ -513,7 +514,8 @@ size_t skvq_paged_weights_workspace_size(const skvq_paged_config *cfg, const skv
  *   weights_out[s][h][t] = (t < L_b - n_b ? weights[s][h][t] : 0) + sum over the counted rows r of KV head h that see token t of
  *                          exp(sm_scale q'_r . K~_t - lse_r)
  * for t < L_b; entries at or beyond L_b are left alone, and a new token's old entry is not read (a slot needs no clearing).  q' and K~ are
- * those of skvq_paged_attention; here the keys are not rounded to fp16: scores carry fp32's error.  Rows: the Hq/Hkv query heads of
+ * those of skvq_paged_attention; here the keys are not rounded to fp16 (but for bf16 rows of the window below 2^-14, to 2^-25): scores
+ * carry fp32's error.  Rows: the Hq/Hkv query heads of
  * KV head h for each counted token; row i of a sequence sees tokens as attention's `causal` says.  A row whose lse is not finite, or
  * whose query is not, adds nothing.  Sums are fp32, in an order that does not change from run to run.
  *   q                dtype [T][Hq][D], token stride in elements (a multiple of 8, >= Hq*D), 16-byte aligned; not rotated when rope is
@@ -555,7 +557,7 @@ size_t skvq_paged_evict_workspace_size(const skvq_paged_config *cfg, const skvq_
  * of those between them the keep - first - recent with the largest weights: at equal weights the lower token number, -0 equal to
  * +0, a weight that is not a number below all others.  The kept rows of keys, values and weights become tokens 0 .. keep-1, in the order they
  * had (heads differ in which tokens these are), and the ring's rows of the `recent` tokens follow (8192 of them at most).  Sequences with L_b <= keep
- * stay as they are, and are copied where the destination is another.
+ * stay as they are, and are copied where the destination is another.  What lies behind the new length, rows and weights, is left as it is.
  *   batch            page_table, lens, slots, ring_from, max_len; starts (may be NULL), n_tokens and max_new are not looked at
  * A destination page is the source's page of the same place in the table, or one that no sequence of the call reads; a destination slot is
  * the sequence's own or one that no sequence of the call has.  So pages that sequences share must not be shortened in place: give

@@ -677,6 +677,7 @@ class SkvqPagedCache:
         count.  Entries at or beyond a sequence's length are left alone.  Without a workspace each call takes one of its own."""
         c, index, rotation = self.cfg, self.index, self._operands(batch, rope)
         out = weights if out is None else out
+        assert out is not None, "weights, or out"
         capacity = self._weights(out)
         assert weights is None or self._weights(weights) == capacity, "weights and out of one capacity"
         qs = self._rows(q, batch, c.n_q_heads)

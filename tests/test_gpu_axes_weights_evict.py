@@ -11,7 +11,7 @@ import shrink_reference as plain
 import test_gpu_rope_paged as base
 from paper_2405_06219_b200 import binding as B
 from paper_2405_06219_b200 import build
-from test_gpu_paged_guards import guarded
+from test_gpu_paged_guards import GuardedPaged, guarded
 
 pytestmark = pytest.mark.gpu
 F16, BF16, F32 = torch.float16, torch.bfloat16, torch.float32
@@ -449,6 +449,42 @@ def test_selection_over_long_sequences(L, keep, levels):
     for x, name in zip(rows, ("k_codes", "v_codes")):
         now = getattr(cache, name)[table[0].long()].transpose(0, 1).flatten(1, 2)[:, :keep]
         assert torch.equal(now, x.gather(1, want[..., None].expand(-1, -1, x.shape[2])))
+
+
+@pytest.mark.parametrize("kw", [dict(D=128, G=32, P=16, W=32, R=37), dict(D=64, G=64, H=3, Hq=3, P=32, W=0)])
+def test_evict_writes_nothing_beside_its_buffers(kw):
+    """Every buffer between guard regions, the workspace of the exact size; bytes behind the new lengths keep what they held."""
+    p = GuardedPaged(n_seqs=3, seed=12, max_len=320, **kw)
+    p.append([300, 10, 77])
+    c, f, guards = p.cache, p.cache.cfg, p.guards
+    lens, keep = p.lens(), 64
+    w = guarded(torch.rand(3, p.H, 301, generator=gen(4)).cuda(), guards, "weights")
+    before, codes = w.clone(), c.k_codes.clone()
+    batch = p.batch([0, 0, 0], lens)
+    kept, lens_out, first = (guarded(torch.full(s, 9, dtype=torch.int32, device="cuda"), guards, n) for n, s in (("kept", (3, p.H, keep)), ("lens out", (3,)), ("ring from", (3,))))
+    size = B.skvq_paged_evict_workspace_size(f, batch)
+    ws = guarded(torch.full((size,), 0xFF, dtype=torch.uint8, device="cuda"), guards, "workspace")
+    args = B.SkvqPagedEvictArgs(keep, 3, 32, 301, w.data_ptr(), w.data_ptr(), None, 0, None, lens_out.data_ptr(), first.data_ptr(), kept.data_ptr(), ws.data_ptr(), size)
+    B.skvq_paged_evict(f, c.struct, batch, args)
+    p.check_guards("evict")
+    assert lens_out.tolist() == [64, 10, 64] and torch.equal(w[:, :, 64:], before[:, :, 64:]) and torch.equal(w[1], before[1])
+    pt = p.page_table.long()
+    for b in (0, 2):      # rows behind the new length
+        for t in range(64, lens[b]):
+            assert torch.equal(c.k_codes[pt[b, t // p.P], :, t % p.P], codes[pt[b, t // p.P], :, t % p.P])
+    assert torch.equal(c.k_codes[pt[1]], codes[pt[1]])
+
+
+def test_a_sequence_without_evictions_moves_to_another_slot():
+    p = base.Paged(n_seqs=2, seed=14, W=16, R=24, slots=[0, 3])
+    p.append([50, 9])
+    w = torch.rand(4, 2, 60, generator=gen(8)).cuda()
+    slots_out = torch.tensor([1, 2], dtype=torch.int32, device="cuda")
+    old = w.clone()
+    kept, lens_out, ring_from = p.cache.evict(p.batch([0, 0], p.lens()), w, 64, 0, 16, slots_out=slots_out)
+    assert lens_out.tolist() == [50, 9] and ring_from.tolist() == [26, 0]
+    assert torch.equal(w[1, :, :50], old[0, :, :50]) and torch.equal(w[2, :, :9], old[3, :, :9]) and torch.equal(w[0], old[0])
+    check_rows(p, p.page_table, [1, 2], lens_out, ring_from)
 
 
 # ------------------------------------------------------------------------------------------------ together
