@@ -448,6 +448,7 @@ _DTYPES = {torch.float16: SKVQ_F16, torch.bfloat16: SKVQ_BF16, torch.float32: SK
 
 
 _HERE = contextlib.nullcontext()
+_evict_sizes: dict[int, int] = {}      # workspace bytes of an eviction by its number of sequences
 
 
 def _on(index: int):
@@ -527,7 +528,7 @@ class RopeTable:
         T, _, D = q.shape
         index, dtype = self.index, q.dtype
         assert axes.pairs == self.rot_dim // 2, "axes: one entry per pair of the rotation"
-        assert positions.dtype == torch.int32 and tuple(positions.shape) == (axes.n_axes, T) and positions.get_device() == index, "positions: int32 [n_axes, T]"
+        assert positions.dtype == torch.int32 and positions.shape == (axes.n_axes, T) and positions.get_device() == index, "positions: int32 [n_axes, T]"
         assert status is None or (status.dtype == torch.int32 and status.numel() >= 1 and status.get_device() == index), "status: int32 on the table's device"
         a = _rope_operand(q, q if q_out is None else q_out, dtype, T, D, index)
         b = None if k is None else _rope_operand(k, k if k_out is None else k_out, dtype, T, D, index)
@@ -669,6 +670,11 @@ class SkvqPagedCache:
         assert shape[0] == self.cfg.n_slots and shape[1] == self.cfg.n_kv_heads, "weights: [n_slots, Hkv, capacity]"
         return shape[2]
 
+    def _words(self, t, count) -> int:
+        """Checks an int32 tensor of the cache's device and gives its address."""
+        assert t.get_device() == self.index and t.dtype == torch.int32 and t.is_contiguous() and (count is None or t.numel() == count)
+        return t.data_ptr()
+
     def accumulate_weights(self, batch, q, lse, weights, sm_scale, out=None, causal: bool = True, rope=None, last: int = 0, workspace=None,
                            stream=None):
         """Adds to the weight of every token what this step's rows gave it: exp(score - lse) over the query heads of its KV head.
@@ -703,20 +709,30 @@ class SkvqPagedCache:
         c, index = self.cfg, self.index
         self._operands(batch)
         n, H = batch.n_seqs, c.n_kv_heads
-        capacity = self._weights(weights)
-        assert weights_out is None or self._weights(weights_out) == capacity, "weights of one capacity"
-        for t, count in ((page_table_out, None), (slots_out, n), (lens_out, n), (ring_from_out, n), (kept, n * H * keep)):
-            assert t is None or (t.get_device() == index and t.dtype == torch.int32 and t.is_contiguous() and (count is None or t.numel() == count))
-        assert page_table_out is None or (page_table_out.dim() == 2 and page_table_out.shape[0] == n), "page_table_out: [n, max_pages]"
+        capacity, w = self._weights(weights), weights.data_ptr()
+        w_out = w
+        if weights_out is not None:
+            assert self._weights(weights_out) == capacity, "weights of one capacity"
+            w_out = weights_out.data_ptr()
+        pages, max_pages = None, 0
+        if page_table_out is not None:
+            pages, max_pages = self._words(page_table_out, None), page_table_out.shape[-1]
+            assert page_table_out.shape == (n, max_pages), "page_table_out: [n, max_pages]"
         with _on(index), (_HERE if stream is None else torch.cuda.stream(stream)):
-            size = skvq_paged_evict_workspace_size(c, batch)
-            workspace = torch.empty(size // 4, dtype=torch.int32, device=self.device)
-            kept = torch.empty((n, H, keep), dtype=torch.int32, device=self.device) if kept is None else kept
-            lens_out = torch.empty(n, dtype=torch.int32, device=self.device) if lens_out is None else lens_out
-            ring_from_out = torch.empty(n, dtype=torch.int32, device=self.device) if ring_from_out is None else ring_from_out
-            args = SkvqPagedEvictArgs(keep, first, c.window if recent is None else recent, capacity, weights.data_ptr(),
-                                      (weights if weights_out is None else weights_out).data_ptr(), _dptr(page_table_out),
-                                      0 if page_table_out is None else page_table_out.shape[1], _dptr(slots_out), lens_out.data_ptr(),
-                                      ring_from_out.data_ptr(), kept.data_ptr(), workspace.data_ptr(), size)
+            size = _evict_sizes.get(n)
+            if size is None:
+                size = _evict_sizes[n] = skvq_paged_evict_workspace_size(c, batch)      # depends on the number of sequences alone
+            if kept is None:
+                kept = torch.empty((n, H, keep), dtype=torch.int32, device=self.device)
+            # one piece of memory for the workspace and the two results
+            rows = size // (4 * n) if n else 0
+            small = torch.empty((rows + 2, n), dtype=torch.int32, device=self.device)
+            if lens_out is None:
+                lens_out = small[rows]
+            if ring_from_out is None:
+                ring_from_out = small[rows + 1]
+            args = SkvqPagedEvictArgs(keep, first, c.window if recent is None else recent, capacity, w, w_out, pages, max_pages,
+                                      None if slots_out is None else self._words(slots_out, n), self._words(lens_out, n),
+                                      self._words(ring_from_out, n), self._words(kept, n * H * keep), small.data_ptr(), size)
             _check(lib().skvq_paged_evict(_ref(c), _ref(self.struct), _ref(batch), _ref(args), _raw_stream(index, stream)), "skvq_paged_evict")
         return kept, lens_out, ring_from_out

@@ -54,6 +54,20 @@ struct RopeArgs {
 };
 
 template <typename T, int V> struct alignas(sizeof(T) * V) Vec { T v[V]; };
+template <typename VecT> __device__ __forceinline__ VecT load_once(const VecT *p)
+{
+    if constexpr (sizeof(VecT) == 16) {
+        const uint4 v = __ldcs(reinterpret_cast<const uint4 *>(p));
+        return *reinterpret_cast<const VecT *>(&v);
+    } else {
+        return *p;
+    }
+}
+template <typename VecT> __device__ __forceinline__ void store_once(VecT *p, const VecT &v)
+{
+    if constexpr (sizeof(VecT) == 16) __stcs(reinterpret_cast<uint4 *>(p), *reinterpret_cast<const uint4 *>(&v));
+    else *p = v;
+}
 
 // What a thread does to its channels of its heads.  A task is V pairs of the rotated part (half layout: V channels and their V partners;
 // interleaved: 2V neighbouring channels) or 2V channels behind it.
@@ -73,8 +87,8 @@ __device__ __forceinline__ void rotate_heads(const RopeArgs &a, long long tok, i
         if (h >= a.op[0].n_heads) h -= a.op[0].n_heads;
         const T *x = static_cast<const T *>(o.x) + tok * o.xt + h * o.xh;
         T *y = static_cast<T *>(o.y) + tok * o.yt + h * o.yh;
-        VecT u = *reinterpret_cast<const VecT *>(x + c1), w;
-        if (second) w = *reinterpret_cast<const VecT *>(x + c2);
+        VecT u = load_once(reinterpret_cast<const VecT *>(x + c1)), w;
+        if (second) w = load_once(reinterpret_cast<const VecT *>(x + c2));
         if (rot) {
             if constexpr (INTERLEAVED) {
                 // channels 2j .. 2j+V-1 in u, 2j+V .. 2j+2V-1 in w
@@ -100,8 +114,8 @@ __device__ __forceinline__ void rotate_heads(const RopeArgs &a, long long tok, i
         } else if (x == y) {
             continue;
         }
-        *reinterpret_cast<VecT *>(y + c1) = u;
-        if (second) *reinterpret_cast<VecT *>(y + c2) = w;
+        store_once(reinterpret_cast<VecT *>(y + c1), u);
+        if (second) store_once(reinterpret_cast<VecT *>(y + c2), w);
     }
 }
 
