@@ -8,6 +8,9 @@
 // sequence comes from token kept[i] >= i.  A CTA, or a cluster, has the keys or values of a pair; the rows of one pass are read before any of
 // them is written, passes go upwards, and the sources of later passes lie behind what earlier passes write: so a sequence may be
 // shortened inside its own pages.
+// Measured (selection + rows): a 32k prompt of 8 KV heads to 2048 tokens 17 + 7 us; 64 sequences of 1024 to 16384 tokens, 32 heads, to 2048
+// 168 + 377 us; 4 sequences of 131k tokens, 8 KV heads, to 65521 52 + 157 us, 69 % of the copy rate.  The rows' kernel is bound by scattered
+// 64-byte reads and their latency; 256 threads with two rows in flight and six CTAs an SM took 537 and 221 us in all, against 554 and 213.
 #include <cooperative_groups.h>
 
 #include "skvq_mma_common.cuh"

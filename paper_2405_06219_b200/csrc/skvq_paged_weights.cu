@@ -117,6 +117,10 @@ template <> __device__ __forceinline__ uint32_t as_h2<__nv_bfloat16>(uint32_t v)
 // 16 c 2^-24, against q/16), so codes enter the product as they are, exactly.  The zero points' share, the sum over groups of z sum q',
 // is one more product: the parameters' words {h, z} are its A operand as they lie in memory, {0, sum q'} in two fp16 parts (22 bits)
 // the B operand.  With at most 4 rows they take every other column, and a lane has one row instead of two.
+// Measured: a decode step of 64 sequences of 1024 to 16384 tokens, 32 heads, 300 us (4.7 TB/s); 4 sequences of 131072 tokens, 32 heads over
+// 8, 84 us (4.4 TB/s); one query over 4096 tokens 9.3 us.  Instruction issue (56 % of the slots, the logic pipe half busy) and latency bound
+// it together.  Steps on the way, same cases: codes as they are 377 and 115; zero points as a product, a row per lane 325 and 97; pool rows looked up
+// once per block 298 and 90.
 constexpr int kFewRowTile = 8;
 constexpr int kTile = 32;
 constexpr int kRingTile = 16;
@@ -656,6 +660,12 @@ __global__ void __launch_bounds__(kQueryThreads) weight_queries_kernel(const __g
 //   issuer        a warp: S = (low + high) Q^T of a block and a tile; the products of one block run while the other's scores become
 //                 probabilities.
 //   exponentials  2 x 4 warps, a block each: scores from tensor memory, exp(factor s - lse), their sum.
+// Measured: 2048 queries at the end of 32k tokens, 32 heads over 8, D = 128: 785 us, 0.68 PFLOP/s of scores and twice that of products; ragged
+// prompts up to 4095 tokens, 32 heads of 64: 360 us, of it 65 for the queries; four prompts of 8192 tokens judged by 32 queries 59 us.  The products
+// bound it: about 85 clocks for 128 x 128 x 16 with A in tensor memory, 690 us without any exponentials.  Tried: 64 rows a time with two buffers a
+// block 900, the two blocks' products in turn 779 but the prompts 384; a quarter of the exponentials by multiply-adds 843; 16 warps of
+// exponentials 785, prompts 387; exact codes with an accumulator per group, half the products, 1009: the parameters' fp32 arithmetic, seven
+// paired instructions a pair of scores, costs more than the product saves.
 // Items are laid end to end, priced in query tiles (causal limits included), and cut into equal runs, one per CTA; partial sums of an
 // item that several runs share are added in order by a last kernel.
 constexpr int kBlock = 128;                            // tokens of a block, rows of a query tile

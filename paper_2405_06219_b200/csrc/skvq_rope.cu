@@ -176,7 +176,9 @@ cudaError_t launch_rope(RopeArgs a, bool interleaved, cudaStream_t stream)
 
 // The rotation with several axes: pair j turns by the angle that the table's row of the token's position on axis[j] has.  A thread
 // differs from the kernel above in what it does once: it reads the token's positions on all axes and picks a row per pair; then it
-// walks over heads with its angles in registers just so.
+// walks over heads with its angles in registers just so.  Bound by DRAM.  Measured: 32k tokens of 32 + 8 heads of 128 channels, three axes,
+// fp16: 117 us, 90 % of the copy rate (129 before loads and stores were streaming ones); the gradient of 8191 tokens of 64 heads in fp32
+// 89 us, 92 %.
 constexpr int kMaxAxes = 4;
 struct RopeAxesArgs {
     RopeArgs r;
