@@ -517,7 +517,8 @@ size_t skvq_paged_weights_workspace_size(const skvq_paged_config *cfg, const skv
  * those of skvq_paged_attention; here the keys are not rounded to fp16 (but for bf16 rows of the window below 2^-14, to 2^-25): scores
  * carry fp32's error.  Rows: the Hq/Hkv query heads of
  * KV head h for each counted token; row i of a sequence sees tokens as attention's `causal` says.  A row whose lse is not finite, or
- * whose query is not, adds nothing.  Sums are fp32, in an order that does not change from run to run.
+ * whose query is not, adds nothing.  Sums are fp32, in an order that the batch's host bounds and lengths decide and that does not change
+ * from run to run.
  *   q                dtype [T][Hq][D], token stride in elements (a multiple of 8, >= Hq*D), 16-byte aligned; not rotated when rope is
  *                    given, as for attention
  *   lse              float [T][Hq], as skvq_paged_attention wrote it

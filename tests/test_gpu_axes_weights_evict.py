@@ -309,6 +309,51 @@ def test_weights_of_a_long_context_are_attentions_own():
         assert (total / (rows * Hq // H) - 1).abs().max() <= 20 * 2.0 ** -10, total
 
 
+@pytest.mark.parametrize("n", [129, 700, 2048])
+def test_weights_of_very_many_sequences(n):
+    """Ragged batches up to the largest: every sequence as a call of its own gives it -- bit for bit where few rows are counted (a token's
+    sum does not depend on the cut), to fp32's sums where many are."""
+    H, Hq, D, P, g = 2, 4, 64, 16, torch.Generator(device="cuda").manual_seed(n)
+    cpu = gen(n)
+    lens = torch.randint(0, 90, (n,), generator=cpu)
+    lens[5], lens[n - 1], lens[7] = 900, 333, 0
+    new = torch.minimum(torch.randint(0, 4, (n,), generator=cpu), lens)
+    new[n // 2] = lens[n // 2] = 64      # one of many rows
+    new[n - 1] = 50
+    pages = -(-900 // P)
+    cache = B.SkvqPagedCache(Hq, H, D, 32, 8, P, 4096, n, F16)
+    for name in ("k_codes", "v_codes"):
+        getattr(cache, name).copy_(torch.randint(0, 256, cache.k_codes.shape, generator=g, device="cuda", dtype=torch.uint8))
+    for name in ("k_meta", "v_meta", "k_win", "v_win"):
+        getattr(cache, name).copy_(torch.rand(getattr(cache, name).shape, generator=g, device="cuda") * 0.1)
+    table = torch.randint(0, 4096, (n, pages), generator=g, device="cuda", dtype=torch.int32)
+    starts = torch.cat((torch.zeros(1, dtype=torch.int64), new.cumsum(0)))
+    T = int(starts[-1])
+    q, lse = torch.randn(T + 1, Hq, D, generator=g, device="cuda").half(), torch.full((T + 1, Hq), 3.0, device="cuda")
+    dev = lambda x: x.to(torch.int32).cuda()      # noqa: E731
+    all_lens, old = dev(lens), torch.rand(n, H, 901, generator=g, device="cuda")
+    got = torch.full_like(old, 7.0)
+    cache.accumulate_weights(cache.batch(table, all_lens, dev(starts), T, 64, 900), q, lse, old, 0.1, out=got)
+    assert int(cache.status[0]) == 0
+    for b in [0, 1, 5, 7, 31, 32, 33, 127, 128, n // 2, n - 2, n - 1]:
+        m, L = int(new[b]), int(lens[b])
+        one = torch.full_like(old, 7.0)
+        # the same bound on new tokens: it chooses how rows lie side by side, and so the order in which a token's rows are added
+        batch = cache.batch(table[b:b + 1].contiguous(), all_lens[b:b + 1], dev(torch.tensor([0, m])), max(m, 1), 64, 900, slots=dev(torch.tensor([b])))
+        cache.accumulate_weights(batch, q[starts[b]:starts[b] + max(m, 1)], lse[:max(m, 1)], old, 0.1, out=one)
+        assert (got[b, :, L:] == 7).all()
+        if m * Hq // H <= 16:
+            assert torch.equal(got[b, :, :L], one[b, :, :L]), b
+        else:
+            assert (got[b, :, :L] - one[b, :, :L]).abs().max() <= m * Hq // H * 2.0 ** -22 * float(one[b, :, :L].max()), b
+    kept, lens_out, _ = cache.evict(cache.batch(table, all_lens, dev(starts), 0, 0, 900), got.clone(), 20, 2, 8, weights_out=torch.zeros_like(got),
+                                    page_table_out=torch.arange(2 * n, device="cuda", dtype=torch.int32).view(n, 2))
+    assert torch.equal(lens_out, all_lens.clamp(max=20))
+    for b in (0, 5, 7, 128, n - 1):
+        mine = [plain.chosen(got[b, h, :int(lens[b])].tolist(), int(lens[b]), 20, 2, 8) for h in range(H)]
+        assert kept[b].tolist() == [m + [-1] * (20 - len(m)) for m in mine], b
+
+
 # ------------------------------------------------------------------------------------------------ eviction
 def shrink(ref_cache, b, kept):
     """The plain cache after the move: token i of head h is token kept[h][i]."""
@@ -473,6 +518,20 @@ def test_evict_writes_nothing_beside_its_buffers(kw):
         for t in range(64, lens[b]):
             assert torch.equal(c.k_codes[pt[b, t // p.P], :, t % p.P], codes[pt[b, t // p.P], :, t % p.P])
     assert torch.equal(c.k_codes[pt[1]], codes[pt[1]])
+
+
+def test_some_pages_in_place_others_fresh():
+    p = base.Paged(n_seqs=2, seed=15, W=16, R=16, P=16, H=3, Hq=3, spare=20, max_len=320)
+    p.append([310, 200])
+    w = torch.rand(2, 3, 320, generator=gen(9)).cuda()
+    table_out = p.page_table[:, :8].contiguous()
+    table_out[0, 1], table_out[0, 4], table_out[1, 0], table_out[1, 7] = 3, 0, 11, 7      # spare pages, that nobody reads
+    mine = [[plain.chosen(w[b, h].tolist(), L, 120, 5, 20) for h in range(3)] for b, L in enumerate(p.lens())]
+    kept, lens_out, ring_from = p.cache.evict(p.batch([0, 0], p.lens()), w, 120, 5, 20, page_table_out=table_out)
+    assert kept.tolist() == mine
+    for b in range(2):
+        shrink(p.ref, b, mine[b])
+    check_rows(p, table_out, [0, 1], lens_out, ring_from)
 
 
 def test_a_sequence_without_evictions_moves_to_another_slot():
