@@ -515,8 +515,9 @@ size_t skvq_paged_weights_workspace_size(const skvq_paged_config *cfg, const skv
  *                          exp(sm_scale q'_r . K~_t - lse_r)
  * for t < L_b; entries at or beyond L_b are left alone, and a new token's old entry is not read (a slot needs no clearing).  q' and K~ are
  * those of skvq_paged_attention; here the keys are not rounded to fp16 (but for bf16 rows of the window below 2^-14, to 2^-25): scores
- * carry fp32's error.  Rows: the Hq/Hkv query heads of
- * KV head h for each counted token; row i of a sequence sees tokens as attention's `causal` says.  A row whose lse is not finite, or
+ * are fp32 sums.  With at most 16 rows per KV head they are sum_g h (q'.c) + sum_g z (sum q'), whose parts may be larger than the score; of a
+ * code's product with an entry of q' what lies below 2^-17 of the row's largest entry is lost there (entries from 2^-7 of it on: nothing).
+ * Rows: the Hq/Hkv query heads of KV head h for each counted token; row i of a sequence sees tokens as attention's `causal` says.  A row whose lse is not finite, or
  * whose query is not, adds nothing.  Sums are fp32, in an order that the batch's host bounds and lengths decide and that does not change
  * from run to run.
  *   q                dtype [T][Hq][D], token stride in elements (a multiple of 8, >= Hq*D), 16-byte aligned; not rotated when rope is

@@ -27,7 +27,7 @@ using mmak::mma16816;
 using mmak::smem_u32;
 using namespace tc5;
 
-constexpr float kSubnormal = 1.f / 16777216.f;      // 2^-24: the least fp16 subnormal, what a code's lowest bit stands for as an operand
+constexpr float kCodeUnit = 1.f / 4194304.f;        // 2^-22: what a code's lowest bit stands for as an operand, four of fp16's least subnormals
 constexpr float kLog2E = 1.4426950408889634f;      // applied to score - lse, which is small where it matters: their own products with it would lose 2^-24 of 20 or 30
 constexpr float kZeroScale = 1.f / 1024.f;           // brings a sum of 128 operands below 2^14 into fp16's range
 constexpr int kQueryThreads = 128;
@@ -113,15 +113,17 @@ template <> __device__ __forceinline__ uint32_t as_h2<__nv_bfloat16>(uint32_t v)
 // Sequences with at most 16 rows per KV head.  What bounds it is reading the keys' codes once; every warp works for itself.
 // The (sequence, KV head) pairs are laid end to end, priced in 32-token tiles (16 tokens of the unquantized window: kRingCost), and cut into
 // equal runs, one per warp.  A warp streams its tiles through a ring of its own in shared memory; 16 tokens' codes are the A
-// operand of mma.m16n8k16, 8 rows the B operand, one accumulator per group.  A nibble under zeros is an fp16 subnormal, c 2^-24 (or
-// 16 c 2^-24, against q/16), so codes enter the product as they are, exactly.  The zero points' share, the sum over groups of z sum q',
+// operand of mma.m16n8k16, 8 rows the B operand, one accumulator per group.  A nibble between zeros is an fp16 subnormal, c 2^-22 (or
+// 16 c 2^-22, against q/16), so codes enter the product as they are, exactly.  The product's sums keep 25 bits below the largest
+// term, a subnormal counted as 2^-14, here 256 codes: moved up two bits from where a byte has them, small entries of a query then keep
+// two bits more (one query over 4096 tokens, one group of 128: 5e-7 against 64 bits instead of 2.4e-6, root mean square).  The zero points' share, the sum over groups of z sum q',
 // is one more product: the parameters' words {h, z} are its A operand as they lie in memory, {0, sum q'} in two fp16 parts (22 bits)
 // the B operand.  With at most 4 rows they take every other column, and a lane has one row instead of two.
 // Measured: a decode step of 64 sequences of 1024 to 16384 tokens, 32 heads, 300 us (4.7 TB/s); 4 sequences of 131072 tokens, 32 heads over
 // 8, 84 us (4.4 TB/s); one query over 4096 tokens 9.3 us.  Instruction issue (56 % of the slots, the logic pipe half busy) and latency bound
 // it together.  Steps on the way, same cases: codes as they are 377 and 115; zero points as a product, a row per lane 325 and 97; pool rows looked up
 // once per block 298 and 90.  Accumulators that start at minus 8 times the group's sum (codes about their middle) cost 90 us instead of 84 for
-// the long contexts and brought nothing: 1.1e-6 against 64 bits in the least exact case either way.
+// the long contexts and brought nothing (measured with codes as c 2^-24).
 constexpr int kFewRowTile = 8;
 constexpr int kTile = 32;
 constexpr int kRingTile = 16;
@@ -433,14 +435,14 @@ __global__ void __launch_bounds__(kFewThreads, kFewCtas) weight_few_kernel(const
                     for (int h2 = 0; h2 < 2; ++h2) {
                         const int st = s2 + h2;
                         constexpr int PER = Geo::SETS / NG;      // granules per group
-                        const uint32_t x = c[2 * h2], y = c[2 * h2 + 1], xs = x >> 8, ys = y >> 8;
+                        const uint32_t x = c[2 * h2] << 2, y = c[2 * h2 + 1] << 2, xs = c[2 * h2] >> 6, ys = c[2 * h2 + 1] >> 6;
 #pragma unroll
                         for (int n = 0; n < NT; ++n) {
                             float (&d)[4] = acc[n][st / PER];
-                            const uint32_t x0 = x & 0x000F000Fu, y0 = y & 0x000F000Fu, x1 = x & 0x00F000F0u, y1 = y & 0x00F000F0u;
+                            const uint32_t x0 = x & 0x003C003Cu, y0 = y & 0x003C003Cu, x1 = x & 0x03C003C0u, y1 = y & 0x03C003C0u;
                             if (st % PER == 0) mma16816_from(d, x0, y0, x1, y1, bq[n][2 * st][0], bq[n][2 * st][1], 0.f, 0.f, 0.f, 0.f);
                             else mma16816(d, x0, y0, x1, y1, bq[n][2 * st][0], bq[n][2 * st][1]);
-                            mma16816(d, xs & 0x000F000Fu, ys & 0x000F000Fu, xs & 0x00F000F0u, ys & 0x00F000F0u, bq[n][2 * st + 1][0], bq[n][2 * st + 1][1]);
+                            mma16816(d, xs & 0x003C003Cu, ys & 0x003C003Cu, xs & 0x03C003C0u, ys & 0x03C003C0u, bq[n][2 * st + 1][0], bq[n][2 * st + 1][1]);
                         }
                     }
                 }
@@ -460,7 +462,7 @@ __global__ void __launch_bounds__(kFewThreads, kFewCtas) weight_few_kernel(const
                             float x = h[0] * acc[n][0][2 * half + e];
 #pragma unroll
                             for (int k = 1; k < NG; ++k) x = fmaf(h[k], acc[n][k][2 * half + e], x);
-                            s[half][n][e] = fmaf(fmaf(x, kZeroScale / kSubnormal, zero[n][2 * half + e]), rs[n][e], nl[n][e]) * kLog2E;
+                            s[half][n][e] = fmaf(fmaf(x, kZeroScale / kCodeUnit, zero[n][2 * half + e]), rs[n][e], nl[n][e]) * kLog2E;
                         }
                 }
                 if (edge) {
