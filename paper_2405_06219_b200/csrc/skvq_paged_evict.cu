@@ -31,16 +31,17 @@ constexpr int kBins = 2048;
 
 // What the second kernel needs of the first: the caller may have lens_out = lens, ring_from_out = ring_from.
 struct alignas(16) EvictSeq {
-    int len, left, ring_from, ok;      // tokens before, after; first token of the ring before
+    int len, left, ring_from, ok;      // tokens before, after; first token of the ring before (of a skipped sequence as given)
 };
 
 __device__ __forceinline__ bool evict_sequence(const PagedEvictArgs &a, int b, EvictSeq &s)
 {
     const skvq_paged_batch &p = a.p.batch;
     s.len = p.lens[b];
-    s.ring_from = p.ring_from ? max(min(p.ring_from[b], s.len), 0) : 0;
+    s.ring_from = p.ring_from ? p.ring_from[b] : 0;
     const int from = p.slots ? p.slots[b] : b, to = a.e.slots_out ? a.e.slots_out[b] : from;
     const bool ok = s.len >= 0 && s.len <= p.max_len && from >= 0 && from < a.p.cfg.n_slots && to >= 0 && to < a.p.cfg.n_slots;
+    if (ok) s.ring_from = max(min(s.ring_from, s.len), 0);
     s.left = min(s.len, a.e.keep);
     s.ok = ok;
     return ok;
