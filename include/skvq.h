@@ -558,7 +558,7 @@ size_t skvq_paged_evict_workspace_size(const skvq_paged_config *cfg, const skvq_
  * Shorten sequences to `keep` tokens.  Of a sequence with L_b > keep every KV head keeps tokens 0 .. first-1, the last `recent` ones, and
  * of those between them the keep - first - recent with the largest weights: at equal weights the lower token number, -0 equal to
  * +0, a weight that is not a number below all others.  The kept rows of keys, values and weights become tokens 0 .. keep-1, in the order they
- * had (heads differ in which tokens these are), and the ring's rows of the `recent` tokens follow (8192 of them at most).  Sequences with L_b <= keep
+ * had (heads differ in which tokens these are), and the ring's rows of the `recent` tokens follow (8192 rows are moved at most).  Sequences with L_b <= keep
  * stay as they are, and are copied where the destination is another.  What lies behind the new length, rows and weights, is left as it is.
  *   batch            page_table, lens, slots, ring_from, max_len; starts (may be NULL), n_tokens and max_new are not looked at
  * A destination page is the source's page of the same place in the table, or one that no sequence of the call reads; a destination slot is

@@ -255,8 +255,10 @@ __global__ void __launch_bounds__(kMoveThreads, 4) evict_move_kernel(const __gri
     const EvictSeq s = static_cast<const EvictSeq *>(a.e.workspace)[b];
     const int slot = s.ok ? (a.p.batch.slots ? a.p.batch.slots[b] : b) : 0, slot_out = s.ok && a.e.slots_out ? a.e.slots_out[b] : slot;
     const int gone = s.len - s.left, R = cfg.ring_tokens;
-    // ring rows that stay: of a sequence that lost tokens those of the recent ones, whose numbers all shift alike
-    const int t0 = cfg.window > 0 ? max(s.len - min(min(R, kMaxRingMoved), gone ? a.e.recent : R), s.ring_from) : 0;
+    // ring rows that stay: of a sequence that lost tokens those of the recent ones, whose numbers all shift alike -- not at all, or by whole turns:
+    // then no row has to move
+    const bool in_place = cfg.window > 0 && slot == slot_out && gone % R == 0;
+    const int t0 = cfg.window > 0 ? max(s.len - min(in_place ? R : min(R, kMaxRingMoved), gone ? a.e.recent : R), s.ring_from) : 0;
     if (pages && h == 0 && side == 0 && rank == 0 && tid == 0) {
         a.e.lens_out[b] = s.ok ? s.left : s.len;
         if (a.e.ring_from_out) a.e.ring_from_out[b] = s.ok && cfg.window > 0 ? max(t0, 0) - gone : s.ring_from;
@@ -363,7 +365,7 @@ __global__ void __launch_bounds__(kMoveThreads, 4) evict_move_kernel(const __gri
         }
     } else {
         // the ring: token t moves from row t % R to row (t - gone) % R, all rows of a strip through shared memory
-        if (slot == slot_out && gone % R == 0) return;
+        if (in_place) return;
         const int first = max(t0, 0), rows = s.len - first, pieces = args.strip / 16;
         uint8_t *win = static_cast<uint8_t *>(side ? a.p.c.v_win : a.p.c.k_win);
         const uint8_t *src = win + ((int64_t)slot * H + h) * R * (D * 2);
