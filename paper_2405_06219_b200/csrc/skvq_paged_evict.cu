@@ -70,7 +70,7 @@ template <int ITEMS>
 __global__ void __launch_bounds__(kSelectThreads, 2) evict_select_kernel(const __grid_constant__ SelectArgs args)
 {
     constexpr int WARPS = kSelectThreads / 32, KEYS = ITEMS ? ITEMS : 1;
-    __shared__ int hist[3][kBins];
+    __shared__ __align__(16) int hist[3 * kBins];      // of the three digits; read four bins at a time
     __shared__ int warp_sum[WARPS], found[2], totals[2];
     __shared__ int2 warp_count[WARPS];
     asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -128,7 +128,7 @@ __global__ void __launch_bounds__(kSelectThreads, 2) evict_select_kernel(const _
         }
     };
     // ---- the threshold: the want-th largest key
-    for (int i = tid; i < 3 * kBins; i += kSelectThreads) hist[0][i] = 0;
+    for (int i = tid; i < 3 * kBins; i += kSelectThreads) hist[i] = 0;
     __syncthreads();
     uint32_t prefix = 0u, one;
     asm volatile("mov.u32 %0, 1;" : "=r"(one));
@@ -136,7 +136,7 @@ __global__ void __launch_bounds__(kSelectThreads, 2) evict_select_kernel(const _
 #pragma unroll 1
     for (int round = 0; round < 3; ++round) {
         const int shift = round == 0 ? 21 : (round == 1 ? 10 : 0), bits = round == 2 ? 10 : 11;
-        int *bins = hist[round];
+        int *bins = hist + round * kBins;
         each([&](int, uint32_t key, bool have) {
             if (have && (round == 0 || (key >> (shift + bits)) == prefix)) count(smem_u32(bins + ((key >> shift) & ((1u << bits) - 1u))), one);
         });
