@@ -1136,14 +1136,15 @@ int64_t most_rows(const skvq_paged_config &cfg, const skvq_paged_batch &batch, i
 {
     return (int64_t)(last && last < batch.max_new ? last : batch.max_new) * (cfg.n_q_heads / cfg.n_kv_heads);
 }
-// The layout of the query tiles: the smaller of a fixed number per sequence and one after the other.
+// The layout of the query tiles: the smaller of a fixed number per sequence and one after the other (by all new tokens: those that `last` leaves out
+// leave their tiles unused).
 int64_t query_tiles(const skvq_paged_config &cfg, const skvq_paged_batch &batch, int last, int &seq_tiles)
 {
     const int64_t rows = most_rows(cfg, batch, last), uniform = (rows + kTileRows - 1) / kTileRows * batch.n_seqs;
     const int64_t together = (int64_t)batch.n_tokens * (cfg.n_q_heads / cfg.n_kv_heads) / kTileRows + batch.n_seqs;
     seq_tiles = 0;
     if (rows <= kFewRows) return 0;
-    if (uniform <= together || (last && last < batch.max_new)) seq_tiles = (int)(uniform / batch.n_seqs);
+    if (uniform <= together) seq_tiles = (int)(uniform / batch.n_seqs);
     return seq_tiles ? uniform : together;
 }
 

@@ -1,0 +1,27 @@
+"""Accumulated weights of batches that mix a chunk with single tokens, judged by their last queries: the query tiles lie one after the other."""
+import pytest
+
+from paper_2405_06219_b200 import binding as B
+from paper_2405_06219_b200 import build
+from test_gpu_axes_weights_evict import Weighed
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _lib():
+    build.build_library()
+    B.lib()
+
+
+@pytest.mark.parametrize("kw", [dict(D=128, G=64), dict(D=64, G=32, H=1, Hq=3)])
+@pytest.mark.parametrize("last", [70, 139, 0])
+def test_ragged_batches_with_last(kw, last):
+    """The workspace of the exact size between guard regions."""
+    p = Weighed(n_seqs=20, seed=last, W=16, **kw)
+    new = [1, 140, 0, 1, 1, 2, 90, 1, 1, 1, 17, 1, 1, 1, 1, 1, 3, 1, 60, 1]
+    p.append([40, 160] + [30] * 4 + [90] * 14)
+    size = B.skvq_paged_weights_workspace_size(p.cache.cfg, p.batch(new, p.lens()), last)
+    assert size <= B.skvq_paged_weights_workspace_size(p.cache.cfg, p.batch(new, p.lens()), 0)
+    p.check(new, last=last)
+    p.check(new, last=last, causal=False)
