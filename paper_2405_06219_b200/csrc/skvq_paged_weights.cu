@@ -1151,8 +1151,11 @@ int64_t query_tiles(const skvq_paged_config &cfg, const skvq_paged_batch &batch,
 // Runs that the work is cut into: a CTA per SM, a query tile each at least.
 int many_slots(const skvq_paged_config &cfg, const skvq_paged_batch &batch, int64_t rows)
 {
-    const int64_t units = (int64_t)batch.n_seqs * cfg.n_kv_heads * ((batch.max_len + kItemTokens - 1) / kItemTokens) * ((rows + kTileRows - 1) / kTileRows);
-    return (int)(units < sm_count() ? (units < 1 ? 1 : units) : sm_count());
+    // one factor at a time: their product may have more than 64 bits
+    const int64_t factors[] = {cfg.n_kv_heads, (batch.max_len + kItemTokens - 1) / kItemTokens, (rows + kTileRows - 1) / kTileRows};
+    int64_t units = batch.n_seqs;
+    for (const int64_t f : factors) units = f && units > sm_count() / f ? sm_count() : units * f;
+    return (int)(units < 1 ? 1 : units);
 }
 
 template <typename T, int D, int NG, int NT, int E> cudaError_t launch_few(const WeightPlan &p, cudaStream_t stream)

@@ -29,3 +29,10 @@ def test_fewer_counted_tokens_need_no_more_scratch(n_seqs, n_tokens, max_new, he
         now = size(last, n_seqs, n_tokens, max_new, heads=heads, D=D)
         assert before <= now <= most, last
         before = now
+
+
+def test_bounds_at_their_limits():
+    """The number of runs is counted from the host bounds, which may be far above what a batch holds: up to 2^63 items and more."""
+    for n_seqs, heads in ((2048, (128, 128)), (2048, (65535, 65535)), (1024, (256, 256))):
+        small, large = (size(0, n_seqs, 1 << 20, 1 << 30, max_len=n, heads=heads) for n in (1 << 20, 1 << 30))
+        assert small == large > 0
