@@ -9,6 +9,8 @@
 // since a key rounded to fp16 would put an error of 2^-11 of its largest terms into the exponent.
 #include <math_constants.h>
 
+#include <algorithm>
+
 #include "skvq_mma_common.cuh"
 #include "skvq_paged.cuh"
 #include "skvq_paged_split.cuh"
@@ -1166,10 +1168,10 @@ template <typename T, int D, int NG, int NT, int E> cudaError_t launch_few(const
     static unsigned long long done = 0;
     const cudaError_t e = configure_smem_once(weight_few_kernel<T, D, NG, NT, E>, Geo::SMEM + (int)sizeof(long long) * (kMaxPagedSeqs + 1), done);
     if (e != cudaSuccess) return e;
-    // one wave of resident CTAs, no more warps than tiles
+    // one wave of resident CTAs, no more warps than tiles; one at least: it reports the sequences that are skipped
     const long long lq = batch.max_len > cfg.window ? batch.max_len - cfg.window : 0;
     const long long tiles = (lq + kTile - 1) / kTile + kRingCost * ((batch.max_len - lq + kRingTile - 1) / kRingTile);
-    const long long wave = (long long)kFewCtas * sm_count(), useful = ((long long)batch.n_seqs * cfg.n_kv_heads * tiles + kFewWarps - 1) / kFewWarps;
+    const long long wave = (long long)kFewCtas * sm_count(), useful = std::max(((long long)batch.n_seqs * cfg.n_kv_heads * tiles + kFewWarps - 1) / kFewWarps, 1LL);
     return launch_chained(weight_few_kernel<T, D, NG, NT, E>, dim3((unsigned)(useful < wave ? useful : wave)), kFewThreads,
                           Geo::SMEM + sizeof(long long) * (batch.n_seqs + 1), stream, p);
 }
@@ -1218,7 +1220,6 @@ size_t paged_weights_workspace_bytes(const skvq_paged_config &cfg, const skvq_pa
 
 cudaError_t launch_paged_weights(const PagedWeightArgs &a, cudaStream_t stream)
 {
-    if (a.p.batch.max_len == 0) return cudaSuccess;
     return a.p.cfg.dtype == SKVQ_F16 ? launch_by_shape<__half>(a, stream) : launch_by_shape<__nv_bfloat16>(a, stream);
 }
 
