@@ -273,7 +273,7 @@ int skvq_decode_attention_noalloc(const skvq_config *cfg, const skvq_cache *cach
 /* Element types of k, v, q and outputs. */
 #define SKVQ_F16 0
 #define SKVQ_BF16 1
-#define SKVQ_F32 2  /* skvq_rope_apply only */
+#define SKVQ_F32 2  /* skvq_rope_apply and skvq_rope_apply_axes only */
 
 /* How the frequencies of a rotation are stretched for contexts longer than the model was trained on. */
 #define SKVQ_ROPE_PLAIN 0  /* f_j = base^(-2j/rot_dim) */
@@ -525,7 +525,8 @@ size_t skvq_paged_weights_workspace_size(const skvq_paged_config *cfg, const skv
  *   lse              float [T][Hq], as skvq_paged_attention wrote it
  * A sequence without new tokens is copied (nothing is done when weights_out is weights).  Skipped sequences (as for
  * skvq_paged_attention; here a slot outside [0, n_slots) always skips): their entries are left alone, SKVQ_STATUS_BAD_BATCH is set.  A token behind a bad page-table
- * entry gains nothing and sets SKVQ_STATUS_BAD_PAGE.  Values need not lie in the cache (v_codes, v_meta, v_win are not read).
+ * entry gains nothing and sets SKVQ_STATUS_BAD_PAGE.  Values are not read (v_codes, v_meta and v_win must
+ * point to buffers all the same, as for every call).
  * Two sequences of a call must not share a slot.  Waits inside are bounded: one that runs out (it never should) sets
  * SKVQ_STATUS_COPY_TIMEOUT, and the weights that it concerns are NaN.
  */
