@@ -121,8 +121,8 @@ template <> __device__ __forceinline__ uint32_t as_h2<__nv_bfloat16>(uint32_t v)
 // two bits more (one query over 4096 tokens, one group of 128: 5e-7 against 64 bits instead of 2.4e-6, root mean square).  The zero points' share, the sum over groups of z sum q',
 // is one more product: the parameters' words {h, z} are its A operand as they lie in memory, {0, sum q'} in two fp16 parts (22 bits)
 // the B operand.  With at most 4 rows they take every other column, and a lane has one row instead of two.
-// Measured: a decode step of 64 sequences of 1024 to 16384 tokens, 32 heads, 300 us (4.7 TB/s); 4 sequences of 131072 tokens, 32 heads over
-// 8, 84 us (4.4 TB/s); one query over 4096 tokens 9.3 us.  Instruction issue (56 % of the slots, the logic pipe half busy) and latency bound
+// Measured: a decode step of 64 sequences of 1024 to 16384 tokens, 32 heads, 295 us (4.8 TB/s); 4 sequences of 131072 tokens, 32 heads over
+// 8, 85 us (4.3 TB/s); one query over 4096 tokens 9.3 us.  Instruction issue (60 % of the slots, the logic pipe half busy) and latency bound
 // it together.  Steps on the way, same cases: codes as they are 377 and 115; zero points as a product, a row per lane 325 and 97; pool rows looked up
 // once per block 298 and 90.  Accumulators that start at minus 8 times the group's sum (codes about their middle) cost 90 us instead of 84 for
 // the long contexts and brought nothing (measured with codes as c 2^-24).
@@ -1184,6 +1184,9 @@ template <typename T, int D, int NG> cudaError_t launch_weights(const PagedWeigh
     p.a = a;
     query_tiles(cfg, batch, a.last, p.seq_tiles);
     const int64_t rows = batch.n_tokens > 0 ? most_rows(cfg, batch, a.last) : 0, rep = cfg.n_q_heads / cfg.n_kv_heads;
+    // The variant for few rows goes by the host's bound, the most rows that a sequence may have.  Measured with a row per sequence (64 sequences of 1024
+    // to 16384 tokens, 32 heads, group 64): 294 us as at most 4 rows, 315 as 8, 419 as 16, 433 where the bound is above 16 and the kernels below follow with
+    // nothing to do; with 4 rows (4 sequences of 131072 tokens, 32 heads over 8, group 32) 87, 90, 141, 147.
     cudaError_t e = rows <= kFewRowTile / 2 ? launch_few<T, D, NG, 1, 1>(p, stream) : rows <= kFewRowTile ? launch_few<T, D, NG, 1, 2>(p, stream) : launch_few<T, D, NG, 2, 2>(p, stream);
     if (e != cudaSuccess || rows <= kFewRows) return e;
     const int64_t padded = (rows + kTileRows - 1) / kTileRows * kTileRows, per = kQueryThreads / (D / 8), chunks = ((padded + rep - 1) / rep + per - 1) / per;
