@@ -10,6 +10,7 @@
 #include <math_constants.h>
 
 #include <algorithm>
+#include <cmath>
 
 #include "skvq_mma_common.cuh"
 #include "skvq_paged.cuh"
@@ -42,6 +43,7 @@ struct WeightPlan {
     PagedWeightArgs a;
     int seq_tiles;        // > 0: sequence b's tiles begin at b * seq_tiles; 0: at starts[b] * Hq/Hkv / kTileRows + b
     int heads;            // query heads that a CTA of the first kernel walks over
+    float many_scale;     // what the kernel for many rows multiplies its scores by: sm_scale, or the fp32 number above it (ManyGeo::CUT)
 };
 __host__ __device__ constexpr int tile_bytes(int D) { return kTileRows * (D * 2 + 8); }
 
@@ -124,8 +126,8 @@ template <> __device__ __forceinline__ uint32_t as_h2<__nv_bfloat16>(uint32_t v)
 // Measured: a decode step of 64 sequences of 1024 to 16384 tokens, 32 heads, 295 us (4.8 TB/s); 4 sequences of 131072 tokens, 32 heads over
 // 8, 85 us (4.3 TB/s); one query over 4096 tokens 9.3 us.  Instruction issue (60 % of the slots, the logic pipe half busy) and latency bound
 // it together.  Steps on the way, same cases: codes as they are 377 and 115; zero points as a product, a row per lane 325 and 97; pool rows looked up
-// once per block 298 and 90.  Accumulators that start at minus 8 times the group's sum (codes about their middle) cost 90 us instead of 84 for
-// the long contexts and brought nothing (measured with codes as c 2^-24).
+// once per block 298 and 90.  Accumulators that start at minus 8 times the group's sum (codes about their middle) cost 303 and 92 us instead of 296
+// and 87 and bring these cases nothing (2.8e-8 and 2.3e-8 of all weights either way); with one group of 128 they take 9e-8 to 5e-8.
 constexpr int kFewRowTile = 8;
 constexpr int kTile = 32;
 constexpr int kRingTile = 16;
@@ -650,7 +652,7 @@ __global__ void __launch_bounds__(kQueryThreads) weight_queries_kernel(const __g
             make_uint4(packed<__half>(x[0], x[1]), packed<__half>(x[2], x[3]), packed<__half>(x[4], x[5]), packed<__half>(x[6], x[7]));
         if (sub == 0) {
             float *constants = reinterpret_cast<float *>(tile + kTileRows * D * 2) + (tr >> 1) * 4 + (tr & 1);
-            constants[0] = a.sm_scale * __uint_as_float((254u << 23) - __float_as_uint(up));      // divided by the power of two
+            constants[0] = plan.many_scale * __uint_as_float((254u << 23) - __float_as_uint(up));      // divided by the power of two
             constants[2] = counts ? -lse : -CUDART_INF_F;
         }
     }
@@ -693,6 +695,10 @@ template <int D> struct ManyGeo {
     static constexpr int A_COLUMNS = D;                          // of a block: high parts, low parts, two to a column
     static constexpr int A_BUFFERS = D == 128 ? 1 : 2;           // what 512 columns leave room for
     static constexpr int TMEM_S = 0, TMEM_A = 256;               // columns: S 2 blocks x 128 rows
+    // The tensor core cuts its sums toward zero, after each of the D / 16 products: on average a score is too small by this share of itself (measured,
+    // queries and keys with outliers, groups of 32 to 128).  Rounding the scale after adding the share to it leaves 0.3 of 2^-24 at sm_scale = 128^-1/2, and at
+    // most half of fp32's step wherever the scale lies; the chunk below is off by 4.9e-7 so against 64 bits, 1.03e-6 without, 6.4e-7 the plain form in fp32.
+    static constexpr float CUT = (D == 128 ? 1.1f : 0.8f) / 16777216.f;
 };
 
 // The items of one sequence: per KV head, 256 tokens each; query tiles that they look at.
@@ -1182,6 +1188,7 @@ template <typename T, int D, int NG> cudaError_t launch_weights(const PagedWeigh
     const skvq_paged_batch &batch = a.p.batch;
     WeightPlan p{};
     p.a = a;
+    p.many_scale = std::fma(a.sm_scale, ManyGeo<D>::CUT, a.sm_scale);
     query_tiles(cfg, batch, a.last, p.seq_tiles);
     const int64_t rows = batch.n_tokens > 0 ? most_rows(cfg, batch, a.last) : 0, rep = cfg.n_q_heads / cfg.n_kv_heads;
     // The variant for few rows goes by the host's bound, the most rows that a sequence may have.  Measured with a row per sequence (64 sequences of 1024
